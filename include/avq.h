@@ -413,6 +413,84 @@ enum { /* a small index's search in one launch, tables to ranking, is all AVQ_ST
 int avq_profile_enable(avq_index *idx, int32_t on);
 int avq_profile_read(avq_index *idx, double *ms_out, int64_t *launches_out, int32_t reset);
 
+/* ---- rows of learned vectors -------------------------------------------------
+ * The points of an index are rows that a model learned, its queries what a model
+ * makes of its input. These calls look rows up, normalise them, give the
+ * probabilities of answers under the softmax of a query's inner products with all
+ * rows, and the gradients that learning the rows needs. They need no index, hold
+ * nothing between calls and run on the current device.
+ *
+ * type: element type of every matrix of a call. Matrices are row-major; ld_*: the
+ * distance of their rows in elements, >= d (d: 1 .. 16384). Pointers need the
+ * alignment of an element; rows that start on 16 bytes are read fastest. Sums,
+ * statistics and scores are fp32, results are rounded once to their type.
+ * Ids are int32. One outside [0, n) is padding (searches return -1): it stands for a
+ * row of zeros, a probability of zero, and gets no gradient.
+ * scratch: device memory of the caller, aligned to 256 bytes, of the size that the
+ * call's *_scratch function returns (a negative status for arguments that the call
+ * would refuse), free again when the call's work on the stream is done. Nothing is
+ * allocated or synchronised, and no memory is cleared by other than kernels, so
+ * that calls can be captured into a graph. Results are the same, bit for bit, each
+ * time. Outputs must not overlap inputs, except that dx of avq_layer_norm_grad may
+ * be its grad or x, and y of avq_layer_norm its x (with the same ld). */
+enum { AVQ_F32 = 0, AVQ_BF16 = 1, AVQ_F16 = 2 };
+
+/* out[t] = scale * table[ids[t]], t < count (0 .. 2^28); table [n][d]. */
+int avq_embed(const void *table, int32_t type, int64_t n, int32_t d, int64_t ld_table, const int32_t *ids, int64_t count,
+              float scale, void *out, int64_t ld_out, void *hip_stream);
+/* Its gradient: out[i] = scale * the sum of grad[t] over the t with ids[t] == i, for
+ * all n rows (zeros where there are none), or, accumulate != 0, out[i] += that for the rows
+ * that have any (the sum is formed in fp32 and added to the row's value before rounding). The
+ * positions are sorted by id, and summed in an order that ids alone determine. */
+int64_t avq_embed_grad_scratch(int64_t n, int32_t d, int64_t count);
+int avq_embed_grad(const void *grad, int32_t type, int64_t ld_grad, const int32_t *ids, int64_t count, float scale, void *out,
+                   int64_t n, int32_t d, int64_t ld_out, int32_t accumulate, void *scratch, int64_t scratch_bytes,
+                   void *hip_stream);
+
+/* y = (x - mean) * rstd * weight + bias for every row, rstd = 1 / sqrt(variance + eps)
+ * (mean and variance over the row's d elements). weight, bias: [d] or NULL (1 and 0).
+ * mean_out, rstd_out: fp32 [rows], for the gradient, or NULL. rows: 0 .. 2^28. */
+int avq_layer_norm(const void *x, int32_t type, int64_t rows, int32_t d, int64_t ld_x, const void *weight, const void *bias,
+                   float eps, void *y, int64_t ld_y, float *mean_out, float *rstd_out, void *hip_stream);
+/* Its gradient from grad [rows][d]: dx [rows][d], dweight and dbias [d] (either may be NULL). */
+int64_t avq_layer_norm_grad_scratch(int64_t rows, int32_t d);
+int avq_layer_norm_grad(const void *grad, int32_t type, int64_t ld_grad, const void *x, int64_t ld_x, int64_t rows, int32_t d,
+                        const float *mean, const float *rstd, const void *weight, void *dx, int64_t ld_dx, void *dweight,
+                        void *dbias, void *scratch, int64_t scratch_bytes, void *hip_stream);
+
+/* The softmax over all n rows of points of s_i = scale * <q, x_i>, for every query:
+ * lse_out [nq] = log sum_i e^s_i; entropy_out [nq] (or NULL) = -sum_i p_i log p_i;
+ * logp_out [nq][m] = log p of the rows ids [nq][m] (-inf for padding; m: 0 .. 4096);
+ * alt_ids_out / alt_logp_out [nq][k] = the k rows of largest s_i and their log p,
+ * by (s descending, id ascending), k: 0 .. min(n, AVQ_MAX_SELECT). The s_i themselves
+ * are not stored. fp32 matrices are multiplied to fp32's accuracy; rows whose s_i
+ * differ by less than its rounding may be ranked either way.
+ * scale: finite, not 0. nq: 0 .. 2^19. */
+int64_t avq_log_probs_scratch(int32_t type, int64_t n, int32_t d, int32_t nq, int32_t m, int32_t k);
+int avq_log_probs(const void *points, int32_t type, int64_t n, int32_t d, int64_t ld_points, const void *queries, int32_t nq,
+                  int64_t ld_queries, float scale, const int32_t *ids, int32_t m, float *logp_out, float *lse_out,
+                  float *entropy_out, int32_t k, int32_t *alt_ids_out, float *alt_logp_out, void *scratch,
+                  int64_t scratch_bytes, void *hip_stream);
+/* Its gradient, for what the loss has as gradients of logp_out (grad_logp [nq][m]), of entropy_out
+ * (grad_entropy [nq] or NULL; entropy: its values) and of lse_out (grad_lse [nq] or NULL): with
+ *   G_ti = sum_j grad_logp_tj [ids_tj = i] - p_ti (a_t + grad_entropy_t log p_ti),
+ *   a_t = sum_j grad_logp_tj - grad_lse_t + grad_entropy_t entropy_t   (sums over ids that are no padding)
+ * dqueries_t = scale * sum_i G_ti x_i and dpoints_i = scale * sum_t G_ti q_t (accumulate != 0: added to
+ * what dpoints holds). Either may be NULL. lse: as avq_log_probs gave it for the same
+ * points, queries and scale. 16-bit types: G is rounded to the type for the products. */
+int64_t avq_log_probs_grad_scratch(int32_t type, int64_t n, int32_t d, int32_t nq, int32_t m);
+int avq_log_probs_grad(const void *points, int32_t type, int64_t n, int32_t d, int64_t ld_points, const void *queries,
+                       int32_t nq, int64_t ld_queries, float scale, const int32_t *ids, int32_t m, const float *lse,
+                       const float *entropy, const float *grad_logp, const float *grad_entropy, const float *grad_lse,
+                       void *dqueries, int64_t ld_dqueries, void *dpoints, int64_t ld_dpoints, int32_t accumulate,
+                       void *scratch, int64_t scratch_bytes, void *hip_stream);
+/* avq_log_probs of the index's own rows (those kept for exact re-scoring, fp32): the log probabilities
+ * of ids that a search returned, and of the best rows. Scratch is the index's (grown with
+ * hipMalloc on the first call of a size). AVQ_ESTATE: no database, or one without its rows. */
+int avq_index_log_probs(avq_index *idx, const float *queries, int32_t nq, float scale, const int32_t *ids, int32_t m,
+                        float *logp_out, float *lse_out, float *entropy_out, int32_t k, int32_t *alt_ids_out,
+                        float *alt_logp_out, void *hip_stream);
+
 const char *avq_last_error(void);
 const char *avq_version(void);
 

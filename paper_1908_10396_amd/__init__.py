@@ -26,6 +26,8 @@ SYMBOLS = [
     "avq_set_database", "avq_get_codes", "avq_get_leaf_assign", "avq_size", "avq_debug_lut",
     "avq_debug_adc_scores", "avq_debug_leaf_select", "avq_debug_stream_codes", "avq_debug_scan_parts", "avq_debug_unverified_queries", "avq_eta", "avq_set_tuning",
     "avq_profile_enable", "avq_profile_read", "avq_last_error", "avq_version",
+    "avq_embed", "avq_embed_grad_scratch", "avq_embed_grad", "avq_layer_norm", "avq_layer_norm_grad_scratch", "avq_layer_norm_grad",
+    "avq_log_probs_scratch", "avq_log_probs", "avq_log_probs_grad_scratch", "avq_log_probs_grad", "avq_index_log_probs",
 ]
 
 
@@ -86,6 +88,20 @@ def lib():
         L.avq_set_tuning.argtypes = [vp, C.c_char_p, i32]
         L.avq_profile_enable.argtypes = [vp, i32]
         L.avq_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_int64), i32]
+        f32 = C.c_float
+        L.avq_embed.argtypes = [vp, i32, i64, i32, i64, vp, i64, f32, vp, i64, vp]
+        L.avq_embed_grad_scratch.argtypes = [i64, i32, i64]
+        L.avq_embed_grad.argtypes = [vp, i32, i64, vp, i64, f32, vp, i64, i32, i64, i32, vp, i64, vp]
+        L.avq_layer_norm.argtypes = [vp, i32, i64, i32, i64, vp, vp, f32, vp, i64, vp, vp, vp]
+        L.avq_layer_norm_grad_scratch.argtypes = [i64, i32]
+        L.avq_layer_norm_grad.argtypes = [vp, i32, i64, vp, i64, i64, i32, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]
+        L.avq_log_probs_scratch.argtypes = [i32, i64, i32, i32, i32, i32]
+        L.avq_log_probs.argtypes = [vp, i32, i64, i32, i64, vp, i32, i64, f32, vp, i32, vp, vp, vp, i32, vp, vp, vp, i64, vp]
+        L.avq_log_probs_grad_scratch.argtypes = [i32, i64, i32, i32, i32]
+        L.avq_log_probs_grad.argtypes = [vp, i32, i64, i32, i64, vp, i32, i64, f32, vp, i32, vp, vp, vp, vp, vp, vp, i64, vp, i64, i32, vp, i64, vp]
+        L.avq_index_log_probs.argtypes = [vp, vp, i32, f32, vp, i32, vp, vp, vp, i32, vp, vp, vp]
+        for name in ("avq_embed_grad_scratch", "avq_layer_norm_grad_scratch", "avq_log_probs_scratch", "avq_log_probs_grad_scratch"):
+            getattr(L, name).restype = i64
         L.avq_last_error.restype = C.c_char_p
         L.avq_version.restype = C.c_char_p
         _lib = L
@@ -328,6 +344,11 @@ class Index:
                                      _stream_ptr(stream)))
         return ids, sc
 
+    def log_probs(self, queries, ids=None, k=0, scale=1.0, stream=None):
+        """avq_index_log_probs: `log_probs` of the index's own rows (e.g. of the ids that a search returned)."""
+        from .rows import _index_log_probs
+        return _index_log_probs(self, queries, ids, k, scale, stream)
+
     def debug_lut(self, queries, lut_mode, stream=None):
         torch = _torch()
         qp = _dev(queries, torch.float32, "queries", (None, self.d))
@@ -387,3 +408,6 @@ class Index:
         _check(lib().avq_debug_leaf_select(self._h, qp, nq, L, ids.data_ptr(), ip.data_ptr(),
                                            _stream_ptr(stream)))
         return ids, ip
+
+
+from .rows import LogProbs, embed, embed_grad, layer_norm, layer_norm_grad, log_probs, log_probs_grad  # noqa: E402,F401

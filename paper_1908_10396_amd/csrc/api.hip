@@ -72,6 +72,7 @@ struct avq_index {
     int tune_sample = 0; // 0 = batches guess the candidate scan's bounds from a sample where possible, 1 = never, 2 = from a sample scanned with lists
     int tune_prefilter_cap = 0; // candidate keys per (query, chunk) of that scan, 0 = built-in
     DevBuf block_max, lists, refined, lut_fail, fail, cand_keys, groups, kept, fail_rows, product;
+    DevBuf probs_ws; // log probabilities of the rows
     DevBuf exact_ws; // exact search: operands, norms, block maxima of a launch's queries (exact_scratch)
     // training and encoding: points by coordinate and the sums of an iteration, undecided points, tables (ScratchKeeper)
     DevBuf train_ws;
@@ -180,7 +181,7 @@ extern "C" int avq_create(const avq_config *cfg, avq_index **out)
 extern "C" void avq_destroy(avq_index *idx)
 {
     if (!idx) return;
-    DevBuf *all[] = {&idx->exact_ws, &idx->codebooks, &idx->centers, &idx->centers_t, &idx->x_own, &idx->codes_logical,
+    DevBuf *all[] = {&idx->probs_ws, &idx->exact_ws, &idx->codebooks, &idx->centers, &idx->centers_t, &idx->x_own, &idx->codes_logical,
                      &idx->codes_blocked, &idx->assign, &idx->perm, &idx->leaf_blk, &idx->lut, &idx->lut8,
                      &idx->scale, &idx->bias, &idx->partial, &idx->cand, &idx->leaf_ids, &idx->leaf_ip,
                      &idx->tmp, &idx->block_max, &idx->lists, &idx->thr, &idx->refined, &idx->lut_fail,
@@ -2031,6 +2032,21 @@ extern "C" int avq_brute_force(avq_index *idx, const float *queries, int32_t nq,
         AVQ_TRY(launch_brute_force(idx->x, idx->n, d, qs, m, k, idx->partial.as<u64>(), chunks, idx->cand.as<u64>(), ids, scores, st, need));
     }
     return AVQ_OK;
+}
+
+extern "C" int avq_index_log_probs(avq_index *idx, const float *queries, int32_t nq, float scale, const int32_t *ids, int32_t m,
+                                   float *logp_out, float *lse_out, float *entropy_out, int32_t k, int32_t *alt_ids_out,
+                                   float *alt_logp_out, void *hip_stream)
+{
+    AVQ_TRY(check_index(idx));
+    if (idx->n <= 0 || !idx->x) { set_error("avq_index_log_probs: no datapoints stored"); return AVQ_ESTATE; }
+    const int d = idx->cfg.d;
+    ProbParams p{idx->x, AVQ_F32, idx->n, d, d, queries, nq, d, scale, ids, m, logp_out, lse_out, entropy_out, k, alt_ids_out, alt_logp_out, nullptr};
+    AVQ_TRY(check_log_probs(p));
+    if (nq == 0) return AVQ_OK;
+    AVQ_TRY(idx->probs_ws.reserve(log_probs_scratch_bytes(AVQ_F32, idx->n, d, nq, m, k)));
+    p.scratch = idx->probs_ws.p;
+    return launch_log_probs(p, (hipStream_t)hip_stream);
 }
 
 // ---- stage-level inspection -------------------------------------------------------------

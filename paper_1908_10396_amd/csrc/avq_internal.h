@@ -548,4 +548,59 @@ int launch_encode(const float *x, int64_t n, int d, int M, int kc, int bits, con
 
 double eta_host(int d, double T, double norm, int mode);
 
+// ---- rows of learned vectors: embed.hip, norm.hip, probs.hip, probs_grad.hip ------------------
+// (arguments as in avq.h, checked by rows_api.hip; strides in elements; type: AVQ_F32, AVQ_BF16 or AVQ_F16)
+struct EmbedParams {
+    const void *table; int32_t type; int64_t n; int32_t d; int64_t ld_table;
+    const int32_t *ids; int64_t count; float scale;
+    void *out; int64_t ld_out;
+};
+int launch_embed(const EmbedParams &p, hipStream_t st);
+struct EmbedGradParams {
+    const void *grad; int32_t type; int64_t ld_grad;
+    const int32_t *ids; int64_t count; float scale;
+    void *out; int64_t n; int32_t d; int64_t ld_out; int32_t accumulate;
+    void *scratch;
+};
+size_t embed_grad_scratch_bytes(int64_t n, int d, int64_t count);
+int launch_embed_grad(const EmbedGradParams &p, hipStream_t st);
+
+struct NormParams {
+    const void *x; int32_t type; int64_t rows; int32_t d; int64_t ld_x;
+    const void *weight, *bias; float eps;
+    void *y; int64_t ld_y; float *mean, *rstd;
+};
+int launch_norm(const NormParams &p, hipStream_t st);
+struct NormGradParams {
+    const void *dy; int32_t type; int64_t ld_dy;
+    const void *x; int64_t ld_x, rows; int32_t d;
+    const float *mean, *rstd; const void *weight;
+    void *dx; int64_t ld_dx; void *dweight, *dbias;
+    void *scratch;
+};
+size_t norm_grad_scratch_bytes(int64_t rows, int d);
+int launch_norm_grad(const NormGradParams &p, hipStream_t st);
+
+struct ProbParams {
+    const void *points; int32_t type; int64_t n; int32_t d; int64_t ld_points;
+    const void *queries; int32_t nq; int64_t ld_queries; float scale;
+    const int32_t *ids; int32_t given; float *logp, *lse, *entropy;
+    int32_t k; int32_t *alt_ids; float *alt_logp;
+    void *scratch;
+};
+size_t log_probs_scratch_bytes(int type, int64_t n, int d, int nq, int given, int k);
+int launch_log_probs(const ProbParams &p, hipStream_t st);
+// what the arguments of log probabilities must satisfy whoever gives them (AVQ_EINVAL if not)
+int check_log_probs(const ProbParams &p);
+struct ProbGradParams {
+    const void *points; int32_t type; int64_t n; int32_t d; int64_t ld_points;
+    const void *queries; int32_t nq; int64_t ld_queries; float scale;
+    const int32_t *ids; int32_t given; const float *lse, *entropy;
+    const float *grad_logp, *grad_entropy, *grad_lse;
+    void *dqueries; int64_t ld_dqueries; void *dpoints; int64_t ld_dpoints; int32_t accumulate;
+    void *scratch;
+};
+size_t log_probs_grad_scratch_bytes(int type, int64_t n, int d, int nq, int given);
+int launch_log_probs_grad(const ProbGradParams &p, hipStream_t st);
+
 } // namespace avq

@@ -1,0 +1,406 @@
+// Rows of a table by their ids (y_t = c E[id_t]), and the gradient of the table (dE_i = c * the sum of dy_t over id_t = i).
+//
+// Both are bound by memory: the lookup reads the rows asked for and writes them, the gradient reads dy once and writes the
+// table once. The gradient sorts the positions by id (stable, so that equal ids keep their order) and sums each id's run of
+// positions in that order in fp32: no atomics on values, the same result every time. Ids outside [0, n) stand for padding:
+// rows of zeros, and nothing in the gradient.
+#include "row_types.h"
+
+namespace avq {
+
+// ---- lookup ------------------------------------------------------------------------------
+
+constexpr int kLookThreads = 256, kLookEach = 4;
+
+template <class T, int V>
+__global__ __launch_bounds__(kLookThreads) void embed_kernel(const T *__restrict__ table, int64_t n, int64_t ld_table, const int32_t *__restrict__ ids,
+                                                             int64_t count, int per_row, uint32_t magic, float scale, T *__restrict__ out, int64_t ld_out)
+{
+    // the rows' vectors as one long list: a workgroup takes 1,024 of them, four loads a thread in flight
+    const int64_t first = (int64_t)blockIdx.x * (kLookThreads * kLookEach);
+    const int64_t row0 = first / per_row;
+    const uint32_t rem0 = (uint32_t)(first - row0 * per_row);
+    Pack<T, V> v[kLookEach];
+    int64_t row[kLookEach];
+    uint32_t col[kLookEach];
+    int32_t id[kLookEach];
+#pragma unroll
+    for (int u = 0; u < kLookEach; ++u) {
+        const uint32_t at = rem0 + (uint32_t)(u * kLookThreads) + threadIdx.x;
+        const uint32_t r = magic_div(at, magic);
+        row[u] = row0 + r;
+        col[u] = at - r * (uint32_t)per_row;
+        id[u] = row[u] < count ? ids[row[u]] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kLookEach; ++u) {
+        v[u] = Pack<T, V>{};
+        if (id[u] >= 0 && (int64_t)id[u] < n) v[u] = *(const Pack<T, V> *)(table + (int64_t)id[u] * ld_table + (int64_t)col[u] * V);
+    }
+#pragma unroll
+    for (int u = 0; u < kLookEach; ++u) {
+        if (row[u] >= count) continue;
+        if (scale != 1.0f) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[u].e[e] = from_f32<T>(to_f32(v[u].e[e]) * scale);
+            if (!(id[u] >= 0 && (int64_t)id[u] < n)) v[u] = Pack<T, V>{}; // (zeros, whatever the scale)
+        }
+        *(Pack<T, V> *)(out + row[u] * ld_out + (int64_t)col[u] * V) = v[u];
+    }
+}
+
+template <class T, int V>
+static int embed_run(const EmbedParams &p, hipStream_t st)
+{
+    const int per_row = p.d / V;
+    const int64_t groups = (p.count * per_row + kLookThreads * kLookEach - 1) / (kLookThreads * kLookEach);
+    embed_kernel<T, V><<<dim3((unsigned)groups), dim3(kLookThreads), 0, st>>>((const T *)p.table, p.n, p.ld_table, p.ids, p.count, per_row, magic_of(per_row),
+                                                                             p.scale, (T *)p.out, p.ld_out);
+    AVQ_HIP(hipGetLastError());
+    return AVQ_OK;
+}
+
+template <class T>
+static int embed_typed(const EmbedParams &p, hipStream_t st)
+{
+    const int w = std::min(row_width(p.table, p.ld_table, p.d, sizeof(T)), row_width(p.out, p.ld_out, p.d, sizeof(T)));
+    if (w == 16) return embed_run<T, 16 / sizeof(T)>(p, st);
+    if (w == 8) return embed_run<T, 8 / sizeof(T)>(p, st);
+    return embed_run<T, 1>(p, st);
+}
+
+int launch_embed(const EmbedParams &p, hipStream_t st)
+{
+    if (p.count == 0) return AVQ_OK;
+    if (p.type == AVQ_F32) return embed_typed<float>(p, st);
+    return p.type == AVQ_BF16 ? embed_typed<bf16_t>(p, st) : embed_typed<f16_t>(p, st);
+}
+
+// ---- positions sorted by id ----------------------------------------------------------------
+
+// Least significant digit first, digits of up to 11 bits; ids outside [0, n) get the key n and so come last. A workgroup
+// takes kSortTile entries; a wave ranks 64 entries at a time among their equals by comparing digits bit by bit, in order,
+// so that the sort is stable.
+constexpr int kSortThreads = 256, kSortEach = 8, kSortTile = kSortThreads * kSortEach, kSortWaves = kSortThreads / 64;
+constexpr int kMaxBins = 2048;
+
+__device__ __forceinline__ uint32_t key_of(int32_t id, uint32_t n) { return (uint32_t)id < n ? (uint32_t)id : n; }
+
+// hist[digit][tile]
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t *__restrict__ ids, const uint32_t *__restrict__ keys, uint32_t count, uint32_t n,
+                                                                  int shift, int bins, uint32_t *__restrict__ hist, int tiles)
+{
+    __shared__ uint32_t h[kMaxBins];
+    for (int b = threadIdx.x; b < bins; b += kSortThreads) h[b] = 0;
+    __syncthreads();
+    const uint32_t first = blockIdx.x * (uint32_t)kSortTile;
+#pragma unroll
+    for (int u = 0; u < kSortEach; ++u) {
+        const uint32_t i = first + (uint32_t)(u * kSortThreads) + threadIdx.x;
+        if (i < count) {
+            const uint32_t key = ids ? key_of(ids[i], n) : keys[i];
+            atomicAdd(&h[(key >> shift) & (uint32_t)(bins - 1)], 1u); // (counts: no order matters)
+        }
+    }
+    __syncthreads();
+    for (int b = threadIdx.x; b < bins; b += kSortThreads) hist[(size_t)b * tiles + blockIdx.x] = h[b];
+}
+
+// Exclusive sums of `total` counters in place, by one workgroup.
+__global__ __launch_bounds__(1024) void sort_scan_kernel(uint32_t *__restrict__ hist, int total)
+{
+    __shared__ uint32_t wave_sum[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t before = 0;
+    for (int base = 0; base < total; base += 4096) {
+        const int at = base + 4 * (int)threadIdx.x;
+        uint32_t c[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = at + e < total ? hist[at + e] : 0u;
+        const uint32_t mine = c[0] + c[1] + c[2] + c[3];
+        uint32_t incl = mine;
+        for (int m = 1; m < 64; m <<= 1) {
+            const uint32_t o = (uint32_t)__shfl_up((int)incl, m, 64);
+            if (lane >= m) incl += o;
+        }
+        if (lane == 63) wave_sum[wave] = incl;
+        __syncthreads();
+        uint32_t waves_before = 0, all = 0;
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) waves_before += wave_sum[w];
+            all += wave_sum[w];
+        }
+        uint32_t run = before + waves_before + incl - mine;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (at + e < total) hist[at + e] = run;
+            run += c[e];
+        }
+        before += all;
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t *__restrict__ ids, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos,
+                                                                  uint32_t count, uint32_t n, int shift, int bits, const uint32_t *__restrict__ offsets, int tiles,
+                                                                  uint32_t *__restrict__ keys_out, uint32_t *__restrict__ pos_out)
+{
+    // a wave's 512 entries lie side by side; [wave][digit]: first its counts, then where its next entry of the digit goes
+    __shared__ uint32_t next[kSortWaves][kMaxBins];
+    const int bins = 1 << bits;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int b = threadIdx.x; b < kSortWaves * kMaxBins; b += kSortThreads) (&next[0][0])[b] = 0;
+    __syncthreads();
+    const uint32_t first = blockIdx.x * (uint32_t)kSortTile + (uint32_t)(wave * 64 * kSortEach);
+    uint32_t key[kSortEach], rank[kSortEach];
+#pragma unroll
+    for (int u = 0; u < kSortEach; ++u) {
+        const uint32_t i = first + (uint32_t)(u * 64 + lane);
+        const bool real = i < count;
+        key[u] = real ? (ids ? key_of(ids[i], n) : keys[i]) : 0u;
+        const uint32_t digit = (key[u] >> shift) & (uint32_t)(bins - 1);
+        u64 same = __ballot(real);
+        for (int b = 0; b < bits; ++b) {
+            const u64 set = __ballot((digit >> b) & 1u);
+            same &= ((digit >> b) & 1u) ? set : ~set;
+        }
+        const uint32_t below = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0u));
+        uint32_t seen = 0;
+        if (real) seen = next[wave][digit];
+        rank[u] = seen + below;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (real && below == 0) next[wave][digit] = seen + (uint32_t)__popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    for (int b = threadIdx.x; b < bins; b += kSortThreads) {
+        uint32_t run = offsets[(size_t)b * tiles + blockIdx.x];
+        for (int w = 0; w < kSortWaves; ++w) {
+            const uint32_t c = next[w][b];
+            next[w][b] = run;
+            run += c;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kSortEach; ++u) {
+        const uint32_t i = first + (uint32_t)(u * 64 + lane);
+        if (i < count) {
+            const uint32_t to = next[wave][(key[u] >> shift) & (uint32_t)(bins - 1)] + rank[u];
+            keys_out[to] = key[u];
+            pos_out[to] = pos ? pos[i] : i;
+        }
+    }
+}
+
+// ---- sums of the runs ----------------------------------------------------------------------
+
+constexpr int kRunChunk = 32; // sorted entries that one group of lanes sums
+
+template <class T, int V>
+__device__ __forceinline__ void write_row(T *__restrict__ row, uint32_t col, const float *acc, float scale, bool accumulate)
+{
+    Pack<T, V> o;
+    if (accumulate) o = *(const Pack<T, V> *)(row + (size_t)col * V);
+#pragma unroll
+    for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(accumulate ? to_f32(o.e[e]) + acc[e] * scale : acc[e] * scale);
+    *(Pack<T, V> *)(row + (size_t)col * V) = o;
+}
+
+// Each group of `lanes` threads takes a chunk of kRunChunk sorted entries. A run that lies within the chunk goes to its
+// row; what belongs to a run that crosses the chunk's start or end goes to partial[chunk][0] or [1] (a run through the
+// whole chunk: [0]).
+template <class T, int V>
+__global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ grad, int64_t ld_grad, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos,
+                                                       uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out, int64_t ld_out, int accumulate,
+                                                       float *__restrict__ partial)
+{
+    const uint32_t chunk = blockIdx.x * (256u / (uint32_t)lanes) + threadIdx.x / (uint32_t)lanes;
+    const uint32_t begin = chunk * (uint32_t)kRunChunk;
+    if (begin >= count) return;
+    const uint32_t end = min(count, begin + (uint32_t)kRunChunk);
+    const uint32_t per_row = (uint32_t)d / V;
+    const uint32_t before = begin > 0 ? keys[begin - 1] : 0xffffffffu; // (no key is that)
+    const uint32_t after = end < count ? keys[end] : 0xffffffffu;
+    for (uint32_t col = threadIdx.x % (uint32_t)lanes; col < per_row; col += (uint32_t)lanes) {
+        float acc[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+        uint32_t key = keys[begin];
+        bool from_start = true;
+        constexpr int kAhead = 8;
+        for (uint32_t i0 = begin; i0 < end; i0 += kAhead) {
+            Pack<T, V> v[kAhead];
+            uint32_t k[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const uint32_t i = min(i0 + (uint32_t)u, end - 1);
+                k[u] = keys[i];
+                v[u] = Pack<T, V>{};
+                if (k[u] < n) v[u] = *(const Pack<T, V> *)(grad + (int64_t)pos[i] * ld_grad + (int64_t)col * V);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (i0 + (uint32_t)u >= end) break;
+                if (k[u] != key) {
+                    if (key < n) {
+                        if (from_start && key == before) {
+#pragma unroll
+                            for (int e = 0; e < V; ++e) partial[((size_t)chunk * 2) * d + (size_t)col * V + e] = acc[e];
+                        } else {
+                            write_row<T, V>(out + (int64_t)key * ld_out, col, acc, scale, accumulate != 0);
+                        }
+                    }
+                    from_start = false;
+                    key = k[u];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] += to_f32(v[u].e[e]);
+            }
+        }
+        if (key >= n) continue;
+        const bool open_start = from_start && key == before;
+        if (open_start || key == after) {
+            const size_t slot = (size_t)chunk * 2 + (open_start ? 0 : 1);
+#pragma unroll
+            for (int e = 0; e < V; ++e) partial[slot * d + (size_t)col * V + e] = acc[e];
+        } else {
+            write_row<T, V>(out + (int64_t)key * ld_out, col, acc, scale, accumulate != 0);
+        }
+    }
+}
+
+// The runs that cross chunks: the group whose chunk such a run begins in adds up its parts in order.
+template <class T, int V>
+__global__ __launch_bounds__(256) void run_joins_kernel(const uint32_t *__restrict__ keys, uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out,
+                                                        int64_t ld_out, int accumulate, const float *__restrict__ partial)
+{
+    const uint32_t chunk = blockIdx.x * (256u / (uint32_t)lanes) + threadIdx.x / (uint32_t)lanes;
+    const uint32_t begin = chunk * (uint32_t)kRunChunk, end = begin + (uint32_t)kRunChunk;
+    if (end >= count) return; // the last chunk's runs end in it
+    const uint32_t key = keys[end - 1];
+    if (key >= n || keys[end] != key) return;
+    if (keys[begin] == key && begin > 0 && keys[begin - 1] == key) return; // it began earlier
+    // the chunks that the run goes on in: those whose first entry has the key
+    uint32_t lo = chunk + 1, hi = (count + kRunChunk - 1) / kRunChunk; // first chunk of another key lies in (lo, hi]
+    while (lo + 1 < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (keys[mid * (uint32_t)kRunChunk] == key) lo = mid; else hi = mid;
+    }
+    const uint32_t last = lo;
+    const uint32_t per_row = (uint32_t)d / V;
+    for (uint32_t col = threadIdx.x % (uint32_t)lanes; col < per_row; col += (uint32_t)lanes) {
+        float acc[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = partial[((size_t)chunk * 2 + 1) * d + (size_t)col * V + e];
+#pragma unroll 8
+        for (uint32_t c = chunk + 1; c <= last; ++c) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] += partial[(size_t)c * 2 * d + (size_t)col * V + e];
+        }
+        write_row<T, V>(out + (int64_t)key * ld_out, col, acc, scale, accumulate != 0);
+    }
+}
+
+template <class T, int V>
+__global__ __launch_bounds__(256) void fill_rows_kernel(T *__restrict__ out, int64_t rows, int64_t ld, int per_row)
+{
+    // (dense rows are one long row)
+    const int64_t step = (int64_t)gridDim.x * 256;
+    if (ld == (int64_t)per_row * V) {
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * per_row; i += step) *(Pack<T, V> *)(out + i * V) = Pack<T, V>{};
+    } else {
+        for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+            for (int c = threadIdx.x; c < per_row; c += 256) *(Pack<T, V> *)(out + r * ld + (int64_t)c * V) = Pack<T, V>{};
+    }
+}
+
+struct GradScratch {
+    uint32_t *keys[2], *pos[2], *hist;
+    float *partial;
+    size_t bytes;
+    int passes, bits, tiles;
+};
+
+static GradScratch grad_scratch(int64_t n, int d, int64_t count, void *base)
+{
+    GradScratch s{};
+    int need = 1;
+    while (((uint64_t)1 << need) <= (uint64_t)n) ++need; // keys are 0 .. n
+    s.passes = (need + 10) / 11;
+    s.bits = (need + s.passes - 1) / s.passes;
+    s.tiles = (int)((count + kSortTile - 1) / kSortTile);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        void *p = base ? (char *)base + at : nullptr;
+        at += (bytes + 255) & ~(size_t)255;
+        return p;
+    };
+    for (int i = 0; i < 2; ++i) {
+        s.keys[i] = (uint32_t *)take(4 * (size_t)count);
+        s.pos[i] = (uint32_t *)take(4 * (size_t)count);
+    }
+    s.hist = (uint32_t *)take(((size_t)4 << s.bits) * s.tiles);
+    s.partial = (float *)take((size_t)((count + kRunChunk - 1) / kRunChunk) * 2 * d * sizeof(float));
+    s.bytes = at;
+    return s;
+}
+
+size_t embed_grad_scratch_bytes(int64_t n, int d, int64_t count) { return grad_scratch(n, d, count, nullptr).bytes; }
+
+template <class T, int V>
+static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
+{
+    if (!p.accumulate) {
+        fill_rows_kernel<T, V><<<dim3(2048), dim3(256), 0, st>>>((T *)p.out, p.n, p.ld_out, p.d / V);
+        AVQ_HIP(hipGetLastError());
+    }
+    if (p.count == 0) return AVQ_OK;
+    const GradScratch s = grad_scratch(p.n, p.d, p.count, p.scratch);
+    const uint32_t count = (uint32_t)p.count, n = (uint32_t)p.n;
+    const int bins = 1 << s.bits;
+    const uint32_t *keys = nullptr, *pos = nullptr;
+    for (int pass = 0; pass < s.passes; ++pass) {
+        const int32_t *ids = pass == 0 ? p.ids : nullptr;
+        const int to = pass & 1;
+        sort_count_kernel<<<dim3(s.tiles), dim3(kSortThreads), 0, st>>>(ids, keys, count, n, pass * s.bits, bins, s.hist, s.tiles);
+        AVQ_HIP(hipGetLastError());
+        sort_scan_kernel<<<dim3(1), dim3(1024), 0, st>>>(s.hist, bins * s.tiles);
+        AVQ_HIP(hipGetLastError());
+        sort_place_kernel<<<dim3(s.tiles), dim3(kSortThreads), 0, st>>>(ids, keys, pos, count, n, pass * s.bits, s.bits, s.hist, s.tiles, s.keys[to], s.pos[to]);
+        AVQ_HIP(hipGetLastError());
+        keys = s.keys[to];
+        pos = s.pos[to];
+    }
+    int lanes = 4;
+    while (lanes < 256 && lanes < p.d / V) lanes *= 2;
+    const int64_t chunks = (p.count + kRunChunk - 1) / kRunChunk;
+    const dim3 grid((unsigned)((chunks + 256 / lanes - 1) / (256 / lanes)));
+    run_sums_kernel<T, V><<<grid, dim3(256), 0, st>>>((const T *)p.grad, p.ld_grad, keys, pos, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
+    AVQ_HIP(hipGetLastError());
+    run_joins_kernel<T, V><<<grid, dim3(256), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
+    AVQ_HIP(hipGetLastError());
+    return AVQ_OK;
+}
+
+template <class T>
+static int embed_grad_typed(const EmbedGradParams &p, hipStream_t st)
+{
+    int w = row_width(p.out, p.ld_out, p.d, sizeof(T));
+    if (p.count > 0) w = std::min(w, row_width(p.grad, p.ld_grad, p.d, sizeof(T)));
+    if (w == 16) return embed_grad_run<T, 16 / sizeof(T)>(p, st);
+    if (w == 8) return embed_grad_run<T, 8 / sizeof(T)>(p, st);
+    return embed_grad_run<T, 1>(p, st);
+}
+
+int launch_embed_grad(const EmbedGradParams &p, hipStream_t st)
+{
+    if (p.type == AVQ_F32) return embed_grad_typed<float>(p, st);
+    return p.type == AVQ_BF16 ? embed_grad_typed<bf16_t>(p, st) : embed_grad_typed<f16_t>(p, st);
+}
+
+} // namespace avq

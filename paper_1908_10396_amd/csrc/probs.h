@@ -1,0 +1,29 @@
+// What the kernels of the log probabilities and of their gradient share.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "avq_internal.h"
+
+namespace avq {
+
+// Running statistics of logits s (in units of log 2): the maximum m, the sums of 2^(s - m) and of 2^(s - m) (s - m).
+struct Stat { float m, l, t; };
+
+// Of two sets of logits; one without any has m = -inf and sums of 0.
+__device__ __forceinline__ Stat join(const Stat &a, const Stat &b)
+{
+    const float m = fmaxf(a.m, b.m);
+    if (!(m > -INFINITY)) return Stat{m, a.l + b.l, a.t + b.t}; // (NaN goes on in the sums)
+    const float da = a.m > -INFINITY ? a.m - m : 0.0f, db = b.m > -INFINITY ? b.m - m : 0.0f;
+    const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+    return Stat{m, a.l * fa + b.l * fb, fa * __fmaf_rn(a.l, da, a.t) + fb * __fmaf_rn(b.l, db, b.t)};
+}
+
+// Dynamic LDS of the kernel that finishes a query: the query in fp32, the keys of 32 rows for each of the k best groups, the
+// k best of them, the groups.
+constexpr size_t kFinishLds = kMaxDynLds - 16 * 1024;
+inline size_t finish_lds(int d, int k) { return (((size_t)d * 4 + 15) & ~(size_t)15) + (size_t)k * (32 * 8 + 8 + 4); }
+
+} // namespace avq
