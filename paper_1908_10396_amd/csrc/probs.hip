@@ -3,9 +3,12 @@
 // and the k rows of largest s_i (ties: the lower id). One pass over the rows keeps, per query and lane, the running maximum m
 // and the sums of e^(s - m) and e^(s - m) (s - m) in fp32; the logits are never stored. For the best rows it leaves the
 // largest inner product of every 32 rows; the k groups with the largest of those hold the k best rows, which are scored again.
+#include "mma_tiles.h"
 #include "probs.h"
 #include "row_types.h"
 #include "wg_select.h"
+
+#include <type_traits>
 
 namespace avq {
 
@@ -77,7 +80,7 @@ constexpr int kStreamThreads = 256, kStreamWaves = kStreamThreads / 64;
 // bytes are the matrix instruction's layout), the queries' from LDS, where they lie in the same order (QLDS), or from memory.
 template <class T, int QT, bool ALIGNED, bool QLDS>
 __global__ __launch_bounds__(kStreamThreads) void prob_stream_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q,
-                                                                     float c2, int negate, float4 *__restrict__ stats, float *__restrict__ gmax)
+                                                                     float c2, int negate, float4 *__restrict__ stats, float *__restrict__ gmax, int64_t gstride)
 {
     extern __shared__ Frag qs[]; // [step][QT][64]
     __shared__ float4 joined[kStreamWaves][QT * 16];
@@ -168,7 +171,7 @@ __global__ __launch_bounds__(kStreamThreads) void prob_stream_kernel(const T *__
             if (gmax) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
-                if (kg == 0 && q0 + i * 16 + r16 < nq) gmax[tile * nq + q0 + i * 16 + r16] = top;
+                if (kg == 0 && q0 + i * 16 + r16 < nq) gmax[(int64_t)(q0 + i * 16 + r16) * gstride + tile] = top;
             }
         }
     }
@@ -186,6 +189,95 @@ __global__ __launch_bounds__(kStreamThreads) void prob_stream_kernel(const T *__
         Stat a{joined[0][i].x, joined[0][i].y, joined[0][i].z};
         for (int w = 1; w < kStreamWaves; ++w) a = join(a, Stat{joined[w][i].x, joined[w][i].y, joined[w][i].z});
         stats[(size_t)blockIdx.x * nq + q0 + i] = make_float4(a.m, a.l, a.t, 0.0f);
+    }
+}
+
+// ---- many queries: tiles of a matrix product ----------------------------------------------------
+
+// Statistics of 128 queries over a part of the rows, 256 rows at a time; a lane has two queries, 64 of a tile's rows of each.
+// X: the launch's rows, Q: all queries, negated where the scale is.
+template <class H, int TERMS, bool BEST>
+__global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Rows16 Q, int halves, float c2, const Largest *__restrict__ largest, const float *__restrict__ q_inv, int parts,
+                                                                    int others, float4 *__restrict__ stats, float *__restrict__ gmax, int64_t gstride)
+{
+    extern __shared__ char lds[];
+    const Place place = place_of(blockIdx.x, others);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t tiles = (X.rows + kTileM - 1) / kTileM;
+    int64_t first;
+    int count;
+    part_tiles(tiles, parts, place.part, &first, &count);
+    const int64_t q0 = (int64_t)place.other * kTileN;
+    float cq[2], m[2], l[2], t[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        cq[j] = c2;
+        if (TERMS > 1) {
+            const int64_t q = min(q0 + acc_col(j), Q.rows - 1);
+            cq[j] = c2 * q_inv[q] * (1.0f / range_scale(largest->points));
+        }
+        m[j] = -INFINITY;
+        l[j] = t[j] = 0.0f;
+    }
+    run_tiles<H, TERMS, BEST, RowCopies>(X, Q, halves, count, lds, [&](int i, RowCopies &c) { c.seek(X, (first + i) * kTileM, Q, q0); },
+        [&](int i, f32x16 (&acc)[4][2]) {
+            const int64_t row0 = (first + i) * kTileM;
+            const bool whole = row0 + kTileM <= X.rows;
+            const int valid = whole ? kTileM : (int)(X.rows - row0);
+            auto take = [&](auto tail) {
+                constexpr bool TAIL = decltype(tail)::value;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float group[4];
+#pragma unroll
+                    for (int a = 0; a < 4; ++a) {
+                        float g = -INFINITY;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (!TAIL || acc_row(a, r) < valid) g = fmaxf(g, acc[a][j][r]);
+                        group[a] = g;
+                    }
+                    const float top = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
+                    if (top > m[j]) {
+                        if (m[j] > -INFINITY) {
+                            const float down = (m[j] - top) * cq[j], f = __builtin_amdgcn_exp2f(down);
+                            t[j] = f * __fmaf_rn(l[j], down, t[j]);
+                            l[j] *= f;
+                        }
+                        m[j] = top;
+                    }
+                    const float shift = m[j] > -INFINITY ? -(m[j] * cq[j]) : 0.0f;
+                    // four sums side by side, then one
+                    float ls[4] = {}, ts[4] = {};
+#pragma unroll
+                    for (int a = 0; a < 4; ++a)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (!TAIL || acc_row(a, r) < valid) {
+                                const float s2 = __fmaf_rn(acc[a][j][r], cq[j], shift), e = __builtin_amdgcn_exp2f(s2);
+                                ls[a] += e;
+                                ts[a] = __fmaf_rn(e, s2, ts[a]);
+                            }
+                    l[j] += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+                    t[j] += (ts[0] + ts[1]) + (ts[2] + ts[3]);
+                    if (BEST) {
+#pragma unroll
+                        for (int a = 0; a < 4; ++a) group[a] = fmaxf(group[a], __shfl_xor(group[a], 32, 64));
+                        const int64_t q = q0 + acc_col(j);
+                        if (lane < 32 && q < Q.rows)
+                            *(float4 *)(gmax + q * gstride + (first + i) * (kTileM / 32) + (wave >> 1) * 4) = make_float4(group[0], group[1], group[2], group[3]);
+                    }
+                }
+            };
+            if (whole) take(std::false_type{});
+            else take(std::true_type{});
+        });
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        Stat a{m[j] > -INFINITY ? m[j] * cq[j] : -INFINITY, l[j], t[j]};
+        a = join(a, Stat{__shfl_xor(a.m, 32, 64), __shfl_xor(a.l, 32, 64), __shfl_xor(a.t, 32, 64)});
+        const int64_t q = q0 + acc_col(j);
+        if (lane < 32 && q < Q.rows) stats[(size_t)(place.part * 2 + (wave >> 1)) * Q.rows + q] = make_float4(a.m, a.l, a.t, 0.0f);
     }
 }
 
@@ -223,7 +315,7 @@ template <class T>
 __global__ __launch_bounds__(kFinishThreads) void prob_finish_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, float scale,
                                                                      const float4 *__restrict__ stats, int parts, const int32_t *__restrict__ ids, int given,
                                                                      float *__restrict__ logp_out, float *__restrict__ lse_out, float *__restrict__ entropy_out,
-                                                                     const float *__restrict__ gmax, int k, int32_t *__restrict__ alt_ids, float *__restrict__ alt_logp)
+                                                                     const float *__restrict__ gmax, int64_t gstride, int k, int32_t *__restrict__ alt_ids, float *__restrict__ alt_logp)
 {
     __shared__ WgSelectScratch sel;
     __shared__ Stat wave_stat[kFinishWaves];
@@ -264,7 +356,7 @@ __global__ __launch_bounds__(kFinishThreads) void prob_finish_kernel(const T *__
 
     const uint32_t n_groups = (uint32_t)((n + 31) / 32);
     if (tid == 0) list_count = 0;
-    auto group_key = [&](uint32_t g) { return ((u64)order_of(gmax[(size_t)g * nq + row]) << 32) | (u64)(0xffffffffu - g); };
+    auto group_key = [&](uint32_t g) { return ((u64)order_of(gmax[row * gstride + g]) << 32) | (u64)(0xffffffffu - g); };
     const u64 least = wg_select_threshold_of([&](auto &&fn) { for (uint32_t g = tid; g < n_groups; g += kFinishThreads) fn(group_key(g)); }, k, &sel);
     __syncthreads();
     for (uint32_t g = tid; g < n_groups; g += kFinishThreads)
@@ -321,26 +413,65 @@ static int stream_tile(int type, int d, int nq)
     return qt;
 }
 
-struct ProbScratch { float4 *stats; float *gmax; size_t bytes; int groups, qt, query_tiles; };
+// From how many queries on the tiles take over: up to 64 the stream reads the rows once.
+static bool by_tiles(int nq) { return nq > 64; }
 
-static ProbScratch prob_scratch(int type, int64_t n, int d, int nq, int k, void *base)
+constexpr int kTileGroups = 512; // two workgroups a compute unit
+constexpr size_t kPackBytes = (size_t)1 << 30; // most that packed rows take at a time
+
+struct ProbScratch {
+    float4 *stats; float *gmax; int64_t gstride;
+    int groups, qt, query_tiles;                         // stream
+    bool pack; int width, parts, launches; int64_t part; // tiles: rows a launch
+    uint16_t *x16, *q16; int64_t x_plane, q_plane; float *q_inv; Largest *largest;
+    size_t bytes;
+};
+
+static ProbScratch prob_scratch(const ProbParams &p, void *base)
 {
     ProbScratch s{};
-    s.qt = stream_tile(type, d, nq);
-    s.query_tiles = (nq + 16 * s.qt - 1) / (16 * s.qt);
-    s.groups = stream_groups(n, s.query_tiles);
-    s.stats = (float4 *)base;
-    s.bytes = (size_t)s.groups * nq * sizeof(float4);
-    s.bytes = (s.bytes + 255) & ~(size_t)255;
-    s.gmax = base && k > 0 ? (float *)((char *)base + s.bytes) : nullptr;
-    if (k > 0) s.bytes += (size_t)((n + 31) / 32) * nq * sizeof(float);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        void *q = base ? (char *)base + at : nullptr;
+        at += (bytes + 255) & ~(size_t)255;
+        return q;
+    };
+    s.gstride = (p.n + kTileM - 1) / kTileM * (kTileM / 32);
+    if (!by_tiles(p.nq)) {
+        s.qt = stream_tile(p.type, p.d, p.nq);
+        s.query_tiles = (p.nq + 16 * s.qt - 1) / (16 * s.qt);
+        s.groups = stream_groups(p.n, s.query_tiles);
+        s.stats = (float4 *)take((size_t)s.groups * p.nq * sizeof(float4));
+    } else {
+        const int planes = p.type == AVQ_F32 ? 2 : 1;
+        s.width = (p.d + 31) / 32 * 32;
+        // (base == NULL: the size for rows that need packing, whatever their place and stride)
+        s.pack = !base || p.type == AVQ_F32 || s.width != p.d || (uintptr_t)p.points % 16 != 0 || p.ld_points % 8 != 0;
+        s.part = p.n;
+        if (s.pack) s.part = std::min<int64_t>(p.n, std::max<int64_t>(65536, (int64_t)(kPackBytes / (2 * planes * (size_t)s.width)) / kTileM * kTileM));
+        s.launches = (int)((p.n + s.part - 1) / s.part);
+        s.query_tiles = (p.nq + kTileN - 1) / kTileN;
+        s.parts = parts_for((s.part + kTileM - 1) / kTileM, s.query_tiles, kTileGroups);
+        // (as many statistics with one launch as with several: the number of parts only falls with the rows a launch has)
+        s.stats = (float4 *)take((size_t)s.launches * std::max(s.parts, parts_for((p.n + kTileM - 1) / kTileM, s.query_tiles, kTileGroups)) * 2 * p.nq * sizeof(float4));
+        s.q_plane = (int64_t)p.nq * s.width;
+        s.q16 = (uint16_t *)take((size_t)s.q_plane * 2 * planes);
+        s.q_inv = (float *)take((size_t)p.nq * sizeof(float));
+        s.largest = (Largest *)take(sizeof(Largest));
+        s.x_plane = s.part * s.width;
+        if (s.pack) s.x16 = (uint16_t *)take((size_t)s.x_plane * 2 * planes);
+    }
+    s.gmax = p.k > 0 ? (float *)take((size_t)s.gstride * p.nq * sizeof(float)) : nullptr;
+    s.bytes = at;
     return s;
 }
 
 size_t log_probs_scratch_bytes(int type, int64_t n, int d, int nq, int given, int k)
 {
     (void)given;
-    return nq == 0 ? 0 : prob_scratch(type, n, d, nq, k, nullptr).bytes;
+    ProbParams p{};
+    p.type = type; p.n = n; p.d = d; p.nq = nq; p.k = k;
+    return nq == 0 ? 0 : prob_scratch(p, nullptr).bytes;
 }
 
 template <class T, int QT, bool ALIGNED, bool QLDS>
@@ -351,7 +482,7 @@ static int stream_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
     AVQ_TRY(set_lds_limit((const void *)prob_stream_kernel<T, QT, ALIGNED, QLDS>, kMaxDynLds - sizeof(float4) * kStreamWaves * 64, &once));
     const float c2 = fabsf(p.scale) * 1.44269504088896341f;
     prob_stream_kernel<T, QT, ALIGNED, QLDS><<<dim3(s.groups, s.query_tiles), dim3(kStreamThreads), lds, st>>>(
-        (const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.nq, p.ld_queries, c2, p.scale < 0.0f, s.stats, s.gmax);
+        (const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.nq, p.ld_queries, c2, p.scale < 0.0f, s.stats, s.gmax, s.gstride);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
@@ -365,16 +496,59 @@ static int stream_sized(const ProbParams &p, const ProbScratch &s, hipStream_t s
     return s.qt == 2 ? stream_run<T, 2, ALIGNED, true>(p, s, st) : stream_run<T, 4, ALIGNED, true>(p, s, st);
 }
 
+template <class H, int TERMS>
+static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
+{
+    const int size = type_bytes(p.type);
+    const float c2 = fabsf(p.scale) * 1.44269504088896341f;
+    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, p.nq, s.width, s.q16, s.q_plane, nullptr, s.q_inv, p.scale < 0.0f, st));
+    if (TERMS > 1) {
+        AVQ_TRY(launch_clear_largest(s.largest, st));
+        AVQ_TRY(launch_largest((const float *)p.points, p.n, p.d, p.ld_points, &s.largest->points, st));
+    }
+    static LdsLimitOnce with_best, without;
+    const Rows16 Q{s.q16, s.width, s.q_plane, p.nq};
+    for (int i = 0; i < s.launches; ++i) {
+        const int64_t lo = i * s.part, rows = std::min<int64_t>(s.part, p.n - lo);
+        const char *from = (const char *)p.points + lo * p.ld_points * size;
+        Rows16 X{(const uint16_t *)from, p.ld_points, 0, rows};
+        if (s.pack) {
+            AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, rows, s.width, s.x16, s.x_plane, &s.largest->points, nullptr, false, st));
+            X = Rows16{s.x16, s.width, s.x_plane, rows};
+        }
+        float4 *stats = s.stats + (size_t)i * s.parts * 2 * p.nq;
+        const dim3 grid((unsigned)(s.parts * s.query_tiles));
+        if (p.k > 0) {
+            AVQ_TRY(set_lds_limit((const void *)prob_tile_kernel<H, TERMS, true>, kTileLds, &with_best));
+            prob_tile_kernel<H, TERMS, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, (p.d + 15) / 16, c2, s.largest, s.q_inv, s.parts, s.query_tiles, stats,
+                                                                                      s.gmax + lo / 32, s.gstride);
+        } else {
+            AVQ_TRY(set_lds_limit((const void *)prob_tile_kernel<H, TERMS, false>, kTileLds, &without));
+            prob_tile_kernel<H, TERMS, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, (p.d + 15) / 16, c2, s.largest, s.q_inv, s.parts, s.query_tiles, stats, nullptr, 0);
+        }
+        AVQ_HIP(hipGetLastError());
+    }
+    return AVQ_OK;
+}
+
 template <class T>
 static int log_probs_typed(const ProbParams &p, hipStream_t st)
 {
-    const ProbScratch s = prob_scratch(p.type, p.n, p.d, p.nq, p.k, p.scratch);
-    const bool aligned = ((uintptr_t)p.points % 16) == 0 && (p.ld_points * sizeof(T)) % 16 == 0;
-    AVQ_TRY(aligned ? (stream_sized<T, true>(p, s, st)) : (stream_sized<T, false>(p, s, st)));
+    const ProbScratch s = prob_scratch(p, p.scratch);
+    int parts = s.groups;
+    if (by_tiles(p.nq)) {
+        if constexpr (sizeof(T) == 4) AVQ_TRY((tiles_run<f16_t, 3>(p, s, st)));
+        else AVQ_TRY((tiles_run<T, 1>(p, s, st)));
+        parts = s.launches * s.parts * 2;
+    } else {
+        const bool aligned = ((uintptr_t)p.points % 16) == 0 && (p.ld_points * sizeof(T)) % 16 == 0;
+        AVQ_TRY(aligned ? (stream_sized<T, true>(p, s, st)) : (stream_sized<T, false>(p, s, st)));
+    }
     static LdsLimitOnce once;
     AVQ_TRY(set_lds_limit((const void *)prob_finish_kernel<T>, kFinishLds, &once));
     prob_finish_kernel<T><<<dim3(p.nq), dim3(kFinishThreads), finish_lds(p.d, p.k), st>>>((const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.nq, p.ld_queries, p.scale,
-                                                                                       s.stats, s.groups, p.ids, p.given, p.logp, p.lse, p.entropy, s.gmax, p.k, p.alt_ids, p.alt_logp);
+                                                                                       s.stats, parts, p.ids, p.given, p.logp, p.lse, p.entropy, s.gmax, s.gstride, p.k, p.alt_ids,
+                                                                                       p.alt_logp);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
