@@ -2,74 +2,129 @@
 // upstream g_tj (of log p of id_tj), h_t (of H_t), l_t (of lse_t):
 //   G_ti = sum_j g_tj [id_tj = i] - p_ti (a_t + h_t log p_ti),  a_t = sum_j g_tj - l_t + h_t H_t,
 //   dq_t = c sum_i G_ti x_i,  dx_i = c sum_t G_ti q_t.
-// A part of the rows at a time: its logits once more, G of them, and the two products.
+// Three products of 2 n nq d operations each, on the matrix instructions, a part of the rows at a time: the part's logits once
+// more, whose epilogue leaves G transposed, [row][query], in 16 bits (fp32: two f16 planes); dx = G^T Q, whose inner dimension
+// both operands hold side by side (Q transposed once); dq += G X by operands that are turned as they are read from LDS. G is kept
+// relative to a bound of its magnitude, so that f16 holds it down to 2^-38 of it; its rounding to 16 bits (bf16: 2^-9) is that of
+// the operands' own type. The entries of the given ids, where p is taken from g, are formed by themselves in fp32 before rounding.
+#include "mma_tiles.h"
 #include "probs.h"
 #include "row_types.h"
 
 namespace avq {
 
-// a_t and h_t
-__global__ void grad_coef_kernel(const int32_t *__restrict__ ids, int64_t n, int nq, int given, const float *__restrict__ g, const float *__restrict__ h, const float *__restrict__ entropy,
-                                 const float *__restrict__ gl, float2 *__restrict__ coef)
-{
-    const int t = blockIdx.x * blockDim.x + threadIdx.x;
-    if (t >= nq) return;
-    float a = 0.0f;
-    for (int j = 0; j < given; ++j) {
-        const int32_t id = ids[(int64_t)t * given + j];
-        if (id >= 0 && (int64_t)id < n) a += g[(int64_t)t * given + j];
-    }
-    if (gl) a -= gl[t];
-    if (h) a += h[t] * entropy[t];
-    coef[t] = make_float2(a, h ? h[t] : 0.0f);
-}
+constexpr float kGradTop = 16384.0f; // what the bound of |G| is brought to
 
-// 64 x 64 tile of A B^T over k, 4 x 4 values a thread.
-template <class LoadA, class LoadB, class Store>
-__device__ __forceinline__ void tile_product(int64_t rows_a, int64_t rows_b, int64_t depth, LoadA load_a, LoadB load_b, Store store)
+// the factor that G is kept with, and its inverse
+__device__ __forceinline__ float grad_bound(const Largest *largest) { return fmaxf(__uint_as_float(largest->upstream), 1e-30f); }
+__device__ __forceinline__ float grad_factor(const Largest *largest) { return kGradTop / grad_bound(largest); }
+
+// a_t and h_t, and the bound of |G|
+__global__ __launch_bounds__(256) void grad_coef_kernel(const int32_t *__restrict__ ids, int64_t n, int nq, int given, const float *__restrict__ g, const float *__restrict__ h,
+                                                        const float *__restrict__ entropy, const float *__restrict__ gl, float2 *__restrict__ coef, Largest *__restrict__ largest)
 {
-    __shared__ float sa[16][68], sb[16][68];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const int64_t a0 = (int64_t)blockIdx.y * 64, b0 = (int64_t)blockIdx.x * 64;
-    float acc[4][4] = {};
-    for (int64_t k0 = 0; k0 < depth; k0 += 16) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < 1024; i += 256) {
-            const int64_t r = i >> 4, k = k0 + (i & 15);
-            sa[i & 15][r] = a0 + r < rows_a && k < depth ? load_a(a0 + r, k) : 0.0f;
-            sb[i & 15][r] = b0 + r < rows_b && k < depth ? load_b(b0 + r, k) : 0.0f;
+    const int t = blockIdx.x * 256 + threadIdx.x;
+    float bound = 0.0f;
+    if (t < nq) {
+        float a = 0.0f, mag = 0.0f;
+        for (int j = 0; j < given; ++j) {
+            const int32_t id = ids[(int64_t)t * given + j];
+            if (id >= 0 && (int64_t)id < n) {
+                const float v = g[(int64_t)t * given + j];
+                a += v;
+                mag += fabsf(v);
+            }
         }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = __fmaf_rn(sa[k][ty * 4 + i], sb[k][tx * 4 + j], acc[i][j]);
+        if (gl) a -= gl[t];
+        if (h) a += h[t] * entropy[t];
+        coef[t] = make_float2(a, h ? h[t] : 0.0f);
+        bound = mag + fabsf(a) + (h ? fabsf(h[t]) : 0.0f); // (p |log p| < 0.37)
     }
+    uint32_t m = bound < INFINITY ? __float_as_uint(bound) : 0u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (a0 + ty * 4 + i < rows_a && b0 + tx * 4 + j < rows_b) store(a0 + ty * 4 + i, b0 + tx * 4 + j, acc[i][j]);
+    for (int w = 1; w < 64; w <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, w, 64));
+    if ((threadIdx.x & 63) == 0 && m != 0) atomicMax(&largest->upstream, m);
 }
 
+__device__ __forceinline__ void put16(uint16_t *to, int64_t, float v, bf16_t) { *to = from_f32<bf16_t>(v).bits; }
+__device__ __forceinline__ void put16(uint16_t *to, int64_t, float v, f16_t) { *to = from_f32<f16_t>(v).bits; }
+__device__ __forceinline__ void put16(uint16_t *to, int64_t plane, float v, float)
+{
+    const _Float16 hi = (_Float16)v;
+    *to = __builtin_bit_cast(uint16_t, hi);
+    to[plane] = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)hi));
+}
+
+// G^T of the part's rows: 256 queries of a workgroup by 128 rows at a time. T: the caller's type, H: the instructions'.
+template <class T, class H, int TERMS, bool ENTROPY>
+__global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Rows16 X, int halves, float c2, const float *__restrict__ lse, const float2 *__restrict__ coef,
+                                                                    const Largest *__restrict__ largest, int parts, int others, uint16_t *__restrict__ G, int width, int64_t plane)
+{
+    extern __shared__ char lds[];
+    __shared__ float4 shift[kTileM / 4], up[kTileM / 4], up_h[kTileM / 4]; // -lse / log 2; a and h, in G's units
+    const Place place = place_of(blockIdx.x, others);
+    const int wave = threadIdx.x >> 6, half = (threadIdx.x & 63) >> 5;
+    const int64_t tiles = (X.rows + kTileN - 1) / kTileN, q0 = (int64_t)place.other * kTileM;
+    int64_t first;
+    int count;
+    part_tiles(tiles, parts, place.part, &first, &count);
+    {
+        const int64_t t = q0 + threadIdx.x;
+        const bool real = t < Q.rows; // (queries past the last: a logit of 0 and no gradient)
+        const float f = grad_factor(largest);
+        const float2 c = real ? coef[t] : make_float2(0.0f, 0.0f);
+        ((float *)shift)[threadIdx.x] = real ? -lse[t] * 1.44269504088896341f : 0.0f;
+        ((float *)up)[threadIdx.x] = -c.x * f;
+        if (ENTROPY) ((float *)up_h)[threadIdx.x] = -c.y * f * 0.693147180559945309f;
+    }
+    const float cq = TERMS > 1 ? c2 * (1.0f / range_scale(largest->points)) * (1.0f / range_scale(largest->queries)) : c2;
+    __syncthreads();
+    run_tiles<H, TERMS, true, RowCopies>(Q, X, halves, count, lds, [&](int i, RowCopies &c) { c.seek(Q, q0, X, (first + i) * kTileN); },
+        [&](int i, f32x16 (&acc)[4][2]) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int64_t row = (first + i) * kTileN + acc_col(j);
+                const bool real = row < X.rows;
+#pragma unroll
+                for (int a = 0; a < 4; ++a)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const int t = (wave >> 1) * 128 + a * 32 + 8 * b + 4 * half; // four queries side by side
+                        const float4 s4 = shift[t / 4], u4 = up[t / 4];
+                        const float sh[4] = {s4.x, s4.y, s4.z, s4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
+                        float hh[4] = {};
+                        if (ENTROPY) { const float4 v = up_h[t / 4]; hh[0] = v.x; hh[1] = v.y; hh[2] = v.z; hh[3] = v.w; }
+                        Pack<uint16_t, 4> hi, lo;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float s2 = __fmaf_rn(acc[a][j][4 * b + e], cq, sh[e]), p = __builtin_amdgcn_exp2f(s2);
+                            float v = p * (ENTROPY ? __fmaf_rn(hh[e], s2, u[e]) : u[e]);
+                            if (ENTROPY && p == 0.0f) v = 0.0f; // (p log p)
+                            if (!real) v = 0.0f;
+                            uint16_t two[2];
+                            put16(two, 1, v, T{});
+                            hi.e[e] = two[0];
+                            if (TERMS > 1) lo.e[e] = two[1];
+                        }
+                        if (q0 + t < width) {
+                            uint16_t *to = G + row * width + q0 + t;
+                            *(Pack<uint16_t, 4> *)to = hi;
+                            if (TERMS > 1) *(Pack<uint16_t, 4> *)(to + plane) = lo;
+                        }
+                    }
+            }
+        });
+}
+
+// The entries of the given ids among the part's rows, a wave each; the first of a query's equal ids has the sum of their g.
 template <class T>
-__global__ __launch_bounds__(256) void grad_logits_kernel(const T *__restrict__ q, int nq, int64_t ld_q, const T *__restrict__ x, int64_t rows, int64_t ld_x, int d, float scale,
-                                                          const float *__restrict__ lse, const float2 *__restrict__ coef, float *__restrict__ G)
+__global__ __launch_bounds__(256) void grad_given_kernel(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, int d, float scale,
+                                                         const int32_t *__restrict__ ids, int given, const float *__restrict__ g, const float *__restrict__ lse,
+                                                         const float2 *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, uint16_t *__restrict__ G, int width,
+                                                         int64_t plane)
 {
-    tile_product(nq, rows, d, [&](int64_t t, int64_t k) { return to_f32(q[t * ld_q + k]); }, [&](int64_t i, int64_t k) { return to_f32(x[i * ld_x + k]); },
-                 [&](int64_t t, int64_t i, float s) {
-                     const float logp = s * scale - lse[t];
-                     const float2 c = coef[t];
-                     G[t * rows + i] = -__expf(logp) * __fmaf_rn(c.y, logp, c.x);
-                 });
-}
-
-// G += g at the given ids; a thread per given id, the first of equal ones adds for all of them
-__global__ void grad_given_kernel(const int32_t *__restrict__ ids, int nq, int given, const float *__restrict__ g, int64_t lo, int64_t rows, float *__restrict__ G)
-{
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    const int lane = threadIdx.x & 63;
+    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (i >= (int64_t)nq * given) return;
     const int64_t t = i / given, j = i - t * given;
     const int64_t id = ids[i];
@@ -80,64 +135,169 @@ __global__ void grad_given_kernel(const int32_t *__restrict__ ids, int nq, int g
             if (o < j) return;
             sum += g[t * given + o];
         }
-    G[t * rows + (id - lo)] += sum;
+    const T *xr = x + id * ld_x, *qr = q + t * ld_q;
+    float s = 0.0f;
+    for (int c = lane; c < d; c += 64) s = __fmaf_rn(to_f32(qr[c]), to_f32(xr[c]), s);
+    s = group_sum<64>(s) * scale - lse[t];
+    if (lane != 0) return;
+    const float2 c = coef[t];
+    const float p = __builtin_amdgcn_exp2f(s * 1.44269504088896341f);
+    const float v = sum - (p > 0.0f || p != p ? p * __fmaf_rn(c.y, s, c.x) : 0.0f);
+    put16(G + (id - lo) * width + t, plane, v * grad_factor(largest), T{});
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void grad_queries_kernel(const float *__restrict__ G, const T *__restrict__ x, int64_t rows, int64_t ld_x, int nq, int d, int first, float *__restrict__ dq)
+// fn for every four rows side by side of a lane's accumulators acc[a][j][4 b ..]. One after the other: the compiler would
+// otherwise keep the addresses of all of them in registers at once.
+template <int A, int B, int J> struct QuadAt { static constexpr int a = A, b = B, j = J; };
+template <int I = 0, class Fn> __device__ __forceinline__ void for_quads(Fn fn)
 {
-    tile_product(nq, d, rows, [&](int64_t t, int64_t i) { return G[t * rows + i]; }, [&](int64_t c, int64_t i) { return to_f32(x[i * ld_x + c]); },
-                 [&](int64_t t, int64_t c, float s) { dq[t * d + c] = first ? s : dq[t * d + c] + s; });
+    if constexpr (I < 32) {
+        fn(QuadAt<I / 4 % 4, I % 4, I / 16>{});
+        asm volatile("" ::: "memory");
+        for_quads<I + 1>(fn);
+    }
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void grad_rows_kernel(const float *__restrict__ G, const T *__restrict__ q, int nq, int64_t ld_q, int64_t rows, int d, float scale, int accumulate,
-                                                        T *__restrict__ dx, int64_t ld_dx)
+// dx of the part's rows: 256 rows by 128 dimensions.
+template <class T, class H, int TERMS, bool ACCUMULATE>
+__global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Rows16 Qt, int halves, float scale, const Largest *__restrict__ largest, int parts, int others, int64_t rows,
+                                                                    int d, T *__restrict__ dx, int64_t ld_dx)
 {
-    tile_product(d, rows, nq, [&](int64_t c, int64_t t) { return to_f32(q[t * ld_q + c]); }, [&](int64_t i, int64_t t) { return G[t * rows + i]; },
-                 [&](int64_t c, int64_t i, float s) { T *to = dx + i * ld_dx + c; *to = from_f32<T>(accumulate ? to_f32(*to) + s * scale : s * scale); });
+    extern __shared__ char lds[];
+    const Place place = place_of(blockIdx.x, others);
+    const int64_t tiles = (rows + kTileM - 1) / kTileM, c0 = (int64_t)place.other * kTileN;
+    int64_t first;
+    int count;
+    part_tiles(tiles, parts, place.part, &first, &count);
+    const float f = grad_bound(largest) * (1.0f / kGradTop) * scale * (TERMS > 1 ? 1.0f / range_scale(largest->queries) : 1.0f);
+    run_tiles<H, TERMS, true, RowCopies>(G, Qt, halves, count, lds, [&](int i, RowCopies &c) { c.seek(G, (first + i) * kTileM, Qt, c0); },
+        [&](int i, f32x16 (&acc)[4][2]) {
+            const int64_t row0 = (first + i) * kTileM + acc_row(0, 0);
+            const int64_t left = rows - row0; // rows from this lane's first one on
+            for_quads([&](auto at) {
+                constexpr int a = decltype(at)::a, b = decltype(at)::b, j = decltype(at)::j;
+                const int64_t c = c0 + acc_col(j);
+                T *to = dx + (row0 + a * 32 + b * 8) * ld_dx + c;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (c < d && a * 32 + b * 8 + e < left) {
+                        const float v = acc[a][j][4 * b + e] * f;
+                        *to = from_f32<T>(ACCUMULATE ? to_f32(*to) + v : v);
+                    }
+                    to += ld_dx;
+                }
+            });
+        });
 }
 
-template <class T>
-__global__ void grad_round_kernel(const float *__restrict__ dq, int nq, int d, float scale, T *__restrict__ out, int64_t ld)
+// The part's share of dq, split over the part's rows: sums[split][nq][d] in fp32, begun (first) or added to.
+template <class H, int TERMS>
+__global__ __launch_bounds__(kTileThreads, 2) void grad_queries_kernel(Rows16 G, Rows16 X, int nq, int width, int d, int splits, int q_tiles, int d_tiles, int begin, float *__restrict__ sums)
 {
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i < (int64_t)nq * d) out[(i / d) * ld + i % d] = from_f32<T>(dq[i] * scale);
+    extern __shared__ char lds[];
+    const Place place = place_of(blockIdx.x, q_tiles * d_tiles);
+    const int64_t t0 = (int64_t)(place.other % q_tiles) * kTileM, c0 = (int64_t)(place.other / q_tiles) * kTileN;
+    const int64_t steps = (G.rows + kTileK - 1) / kTileK;
+    int64_t first;
+    int count;
+    part_tiles(steps, splits, place.part, &first, &count);
+    float *mine = sums + (int64_t)place.part * nq * d;
+    auto store = [&](int, f32x16 (&acc)[4][2]) {
+        const int64_t row0 = t0 + acc_row(0, 0), left = nq - row0;
+        for_quads([&](auto at) {
+            constexpr int a = decltype(at)::a, b = decltype(at)::b, j = decltype(at)::j;
+            const int64_t c = c0 + acc_col(j);
+            float *to = mine + (row0 + a * 32 + b * 8) * d + c;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (c < d && a * 32 + b * 8 + e < left) *to = begin ? acc[a][j][4 * b + e] : *to + acc[a][j][4 * b + e];
+                to += d;
+            }
+        });
+    };
+    if (count == 0) { // (a workgroup without rows still begins its sums)
+        f32x16 none[4][2] = {};
+        if (begin) store(0, none);
+        return;
+    }
+    run_tiles<H, TERMS, true, ColumnCopies>(G, X, 2 * count, 1, lds, [&](int, ColumnCopies &c) { c.row = first * kTileK; c.seek(G, t0, width, X, c0); }, store);
+}
+
+// dq = the splits' sums, in their order
+template <class T>
+__global__ __launch_bounds__(256) void grad_join_kernel(const float *__restrict__ sums, int splits, int nq, int d, float scale, int fp32, const Largest *__restrict__ largest,
+                                                        T *__restrict__ out, int64_t ld)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)nq * d;
+    if (i >= all) return;
+    float s = 0.0f;
+#pragma unroll 8
+    for (int p = 0; p < splits; ++p) s += sums[p * all + i];
+    const float f = grad_bound(largest) * (1.0f / kGradTop) * scale * (fp32 ? 1.0f / range_scale(largest->points) : 1.0f);
+    out[(i / d) * ld + i % d] = from_f32<T>(s * f);
 }
 
 template <class T>
-__global__ void grad_zero_kernel(T *__restrict__ out, int64_t rows, int d, int64_t ld)
+__global__ __launch_bounds__(256) void grad_zero_kernel(T *__restrict__ out, int64_t rows, int d, int64_t ld)
 {
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-        for (int c = threadIdx.x; c < d; c += blockDim.x) out[r * ld + c] = T{};
+        for (int c = threadIdx.x; c < d; c += 256) out[r * ld + c] = T{};
 }
 
-struct ProbGradScratch { float2 *coef; float *dq, *G; size_t bytes; int64_t part; };
+constexpr int kGradGroups = 512;                  // two workgroups a compute unit
+constexpr size_t kGradBytes = (size_t)256 << 20;  // most that G of a part takes where a part has more than the least rows
 
-static ProbGradScratch prob_grad_scratch(int64_t n, int d, int nq, void *base)
+struct ProbGradScratch {
+    bool pack;
+    int planes, width, qw, splits, q_tiles, d_tiles; // width: of packed rows and queries; qw: of G^T and of the transposed queries
+    int64_t part, x_plane, q_plane, qt_plane, g_plane;
+    Largest *largest; float2 *coef; float *sums; uint16_t *q16, *qt16, *x16, *G;
+    size_t bytes;
+};
+
+static ProbGradScratch prob_grad_scratch(const ProbGradParams &p, void *base)
 {
     ProbGradScratch s{};
-    s.part = std::max<int64_t>(64, std::min<int64_t>((n + 63) / 64 * 64, ((int64_t)64 << 20) / nq / 64 * 64));
+    s.planes = p.type == AVQ_F32 ? 2 : 1;
+    s.width = (p.d + kTileN - 1) / kTileN * kTileN; // (the product over rows reads whole tiles of columns)
+    s.qw = (p.nq + 31) / 32 * 32;
+    // (base == NULL: the size for rows that need packing, whatever their place and stride)
+    s.pack = !base || p.type == AVQ_F32 || s.width != p.d || (uintptr_t)p.points % 16 != 0 || p.ld_points % 8 != 0;
+    const int64_t most = (int64_t)(kGradBytes / (2 * s.planes * (size_t)s.qw)) / kTileM * kTileM;
+    s.part = std::min<int64_t>((p.n + kTileM - 1) / kTileM * kTileM, std::max<int64_t>(4096, most));
+    s.q_tiles = (p.nq + kTileM - 1) / kTileM;
+    s.d_tiles = (p.d + kTileN - 1) / kTileN;
+    s.splits = parts_for(std::max<int64_t>(1, s.part / (4 * kTileK)), s.q_tiles * s.d_tiles, kGradGroups);
     size_t at = 0;
     auto take = [&](size_t bytes) {
-        void *p = base ? (char *)base + at : nullptr;
+        void *q = base ? (char *)base + at : nullptr;
         at += (bytes + 255) & ~(size_t)255;
-        return p;
+        return q;
     };
-    s.coef = (float2 *)take(sizeof(float2) * (size_t)nq);
-    s.dq = (float *)take(sizeof(float) * (size_t)nq * d);
-    s.G = (float *)take(sizeof(float) * (size_t)nq * s.part);
+    s.largest = (Largest *)take(sizeof(Largest));
+    s.coef = (float2 *)take(sizeof(float2) * (size_t)p.nq);
+    s.sums = (float *)take(sizeof(float) * (size_t)s.splits * p.nq * p.d);
+    s.q_plane = (int64_t)p.nq * s.width;
+    s.q16 = (uint16_t *)take((size_t)s.q_plane * 2 * s.planes);
+    s.qt_plane = (int64_t)p.d * s.qw;
+    s.qt16 = (uint16_t *)take((size_t)s.qt_plane * 2 * s.planes);
+    s.g_plane = s.part * s.qw;
+    s.G = (uint16_t *)take((size_t)s.g_plane * 2 * s.planes);
+    s.x_plane = s.part * s.width;
+    if (s.pack) s.x16 = (uint16_t *)take((size_t)s.x_plane * 2 * s.planes);
     s.bytes = at;
     return s;
 }
 
 size_t log_probs_grad_scratch_bytes(int type, int64_t n, int d, int nq, int given)
 {
-    (void)type; (void)given;
-    return nq == 0 ? 0 : prob_grad_scratch(n, d, nq, nullptr).bytes;
+    (void)given;
+    ProbGradParams p{};
+    p.type = type; p.n = n; p.d = d; p.nq = nq;
+    return nq == 0 ? 0 : prob_grad_scratch(p, nullptr).bytes;
 }
 
-template <class T>
+template <class T, class H, int TERMS>
 static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
 {
     if (p.nq == 0) {
@@ -147,31 +307,61 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         }
         return AVQ_OK;
     }
-    const ProbGradScratch s = prob_grad_scratch(p.n, p.d, p.nq, p.scratch);
-    grad_coef_kernel<<<dim3((p.nq + 255) / 256), dim3(256), 0, st>>>(p.ids, p.n, p.nq, p.given, p.grad_logp, p.grad_entropy, p.entropy, p.grad_lse, s.coef);
+    const ProbGradScratch s = prob_grad_scratch(p, p.scratch);
+    static LdsLimitOnce once[5];
+    AVQ_TRY(set_lds_limit((const void *)grad_tile_kernel<T, H, TERMS, false>, kTileLds, &once[0]));
+    AVQ_TRY(set_lds_limit((const void *)grad_tile_kernel<T, H, TERMS, true>, kTileLds, &once[1]));
+    AVQ_TRY(set_lds_limit((const void *)grad_rows_kernel<T, H, TERMS, false>, kTileLds, &once[2]));
+    AVQ_TRY(set_lds_limit((const void *)grad_rows_kernel<T, H, TERMS, true>, kTileLds, &once[4]));
+    AVQ_TRY(set_lds_limit((const void *)grad_queries_kernel<H, TERMS>, kTileLds, &once[3]));
+    const float c2 = p.scale * 1.44269504088896341f;
+    const T *q = (const T *)p.queries;
+    AVQ_TRY(launch_clear_largest(s.largest, st));
+    grad_coef_kernel<<<dim3((p.nq + 255) / 256), dim3(256), 0, st>>>(p.ids, p.n, p.nq, p.given, p.grad_logp, p.grad_entropy, p.entropy, p.grad_lse, s.coef, s.largest);
     AVQ_HIP(hipGetLastError());
-    const unsigned qt = (p.nq + 63) / 64, dt = (p.d + 63) / 64;
+    if (TERMS > 1) {
+        AVQ_TRY(launch_largest((const float *)p.points, p.n, p.d, p.ld_points, &s.largest->points, st));
+        AVQ_TRY(launch_largest((const float *)p.queries, p.nq, p.d, p.ld_queries, &s.largest->queries, st));
+    }
+    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, p.nq, s.width, s.q16, s.q_plane, &s.largest->queries, nullptr, false, st));
+    if (p.dpoints) AVQ_TRY(launch_pack_transposed(p.queries, p.type, p.nq, p.d, p.ld_queries, p.d, s.qw, s.qt16, s.qt_plane, &s.largest->queries, st));
+    const Rows16 Q{s.q16, s.width, s.q_plane, p.nq}, Qt{s.qt16, s.qw, s.qt_plane, p.d};
     for (int64_t lo = 0; lo < p.n; lo += s.part) {
-        const int64_t rows = std::min<int64_t>(s.part, p.n - lo);
-        const unsigned rt = (unsigned)((rows + 63) / 64);
-        const T *x = (const T *)p.points + lo * p.ld_points, *q = (const T *)p.queries;
-        grad_logits_kernel<T><<<dim3(rt, qt), dim3(256), 0, st>>>(q, p.nq, p.ld_queries, x, rows, p.ld_points, p.d, p.scale, p.lse, s.coef, s.G);
+        const int64_t rows = std::min<int64_t>(s.part, p.n - lo), whole = (rows + kTileN - 1) / kTileN * kTileN; // rows past the last have G = 0
+        const T *x = (const T *)p.points + lo * p.ld_points;
+        Rows16 X{(const uint16_t *)x, p.ld_points, 0, rows};
+        if (s.pack) {
+            AVQ_TRY(launch_pack_rows(x, p.type, rows, p.d, p.ld_points, rows, s.width, s.x16, s.x_plane, &s.largest->points, nullptr, false, st));
+            X = Rows16{s.x16, s.width, s.x_plane, rows};
+        }
+        const Rows16 G{s.G, s.qw, s.g_plane, whole};
+        const int parts = parts_for((rows + kTileN - 1) / kTileN, s.q_tiles, kGradGroups);
+        const dim3 grid((unsigned)(parts * s.q_tiles));
+        if (p.grad_entropy) grad_tile_kernel<T, H, TERMS, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, (p.d + 15) / 16, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, s.g_plane);
+        else grad_tile_kernel<T, H, TERMS, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, (p.d + 15) / 16, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, s.g_plane);
         AVQ_HIP(hipGetLastError());
         if (p.given > 0) {
-            grad_given_kernel<<<dim3((unsigned)(((int64_t)p.nq * p.given + 255) / 256)), dim3(256), 0, st>>>(p.ids, p.nq, p.given, p.grad_logp, lo, rows, s.G);
-            AVQ_HIP(hipGetLastError());
-        }
-        if (p.dqueries) {
-            grad_queries_kernel<T><<<dim3(dt, qt), dim3(256), 0, st>>>(s.G, x, rows, p.ld_points, p.nq, p.d, lo == 0, s.dq);
+            grad_given_kernel<T><<<dim3((unsigned)(((int64_t)p.nq * p.given + 3) / 4)), dim3(256), 0, st>>>((const T *)p.points, p.ld_points, q, p.nq, p.ld_queries, p.d, p.scale, p.ids, p.given,
+                                                                                                        p.grad_logp, p.lse, s.coef, s.largest, lo, rows, s.G, s.qw, s.g_plane);
             AVQ_HIP(hipGetLastError());
         }
         if (p.dpoints) {
-            grad_rows_kernel<T><<<dim3(rt, dt), dim3(256), 0, st>>>(s.G, q, p.nq, p.ld_queries, rows, p.d, p.scale, p.accumulate, (T *)p.dpoints + lo * p.ld_dpoints, p.ld_dpoints);
+            const int row_parts = parts_for((rows + kTileM - 1) / kTileM, s.d_tiles, kGradGroups);
+            const dim3 row_grid((unsigned)(row_parts * s.d_tiles));
+            T *dx = (T *)p.dpoints + lo * p.ld_dpoints;
+            if (p.accumulate) grad_rows_kernel<T, H, TERMS, true><<<row_grid, dim3(kTileThreads), kTileLds, st>>>(G, Qt, (p.nq + 15) / 16, p.scale, s.largest, row_parts, s.d_tiles, rows, p.d, dx, p.ld_dpoints);
+            else grad_rows_kernel<T, H, TERMS, false><<<row_grid, dim3(kTileThreads), kTileLds, st>>>(G, Qt, (p.nq + 15) / 16, p.scale, s.largest, row_parts, s.d_tiles, rows, p.d, dx, p.ld_dpoints);
+            AVQ_HIP(hipGetLastError());
+        }
+        if (p.dqueries) {
+            grad_queries_kernel<H, TERMS><<<dim3((unsigned)(s.splits * s.q_tiles * s.d_tiles)), dim3(kTileThreads), kTileLds, st>>>(G, X, p.nq, s.qw, p.d, s.splits, s.q_tiles, s.d_tiles,
+                                                                                                                             lo == 0, s.sums);
             AVQ_HIP(hipGetLastError());
         }
     }
     if (p.dqueries) {
-        grad_round_kernel<T><<<dim3((unsigned)(((int64_t)p.nq * p.d + 255) / 256)), dim3(256), 0, st>>>(s.dq, p.nq, p.d, p.scale, (T *)p.dqueries, p.ld_dqueries);
+        grad_join_kernel<T><<<dim3((unsigned)(((int64_t)p.nq * p.d + 255) / 256)), dim3(256), 0, st>>>(s.sums, s.splits, p.nq, p.d, p.scale, TERMS > 1, s.largest, (T *)p.dqueries,
+                                                                                                   p.ld_dqueries);
         AVQ_HIP(hipGetLastError());
     }
     return AVQ_OK;
@@ -179,8 +369,8 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
 
 int launch_log_probs_grad(const ProbGradParams &p, hipStream_t st)
 {
-    if (p.type == AVQ_F32) return log_probs_grad_typed<float>(p, st);
-    return p.type == AVQ_BF16 ? log_probs_grad_typed<bf16_t>(p, st) : log_probs_grad_typed<f16_t>(p, st);
+    if (p.type == AVQ_F32) return log_probs_grad_typed<float, f16_t, 3>(p, st);
+    return p.type == AVQ_BF16 ? log_probs_grad_typed<bf16_t, bf16_t, 1>(p, st) : log_probs_grad_typed<f16_t, f16_t, 1>(p, st);
 }
 
 } // namespace avq
