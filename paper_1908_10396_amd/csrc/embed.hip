@@ -80,16 +80,45 @@ int launch_embed(const EmbedParams &p, hipStream_t st)
 
 // Least significant digit first, digits of up to 11 bits; ids outside [0, n) get the key n and so come last. A workgroup
 // takes kSortTile entries; a wave ranks 64 entries at a time among their equals by comparing digits bit by bit, in order,
-// so that the sort is stable.
+// so that the sort is stable. All of it is latency: the launches also clear the table's rows, which needs none of it (FillJob).
 constexpr int kSortThreads = 256, kSortEach = 8, kSortTile = kSortThreads * kSortEach, kSortWaves = kSortThreads / 64;
 constexpr int kMaxBins = 2048;
+constexpr int kSortDirect = 4; // up to so many tiles every tile adds up the counts of the tiles itself, beyond a launch does (25 tiles: 40 against 5 us)
 
 __device__ __forceinline__ uint32_t key_of(int32_t id, uint32_t n) { return (uint32_t)id < n ? (uint32_t)id : n; }
 
-// hist[digit][tile]
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t *__restrict__ ids, const uint32_t *__restrict__ keys, uint32_t count, uint32_t n,
-                                                                  int shift, int bins, uint32_t *__restrict__ hist, int tiles)
+// Rows [lo, hi) of the table to be cleared by the workgroups of a launch beyond its own ones; 16, 8, 4 or 2 bytes at a time.
+struct FillJob { char *out; int64_t lo, hi, ld, row_bytes; int32_t width; };
+
+template <int W> __device__ __forceinline__ void fill_rows(const FillJob &f, int group, int groups)
 {
+    typedef Pack<uint16_t, W / 2> Unit;
+    const int64_t step = (int64_t)groups * blockDim.x;
+    if (f.ld == f.row_bytes) { // dense rows are one long row
+        char *from = f.out + f.lo * f.ld;
+        const int64_t units = (f.hi - f.lo) * f.row_bytes / W;
+        for (int64_t i = (int64_t)group * blockDim.x + threadIdx.x; i < units; i += step) *(Unit *)(from + i * W) = Unit{};
+    } else {
+        for (int64_t r = f.lo + group; r < f.hi; r += groups)
+            for (int64_t c = threadIdx.x; c < f.row_bytes / W; c += blockDim.x) *(Unit *)(f.out + r * f.ld + c * W) = Unit{};
+    }
+}
+
+__device__ __forceinline__ void fill_rows(const FillJob &f, int group, int groups)
+{
+    if (f.width == 16) fill_rows<16>(f, group, groups);
+    else if (f.width == 8) fill_rows<8>(f, group, groups);
+    else if (f.width == 4) fill_rows<4>(f, group, groups);
+    else fill_rows<2>(f, group, groups);
+}
+
+__global__ __launch_bounds__(256) void fill_rows_kernel(FillJob fill) { fill_rows(fill, blockIdx.x, gridDim.x); }
+
+// hist[tile][digit]
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t *__restrict__ ids, const uint32_t *__restrict__ keys, uint32_t count, uint32_t n,
+                                                                  int shift, int bins, uint32_t *__restrict__ hist, int tiles, FillJob fill)
+{
+    if ((int)blockIdx.x >= tiles) { fill_rows(fill, blockIdx.x - tiles, gridDim.x - tiles); return; }
     __shared__ uint32_t h[kMaxBins];
     for (int b = threadIdx.x; b < bins; b += kSortThreads) h[b] = 0;
     __syncthreads();
@@ -103,61 +132,86 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t 
         }
     }
     __syncthreads();
-    for (int b = threadIdx.x; b < bins; b += kSortThreads) hist[(size_t)b * tiles + blockIdx.x] = h[b];
+    for (int b = threadIdx.x; b < bins; b += kSortThreads) hist[(size_t)blockIdx.x * bins + b] = h[b];
 }
 
-// Exclusive sums of `total` counters in place, by one workgroup.
-__global__ __launch_bounds__(1024) void sort_scan_kernel(uint32_t *__restrict__ hist, int total)
+// Many tiles: each digit's counts become the counts of the tiles before, and totals[digit] their sum. A thread a digit.
+__global__ __launch_bounds__(64) void sort_sums_kernel(uint32_t *__restrict__ hist, int bins, int tiles, uint32_t *__restrict__ totals)
 {
-    __shared__ uint32_t wave_sum[16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t before = 0;
-    for (int base = 0; base < total; base += 4096) {
-        const int at = base + 4 * (int)threadIdx.x;
-        uint32_t c[4];
+    const int b = blockIdx.x * 64 + threadIdx.x;
+    if (b >= bins) return;
+    uint32_t run = 0;
+    for (int t0 = 0; t0 < tiles; t0 += 16) {
+        uint32_t c[16];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c[e] = at + e < total ? hist[at + e] : 0u;
-        const uint32_t mine = c[0] + c[1] + c[2] + c[3];
-        uint32_t incl = mine;
-        for (int m = 1; m < 64; m <<= 1) {
-            const uint32_t o = (uint32_t)__shfl_up((int)incl, m, 64);
-            if (lane >= m) incl += o;
-        }
-        if (lane == 63) wave_sum[wave] = incl;
-        __syncthreads();
-        uint32_t waves_before = 0, all = 0;
-        for (int w = 0; w < 16; ++w) {
-            if (w < wave) waves_before += wave_sum[w];
-            all += wave_sum[w];
-        }
-        uint32_t run = before + waves_before + incl - mine;
+        for (int u = 0; u < 16; ++u) c[u] = t0 + u < tiles ? hist[(size_t)(t0 + u) * bins + b] : 0u;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (at + e < total) hist[at + e] = run;
-            run += c[e];
+        for (int u = 0; u < 16; ++u) {
+            if (t0 + u < tiles) hist[(size_t)(t0 + u) * bins + b] = run;
+            run += c[u];
         }
-        before += all;
-        __syncthreads();
     }
+    totals[b] = run;
 }
 
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t *__restrict__ ids, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos,
-                                                                  uint32_t count, uint32_t n, int shift, int bits, const uint32_t *__restrict__ offsets, int tiles,
-                                                                  uint32_t *__restrict__ keys_out, uint32_t *__restrict__ pos_out)
+                                                                  uint32_t count, uint32_t n, int shift, int bits, const uint32_t *__restrict__ hist,
+                                                                  const uint32_t *__restrict__ totals, int tiles, uint32_t *__restrict__ keys_out, uint32_t *__restrict__ pos_out,
+                                                                  FillJob fill)
 {
+    if ((int)blockIdx.x >= tiles) { fill_rows(fill, blockIdx.x - tiles, gridDim.x - tiles); return; }
     // a wave's 512 entries lie side by side; [wave][digit]: first its counts, then where its next entry of the digit goes
     __shared__ uint32_t next[kSortWaves][kMaxBins];
+    __shared__ uint32_t wave_sum[kSortWaves];
     const int bins = 1 << bits;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int b = threadIdx.x; b < kSortWaves * kMaxBins; b += kSortThreads) (&next[0][0])[b] = 0;
+    // of this thread's digits: entries in earlier tiles, in all
+    constexpr int kPer = kMaxBins / kSortThreads;
+    const int per = bins / kSortThreads > 0 ? bins / kSortThreads : 1, b0 = threadIdx.x * per; // (threads past the digits have none)
+    uint32_t earlier[kPer], all[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) earlier[j] = all[j] = 0;
+    if (b0 < bins) {
+        if (totals) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (j < per) {
+                    earlier[j] = hist[(size_t)blockIdx.x * bins + b0 + j];
+                    all[j] = totals[b0 + j];
+                }
+        } else {
+            for (int t = 0; t < tiles; ++t)
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (j < per) {
+                        const uint32_t c = hist[(size_t)t * bins + b0 + j];
+                        if (t < (int)blockIdx.x) earlier[j] += c;
+                        all[j] += c;
+                    }
+        }
+    }
+    uint32_t mine = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) mine += all[j];
+    uint32_t incl = mine;
+    for (int m = 1; m < 64; m <<= 1) {
+        const uint32_t o = (uint32_t)__shfl_up((int)incl, m, 64);
+        if (lane >= m) incl += o;
+    }
+    if (lane == 63) wave_sum[wave] = incl;
     __syncthreads();
     const uint32_t first = blockIdx.x * (uint32_t)kSortTile + (uint32_t)(wave * 64 * kSortEach);
-    uint32_t key[kSortEach], rank[kSortEach];
+    uint32_t key[kSortEach], from[kSortEach], rank[kSortEach];
 #pragma unroll
     for (int u = 0; u < kSortEach; ++u) {
         const uint32_t i = first + (uint32_t)(u * 64 + lane);
-        const bool real = i < count;
-        key[u] = real ? (ids ? key_of(ids[i], n) : keys[i]) : 0u;
+        key[u] = i < count ? (ids ? key_of(ids[i], n) : keys[i]) : 0u;
+        from[u] = i < count ? (pos ? pos[i] : i) : 0u;
+    }
+#pragma unroll
+    for (int u = 0; u < kSortEach; ++u) {
+        const bool real = first + (uint32_t)(u * 64 + lane) < count;
         const uint32_t digit = (key[u] >> shift) & (uint32_t)(bins - 1);
         u64 same = __ballot(real);
         for (int b = 0; b < bits; ++b) {
@@ -175,23 +229,28 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t 
         __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
-    for (int b = threadIdx.x; b < bins; b += kSortThreads) {
-        uint32_t run = offsets[(size_t)b * tiles + blockIdx.x];
-        for (int w = 0; w < kSortWaves; ++w) {
-            const uint32_t c = next[w][b];
-            next[w][b] = run;
-            run += c;
+    if (b0 < bins) {
+        uint32_t run = incl - mine;
+        for (int w = 0; w < wave; ++w) run += wave_sum[w];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            if (j >= per) break;
+            uint32_t to = run + earlier[j];
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t c = next[w][b0 + j];
+                next[w][b0 + j] = to;
+                to += c;
+            }
+            run += all[j];
         }
     }
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < kSortEach; ++u) {
-        const uint32_t i = first + (uint32_t)(u * 64 + lane);
-        if (i < count) {
-            const uint32_t to = next[wave][(key[u] >> shift) & (uint32_t)(bins - 1)] + rank[u];
-            keys_out[to] = key[u];
-            pos_out[to] = pos ? pos[i] : i;
-        }
+        if (first + (uint32_t)(u * 64 + lane) >= count) continue;
+        const uint32_t to = next[wave][(key[u] >> shift) & (uint32_t)(bins - 1)] + rank[u];
+        keys_out[to] = key[u];
+        pos_out[to] = from[u];
     }
 }
 
@@ -209,17 +268,26 @@ __device__ __forceinline__ void write_row(T *__restrict__ row, uint32_t col, con
     *(Pack<T, V> *)(row + (size_t)col * V) = o;
 }
 
-// Each group of `lanes` threads takes a chunk of kRunChunk sorted entries. A run that lies within the chunk goes to its
+// Each team of `lanes` threads takes a chunk of kRunChunk sorted entries. A run that lies within the chunk goes to its
 // row; what belongs to a run that crosses the chunk's start or end goes to partial[chunk][0] or [1] (a run through the
-// whole chunk: [0]).
+// whole chunk: [0]). The rows of eight entries are asked for while the eight before are added up.
 template <class T, int V>
 __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ grad, int64_t ld_grad, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos,
                                                        uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out, int64_t ld_out, int accumulate,
                                                        float *__restrict__ partial)
 {
-    const uint32_t chunk = blockIdx.x * (256u / (uint32_t)lanes) + threadIdx.x / (uint32_t)lanes;
-    const uint32_t begin = chunk * (uint32_t)kRunChunk;
+    constexpr int kTeams = 64; // of 4 lanes, at most
+    __shared__ uint32_t skeys[kTeams * kRunChunk], spos[kTeams * kRunChunk];
+    const uint32_t teams = 256u / (uint32_t)lanes, team = threadIdx.x / (uint32_t)lanes;
+    const uint32_t all_begin = blockIdx.x * teams * (uint32_t)kRunChunk;
+    for (uint32_t i = threadIdx.x; i < teams * (uint32_t)kRunChunk; i += 256) {
+        skeys[i] = all_begin + i < count ? keys[all_begin + i] : n; // (n: nothing to add)
+        spos[i] = all_begin + i < count ? pos[all_begin + i] : 0u;
+    }
+    __syncthreads();
+    const uint32_t chunk = blockIdx.x * teams + team, begin = chunk * (uint32_t)kRunChunk;
     if (begin >= count) return;
+    const uint32_t *ks = skeys + team * kRunChunk, *ps = spos + team * kRunChunk;
     const uint32_t end = min(count, begin + (uint32_t)kRunChunk);
     const uint32_t per_row = (uint32_t)d / V;
     const uint32_t before = begin > 0 ? keys[begin - 1] : 0xffffffffu; // (no key is that)
@@ -228,99 +296,123 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
         float acc[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] = 0.0f;
-        uint32_t key = keys[begin];
+        uint32_t key = ks[0];
         bool from_start = true;
         constexpr int kAhead = 8;
-        for (uint32_t i0 = begin; i0 < end; i0 += kAhead) {
-            Pack<T, V> v[kAhead];
-            uint32_t k[kAhead];
+        struct Rows { Pack<T, V> v[kAhead]; };
+        const T *from = grad + (int64_t)col * V;
+        auto ask = [&](Rows &r, int i0) __attribute__((always_inline)) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const uint32_t i = min(i0 + (uint32_t)u, end - 1);
-                k[u] = keys[i];
-                v[u] = Pack<T, V>{};
-                if (k[u] < n) v[u] = *(const Pack<T, V> *)(grad + (int64_t)pos[i] * ld_grad + (int64_t)col * V);
+                r.v[u] = Pack<T, V>{};
+                if (ks[i0 + u] < n) r.v[u] = *(const Pack<T, V> *)(from + (int64_t)ps[i0 + u] * ld_grad);
             }
+        };
+        auto partial_row = [&](int slot) __attribute__((always_inline)) {
+            Pack<float, V> o;
+#pragma unroll
+            for (int e = 0; e < V; ++e) o.e[e] = acc[e];
+            float *to = partial + ((size_t)chunk * 2 + slot) * d + (size_t)col * V;
+            __builtin_memcpy(to, &o, sizeof(o));
+        };
+        auto add = [&](const Rows &r, int i0) __attribute__((always_inline)) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                if (i0 + (uint32_t)u >= end) break;
-                if (k[u] != key) {
+                const uint32_t next = ks[i0 + u];
+                if (next != key) {
                     if (key < n) {
-                        if (from_start && key == before) {
-#pragma unroll
-                            for (int e = 0; e < V; ++e) partial[((size_t)chunk * 2) * d + (size_t)col * V + e] = acc[e];
-                        } else {
-                            write_row<T, V>(out + (int64_t)key * ld_out, col, acc, scale, accumulate != 0);
-                        }
+                        if (from_start && key == before) partial_row(0);
+                        else write_row<T, V>(out + (int64_t)key * ld_out, col, acc, scale, accumulate != 0);
                     }
                     from_start = false;
-                    key = k[u];
+                    key = next;
 #pragma unroll
                     for (int e = 0; e < V; ++e) acc[e] = 0.0f;
                 }
 #pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] += to_f32(v[u].e[e]);
+                for (int e = 0; e < V; ++e) acc[e] += to_f32(r.v[u].e[e]);
             }
-        }
-        if (key >= n) continue;
+        };
+        static_assert(kRunChunk == 4 * kAhead, "two pairs of eights");
+        Rows here, next;
+        ask(here, 0);
+        ask(next, kAhead);
+        add(here, 0);
+        ask(here, 2 * kAhead);
+        add(next, kAhead);
+        ask(next, 3 * kAhead);
+        add(here, 2 * kAhead);
+        add(next, 3 * kAhead);
+        if (key >= n) continue; // (the last chunk's entries past the end have the key n)
         const bool open_start = from_start && key == before;
-        if (open_start || key == after) {
-            const size_t slot = (size_t)chunk * 2 + (open_start ? 0 : 1);
-#pragma unroll
-            for (int e = 0; e < V; ++e) partial[slot * d + (size_t)col * V + e] = acc[e];
-        } else {
-            write_row<T, V>(out + (int64_t)key * ld_out, col, acc, scale, accumulate != 0);
-        }
+        if (open_start || key == after) partial_row(open_start ? 0 : 1);
+        else write_row<T, V>(out + (int64_t)key * ld_out, col, acc, scale, accumulate != 0);
     }
 }
 
-// The runs that cross chunks: the group whose chunk such a run begins in adds up its parts in order.
+// The runs that cross chunks: each by the workgroup that has the chunk which it begins in. Teams of `lanes` threads add up a share
+// of the chunks each, in order, and then the shares in order.
+constexpr int kJoinThreads = 512;
+
 template <class T, int V>
-__global__ __launch_bounds__(256) void run_joins_kernel(const uint32_t *__restrict__ keys, uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out,
-                                                        int64_t ld_out, int accumulate, const float *__restrict__ partial)
+__global__ __launch_bounds__(kJoinThreads) void run_joins_kernel(const uint32_t *__restrict__ keys, uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out,
+                                                                 int64_t ld_out, int accumulate, const float *__restrict__ partial)
 {
-    const uint32_t chunk = blockIdx.x * (256u / (uint32_t)lanes) + threadIdx.x / (uint32_t)lanes;
+    __shared__ float shares[kJoinThreads * V];
+    const uint32_t chunks = (count + kRunChunk - 1) / kRunChunk, per_row = (uint32_t)d / V;
+    const uint32_t teams = kJoinThreads / (uint32_t)lanes, team = threadIdx.x / (uint32_t)lanes, lane = threadIdx.x % (uint32_t)lanes;
+    const uint32_t chunk = blockIdx.x;
     const uint32_t begin = chunk * (uint32_t)kRunChunk, end = begin + (uint32_t)kRunChunk;
     if (end >= count) return; // the last chunk's runs end in it
     const uint32_t key = keys[end - 1];
     if (key >= n || keys[end] != key) return;
     if (keys[begin] == key && begin > 0 && keys[begin - 1] == key) return; // it began earlier
     // the chunks that the run goes on in: those whose first entry has the key
-    uint32_t lo = chunk + 1, hi = (count + kRunChunk - 1) / kRunChunk; // first chunk of another key lies in (lo, hi]
+    uint32_t lo = chunk + 1, hi = min(chunks, lo + 1); // the first chunk of another key lies in (lo, hi]
+    while (hi < chunks && keys[hi * (uint32_t)kRunChunk] == key) {
+        const uint32_t step = 2 * (hi - chunk);
+        lo = hi;
+        hi = min(chunks, chunk + step);
+    }
     while (lo + 1 < hi) {
         const uint32_t mid = lo + (hi - lo) / 2;
         if (keys[mid * (uint32_t)kRunChunk] == key) lo = mid; else hi = mid;
     }
-    const uint32_t last = lo;
-    const uint32_t per_row = (uint32_t)d / V;
-    for (uint32_t col = threadIdx.x % (uint32_t)lanes; col < per_row; col += (uint32_t)lanes) {
-        float acc[V];
+    const uint32_t more = lo - chunk; // chunk + 1 .. lo
+    const uint32_t used = min(teams, (more + 3) / 4); // (four chunks a team at least)
+    for (uint32_t c0 = 0; c0 < per_row; c0 += (uint32_t)lanes) {
+        const uint32_t col = c0 + lane;
+        if (team < used && col < per_row) {
+            float acc[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] = partial[((size_t)chunk * 2 + 1) * d + (size_t)col * V + e];
-#pragma unroll 8
-        for (uint32_t c = chunk + 1; c <= last; ++c) {
+            for (int e = 0; e < V; ++e) acc[e] = team == 0 ? partial[((size_t)chunk * 2 + 1) * d + (size_t)col * V + e] : 0.0f;
+            const uint32_t from = chunk + 1 + more * team / used, to = chunk + 1 + more * (team + 1) / used;
+#pragma unroll 16
+            for (uint32_t c = from; c < to; ++c) {
+                Pack<float, V> v;
+                __builtin_memcpy(&v, partial + (size_t)c * 2 * d + (size_t)col * V, sizeof(v));
 #pragma unroll
-            for (int e = 0; e < V; ++e) acc[e] += partial[(size_t)c * 2 * d + (size_t)col * V + e];
+                for (int e = 0; e < V; ++e) acc[e] += v.e[e];
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) shares[(team * (uint32_t)lanes + lane) * V + e] = acc[e];
         }
-        write_row<T, V>(out + (int64_t)key * ld_out, col, acc, scale, accumulate != 0);
-    }
-}
-
-template <class T, int V>
-__global__ __launch_bounds__(256) void fill_rows_kernel(T *__restrict__ out, int64_t rows, int64_t ld, int per_row)
-{
-    // (dense rows are one long row)
-    const int64_t step = (int64_t)gridDim.x * 256;
-    if (ld == (int64_t)per_row * V) {
-        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * per_row; i += step) *(Pack<T, V> *)(out + i * V) = Pack<T, V>{};
-    } else {
-        for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-            for (int c = threadIdx.x; c < per_row; c += 256) *(Pack<T, V> *)(out + r * ld + (int64_t)c * V) = Pack<T, V>{};
+        __syncthreads();
+        if (team == 0 && col < per_row) {
+            float acc[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+            for (uint32_t t = 0; t < used; ++t)
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] += shares[(t * (uint32_t)lanes + lane) * V + e];
+            write_row<T, V>(out + (int64_t)key * ld_out, col, acc, scale, accumulate != 0);
+        }
+        __syncthreads();
     }
 }
 
 struct GradScratch {
-    uint32_t *keys[2], *pos[2], *hist;
+    uint32_t *keys[2], *pos[2], *hist, *totals;
     float *partial;
     size_t bytes;
     int passes, bits, tiles;
@@ -345,6 +437,7 @@ static GradScratch grad_scratch(int64_t n, int d, int64_t count, void *base)
         s.pos[i] = (uint32_t *)take(4 * (size_t)count);
     }
     s.hist = (uint32_t *)take(((size_t)4 << s.bits) * s.tiles);
+    s.totals = (uint32_t *)take((size_t)4 << s.bits);
     s.partial = (float *)take((size_t)((count + kRunChunk - 1) / kRunChunk) * 2 * d * sizeof(float));
     s.bytes = at;
     return s;
@@ -352,26 +445,46 @@ static GradScratch grad_scratch(int64_t n, int d, int64_t count, void *base)
 
 size_t embed_grad_scratch_bytes(int64_t n, int d, int64_t count) { return grad_scratch(n, d, count, nullptr).bytes; }
 
+constexpr int kFillGroups = 1024;
+
 template <class T, int V>
 static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
 {
-    if (!p.accumulate) {
-        fill_rows_kernel<T, V><<<dim3(2048), dim3(256), 0, st>>>((T *)p.out, p.n, p.ld_out, p.d / V);
+    FillJob fill{(char *)p.out, 0, p.accumulate ? 0 : p.n, p.ld_out * (int64_t)sizeof(T), p.d * (int64_t)sizeof(T), V * (int)sizeof(T)};
+    if (p.count == 0) {
+        if (p.accumulate) return AVQ_OK;
+        fill_rows_kernel<<<dim3(kFillGroups), dim3(256), 0, st>>>(fill);
         AVQ_HIP(hipGetLastError());
+        return AVQ_OK;
     }
-    if (p.count == 0) return AVQ_OK;
     const GradScratch s = grad_scratch(p.n, p.d, p.count, p.scratch);
     const uint32_t count = (uint32_t)p.count, n = (uint32_t)p.n;
     const int bins = 1 << s.bits;
+    // a share of the rows to be cleared with each launch of the sort
+    const int launches = 2 * s.passes;
+    const bool filling = !p.accumulate;
+    int launch = 0;
+    auto share = [&]() {
+        FillJob f = fill;
+        f.lo = fill.hi * launch / launches;
+        f.hi = fill.hi * (launch + 1) / launches;
+        ++launch;
+        return f;
+    };
+    const int groups = s.tiles + (filling ? kFillGroups : 0);
     const uint32_t *keys = nullptr, *pos = nullptr;
     for (int pass = 0; pass < s.passes; ++pass) {
         const int32_t *ids = pass == 0 ? p.ids : nullptr;
         const int to = pass & 1;
-        sort_count_kernel<<<dim3(s.tiles), dim3(kSortThreads), 0, st>>>(ids, keys, count, n, pass * s.bits, bins, s.hist, s.tiles);
+        sort_count_kernel<<<dim3(groups), dim3(kSortThreads), 0, st>>>(ids, keys, count, n, pass * s.bits, bins, s.hist, s.tiles, share());
         AVQ_HIP(hipGetLastError());
-        sort_scan_kernel<<<dim3(1), dim3(1024), 0, st>>>(s.hist, bins * s.tiles);
-        AVQ_HIP(hipGetLastError());
-        sort_place_kernel<<<dim3(s.tiles), dim3(kSortThreads), 0, st>>>(ids, keys, pos, count, n, pass * s.bits, s.bits, s.hist, s.tiles, s.keys[to], s.pos[to]);
+        const bool direct = s.tiles <= kSortDirect;
+        if (!direct) {
+            sort_sums_kernel<<<dim3((bins + 63) / 64), dim3(64), 0, st>>>(s.hist, bins, s.tiles, s.totals);
+            AVQ_HIP(hipGetLastError());
+        }
+        sort_place_kernel<<<dim3(groups), dim3(kSortThreads), 0, st>>>(ids, keys, pos, count, n, pass * s.bits, s.bits, s.hist, direct ? nullptr : s.totals, s.tiles, s.keys[to],
+                                                                       s.pos[to], share());
         AVQ_HIP(hipGetLastError());
         keys = s.keys[to];
         pos = s.pos[to];
@@ -382,7 +495,7 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
     const dim3 grid((unsigned)((chunks + 256 / lanes - 1) / (256 / lanes)));
     run_sums_kernel<T, V><<<grid, dim3(256), 0, st>>>((const T *)p.grad, p.ld_grad, keys, pos, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
     AVQ_HIP(hipGetLastError());
-    run_joins_kernel<T, V><<<grid, dim3(256), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
+    run_joins_kernel<T, V><<<dim3((unsigned)chunks), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }

@@ -4,6 +4,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "avq_internal.h"
 
 namespace avq {
@@ -21,9 +23,13 @@ __device__ __forceinline__ Stat join(const Stat &a, const Stat &b)
     return Stat{m, a.l * fa + b.l * fb, fa * __fmaf_rn(a.l, da, a.t) + fb * __fmaf_rn(b.l, db, b.t)};
 }
 
-// Dynamic LDS of the kernel that finishes a query: the query in fp32, the keys of 32 rows for each of the k best groups, the
-// k best of them, the groups.
+// Dynamic LDS of the kernel that finishes a query: the query in fp32; candidate groups, then the keys of 32 rows for each of the k
+// best groups; the k best of them; the groups.
 constexpr size_t kFinishLds = kMaxDynLds - 16 * 1024;
-inline size_t finish_lds(int d, int k) { return (((size_t)d * 4 + 15) & ~(size_t)15) + (size_t)k * (32 * 8 + 8 + 4); }
+constexpr int kFinishList = 2048; // candidate groups that are kept (and room for a value of each of 1,024 threads)
+inline size_t finish_lds(int d, int k)
+{
+    return (((size_t)d * 4 + 15) & ~(size_t)15) + (k == 0 ? 0 : (size_t)std::max(32 * k, kFinishList) * 8 + (size_t)k * (8 + 4));
+}
 
 } // namespace avq

@@ -75,20 +75,58 @@ template <class T> __device__ __forceinline__ Frag negated(Frag f)
 // ---- a few queries: the rows streamed once -------------------------------------------------
 
 constexpr int kStreamThreads = 256, kStreamWaves = kStreamThreads / 64;
+constexpr int kStreamSteps = 8; // steps of a batch: 16 loads of 16 bytes a lane, of which the next batch's are in flight too
 
 // A wave takes 32 rows at a time, a query tile is QT x 16 queries. The rows' operands come straight from memory (a lane's 16
 // bytes are the matrix instruction's layout), the queries' from LDS, where they lie in the same order (QLDS), or from memory.
+// Bound by memory; a batch is asked for while the one before is multiplied.
 template <class T, int QT, bool ALIGNED, bool QLDS>
-__global__ __launch_bounds__(kStreamThreads) void prob_stream_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q,
-                                                                     float c2, int negate, float4 *__restrict__ stats, float *__restrict__ gmax, int64_t gstride)
+__global__ __launch_bounds__(kStreamThreads, 2) void prob_stream_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q,
+                                                                        float c2, int negate, float4 *__restrict__ stats, float *__restrict__ gmax, int64_t gstride)
 {
     extern __shared__ Frag qs[]; // [step][QT][64]
     __shared__ float4 joined[kStreamWaves][QT * 16];
-    constexpr int S = kStepElems<T>, E = kFragElems<T>;
+    constexpr int S = kStepElems<T>, E = kFragElems<T>, NB = kStreamSteps;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r16 = lane & 15, kg = lane >> 4;
     const int q0 = blockIdx.y * QT * 16;
     const int steps = (d + S - 1) / S;
+    // The last step's 16 bytes may run past the row's end, into what lies between it and the next row or into that: they are read all
+    // the same and masked; lanes whose bytes lie past the end altogether read the row's first. The tile that holds the last row, and
+    // rows shorter than 16 bytes, go by themselves.
+    const int k_last = (steps - 1) * S + kg * E, k_read = k_last < d ? k_last : 0;
+    uint32_t mask[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (sizeof(T) == 4) mask[w] = k_last + w < d ? ~0u : 0u;
+        else mask[w] = (k_last + 2 * w < d ? 0xffffu : 0u) | (k_last + 2 * w + 1 < d ? 0xffff0000u : 0u);
+    }
+    float m[QT], l[QT], t[QT];
+    f32x4 acc[2][QT];
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        m[i] = -INFINITY;
+        l[i] = t[i] = 0.0f;
+        acc[0][i] = acc[1][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    const int64_t tiles = (n + 31) / 32, whole_tiles = d >= E ? (n - 1) / 32 : 0, stride = (int64_t)gridDim.x * kStreamWaves;
+    const int batches = (steps + NB - 1) / NB;
+
+    struct Batch { Frag a[2][NB]; };
+    auto fetch = [&](Batch &f, int64_t tile, int batch) __attribute__((always_inline)) {
+        const T *p0 = x + (tile * 32 + r16) * ld_x, *p1 = p0 + 16 * ld_x;
+        const int s0 = batch * NB;
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+            if (s0 + u >= steps) break;
+            const int k = s0 + u == steps - 1 ? k_read : (s0 + u) * S + kg * E;
+            f.a[0][u] = load_whole<T, ALIGNED>(p0 + k);
+            f.a[1][u] = load_whole<T, ALIGNED>(p1 + k);
+        }
+    };
+    int64_t tile = (int64_t)blockIdx.x * kStreamWaves + wave;
+    Batch here, next;
+    if (tile < whole_tiles) fetch(here, tile, 0);
     if (QLDS) {
         for (int i = threadIdx.x; i < steps * QT * 64; i += kStreamThreads) {
             const int l = i & 63, t = (i >> 6) % QT, s = (i >> 6) / QT;
@@ -99,48 +137,35 @@ __global__ __launch_bounds__(kStreamThreads) void prob_stream_kernel(const T *__
         }
         __syncthreads();
     }
-    float m[QT], l[QT], t[QT];
+    auto multiply_step = [&](int s, const Frag &a0, const Frag &a1) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < QT; ++i) { m[i] = -INFINITY; l[i] = 0.0f; t[i] = 0.0f; }
-    const int64_t tiles = (n + 31) / 32;
-    const int64_t waves = (int64_t)gridDim.x * kStreamWaves;
-    for (int64_t tile = (int64_t)blockIdx.x * kStreamWaves + wave; tile < tiles; tile += waves) {
-        const int64_t r0 = tile * 32 + r16, r1 = r0 + 16;
-        const T *p0 = x + (r0 < n ? r0 : n - 1) * ld_x, *p1 = x + (r1 < n ? r1 : n - 1) * ld_x;
-        f32x4 acc[2][QT];
-#pragma unroll
-        for (int i = 0; i < QT; ++i) acc[0][i] = acc[1][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        auto step = [&](int s, const Frag &a0, const Frag &a1) {
-            const int k = s * S + kg * E;
-#pragma unroll
-            for (int i = 0; i < QT; ++i) {
-                Frag b{};
-                if (QLDS) {
-                    b = qs[(s * QT + i) * 64 + lane];
-                } else {
-                    const int row = q0 + i * 16 + r16;
-                    if (row < nq) b = load_frag<T, false>(q + (int64_t)row * ld_q, k, d);
-                    if (negate) b = negated<T>(b);
-                }
-                acc[0][i] = mma16(a0, b, acc[0][i], T{});
-                acc[1][i] = mma16(a1, b, acc[1][i], T{});
+        for (int i = 0; i < QT; ++i) {
+            Frag b{};
+            if (QLDS) {
+                b = qs[(s * QT + i) * 64 + lane];
+            } else {
+                const int row = q0 + i * 16 + r16;
+                if (row < nq) b = load_frag<T, false>(q + (int64_t)row * ld_q, s * S + kg * E, d);
+                if (negate) b = negated<T>(b);
             }
-        };
-        // whole steps, four of them asked for at a time
-        const int whole = d / S;
-        int s = 0;
-        for (; s + 4 <= whole; s += 4) {
-            Frag a[2][4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                a[0][u] = load_whole<T, ALIGNED>(p0 + (s + u) * S + kg * E);
-                a[1][u] = load_whole<T, ALIGNED>(p1 + (s + u) * S + kg * E);
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) step(s + u, a[0][u], a[1][u]);
+            acc[0][i] = mma16(a0, b, acc[0][i], T{});
+            acc[1][i] = mma16(a1, b, acc[1][i], T{});
         }
-        for (; s < steps; ++s) step(s, load_frag<T, ALIGNED>(p0, s * S + kg * E, d), load_frag<T, ALIGNED>(p1, s * S + kg * E, d));
-        // lane: query i * 16 + (lane & 15), rows 4 (lane >> 4) + 0 .. 3 of either half
+    };
+    auto multiply = [&](Batch &f, int batch) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+            const int s = batch * NB + u;
+            if (s >= steps) break;
+            if (s == steps - 1) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) { f.a[0][u].w[w] &= mask[w]; f.a[1][u].w[w] &= mask[w]; }
+            }
+            multiply_step(s, f.a[0][u], f.a[1][u]);
+        }
+    };
+    // lane: query i * 16 + (lane & 15), rows 4 (lane >> 4) + 0 .. 3 of either half
+    auto take = [&](int64_t tile) __attribute__((always_inline)) {
         const int valid = (int)(n - tile * 32 < 32 ? n - tile * 32 : 32);
 #pragma unroll
         for (int i = 0; i < QT; ++i) {
@@ -173,7 +198,32 @@ __global__ __launch_bounds__(kStreamThreads) void prob_stream_kernel(const T *__
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
                 if (kg == 0 && q0 + i * 16 + r16 < nq) gmax[(int64_t)(q0 + i * 16 + r16) * gstride + tile] = top;
             }
+            acc[0][i] = acc[1][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
+    };
+    if (tile < whole_tiles) {
+        int batch = 0;
+        // one batch: asks for the one after it, multiplies, and at a tile's end takes its logits; false after the last
+        auto turn = [&](Batch &now, Batch &then) __attribute__((always_inline)) {
+            int64_t then_tile = tile;
+            int then_batch = batch + 1;
+            if (then_batch == batches) { then_batch = 0; then_tile += stride; }
+            const bool more = then_tile < whole_tiles;
+            if (more) fetch(then, then_tile, then_batch);
+            multiply(now, batch);
+            if (then_batch == 0) take(tile);
+            tile = then_tile;
+            batch = then_batch;
+            return more;
+        };
+        while (turn(here, next) && turn(next, here)) {}
+    }
+    for (; tile < tiles; tile += stride) {
+        const int64_t r0 = tile * 32 + r16, r1 = r0 + 16;
+        const T *p0 = x + (r0 < n ? r0 : n - 1) * ld_x, *p1 = x + (r1 < n ? r1 : n - 1) * ld_x;
+#pragma unroll 1
+        for (int s = 0; s < steps; ++s) multiply_step(s, load_frag<T, ALIGNED>(p0, s * S + kg * E, d), load_frag<T, ALIGNED>(p1, s * S + kg * E, d));
+        take(tile);
     }
     // the four lanes of a query, then the waves
 #pragma unroll
@@ -283,8 +333,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
 
 // ---- what a query's statistics give ----------------------------------------------------------
 
-constexpr int kFinishThreads = 512, kFinishWaves = kFinishThreads / 64;
-
 __device__ __forceinline__ uint32_t order_of(float v)
 {
     const uint32_t b = __float_as_uint(v + 0.0f); // (-0 is 0)
@@ -293,59 +341,118 @@ __device__ __forceinline__ uint32_t order_of(float v)
 
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
 
-// <q, x> by 16 lanes (fp32, in a fixed order); every lane of the group gets it
-template <class T>
-__device__ __forceinline__ float dot16(const float *__restrict__ qf, const T *__restrict__ row, int d, int lane16)
+template <int R, int F> struct Shape { static constexpr int rows = R, loads = F; };
+
+// <q, x> of R rows at once by 16 lanes, F loads of 16 bytes a row in flight (fp32, the same order of additions whatever R and F:
+// a lane's coordinates in order, then the lanes); every lane of the group gets them. NULL: a row that is not there.
+template <class T, int R, int F>
+__device__ __forceinline__ void dots16(const float *__restrict__ qf, const T *const (&row)[R], int d, int lane16, float (&s)[R])
 {
     constexpr int E = kFragElems<T>;
-    float s = 0.0f;
-    for (int k = lane16 * E; k < d; k += 16 * E) {
-        const Frag f = load_frag<T, false>(row, k, d);
-        T e[E];
-        __builtin_memcpy(e, &f, 16);
 #pragma unroll
-        for (int j = 0; j < E; ++j)
-            if (k + j < d) s = __fmaf_rn(qf[k + j], to_f32(e[j]), s);
+    for (int r = 0; r < R; ++r) s[r] = 0.0f;
+    for (int k0 = lane16 * E; k0 < d; k0 += F * 16 * E) {
+        Frag f[R][F];
+#pragma unroll
+        for (int u = 0; u < F; ++u)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                f[r][u] = Frag{};
+                if (row[r] && k0 + u * 16 * E < d) f[r][u] = load_frag<T, false>(row[r], k0 + u * 16 * E, d);
+            }
+#pragma unroll
+        for (int u = 0; u < F; ++u) {
+            const int k = k0 + u * 16 * E;
+            if (k >= d) break;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                T e[E];
+                __builtin_memcpy(e, &f[r][u], 16);
+#pragma unroll
+                for (int j = 0; j < E; ++j) s[r] = __fmaf_rn(k + j < d ? qf[k + j] : 0.0f, to_f32(e[j]), s[r]);
+            }
+        }
     }
-    return group_sum<16>(s);
+#pragma unroll
+    for (int r = 0; r < R; ++r) s[r] = group_sum<16>(s[r]);
+}
+
+template <class T> __device__ __forceinline__ float dot16(const float *__restrict__ qf, const T *row, int d, int lane16)
+{
+    const T *const one[1] = {row};
+    float s[1];
+    dots16<T, 1, 8>(qf, one, d, lane16, s);
+    return s[0];
 }
 
 // A workgroup a query: joins the statistics, scores the given rows and the best ones.
-template <class T>
-__global__ __launch_bounds__(kFinishThreads) void prob_finish_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, float scale,
-                                                                     const float4 *__restrict__ stats, int parts, const int32_t *__restrict__ ids, int given,
-                                                                     float *__restrict__ logp_out, float *__restrict__ lse_out, float *__restrict__ entropy_out,
-                                                                     const float *__restrict__ gmax, int64_t gstride, int k, int32_t *__restrict__ alt_ids, float *__restrict__ alt_logp)
+template <class T, int NT>
+__global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, float scale,
+                                                         const float4 *__restrict__ stats, int parts, const int32_t *__restrict__ ids, int given, float *__restrict__ logp_out,
+                                                         float *__restrict__ lse_out, float *__restrict__ entropy_out, const float *__restrict__ gmax, int64_t gstride, int k,
+                                                         int32_t *__restrict__ alt_ids, float *__restrict__ alt_logp)
 {
     __shared__ WgSelectScratch sel;
-    __shared__ Stat wave_stat[kFinishWaves];
-    __shared__ uint32_t list_count;
+    __shared__ Stat wave_stat[NT / 64];
+    __shared__ uint32_t list_count, bound_shared;
     extern __shared__ char lds[];
-    float *qf = (float *)lds;                                       // [d]
-    u64 *keys = (u64 *)(lds + (((size_t)d * 4 + 15) & ~(size_t)15)); // [32 k] scores of the listed groups' rows
-    u64 *best = keys + 32 * (size_t)k;                               // [k]
+    float *qf = (float *)lds;                                        // [d]
+    u64 *keys = (u64 *)(lds + (((size_t)d * 4 + 15) & ~(size_t)15)); // [max(32 k, kFinishList)]: candidate groups, then rows
+    u64 *best = keys + std::max(32 * k, kFinishList);                // [k]
     uint32_t *groups = (uint32_t *)(best + k);                       // [k]
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = blockIdx.x;
-    for (int c = tid; c < d; c += kFinishThreads) qf[c] = to_f32(q[(int64_t)row * ld_q + c]);
+    for (int c = tid; c < d; c += NT) qf[c] = to_f32(q[(int64_t)row * ld_q + c]);
     Stat a{-INFINITY, 0.0f, 0.0f};
-    for (int p = tid; p < parts; p += kFinishThreads) {
+    for (int p = tid; p < parts; p += NT) {
         const float4 v = stats[(size_t)p * nq + row];
         a = join(a, Stat{v.x, v.y, v.z});
     }
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) a = join(a, Stat{__shfl_xor(a.m, w, 64), __shfl_xor(a.l, w, 64), __shfl_xor(a.t, w, 64)});
     if (lane == 0) wave_stat[wave] = a;
+    if (tid == 0) list_count = 0;
+
+    // The largest group of every few threads, 4 k classes or more: the k-th largest of those bounds the k-th largest group from below.
+    const uint32_t n_groups = (uint32_t)((n + 31) / 32);
+    const float *gm = gmax + row * gstride;
+    auto each_group = [&](auto &&fn) { // (four groups a load; the last four may lie past the end)
+        constexpr int U = 4;
+        for (uint32_t g0 = 4 * tid; g0 < n_groups; g0 += 4 * NT * U) {
+            float4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = g0 + 4 * NT * u < n_groups ? *(const float4 *)(gm + g0 + 4 * NT * u) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float e[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t g = g0 + 4 * NT * u + i;
+                    if (g < n_groups) fn(g, order_of(e[i]));
+                }
+            }
+        }
+    };
+    uint32_t *tops = (uint32_t *)keys;
+    int per = 16; // threads a class
+    while (per > 1 && NT / per < 4 * k) per /= 2;
+    const int classes = NT / per;
+    if (k > 0) {
+        uint32_t mine = 0;
+        each_group([&](uint32_t, uint32_t o) { mine = max(mine, o); });
+        for (int w = 1; w < per; w <<= 1) mine = max(mine, (uint32_t)__shfl_xor((int)mine, w, 64));
+        if (tid % per == 0) tops[tid / per] = mine;
+    }
     __syncthreads();
     a = wave_stat[0];
-    for (int w = 1; w < kFinishWaves; ++w) a = join(a, wave_stat[w]);
+    for (int w = 1; w < NT / 64; ++w) a = join(a, wave_stat[w]);
     constexpr float ln2 = 0.693147180559945309f;
     const float log_l = logf(a.l), lse = __fmaf_rn(a.m, ln2, log_l);
     if (tid == 0) {
         lse_out[row] = lse;
         if (entropy_out) entropy_out[row] = log_l - ln2 * (a.t / a.l);
     }
-    const int sub = tid >> 4, subs = kFinishThreads / 16, lane16 = tid & 15;
+    const int sub = tid >> 4, subs = NT / 16, lane16 = tid & 15;
     for (int j = sub; j < given; j += subs) {
         const int32_t id = ids[(int64_t)row * given + j];
         const bool real = id >= 0 && (int64_t)id < n;
@@ -354,39 +461,76 @@ __global__ __launch_bounds__(kFinishThreads) void prob_finish_kernel(const T *__
     }
     if (k == 0) return;
 
-    const uint32_t n_groups = (uint32_t)((n + 31) / 32);
-    if (tid == 0) list_count = 0;
-    auto group_key = [&](uint32_t g) { return ((u64)order_of(gmax[row * gstride + g]) << 32) | (u64)(0xffffffffu - g); };
-    const u64 least = wg_select_threshold_of([&](auto &&fn) { for (uint32_t g = tid; g < n_groups; g += kFinishThreads) fn(group_key(g)); }, k, &sel);
-    __syncthreads();
-    for (uint32_t g = tid; g < n_groups; g += kFinishThreads)
-        if (group_key(g) >= least) {
-            const uint32_t at = atomicAdd(&list_count, 1u); // (the order of the list does not matter)
-            if (at < (uint32_t)k) groups[at] = g;
+    if (tid < classes) {
+        const uint32_t mine = tops[tid];
+        uint32_t rank = 0;
+#pragma unroll 4
+        for (int o = 0; o < classes; o += 4) {
+            const uint4 v = *(const uint4 *)(tops + o);
+            rank += (v.x > mine || (v.x == mine && o + 0 < tid)) + (v.y > mine || (v.y == mine && o + 1 < tid)) + (v.z > mine || (v.z == mine && o + 2 < tid)) +
+                    (v.w > mine || (v.w == mine && o + 3 < tid));
         }
+        if (rank == (uint32_t)k - 1) bound_shared = mine; // (k <= classes)
+    }
+    __syncthreads();
+    const uint32_t bound = bound_shared;
+    auto key_of = [](uint32_t g, uint32_t o) { return ((u64)o << 32) | (u64)(0xffffffffu - g); };
+    each_group([&](uint32_t g, uint32_t o) {
+        if (o < bound) return;
+        const uint32_t at = atomicAdd(&list_count, 1u); // (the order of the list does not matter)
+        if (at < kFinishList) keys[at] = key_of(g, o);
+    });
+    __syncthreads();
+    const uint32_t listed = list_count;
+    u64 least;
+    if (listed <= kFinishList) least = wg_select_threshold_of([&](auto &&fn) { for (uint32_t i = tid; i < listed; i += NT) fn(keys[i]); }, k, &sel);
+    else least = wg_select_threshold_of([&](auto &&fn) { each_group([&](uint32_t g, uint32_t o) { fn(key_of(g, o)); }); }, k, &sel);
+    __syncthreads();
+    if (tid == 0) list_count = 0;
+    __syncthreads();
+    auto choose = [&](u64 key) {
+        if (key < least) return;
+        const uint32_t at = atomicAdd(&list_count, 1u);
+        if (at < (uint32_t)k) groups[at] = 0xffffffffu - (uint32_t)key;
+    };
+    if (listed <= kFinishList) for (uint32_t i = tid; i < listed; i += NT) choose(keys[i]);
+    else each_group([&](uint32_t g, uint32_t o) { choose(key_of(g, o)); });
     __syncthreads();
     const uint32_t rows = min(list_count, (uint32_t)k) * 32u;
-    for (uint32_t i = sub; i < rows; i += subs) {
-        const int64_t id = (int64_t)groups[i / 32] * 32 + (i & 31);
-        u64 key = 0;
-        if (id < n) {
-            const float s = dot16<T>(qf, x + id * ld_x, d, lane16) * scale;
-            key = ((u64)order_of(s) << 32) | (u64)(0xffffffffu - (uint32_t)id);
+    auto score = [&](auto shape) {
+        constexpr int R = decltype(shape)::rows, F = decltype(shape)::loads;
+        for (uint32_t i = sub * R; i < rows; i += subs * R) {
+            const T *p[R];
+            int64_t id[R];
+            float s[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                id[r] = (int64_t)groups[i / 32] * 32 + (i & 31) + r; // (R divides 32)
+                p[r] = id[r] < n ? x + id[r] * ld_x : nullptr;
+            }
+            dots16<T, R, F>(qf, p, d, lane16, s);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (lane16 == r) keys[i + r] = p[r] ? ((u64)order_of(s[r] * scale) << 32) | (u64)(0xffffffffu - (uint32_t)id[r]) : 0;
         }
-        if (lane16 == 0) keys[i] = key;
-    }
+    };
+    // short rows several at a time, so that as many loads are in flight
+    constexpr int kPer = 16 * kFragElems<T>;
+    if (d <= 2 * kPer) score(Shape<4, 2>{});
+    else if (d <= 4 * kPer) score(Shape<2, 4>{});
+    else score(Shape<1, 8>{});
     if (tid == 0) list_count = 0;
     __syncthreads();
-    const u64 kth = wg_select_threshold_of([&](auto &&fn) { for (uint32_t i = tid; i < rows; i += kFinishThreads) if (keys[i]) fn(keys[i]); }, k, &sel);
+    const u64 kth = wg_select_threshold_of([&](auto &&fn) { for (uint32_t i = tid; i < rows; i += NT) if (keys[i]) fn(keys[i]); }, k, &sel);
     __syncthreads();
-    for (uint32_t i = tid; i < rows; i += kFinishThreads)
+    for (uint32_t i = tid; i < rows; i += NT)
         if (keys[i] && keys[i] >= kth) {
             const uint32_t at = atomicAdd(&list_count, 1u);
             if (at < (uint32_t)k) best[at] = keys[i];
         }
     __syncthreads();
     const uint32_t found = min(list_count, (uint32_t)k);
-    for (uint32_t i = tid; i < found; i += kFinishThreads) {
+    for (uint32_t i = tid; i < found; i += NT) {
         const u64 mine = best[i];
         uint32_t rank = 0;
         for (uint32_t o = 0; o < found; ++o) rank += best[o] > mine;
@@ -400,7 +544,7 @@ __global__ __launch_bounds__(kFinishThreads) void prob_finish_kernel(const T *__
 // Workgroups that share the rows of the stream.
 static int stream_groups(int64_t n, int query_tiles)
 {
-    const int64_t tiles = (n + 31) / 32, most = std::max(1, 1024 / query_tiles);
+    const int64_t tiles = (n + 31) / 32, most = std::max(1, 512 / query_tiles); // two workgroups a compute unit
     return (int)std::max<int64_t>(1, std::min<int64_t>((tiles + kStreamWaves - 1) / kStreamWaves, most));
 }
 
@@ -531,6 +675,17 @@ static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
     return AVQ_OK;
 }
 
+template <class T, int NT>
+static int finish_run(const ProbParams &p, const ProbScratch &s, int parts, hipStream_t st)
+{
+    static LdsLimitOnce once;
+    AVQ_TRY(set_lds_limit((const void *)prob_finish_kernel<T, NT>, kFinishLds, &once));
+    prob_finish_kernel<T, NT><<<dim3(p.nq), dim3(NT), finish_lds(p.d, p.k), st>>>((const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.nq, p.ld_queries, p.scale, s.stats,
+                                                                                parts, p.ids, p.given, p.logp, p.lse, p.entropy, s.gmax, s.gstride, p.k, p.alt_ids, p.alt_logp);
+    AVQ_HIP(hipGetLastError());
+    return AVQ_OK;
+}
+
 template <class T>
 static int log_probs_typed(const ProbParams &p, hipStream_t st)
 {
@@ -544,13 +699,8 @@ static int log_probs_typed(const ProbParams &p, hipStream_t st)
         const bool aligned = ((uintptr_t)p.points % 16) == 0 && (p.ld_points * sizeof(T)) % 16 == 0;
         AVQ_TRY(aligned ? (stream_sized<T, true>(p, s, st)) : (stream_sized<T, false>(p, s, st)));
     }
-    static LdsLimitOnce once;
-    AVQ_TRY(set_lds_limit((const void *)prob_finish_kernel<T>, kFinishLds, &once));
-    prob_finish_kernel<T><<<dim3(p.nq), dim3(kFinishThreads), finish_lds(p.d, p.k), st>>>((const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.nq, p.ld_queries, p.scale,
-                                                                                       s.stats, parts, p.ids, p.given, p.logp, p.lse, p.entropy, s.gmax, s.gstride, p.k, p.alt_ids,
-                                                                                       p.alt_logp);
-    AVQ_HIP(hipGetLastError());
-    return AVQ_OK;
+    // a few queries: as many threads a query as there can be
+    return p.nq <= 256 ? finish_run<T, 1024>(p, s, parts, st) : finish_run<T, 512>(p, s, parts, st);
 }
 
 int launch_log_probs(const ProbParams &p, hipStream_t st)

@@ -245,7 +245,7 @@ __global__ __launch_bounds__(256) void grad_zero_kernel(T *__restrict__ out, int
 }
 
 constexpr int kGradGroups = 512;                  // two workgroups a compute unit
-constexpr size_t kGradBytes = (size_t)256 << 20;  // most that G of a part takes where a part has more than the least rows
+constexpr size_t kGradBytes = (size_t)1 << 30;    // most that G of a part takes where a part has more than the least rows
 
 struct ProbGradScratch {
     bool pack;
