@@ -281,7 +281,8 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
     const uint32_t teams = 256u / (uint32_t)lanes, team = threadIdx.x / (uint32_t)lanes;
     const uint32_t all_begin = blockIdx.x * teams * (uint32_t)kRunChunk;
     for (uint32_t i = threadIdx.x; i < teams * (uint32_t)kRunChunk; i += 256) {
-        skeys[i] = all_begin + i < count ? keys[all_begin + i] : n; // (n: nothing to add)
+        // (key n: a run that goes nowhere; its rows are read all the same, so that no load waits for a branch)
+        skeys[i] = all_begin + i < count ? keys[all_begin + i] : n;
         spos[i] = all_begin + i < count ? pos[all_begin + i] : 0u;
     }
     __syncthreads();
@@ -303,10 +304,7 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
         const T *from = grad + (int64_t)col * V;
         auto ask = [&](Rows &r, int i0) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                r.v[u] = Pack<T, V>{};
-                if (ks[i0 + u] < n) r.v[u] = *(const Pack<T, V> *)(from + (int64_t)ps[i0 + u] * ld_grad);
-            }
+            for (int u = 0; u < kAhead; ++u) r.v[u] = *(const Pack<T, V> *)(from + (int64_t)ps[i0 + u] * ld_grad);
         };
         auto partial_row = [&](int slot) __attribute__((always_inline)) {
             Pack<float, V> o;
