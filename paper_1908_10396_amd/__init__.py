@@ -410,4 +410,13 @@ class Index:
         return ids, ip
 
 
-from .rows import LogProbs, embed, embed_grad, layer_norm, layer_norm_grad, log_probs, log_probs_grad  # noqa: E402,F401
+# the operators on rows of learned vectors; their module imports torch, which this one does not need to be imported
+_ROWS = ("LogProbs", "embed", "embed_grad", "layer_norm", "layer_norm_grad", "log_probs", "log_probs_grad")
+
+
+def __getattr__(name):
+    if name not in _ROWS:
+        raise AttributeError("module %r has no attribute %r" % (__name__, name))
+    from . import rows
+    globals().update({n: getattr(rows, n) for n in _ROWS})
+    return globals()[name]
