@@ -29,4 +29,10 @@ __device__ __forceinline__ void lds_copy16_once(const void *src, void *dst)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" : : "s"(at), "v"((uint64_t)(uintptr_t)src) : "m0", "memory");
 }
 
+// 16 bytes a lane from base + offset bytes (base the same for the whole wave) to the LDS address `at` (the same too) + 16 lane.
+__device__ __forceinline__ void lds_copy16_from(const void *base, uint32_t offset, uint32_t at)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(at), "v"(offset), "s"((uint64_t)(uintptr_t)base) : "m0", "memory");
+}
+
 } // namespace avq

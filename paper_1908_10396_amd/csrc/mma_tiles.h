@@ -1,14 +1,15 @@
 // Tiles of matrix products on the 16-bit matrix instructions (32 x 32 x 16), for operands laid out by rows_pack.hip or
 // used as they are.
 //
-// fp32 operands are two f16 planes: v = (hi + lo) / s with s a power of two that brings the largest magnitude to 2^14 .. 2^15,
-// hi = f16(v s), lo = f16(v s - hi). hi hi' + hi lo' + lo hi' differs from v v' s s' by less than 1.5 * 2^-23 of it (values
+// fp32 operands (SPLIT) are two f16 values each: v = (hi + lo) / s with s a power of two that brings the largest magnitude to
+// 2^14 .. 2^15, hi = f16(v s), lo = f16(v s - hi). hi hi' + hi lo' + lo hi' differs from v v' s s' by less than 1.5 * 2^-23 of it (values
 // down to 2^-28 of the largest; below, by 2^-40 of the largest), which is what an fp32 product and its sum lose anyway, at a third
-// of the 16-bit rate: five times the fp32 matrix instruction's.
+// of the 16-bit rate: five times the fp32 matrix instruction's. A row holds 16 hi, then their 16 lo, and so on.
 //
 // A workgroup of four waves forms 256 x 128 values, a wave 128 x 64 (4 x 2 matrix instructions, 128 accumulators), over steps
-// of 32 of the inner dimension. A step's operands (24 KB) come by copies straight to LDS, two steps ahead in a ring of three; one
-// barrier a step. Two workgroups share a compute unit, so that one's epilogue runs beside the other's matrix instructions.
+// of 32 of the inner dimension (SPLIT: 16, 24 matrix instructions rather than 16). A step's operands (24 KB, 64 bytes a row) come by
+// copies straight to LDS, two steps ahead in a ring of three; one barrier a step. Two workgroups share a compute unit, so that
+// one's epilogue runs beside the other's matrix instructions.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -24,12 +25,18 @@ typedef __bf16 bf16v8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16v8 __attribute__((ext_vector_type(8)));
 struct alignas(16) Quad { uint32_t w[4]; };
 
-constexpr int kTileM = 256, kTileN = 128, kTileK = 32, kTileThreads = 256;
-constexpr int kStageA = kTileM * kTileK * 2, kStageB = kTileN * kTileK * 2, kStageBytes = kStageA + kStageB, kStages = 3;
+constexpr int kTileM = 256, kTileN = 128, kStepBytes = 64 /* of a row */, kTileThreads = 256;
+constexpr int kStageA = kTileM * kStepBytes, kStageB = kTileN * kStepBytes, kStageBytes = kStageA + kStageB, kStages = 3;
 constexpr int kTileLds = kStages * kStageBytes;
 
-// Rows of 16-bit elements: `rows` of them, ld elements apart, 16-byte aligned; plane: elements from the hi to the lo plane.
-struct Rows16 { const uint16_t *p; int64_t ld, plane, rows; };
+// Rows of 16-bit elements (SPLIT: of pairs of them): `rows` of them, ld elements apart, 16-byte aligned.
+struct Rows16 { const uint16_t *p; int64_t ld, rows; };
+constexpr int64_t kMaxLd16 = (int64_t)1 << 22; // (256 rows' places are 32-bit offsets)
+
+// Where element c of a row lies; SPLIT: its hi, 16 elements before its lo.
+template <bool SPLIT> __host__ __device__ inline int64_t place16(int64_t c) { return SPLIT ? (c >> 4) * 32 + (c & 15) : c; }
+// The steps that an inner dimension of d takes, and the elements a row of it must have.
+template <bool SPLIT> __host__ __device__ inline int steps_of(int64_t d) { return (int)((d + (SPLIT ? 15 : 31)) / (SPLIT ? 16 : 32)); }
 
 __device__ __forceinline__ f32x16 mma32(const Quad &a, const Quad &b, f32x16 c, bf16_t)
 {
@@ -52,78 +59,81 @@ template <int NEWER> __device__ __forceinline__ void step_barrier()
 }
 constexpr int kCopies = 6; // of a wave a step (the 6 above)
 
-// The products that make up one: with fp32 operands hi hi', hi lo', lo hi', else the one there is.
-__device__ __forceinline__ int plane_of_a(int term) { return term == 2; }
-__device__ __forceinline__ int plane_of_b(int term) { return term == 1; }
-
-// Copies of operands whose rows hold the inner dimension (C = A B^T). In LDS a row's 32 elements are four 16-byte chunks, chunk c
+// Copies of operands whose rows hold the inner dimension (C = A B^T). In LDS a row's step is four 16-byte chunks, chunk c
 // of row r at c ^ (r / 4 % 4): sixteen rows' reads of one chunk touch every bank once.
 struct RowCopies {
-    const char *a[4], *b[2];
+    const char *pa, *pb; // the tile's first rows
+    uint32_t a[4], b[2]; // this lane's places from there
     __device__ __forceinline__ void seek(const Rows16 &A, int64_t a0, const Rows16 &B, int64_t b0)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const int chunk = (lane & 3) ^ ((lane >> 4) & 3);
+        const uint32_t chunk = (uint32_t)((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+        const int last_a = (int)min(A.rows - 1 - a0, (int64_t)kTileM), last_b = (int)min(B.rows - 1 - b0, (int64_t)kTileN);
+        pa = (const char *)(A.p + a0 * A.ld);
+        pb = (const char *)(B.p + b0 * B.ld);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = (const char *)(A.p + min(a0 + (wave * 4 + j) * 16 + (lane >> 2), A.rows - 1) * A.ld) + chunk * 16;
+        for (int j = 0; j < 4; ++j) a[j] = (uint32_t)min((wave * 4 + j) * 16 + (lane >> 2), last_a) * (uint32_t)(A.ld * 2) + chunk;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) b[j] = (const char *)(B.p + min(b0 + (wave * 2 + j) * 16 + (lane >> 2), B.rows - 1) * B.ld) + chunk * 16;
+        for (int j = 0; j < 2; ++j) b[j] = (uint32_t)min((wave * 2 + j) * 16 + (lane >> 2), last_b) * (uint32_t)(B.ld * 2) + chunk;
     }
-    __device__ __forceinline__ void issue(const Rows16 &A, const Rows16 &B, int term, int step, char *stage) const
+    __device__ __forceinline__ void issue(const Rows16 &, const Rows16 &, int step, uint32_t stage) const
     {
-        const int wave = threadIdx.x >> 6;
-        const int64_t oa = (plane_of_a(term) ? A.plane * 2 : 0) + (int64_t)step * (kTileK * 2), ob = (plane_of_b(term) ? B.plane * 2 : 0) + (int64_t)step * (kTileK * 2);
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const char *fa = pa + (int64_t)step * kStepBytes, *fb = pb + (int64_t)step * kStepBytes;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) lds_copy16(a[j] + oa, stage + (wave * 4 + j) * 1024);
+        for (int j = 0; j < 4; ++j) lds_copy16_from(fa, a[j], stage + (wave * 4 + j) * 1024);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) lds_copy16(b[j] + ob, stage + kStageA + (wave * 2 + j) * 1024);
+        for (int j = 0; j < 2; ++j) lds_copy16_from(fb, b[j], stage + kStageA + (wave * 2 + j) * 1024);
     }
-    // the products of half a step (16 of the inner dimension)
-    template <class H> static __device__ __forceinline__ void multiply(const char *stage, int half, f32x16 (&acc)[4][2])
+    // operands of 16 of the inner dimension: the step's first or second half (SPLIT: its hi or lo)
+    static __device__ __forceinline__ void read(const char *stage, int half, Quad (&a)[4], Quad (&b)[2])
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         const int at = (lane & 31) * 64 + ((((lane >> 5) + half * 2) ^ ((lane >> 2) & 3)) * 16);
-        Quad a[4], b[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) b[j] = *(const Quad *)(stage + kStageA + ((wave & 1) * 64 + j * 32) * 64 + at);
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = *(const Quad *)(stage + ((wave >> 1) * 128 + i * 32) * 64 + at);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = mma32(a[i], b[j], acc[i][j], H{});
     }
 };
 
-// Copies of operands whose rows are the inner dimension (C = A^T B): 32 rows of 256 columns of A and 128 of B a step. A row's
-// 16-byte chunk c lies at c ^ (4 (r % 4)); the reads transpose 4 x 16 elements for 16 lanes, from four rows at once, which so lie in
-// different banks.
-struct ColumnCopies {
-    const char *a[4], *b[2];
-    int64_t row; // of the first step
+// Copies of operands whose rows are the inner dimension (C = A^T B): 32 rows (SPLIT: 16 of pairs) of 256 columns of A and 128 of B a
+// step. The reads transpose 4 x 16 elements for 16 lanes: 32 lanes read two pieces of 32 bytes, 32 (SPLIT: 64) apart, of four rows. So
+// that these lie in different banks, a row's 16-byte chunk c lies at c ^ turn(row % 4).
+template <bool SPLIT> struct ColumnCopies {
+    static constexpr int kRows = SPLIT ? 16 : 32, kRowA = kStageA / kRows, kRowB = kStageB / kRows; // of a step; bytes of a row in LDS
+    static constexpr int kChunksA = kRowA / 16, kChunksB = kRowB / 16;
+    static __device__ __forceinline__ int turn(int r) { return SPLIT ? (r & 1) * 2 + (r >> 1) * 8 : r * 4; }
+    const char *pa, *pb; // the tile's first columns
+    uint32_t a[4], b[2]; // this lane's columns from there
+    int64_t row;         // of the first step
     __device__ __forceinline__ void seek(const Rows16 &A, int64_t a0, int64_t a_columns, const Rows16 &B, int64_t b0)
     {
         // (columns of A past its last come from its last: nothing uses their products; B is as wide as its tiles)
         const int lane = threadIdx.x & 63;
+        const int last = (int)min((place16<SPLIT>(a_columns) - place16<SPLIT>(a0)) / 8 - 1, (int64_t)kChunksA);
+        pa = (const char *)(A.p + place16<SPLIT>(a0));
+        pb = (const char *)(B.p + place16<SPLIT>(b0));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = (j * 2 + (lane >> 5)) & 3;
-            a[j] = (const char *)(A.p + min(a0 + ((lane & 31) ^ (r * 4)) * 8, a_columns - 8));
-        }
+        for (int j = 0; j < 4; ++j) a[j] = (uint32_t)min((lane % kChunksA) ^ turn((j * (64 / kChunksA) + lane / kChunksA + (SPLIT ? (threadIdx.x >> 6) * 4 : 0)) & 3), last) * 16;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) b[j] = (const char *)(B.p + b0 + ((lane & 15) ^ ((lane >> 4) * 4)) * 8);
+        for (int j = 0; j < 2; ++j) b[j] = (uint32_t)((lane % kChunksB) ^ turn((j * (64 / kChunksB) + lane / kChunksB) & 3)) * 16;
     }
-    __device__ __forceinline__ void issue(const Rows16 &A, const Rows16 &B, int term, int step, char *stage) const
+    __device__ __forceinline__ void issue(const Rows16 &A, const Rows16 &B, int step, uint32_t stage) const
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const int64_t oa = plane_of_a(term) ? A.plane * 2 : 0, ob = plane_of_b(term) ? B.plane * 2 : 0;
-        const int64_t first = row + (int64_t)step * kTileK;
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        // (a step's rows past an operand's last, of which a whole step may consist, are its last row)
+        const int64_t first = row + (int64_t)step * kRows, first_a = min(first, A.rows - 1), first_b = min(first, B.rows - 1);
+        const char *fa = pa + first_a * A.ld * 2, *fb = pb + first_b * B.ld * 2;
+        const int last_a = (int)min(A.rows - 1 - first_a, (int64_t)kRows), last_b = (int)min(B.rows - 1 - first_b, (int64_t)kRows);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) lds_copy16(a[j] + oa + min(first + (wave * 4 + j) * 2 + (lane >> 5), A.rows - 1) * A.ld * 2, stage + (wave * 4 + j) * 1024);
+        for (int j = 0; j < 4; ++j)
+            lds_copy16_from(fa, (uint32_t)min((wave * 4 + j) * (64 / kChunksA) + lane / kChunksA, last_a) * (uint32_t)(A.ld * 2) + a[j], stage + (wave * 4 + j) * 1024);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) lds_copy16(b[j] + ob + min(first + (wave * 2 + j) * 4 + (lane >> 4), B.rows - 1) * B.ld * 2, stage + kStageA + (wave * 2 + j) * 1024);
+        for (int j = 0; j < 2; ++j)
+            lds_copy16_from(fb, (uint32_t)min((wave * 2 + j) * (64 / kChunksB) + lane / kChunksB, last_b) * (uint32_t)(B.ld * 2) + b[j], stage + kStageA + (wave * 2 + j) * 1024);
     }
-    static __device__ __forceinline__ Quad read(const char *p, int row_bytes)
+    static __device__ __forceinline__ Quad read_turned(const char *p, int row_bytes)
     {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
@@ -133,49 +143,50 @@ struct ColumnCopies {
         __builtin_memcpy(&q.w[2], &hi, 8);
         return q;
     }
-    template <class H> static __device__ __forceinline__ void multiply(const char *stage, int half, f32x16 (&acc)[4][2])
+    static __device__ __forceinline__ void read(const char *stage, int half, Quad (&a)[4], Quad (&b)[2])
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const int i16 = lane & 15, g = lane >> 4, r = i16 >> 2; // row of the four, which the chunk's place goes by
-        const int row_at = half * 16 + 8 * (g >> 1) + r, in_chunk = (2 * (g & 1) + ((i16 & 3) >> 1)) * 16 + (i16 & 1) * 8;
-        Quad a[4], b[2];
+        const int i16 = lane & 15, g = lane >> 4, r = i16 >> 2; // r: row of the four
+        const int row_at = (SPLIT ? 0 : half * 16) + 8 * (g >> 1) + r;
+        // the chunk of columns 32 m + 16 (g & 1) + 4 (i16 & 3) onwards, and the place in it
+        auto at = [&](int m) { return ((SPLIT ? m * 8 + (g & 1) * 4 + half * 2 + ((i16 & 3) >> 1) : m * 4 + (g & 1) * 2 + ((i16 & 3) >> 1)) ^ turn(r)) * 16 + (i16 & 1) * 8; };
 #pragma unroll
-        for (int j = 0; j < 2; ++j) b[j] = read(stage + kStageA + row_at * (kTileN * 2) + ((((wave & 1) * 2 + j) ^ r) * 64) + in_chunk, kTileN * 2);
+        for (int j = 0; j < 2; ++j) b[j] = read_turned(stage + kStageA + row_at * kRowB + at((wave & 1) * 2 + j), kRowB);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = read(stage + row_at * (kTileM * 2) + ((((wave >> 1) * 4 + i) ^ r) * 64) + in_chunk, kTileM * 2);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = mma32(a[i], b[j], acc[i][j], H{});
+        for (int i = 0; i < 4; ++i) a[i] = read_turned(stage + row_at * kRowA + at((wave >> 1) * 4 + i), kRowA);
     }
 };
 
-// `tiles` tiles one after the other, the copies running ahead over their borders. halves: 16s of the inner dimension.
-// seek(i, copies): turns to tile i; epilogue(i, acc): takes its values. MEMORY: the epilogue loads or stores.
-template <class H, int TERMS, bool MEMORY, class Copies, class Seek, class Epilogue>
-__device__ __forceinline__ void run_tiles(const Rows16 &A, const Rows16 &B, int halves, int tiles, char *lds, Seek seek, Epilogue epilogue)
+template <class H> __device__ __forceinline__ void multiply(const Quad (&a)[4], const Quad (&b)[2], f32x16 (&acc)[4][2])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = mma32(a[i], b[j], acc[i][j], H{});
+}
+
+// `tiles` tiles of `steps` steps one after the other, the copies running ahead over their borders. seek(i, copies): turns to tile i;
+// epilogue(i, acc): takes its values. MEMORY: the epilogue loads or stores.
+template <class H, bool SPLIT, bool MEMORY, class Copies, class Seek, class Epilogue>
+__device__ __forceinline__ void run_tiles(const Rows16 &A, const Rows16 &B, int steps, int tiles, char *lds, Seek seek, Epilogue epilogue)
 {
     if (tiles <= 0) return;
-    const int steps = (halves + 1) / 2;
     Copies copies;
-    int tile = 0, term = 0, step = 0, stage = 0; // of the next copies
+    int tile = 0, step = 0, stage = 0; // of the next copies
     bool more = true;
     seek(0, copies);
-    auto issue = [&]() {
-        copies.issue(A, B, term, step, lds + stage * kStageBytes);
+    const uint32_t lds_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds);
+    auto issue = [&]() __attribute__((always_inline)) {
+        copies.issue(A, B, step, lds_at + stage * kStageBytes);
         stage = stage + 1 == kStages ? 0 : stage + 1;
         if (++step == steps) {
             step = 0;
-            if (TERMS == 1 || ++term == TERMS) {
-                term = 0;
-                if (++tile == tiles) more = false;
-                else seek(tile, copies);
-            }
+            if (++tile == tiles) more = false;
+            else seek(tile, copies);
         }
     };
     issue();
     if (more) issue();
-    const int total_steps = steps * TERMS;
     int at = 0;
     for (int t = 0; t < tiles; ++t) {
         f32x16 acc[4][2];
@@ -185,18 +196,23 @@ __device__ __forceinline__ void run_tiles(const Rows16 &A, const Rows16 &B, int 
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-        int s_in_term = 0;
-        for (int s = 0; s < total_steps; ++s) {
+        for (int s = 0; s < steps; ++s) {
             // the last step of all has no younger copies; after an epilogue with memory operations all are waited for
-            const bool last = t + 1 == tiles && s + 1 == total_steps;
-            if (last || (MEMORY && s == 0)) step_barrier<0>();
+            if ((t + 1 == tiles && s + 1 == steps) || (MEMORY && s == 0)) step_barrier<0>();
             else step_barrier<kCopies>();
             if (more) issue();
             const char *here = lds + at * kStageBytes;
             at = at + 1 == kStages ? 0 : at + 1;
-            Copies::template multiply<H>(here, 0, acc);
-            if (2 * s_in_term + 1 < halves) Copies::template multiply<H>(here, 1, acc);
-            if (++s_in_term == steps) s_in_term = 0;
+            Quad a[2][4], b[2][2];
+            Copies::read(here, 0, a[0], b[0]);
+            Copies::read(here, 1, a[1], b[1]);
+            multiply<H>(a[0], b[0], acc);
+            if (SPLIT) {
+                multiply<H>(a[0], b[1], acc);
+                multiply<H>(a[1], b[0], acc);
+            } else {
+                multiply<H>(a[1], b[1], acc);
+            }
         }
         epilogue(t, acc);
     }
@@ -240,13 +256,13 @@ __device__ __forceinline__ float range_scale(uint32_t largest_bits)
 int launch_clear_largest(Largest *to, hipStream_t st);
 // max over finite elements into *to
 int launch_largest(const float *x, int64_t rows, int d, int64_t ld, uint32_t *to, hipStream_t st);
-// Rows as 16-bit elements padded with zeros to `width` (a multiple of 8) elements, rows_out >= rows of them (zeros past the last).
-// fp32: hi and lo plane, scaled by range_scale(*largest), or, largest == NULL, each row by its own, whose inverse goes to inv[row].
+// Rows as 16-bit elements padded with zeros to `width` (a multiple of 16) elements.
+// fp32: pairs (a row has 2 width elements), scaled by range_scale(*largest), or, largest == NULL, each row by its own, whose inverse
+// goes to inv[row].
 // negate: with the other sign (16-bit types, and rows with scales of their own).
-int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int64_t rows_out, int width, uint16_t *out, int64_t plane, const uint32_t *largest, float *inv,
-                     bool negate, hipStream_t st);
-// The transpose: out[c][t] = x[t][c] for c < columns_out (zeros past d), t < width (zeros past rows).
-int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int columns_out, int width, uint16_t *out, int64_t plane, const uint32_t *largest,
-                           hipStream_t st);
+int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int width, uint16_t *out, const uint32_t *largest, float *inv, bool negate,
+                     hipStream_t st);
+// The transpose: row c < d of out holds x[t][c] at t < width (a multiple of 16; zeros past rows).
+int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int width, uint16_t *out, const uint32_t *largest, hipStream_t st);
 
 } // namespace avq

@@ -246,8 +246,8 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prob_stream_kernel(const T 
 
 // Statistics of 128 queries over a part of the rows, 256 rows at a time; a lane has two queries, 64 of a tile's rows of each.
 // X: the launch's rows, Q: all queries, negated where the scale is.
-template <class H, int TERMS, bool BEST>
-__global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Rows16 Q, int halves, float c2, const Largest *__restrict__ largest, const float *__restrict__ q_inv, int parts,
+template <class H, bool SPLIT, bool BEST>
+__global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Rows16 Q, int steps, float c2, const Largest *__restrict__ largest, const float *__restrict__ q_inv, int parts,
                                                                     int others, float4 *__restrict__ stats, float *__restrict__ gmax, int64_t gstride)
 {
     extern __shared__ char lds[];
@@ -262,14 +262,14 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         cq[j] = c2;
-        if (TERMS > 1) {
+        if (SPLIT) {
             const int64_t q = min(q0 + acc_col(j), Q.rows - 1);
             cq[j] = c2 * q_inv[q] * (1.0f / range_scale(largest->points));
         }
         m[j] = -INFINITY;
         l[j] = t[j] = 0.0f;
     }
-    run_tiles<H, TERMS, BEST, RowCopies>(X, Q, halves, count, lds, [&](int i, RowCopies &c) { c.seek(X, (first + i) * kTileM, Q, q0); },
+    run_tiles<H, SPLIT, BEST, RowCopies>(X, Q, steps, count, lds, [&](int i, RowCopies &c) { c.seek(X, (first + i) * kTileM, Q, q0); },
         [&](int i, f32x16 (&acc)[4][2]) {
             const int64_t row0 = (first + i) * kTileM;
             const bool whole = row0 + kTileM <= X.rows;
@@ -566,8 +566,8 @@ constexpr size_t kPackBytes = (size_t)1 << 30; // most that packed rows take at 
 struct ProbScratch {
     float4 *stats; float *gmax; int64_t gstride;
     int groups, qt, query_tiles;                         // stream
-    bool pack; int width, parts, launches; int64_t part; // tiles: rows a launch
-    uint16_t *x16, *q16; int64_t x_plane, q_plane; float *q_inv; Largest *largest;
+    bool pack; int width, parts, launches; int64_t part, ld; // tiles: rows a launch, elements of a packed row
+    uint16_t *x16, *q16; float *q_inv; Largest *largest;
     size_t bytes;
 };
 
@@ -587,23 +587,22 @@ static ProbScratch prob_scratch(const ProbParams &p, void *base)
         s.groups = stream_groups(p.n, s.query_tiles);
         s.stats = (float4 *)take((size_t)s.groups * p.nq * sizeof(float4));
     } else {
-        const int planes = p.type == AVQ_F32 ? 2 : 1;
-        s.width = (p.d + 31) / 32 * 32;
+        const bool split = p.type == AVQ_F32;
+        s.width = split ? (p.d + 15) / 16 * 16 : (p.d + 31) / 32 * 32;
+        s.ld = split ? 2 * s.width : s.width;
         // (base == NULL: the size for rows that need packing, whatever their place and stride)
-        s.pack = !base || p.type == AVQ_F32 || s.width != p.d || (uintptr_t)p.points % 16 != 0 || p.ld_points % 8 != 0;
+        s.pack = !base || p.type == AVQ_F32 || s.width != p.d || (uintptr_t)p.points % 16 != 0 || p.ld_points % 8 != 0 || p.ld_points >= kMaxLd16;
         s.part = p.n;
-        if (s.pack) s.part = std::min<int64_t>(p.n, std::max<int64_t>(65536, (int64_t)(kPackBytes / (2 * planes * (size_t)s.width)) / kTileM * kTileM));
+        if (s.pack) s.part = std::min<int64_t>(p.n, std::max<int64_t>(65536, (int64_t)(kPackBytes / (2 * (size_t)s.ld)) / kTileM * kTileM));
         s.launches = (int)((p.n + s.part - 1) / s.part);
         s.query_tiles = (p.nq + kTileN - 1) / kTileN;
         s.parts = parts_for((s.part + kTileM - 1) / kTileM, s.query_tiles, kTileGroups);
         // (as many statistics with one launch as with several: the number of parts only falls with the rows a launch has)
         s.stats = (float4 *)take((size_t)s.launches * std::max(s.parts, parts_for((p.n + kTileM - 1) / kTileM, s.query_tiles, kTileGroups)) * 2 * p.nq * sizeof(float4));
-        s.q_plane = (int64_t)p.nq * s.width;
-        s.q16 = (uint16_t *)take((size_t)s.q_plane * 2 * planes);
+        s.q16 = (uint16_t *)take((size_t)p.nq * s.ld * 2);
         s.q_inv = (float *)take((size_t)p.nq * sizeof(float));
         s.largest = (Largest *)take(sizeof(Largest));
-        s.x_plane = s.part * s.width;
-        if (s.pack) s.x16 = (uint16_t *)take((size_t)s.x_plane * 2 * planes);
+        if (s.pack) s.x16 = (uint16_t *)take((size_t)s.part * s.ld * 2);
     }
     s.gmax = p.k > 0 ? (float *)take((size_t)s.gstride * p.nq * sizeof(float)) : nullptr;
     s.bytes = at;
@@ -640,35 +639,35 @@ static int stream_sized(const ProbParams &p, const ProbScratch &s, hipStream_t s
     return s.qt == 2 ? stream_run<T, 2, ALIGNED, true>(p, s, st) : stream_run<T, 4, ALIGNED, true>(p, s, st);
 }
 
-template <class H, int TERMS>
+template <class H, bool SPLIT>
 static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
 {
     const int size = type_bytes(p.type);
     const float c2 = fabsf(p.scale) * 1.44269504088896341f;
-    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, p.nq, s.width, s.q16, s.q_plane, nullptr, s.q_inv, p.scale < 0.0f, st));
-    if (TERMS > 1) {
+    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.width, s.q16, nullptr, s.q_inv, p.scale < 0.0f, st));
+    if (SPLIT) {
         AVQ_TRY(launch_clear_largest(s.largest, st));
         AVQ_TRY(launch_largest((const float *)p.points, p.n, p.d, p.ld_points, &s.largest->points, st));
     }
     static LdsLimitOnce with_best, without;
-    const Rows16 Q{s.q16, s.width, s.q_plane, p.nq};
+    const Rows16 Q{s.q16, s.ld, p.nq};
     for (int i = 0; i < s.launches; ++i) {
         const int64_t lo = i * s.part, rows = std::min<int64_t>(s.part, p.n - lo);
         const char *from = (const char *)p.points + lo * p.ld_points * size;
-        Rows16 X{(const uint16_t *)from, p.ld_points, 0, rows};
+        Rows16 X{(const uint16_t *)from, p.ld_points, rows};
         if (s.pack) {
-            AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, rows, s.width, s.x16, s.x_plane, &s.largest->points, nullptr, false, st));
-            X = Rows16{s.x16, s.width, s.x_plane, rows};
+            AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, s.width, s.x16, SPLIT ? &s.largest->points : nullptr, nullptr, false, st));
+            X = Rows16{s.x16, s.ld, rows};
         }
         float4 *stats = s.stats + (size_t)i * s.parts * 2 * p.nq;
         const dim3 grid((unsigned)(s.parts * s.query_tiles));
         if (p.k > 0) {
-            AVQ_TRY(set_lds_limit((const void *)prob_tile_kernel<H, TERMS, true>, kTileLds, &with_best));
-            prob_tile_kernel<H, TERMS, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, (p.d + 15) / 16, c2, s.largest, s.q_inv, s.parts, s.query_tiles, stats,
+            AVQ_TRY(set_lds_limit((const void *)prob_tile_kernel<H, SPLIT, true>, kTileLds, &with_best));
+            prob_tile_kernel<H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, steps_of<SPLIT>(p.d), c2, s.largest, s.q_inv, s.parts, s.query_tiles, stats,
                                                                                       s.gmax + lo / 32, s.gstride);
         } else {
-            AVQ_TRY(set_lds_limit((const void *)prob_tile_kernel<H, TERMS, false>, kTileLds, &without));
-            prob_tile_kernel<H, TERMS, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, (p.d + 15) / 16, c2, s.largest, s.q_inv, s.parts, s.query_tiles, stats, nullptr, 0);
+            AVQ_TRY(set_lds_limit((const void *)prob_tile_kernel<H, SPLIT, false>, kTileLds, &without));
+            prob_tile_kernel<H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, steps_of<SPLIT>(p.d), c2, s.largest, s.q_inv, s.parts, s.query_tiles, stats, nullptr, 0);
         }
         AVQ_HIP(hipGetLastError());
     }
@@ -692,8 +691,8 @@ static int log_probs_typed(const ProbParams &p, hipStream_t st)
     const ProbScratch s = prob_scratch(p, p.scratch);
     int parts = s.groups;
     if (by_tiles(p.nq)) {
-        if constexpr (sizeof(T) == 4) AVQ_TRY((tiles_run<f16_t, 3>(p, s, st)));
-        else AVQ_TRY((tiles_run<T, 1>(p, s, st)));
+        if constexpr (sizeof(T) == 4) AVQ_TRY((tiles_run<f16_t, true>(p, s, st)));
+        else AVQ_TRY((tiles_run<T, false>(p, s, st)));
         parts = s.launches * s.parts * 2;
     } else {
         const bool aligned = ((uintptr_t)p.points % 16) == 0 && (p.ld_points * sizeof(T)) % 16 == 0;

@@ -3,7 +3,7 @@
 //   G_ti = sum_j g_tj [id_tj = i] - p_ti (a_t + h_t log p_ti),  a_t = sum_j g_tj - l_t + h_t H_t,
 //   dq_t = c sum_i G_ti x_i,  dx_i = c sum_t G_ti q_t.
 // Three products of 2 n nq d operations each, on the matrix instructions, a part of the rows at a time: the part's logits once
-// more, whose epilogue leaves G transposed, [row][query], in 16 bits (fp32: two f16 planes); dx = G^T Q, whose inner dimension
+// more, whose epilogue leaves G transposed, [row][query], in 16 bits (fp32: pairs of f16); dx = G^T Q, whose inner dimension
 // both operands hold side by side (Q transposed once); dq += G X by operands that are turned as they are read from LDS. G is kept
 // relative to a bound of its magnitude, so that f16 holds it down to 2^-38 of it; its rounding to 16 bits (bf16: 2^-9) is that of
 // the operands' own type. The entries of the given ids, where p is taken from g, are formed by themselves in fp32 before rounding.
@@ -46,19 +46,20 @@ __global__ __launch_bounds__(256) void grad_coef_kernel(const int32_t *__restric
     if ((threadIdx.x & 63) == 0 && m != 0) atomicMax(&largest->upstream, m);
 }
 
-__device__ __forceinline__ void put16(uint16_t *to, int64_t, float v, bf16_t) { *to = from_f32<bf16_t>(v).bits; }
-__device__ __forceinline__ void put16(uint16_t *to, int64_t, float v, f16_t) { *to = from_f32<f16_t>(v).bits; }
-__device__ __forceinline__ void put16(uint16_t *to, int64_t plane, float v, float)
+// a value as an operand: rounded to the type, or (fp32) hi and, 16 elements on, lo
+__device__ __forceinline__ void put16(uint16_t *to, float v, bf16_t) { *to = from_f32<bf16_t>(v).bits; }
+__device__ __forceinline__ void put16(uint16_t *to, float v, f16_t) { *to = from_f32<f16_t>(v).bits; }
+__device__ __forceinline__ void put16(uint16_t *to, float v, float)
 {
     const _Float16 hi = (_Float16)v;
-    *to = __builtin_bit_cast(uint16_t, hi);
-    to[plane] = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)hi));
+    to[0] = __builtin_bit_cast(uint16_t, hi);
+    to[16] = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)hi));
 }
 
 // G^T of the part's rows: 256 queries of a workgroup by 128 rows at a time. T: the caller's type, H: the instructions'.
-template <class T, class H, int TERMS, bool ENTROPY>
-__global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Rows16 X, int halves, float c2, const float *__restrict__ lse, const float2 *__restrict__ coef,
-                                                                    const Largest *__restrict__ largest, int parts, int others, uint16_t *__restrict__ G, int width, int64_t plane)
+template <class T, class H, bool SPLIT, bool ENTROPY>
+__global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Rows16 X, int steps, float c2, const float *__restrict__ lse, const float2 *__restrict__ coef,
+                                                                    const Largest *__restrict__ largest, int parts, int others, uint16_t *__restrict__ G, int width, int64_t ld)
 {
     extern __shared__ char lds[];
     __shared__ float4 shift[kTileM / 4], up[kTileM / 4], up_h[kTileM / 4]; // -lse / log 2; a and h, in G's units
@@ -77,9 +78,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
         ((float *)up)[threadIdx.x] = -c.x * f;
         if (ENTROPY) ((float *)up_h)[threadIdx.x] = -c.y * f * 0.693147180559945309f;
     }
-    const float cq = TERMS > 1 ? c2 * (1.0f / range_scale(largest->points)) * (1.0f / range_scale(largest->queries)) : c2;
+    const float cq = SPLIT ? c2 * (1.0f / range_scale(largest->points)) * (1.0f / range_scale(largest->queries)) : c2;
     __syncthreads();
-    run_tiles<H, TERMS, true, RowCopies>(Q, X, halves, count, lds, [&](int i, RowCopies &c) { c.seek(Q, q0, X, (first + i) * kTileN); },
+    run_tiles<H, SPLIT, true, RowCopies>(Q, X, steps, count, lds, [&](int i, RowCopies &c) { c.seek(Q, q0, X, (first + i) * kTileN); },
         [&](int i, f32x16 (&acc)[4][2]) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -101,15 +102,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
                             float v = p * (ENTROPY ? __fmaf_rn(hh[e], s2, u[e]) : u[e]);
                             if (ENTROPY && p == 0.0f) v = 0.0f; // (p log p)
                             if (!real) v = 0.0f;
-                            uint16_t two[2];
-                            put16(two, 1, v, T{});
+                            uint16_t two[17];
+                            put16(two, v, T{});
                             hi.e[e] = two[0];
-                            if (TERMS > 1) lo.e[e] = two[1];
+                            if (SPLIT) lo.e[e] = two[16];
                         }
                         if (q0 + t < width) {
-                            uint16_t *to = G + row * width + q0 + t;
+                            uint16_t *to = G + row * ld + place16<SPLIT>(q0 + t);
                             *(Pack<uint16_t, 4> *)to = hi;
-                            if (TERMS > 1) *(Pack<uint16_t, 4> *)(to + plane) = lo;
+                            if (SPLIT) *(Pack<uint16_t, 4> *)(to + 16) = lo;
                         }
                     }
             }
@@ -120,8 +121,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
 template <class T>
 __global__ __launch_bounds__(256) void grad_given_kernel(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, int d, float scale,
                                                          const int32_t *__restrict__ ids, int given, const float *__restrict__ g, const float *__restrict__ lse,
-                                                         const float2 *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, uint16_t *__restrict__ G, int width,
-                                                         int64_t plane)
+                                                         const float2 *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, uint16_t *__restrict__ G, int64_t ld)
 {
     const int lane = threadIdx.x & 63;
     const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(256) void grad_given_kernel(const T *__restrict__ x
     const float2 c = coef[t];
     const float p = __builtin_amdgcn_exp2f(s * 1.44269504088896341f);
     const float v = sum - (p > 0.0f || p != p ? p * __fmaf_rn(c.y, s, c.x) : 0.0f);
-    put16(G + (id - lo) * width + t, plane, v * grad_factor(largest), T{});
+    put16(G + (id - lo) * ld + place16<sizeof(T) == 4>(t), v * grad_factor(largest), T{});
 }
 
 // fn for every four rows side by side of a lane's accumulators acc[a][j][4 b ..]. One after the other: the compiler would
@@ -159,8 +159,8 @@ template <int I = 0, class Fn> __device__ __forceinline__ void for_quads(Fn fn)
 }
 
 // dx of the part's rows: 256 rows by 128 dimensions.
-template <class T, class H, int TERMS, bool ACCUMULATE>
-__global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Rows16 Qt, int halves, float scale, const Largest *__restrict__ largest, int parts, int others, int64_t rows,
+template <class T, class H, bool SPLIT, bool ACCUMULATE>
+__global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Rows16 Qt, int steps, float scale, const Largest *__restrict__ largest, int parts, int others, int64_t rows,
                                                                     int d, T *__restrict__ dx, int64_t ld_dx)
 {
     extern __shared__ char lds[];
@@ -169,8 +169,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Ro
     int64_t first;
     int count;
     part_tiles(tiles, parts, place.part, &first, &count);
-    const float f = grad_bound(largest) * (1.0f / kGradTop) * scale * (TERMS > 1 ? 1.0f / range_scale(largest->queries) : 1.0f);
-    run_tiles<H, TERMS, true, RowCopies>(G, Qt, halves, count, lds, [&](int i, RowCopies &c) { c.seek(G, (first + i) * kTileM, Qt, c0); },
+    const float f = grad_bound(largest) * (1.0f / kGradTop) * scale * (SPLIT ? 1.0f / range_scale(largest->queries) : 1.0f);
+    run_tiles<H, SPLIT, true, RowCopies>(G, Qt, steps, count, lds, [&](int i, RowCopies &c) { c.seek(G, (first + i) * kTileM, Qt, c0); },
         [&](int i, f32x16 (&acc)[4][2]) {
             const int64_t row0 = (first + i) * kTileM + acc_row(0, 0);
             const int64_t left = rows - row0; // rows from this lane's first one on
@@ -191,13 +191,14 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Ro
 }
 
 // The part's share of dq, split over the part's rows: sums[split][nq][d] in fp32, begun (first) or added to.
-template <class H, int TERMS>
+template <class H, bool SPLIT>
 __global__ __launch_bounds__(kTileThreads, 2) void grad_queries_kernel(Rows16 G, Rows16 X, int nq, int width, int d, int splits, int q_tiles, int d_tiles, int begin, float *__restrict__ sums)
 {
     extern __shared__ char lds[];
     const Place place = place_of(blockIdx.x, q_tiles * d_tiles);
     const int64_t t0 = (int64_t)(place.other % q_tiles) * kTileM, c0 = (int64_t)(place.other / q_tiles) * kTileN;
-    const int64_t steps = (G.rows + kTileK - 1) / kTileK;
+    typedef ColumnCopies<SPLIT> Copies;
+    const int64_t steps = (G.rows + Copies::kRows - 1) / Copies::kRows;
     int64_t first;
     int count;
     part_tiles(steps, splits, place.part, &first, &count);
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_queries_kernel(Rows16 G,
         if (begin) store(0, none);
         return;
     }
-    run_tiles<H, TERMS, true, ColumnCopies>(G, X, 2 * count, 1, lds, [&](int, ColumnCopies &c) { c.row = first * kTileK; c.seek(G, t0, width, X, c0); }, store);
+    run_tiles<H, SPLIT, true, Copies>(G, X, count, 1, lds, [&](int, Copies &c) { c.row = first * Copies::kRows; c.seek(G, t0, width, X, c0); }, store);
 }
 
 // dq = the splits' sums, in their order
@@ -249,8 +250,8 @@ constexpr size_t kGradBytes = (size_t)1 << 30;    // most that G of a part takes
 
 struct ProbGradScratch {
     bool pack;
-    int planes, width, qw, splits, q_tiles, d_tiles; // width: of packed rows and queries; qw: of G^T and of the transposed queries
-    int64_t part, x_plane, q_plane, qt_plane, g_plane;
+    int width, qw, splits, q_tiles, d_tiles; // width: of packed rows and queries; qw: of G^T and of the transposed queries
+    int64_t part, ld, g_ld;                  // elements of a row of those
     Largest *largest; float2 *coef; float *sums; uint16_t *q16, *qt16, *x16, *G;
     size_t bytes;
 };
@@ -258,16 +259,18 @@ struct ProbGradScratch {
 static ProbGradScratch prob_grad_scratch(const ProbGradParams &p, void *base)
 {
     ProbGradScratch s{};
-    s.planes = p.type == AVQ_F32 ? 2 : 1;
+    const int pair = p.type == AVQ_F32 ? 2 : 1;
     s.width = (p.d + kTileN - 1) / kTileN * kTileN; // (the product over rows reads whole tiles of columns)
     s.qw = (p.nq + 31) / 32 * 32;
+    s.ld = (int64_t)pair * s.width;
+    s.g_ld = (int64_t)pair * s.qw;
     // (base == NULL: the size for rows that need packing, whatever their place and stride)
-    s.pack = !base || p.type == AVQ_F32 || s.width != p.d || (uintptr_t)p.points % 16 != 0 || p.ld_points % 8 != 0;
-    const int64_t most = (int64_t)(kGradBytes / (2 * s.planes * (size_t)s.qw)) / kTileM * kTileM;
+    s.pack = !base || p.type == AVQ_F32 || s.width != p.d || (uintptr_t)p.points % 16 != 0 || p.ld_points % 8 != 0 || p.ld_points >= kMaxLd16;
+    const int64_t most = (int64_t)(kGradBytes / (2 * (size_t)s.g_ld)) / kTileM * kTileM;
     s.part = std::min<int64_t>((p.n + kTileM - 1) / kTileM * kTileM, std::max<int64_t>(4096, most));
     s.q_tiles = (p.nq + kTileM - 1) / kTileM;
     s.d_tiles = (p.d + kTileN - 1) / kTileN;
-    s.splits = parts_for(std::max<int64_t>(1, s.part / (4 * kTileK)), s.q_tiles * s.d_tiles, kGradGroups);
+    s.splits = parts_for(std::max<int64_t>(1, s.part / 128), s.q_tiles * s.d_tiles, kGradGroups);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         void *q = base ? (char *)base + at : nullptr;
@@ -277,14 +280,10 @@ static ProbGradScratch prob_grad_scratch(const ProbGradParams &p, void *base)
     s.largest = (Largest *)take(sizeof(Largest));
     s.coef = (float2 *)take(sizeof(float2) * (size_t)p.nq);
     s.sums = (float *)take(sizeof(float) * (size_t)s.splits * p.nq * p.d);
-    s.q_plane = (int64_t)p.nq * s.width;
-    s.q16 = (uint16_t *)take((size_t)s.q_plane * 2 * s.planes);
-    s.qt_plane = (int64_t)p.d * s.qw;
-    s.qt16 = (uint16_t *)take((size_t)s.qt_plane * 2 * s.planes);
-    s.g_plane = s.part * s.qw;
-    s.G = (uint16_t *)take((size_t)s.g_plane * 2 * s.planes);
-    s.x_plane = s.part * s.width;
-    if (s.pack) s.x16 = (uint16_t *)take((size_t)s.x_plane * 2 * s.planes);
+    s.q16 = (uint16_t *)take((size_t)p.nq * s.ld * 2);
+    s.qt16 = (uint16_t *)take((size_t)p.d * s.g_ld * 2);
+    s.G = (uint16_t *)take((size_t)s.part * s.g_ld * 2);
+    if (s.pack) s.x16 = (uint16_t *)take((size_t)s.part * s.ld * 2);
     s.bytes = at;
     return s;
 }
@@ -297,7 +296,7 @@ size_t log_probs_grad_scratch_bytes(int type, int64_t n, int d, int nq, int give
     return nq == 0 ? 0 : prob_grad_scratch(p, nullptr).bytes;
 }
 
-template <class T, class H, int TERMS>
+template <class T, class H, bool SPLIT>
 static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
 {
     if (p.nq == 0) {
@@ -309,58 +308,58 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
     }
     const ProbGradScratch s = prob_grad_scratch(p, p.scratch);
     static LdsLimitOnce once[5];
-    AVQ_TRY(set_lds_limit((const void *)grad_tile_kernel<T, H, TERMS, false>, kTileLds, &once[0]));
-    AVQ_TRY(set_lds_limit((const void *)grad_tile_kernel<T, H, TERMS, true>, kTileLds, &once[1]));
-    AVQ_TRY(set_lds_limit((const void *)grad_rows_kernel<T, H, TERMS, false>, kTileLds, &once[2]));
-    AVQ_TRY(set_lds_limit((const void *)grad_rows_kernel<T, H, TERMS, true>, kTileLds, &once[4]));
-    AVQ_TRY(set_lds_limit((const void *)grad_queries_kernel<H, TERMS>, kTileLds, &once[3]));
+    AVQ_TRY(set_lds_limit((const void *)grad_tile_kernel<T, H, SPLIT, false>, kTileLds, &once[0]));
+    AVQ_TRY(set_lds_limit((const void *)grad_tile_kernel<T, H, SPLIT, true>, kTileLds, &once[1]));
+    AVQ_TRY(set_lds_limit((const void *)grad_rows_kernel<T, H, SPLIT, false>, kTileLds, &once[2]));
+    AVQ_TRY(set_lds_limit((const void *)grad_rows_kernel<T, H, SPLIT, true>, kTileLds, &once[4]));
+    AVQ_TRY(set_lds_limit((const void *)grad_queries_kernel<H, SPLIT>, kTileLds, &once[3]));
     const float c2 = p.scale * 1.44269504088896341f;
     const T *q = (const T *)p.queries;
     AVQ_TRY(launch_clear_largest(s.largest, st));
     grad_coef_kernel<<<dim3((p.nq + 255) / 256), dim3(256), 0, st>>>(p.ids, p.n, p.nq, p.given, p.grad_logp, p.grad_entropy, p.entropy, p.grad_lse, s.coef, s.largest);
     AVQ_HIP(hipGetLastError());
-    if (TERMS > 1) {
+    if (SPLIT) {
         AVQ_TRY(launch_largest((const float *)p.points, p.n, p.d, p.ld_points, &s.largest->points, st));
         AVQ_TRY(launch_largest((const float *)p.queries, p.nq, p.d, p.ld_queries, &s.largest->queries, st));
     }
-    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, p.nq, s.width, s.q16, s.q_plane, &s.largest->queries, nullptr, false, st));
-    if (p.dpoints) AVQ_TRY(launch_pack_transposed(p.queries, p.type, p.nq, p.d, p.ld_queries, p.d, s.qw, s.qt16, s.qt_plane, &s.largest->queries, st));
-    const Rows16 Q{s.q16, s.width, s.q_plane, p.nq}, Qt{s.qt16, s.qw, s.qt_plane, p.d};
+    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.width, s.q16, SPLIT ? &s.largest->queries : nullptr, nullptr, false, st));
+    if (p.dpoints) AVQ_TRY(launch_pack_transposed(p.queries, p.type, p.nq, p.d, p.ld_queries, s.qw, s.qt16, &s.largest->queries, st));
+    const Rows16 Q{s.q16, s.ld, p.nq}, Qt{s.qt16, s.g_ld, p.d};
     for (int64_t lo = 0; lo < p.n; lo += s.part) {
         const int64_t rows = std::min<int64_t>(s.part, p.n - lo), whole = (rows + kTileN - 1) / kTileN * kTileN; // rows past the last have G = 0
         const T *x = (const T *)p.points + lo * p.ld_points;
-        Rows16 X{(const uint16_t *)x, p.ld_points, 0, rows};
+        Rows16 X{(const uint16_t *)x, p.ld_points, rows};
         if (s.pack) {
-            AVQ_TRY(launch_pack_rows(x, p.type, rows, p.d, p.ld_points, rows, s.width, s.x16, s.x_plane, &s.largest->points, nullptr, false, st));
-            X = Rows16{s.x16, s.width, s.x_plane, rows};
+            AVQ_TRY(launch_pack_rows(x, p.type, rows, p.d, p.ld_points, s.width, s.x16, SPLIT ? &s.largest->points : nullptr, nullptr, false, st));
+            X = Rows16{s.x16, s.ld, rows};
         }
-        const Rows16 G{s.G, s.qw, s.g_plane, whole};
+        const Rows16 G{s.G, s.g_ld, whole};
         const int parts = parts_for((rows + kTileN - 1) / kTileN, s.q_tiles, kGradGroups);
         const dim3 grid((unsigned)(parts * s.q_tiles));
-        if (p.grad_entropy) grad_tile_kernel<T, H, TERMS, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, (p.d + 15) / 16, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, s.g_plane);
-        else grad_tile_kernel<T, H, TERMS, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, (p.d + 15) / 16, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, s.g_plane);
+        if (p.grad_entropy) grad_tile_kernel<T, H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, steps_of<SPLIT>(p.d), c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, s.g_ld);
+        else grad_tile_kernel<T, H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, steps_of<SPLIT>(p.d), c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, s.g_ld);
         AVQ_HIP(hipGetLastError());
         if (p.given > 0) {
             grad_given_kernel<T><<<dim3((unsigned)(((int64_t)p.nq * p.given + 3) / 4)), dim3(256), 0, st>>>((const T *)p.points, p.ld_points, q, p.nq, p.ld_queries, p.d, p.scale, p.ids, p.given,
-                                                                                                        p.grad_logp, p.lse, s.coef, s.largest, lo, rows, s.G, s.qw, s.g_plane);
+                                                                                                        p.grad_logp, p.lse, s.coef, s.largest, lo, rows, s.G, s.g_ld);
             AVQ_HIP(hipGetLastError());
         }
         if (p.dpoints) {
             const int row_parts = parts_for((rows + kTileM - 1) / kTileM, s.d_tiles, kGradGroups);
             const dim3 row_grid((unsigned)(row_parts * s.d_tiles));
             T *dx = (T *)p.dpoints + lo * p.ld_dpoints;
-            if (p.accumulate) grad_rows_kernel<T, H, TERMS, true><<<row_grid, dim3(kTileThreads), kTileLds, st>>>(G, Qt, (p.nq + 15) / 16, p.scale, s.largest, row_parts, s.d_tiles, rows, p.d, dx, p.ld_dpoints);
-            else grad_rows_kernel<T, H, TERMS, false><<<row_grid, dim3(kTileThreads), kTileLds, st>>>(G, Qt, (p.nq + 15) / 16, p.scale, s.largest, row_parts, s.d_tiles, rows, p.d, dx, p.ld_dpoints);
+            if (p.accumulate) grad_rows_kernel<T, H, SPLIT, true><<<row_grid, dim3(kTileThreads), kTileLds, st>>>(G, Qt, steps_of<SPLIT>(p.nq), p.scale, s.largest, row_parts, s.d_tiles, rows, p.d, dx, p.ld_dpoints);
+            else grad_rows_kernel<T, H, SPLIT, false><<<row_grid, dim3(kTileThreads), kTileLds, st>>>(G, Qt, steps_of<SPLIT>(p.nq), p.scale, s.largest, row_parts, s.d_tiles, rows, p.d, dx, p.ld_dpoints);
             AVQ_HIP(hipGetLastError());
         }
         if (p.dqueries) {
-            grad_queries_kernel<H, TERMS><<<dim3((unsigned)(s.splits * s.q_tiles * s.d_tiles)), dim3(kTileThreads), kTileLds, st>>>(G, X, p.nq, s.qw, p.d, s.splits, s.q_tiles, s.d_tiles,
+            grad_queries_kernel<H, SPLIT><<<dim3((unsigned)(s.splits * s.q_tiles * s.d_tiles)), dim3(kTileThreads), kTileLds, st>>>(G, X, p.nq, s.qw, p.d, s.splits, s.q_tiles, s.d_tiles,
                                                                                                                              lo == 0, s.sums);
             AVQ_HIP(hipGetLastError());
         }
     }
     if (p.dqueries) {
-        grad_join_kernel<T><<<dim3((unsigned)(((int64_t)p.nq * p.d + 255) / 256)), dim3(256), 0, st>>>(s.sums, s.splits, p.nq, p.d, p.scale, TERMS > 1, s.largest, (T *)p.dqueries,
+        grad_join_kernel<T><<<dim3((unsigned)(((int64_t)p.nq * p.d + 255) / 256)), dim3(256), 0, st>>>(s.sums, s.splits, p.nq, p.d, p.scale, SPLIT, s.largest, (T *)p.dqueries,
                                                                                                    p.ld_dqueries);
         AVQ_HIP(hipGetLastError());
     }
@@ -369,8 +368,8 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
 
 int launch_log_probs_grad(const ProbGradParams &p, hipStream_t st)
 {
-    if (p.type == AVQ_F32) return log_probs_grad_typed<float, f16_t, 3>(p, st);
-    return p.type == AVQ_BF16 ? log_probs_grad_typed<bf16_t, bf16_t, 1>(p, st) : log_probs_grad_typed<f16_t, f16_t, 1>(p, st);
+    if (p.type == AVQ_F32) return log_probs_grad_typed<float, f16_t, true>(p, st);
+    return p.type == AVQ_BF16 ? log_probs_grad_typed<bf16_t, bf16_t, false>(p, st) : log_probs_grad_typed<f16_t, f16_t, false>(p, st);
 }
 
 } // namespace avq

@@ -1,5 +1,5 @@
-// Rows laid out as operands of the 16-bit matrix instructions (mma_tiles.h): padded, and fp32 as two f16 planes.
-// Bound by memory: rows read once, both planes written once.
+// Rows laid out as operands of the 16-bit matrix instructions (mma_tiles.h): padded, and fp32 as pairs of f16.
+// Bound by memory: rows read once, operands written once.
 #include "mma_tiles.h"
 
 namespace avq {
@@ -71,82 +71,78 @@ __device__ __forceinline__ void split_f16(float v, uint16_t *hi, uint16_t *lo)
 
 // eight elements a thread; WHOLE: a row is a whole number of eights on 16 bytes
 template <class T, bool WHOLE>
-__global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int64_t rows_out, int per_row, uint32_t magic,
-                                                        uint16_t *__restrict__ out, int64_t plane, const uint32_t *__restrict__ largest, uint16_t flip)
+__global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int per_row, uint32_t magic, uint16_t *__restrict__ out,
+                                                        const uint32_t *__restrict__ largest, uint16_t flip)
 {
+    constexpr bool SPLIT = sizeof(T) == 4;
     const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / per_row;
     const uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x, dr = magic_div(at, magic);
     const int64_t row = row0 + dr;
-    if (row >= rows_out) return;
+    if (row >= rows) return;
     const int c = (int)(at - dr * (uint32_t)per_row) * 8;
     T v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = T{};
-    if (row < rows) {
-        const T *from = x + row * ld + c;
-        if (WHOLE || c + 8 <= d) {
-            if (!WHOLE || c < d) __builtin_memcpy(v, WHOLE ? __builtin_assume_aligned(from, 16) : from, sizeof(v));
-        } else {
+    const T *from = x + row * ld + c;
+    if (WHOLE || c + 8 <= d) {
+        if (!WHOLE || c < d) __builtin_memcpy(v, WHOLE ? __builtin_assume_aligned(from, 16) : from, sizeof(v));
+    } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (c + e < d) v[e] = from[e];
-        }
+        for (int e = 0; e < 8; ++e)
+            if (c + e < d) v[e] = from[e];
     }
+    uint16_t *to = out + row * (int64_t)per_row * (SPLIT ? 16 : 8) + place16<SPLIT>(c);
     Pack<uint16_t, 8> hi, lo;
-    if constexpr (sizeof(T) == 4) {
+    if constexpr (SPLIT) {
         const float s = range_scale(*largest);
 #pragma unroll
         for (int e = 0; e < 8; ++e) split_f16(v[e] * s, &hi.e[e], &lo.e[e]);
-        *(Pack<uint16_t, 8> *)(out + plane + row * (int64_t)per_row * 8 + c) = lo;
+        *(Pack<uint16_t, 8> *)(to + 16) = lo;
     } else {
         __builtin_memcpy(&hi, v, 16);
 #pragma unroll
         for (int e = 0; e < 8; ++e) hi.e[e] ^= flip;
     }
-    *(Pack<uint16_t, 8> *)(out + row * (int64_t)per_row * 8 + c) = hi;
+    *(Pack<uint16_t, 8> *)to = hi;
 }
 
 // each row by its own scale, a workgroup a row
-__global__ __launch_bounds__(256) void pack_own_scale_kernel(const float *__restrict__ x, int64_t rows, int d, int64_t ld, int width, uint16_t *__restrict__ out, int64_t plane,
-                                                             float *__restrict__ inv, float sign)
+__global__ __launch_bounds__(256) void pack_own_scale_kernel(const float *__restrict__ x, int d, int64_t ld, int width, uint16_t *__restrict__ out, float *__restrict__ inv, float sign)
 {
     __shared__ uint32_t red[4];
     const int64_t row = blockIdx.x;
     uint32_t m = 0;
-    if (row < rows)
-        for (int c = threadIdx.x; c < d; c += 256) m = max(m, finite_bits(x[row * ld + c]));
+    for (int c = threadIdx.x; c < d; c += 256) m = max(m, finite_bits(x[row * ld + c]));
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, w, 64));
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
     __syncthreads();
     const float s = range_scale(max(max(red[0], red[1]), max(red[2], red[3])));
     for (int c = threadIdx.x; c < width; c += 256) {
-        uint16_t hi, lo;
-        split_f16(row < rows && c < d ? x[row * ld + c] * (s * sign) : 0.0f, &hi, &lo);
-        out[row * width + c] = hi;
-        out[plane + row * width + c] = lo;
+        uint16_t *to = out + row * width * 2 + place16<true>(c);
+        split_f16(c < d ? x[row * ld + c] * (s * sign) : 0.0f, to, to + 16);
     }
-    if (threadIdx.x == 0 && row < rows) inv[row] = 1.0f / s;
+    if (threadIdx.x == 0) inv[row] = 1.0f / s;
 }
 
-int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int64_t rows_out, int width, uint16_t *out, int64_t plane, const uint32_t *largest, float *inv,
-                     bool negate, hipStream_t st)
+int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int width, uint16_t *out, const uint32_t *largest, float *inv, bool negate, hipStream_t st)
 {
     if (type == AVQ_F32 && !largest) {
-        pack_own_scale_kernel<<<dim3((unsigned)rows_out), dim3(256), 0, st>>>((const float *)x, rows, d, ld, width, out, plane, inv, negate ? -1.0f : 1.0f);
+        pack_own_scale_kernel<<<dim3((unsigned)rows), dim3(256), 0, st>>>((const float *)x, d, ld, width, out, inv, negate ? -1.0f : 1.0f);
         AVQ_HIP(hipGetLastError());
         return AVQ_OK;
     }
     const int per_row = width / 8;
-    const dim3 grid((unsigned)((rows_out * per_row + 255) / 256));
+    const dim3 grid((unsigned)((rows * per_row + 255) / 256));
     const uint32_t magic = magic_of(per_row);
     const bool whole = row_width(x, ld, d, type_bytes(type)) == 16 && d % 8 == 0;
+    const uint16_t flip = negate ? 0x8000 : 0;
     if (type == AVQ_F32) {
-        if (whole) pack_rows_kernel<float, true><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, rows_out, per_row, magic, out, plane, largest, 0);
-        else pack_rows_kernel<float, false><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, rows_out, per_row, magic, out, plane, largest, 0);
+        if (whole) pack_rows_kernel<float, true><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, per_row, magic, out, largest, 0);
+        else pack_rows_kernel<float, false><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, per_row, magic, out, largest, 0);
     } else {
-        if (whole) pack_rows_kernel<uint16_t, true><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, rows_out, per_row, magic, out, plane, nullptr, negate ? 0x8000 : 0);
-        else pack_rows_kernel<uint16_t, false><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, rows_out, per_row, magic, out, plane, nullptr, negate ? 0x8000 : 0);
+        if (whole) pack_rows_kernel<uint16_t, true><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, per_row, magic, out, nullptr, flip);
+        else pack_rows_kernel<uint16_t, false><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, per_row, magic, out, nullptr, flip);
     }
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
@@ -154,8 +150,8 @@ int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, i
 
 // 64 x 64 elements a workgroup, turned in LDS
 template <class T>
-__global__ __launch_bounds__(256) void pack_transposed_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int columns_out, int width, uint16_t *__restrict__ out,
-                                                              int64_t plane, const uint32_t *__restrict__ largest)
+__global__ __launch_bounds__(256) void pack_transposed_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int width, uint16_t *__restrict__ out,
+                                                              const uint32_t *__restrict__ largest)
 {
     __shared__ T tile[64][65];
     const int64_t t0 = (int64_t)blockIdx.x * 64;
@@ -171,23 +167,21 @@ __global__ __launch_bounds__(256) void pack_transposed_kernel(const T *__restric
     for (int i = threadIdx.x; i < 4096; i += 256) {
         const int c = c0 + (i >> 6);
         const int64_t t = t0 + (i & 63);
-        if (c >= columns_out || t >= width) continue;
+        if (c >= d || t >= width) continue;
         if constexpr (sizeof(T) == 4) {
-            uint16_t hi, lo;
-            split_f16(tile[i & 63][i >> 6] * s, &hi, &lo);
-            out[(int64_t)c * width + t] = hi;
-            out[plane + (int64_t)c * width + t] = lo;
+            uint16_t *to = out + (int64_t)c * width * 2 + place16<true>(t);
+            split_f16(tile[i & 63][i >> 6] * s, to, to + 16);
         } else {
             out[(int64_t)c * width + t] = tile[i & 63][i >> 6];
         }
     }
 }
 
-int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int columns_out, int width, uint16_t *out, int64_t plane, const uint32_t *largest, hipStream_t st)
+int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int width, uint16_t *out, const uint32_t *largest, hipStream_t st)
 {
-    const dim3 grid((unsigned)((width + 63) / 64), (unsigned)((columns_out + 63) / 64));
-    if (type == AVQ_F32) pack_transposed_kernel<float><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, columns_out, width, out, plane, largest);
-    else pack_transposed_kernel<uint16_t><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, columns_out, width, out, plane, nullptr);
+    const dim3 grid((unsigned)((width + 63) / 64), (unsigned)((d + 63) / 64));
+    if (type == AVQ_F32) pack_transposed_kernel<float><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, width, out, largest);
+    else pack_transposed_kernel<uint16_t><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, width, out, nullptr);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
