@@ -29,13 +29,18 @@ constexpr int kTileM = 256, kTileN = 128, kStepBytes = 64 /* of a row */, kTileT
 constexpr int kStageA = kTileM * kStepBytes, kStageB = kTileN * kStepBytes, kStageBytes = kStageA + kStageB, kStages = 3;
 constexpr int kTileLds = kStages * kStageBytes;
 
-// Rows of 16-bit elements (SPLIT: of pairs of them): `rows` of them, ld elements apart, 16-byte aligned.
-struct Rows16 { const uint16_t *p; int64_t ld, rows; };
-constexpr int64_t kMaxLd16 = (int64_t)1 << 22; // (256 rows' places are 32-bit offsets)
+// Rows of 16-bit elements (SPLIT: of pairs of them): `rows` of them, `row` elements apart, 16-byte aligned; a step's 32 elements lie
+// `step` elements after the step's before. Rows as a caller has them: step = 32. Packed ones: row = 32, so that the rows of a
+// step lie side by side and copies read whole lines (a step of 64 bytes a row is half a line, and the copies of the products over
+// rows, which read 512 bytes at a time, reached 1,020 TFLOP/s where those of 64 bytes reached 770).
+struct Rows16 { const uint16_t *p; int64_t row, step, rows; };
+constexpr int64_t kMaxRow16 = (int64_t)1 << 22; // (256 rows' places are 32-bit offsets)
+constexpr int kStepElems16 = 32;
 
-// Where element c of a row lies; SPLIT: its hi, 16 elements before its lo.
-template <bool SPLIT> __host__ __device__ inline int64_t place16(int64_t c) { return SPLIT ? (c >> 4) * 32 + (c & 15) : c; }
-// The steps that an inner dimension of d takes, and the elements a row of it must have.
+// The step that element c of a row belongs to, and its place there; SPLIT: of its hi, 16 elements before its lo.
+template <bool SPLIT> __host__ __device__ inline int64_t step16(int64_t c) { return SPLIT ? c >> 4 : c >> 5; }
+template <bool SPLIT> __host__ __device__ inline int in_step16(int64_t c) { return (int)(SPLIT ? c & 15 : c & 31); }
+// The steps that an inner dimension of d takes.
 template <bool SPLIT> __host__ __device__ inline int steps_of(int64_t d) { return (int)((d + (SPLIT ? 15 : 31)) / (SPLIT ? 16 : 32)); }
 
 __device__ __forceinline__ f32x16 mma32(const Quad &a, const Quad &b, f32x16 c, bf16_t)
@@ -69,17 +74,17 @@ struct RowCopies {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         const uint32_t chunk = (uint32_t)((lane & 3) ^ ((lane >> 4) & 3)) * 16;
         const int last_a = (int)min(A.rows - 1 - a0, (int64_t)kTileM), last_b = (int)min(B.rows - 1 - b0, (int64_t)kTileN);
-        pa = (const char *)(A.p + a0 * A.ld);
-        pb = (const char *)(B.p + b0 * B.ld);
+        pa = (const char *)(A.p + a0 * A.row);
+        pb = (const char *)(B.p + b0 * B.row);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = (uint32_t)min((wave * 4 + j) * 16 + (lane >> 2), last_a) * (uint32_t)(A.ld * 2) + chunk;
+        for (int j = 0; j < 4; ++j) a[j] = (uint32_t)min((wave * 4 + j) * 16 + (lane >> 2), last_a) * (uint32_t)(A.row * 2) + chunk;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) b[j] = (uint32_t)min((wave * 2 + j) * 16 + (lane >> 2), last_b) * (uint32_t)(B.ld * 2) + chunk;
+        for (int j = 0; j < 2; ++j) b[j] = (uint32_t)min((wave * 2 + j) * 16 + (lane >> 2), last_b) * (uint32_t)(B.row * 2) + chunk;
     }
-    __device__ __forceinline__ void issue(const Rows16 &, const Rows16 &, int step, uint32_t stage) const
+    __device__ __forceinline__ void issue(const Rows16 &A, const Rows16 &B, int step, uint32_t stage) const
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const char *fa = pa + (int64_t)step * kStepBytes, *fb = pb + (int64_t)step * kStepBytes;
+        const char *fa = pa + step * A.step * 2, *fb = pb + step * B.step * 2;
 #pragma unroll
         for (int j = 0; j < 4; ++j) lds_copy16_from(fa, a[j], stage + (wave * 4 + j) * 1024);
 #pragma unroll
@@ -111,27 +116,28 @@ template <bool SPLIT> struct ColumnCopies {
     {
         // (columns of A past its last come from its last: nothing uses their products; B is as wide as its tiles)
         const int lane = threadIdx.x & 63;
-        const int last = (int)min((place16<SPLIT>(a_columns) - place16<SPLIT>(a0)) / 8 - 1, (int64_t)kChunksA);
-        pa = (const char *)(A.p + place16<SPLIT>(a0));
-        pb = (const char *)(B.p + place16<SPLIT>(b0));
+        const int last = (int)min((step16<SPLIT>(a_columns) - step16<SPLIT>(a0)) * 4 - 1, (int64_t)kChunksA);
+        pa = (const char *)(A.p + step16<SPLIT>(a0) * A.step);
+        pb = (const char *)(B.p + step16<SPLIT>(b0) * B.step);
+        auto at = [](int chunk, const Rows16 &r) { return (uint32_t)(chunk >> 2) * (uint32_t)(r.step * 2) + (uint32_t)(chunk & 3) * 16; };
 #pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = (uint32_t)min((lane % kChunksA) ^ turn((j * (64 / kChunksA) + lane / kChunksA + (SPLIT ? (threadIdx.x >> 6) * 4 : 0)) & 3), last) * 16;
+        for (int j = 0; j < 4; ++j) a[j] = at(min((lane % kChunksA) ^ turn((j * (64 / kChunksA) + lane / kChunksA + (SPLIT ? (threadIdx.x >> 6) * 4 : 0)) & 3), last), A);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) b[j] = (uint32_t)((lane % kChunksB) ^ turn((j * (64 / kChunksB) + lane / kChunksB) & 3)) * 16;
+        for (int j = 0; j < 2; ++j) b[j] = at((lane % kChunksB) ^ turn((j * (64 / kChunksB) + lane / kChunksB) & 3), B);
     }
     __device__ __forceinline__ void issue(const Rows16 &A, const Rows16 &B, int step, uint32_t stage) const
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         // (a step's rows past an operand's last, of which a whole step may consist, are its last row)
         const int64_t first = row + (int64_t)step * kRows, first_a = min(first, A.rows - 1), first_b = min(first, B.rows - 1);
-        const char *fa = pa + first_a * A.ld * 2, *fb = pb + first_b * B.ld * 2;
+        const char *fa = pa + first_a * A.row * 2, *fb = pb + first_b * B.row * 2;
         const int last_a = (int)min(A.rows - 1 - first_a, (int64_t)kRows), last_b = (int)min(B.rows - 1 - first_b, (int64_t)kRows);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            lds_copy16_from(fa, (uint32_t)min((wave * 4 + j) * (64 / kChunksA) + lane / kChunksA, last_a) * (uint32_t)(A.ld * 2) + a[j], stage + (wave * 4 + j) * 1024);
+            lds_copy16_from(fa, (uint32_t)min((wave * 4 + j) * (64 / kChunksA) + lane / kChunksA, last_a) * (uint32_t)(A.row * 2) + a[j], stage + (wave * 4 + j) * 1024);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-            lds_copy16_from(fb, (uint32_t)min((wave * 2 + j) * (64 / kChunksB) + lane / kChunksB, last_b) * (uint32_t)(B.ld * 2) + b[j], stage + kStageA + (wave * 2 + j) * 1024);
+            lds_copy16_from(fb, (uint32_t)min((wave * 2 + j) * (64 / kChunksB) + lane / kChunksB, last_b) * (uint32_t)(B.row * 2) + b[j], stage + kStageA + (wave * 2 + j) * 1024);
     }
     static __device__ __forceinline__ Quad read_turned(const char *p, int row_bytes)
     {
@@ -256,13 +262,11 @@ __device__ __forceinline__ float range_scale(uint32_t largest_bits)
 int launch_clear_largest(Largest *to, hipStream_t st);
 // max over finite elements into *to
 int launch_largest(const float *x, int64_t rows, int d, int64_t ld, uint32_t *to, hipStream_t st);
-// Rows as 16-bit elements padded with zeros to `width` (a multiple of 16) elements.
-// fp32: pairs (a row has 2 width elements), scaled by range_scale(*largest), or, largest == NULL, each row by its own, whose inverse
-// goes to inv[row].
-// negate: with the other sign (16-bit types, and rows with scales of their own).
-int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int width, uint16_t *out, const uint32_t *largest, float *inv, bool negate,
+// Packed rows: out[step][row of `total`][32], `steps` steps, zeros past a row's end. fp32: pairs, scaled by range_scale(*largest), or,
+// largest == NULL, each row by its own, whose inverse goes to inv[row]. negate: with the other sign.
+int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, int64_t total, uint16_t *out, const uint32_t *largest, float *inv, bool negate,
                      hipStream_t st);
-// The transpose: row c < d of out holds x[t][c] at t < width (a multiple of 16; zeros past rows).
-int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int width, uint16_t *out, const uint32_t *largest, hipStream_t st);
+// The transpose packed: row c < d of d holds x[t][c], zeros past the last t.
+int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, uint16_t *out, const uint32_t *largest, hipStream_t st);
 
 } // namespace avq

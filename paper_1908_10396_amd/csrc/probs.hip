@@ -566,7 +566,7 @@ constexpr size_t kPackBytes = (size_t)1 << 30; // most that packed rows take at 
 struct ProbScratch {
     float4 *stats; float *gmax; int64_t gstride;
     int groups, qt, query_tiles;                         // stream
-    bool pack; int width, parts, launches; int64_t part, ld; // tiles: rows a launch, elements of a packed row
+    bool pack; int steps, parts, launches; int64_t part; // tiles: steps of an inner product, rows a launch
     uint16_t *x16, *q16; float *q_inv; Largest *largest;
     size_t bytes;
 };
@@ -588,21 +588,21 @@ static ProbScratch prob_scratch(const ProbParams &p, void *base)
         s.stats = (float4 *)take((size_t)s.groups * p.nq * sizeof(float4));
     } else {
         const bool split = p.type == AVQ_F32;
-        s.width = split ? (p.d + 15) / 16 * 16 : (p.d + 31) / 32 * 32;
-        s.ld = split ? 2 * s.width : s.width;
+        s.steps = split ? steps_of<true>(p.d) : steps_of<false>(p.d);
+        const size_t row_bytes = (size_t)s.steps * kStepBytes; // of a packed row
         // (base == NULL: the size for rows that need packing, whatever their place and stride)
-        s.pack = !base || p.type == AVQ_F32 || s.width != p.d || (uintptr_t)p.points % 16 != 0 || p.ld_points % 8 != 0 || p.ld_points >= kMaxLd16;
+        s.pack = !base || p.type == AVQ_F32 || p.d % 32 != 0 || (uintptr_t)p.points % 16 != 0 || p.ld_points % 8 != 0 || p.ld_points >= kMaxRow16;
         s.part = p.n;
-        if (s.pack) s.part = std::min<int64_t>(p.n, std::max<int64_t>(65536, (int64_t)(kPackBytes / (2 * (size_t)s.ld)) / kTileM * kTileM));
+        if (s.pack) s.part = std::min<int64_t>(p.n, std::max<int64_t>(65536, (int64_t)(kPackBytes / row_bytes) / kTileM * kTileM));
         s.launches = (int)((p.n + s.part - 1) / s.part);
         s.query_tiles = (p.nq + kTileN - 1) / kTileN;
         s.parts = parts_for((s.part + kTileM - 1) / kTileM, s.query_tiles, kTileGroups);
         // (as many statistics with one launch as with several: the number of parts only falls with the rows a launch has)
         s.stats = (float4 *)take((size_t)s.launches * std::max(s.parts, parts_for((p.n + kTileM - 1) / kTileM, s.query_tiles, kTileGroups)) * 2 * p.nq * sizeof(float4));
-        s.q16 = (uint16_t *)take((size_t)p.nq * s.ld * 2);
+        s.q16 = (uint16_t *)take((size_t)p.nq * row_bytes);
         s.q_inv = (float *)take((size_t)p.nq * sizeof(float));
         s.largest = (Largest *)take(sizeof(Largest));
-        if (s.pack) s.x16 = (uint16_t *)take((size_t)s.part * s.ld * 2);
+        if (s.pack) s.x16 = (uint16_t *)take((size_t)s.part * row_bytes);
     }
     s.gmax = p.k > 0 ? (float *)take((size_t)s.gstride * p.nq * sizeof(float)) : nullptr;
     s.bytes = at;
@@ -644,30 +644,30 @@ static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
 {
     const int size = type_bytes(p.type);
     const float c2 = fabsf(p.scale) * 1.44269504088896341f;
-    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.width, s.q16, nullptr, s.q_inv, p.scale < 0.0f, st));
+    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, p.nq, s.q16, nullptr, s.q_inv, p.scale < 0.0f, st));
     if (SPLIT) {
         AVQ_TRY(launch_clear_largest(s.largest, st));
         AVQ_TRY(launch_largest((const float *)p.points, p.n, p.d, p.ld_points, &s.largest->points, st));
     }
     static LdsLimitOnce with_best, without;
-    const Rows16 Q{s.q16, s.ld, p.nq};
+    const Rows16 Q{s.q16, kStepElems16, (int64_t)p.nq * kStepElems16, p.nq};
     for (int i = 0; i < s.launches; ++i) {
         const int64_t lo = i * s.part, rows = std::min<int64_t>(s.part, p.n - lo);
         const char *from = (const char *)p.points + lo * p.ld_points * size;
-        Rows16 X{(const uint16_t *)from, p.ld_points, rows};
+        Rows16 X{(const uint16_t *)from, p.ld_points, kStepElems16, rows};
         if (s.pack) {
-            AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, s.width, s.x16, SPLIT ? &s.largest->points : nullptr, nullptr, false, st));
-            X = Rows16{s.x16, s.ld, rows};
+            AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, s.steps, rows, s.x16, SPLIT ? &s.largest->points : nullptr, nullptr, false, st));
+            X = Rows16{s.x16, kStepElems16, rows * kStepElems16, rows};
         }
         float4 *stats = s.stats + (size_t)i * s.parts * 2 * p.nq;
         const dim3 grid((unsigned)(s.parts * s.query_tiles));
         if (p.k > 0) {
             AVQ_TRY(set_lds_limit((const void *)prob_tile_kernel<H, SPLIT, true>, kTileLds, &with_best));
-            prob_tile_kernel<H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, steps_of<SPLIT>(p.d), c2, s.largest, s.q_inv, s.parts, s.query_tiles, stats,
+            prob_tile_kernel<H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, s.steps, c2, s.largest, s.q_inv, s.parts, s.query_tiles, stats,
                                                                                       s.gmax + lo / 32, s.gstride);
         } else {
             AVQ_TRY(set_lds_limit((const void *)prob_tile_kernel<H, SPLIT, false>, kTileLds, &without));
-            prob_tile_kernel<H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, steps_of<SPLIT>(p.d), c2, s.largest, s.q_inv, s.parts, s.query_tiles, stats, nullptr, 0);
+            prob_tile_kernel<H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, s.steps, c2, s.largest, s.q_inv, s.parts, s.query_tiles, stats, nullptr, 0);
         }
         AVQ_HIP(hipGetLastError());
     }

@@ -3,7 +3,7 @@
 //   G_ti = sum_j g_tj [id_tj = i] - p_ti (a_t + h_t log p_ti),  a_t = sum_j g_tj - l_t + h_t H_t,
 //   dq_t = c sum_i G_ti x_i,  dx_i = c sum_t G_ti q_t.
 // Three products of 2 n nq d operations each, on the matrix instructions, a part of the rows at a time: the part's logits once
-// more, whose epilogue leaves G transposed, [row][query], in 16 bits (fp32: pairs of f16); dx = G^T Q, whose inner dimension
+// more, whose epilogue leaves G transposed, a row's queries side by side, in 16 bits (fp32: pairs of f16); dx = G^T Q, whose inner dimension
 // both operands hold side by side (Q transposed once); dq += G X by operands that are turned as they are read from LDS. G is kept
 // relative to a bound of its magnitude, so that f16 holds it down to 2^-38 of it; its rounding to 16 bits (bf16: 2^-9) is that of
 // the operands' own type. The entries of the given ids, where p is taken from g, are formed by themselves in fp32 before rounding.
@@ -59,7 +59,7 @@ __device__ __forceinline__ void put16(uint16_t *to, float v, float)
 // G^T of the part's rows: 256 queries of a workgroup by 128 rows at a time. T: the caller's type, H: the instructions'.
 template <class T, class H, bool SPLIT, bool ENTROPY>
 __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Rows16 X, int steps, float c2, const float *__restrict__ lse, const float2 *__restrict__ coef,
-                                                                    const Largest *__restrict__ largest, int parts, int others, uint16_t *__restrict__ G, int width, int64_t ld)
+                                                                    const Largest *__restrict__ largest, int parts, int others, uint16_t *__restrict__ G, int width, int64_t total)
 {
     extern __shared__ char lds[];
     __shared__ float4 shift[kTileM / 4], up[kTileM / 4], up_h[kTileM / 4]; // -lse / log 2; a and h, in G's units
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
                             if (SPLIT) lo.e[e] = two[16];
                         }
                         if (q0 + t < width) {
-                            uint16_t *to = G + row * ld + place16<SPLIT>(q0 + t);
+                            uint16_t *to = G + (step16<SPLIT>(q0 + t) * total + row) * kStepElems16 + in_step16<SPLIT>(q0 + t);
                             *(Pack<uint16_t, 4> *)to = hi;
                             if (SPLIT) *(Pack<uint16_t, 4> *)(to + 16) = lo;
                         }
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
 template <class T>
 __global__ __launch_bounds__(256) void grad_given_kernel(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, int d, float scale,
                                                          const int32_t *__restrict__ ids, int given, const float *__restrict__ g, const float *__restrict__ lse,
-                                                         const float2 *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, uint16_t *__restrict__ G, int64_t ld)
+                                                         const float2 *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, uint16_t *__restrict__ G, int64_t total)
 {
     const int lane = threadIdx.x & 63;
     const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -143,7 +143,8 @@ __global__ __launch_bounds__(256) void grad_given_kernel(const T *__restrict__ x
     const float2 c = coef[t];
     const float p = __builtin_amdgcn_exp2f(s * 1.44269504088896341f);
     const float v = sum - (p > 0.0f || p != p ? p * __fmaf_rn(c.y, s, c.x) : 0.0f);
-    put16(G + (id - lo) * ld + place16<sizeof(T) == 4>(t), v * grad_factor(largest), T{});
+    constexpr bool SPLIT = sizeof(T) == 4;
+    put16(G + (step16<SPLIT>(t) * total + id - lo) * kStepElems16 + in_step16<SPLIT>(t), v * grad_factor(largest), T{});
 }
 
 // fn for every four rows side by side of a lane's accumulators acc[a][j][4 b ..]. One after the other: the compiler would
@@ -250,8 +251,8 @@ constexpr size_t kGradBytes = (size_t)1 << 30;    // most that G of a part takes
 
 struct ProbGradScratch {
     bool pack;
-    int width, qw, splits, q_tiles, d_tiles; // width: of packed rows and queries; qw: of G^T and of the transposed queries
-    int64_t part, ld, g_ld;                  // elements of a row of those
+    int steps, d_steps, qw, q_steps, splits, q_tiles, d_tiles; // steps of products over dimensions, of packed rows, of products over queries
+    int64_t part;                                              // rows at a time
     Largest *largest; float2 *coef; float *sums; uint16_t *q16, *qt16, *x16, *G;
     size_t bytes;
 };
@@ -260,16 +261,18 @@ static ProbGradScratch prob_grad_scratch(const ProbGradParams &p, void *base)
 {
     ProbGradScratch s{};
     const int pair = p.type == AVQ_F32 ? 2 : 1;
-    s.width = (p.d + kTileN - 1) / kTileN * kTileN; // (the product over rows reads whole tiles of columns)
-    s.qw = (p.nq + 31) / 32 * 32;
-    s.ld = (int64_t)pair * s.width;
-    s.g_ld = (int64_t)pair * s.qw;
-    // (base == NULL: the size for rows that need packing, whatever their place and stride)
-    s.pack = !base || p.type == AVQ_F32 || s.width != p.d || (uintptr_t)p.points % 16 != 0 || p.ld_points % 8 != 0 || p.ld_points >= kMaxLd16;
-    const int64_t most = (int64_t)(kGradBytes / (2 * (size_t)s.g_ld)) / kTileM * kTileM;
-    s.part = std::min<int64_t>((p.n + kTileM - 1) / kTileM * kTileM, std::max<int64_t>(4096, most));
+    const bool split = pair == 2;
     s.q_tiles = (p.nq + kTileM - 1) / kTileM;
     s.d_tiles = (p.d + kTileN - 1) / kTileN;
+    s.steps = split ? steps_of<true>(p.d) : steps_of<false>(p.d);
+    s.d_steps = s.d_tiles * (kTileN * pair / 32); // (the product over rows reads whole tiles of columns)
+    s.qw = (p.nq + 31) / 32 * 32;
+    s.q_steps = s.qw * pair / 32;
+    const size_t row_bytes = (size_t)s.d_steps * kStepBytes, g_bytes = (size_t)s.q_steps * kStepBytes;
+    // (base == NULL: the size for rows that need packing, whatever their place and stride)
+    s.pack = !base || split || p.d % kTileN != 0 || (uintptr_t)p.points % 16 != 0 || p.ld_points % 8 != 0 || p.ld_points >= kMaxRow16;
+    const int64_t most = (int64_t)(kGradBytes / std::max(row_bytes, g_bytes)) / kTileM * kTileM;
+    s.part = std::min<int64_t>((p.n + kTileM - 1) / kTileM * kTileM, std::max<int64_t>(4096, most));
     s.splits = parts_for(std::max<int64_t>(1, s.part / 128), s.q_tiles * s.d_tiles, kGradGroups);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -280,10 +283,10 @@ static ProbGradScratch prob_grad_scratch(const ProbGradParams &p, void *base)
     s.largest = (Largest *)take(sizeof(Largest));
     s.coef = (float2 *)take(sizeof(float2) * (size_t)p.nq);
     s.sums = (float *)take(sizeof(float) * (size_t)s.splits * p.nq * p.d);
-    s.q16 = (uint16_t *)take((size_t)p.nq * s.ld * 2);
-    s.qt16 = (uint16_t *)take((size_t)p.d * s.g_ld * 2);
-    s.G = (uint16_t *)take((size_t)s.part * s.g_ld * 2);
-    if (s.pack) s.x16 = (uint16_t *)take((size_t)s.part * s.ld * 2);
+    s.q16 = (uint16_t *)take((size_t)p.nq * s.steps * kStepBytes);
+    s.qt16 = (uint16_t *)take((size_t)p.d * g_bytes);
+    s.G = (uint16_t *)take((size_t)s.part * g_bytes);
+    if (s.pack) s.x16 = (uint16_t *)take((size_t)s.part * row_bytes);
     s.bytes = at;
     return s;
 }
@@ -322,26 +325,26 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         AVQ_TRY(launch_largest((const float *)p.points, p.n, p.d, p.ld_points, &s.largest->points, st));
         AVQ_TRY(launch_largest((const float *)p.queries, p.nq, p.d, p.ld_queries, &s.largest->queries, st));
     }
-    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.width, s.q16, SPLIT ? &s.largest->queries : nullptr, nullptr, false, st));
-    if (p.dpoints) AVQ_TRY(launch_pack_transposed(p.queries, p.type, p.nq, p.d, p.ld_queries, s.qw, s.qt16, &s.largest->queries, st));
-    const Rows16 Q{s.q16, s.ld, p.nq}, Qt{s.qt16, s.g_ld, p.d};
+    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, p.nq, s.q16, SPLIT ? &s.largest->queries : nullptr, nullptr, false, st));
+    if (p.dpoints) AVQ_TRY(launch_pack_transposed(p.queries, p.type, p.nq, p.d, p.ld_queries, s.q_steps, s.qt16, &s.largest->queries, st));
+    const Rows16 Q{s.q16, kStepElems16, (int64_t)p.nq * kStepElems16, p.nq}, Qt{s.qt16, kStepElems16, (int64_t)p.d * kStepElems16, p.d};
     for (int64_t lo = 0; lo < p.n; lo += s.part) {
         const int64_t rows = std::min<int64_t>(s.part, p.n - lo), whole = (rows + kTileN - 1) / kTileN * kTileN; // rows past the last have G = 0
         const T *x = (const T *)p.points + lo * p.ld_points;
-        Rows16 X{(const uint16_t *)x, p.ld_points, rows};
+        Rows16 X{(const uint16_t *)x, p.ld_points, kStepElems16, rows};
         if (s.pack) {
-            AVQ_TRY(launch_pack_rows(x, p.type, rows, p.d, p.ld_points, s.width, s.x16, SPLIT ? &s.largest->points : nullptr, nullptr, false, st));
-            X = Rows16{s.x16, s.ld, rows};
+            AVQ_TRY(launch_pack_rows(x, p.type, rows, p.d, p.ld_points, s.d_steps, rows, s.x16, SPLIT ? &s.largest->points : nullptr, nullptr, false, st));
+            X = Rows16{s.x16, kStepElems16, rows * kStepElems16, rows};
         }
-        const Rows16 G{s.G, s.g_ld, whole};
+        const Rows16 G{s.G, kStepElems16, whole * kStepElems16, whole};
         const int parts = parts_for((rows + kTileN - 1) / kTileN, s.q_tiles, kGradGroups);
         const dim3 grid((unsigned)(parts * s.q_tiles));
-        if (p.grad_entropy) grad_tile_kernel<T, H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, steps_of<SPLIT>(p.d), c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, s.g_ld);
-        else grad_tile_kernel<T, H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, steps_of<SPLIT>(p.d), c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, s.g_ld);
+        if (p.grad_entropy) grad_tile_kernel<T, H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, s.steps, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, whole);
+        else grad_tile_kernel<T, H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, s.steps, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, whole);
         AVQ_HIP(hipGetLastError());
         if (p.given > 0) {
             grad_given_kernel<T><<<dim3((unsigned)(((int64_t)p.nq * p.given + 3) / 4)), dim3(256), 0, st>>>((const T *)p.points, p.ld_points, q, p.nq, p.ld_queries, p.d, p.scale, p.ids, p.given,
-                                                                                                        p.grad_logp, p.lse, s.coef, s.largest, lo, rows, s.G, s.g_ld);
+                                                                                                        p.grad_logp, p.lse, s.coef, s.largest, lo, rows, s.G, whole);
             AVQ_HIP(hipGetLastError());
         }
         if (p.dpoints) {

@@ -69,45 +69,53 @@ __device__ __forceinline__ void split_f16(float v, uint16_t *hi, uint16_t *lo)
     *lo = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)h));
 }
 
-// eight elements a thread; WHOLE: a row is a whole number of eights on 16 bytes
+constexpr int kPackRows = 32;
+
+// 32 rows a workgroup, eight elements a thread: threads side by side write the rows of a step, 2 KB; what they read of a row's line at
+// one step comes from the cache at the next. WHOLE: a row is a whole number of eights on 16 bytes.
 template <class T, bool WHOLE>
-__global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int per_row, uint32_t magic, uint16_t *__restrict__ out,
+__global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int steps, int64_t total, uint16_t *__restrict__ out,
                                                         const uint32_t *__restrict__ largest, uint16_t flip)
 {
     constexpr bool SPLIT = sizeof(T) == 4;
-    const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / per_row;
-    const uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x, dr = magic_div(at, magic);
-    const int64_t row = row0 + dr;
+    constexpr int kEights = SPLIT ? 2 : 4, kAtOnce = 256 / (kPackRows * kEights); // eights of a step; steps at once
+    const int u = threadIdx.x % kEights, r = threadIdx.x / kEights % kPackRows, s0 = threadIdx.x / (kEights * kPackRows);
+    const int64_t row = (int64_t)blockIdx.x * kPackRows + r;
     if (row >= rows) return;
-    const int c = (int)(at - dr * (uint32_t)per_row) * 8;
-    T v[8];
+    float scale = 1.0f;
+    if (SPLIT) scale = range_scale(*largest);
+#pragma unroll 4
+    for (int s = s0; s < steps; s += kAtOnce) {
+        const int c = (s * kEights + u) * 8;
+        const T *from = x + row * ld + c;
+        T v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = T{};
-    const T *from = x + row * ld + c;
-    if (WHOLE || c + 8 <= d) {
-        if (!WHOLE || c < d) __builtin_memcpy(v, WHOLE ? __builtin_assume_aligned(from, 16) : from, sizeof(v));
-    } else {
+        for (int e = 0; e < 8; ++e) v[e] = T{};
+        if (c + 8 <= d) {
+            __builtin_memcpy(v, WHOLE ? __builtin_assume_aligned(from, 16) : from, sizeof(v));
+        } else if (!WHOLE) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (c + e < d) v[e] = from[e];
+            for (int e = 0; e < 8; ++e)
+                if (c + e < d) v[e] = from[e];
+        }
+        uint16_t *to = out + (s * total + row) * kStepElems16 + u * 8;
+        Pack<uint16_t, 8> hi, lo;
+        if constexpr (SPLIT) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) split_f16(v[e] * scale, &hi.e[e], &lo.e[e]);
+            *(Pack<uint16_t, 8> *)(to + 16) = lo;
+        } else {
+            __builtin_memcpy(&hi, v, 16);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) hi.e[e] ^= flip;
+        }
+        *(Pack<uint16_t, 8> *)to = hi;
     }
-    uint16_t *to = out + row * (int64_t)per_row * (SPLIT ? 16 : 8) + place16<SPLIT>(c);
-    Pack<uint16_t, 8> hi, lo;
-    if constexpr (SPLIT) {
-        const float s = range_scale(*largest);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) split_f16(v[e] * s, &hi.e[e], &lo.e[e]);
-        *(Pack<uint16_t, 8> *)(to + 16) = lo;
-    } else {
-        __builtin_memcpy(&hi, v, 16);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) hi.e[e] ^= flip;
-    }
-    *(Pack<uint16_t, 8> *)to = hi;
 }
 
 // each row by its own scale, a workgroup a row
-__global__ __launch_bounds__(256) void pack_own_scale_kernel(const float *__restrict__ x, int d, int64_t ld, int width, uint16_t *__restrict__ out, float *__restrict__ inv, float sign)
+__global__ __launch_bounds__(256) void pack_own_scale_kernel(const float *__restrict__ x, int d, int64_t ld, int steps, int64_t total, uint16_t *__restrict__ out,
+                                                             float *__restrict__ inv, float sign)
 {
     __shared__ uint32_t red[4];
     const int64_t row = blockIdx.x;
@@ -118,31 +126,30 @@ __global__ __launch_bounds__(256) void pack_own_scale_kernel(const float *__rest
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
     __syncthreads();
     const float s = range_scale(max(max(red[0], red[1]), max(red[2], red[3])));
-    for (int c = threadIdx.x; c < width; c += 256) {
-        uint16_t *to = out + row * width * 2 + place16<true>(c);
+    for (int c = threadIdx.x; c < steps * 16; c += 256) {
+        uint16_t *to = out + (step16<true>(c) * total + row) * kStepElems16 + in_step16<true>(c);
         split_f16(c < d ? x[row * ld + c] * (s * sign) : 0.0f, to, to + 16);
     }
     if (threadIdx.x == 0) inv[row] = 1.0f / s;
 }
 
-int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int width, uint16_t *out, const uint32_t *largest, float *inv, bool negate, hipStream_t st)
+int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, int64_t total, uint16_t *out, const uint32_t *largest, float *inv, bool negate,
+                     hipStream_t st)
 {
     if (type == AVQ_F32 && !largest) {
-        pack_own_scale_kernel<<<dim3((unsigned)rows), dim3(256), 0, st>>>((const float *)x, d, ld, width, out, inv, negate ? -1.0f : 1.0f);
+        pack_own_scale_kernel<<<dim3((unsigned)rows), dim3(256), 0, st>>>((const float *)x, d, ld, steps, total, out, inv, negate ? -1.0f : 1.0f);
         AVQ_HIP(hipGetLastError());
         return AVQ_OK;
     }
-    const int per_row = width / 8;
-    const dim3 grid((unsigned)((rows * per_row + 255) / 256));
-    const uint32_t magic = magic_of(per_row);
+    const dim3 grid((unsigned)((rows + kPackRows - 1) / kPackRows));
     const bool whole = row_width(x, ld, d, type_bytes(type)) == 16 && d % 8 == 0;
     const uint16_t flip = negate ? 0x8000 : 0;
     if (type == AVQ_F32) {
-        if (whole) pack_rows_kernel<float, true><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, per_row, magic, out, largest, 0);
-        else pack_rows_kernel<float, false><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, per_row, magic, out, largest, 0);
+        if (whole) pack_rows_kernel<float, true><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, steps, total, out, largest, 0);
+        else pack_rows_kernel<float, false><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, steps, total, out, largest, 0);
     } else {
-        if (whole) pack_rows_kernel<uint16_t, true><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, per_row, magic, out, nullptr, flip);
-        else pack_rows_kernel<uint16_t, false><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, per_row, magic, out, nullptr, flip);
+        if (whole) pack_rows_kernel<uint16_t, true><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, steps, total, out, nullptr, flip);
+        else pack_rows_kernel<uint16_t, false><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, steps, total, out, nullptr, flip);
     }
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
@@ -153,6 +160,7 @@ template <class T>
 __global__ __launch_bounds__(256) void pack_transposed_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int width, uint16_t *__restrict__ out,
                                                               const uint32_t *__restrict__ largest)
 {
+    constexpr bool SPLIT = sizeof(T) == 4;
     __shared__ T tile[64][65];
     const int64_t t0 = (int64_t)blockIdx.x * 64;
     const int c0 = blockIdx.y * 64;
@@ -163,22 +171,20 @@ __global__ __launch_bounds__(256) void pack_transposed_kernel(const T *__restric
     }
     __syncthreads();
     float s = 1.0f;
-    if constexpr (sizeof(T) == 4) s = range_scale(*largest);
+    if constexpr (SPLIT) s = range_scale(*largest);
     for (int i = threadIdx.x; i < 4096; i += 256) {
         const int c = c0 + (i >> 6);
         const int64_t t = t0 + (i & 63);
         if (c >= d || t >= width) continue;
-        if constexpr (sizeof(T) == 4) {
-            uint16_t *to = out + (int64_t)c * width * 2 + place16<true>(t);
-            split_f16(tile[i & 63][i >> 6] * s, to, to + 16);
-        } else {
-            out[(int64_t)c * width + t] = tile[i & 63][i >> 6];
-        }
+        uint16_t *to = out + (step16<SPLIT>(t) * d + c) * kStepElems16 + in_step16<SPLIT>(t);
+        if constexpr (SPLIT) split_f16(tile[i & 63][i >> 6] * s, to, to + 16);
+        else *to = tile[i & 63][i >> 6];
     }
 }
 
-int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int width, uint16_t *out, const uint32_t *largest, hipStream_t st)
+int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, uint16_t *out, const uint32_t *largest, hipStream_t st)
 {
+    const int width = steps * (type == AVQ_F32 ? 16 : 32);
     const dim3 grid((unsigned)((width + 63) / 64), (unsigned)((d + 63) / 64));
     if (type == AVQ_F32) pack_transposed_kernel<float><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, width, out, largest);
     else pack_transposed_kernel<uint16_t><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, width, out, nullptr);
