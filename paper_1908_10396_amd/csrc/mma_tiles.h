@@ -29,19 +29,21 @@ constexpr int kTileM = 256, kTileN = 128, kStepBytes = 64 /* of a row */, kTileT
 constexpr int kStageA = kTileM * kStepBytes, kStageB = kTileN * kStepBytes, kStageBytes = kStageA + kStageB, kStages = 3;
 constexpr int kTileLds = kStages * kStageBytes;
 
-// Rows of 16-bit elements (SPLIT: of pairs of them): `rows` of them, `row` elements apart, 16-byte aligned; a step's 32 elements lie
-// `step` elements after the step's before. Rows as a caller has them: step = 32. Packed ones: row = 32, so that the rows of a
-// step lie side by side and copies read whole lines (a step of 64 bytes a row is half a line, and the copies of the products over
-// rows, which read 512 bytes at a time, reached 1,020 TFLOP/s where those of 64 bytes reached 770).
-struct Rows16 { const uint16_t *p; int64_t row, step, rows; };
+// Rows of 16-bit elements (SPLIT: of pairs of them): `rows` of them, in blocks of 16 elements (32 bytes), 16-byte aligned: block b of
+// row r at p + b block + r row. A step is two blocks: 32 elements, or (SPLIT) the hi of 16 and their lo. Rows as a caller has them:
+// block = 16. Packed ones: row = 16, so that the rows of a block lie side by side, and copies read, and stores write, whole lines;
+// SPLIT ones always, others where they are not a caller's rows (or a copy of them, padded).
+struct Rows16 { const uint16_t *p; int64_t row, block, rows; };
 constexpr int64_t kMaxRow16 = (int64_t)1 << 22; // (256 rows' places are 32-bit offsets)
-constexpr int kStepElems16 = 32;
+inline Rows16 packed_rows(const uint16_t *p, int64_t rows) { return Rows16{p, 16, rows * 16, rows}; }
 
-// The step that element c of a row belongs to, and its place there; SPLIT: of its hi, 16 elements before its lo.
-template <bool SPLIT> __host__ __device__ inline int64_t step16(int64_t c) { return SPLIT ? c >> 4 : c >> 5; }
-template <bool SPLIT> __host__ __device__ inline int in_step16(int64_t c) { return (int)(SPLIT ? c & 15 : c & 31); }
+// The block that element c of a row belongs to; SPLIT: of its hi, the lo's is the next.
+template <bool SPLIT> __host__ __device__ inline int64_t block16(int64_t c) { return SPLIT ? (c >> 4) * 2 : c >> 4; }
 // The steps that an inner dimension of d takes.
 template <bool SPLIT> __host__ __device__ inline int steps_of(int64_t d) { return (int)((d + (SPLIT ? 15 : 31)) / (SPLIT ? 16 : 32)); }
+// G's and the transposed queries' order of 16 queries: a lane of the product that makes G has queries 8 b + 4 h + e of a block, and
+// stores them side by side, at 8 h + 4 b + e. (Its own inverse.)
+__host__ __device__ inline int turned16(int i) { return ((i >> 2) & 1) * 8 + (i >> 3 & 1) * 4 + (i & 3); }
 
 __device__ __forceinline__ f32x16 mma32(const Quad &a, const Quad &b, f32x16 c, bf16_t)
 {
@@ -64,67 +66,86 @@ template <int NEWER> __device__ __forceinline__ void step_barrier()
 }
 constexpr int kCopies = 6; // of a wave a step (the 6 above)
 
-// Copies of operands whose rows hold the inner dimension (C = A B^T). In LDS a row's step is four 16-byte chunks, chunk c
-// of row r at c ^ (r / 4 % 4): sixteen rows' reads of one chunk touch every bank once.
-struct RowCopies {
-    const char *pa, *pb; // the tile's first rows
-    uint32_t a[4], b[2]; // this lane's places from there
-    __device__ __forceinline__ void seek(const Rows16 &A, int64_t a0, const Rows16 &B, int64_t b0)
+// Copies of operands whose rows hold the inner dimension (C = A B^T). Lanes side by side read what lies side by side. In LDS a step of
+// a caller's rows is 64 bytes a row, of which the 16-byte chunk c lies at c ^ (row / 4 % 4); of packed rows two blocks of 32 bytes a row,
+// chunk c of a block at c ^ (row / 8 % 2). Either way sixteen rows' reads of one chunk touch every bank once.
+template <bool PACKED, int ROWS> struct RowOperand {
+    static constexpr int kEach = ROWS * kStepBytes / 1024 / 4; // copies of a wave
+    const char *p;        // the tile's first row
+    uint32_t at[kEach];   // this lane's places from there
+    __device__ __forceinline__ void seek(const Rows16 &R, int64_t r0)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const uint32_t chunk = (uint32_t)((lane & 3) ^ ((lane >> 4) & 3)) * 16;
-        const int last_a = (int)min(A.rows - 1 - a0, (int64_t)kTileM), last_b = (int)min(B.rows - 1 - b0, (int64_t)kTileN);
-        pa = (const char *)(A.p + a0 * A.row);
-        pb = (const char *)(B.p + b0 * B.row);
+        const int last = (int)min(R.rows - 1 - r0, (int64_t)ROWS);
+        p = (const char *)(R.p + r0 * R.row);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = (uint32_t)min((wave * 4 + j) * 16 + (lane >> 2), last_a) * (uint32_t)(A.row * 2) + chunk;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) b[j] = (uint32_t)min((wave * 2 + j) * 16 + (lane >> 2), last_b) * (uint32_t)(B.row * 2) + chunk;
+        for (int j = 0; j < kEach; ++j) {
+            const int i = wave * kEach + j;
+            const int row = PACKED ? i % (ROWS / 32) * 32 + (lane >> 1) : i * 16 + (lane >> 2);
+            const int chunk = PACKED ? i / (ROWS / 32) * 2 + ((lane & 1) ^ ((lane >> 4) & 1)) : (lane & 3) ^ ((lane >> 4) & 3);
+            at[j] = (uint32_t)min(row, last) * (uint32_t)(R.row * 2) + (uint32_t)(chunk >> 1) * (uint32_t)(R.block * 2) + (chunk & 1) * 16;
+        }
     }
-    __device__ __forceinline__ void issue(const Rows16 &A, const Rows16 &B, int step, uint32_t stage) const
+    __device__ __forceinline__ void issue(const Rows16 &R, int step, uint32_t lds) const
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const char *fa = pa + step * A.step * 2, *fb = pb + step * B.step * 2;
+        const char *from = p + step * R.block * 4;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) lds_copy16_from(fa, a[j], stage + (wave * 4 + j) * 1024);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) lds_copy16_from(fb, b[j], stage + kStageA + (wave * 2 + j) * 1024);
+        for (int j = 0; j < kEach; ++j) lds_copy16_from(from, at[j], lds + (wave * kEach + j) * 1024);
     }
-    // operands of 16 of the inner dimension: the step's first or second half (SPLIT: its hi or lo)
-    static __device__ __forceinline__ void read(const char *stage, int half, Quad (&a)[4], Quad (&b)[2])
+    // row0 + (lane & 31) of 32 rows, the step's first or second half (SPLIT: hi or lo)
+    static __device__ __forceinline__ Quad read(const char *lds, int row0, int half)
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const int at = (lane & 31) * 64 + ((((lane >> 5) + half * 2) ^ ((lane >> 2) & 3)) * 16);
+        const int lane = threadIdx.x & 63;
+        if (PACKED) return *(const Quad *)(lds + half * (ROWS * 32) + (row0 + (lane & 31)) * 32 + ((lane >> 5) ^ ((lane >> 3) & 1)) * 16);
+        return *(const Quad *)(lds + (row0 + (lane & 31)) * 64 + ((((lane >> 5) + half * 2) ^ ((lane >> 2) & 3)) * 16));
+    }
+};
+
+template <bool PACKED_A, bool PACKED_B> struct RowCopies {
+    typedef RowOperand<PACKED_A, kTileM> OfA;
+    typedef RowOperand<PACKED_B, kTileN> OfB;
+    OfA a;
+    OfB b;
+    __device__ __forceinline__ void seek(const Rows16 &A, int64_t a0, const Rows16 &B, int64_t b0) { a.seek(A, a0); b.seek(B, b0); }
+    __device__ __forceinline__ void issue(const Rows16 &A, const Rows16 &B, int step, uint32_t stage) const { a.issue(A, step, stage); b.issue(B, step, stage + kStageA); }
+    // operands of 16 of the inner dimension
+    static __device__ __forceinline__ void read(const char *stage, int half, Quad (&qa)[4], Quad (&qb)[2])
+    {
+        const int wave = threadIdx.x >> 6;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) b[j] = *(const Quad *)(stage + kStageA + ((wave & 1) * 64 + j * 32) * 64 + at);
+        for (int j = 0; j < 2; ++j) qb[j] = OfB::read(stage + kStageA, (wave & 1) * 64 + j * 32, half);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = *(const Quad *)(stage + ((wave >> 1) * 128 + i * 32) * 64 + at);
+        for (int i = 0; i < 4; ++i) qa[i] = OfA::read(stage, (wave >> 1) * 128 + i * 32, half);
     }
 };
 
 // Copies of operands whose rows are the inner dimension (C = A^T B): 32 rows (SPLIT: 16 of pairs) of 256 columns of A and 128 of B a
-// step. The reads transpose 4 x 16 elements for 16 lanes: 32 lanes read two pieces of 32 bytes, 32 (SPLIT: 64) apart, of four rows. So
-// that these lie in different banks, a row's 16-byte chunk c lies at c ^ turn(row % 4).
+// step. Reads transpose 4 x 16 elements for 16 lanes: 32 lanes read 32 bytes of four rows in two blocks of columns. Packed rows lie in
+// LDS as they do in memory, [block][row][32 bytes], rows of every other block of columns turned by four, so that the two blocks' reads
+// touch different banks; a caller's rows (B where not SPLIT) [row][256 bytes], chunk c at c ^ (4 (row % 4)), so that the four rows' do.
 template <bool SPLIT> struct ColumnCopies {
-    static constexpr int kRows = SPLIT ? 16 : 32, kRowA = kStageA / kRows, kRowB = kStageB / kRows; // of a step; bytes of a row in LDS
-    static constexpr int kChunksA = kRowA / 16, kChunksB = kRowB / 16;
-    static __device__ __forceinline__ int turn(int r) { return SPLIT ? (r & 1) * 2 + (r >> 1) * 8 : r * 4; }
+    static constexpr int kRows = SPLIT ? 16 : 32, kBlock = kRows * 32; // of a step; bytes of a block in LDS
     const char *pa, *pb; // the tile's first columns
     uint32_t a[4], b[2]; // this lane's columns from there
     int64_t row;         // of the first step
     __device__ __forceinline__ void seek(const Rows16 &A, int64_t a0, int64_t a_columns, const Rows16 &B, int64_t b0)
     {
         // (columns of A past its last come from its last: nothing uses their products; B is as wide as its tiles)
-        const int lane = threadIdx.x & 63;
-        const int last = (int)min((step16<SPLIT>(a_columns) - step16<SPLIT>(a0)) * 4 - 1, (int64_t)kChunksA);
-        pa = (const char *)(A.p + step16<SPLIT>(a0) * A.step);
-        pb = (const char *)(B.p + step16<SPLIT>(b0) * B.step);
-        auto at = [](int chunk, const Rows16 &r) { return (uint32_t)(chunk >> 2) * (uint32_t)(r.step * 2) + (uint32_t)(chunk & 3) * 16; };
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int last = (int)min(block16<SPLIT>(a_columns) - block16<SPLIT>(a0) - 1, (int64_t)kStageA);
+        pa = (const char *)(A.p + block16<SPLIT>(a0) * A.block);
+        pb = (const char *)(B.p + block16<SPLIT>(b0) * B.block);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = at(min((lane % kChunksA) ^ turn((j * (64 / kChunksA) + lane / kChunksA + (SPLIT ? (threadIdx.x >> 6) * 4 : 0)) & 3), last), A);
+        for (int j = 0; j < 4; ++j) a[j] = (uint32_t)min(SPLIT ? (wave * 4 + j) * 2 + (lane >> 5) : wave * 4 + j, last) * (uint32_t)(A.block * 2) + (lane & 1) * 16;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) b[j] = at((lane % kChunksB) ^ turn((j * (64 / kChunksB) + lane / kChunksB) & 3), B);
+        for (int j = 0; j < 2; ++j) {
+            if (SPLIT) b[j] = (uint32_t)((wave * 2 + j) * 2 + (lane >> 5)) * (uint32_t)(B.block * 2) + (lane & 1) * 16;
+            else b[j] = (uint32_t)((lane & 15) ^ ((lane >> 4) * 4)) * 16; // (B.block == 16)
+        }
     }
+    // the row that a lane of the j-th copy has, of packed rows
+    static __device__ __forceinline__ int packed_row(int lane, int j) { return ((lane >> 1) & (kRows - 1)) ^ ((j & 1) * 4); }
     __device__ __forceinline__ void issue(const Rows16 &A, const Rows16 &B, int step, uint32_t stage) const
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -133,33 +154,46 @@ template <bool SPLIT> struct ColumnCopies {
         const char *fa = pa + first_a * A.row * 2, *fb = pb + first_b * B.row * 2;
         const int last_a = (int)min(A.rows - 1 - first_a, (int64_t)kRows), last_b = (int)min(B.rows - 1 - first_b, (int64_t)kRows);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            lds_copy16_from(fa, (uint32_t)min((wave * 4 + j) * (64 / kChunksA) + lane / kChunksA, last_a) * (uint32_t)(A.row * 2) + a[j], stage + (wave * 4 + j) * 1024);
+        for (int j = 0; j < 4; ++j) lds_copy16_from(fa, (uint32_t)min(packed_row(lane, j), last_a) * (uint32_t)(A.row * 2) + a[j], stage + (wave * 4 + j) * 1024);
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-            lds_copy16_from(fb, (uint32_t)min((wave * 2 + j) * (64 / kChunksB) + lane / kChunksB, last_b) * (uint32_t)(B.row * 2) + b[j], stage + kStageA + (wave * 2 + j) * 1024);
+        for (int j = 0; j < 2; ++j) {
+            const int r = SPLIT ? packed_row(lane, j) : (wave * 2 + j) * 4 + (lane >> 4);
+            lds_copy16_from(fb, (uint32_t)min(r, last_b) * (uint32_t)(B.row * 2) + b[j], stage + kStageA + (wave * 2 + j) * 1024);
+        }
     }
-    static __device__ __forceinline__ Quad read_turned(const char *p, int row_bytes)
+    // four rows at p and the four after them, at q, of which a lane gets its column
+    static __device__ __forceinline__ Quad read_turned(const char *p, const char *q)
     {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4 *lds_ptr;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * row_bytes));
-        Quad q;
-        __builtin_memcpy(&q.w[0], &lo, 8);
-        __builtin_memcpy(&q.w[2], &hi, 8);
-        return q;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)q);
+        Quad v;
+        __builtin_memcpy(&v.w[0], &lo, 8);
+        __builtin_memcpy(&v.w[2], &hi, 8);
+        return v;
     }
-    static __device__ __forceinline__ void read(const char *stage, int half, Quad (&a)[4], Quad (&b)[2])
+    static __device__ __forceinline__ void read(const char *stage, int half, Quad (&qa)[4], Quad (&qb)[2])
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         const int i16 = lane & 15, g = lane >> 4, r = i16 >> 2; // r: row of the four
-        const int row_at = (SPLIT ? 0 : half * 16) + 8 * (g >> 1) + r;
-        // the chunk of columns 32 m + 16 (g & 1) + 4 (i16 & 3) onwards, and the place in it
-        auto at = [&](int m) { return ((SPLIT ? m * 8 + (g & 1) * 4 + half * 2 + ((i16 & 3) >> 1) : m * 4 + (g & 1) * 2 + ((i16 & 3) >> 1)) ^ turn(r)) * 16 + (i16 & 1) * 8; };
+        const int first = (SPLIT ? 0 : half * 16) + 8 * (g >> 1);
+        // of packed rows: columns 32 m + 16 (g & 1) + 4 (i16 & 3) onwards
+        auto packed = [&](const char *lds, int m) __attribute__((always_inline)) {
+            const int block = SPLIT ? (m * 2 + (g & 1)) * 2 + half : m * 2 + (g & 1);
+            const char *rows = lds + block * kBlock + first * 32 + (i16 & 3) * 8;
+            return read_turned(rows + (r + 4 * (g & 1)) * 32, rows + (r + 4 - 4 * (g & 1)) * 32);
+        };
 #pragma unroll
-        for (int j = 0; j < 2; ++j) b[j] = read_turned(stage + kStageA + row_at * kRowB + at((wave & 1) * 2 + j), kRowB);
+        for (int j = 0; j < 2; ++j) {
+            if (SPLIT) {
+                qb[j] = packed(stage + kStageA, (wave & 1) * 2 + j);
+            } else {
+                const char *p = stage + kStageA + (first + r) * 256 + ((((wave & 1) * 2 + j) ^ r) * 64) + (2 * (g & 1) + ((i16 & 3) >> 1)) * 16 + (i16 & 1) * 8;
+                qb[j] = read_turned(p, p + 4 * 256);
+            }
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = read_turned(stage + row_at * kRowA + at((wave >> 1) * 4 + i), kRowA);
+        for (int i = 0; i < 4; ++i) qa[i] = packed(stage, (wave >> 1) * 4 + i);
     }
 };
 
@@ -262,11 +296,10 @@ __device__ __forceinline__ float range_scale(uint32_t largest_bits)
 int launch_clear_largest(Largest *to, hipStream_t st);
 // max over finite elements into *to
 int launch_largest(const float *x, int64_t rows, int d, int64_t ld, uint32_t *to, hipStream_t st);
-// Packed rows: out[step][row of `total`][32], `steps` steps, zeros past a row's end. fp32: pairs, scaled by range_scale(*largest), or,
-// largest == NULL, each row by its own, whose inverse goes to inv[row]. negate: with the other sign.
-int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, int64_t total, uint16_t *out, const uint32_t *largest, float *inv, bool negate,
-                     hipStream_t st);
-// The transpose packed: row c < d of d holds x[t][c], zeros past the last t.
+// Rows laid out as `to` says (to.p: where), `steps` steps of them, zeros past a row's end. fp32: pairs, scaled by
+// range_scale(*largest), or, largest == NULL, each row by its own, whose inverse goes to inv[row]. negate: with the other sign.
+int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, float *inv, bool negate, hipStream_t st);
+// The transpose packed: row c < d of d holds x[t][c], 16 t in the order of turned16, zeros past the last t.
 int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, uint16_t *out, const uint32_t *largest, hipStream_t st);
 
 } // namespace avq

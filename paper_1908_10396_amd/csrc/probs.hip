@@ -269,7 +269,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
         m[j] = -INFINITY;
         l[j] = t[j] = 0.0f;
     }
-    run_tiles<H, SPLIT, BEST, RowCopies>(X, Q, steps, count, lds, [&](int i, RowCopies &c) { c.seek(X, (first + i) * kTileM, Q, q0); },
+    typedef RowCopies<SPLIT, true> Copies;
+    run_tiles<H, SPLIT, BEST, Copies>(X, Q, steps, count, lds, [&](int i, Copies &c) { c.seek(X, (first + i) * kTileM, Q, q0); },
         [&](int i, f32x16 (&acc)[4][2]) {
             const int64_t row0 = (first + i) * kTileM;
             const bool whole = row0 + kTileM <= X.rows;
@@ -644,20 +645,20 @@ static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
 {
     const int size = type_bytes(p.type);
     const float c2 = fabsf(p.scale) * 1.44269504088896341f;
-    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, p.nq, s.q16, nullptr, s.q_inv, p.scale < 0.0f, st));
+    const Rows16 Q = packed_rows(s.q16, p.nq);
+    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, Q, nullptr, s.q_inv, p.scale < 0.0f, st));
     if (SPLIT) {
         AVQ_TRY(launch_clear_largest(s.largest, st));
         AVQ_TRY(launch_largest((const float *)p.points, p.n, p.d, p.ld_points, &s.largest->points, st));
     }
     static LdsLimitOnce with_best, without;
-    const Rows16 Q{s.q16, kStepElems16, (int64_t)p.nq * kStepElems16, p.nq};
     for (int i = 0; i < s.launches; ++i) {
         const int64_t lo = i * s.part, rows = std::min<int64_t>(s.part, p.n - lo);
         const char *from = (const char *)p.points + lo * p.ld_points * size;
-        Rows16 X{(const uint16_t *)from, p.ld_points, kStepElems16, rows};
+        Rows16 X{(const uint16_t *)from, p.ld_points, 16, rows};
         if (s.pack) {
-            AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, s.steps, rows, s.x16, SPLIT ? &s.largest->points : nullptr, nullptr, false, st));
-            X = Rows16{s.x16, kStepElems16, rows * kStepElems16, rows};
+            X = SPLIT ? packed_rows(s.x16, rows) : Rows16{s.x16, (int64_t)s.steps * 32, 16, rows};
+            AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, s.steps, X, SPLIT ? &s.largest->points : nullptr, nullptr, false, st));
         }
         float4 *stats = s.stats + (size_t)i * s.parts * 2 * p.nq;
         const dim3 grid((unsigned)(s.parts * s.query_tiles));

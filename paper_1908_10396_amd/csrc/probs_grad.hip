@@ -46,14 +46,14 @@ __global__ __launch_bounds__(256) void grad_coef_kernel(const int32_t *__restric
     if ((threadIdx.x & 63) == 0 && m != 0) atomicMax(&largest->upstream, m);
 }
 
-// a value as an operand: rounded to the type, or (fp32) hi and, 16 elements on, lo
-__device__ __forceinline__ void put16(uint16_t *to, float v, bf16_t) { *to = from_f32<bf16_t>(v).bits; }
-__device__ __forceinline__ void put16(uint16_t *to, float v, f16_t) { *to = from_f32<f16_t>(v).bits; }
-__device__ __forceinline__ void put16(uint16_t *to, float v, float)
+// a value as an operand: rounded to the type, or (fp32) hi and lo
+__device__ __forceinline__ void put16(float v, uint16_t *hi, uint16_t *, bf16_t) { *hi = from_f32<bf16_t>(v).bits; }
+__device__ __forceinline__ void put16(float v, uint16_t *hi, uint16_t *, f16_t) { *hi = from_f32<f16_t>(v).bits; }
+__device__ __forceinline__ void put16(float v, uint16_t *hi, uint16_t *lo, float)
 {
-    const _Float16 hi = (_Float16)v;
-    to[0] = __builtin_bit_cast(uint16_t, hi);
-    to[16] = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)hi));
+    const _Float16 h = (_Float16)v;
+    *hi = __builtin_bit_cast(uint16_t, h);
+    *lo = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)h));
 }
 
 // G^T of the part's rows: 256 queries of a workgroup by 128 rows at a time. T: the caller's type, H: the instructions'.
@@ -80,7 +80,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
     }
     const float cq = SPLIT ? c2 * (1.0f / range_scale(largest->points)) * (1.0f / range_scale(largest->queries)) : c2;
     __syncthreads();
-    run_tiles<H, SPLIT, true, RowCopies>(Q, X, steps, count, lds, [&](int i, RowCopies &c) { c.seek(Q, q0, X, (first + i) * kTileN); },
+    typedef RowCopies<true, SPLIT> Copies;
+    run_tiles<H, SPLIT, true, Copies>(Q, X, steps, count, lds, [&](int i, Copies &c) { c.seek(Q, q0, X, (first + i) * kTileN); },
         [&](int i, f32x16 (&acc)[4][2]) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -89,28 +90,30 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
 #pragma unroll
                 for (int a = 0; a < 4; ++a)
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        const int t = (wave >> 1) * 128 + a * 32 + 8 * b + 4 * half; // four queries side by side
-                        const float4 s4 = shift[t / 4], u4 = up[t / 4];
-                        const float sh[4] = {s4.x, s4.y, s4.z, s4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
-                        float hh[4] = {};
-                        if (ENTROPY) { const float4 v = up_h[t / 4]; hh[0] = v.x; hh[1] = v.y; hh[2] = v.z; hh[3] = v.w; }
-                        Pack<uint16_t, 4> hi, lo;
+                    for (int block = 0; block < 2; ++block) {
+                        // queries 16 block + 8 b + 4 half + e of the 32: stored side by side, two lanes' 32 bytes
+                        Pack<uint16_t, 8> hi, lo;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float s2 = __fmaf_rn(acc[a][j][4 * b + e], cq, sh[e]), p = __builtin_amdgcn_exp2f(s2);
-                            float v = p * (ENTROPY ? __fmaf_rn(hh[e], s2, u[e]) : u[e]);
-                            if (ENTROPY && p == 0.0f) v = 0.0f; // (p log p)
-                            if (!real) v = 0.0f;
-                            uint16_t two[17];
-                            put16(two, v, T{});
-                            hi.e[e] = two[0];
-                            if (SPLIT) lo.e[e] = two[16];
+                        for (int b = 0; b < 2; ++b) {
+                            const int t = (wave >> 1) * 128 + a * 32 + block * 16 + 8 * b + 4 * half;
+                            const float4 s4 = shift[t / 4], u4 = up[t / 4];
+                            const float sh[4] = {s4.x, s4.y, s4.z, s4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
+                            float hh[4] = {};
+                            if (ENTROPY) { const float4 v = up_h[t / 4]; hh[0] = v.x; hh[1] = v.y; hh[2] = v.z; hh[3] = v.w; }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float s2 = __fmaf_rn(acc[a][j][8 * block + 4 * b + e], cq, sh[e]), p = __builtin_amdgcn_exp2f(s2);
+                                float v = p * (ENTROPY ? __fmaf_rn(hh[e], s2, u[e]) : u[e]);
+                                if (ENTROPY && p == 0.0f) v = 0.0f; // (p log p)
+                                if (!real) v = 0.0f;
+                                put16(v, &hi.e[4 * b + e], &lo.e[4 * b + e], T{});
+                            }
                         }
-                        if (q0 + t < width) {
-                            uint16_t *to = G + (step16<SPLIT>(q0 + t) * total + row) * kStepElems16 + in_step16<SPLIT>(q0 + t);
-                            *(Pack<uint16_t, 4> *)to = hi;
-                            if (SPLIT) *(Pack<uint16_t, 4> *)(to + 16) = lo;
+                        const int64_t t0 = q0 + (wave >> 1) * 128 + a * 32 + block * 16;
+                        if (t0 < width) {
+                            uint16_t *to = G + (block16<SPLIT>(t0) * total + row) * 16 + half * 8;
+                            *(Pack<uint16_t, 8> *)to = hi;
+                            if (SPLIT) *(Pack<uint16_t, 8> *)(to + total * 16) = lo;
                         }
                     }
             }
@@ -143,8 +146,11 @@ __global__ __launch_bounds__(256) void grad_given_kernel(const T *__restrict__ x
     const float2 c = coef[t];
     const float p = __builtin_amdgcn_exp2f(s * 1.44269504088896341f);
     const float v = sum - (p > 0.0f || p != p ? p * __fmaf_rn(c.y, s, c.x) : 0.0f);
-    constexpr bool SPLIT = sizeof(T) == 4;
-    put16(G + (step16<SPLIT>(t) * total + id - lo) * kStepElems16 + in_step16<SPLIT>(t), v * grad_factor(largest), T{});
+    uint16_t *to = G + (block16<sizeof(T) == 4>(t) * total + id - lo) * 16 + turned16((int)t & 15);
+    uint16_t hi, low = 0;
+    put16(v * grad_factor(largest), &hi, &low, T{});
+    *to = hi;
+    if (sizeof(T) == 4) to[total * 16] = low;
 }
 
 // fn for every four rows side by side of a lane's accumulators acc[a][j][4 b ..]. One after the other: the compiler would
@@ -171,7 +177,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Ro
     int count;
     part_tiles(tiles, parts, place.part, &first, &count);
     const float f = grad_bound(largest) * (1.0f / kGradTop) * scale * (SPLIT ? 1.0f / range_scale(largest->queries) : 1.0f);
-    run_tiles<H, SPLIT, true, RowCopies>(G, Qt, steps, count, lds, [&](int i, RowCopies &c) { c.seek(G, (first + i) * kTileM, Qt, c0); },
+    typedef RowCopies<true, true> Copies;
+    run_tiles<H, SPLIT, true, Copies>(G, Qt, steps, count, lds, [&](int i, Copies &c) { c.seek(G, (first + i) * kTileM, Qt, c0); },
         [&](int i, f32x16 (&acc)[4][2]) {
             const int64_t row0 = (first + i) * kTileM + acc_row(0, 0);
             const int64_t left = rows - row0; // rows from this lane's first one on
@@ -205,14 +212,17 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_queries_kernel(Rows16 G,
     part_tiles(steps, splits, place.part, &first, &count);
     float *mine = sums + (int64_t)place.part * nq * d;
     auto store = [&](int, f32x16 (&acc)[4][2]) {
-        const int64_t row0 = t0 + acc_row(0, 0), left = nq - row0;
+        // the order of 16 queries is turned: position 8 b + 4 h + e of a block is query 8 h + 4 b + e
+        const int half = (threadIdx.x & 63) >> 5;
+        const int64_t row0 = t0 + (acc_row(0, 0) - 4 * half) + 8 * half, left = nq - row0;
         for_quads([&](auto at) {
             constexpr int a = decltype(at)::a, b = decltype(at)::b, j = decltype(at)::j;
+            constexpr int off = a * 32 + (b >> 1) * 16 + (b & 1) * 4;
             const int64_t c = c0 + acc_col(j);
-            float *to = mine + (row0 + a * 32 + b * 8) * d + c;
+            float *to = mine + (row0 + off) * d + c;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (c < d && a * 32 + b * 8 + e < left) *to = begin ? acc[a][j][4 * b + e] : *to + acc[a][j][4 * b + e];
+                if (c < d && off + e < left) *to = begin ? acc[a][j][4 * b + e] : *to + acc[a][j][4 * b + e];
                 to += d;
             }
         });
@@ -325,18 +335,18 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         AVQ_TRY(launch_largest((const float *)p.points, p.n, p.d, p.ld_points, &s.largest->points, st));
         AVQ_TRY(launch_largest((const float *)p.queries, p.nq, p.d, p.ld_queries, &s.largest->queries, st));
     }
-    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, p.nq, s.q16, SPLIT ? &s.largest->queries : nullptr, nullptr, false, st));
+    const Rows16 Q = packed_rows(s.q16, p.nq), Qt = packed_rows(s.qt16, p.d);
+    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, Q, SPLIT ? &s.largest->queries : nullptr, nullptr, false, st));
     if (p.dpoints) AVQ_TRY(launch_pack_transposed(p.queries, p.type, p.nq, p.d, p.ld_queries, s.q_steps, s.qt16, &s.largest->queries, st));
-    const Rows16 Q{s.q16, kStepElems16, (int64_t)p.nq * kStepElems16, p.nq}, Qt{s.qt16, kStepElems16, (int64_t)p.d * kStepElems16, p.d};
     for (int64_t lo = 0; lo < p.n; lo += s.part) {
         const int64_t rows = std::min<int64_t>(s.part, p.n - lo), whole = (rows + kTileN - 1) / kTileN * kTileN; // rows past the last have G = 0
         const T *x = (const T *)p.points + lo * p.ld_points;
-        Rows16 X{(const uint16_t *)x, p.ld_points, kStepElems16, rows};
+        Rows16 X{(const uint16_t *)x, p.ld_points, 16, rows};
         if (s.pack) {
-            AVQ_TRY(launch_pack_rows(x, p.type, rows, p.d, p.ld_points, s.d_steps, rows, s.x16, SPLIT ? &s.largest->points : nullptr, nullptr, false, st));
-            X = Rows16{s.x16, kStepElems16, rows * kStepElems16, rows};
+            X = SPLIT ? packed_rows(s.x16, rows) : Rows16{s.x16, (int64_t)s.d_steps * 32, 16, rows};
+            AVQ_TRY(launch_pack_rows(x, p.type, rows, p.d, p.ld_points, s.d_steps, X, SPLIT ? &s.largest->points : nullptr, nullptr, false, st));
         }
-        const Rows16 G{s.G, kStepElems16, whole * kStepElems16, whole};
+        const Rows16 G = packed_rows(s.G, whole);
         const int parts = parts_for((rows + kTileN - 1) / kTileN, s.q_tiles, kGradGroups);
         const dim3 grid((unsigned)(parts * s.q_tiles));
         if (p.grad_entropy) grad_tile_kernel<T, H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, s.steps, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, whole);

@@ -69,24 +69,24 @@ __device__ __forceinline__ void split_f16(float v, uint16_t *hi, uint16_t *lo)
     *lo = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)h));
 }
 
-constexpr int kPackRows = 32;
+constexpr int kPackRows = 64;
 
-// 32 rows a workgroup, eight elements a thread: threads side by side write the rows of a step, 2 KB; what they read of a row's line at
-// one step comes from the cache at the next. WHOLE: a row is a whole number of eights on 16 bytes.
+// 64 rows a workgroup, half a block of 16 elements a thread, so that threads side by side write the rows of a block, 2 KB. What they
+// read lies in 64 lines, the rest of which comes from the cache at the next blocks. WHOLE: a row is a whole number of eights on 16 bytes.
 template <class T, bool WHOLE>
-__global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int steps, int64_t total, uint16_t *__restrict__ out,
+__global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int blocks, Rows16 to_rows,
                                                         const uint32_t *__restrict__ largest, uint16_t flip)
 {
     constexpr bool SPLIT = sizeof(T) == 4;
-    constexpr int kEights = SPLIT ? 2 : 4, kAtOnce = 256 / (kPackRows * kEights); // eights of a step; steps at once
-    const int u = threadIdx.x % kEights, r = threadIdx.x / kEights % kPackRows, s0 = threadIdx.x / (kEights * kPackRows);
+    constexpr int kAtOnce = 256 / (kPackRows * 2); // blocks
+    const int u = threadIdx.x & 1, r = threadIdx.x / 2 % kPackRows, b0 = threadIdx.x / (2 * kPackRows);
     const int64_t row = (int64_t)blockIdx.x * kPackRows + r;
     if (row >= rows) return;
     float scale = 1.0f;
     if (SPLIT) scale = range_scale(*largest);
 #pragma unroll 4
-    for (int s = s0; s < steps; s += kAtOnce) {
-        const int c = (s * kEights + u) * 8;
+    for (int b = b0; b < blocks; b += kAtOnce) {
+        const int c = b * 16 + u * 8;
         const T *from = x + row * ld + c;
         T v[8];
 #pragma unroll
@@ -98,12 +98,12 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x,
             for (int e = 0; e < 8; ++e)
                 if (c + e < d) v[e] = from[e];
         }
-        uint16_t *to = out + (s * total + row) * kStepElems16 + u * 8;
+        uint16_t *to = (uint16_t *)to_rows.p + block16<SPLIT>(c) * to_rows.block + row * to_rows.row + u * 8;
         Pack<uint16_t, 8> hi, lo;
         if constexpr (SPLIT) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) split_f16(v[e] * scale, &hi.e[e], &lo.e[e]);
-            *(Pack<uint16_t, 8> *)(to + 16) = lo;
+            *(Pack<uint16_t, 8> *)(to + to_rows.block) = lo;
         } else {
             __builtin_memcpy(&hi, v, 16);
 #pragma unroll
@@ -114,8 +114,8 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x,
 }
 
 // each row by its own scale, a workgroup a row
-__global__ __launch_bounds__(256) void pack_own_scale_kernel(const float *__restrict__ x, int d, int64_t ld, int steps, int64_t total, uint16_t *__restrict__ out,
-                                                             float *__restrict__ inv, float sign)
+__global__ __launch_bounds__(256) void pack_own_scale_kernel(const float *__restrict__ x, int d, int64_t ld, int steps, Rows16 to_rows, float *__restrict__ inv,
+                                                             float sign)
 {
     __shared__ uint32_t red[4];
     const int64_t row = blockIdx.x;
@@ -127,29 +127,29 @@ __global__ __launch_bounds__(256) void pack_own_scale_kernel(const float *__rest
     __syncthreads();
     const float s = range_scale(max(max(red[0], red[1]), max(red[2], red[3])));
     for (int c = threadIdx.x; c < steps * 16; c += 256) {
-        uint16_t *to = out + (step16<true>(c) * total + row) * kStepElems16 + in_step16<true>(c);
-        split_f16(c < d ? x[row * ld + c] * (s * sign) : 0.0f, to, to + 16);
+        uint16_t *to = (uint16_t *)to_rows.p + block16<true>(c) * to_rows.block + row * to_rows.row + (c & 15);
+        split_f16(c < d ? x[row * ld + c] * (s * sign) : 0.0f, to, to + to_rows.block);
     }
     if (threadIdx.x == 0) inv[row] = 1.0f / s;
 }
 
-int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, int64_t total, uint16_t *out, const uint32_t *largest, float *inv, bool negate,
-                     hipStream_t st)
+int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, float *inv, bool negate, hipStream_t st)
 {
     if (type == AVQ_F32 && !largest) {
-        pack_own_scale_kernel<<<dim3((unsigned)rows), dim3(256), 0, st>>>((const float *)x, d, ld, steps, total, out, inv, negate ? -1.0f : 1.0f);
+        pack_own_scale_kernel<<<dim3((unsigned)rows), dim3(256), 0, st>>>((const float *)x, d, ld, steps, to, inv, negate ? -1.0f : 1.0f);
         AVQ_HIP(hipGetLastError());
         return AVQ_OK;
     }
     const dim3 grid((unsigned)((rows + kPackRows - 1) / kPackRows));
     const bool whole = row_width(x, ld, d, type_bytes(type)) == 16 && d % 8 == 0;
     const uint16_t flip = negate ? 0x8000 : 0;
+    const int blocks = type == AVQ_F32 ? steps : 2 * steps; // of 16 coordinates
     if (type == AVQ_F32) {
-        if (whole) pack_rows_kernel<float, true><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, steps, total, out, largest, 0);
-        else pack_rows_kernel<float, false><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, steps, total, out, largest, 0);
+        if (whole) pack_rows_kernel<float, true><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, largest, 0);
+        else pack_rows_kernel<float, false><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, largest, 0);
     } else {
-        if (whole) pack_rows_kernel<uint16_t, true><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, steps, total, out, nullptr, flip);
-        else pack_rows_kernel<uint16_t, false><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, steps, total, out, nullptr, flip);
+        if (whole) pack_rows_kernel<uint16_t, true><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
+        else pack_rows_kernel<uint16_t, false><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
     }
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
@@ -176,8 +176,8 @@ __global__ __launch_bounds__(256) void pack_transposed_kernel(const T *__restric
         const int c = c0 + (i >> 6);
         const int64_t t = t0 + (i & 63);
         if (c >= d || t >= width) continue;
-        uint16_t *to = out + (step16<SPLIT>(t) * d + c) * kStepElems16 + in_step16<SPLIT>(t);
-        if constexpr (SPLIT) split_f16(tile[i & 63][i >> 6] * s, to, to + 16);
+        uint16_t *to = out + (block16<SPLIT>(t) * d + c) * 16 + turned16((int)t & 15);
+        if constexpr (SPLIT) split_f16(tile[i & 63][i >> 6] * s, to, to + (int64_t)d * 16);
         else *to = tile[i & 63][i >> 6];
     }
 }
