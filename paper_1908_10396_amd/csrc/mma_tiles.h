@@ -35,7 +35,10 @@ constexpr int kTileLds = kStages * kStageBytes;
 // SPLIT ones always, others where they are not a caller's rows (or a copy of them, padded).
 struct Rows16 { const uint16_t *p; int64_t row, block, rows; };
 constexpr int64_t kMaxRow16 = (int64_t)1 << 22; // (256 rows' places are 32-bit offsets)
-inline Rows16 packed_rows(const uint16_t *p, int64_t rows) { return Rows16{p, 16, rows * 16, rows}; }
+// Blocks lie apart by a little more than their rows: by a power of two, all of a row's blocks would be on few memory channels.
+constexpr int kBlockGap = 72; // rows
+inline Rows16 packed_rows(const uint16_t *p, int64_t rows) { return Rows16{p, 16, (rows + kBlockGap) * 16, rows}; }
+inline size_t packed_bytes(int64_t rows, int steps) { return (size_t)(rows + kBlockGap) * steps * kStepBytes; }
 
 // The block that element c of a row belongs to; SPLIT: of its hi, the lo's is the next.
 template <bool SPLIT> __host__ __device__ inline int64_t block16(int64_t c) { return SPLIT ? (c >> 4) * 2 : c >> 4; }
@@ -300,6 +303,6 @@ int launch_largest(const float *x, int64_t rows, int d, int64_t ld, uint32_t *to
 // range_scale(*largest), or, largest == NULL, each row by its own, whose inverse goes to inv[row]. negate: with the other sign.
 int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, float *inv, bool negate, hipStream_t st);
 // The transpose packed: row c < d of d holds x[t][c], 16 t in the order of turned16, zeros past the last t.
-int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, uint16_t *out, const uint32_t *largest, hipStream_t st);
+int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, hipStream_t st);
 
 } // namespace avq

@@ -600,10 +600,10 @@ static ProbScratch prob_scratch(const ProbParams &p, void *base)
         s.parts = parts_for((s.part + kTileM - 1) / kTileM, s.query_tiles, kTileGroups);
         // (as many statistics with one launch as with several: the number of parts only falls with the rows a launch has)
         s.stats = (float4 *)take((size_t)s.launches * std::max(s.parts, parts_for((p.n + kTileM - 1) / kTileM, s.query_tiles, kTileGroups)) * 2 * p.nq * sizeof(float4));
-        s.q16 = (uint16_t *)take((size_t)p.nq * row_bytes);
+        s.q16 = (uint16_t *)take(packed_bytes(p.nq, s.steps));
         s.q_inv = (float *)take((size_t)p.nq * sizeof(float));
         s.largest = (Largest *)take(sizeof(Largest));
-        if (s.pack) s.x16 = (uint16_t *)take((size_t)s.part * row_bytes);
+        if (s.pack) s.x16 = (uint16_t *)take(packed_bytes(s.part, s.steps));
     }
     s.gmax = p.k > 0 ? (float *)take((size_t)s.gstride * p.nq * sizeof(float)) : nullptr;
     s.bytes = at;

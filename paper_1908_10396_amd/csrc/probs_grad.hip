@@ -59,7 +59,7 @@ __device__ __forceinline__ void put16(float v, uint16_t *hi, uint16_t *lo, float
 // G^T of the part's rows: 256 queries of a workgroup by 128 rows at a time. T: the caller's type, H: the instructions'.
 template <class T, class H, bool SPLIT, bool ENTROPY>
 __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Rows16 X, int steps, float c2, const float *__restrict__ lse, const float2 *__restrict__ coef,
-                                                                    const Largest *__restrict__ largest, int parts, int others, uint16_t *__restrict__ G, int width, int64_t total)
+                                                                    const Largest *__restrict__ largest, int parts, int others, Rows16 G, int width)
 {
     extern __shared__ char lds[];
     __shared__ float4 shift[kTileM / 4], up[kTileM / 4], up_h[kTileM / 4]; // -lse / log 2; a and h, in G's units
@@ -111,9 +111,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
                         }
                         const int64_t t0 = q0 + (wave >> 1) * 128 + a * 32 + block * 16;
                         if (t0 < width) {
-                            uint16_t *to = G + (block16<SPLIT>(t0) * total + row) * 16 + half * 8;
+                            uint16_t *to = (uint16_t *)G.p + block16<SPLIT>(t0) * G.block + row * G.row + half * 8;
                             *(Pack<uint16_t, 8> *)to = hi;
-                            if (SPLIT) *(Pack<uint16_t, 8> *)(to + total * 16) = lo;
+                            if (SPLIT) *(Pack<uint16_t, 8> *)(to + G.block) = lo;
                         }
                     }
             }
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
 template <class T>
 __global__ __launch_bounds__(256) void grad_given_kernel(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, int d, float scale,
                                                          const int32_t *__restrict__ ids, int given, const float *__restrict__ g, const float *__restrict__ lse,
-                                                         const float2 *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, uint16_t *__restrict__ G, int64_t total)
+                                                         const float2 *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, Rows16 G)
 {
     const int lane = threadIdx.x & 63;
     const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -146,11 +146,11 @@ __global__ __launch_bounds__(256) void grad_given_kernel(const T *__restrict__ x
     const float2 c = coef[t];
     const float p = __builtin_amdgcn_exp2f(s * 1.44269504088896341f);
     const float v = sum - (p > 0.0f || p != p ? p * __fmaf_rn(c.y, s, c.x) : 0.0f);
-    uint16_t *to = G + (block16<sizeof(T) == 4>(t) * total + id - lo) * 16 + turned16((int)t & 15);
+    uint16_t *to = (uint16_t *)G.p + block16<sizeof(T) == 4>(t) * G.block + (id - lo) * G.row + turned16((int)t & 15);
     uint16_t hi, low = 0;
     put16(v * grad_factor(largest), &hi, &low, T{});
     *to = hi;
-    if (sizeof(T) == 4) to[total * 16] = low;
+    if (sizeof(T) == 4) to[G.block] = low;
 }
 
 // fn for every four rows side by side of a lane's accumulators acc[a][j][4 b ..]. One after the other: the compiler would
@@ -293,10 +293,10 @@ static ProbGradScratch prob_grad_scratch(const ProbGradParams &p, void *base)
     s.largest = (Largest *)take(sizeof(Largest));
     s.coef = (float2 *)take(sizeof(float2) * (size_t)p.nq);
     s.sums = (float *)take(sizeof(float) * (size_t)s.splits * p.nq * p.d);
-    s.q16 = (uint16_t *)take((size_t)p.nq * s.steps * kStepBytes);
-    s.qt16 = (uint16_t *)take((size_t)p.d * g_bytes);
-    s.G = (uint16_t *)take((size_t)s.part * g_bytes);
-    if (s.pack) s.x16 = (uint16_t *)take((size_t)s.part * row_bytes);
+    s.q16 = (uint16_t *)take(packed_bytes(p.nq, s.steps));
+    s.qt16 = (uint16_t *)take(packed_bytes(p.d, s.q_steps));
+    s.G = (uint16_t *)take(packed_bytes(s.part, s.q_steps));
+    if (s.pack) s.x16 = (uint16_t *)take(packed_bytes(s.part, s.d_steps));
     s.bytes = at;
     return s;
 }
@@ -337,7 +337,7 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
     }
     const Rows16 Q = packed_rows(s.q16, p.nq), Qt = packed_rows(s.qt16, p.d);
     AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, Q, SPLIT ? &s.largest->queries : nullptr, nullptr, false, st));
-    if (p.dpoints) AVQ_TRY(launch_pack_transposed(p.queries, p.type, p.nq, p.d, p.ld_queries, s.q_steps, s.qt16, &s.largest->queries, st));
+    if (p.dpoints) AVQ_TRY(launch_pack_transposed(p.queries, p.type, p.nq, p.d, p.ld_queries, s.q_steps, Qt, &s.largest->queries, st));
     for (int64_t lo = 0; lo < p.n; lo += s.part) {
         const int64_t rows = std::min<int64_t>(s.part, p.n - lo), whole = (rows + kTileN - 1) / kTileN * kTileN; // rows past the last have G = 0
         const T *x = (const T *)p.points + lo * p.ld_points;
@@ -349,12 +349,12 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         const Rows16 G = packed_rows(s.G, whole);
         const int parts = parts_for((rows + kTileN - 1) / kTileN, s.q_tiles, kGradGroups);
         const dim3 grid((unsigned)(parts * s.q_tiles));
-        if (p.grad_entropy) grad_tile_kernel<T, H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, s.steps, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, whole);
-        else grad_tile_kernel<T, H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, s.steps, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, s.G, s.qw, whole);
+        if (p.grad_entropy) grad_tile_kernel<T, H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, s.steps, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, G, s.qw);
+        else grad_tile_kernel<T, H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, s.steps, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, G, s.qw);
         AVQ_HIP(hipGetLastError());
         if (p.given > 0) {
             grad_given_kernel<T><<<dim3((unsigned)(((int64_t)p.nq * p.given + 3) / 4)), dim3(256), 0, st>>>((const T *)p.points, p.ld_points, q, p.nq, p.ld_queries, p.d, p.scale, p.ids, p.given,
-                                                                                                        p.grad_logp, p.lse, s.coef, s.largest, lo, rows, s.G, whole);
+                                                                                                        p.grad_logp, p.lse, s.coef, s.largest, lo, rows, G);
             AVQ_HIP(hipGetLastError());
         }
         if (p.dpoints) {

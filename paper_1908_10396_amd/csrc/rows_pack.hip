@@ -157,7 +157,7 @@ int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, i
 
 // 64 x 64 elements a workgroup, turned in LDS
 template <class T>
-__global__ __launch_bounds__(256) void pack_transposed_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int width, uint16_t *__restrict__ out,
+__global__ __launch_bounds__(256) void pack_transposed_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int width, Rows16 to_rows,
                                                               const uint32_t *__restrict__ largest)
 {
     constexpr bool SPLIT = sizeof(T) == 4;
@@ -176,18 +176,18 @@ __global__ __launch_bounds__(256) void pack_transposed_kernel(const T *__restric
         const int c = c0 + (i >> 6);
         const int64_t t = t0 + (i & 63);
         if (c >= d || t >= width) continue;
-        uint16_t *to = out + (block16<SPLIT>(t) * d + c) * 16 + turned16((int)t & 15);
-        if constexpr (SPLIT) split_f16(tile[i & 63][i >> 6] * s, to, to + (int64_t)d * 16);
+        uint16_t *to = (uint16_t *)to_rows.p + block16<SPLIT>(t) * to_rows.block + c * to_rows.row + turned16((int)t & 15);
+        if constexpr (SPLIT) split_f16(tile[i & 63][i >> 6] * s, to, to + to_rows.block);
         else *to = tile[i & 63][i >> 6];
     }
 }
 
-int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, uint16_t *out, const uint32_t *largest, hipStream_t st)
+int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, hipStream_t st)
 {
     const int width = steps * (type == AVQ_F32 ? 16 : 32);
     const dim3 grid((unsigned)((width + 63) / 64), (unsigned)((d + 63) / 64));
-    if (type == AVQ_F32) pack_transposed_kernel<float><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, width, out, largest);
-    else pack_transposed_kernel<uint16_t><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, width, out, nullptr);
+    if (type == AVQ_F32) pack_transposed_kernel<float><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, width, to, largest);
+    else pack_transposed_kernel<uint16_t><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, width, to, nullptr);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
