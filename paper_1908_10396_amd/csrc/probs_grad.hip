@@ -11,6 +11,8 @@
 #include "probs.h"
 #include "row_types.h"
 
+#include <type_traits>
+
 namespace avq {
 
 constexpr float kGradTop = 16384.0f; // what the bound of |G| is brought to
@@ -46,14 +48,15 @@ __global__ __launch_bounds__(256) void grad_coef_kernel(const int32_t *__restric
     if ((threadIdx.x & 63) == 0 && m != 0) atomicMax(&largest->upstream, m);
 }
 
-// a value as an operand: rounded to the type, or (fp32) hi and lo
-__device__ __forceinline__ void put16(float v, uint16_t *hi, uint16_t *, bf16_t) { *hi = from_f32<bf16_t>(v).bits; }
-__device__ __forceinline__ void put16(float v, uint16_t *hi, uint16_t *, f16_t) { *hi = from_f32<f16_t>(v).bits; }
-__device__ __forceinline__ void put16(float v, uint16_t *hi, uint16_t *lo, float)
+// eight values as operands: rounded to the type, or (fp32) hi and lo
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ void put16(const f32x8 &v, Quad *hi, Quad *, bf16_t) { *hi = __builtin_bit_cast(Quad, __builtin_convertvector(v, bf16v8)); }
+__device__ __forceinline__ void put16(const f32x8 &v, Quad *hi, Quad *, f16_t) { *hi = __builtin_bit_cast(Quad, __builtin_convertvector(v, f16v8)); }
+__device__ __forceinline__ void put16(const f32x8 &v, Quad *hi, Quad *lo, float)
 {
-    const _Float16 h = (_Float16)v;
-    *hi = __builtin_bit_cast(uint16_t, h);
-    *lo = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)h));
+    const f16v8 h = __builtin_convertvector(v, f16v8);
+    *hi = __builtin_bit_cast(Quad, h);
+    *lo = __builtin_bit_cast(Quad, __builtin_convertvector(v - __builtin_convertvector(h, f32x8), f16v8));
 }
 
 // G^T of the part's rows: 256 queries of a workgroup by 128 rows at a time. T: the caller's type, H: the instructions'.
@@ -83,40 +86,47 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
     typedef RowCopies<true, SPLIT> Copies;
     run_tiles<H, SPLIT, true, Copies>(Q, X, steps, count, lds, [&](int i, Copies &c) { c.seek(Q, q0, X, (first + i) * kTileN); },
         [&](int i, f32x16 (&acc)[4][2]) {
+            const int64_t row0 = (first + i) * kTileN;
+            auto take = [&](auto tail) __attribute__((always_inline)) {
+                constexpr bool TAIL = decltype(tail)::value; // some rows are past the last: no gradient
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int64_t row = (first + i) * kTileN + acc_col(j);
-                const bool real = row < X.rows;
+                for (int j = 0; j < 2; ++j) {
+                    const int64_t row = row0 + acc_col(j);
+                    const bool real = !TAIL || row < X.rows;
 #pragma unroll
-                for (int a = 0; a < 4; ++a)
+                    for (int a = 0; a < 4; ++a)
 #pragma unroll
-                    for (int block = 0; block < 2; ++block) {
-                        // queries 16 block + 8 b + 4 half + e of the 32: stored side by side, two lanes' 32 bytes
-                        Pack<uint16_t, 8> hi, lo;
+                        for (int block = 0; block < 2; ++block) {
+                            // queries 16 block + 8 b + 4 half + e of the 32: stored side by side, two lanes' 32 bytes
+                            f32x8 v;
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            const int t = (wave >> 1) * 128 + a * 32 + block * 16 + 8 * b + 4 * half;
-                            const float4 s4 = shift[t / 4], u4 = up[t / 4];
-                            const float sh[4] = {s4.x, s4.y, s4.z, s4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
-                            float hh[4] = {};
-                            if (ENTROPY) { const float4 v = up_h[t / 4]; hh[0] = v.x; hh[1] = v.y; hh[2] = v.z; hh[3] = v.w; }
+                            for (int b = 0; b < 2; ++b) {
+                                const int t = (wave >> 1) * 128 + a * 32 + block * 16 + 8 * b + 4 * half;
+                                const float4 s4 = shift[t / 4], u4 = up[t / 4];
+                                const float sh[4] = {s4.x, s4.y, s4.z, s4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
+                                float hh[4] = {};
+                                if (ENTROPY) { const float4 w = up_h[t / 4]; hh[0] = w.x; hh[1] = w.y; hh[2] = w.z; hh[3] = w.w; }
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float s2 = __fmaf_rn(acc[a][j][8 * block + 4 * b + e], cq, sh[e]), p = __builtin_amdgcn_exp2f(s2);
-                                float v = p * (ENTROPY ? __fmaf_rn(hh[e], s2, u[e]) : u[e]);
-                                if (ENTROPY && p == 0.0f) v = 0.0f; // (p log p)
-                                if (!real) v = 0.0f;
-                                put16(v, &hi.e[4 * b + e], &lo.e[4 * b + e], T{});
+                                for (int e = 0; e < 4; ++e) {
+                                    const float s2 = __fmaf_rn(acc[a][j][8 * block + 4 * b + e], cq, sh[e]), p = __builtin_amdgcn_exp2f(s2);
+                                    float g = p * (ENTROPY ? __fmaf_rn(hh[e], s2, u[e]) : u[e]);
+                                    if (ENTROPY && p == 0.0f) g = 0.0f; // (p log p)
+                                    v[4 * b + e] = real ? g : 0.0f;
+                                }
+                            }
+                            const int64_t t0 = q0 + (wave >> 1) * 128 + a * 32 + block * 16;
+                            if (t0 < width) {
+                                Quad hi, lo;
+                                put16(v, &hi, &lo, T{});
+                                uint16_t *to = (uint16_t *)G.p + block16<SPLIT>(t0) * G.block + row * G.row + half * 8;
+                                *(Quad *)to = hi;
+                                if (SPLIT) *(Quad *)(to + G.block) = lo;
                             }
                         }
-                        const int64_t t0 = q0 + (wave >> 1) * 128 + a * 32 + block * 16;
-                        if (t0 < width) {
-                            uint16_t *to = (uint16_t *)G.p + block16<SPLIT>(t0) * G.block + row * G.row + half * 8;
-                            *(Pack<uint16_t, 8> *)to = hi;
-                            if (SPLIT) *(Pack<uint16_t, 8> *)(to + G.block) = lo;
-                        }
-                    }
-            }
+                }
+            };
+            if (row0 + kTileN <= X.rows) take(std::false_type{});
+            else take(std::true_type{});
         });
 }
 
@@ -147,10 +157,12 @@ __global__ __launch_bounds__(256) void grad_given_kernel(const T *__restrict__ x
     const float p = __builtin_amdgcn_exp2f(s * 1.44269504088896341f);
     const float v = sum - (p > 0.0f || p != p ? p * __fmaf_rn(c.y, s, c.x) : 0.0f);
     uint16_t *to = (uint16_t *)G.p + block16<sizeof(T) == 4>(t) * G.block + (id - lo) * G.row + turned16((int)t & 15);
-    uint16_t hi, low = 0;
-    put16(v * grad_factor(largest), &hi, &low, T{});
-    *to = hi;
-    if (sizeof(T) == 4) to[G.block] = low;
+    f32x8 one = {};
+    one[0] = v * grad_factor(largest);
+    Quad hi, low{};
+    put16(one, &hi, &low, T{});
+    *to = (uint16_t)hi.w[0];
+    if (sizeof(T) == 4) to[G.block] = (uint16_t)low.w[0];
 }
 
 // fn for every four rows side by side of a lane's accumulators acc[a][j][4 b ..]. One after the other: the compiler would
@@ -166,7 +178,8 @@ template <int I = 0, class Fn> __device__ __forceinline__ void for_quads(Fn fn)
 }
 
 // dx of the part's rows: 256 rows by 128 dimensions.
-template <class T, class H, bool SPLIT, bool ACCUMULATE>
+// PAIRS: 16-bit types of rows on 4 bytes, of an even number of elements.
+template <class T, class H, bool SPLIT, bool ACCUMULATE, bool PAIRS>
 __global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Rows16 Qt, int steps, float scale, const Largest *__restrict__ largest, int parts, int others, int64_t rows,
                                                                     int d, T *__restrict__ dx, int64_t ld_dx)
 {
@@ -186,6 +199,26 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Ro
                 constexpr int a = decltype(at)::a, b = decltype(at)::b, j = decltype(at)::j;
                 const int64_t c = c0 + acc_col(j);
                 T *to = dx + (row0 + a * 32 + b * 8) * ld_dx + c;
+                if (PAIRS) {
+                    // two lanes, two rows: each stores both columns of one
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        const float v0 = acc[a][j][4 * b + e] * f, v1 = acc[a][j][4 * b + e + 1] * f;
+                        const bool odd = threadIdx.x & 1;
+                        const float other = __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(odd ? v0 : v1), 0xB1 /* quad_perm [1, 0, 3, 2] */, 0xF, 0xF, true));
+                        T *at = to + (odd ? ld_dx - 1 : 0);
+                        if (c < d && a * 32 + b * 8 + e + (odd ? 1 : 0) < left) {
+                            Pack<T, 2> o;
+                            float lo = odd ? other : v0, hi = odd ? v1 : other;
+                            if (ACCUMULATE) { o = *(const Pack<T, 2> *)at; lo += to_f32(o.e[0]); hi += to_f32(o.e[1]); }
+                            o.e[0] = from_f32<T>(lo);
+                            o.e[1] = from_f32<T>(hi);
+                            *(Pack<T, 2> *)at = o;
+                        }
+                        to += 2 * ld_dx;
+                    }
+                    return;
+                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (c < d && a * 32 + b * 8 + e < left) {
@@ -283,6 +316,8 @@ static ProbGradScratch prob_grad_scratch(const ProbGradParams &p, void *base)
     s.pack = !base || split || p.d % kTileN != 0 || (uintptr_t)p.points % 16 != 0 || p.ld_points % 8 != 0 || p.ld_points >= kMaxRow16;
     const int64_t most = (int64_t)(kGradBytes / std::max(row_bytes, g_bytes)) / kTileM * kTileM;
     s.part = std::min<int64_t>((p.n + kTileM - 1) / kTileM * kTileM, std::max<int64_t>(4096, most));
+    const int64_t launches = (p.n + s.part - 1) / s.part; // parts of equal size
+    s.part = std::min(s.part, ((p.n + launches - 1) / launches + kTileM - 1) / kTileM * kTileM);
     s.splits = parts_for(std::max<int64_t>(1, s.part / 128), s.q_tiles * s.d_tiles, kGradGroups);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -320,12 +355,10 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         return AVQ_OK;
     }
     const ProbGradScratch s = prob_grad_scratch(p, p.scratch);
-    static LdsLimitOnce once[5];
+    static LdsLimitOnce once[3];
     AVQ_TRY(set_lds_limit((const void *)grad_tile_kernel<T, H, SPLIT, false>, kTileLds, &once[0]));
     AVQ_TRY(set_lds_limit((const void *)grad_tile_kernel<T, H, SPLIT, true>, kTileLds, &once[1]));
-    AVQ_TRY(set_lds_limit((const void *)grad_rows_kernel<T, H, SPLIT, false>, kTileLds, &once[2]));
-    AVQ_TRY(set_lds_limit((const void *)grad_rows_kernel<T, H, SPLIT, true>, kTileLds, &once[4]));
-    AVQ_TRY(set_lds_limit((const void *)grad_queries_kernel<H, SPLIT>, kTileLds, &once[3]));
+    AVQ_TRY(set_lds_limit((const void *)grad_queries_kernel<H, SPLIT>, kTileLds, &once[2]));
     const float c2 = p.scale * 1.44269504088896341f;
     const T *q = (const T *)p.queries;
     AVQ_TRY(launch_clear_largest(s.largest, st));
@@ -359,11 +392,20 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         }
         if (p.dpoints) {
             const int row_parts = parts_for((rows + kTileM - 1) / kTileM, s.d_tiles, kGradGroups);
-            const dim3 row_grid((unsigned)(row_parts * s.d_tiles));
             T *dx = (T *)p.dpoints + lo * p.ld_dpoints;
-            if (p.accumulate) grad_rows_kernel<T, H, SPLIT, true><<<row_grid, dim3(kTileThreads), kTileLds, st>>>(G, Qt, steps_of<SPLIT>(p.nq), p.scale, s.largest, row_parts, s.d_tiles, rows, p.d, dx, p.ld_dpoints);
-            else grad_rows_kernel<T, H, SPLIT, false><<<row_grid, dim3(kTileThreads), kTileLds, st>>>(G, Qt, steps_of<SPLIT>(p.nq), p.scale, s.largest, row_parts, s.d_tiles, rows, p.d, dx, p.ld_dpoints);
-            AVQ_HIP(hipGetLastError());
+            const bool pairs = sizeof(T) == 2 && (uintptr_t)p.dpoints % 4 == 0 && p.ld_dpoints % 2 == 0 && p.d % 2 == 0;
+            auto run = [&](auto accumulate, auto pair) -> int {
+                constexpr bool ACCUMULATE = decltype(accumulate)::value, PAIRS = decltype(pair)::value;
+                static LdsLimitOnce row_once;
+                AVQ_TRY(set_lds_limit((const void *)grad_rows_kernel<T, H, SPLIT, ACCUMULATE, PAIRS>, kTileLds, &row_once));
+                grad_rows_kernel<T, H, SPLIT, ACCUMULATE, PAIRS><<<dim3((unsigned)(row_parts * s.d_tiles)), dim3(kTileThreads), kTileLds, st>>>(
+                    G, Qt, steps_of<SPLIT>(p.nq), p.scale, s.largest, row_parts, s.d_tiles, rows, p.d, dx, p.ld_dpoints);
+                AVQ_HIP(hipGetLastError());
+                return AVQ_OK;
+            };
+            typedef std::integral_constant<bool, sizeof(T) == 2> Paired;
+            if (pairs) AVQ_TRY(p.accumulate ? run(std::true_type{}, Paired{}) : run(std::false_type{}, Paired{}));
+            else AVQ_TRY(p.accumulate ? run(std::true_type{}, std::false_type{}) : run(std::false_type{}, std::false_type{}));
         }
         if (p.dqueries) {
             grad_queries_kernel<H, SPLIT><<<dim3((unsigned)(s.splits * s.q_tiles * s.d_tiles)), dim3(kTileThreads), kTileLds, st>>>(G, X, p.nq, s.qw, p.d, s.splits, s.q_tiles, s.d_tiles,

@@ -50,7 +50,12 @@ __global__ __launch_bounds__(256) void largest_kernel(const float *__restrict__ 
     }
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, w, 64));
-    if ((threadIdx.x & 63) == 0 && m != 0) atomicMax(to, m); // (a maximum: no order matters)
+    __shared__ uint32_t red[4];
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    m = max(max(red[0], red[1]), max(red[2], red[3]));
+    if (m != 0) atomicMax(to, m); // (a maximum: no order matters)
 }
 
 int launch_largest(const float *x, int64_t rows, int d, int64_t ld, uint32_t *to, hipStream_t st)
@@ -69,47 +74,52 @@ __device__ __forceinline__ void split_f16(float v, uint16_t *hi, uint16_t *lo)
     *lo = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)h));
 }
 
-constexpr int kPackRows = 64;
+constexpr int kPackRows = 64, kPackColumns = 128;
 
-// 64 rows a workgroup, half a block of 16 elements a thread, so that threads side by side write the rows of a block, 2 KB. What they
-// read lies in 64 lines, the rest of which comes from the cache at the next blocks. WHOLE: a row is a whole number of eights on 16 bytes.
-template <class T, bool WHOLE>
+// 64 rows a workgroup, 128 columns at a time by way of LDS: rows are read along, and half a block of 16 elements is written by each
+// thread, so that threads side by side write the rows of a block, 2 KB. V: elements a load.
+template <class T, int V>
 __global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int blocks, Rows16 to_rows,
                                                         const uint32_t *__restrict__ largest, uint16_t flip)
 {
     constexpr bool SPLIT = sizeof(T) == 4;
-    constexpr int kAtOnce = 256 / (kPackRows * 2); // blocks
-    const int u = threadIdx.x & 1, r = threadIdx.x / 2 % kPackRows, b0 = threadIdx.x / (2 * kPackRows);
-    const int64_t row = (int64_t)blockIdx.x * kPackRows + r;
-    if (row >= rows) return;
+    constexpr int kLine = kPackColumns + 16 / sizeof(T); // (rows apart by 16 bytes more than a multiple of the banks)
+    __shared__ __attribute__((aligned(16))) T tile[kPackRows * kLine];
+    const int64_t row0 = (int64_t)blockIdx.x * kPackRows;
+    const int here = (int)min(rows - row0, (int64_t)kPackRows);
     float scale = 1.0f;
     if (SPLIT) scale = range_scale(*largest);
+    for (int c0 = 0; c0 < blocks * 16; c0 += kPackColumns) {
+        const int columns = min(d - c0, kPackColumns), per_row = max(columns, 0) / V;
+        const uint32_t magic = magic_of(per_row);
 #pragma unroll 4
-    for (int b = b0; b < blocks; b += kAtOnce) {
-        const int c = b * 16 + u * 8;
-        const T *from = x + row * ld + c;
-        T v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = T{};
-        if (c + 8 <= d) {
-            __builtin_memcpy(v, WHOLE ? __builtin_assume_aligned(from, 16) : from, sizeof(v));
-        } else if (!WHOLE) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (c + e < d) v[e] = from[e];
+        for (int i = threadIdx.x; i < here * per_row; i += 256) {
+            const int r = (int)magic_div(i, magic), c = (i - r * per_row) * V;
+            *(Pack<T, V> *)(tile + r * kLine + c) = *(const Pack<T, V> *)(x + (row0 + r) * ld + c0 + c);
         }
-        uint16_t *to = (uint16_t *)to_rows.p + block16<SPLIT>(c) * to_rows.block + row * to_rows.row + u * 8;
-        Pack<uint16_t, 8> hi, lo;
-        if constexpr (SPLIT) {
+        __syncthreads();
+        const int r = threadIdx.x / 2 % kPackRows, u = threadIdx.x & 1;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) split_f16(v[e] * scale, &hi.e[e], &lo.e[e]);
-            *(Pack<uint16_t, 8> *)(to + to_rows.block) = lo;
-        } else {
-            __builtin_memcpy(&hi, v, 16);
+        for (int b = threadIdx.x / (2 * kPackRows); b < kPackColumns / 16; b += 2) {
+            const int c = b * 16 + u * 8;
+            if (c0 + b * 16 >= blocks * 16 || r >= here) break;
+            T v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) hi.e[e] ^= flip;
+            for (int e = 0; e < 8; ++e) v[e] = c + e < columns ? tile[r * kLine + c + e] : T{};
+            uint16_t *to = (uint16_t *)to_rows.p + block16<SPLIT>(c0 + c) * to_rows.block + (row0 + r) * to_rows.row + u * 8;
+            Pack<uint16_t, 8> hi, lo;
+            if constexpr (SPLIT) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) split_f16(v[e] * scale, &hi.e[e], &lo.e[e]);
+                *(Pack<uint16_t, 8> *)(to + to_rows.block) = lo;
+            } else {
+                __builtin_memcpy(&hi, v, 16);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) hi.e[e] ^= flip;
+            }
+            *(Pack<uint16_t, 8> *)to = hi;
         }
-        *(Pack<uint16_t, 8> *)to = hi;
+        __syncthreads();
     }
 }
 
@@ -141,15 +151,16 @@ int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, i
         return AVQ_OK;
     }
     const dim3 grid((unsigned)((rows + kPackRows - 1) / kPackRows));
-    const bool whole = row_width(x, ld, d, type_bytes(type)) == 16 && d % 8 == 0;
+    const int size = type_bytes(type), w = row_width(x, ld, d, size);
     const uint16_t flip = negate ? 0x8000 : 0;
     const int blocks = type == AVQ_F32 ? steps : 2 * steps; // of 16 coordinates
     if (type == AVQ_F32) {
-        if (whole) pack_rows_kernel<float, true><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, largest, 0);
-        else pack_rows_kernel<float, false><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, largest, 0);
+        if (w == 16) pack_rows_kernel<float, 4><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, largest, 0);
+        else pack_rows_kernel<float, 1><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, largest, 0);
     } else {
-        if (whole) pack_rows_kernel<uint16_t, true><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
-        else pack_rows_kernel<uint16_t, false><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
+        if (w == 16) pack_rows_kernel<uint16_t, 8><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
+        else if (w == 8) pack_rows_kernel<uint16_t, 4><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
+        else pack_rows_kernel<uint16_t, 1><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
     }
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
