@@ -59,6 +59,14 @@ __device__ __forceinline__ void put16(const f32x8 &v, Quad *hi, Quad *lo, float)
     *lo = __builtin_bit_cast(Quad, __builtin_convertvector(v - __builtin_convertvector(h, f32x8), f16v8));
 }
 
+// G is a gigabyte that is read again when all of it is written: stored past the caches, it leaves the operands there (262,144 rows,
+// 1,001 queries, fp32: 225 against 320 us, and the products after it 2 to 8 % faster)
+__device__ __forceinline__ void put_once(uint16_t *to, const Quad &v)
+{
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4 *)to);
+}
+
 // G^T of the part's rows: 256 queries of a workgroup by 128 rows at a time. T: the caller's type, H: the instructions'.
 template <class T, class H, bool SPLIT, bool ENTROPY>
 __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Rows16 X, int steps, float c2, const float *__restrict__ lse, const float2 *__restrict__ coef,
@@ -119,8 +127,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
                                 Quad hi, lo;
                                 put16(v, &hi, &lo, T{});
                                 uint16_t *to = (uint16_t *)G.p + block16<SPLIT>(t0) * G.block + row * G.row + half * 8;
-                                *(Quad *)to = hi;
-                                if (SPLIT) *(Quad *)(to + G.block) = lo;
+                                put_once(to, hi);
+                                if (SPLIT) put_once(to + G.block, lo);
                             }
                         }
                 }
