@@ -24,12 +24,13 @@ __device__ __forceinline__ Stat join(const Stat &a, const Stat &b)
 }
 
 // Dynamic LDS of the kernel that finishes a query: the query in fp32; candidate groups, then the keys of 32 rows for each of the k
-// best groups; the k best of them; the groups.
+// best groups; the rows that may be among the k best; the groups.
 constexpr size_t kFinishLds = kMaxDynLds - 16 * 1024;
-constexpr int kFinishList = 2048; // candidate groups that are kept (and room for a value of each of 1,024 threads)
+constexpr int kFinishList = 2048; // candidate groups that are kept
+__host__ __device__ constexpr int finish_best(int k) { return k < 192 ? 256 : k + 64; }
 inline size_t finish_lds(int d, int k)
 {
-    return (((size_t)d * 4 + 15) & ~(size_t)15) + (k == 0 ? 0 : (size_t)std::max(32 * k, kFinishList) * 8 + (size_t)k * (8 + 4));
+    return (((size_t)d * 4 + 15) & ~(size_t)15) + (k == 0 ? 0 : (size_t)std::max(32 * k, kFinishList) * 8 + (size_t)finish_best(k) * 8 + (size_t)k * 4);
 }
 
 } // namespace avq

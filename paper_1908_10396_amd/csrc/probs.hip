@@ -231,14 +231,21 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prob_stream_kernel(const T 
         Stat a{m[i] > -INFINITY ? m[i] * c2 : -INFINITY, l[i], t[i]};
 #pragma unroll
         for (int x16 = 16; x16 < 64; x16 *= 2) a = join(a, Stat{__shfl_xor(a.m, x16, 64), __shfl_xor(a.l, x16, 64), __shfl_xor(a.t, x16, 64)});
-        if (kg == 0) joined[wave][i * 16 + r16] = make_float4(a.m, a.l, a.t, 0.0f);
+        float top = m[i];
+#pragma unroll
+        for (int x16 = 16; x16 < 64; x16 *= 2) top = fmaxf(top, __shfl_xor(top, x16, 64));
+        if (kg == 0) joined[wave][i * 16 + r16] = make_float4(a.m, a.l, a.t, top);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < QT * 16; i += kStreamThreads) {
         if (q0 + i >= nq) continue;
         Stat a{joined[0][i].x, joined[0][i].y, joined[0][i].z};
-        for (int w = 1; w < kStreamWaves; ++w) a = join(a, Stat{joined[w][i].x, joined[w][i].y, joined[w][i].z});
-        stats[(size_t)blockIdx.x * nq + q0 + i] = make_float4(a.m, a.l, a.t, 0.0f);
+        float top = joined[0][i].w;
+        for (int w = 1; w < kStreamWaves; ++w) {
+            a = join(a, Stat{joined[w][i].x, joined[w][i].y, joined[w][i].z});
+            top = fmaxf(top, joined[w][i].w);
+        }
+        stats[(size_t)blockIdx.x * nq + q0 + i] = make_float4(a.m, a.l, a.t, top);
     }
 }
 
@@ -327,8 +334,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
     for (int j = 0; j < 2; ++j) {
         Stat a{m[j] > -INFINITY ? m[j] * cq[j] : -INFINITY, l[j], t[j]};
         a = join(a, Stat{__shfl_xor(a.m, 32, 64), __shfl_xor(a.l, 32, 64), __shfl_xor(a.t, 32, 64)});
+        const float top = fmaxf(m[j], __shfl_xor(m[j], 32, 64));
         const int64_t q = q0 + acc_col(j);
-        if (lane < 32 && q < Q.rows) stats[(size_t)(place.part * 2 + (wave >> 1)) * Q.rows + q] = make_float4(a.m, a.l, a.t, 0.0f);
+        if (lane < 32 && q < Q.rows) stats[(size_t)(place.part * 2 + (wave >> 1)) * Q.rows + q] = make_float4(a.m, a.l, a.t, top);
     }
 }
 
@@ -345,34 +353,46 @@ __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o
 template <int R, int F> struct Shape { static constexpr int rows = R, loads = F; };
 
 // <q, x> of R rows at once by 16 lanes, F loads of 16 bytes a row in flight (fp32, the same order of additions whatever R and F:
-// a lane's coordinates in order, then the lanes); every lane of the group gets them. NULL: a row that is not there.
+// a lane's coordinates in order, then the lanes); every lane of the group gets them. Loads past a row's last 16 bytes are made at
+// its start and count for nothing: no load waits for a branch.
 template <class T, int R, int F>
 __device__ __forceinline__ void dots16(const float *__restrict__ qf, const T *const (&row)[R], int d, int lane16, float (&s)[R])
 {
     constexpr int E = kFragElems<T>;
+    const int whole = d / E * E;
 #pragma unroll
     for (int r = 0; r < R; ++r) s[r] = 0.0f;
-    for (int k0 = lane16 * E; k0 < d; k0 += F * 16 * E) {
+#pragma unroll 1
+    for (int k0 = 0; k0 < whole; k0 += F * 16 * E) {
         Frag f[R][F];
 #pragma unroll
-        for (int u = 0; u < F; ++u)
+        for (int u = 0; u < F; ++u) {
+            const int k = k0 + (u * 16 + lane16) * E;
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                f[r][u] = Frag{};
-                if (row[r] && k0 + u * 16 * E < d) f[r][u] = load_frag<T, false>(row[r], k0 + u * 16 * E, d);
-            }
+            for (int r = 0; r < R; ++r) f[r][u] = load_whole<T, false>(row[r] + (k < whole ? k : 0));
+        }
 #pragma unroll
         for (int u = 0; u < F; ++u) {
-            const int k = k0 + u * 16 * E;
-            if (k >= d) break;
+            const int k = k0 + (u * 16 + lane16) * E;
+            if (k0 + u * 16 * E >= whole) break;
+            float qv[E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) qv[j] = qf[k < whole ? k + j : 0];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 T e[E];
                 __builtin_memcpy(e, &f[r][u], 16);
 #pragma unroll
-                for (int j = 0; j < E; ++j) s[r] = __fmaf_rn(k + j < d ? qf[k + j] : 0.0f, to_f32(e[j]), s[r]);
+                for (int j = 0; j < E; ++j) {
+                    const float with = __fmaf_rn(qv[j], to_f32(e[j]), s[r]);
+                    s[r] = k < whole ? with : s[r];
+                }
             }
         }
+    }
+    if (lane16 < d - whole) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r] = __fmaf_rn(qf[whole + lane16], to_f32(row[r][whole + lane16]), s[r]);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) s[r] = group_sum<16>(s[r]);
@@ -386,7 +406,8 @@ template <class T> __device__ __forceinline__ float dot16(const float *__restric
     return s[0];
 }
 
-// A workgroup a query: joins the statistics, scores the given rows and the best ones.
+// A workgroup a query: joins the statistics, scores the given rows and the best ones. Latency: the fewest steps that wait for
+// one another. stats.w is the largest product of a part.
 template <class T, int NT>
 __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, float scale,
                                                          const float4 *__restrict__ stats, int parts, const int32_t *__restrict__ ids, int given, float *__restrict__ logp_out,
@@ -395,26 +416,30 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
 {
     __shared__ WgSelectScratch sel;
     __shared__ Stat wave_stat[NT / 64];
-    __shared__ uint32_t list_count, bound_shared;
+    __shared__ uint32_t list_count, found_count, bound_shared;
+    __shared__ u64 least_best;
     extern __shared__ char lds[];
     float *qf = (float *)lds;                                        // [d]
     u64 *keys = (u64 *)(lds + (((size_t)d * 4 + 15) & ~(size_t)15)); // [max(32 k, kFinishList)]: candidate groups, then rows
-    u64 *best = keys + std::max(32 * k, kFinishList);                // [k]
-    uint32_t *groups = (uint32_t *)(best + k);                       // [k]
+    u64 *best = keys + std::max(32 * k, kFinishList);                // [kFinishBest(k)]
+    uint32_t *groups = (uint32_t *)(best + finish_best(k));          // [k]
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = blockIdx.x;
+    uint32_t *tops = (uint32_t *)keys;      // [NT / per] largest product of a class
+    const bool by_parts = parts >= 4 * k; // the parts' largest products are classes enough
+    uint32_t mine_top = 0;
     for (int c = tid; c < d; c += NT) qf[c] = to_f32(q[(int64_t)row * ld_q + c]);
     Stat a{-INFINITY, 0.0f, 0.0f};
     for (int p = tid; p < parts; p += NT) {
         const float4 v = stats[(size_t)p * nq + row];
         a = join(a, Stat{v.x, v.y, v.z});
+        if (by_parts) mine_top = max(mine_top, order_of(v.w));
     }
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) a = join(a, Stat{__shfl_xor(a.m, w, 64), __shfl_xor(a.l, w, 64), __shfl_xor(a.t, w, 64)});
     if (lane == 0) wave_stat[wave] = a;
-    if (tid == 0) list_count = 0;
+    if (tid == 0) { list_count = found_count = bound_shared = 0; least_best = ~0ull; }
 
-    // The largest group of every few threads, 4 k classes or more: the k-th largest of those bounds the k-th largest group from below.
     const uint32_t n_groups = (uint32_t)((n + 31) / 32);
     const float *gm = gmax + row * gstride;
     auto each_group = [&](auto &&fn) { // (four groups a load; the last four may lie past the end)
@@ -422,7 +447,7 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
         for (uint32_t g0 = 4 * tid; g0 < n_groups; g0 += 4 * NT * U) {
             float4 v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = g0 + 4 * NT * u < n_groups ? *(const float4 *)(gm + g0 + 4 * NT * u) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int u = 0; u < U; ++u) v[u] = *(const float4 *)(gm + min(g0 + 4 * NT * u, (n_groups - 1) & ~3u));
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const float e[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
@@ -434,15 +459,17 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
             }
         }
     };
-    uint32_t *tops = (uint32_t *)keys;
+    // Classes of groups, 4 k or more where there are: the k-th largest of their maxima bounds the k-th largest group from below. A
+    // class is what a few threads see of the parts or, where these are too few, of a pass over the groups.
     int per = 16; // threads a class
-    while (per > 1 && NT / per < 4 * k) per /= 2;
-    const int classes = NT / per;
+    const int seen = by_parts ? min(parts, NT) : NT; // threads that have seen any
+    while (per > 1 && seen / per < 4 * k) per /= 2;
+    const int classes = (seen + per - 1) / per;
     if (k > 0) {
-        uint32_t mine = 0;
-        each_group([&](uint32_t, uint32_t o) { mine = max(mine, o); });
-        for (int w = 1; w < per; w <<= 1) mine = max(mine, (uint32_t)__shfl_xor((int)mine, w, 64));
-        if (tid % per == 0) tops[tid / per] = mine;
+        if (!by_parts) each_group([&](uint32_t, uint32_t o) { mine_top = max(mine_top, o); });
+        for (int w = 1; w < per; w <<= 1) mine_top = max(mine_top, (uint32_t)__shfl_xor((int)mine_top, w, 64));
+        // (the last bits make classes different; without them the bound is a little lower)
+        if (tid % per == 0) tops[tid / per] = (mine_top & ~1023u) | (uint32_t)(1023 - tid / per);
     }
     __syncthreads();
     a = wave_stat[0];
@@ -465,13 +492,9 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
     if (tid < classes) {
         const uint32_t mine = tops[tid];
         uint32_t rank = 0;
-#pragma unroll 4
-        for (int o = 0; o < classes; o += 4) {
-            const uint4 v = *(const uint4 *)(tops + o);
-            rank += (v.x > mine || (v.x == mine && o + 0 < tid)) + (v.y > mine || (v.y == mine && o + 1 < tid)) + (v.z > mine || (v.z == mine && o + 2 < tid)) +
-                    (v.w > mine || (v.w == mine && o + 3 < tid));
-        }
-        if (rank == (uint32_t)k - 1) bound_shared = mine; // (k <= classes)
+#pragma unroll 8
+        for (int o = 0; o < classes; ++o) rank += tops[o] > mine;
+        if (rank == (uint32_t)k - 1) bound_shared = mine & ~1023u; // (k <= classes)
     }
     __syncthreads();
     const uint32_t bound = bound_shared;
@@ -483,21 +506,32 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
     });
     __syncthreads();
     const uint32_t listed = list_count;
-    u64 least;
-    if (listed <= kFinishList) least = wg_select_threshold_of([&](auto &&fn) { for (uint32_t i = tid; i < listed; i += NT) fn(keys[i]); }, k, &sel);
-    else least = wg_select_threshold_of([&](auto &&fn) { each_group([&](uint32_t g, uint32_t o) { fn(key_of(g, o)); }); }, k, &sel);
-    __syncthreads();
-    if (tid == 0) list_count = 0;
-    __syncthreads();
-    auto choose = [&](u64 key) {
-        if (key < least) return;
-        const uint32_t at = atomicAdd(&list_count, 1u);
-        if (at < (uint32_t)k) groups[at] = 0xffffffffu - (uint32_t)key;
-    };
-    if (listed <= kFinishList) for (uint32_t i = tid; i < listed; i += NT) choose(keys[i]);
-    else each_group([&](uint32_t g, uint32_t o) { choose(key_of(g, o)); });
-    __syncthreads();
-    const uint32_t rows = min(list_count, (uint32_t)k) * 32u;
+    if (listed <= 256) {
+        for (uint32_t i = tid; i < listed; i += NT) {
+            const u64 mine = keys[i];
+            uint32_t rank = 0;
+#pragma unroll 8
+            for (uint32_t o = 0; o < listed; ++o) rank += keys[o] > mine;
+            if (rank < (uint32_t)k) groups[rank] = 0xffffffffu - (uint32_t)mine;
+        }
+        __syncthreads();
+    } else {
+        u64 least;
+        if (listed <= kFinishList) least = wg_select_threshold_of([&](auto &&fn) { for (uint32_t i = tid; i < listed; i += NT) fn(keys[i]); }, k, &sel);
+        else least = wg_select_threshold_of([&](auto &&fn) { each_group([&](uint32_t g, uint32_t o) { fn(key_of(g, o)); }); }, k, &sel);
+        __syncthreads();
+        if (tid == 0) list_count = 0;
+        __syncthreads();
+        auto choose = [&](u64 key) {
+            if (key < least) return;
+            const uint32_t at = atomicAdd(&list_count, 1u);
+            if (at < (uint32_t)k) groups[at] = 0xffffffffu - (uint32_t)key;
+        };
+        if (listed <= kFinishList) for (uint32_t i = tid; i < listed; i += NT) choose(keys[i]);
+        else each_group([&](uint32_t g, uint32_t o) { choose(key_of(g, o)); });
+        __syncthreads();
+    }
+    const uint32_t chosen = min(min(list_count, listed), (uint32_t)k), rows = chosen * 32u;
     auto score = [&](auto shape) {
         constexpr int R = decltype(shape)::rows, F = decltype(shape)::loads;
         for (uint32_t i = sub * R; i < rows; i += subs * R) {
@@ -507,12 +541,12 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 id[r] = (int64_t)groups[i / 32] * 32 + (i & 31) + r; // (R divides 32)
-                p[r] = id[r] < n ? x + id[r] * ld_x : nullptr;
+                p[r] = x + min(id[r], n - 1) * ld_x;
             }
             dots16<T, R, F>(qf, p, d, lane16, s);
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                if (lane16 == r) keys[i + r] = p[r] ? ((u64)order_of(s[r] * scale) << 32) | (u64)(0xffffffffu - (uint32_t)id[r]) : 0;
+                if (lane16 == r) keys[i + r] = id[r] < n ? ((u64)order_of(s[r] * scale) << 32) | (u64)(0xffffffffu - (uint32_t)id[r]) : 0;
         }
     };
     // short rows several at a time, so that as many loads are in flight
@@ -520,21 +554,47 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
     if (d <= 2 * kPer) score(Shape<4, 2>{});
     else if (d <= 4 * kPer) score(Shape<2, 4>{});
     else score(Shape<1, 8>{});
-    if (tid == 0) list_count = 0;
     __syncthreads();
-    const u64 kth = wg_select_threshold_of([&](auto &&fn) { for (uint32_t i = tid; i < rows; i += NT) if (keys[i]) fn(keys[i]); }, k, &sel);
-    __syncthreads();
+    // The best row of every chosen group: with k of them, the least of those bounds the k-th best row from below.
+    if (chosen == (uint32_t)k) {
+        for (uint32_t i = tid; i < rows; i += NT) { // (32 lanes a group)
+            u64 top = keys[i];
+#pragma unroll
+            for (int w = 1; w < 32; w <<= 1) {
+                const u64 o = ((u64)(uint32_t)__shfl_xor((int)(top >> 32), w, 64) << 32) | (uint32_t)__shfl_xor((int)(uint32_t)top, w, 64);
+                top = o > top ? o : top;
+            }
+            if ((i & 31) == 0) atomicMin(&least_best, top);
+        }
+        __syncthreads();
+    }
+    const u64 floor_key = chosen == (uint32_t)k ? least_best : 1ull;
     for (uint32_t i = tid; i < rows; i += NT)
-        if (keys[i] && keys[i] >= kth) {
-            const uint32_t at = atomicAdd(&list_count, 1u);
-            if (at < (uint32_t)k) best[at] = keys[i];
+        if (keys[i] >= floor_key) {
+            const uint32_t at = atomicAdd(&found_count, 1u);
+            if (at < (uint32_t)finish_best(k)) best[at] = keys[i];
         }
     __syncthreads();
-    const uint32_t found = min(list_count, (uint32_t)k);
+    uint32_t found = found_count;
+    if (found > (uint32_t)finish_best(k)) { // many rows alike
+        const u64 kth = wg_select_threshold_of([&](auto &&fn) { for (uint32_t i = tid; i < rows; i += NT) if (keys[i]) fn(keys[i]); }, k, &sel);
+        __syncthreads();
+        if (tid == 0) found_count = 0;
+        __syncthreads();
+        for (uint32_t i = tid; i < rows; i += NT)
+            if (keys[i] && keys[i] >= kth) {
+                const uint32_t at = atomicAdd(&found_count, 1u);
+                if (at < (uint32_t)k) best[at] = keys[i];
+            }
+        __syncthreads();
+        found = min(found_count, (uint32_t)k);
+    }
     for (uint32_t i = tid; i < found; i += NT) {
         const u64 mine = best[i];
         uint32_t rank = 0;
+#pragma unroll 4
         for (uint32_t o = 0; o < found; ++o) rank += best[o] > mine;
+        if (rank >= (uint32_t)k) continue;
         alt_ids[(int64_t)row * k + rank] = (int32_t)(0xffffffffu - (uint32_t)mine);
         alt_logp[(int64_t)row * k + rank] = value_of((uint32_t)(mine >> 32)) - lse;
     }
