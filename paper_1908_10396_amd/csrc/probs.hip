@@ -249,6 +249,163 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prob_stream_kernel(const T 
     }
 }
 
+// ---- one or two queries: rows by lanes side by side -----------------------------------------------
+
+constexpr int kRowThreads = 256, kRowWaves = kRowThreads / 64;
+constexpr int kRowLoads = 8; // of 16 bytes a lane in flight, and as many of the next rows
+
+// A row by L lanes that hold F times 16 bytes of it each, so that a wave's loads lie side by side in memory (the matrix
+// instruction's layout reads 64 bytes here and there: 1,183,514 x 100 fp32 98 us). Bound by memory. A wave takes 32 rows at a time,
+// U x 64 / L of them at once; the lanes' parts of U rows' products are added up together, each exchange halving the rows a lane has.
+template <class T, int NQ, int L, int F>
+__global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int64_t ld_q, float c2,
+                                                               float4 *__restrict__ stats, float *__restrict__ gmax, int64_t gstride)
+{
+    constexpr int E = kFragElems<T>, U = kRowLoads / F, kGroups = 64 / L, kAtOnce = U * kGroups, kTurns = 32 / kAtOnce;
+    static_assert(kTurns >= 1 && kTurns * kAtOnce == 32, "a wave's 32 rows");
+    __shared__ float4 joined[kRowWaves][NQ];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in_row = lane % L, group = lane / L;
+    const bool mine = in_row < U; // lanes of a row beyond hold the same sums
+    float qf[NQ][F][E];
+    int at[F];         // the lane's elements
+    uint32_t mask[F][4]; // those before the row's end
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+        const int k = (f * L + in_row) * E;
+        at[f] = k < d ? k : 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if (sizeof(T) == 4) mask[f][w] = k + w < d ? ~0u : 0u;
+            else mask[f][w] = (k + 2 * w < d ? 0xffffu : 0u) | (k + 2 * w + 1 < d ? 0xffff0000u : 0u);
+        }
+#pragma unroll
+        for (int i = 0; i < NQ; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) qf[i][f][e] = k + e < d ? (c2 < 0.0f ? -1.0f : 1.0f) * to_f32(q[i * ld_q + k + e]) : 0.0f;
+    }
+    c2 = fabsf(c2); // (so that the largest product is the largest logit)
+    float m[NQ], l[NQ], t[NQ], top[NQ], best[NQ];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) { m[i] = top[i] = best[i] = -INFINITY; l[i] = t[i] = 0.0f; }
+    // (16 bytes of the last row may run past the last element: the tile that holds it, and rows shorter than 16 bytes, go by themselves)
+    const int64_t tiles = (n + 31) / 32, whole = d >= E ? (n - 1) / 32 : 0, stride = (int64_t)gridDim.x * kRowWaves;
+
+    struct Rows { Frag f[U][F]; };
+    auto row_of = [&](int64_t tile, int turn, int u) __attribute__((always_inline)) { return tile * 32 + turn * kAtOnce + u * kGroups + group; };
+    auto fetch = [&](Rows &r, int64_t tile, int turn) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int f = 0; f < F; ++f) r.f[u][f] = load_whole<T, false>(x + row_of(tile, turn, u) * ld_x + at[f]);
+    };
+    auto take = [&](const Rows &r, int64_t tile, int turn) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            float s[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                s[u] = 0.0f;
+#pragma unroll
+                for (int f = 0; f < F; ++f) {
+                    Frag v = r.f[u][f];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) v.w[w] &= mask[f][w];
+                    T e[E];
+                    __builtin_memcpy(e, &v, 16);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) s[u] = __fmaf_rn(qf[i][f][j], to_f32(e[j]), s[u]);
+                }
+            }
+            // U sums over L lanes: after log U exchanges lane l has those of row l % U, over the lanes alike but for these bits
+#pragma unroll
+            for (int w = 1; w < U; w <<= 1) {
+                const bool upper = (lane & w) != 0;
+#pragma unroll
+                for (int u = 0; u < U; u += 2 * w) {
+                    const float give = upper ? s[u] : s[u + w], keep = upper ? s[u + w] : s[u];
+                    s[u] = keep + __shfl_xor(give, w, 64);
+                }
+            }
+            float sum = s[0];
+#pragma unroll
+            for (int w = U; w < L; w <<= 1) sum += __shfl_xor(sum, w, 64);
+            const int64_t row = row_of(tile, turn, in_row % U);
+            const bool real = mine && row < n;
+            if (real && sum > m[i]) {
+                if (m[i] > -INFINITY) {
+                    const float down = (m[i] - sum) * c2, f = __builtin_amdgcn_exp2f(down);
+                    t[i] = f * __fmaf_rn(l[i], down, t[i]);
+                    l[i] *= f;
+                }
+                m[i] = sum;
+            }
+            const float s2 = m[i] > -INFINITY ? (sum - m[i]) * c2 : sum, e = __builtin_amdgcn_exp2f(s2);
+            if (real) {
+                l[i] += e;
+                t[i] = __fmaf_rn(e, s2, t[i]);
+                top[i] = fmaxf(top[i], sum);
+            }
+            if (turn == kTurns - 1 && gmax) {
+                float g = top[i];
+#pragma unroll
+                for (int w = 1; w < 64; w <<= 1) g = fmaxf(g, __shfl_xor(g, w, 64));
+                if (lane == 0) gmax[i * gstride + tile] = g;
+                best[i] = fmaxf(best[i], g);
+                top[i] = -INFINITY;
+            }
+        }
+    };
+    int64_t tile = (int64_t)blockIdx.x * kRowWaves + wave;
+    Rows here, next;
+    if (tile < whole) {
+        int turn = 0;
+        fetch(here, tile, 0);
+        auto step = [&](Rows &now, Rows &then) __attribute__((always_inline)) {
+            int64_t then_tile = tile;
+            int then_turn = turn + 1;
+            if (then_turn == kTurns) { then_turn = 0; then_tile += stride; }
+            const bool more = then_tile < whole;
+            if (more) fetch(then, then_tile, then_turn);
+            take(now, tile, turn);
+            tile = then_tile;
+            turn = then_turn;
+            return more;
+        };
+        while (step(here, next) && step(next, here)) {}
+    }
+    for (; tile < tiles; tile += stride)
+#pragma unroll 1
+        for (int turn = 0; turn < kTurns; ++turn) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int f = 0; f < F; ++f) {
+                    const int64_t row = row_of(tile, turn, u);
+                    here.f[u][f] = load_frag<T, false>(x + (row < n ? row : n - 1) * ld_x, (f * L + in_row) * E, d);
+                }
+            take(here, tile, turn);
+        }
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        Stat a{m[i] > -INFINITY ? 0.0f : -INFINITY, l[i], t[i]};
+        if (m[i] > -INFINITY) a.m = m[i] * c2;
+#pragma unroll
+        for (int w = 1; w < 64; w <<= 1) a = join(a, Stat{__shfl_xor(a.m, w, 64), __shfl_xor(a.l, w, 64), __shfl_xor(a.t, w, 64)});
+        if (lane == 0) joined[wave][i] = make_float4(a.m, a.l, a.t, best[i]);
+    }
+    __syncthreads();
+    if (threadIdx.x < NQ) {
+        const int i = threadIdx.x;
+        Stat a{joined[0][i].x, joined[0][i].y, joined[0][i].z};
+        float b = joined[0][i].w;
+        for (int w = 1; w < kRowWaves; ++w) {
+            a = join(a, Stat{joined[w][i].x, joined[w][i].y, joined[w][i].z});
+            b = fmaxf(b, joined[w][i].w);
+        }
+        stats[(size_t)blockIdx.x * NQ + i] = make_float4(a.m, a.l, a.t, b);
+    }
+}
+
 // ---- many queries: tiles of a matrix product ----------------------------------------------------
 
 // Statistics of 128 queries over a part of the rows, 256 rows at a time; a lane has two queries, 64 of a tile's rows of each.
@@ -551,9 +708,10 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
     };
     // short rows several at a time, so that as many loads are in flight
     constexpr int kPer = 16 * kFragElems<T>;
+    constexpr int kMore = NT == 1024 ? 2 : 1; // (a few queries: few workgroups, each of which has registers for it)
     if (d <= 2 * kPer) score(Shape<4, 2>{});
-    else if (d <= 4 * kPer) score(Shape<2, 4>{});
-    else score(Shape<1, 8>{});
+    else if (d <= 4 * kPer) score(Shape<2 * kMore, 4>{});
+    else score(Shape<kMore, 8>{});
     __syncthreads();
     // The best row of every chosen group: with k of them, the least of those bounds the k-th best row from below.
     if (chosen == (uint32_t)k) {
@@ -602,12 +760,16 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
 
 // ---- launches ----------------------------------------------------------------------------------
 
+constexpr int kRowGroups = 1024; // four a compute unit
+
 // Workgroups that share the rows of the stream.
 static int stream_groups(int64_t n, int query_tiles)
 {
     const int64_t tiles = (n + 31) / 32, most = std::max(1, 512 / query_tiles); // two workgroups a compute unit
     return (int)std::max<int64_t>(1, std::min<int64_t>((tiles + kStreamWaves - 1) / kStreamWaves, most));
 }
+
+static int row_groups(int64_t n) { return (int)std::min<int64_t>(((n + 31) / 32 + kRowWaves - 1) / kRowWaves, kRowGroups); }
 
 // Query tiles of 16 that a workgroup takes: as many as fit LDS beside another workgroup's, at most 4 (64 queries).
 static int stream_tile(int type, int d, int nq)
@@ -623,6 +785,9 @@ static bool by_tiles(int nq) { return nq > 64; }
 
 constexpr int kTileGroups = 512; // two workgroups a compute unit
 constexpr size_t kPackBytes = (size_t)1 << 30; // most that packed rows take at a time
+
+// One or two queries whose rows fit four loads of a wave go by rows.
+static bool by_rows(int type, int d, int nq) { return nq <= 2 && (size_t)d * type_bytes(type) <= 64 * 16 * 4; }
 
 struct ProbScratch {
     float4 *stats; float *gmax; int64_t gstride;
@@ -645,7 +810,7 @@ static ProbScratch prob_scratch(const ProbParams &p, void *base)
     if (!by_tiles(p.nq)) {
         s.qt = stream_tile(p.type, p.d, p.nq);
         s.query_tiles = (p.nq + 16 * s.qt - 1) / (16 * s.qt);
-        s.groups = stream_groups(p.n, s.query_tiles);
+        s.groups = by_rows(p.type, p.d, p.nq) ? row_groups(p.n) : stream_groups(p.n, s.query_tiles);
         s.stats = (float4 *)take((size_t)s.groups * p.nq * sizeof(float4));
     } else {
         const bool split = p.type == AVQ_F32;
@@ -689,6 +854,25 @@ static int stream_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
         (const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.nq, p.ld_queries, c2, p.scale < 0.0f, s.stats, s.gmax, s.gstride);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
+}
+
+template <class T, int NQ, int L, int F>
+static int row_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
+{
+    const float c2 = p.scale * 1.44269504088896341f;
+    prob_row_kernel<T, NQ, L, F><<<dim3(s.groups), dim3(kRowThreads), 0, st>>>((const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.ld_queries, c2, s.stats, s.gmax, s.gstride);
+    AVQ_HIP(hipGetLastError());
+    return AVQ_OK;
+}
+
+template <class T, int NQ>
+static int row_sized(const ProbParams &p, const ProbScratch &s, hipStream_t st)
+{
+    const int loads = (p.d + kFragElems<T> - 1) / kFragElems<T>; // 16 bytes of a row
+    if (loads <= 16) return row_run<T, NQ, 16, 1>(p, s, st);
+    if (loads <= 32) return row_run<T, NQ, 32, 1>(p, s, st);
+    if (loads <= 64) return row_run<T, NQ, 64, 1>(p, s, st);
+    return loads <= 128 ? row_run<T, NQ, 64, 2>(p, s, st) : row_run<T, NQ, 64, 4>(p, s, st);
 }
 
 template <class T, bool ALIGNED>
@@ -755,6 +939,8 @@ static int log_probs_typed(const ProbParams &p, hipStream_t st)
         if constexpr (sizeof(T) == 4) AVQ_TRY((tiles_run<f16_t, true>(p, s, st)));
         else AVQ_TRY((tiles_run<T, false>(p, s, st)));
         parts = s.launches * s.parts * 2;
+    } else if (by_rows(p.type, p.d, p.nq)) {
+        AVQ_TRY(p.nq == 1 ? (row_sized<T, 1>(p, s, st)) : (row_sized<T, 2>(p, s, st)));
     } else {
         const bool aligned = ((uintptr_t)p.points % 16) == 0 && (p.ld_points * sizeof(T)) % 16 == 0;
         AVQ_TRY(aligned ? (stream_sized<T, true>(p, s, st)) : (stream_sized<T, false>(p, s, st)));

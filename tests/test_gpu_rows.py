@@ -256,6 +256,16 @@ def test_log_probs(kind, n, d, nq):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [1, 2])
+@pytest.mark.parametrize("n,d", [(1, 7), (31, 3), (32, 64), (33, 8), (2000, 16), (4096, 60), (5000, 100), (777, 128), (3001, 131), (999, 256), (1025, 511), (1500, 1024), (700, 1030), (300, 2048), (100, 4100)])
+def test_log_probs_of_one_or_two_queries(kind, nq, n, d):
+    g, x, q, scale = _prob_inputs(n, d, nq, kind, 2)
+    ids, k = random_ids((nq, 2), n, g), min(n, 6)
+    _check_probs(avq.log_probs(x, q, ids, k, scale), x, q, scale, ids, k)
+    _check_probs(avq.log_probs(strided(x, 5, 3), strided(q, 1), k=k, scale=-scale), x, q, -scale, None, k)
+
+
+@pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("n,d,nq,k", [(100, 8, 3, 100), (3000, 16, 2, 512), (513, 4, 70, 512), (40_000, 100, 3, 50), (9000, 24, 140, 33), (2100, 40, 300, 7)])
 def test_alternatives_are_those_of_lowest_id_among_equals(kind, n, d, nq, k):
     """Rows and queries of small whole numbers: sums are exact, and most scores occur many times."""
