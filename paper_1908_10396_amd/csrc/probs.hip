@@ -31,6 +31,15 @@ __device__ __forceinline__ Frag load_whole(const T *__restrict__ p)
     return f;
 }
 
+// of what is not read again, and had better not displace what the caches hold
+template <class T>
+__device__ __forceinline__ Frag load_once(const T *__restrict__ p)
+{
+    typedef uint32_t on4 __attribute__((ext_vector_type(4), aligned(4)));
+    typedef uint32_t on2 __attribute__((ext_vector_type(4), aligned(2)));
+    return __builtin_bit_cast(Frag, sizeof(T) == 4 ? __builtin_nontemporal_load((const on4 *)p) : __builtin_nontemporal_load((const on2 *)p));
+}
+
 // The coordinates k .. k + kFragElems - 1 of a row of d, zeros past its end. ALIGNED: the row starts on 16 bytes.
 template <class T, bool ALIGNED>
 __device__ __forceinline__ Frag load_frag(const T *__restrict__ row, int k, int d)
@@ -249,24 +258,25 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prob_stream_kernel(const T 
     }
 }
 
-// ---- one or two queries: rows by lanes side by side -----------------------------------------------
+// ---- one query: rows by lanes side by side ---------------------------------------------------------
 
 constexpr int kRowThreads = 256, kRowWaves = kRowThreads / 64;
 constexpr int kRowLoads = 8; // of 16 bytes a lane in flight, and as many of the next rows
 
 // A row by L lanes that hold F times 16 bytes of it each, so that a wave's loads lie side by side in memory (the matrix
-// instruction's layout reads 64 bytes here and there: 1,183,514 x 100 fp32 98 us). Bound by memory. A wave takes 32 rows at a time,
+// instruction's layout reads 64 bytes here and there). Bound by memory: 1,183,514 x 100 fp32, one query, 71 us (6.7 TB/s), against 98
+// through the matrix instructions; with loads that stay in the caches, or with twice the waves, 84. A wave takes 32 rows at a time,
 // U x 64 / L of them at once; the lanes' parts of U rows' products are added up together, each exchange halving the rows a lane has.
-template <class T, int NQ, int L, int F>
-__global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int64_t ld_q, float c2,
-                                                               float4 *__restrict__ stats, float *__restrict__ gmax, int64_t gstride)
+template <class T, int L, int F, bool ONCE>
+__global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, float c2,
+                                                               float4 *__restrict__ stats, float *__restrict__ gmax)
 {
     constexpr int E = kFragElems<T>, U = kRowLoads / F, kGroups = 64 / L, kAtOnce = U * kGroups, kTurns = 32 / kAtOnce;
     static_assert(kTurns >= 1 && kTurns * kAtOnce == 32, "a wave's 32 rows");
-    __shared__ float4 joined[kRowWaves][NQ];
+    __shared__ float4 joined[kRowWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in_row = lane % L, group = lane / L;
     const bool mine = in_row < U; // lanes of a row beyond hold the same sums
-    float qf[NQ][F][E];
+    float qf[F][E];
     int at[F];         // the lane's elements
     uint32_t mask[F][4]; // those before the row's end
 #pragma unroll
@@ -279,14 +289,10 @@ __global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restri
             else mask[f][w] = (k + 2 * w < d ? 0xffffu : 0u) | (k + 2 * w + 1 < d ? 0xffff0000u : 0u);
         }
 #pragma unroll
-        for (int i = 0; i < NQ; ++i)
-#pragma unroll
-            for (int e = 0; e < E; ++e) qf[i][f][e] = k + e < d ? (c2 < 0.0f ? -1.0f : 1.0f) * to_f32(q[i * ld_q + k + e]) : 0.0f;
+        for (int e = 0; e < E; ++e) qf[f][e] = k + e < d ? (c2 < 0.0f ? -1.0f : 1.0f) * to_f32(q[k + e]) : 0.0f;
     }
     c2 = fabsf(c2); // (so that the largest product is the largest logit)
-    float m[NQ], l[NQ], t[NQ], top[NQ], best[NQ];
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) { m[i] = top[i] = best[i] = -INFINITY; l[i] = t[i] = 0.0f; }
+    float m = -INFINITY, l = 0.0f, t = 0.0f, top = -INFINITY, best = -INFINITY;
     // (16 bytes of the last row may run past the last element: the tile that holds it, and rows shorter than 16 bytes, go by themselves)
     const int64_t tiles = (n + 31) / 32, whole = d >= E ? (n - 1) / 32 : 0, stride = (int64_t)gridDim.x * kRowWaves;
 
@@ -296,63 +302,63 @@ __global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restri
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int f = 0; f < F; ++f) r.f[u][f] = load_whole<T, false>(x + row_of(tile, turn, u) * ld_x + at[f]);
+            for (int f = 0; f < F; ++f) {
+                const T *p = x + row_of(tile, turn, u) * ld_x + at[f];
+                r.f[u][f] = ONCE ? load_once<T>(p) : load_whole<T, false>(p);
+            }
     };
     auto take = [&](const Rows &r, int64_t tile, int turn) __attribute__((always_inline)) {
+        float s[U];
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            float s[U];
+        for (int u = 0; u < U; ++u) {
+            s[u] = 0.0f;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                s[u] = 0.0f;
+            for (int f = 0; f < F; ++f) {
+                Frag v = r.f[u][f];
 #pragma unroll
-                for (int f = 0; f < F; ++f) {
-                    Frag v = r.f[u][f];
+                for (int w = 0; w < 4; ++w) v.w[w] &= mask[f][w];
+                T e[E];
+                __builtin_memcpy(e, &v, 16);
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) v.w[w] &= mask[f][w];
-                    T e[E];
-                    __builtin_memcpy(e, &v, 16);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) s[u] = __fmaf_rn(qf[i][f][j], to_f32(e[j]), s[u]);
-                }
+                for (int j = 0; j < E; ++j) s[u] = __fmaf_rn(qf[f][j], to_f32(e[j]), s[u]);
             }
-            // U sums over L lanes: after log U exchanges lane l has those of row l % U, over the lanes alike but for these bits
+        }
+        // U sums over L lanes: after log U exchanges lane l has those of row l % U, over the lanes alike but for these bits
 #pragma unroll
-            for (int w = 1; w < U; w <<= 1) {
-                const bool upper = (lane & w) != 0;
+        for (int w = 1; w < U; w <<= 1) {
+            const bool upper = (lane & w) != 0;
 #pragma unroll
-                for (int u = 0; u < U; u += 2 * w) {
-                    const float give = upper ? s[u] : s[u + w], keep = upper ? s[u + w] : s[u];
-                    s[u] = keep + __shfl_xor(give, w, 64);
-                }
+            for (int u = 0; u < U; u += 2 * w) {
+                const float give = upper ? s[u] : s[u + w], keep = upper ? s[u + w] : s[u];
+                s[u] = keep + __shfl_xor(give, w, 64);
             }
-            float sum = s[0];
+        }
+        float sum = s[0];
 #pragma unroll
-            for (int w = U; w < L; w <<= 1) sum += __shfl_xor(sum, w, 64);
-            const int64_t row = row_of(tile, turn, in_row % U);
-            const bool real = mine && row < n;
-            if (real && sum > m[i]) {
-                if (m[i] > -INFINITY) {
-                    const float down = (m[i] - sum) * c2, f = __builtin_amdgcn_exp2f(down);
-                    t[i] = f * __fmaf_rn(l[i], down, t[i]);
-                    l[i] *= f;
-                }
-                m[i] = sum;
+        for (int w = U; w < L; w <<= 1) sum += __shfl_xor(sum, w, 64);
+        const int64_t row = row_of(tile, turn, in_row % U);
+        const bool real = mine && row < n;
+        if (real && sum > m) {
+            if (m > -INFINITY) {
+                const float down = (m - sum) * c2, f = __builtin_amdgcn_exp2f(down);
+                t = f * __fmaf_rn(l, down, t);
+                l *= f;
             }
-            const float s2 = m[i] > -INFINITY ? (sum - m[i]) * c2 : sum, e = __builtin_amdgcn_exp2f(s2);
-            if (real) {
-                l[i] += e;
-                t[i] = __fmaf_rn(e, s2, t[i]);
-                top[i] = fmaxf(top[i], sum);
-            }
-            if (turn == kTurns - 1 && gmax) {
-                float g = top[i];
+            m = sum;
+        }
+        const float s2 = m > -INFINITY ? (sum - m) * c2 : sum, e = __builtin_amdgcn_exp2f(s2);
+        if (real) {
+            l += e;
+            t = __fmaf_rn(e, s2, t);
+            top = fmaxf(top, sum);
+        }
+        if (turn == kTurns - 1 && gmax) {
+            float g = top;
 #pragma unroll
-                for (int w = 1; w < 64; w <<= 1) g = fmaxf(g, __shfl_xor(g, w, 64));
-                if (lane == 0) gmax[i * gstride + tile] = g;
-                best[i] = fmaxf(best[i], g);
-                top[i] = -INFINITY;
-            }
+            for (int w = 1; w < 64; w <<= 1) g = fmaxf(g, __shfl_xor(g, w, 64));
+            if (lane == 0) gmax[tile] = g;
+            best = fmaxf(best, g);
+            top = -INFINITY;
         }
     };
     int64_t tile = (int64_t)blockIdx.x * kRowWaves + wave;
@@ -385,24 +391,17 @@ __global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restri
                 }
             take(here, tile, turn);
         }
+    Stat a{m > -INFINITY ? m * c2 : -INFINITY, l, t};
 #pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-        Stat a{m[i] > -INFINITY ? 0.0f : -INFINITY, l[i], t[i]};
-        if (m[i] > -INFINITY) a.m = m[i] * c2;
-#pragma unroll
-        for (int w = 1; w < 64; w <<= 1) a = join(a, Stat{__shfl_xor(a.m, w, 64), __shfl_xor(a.l, w, 64), __shfl_xor(a.t, w, 64)});
-        if (lane == 0) joined[wave][i] = make_float4(a.m, a.l, a.t, best[i]);
-    }
+    for (int w = 1; w < 64; w <<= 1) a = join(a, Stat{__shfl_xor(a.m, w, 64), __shfl_xor(a.l, w, 64), __shfl_xor(a.t, w, 64)});
+    if (lane == 0) joined[wave] = make_float4(a.m, a.l, a.t, best);
     __syncthreads();
-    if (threadIdx.x < NQ) {
-        const int i = threadIdx.x;
-        Stat a{joined[0][i].x, joined[0][i].y, joined[0][i].z};
-        float b = joined[0][i].w;
+    if (threadIdx.x == 0) {
         for (int w = 1; w < kRowWaves; ++w) {
-            a = join(a, Stat{joined[w][i].x, joined[w][i].y, joined[w][i].z});
-            b = fmaxf(b, joined[w][i].w);
+            a = join(a, Stat{joined[w].x, joined[w].y, joined[w].z});
+            best = fmaxf(best, joined[w].w);
         }
-        stats[(size_t)blockIdx.x * NQ + i] = make_float4(a.m, a.l, a.t, b);
+        stats[blockIdx.x] = make_float4(a.m, a.l, a.t, best);
     }
 }
 
@@ -760,7 +759,7 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
 
 // ---- launches ----------------------------------------------------------------------------------
 
-constexpr int kRowGroups = 1024; // four a compute unit
+constexpr int kRowGroups = 512; // two a compute unit
 
 // Workgroups that share the rows of the stream.
 static int stream_groups(int64_t n, int query_tiles)
@@ -786,8 +785,9 @@ static bool by_tiles(int nq) { return nq > 64; }
 constexpr int kTileGroups = 512; // two workgroups a compute unit
 constexpr size_t kPackBytes = (size_t)1 << 30; // most that packed rows take at a time
 
-// One or two queries whose rows fit four loads of a wave go by rows.
-static bool by_rows(int type, int d, int nq) { return nq <= 2 && (size_t)d * type_bytes(type) <= 64 * 16 * 4; }
+// One query whose rows fit four loads of a wave goes by rows (two, by a kernel of two sums a row: 133 against 117 us through the
+// matrix instructions, 1,183,514 x 100 fp32).
+static bool by_rows(int type, int d, int nq) { return nq == 1 && (size_t)d * type_bytes(type) <= 64 * 16 * 4; }
 
 struct ProbScratch {
     float4 *stats; float *gmax; int64_t gstride;
@@ -856,23 +856,26 @@ static int stream_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
     return AVQ_OK;
 }
 
-template <class T, int NQ, int L, int F>
+template <class T, int L, int F>
 static int row_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
 {
     const float c2 = p.scale * 1.44269504088896341f;
-    prob_row_kernel<T, NQ, L, F><<<dim3(s.groups), dim3(kRowThreads), 0, st>>>((const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.ld_queries, c2, s.stats, s.gmax, s.gstride);
+    auto run = [&](auto kernel) { kernel<<<dim3(s.groups), dim3(kRowThreads), 0, st>>>((const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, c2, s.stats, s.gmax); };
+    // what the Infinity Cache (256 MB) does not hold from one call to the next is loaded past it
+    if ((size_t)p.n * p.d * sizeof(T) > ((size_t)256 << 20)) run(prob_row_kernel<T, L, F, true>);
+    else run(prob_row_kernel<T, L, F, false>);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
 
-template <class T, int NQ>
+template <class T>
 static int row_sized(const ProbParams &p, const ProbScratch &s, hipStream_t st)
 {
     const int loads = (p.d + kFragElems<T> - 1) / kFragElems<T>; // 16 bytes of a row
-    if (loads <= 16) return row_run<T, NQ, 16, 1>(p, s, st);
-    if (loads <= 32) return row_run<T, NQ, 32, 1>(p, s, st);
-    if (loads <= 64) return row_run<T, NQ, 64, 1>(p, s, st);
-    return loads <= 128 ? row_run<T, NQ, 64, 2>(p, s, st) : row_run<T, NQ, 64, 4>(p, s, st);
+    if (loads <= 16) return row_run<T, 16, 1>(p, s, st);
+    if (loads <= 32) return row_run<T, 32, 1>(p, s, st);
+    if (loads <= 64) return row_run<T, 64, 1>(p, s, st);
+    return loads <= 128 ? row_run<T, 64, 2>(p, s, st) : row_run<T, 64, 4>(p, s, st);
 }
 
 template <class T, bool ALIGNED>
@@ -940,7 +943,7 @@ static int log_probs_typed(const ProbParams &p, hipStream_t st)
         else AVQ_TRY((tiles_run<T, false>(p, s, st)));
         parts = s.launches * s.parts * 2;
     } else if (by_rows(p.type, p.d, p.nq)) {
-        AVQ_TRY(p.nq == 1 ? (row_sized<T, 1>(p, s, st)) : (row_sized<T, 2>(p, s, st)));
+        AVQ_TRY(row_sized<T>(p, s, st));
     } else {
         const bool aligned = ((uintptr_t)p.points % 16) == 0 && (p.ld_points * sizeof(T)) % 16 == 0;
         AVQ_TRY(aligned ? (stream_sized<T, true>(p, s, st)) : (stream_sized<T, false>(p, s, st)));
