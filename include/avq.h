@@ -464,8 +464,9 @@ int avq_layer_norm_grad(const void *grad, int32_t type, int64_t ld_grad, const v
  * alt_ids_out / alt_logp_out [nq][k] = the k rows of largest s_i and their log p,
  * by (s descending, id ascending), k: 0 .. min(n, AVQ_MAX_SELECT). The s_i themselves
  * are not stored. fp32 matrices are multiplied to fp32's accuracy; rows whose s_i
- * differ by less than its rounding may be ranked either way.
- * scale: finite, not 0. nq: 0 .. 2^19. */
+ * differ by less than its rounding may be ranked either way. log p is formed before
+ * lse is rounded, so that it keeps its relative accuracy where p is nearly 1.
+ * scale: finite, not 0. nq: 0 .. 2^19, nq x m at most 2^28. */
 int64_t avq_log_probs_scratch(int32_t type, int64_t n, int32_t d, int32_t nq, int32_t m, int32_t k);
 int avq_log_probs(const void *points, int32_t type, int64_t n, int32_t d, int64_t ld_points, const void *queries, int32_t nq,
                   int64_t ld_queries, float scale, const int32_t *ids, int32_t m, float *logp_out, float *lse_out,

@@ -48,6 +48,13 @@ template <bool SPLIT> __host__ __device__ inline int steps_of(int64_t d) { retur
 // stores them side by side, at 8 h + 4 b + e. (Its own inverse.)
 __host__ __device__ inline int turned16(int i) { return ((i >> 2) & 1) * 8 + (i >> 3 & 1) * 4 + (i & 3); }
 
+__device__ __forceinline__ void split_f16(float v, uint16_t *hi, uint16_t *lo)
+{
+    const _Float16 h = (_Float16)v;
+    *hi = __builtin_bit_cast(uint16_t, h);
+    *lo = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)h));
+}
+
 __device__ __forceinline__ f32x16 mma32(const Quad &a, const Quad &b, f32x16 c, bf16_t)
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16v8, a), __builtin_bit_cast(bf16v8, b), c, 0, 0, 0);

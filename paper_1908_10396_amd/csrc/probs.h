@@ -23,14 +23,26 @@ __device__ __forceinline__ Stat join(const Stat &a, const Stat &b)
     return Stat{m, a.l * fa + b.l * fb, fa * __fmaf_rn(a.l, da, a.t) + fb * __fmaf_rn(b.l, db, b.t)};
 }
 
-// Dynamic LDS of the kernel that finishes a query: the query in fp32; candidate groups, then the keys of 32 rows for each of the k
+// The pass that forms a query's statistics: one query whose rows fit four loads of a wave goes by rows (two, by a kernel of two sums a
+// row: 133 against 117 us through the matrix instructions, 1,183,514 x 100 fp32); up to 64 queries the rows are streamed once; more go
+// by tiles of a matrix product.
+enum { kByRow = 0, kByStream = 1, kByTiles = 2 };
+inline int prob_path(int size, int d, int nq) { return nq > 64 ? kByTiles : nq == 1 && (size_t)d * size <= 64 * 16 * 4 ? kByRow : kByStream; }
+// Lanes of a row that goes by rows.
+inline int row_lanes(int size, int d)
+{
+    const int loads = (d * size + 15) / 16;
+    return loads <= 16 ? 16 : loads <= 32 ? 32 : 64;
+}
+
+// Dynamic LDS of the kernel that finishes a query: the query; candidate groups, then the keys of 32 rows for each of the k
 // best groups; the rows that may be among the k best; the groups.
 constexpr size_t kFinishLds = kMaxDynLds - 16 * 1024;
 constexpr int kFinishList = 2048; // candidate groups that are kept
 __host__ __device__ constexpr int finish_best(int k) { return k < 192 ? 256 : k + 64; }
 inline size_t finish_lds(int d, int k)
 {
-    return (((size_t)d * 4 + 15) & ~(size_t)15) + (k == 0 ? 0 : (size_t)std::max(32 * k, kFinishList) * 8 + (size_t)finish_best(k) * 8 + (size_t)k * 4);
+    return (size_t)(d + 31) / 32 * 32 * 4 + (k == 0 ? 0 : (size_t)std::max(32 * k, kFinishList) * 8 + (size_t)finish_best(k) * 8 + (size_t)k * 4);
 }
 
 } // namespace avq

@@ -4,6 +4,7 @@
 // and the sums of e^(s - m) and e^(s - m) (s - m) in fp32; the logits are never stored. For the best rows it leaves the
 // largest inner product of every 32 rows; the k groups with the largest of those hold the k best rows, which are scored again.
 #include "mma_tiles.h"
+#include "prob_score.h"
 #include "probs.h"
 #include "row_types.h"
 #include "wg_select.h"
@@ -11,75 +12,6 @@
 #include <type_traits>
 
 namespace avq {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
-// ---- operands: 16 bytes a lane -------------------------------------------------------------
-
-struct alignas(16) Frag { uint32_t w[4]; };
-template <class T> constexpr int kFragElems = 16 / sizeof(T);
-template <class T> constexpr int kStepElems = 4 * kFragElems<T>; // coordinates that a step of 64 lanes covers (16 rows by 4 lanes)
-
-template <class T, bool ALIGNED>
-__device__ __forceinline__ Frag load_whole(const T *__restrict__ p)
-{
-    Frag f;
-    if (ALIGNED) f = *(const Frag *)p;
-    else __builtin_memcpy(&f, p, 16);
-    return f;
-}
-
-// of what is not read again, and had better not displace what the caches hold
-template <class T>
-__device__ __forceinline__ Frag load_once(const T *__restrict__ p)
-{
-    typedef uint32_t on4 __attribute__((ext_vector_type(4), aligned(4)));
-    typedef uint32_t on2 __attribute__((ext_vector_type(4), aligned(2)));
-    return __builtin_bit_cast(Frag, sizeof(T) == 4 ? __builtin_nontemporal_load((const on4 *)p) : __builtin_nontemporal_load((const on2 *)p));
-}
-
-// The coordinates k .. k + kFragElems - 1 of a row of d, zeros past its end. ALIGNED: the row starts on 16 bytes.
-template <class T, bool ALIGNED>
-__device__ __forceinline__ Frag load_frag(const T *__restrict__ row, int k, int d)
-{
-    constexpr int E = kFragElems<T>;
-    Frag f{};
-    if (k + E <= d) {
-        f = load_whole<T, ALIGNED>(row + k);
-    } else {
-        T e[E];
-#pragma unroll
-        for (int j = 0; j < E; ++j) e[j] = k + j < d ? row[k + j] : T{};
-        __builtin_memcpy(&f, e, 16);
-    }
-    return f;
-}
-
-// acc += A B^T over the step's coordinates; both operands: lane l has row l & 15, coordinates kFragElems (l >> 4) onwards.
-// (fp32: which four coordinates share an instruction does not matter as long as both operands agree.)
-__device__ __forceinline__ f32x4 mma16(const Frag &a, const Frag &b, f32x4 acc, float)
-{
-#pragma unroll
-    for (int c = 0; c < 4; ++c) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w[c]), __uint_as_float(b.w[c]), acc, 0, 0, 0);
-    return acc;
-}
-__device__ __forceinline__ f32x4 mma16(const Frag &a, const Frag &b, f32x4 acc, bf16_t)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mma16(const Frag &a, const Frag &b, f32x4 acc, f16_t)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
-}
-
-template <class T> __device__ __forceinline__ Frag negated(Frag f)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f.w[i] ^= sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
-    return f;
-}
 
 // ---- a few queries: the rows streamed once -------------------------------------------------
 
@@ -186,7 +118,7 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prob_stream_kernel(const T 
                     if (h * 16 + kg * 4 + r < valid) top = fmaxf(top, acc[h][i][r]);
             if (top > m[i]) {
                 if (m[i] > -INFINITY) {
-                    const float down = (m[i] - top) * c2, f = __builtin_amdgcn_exp2f(down);
+                    const float down = m[i] * c2 - top * c2, f = __builtin_amdgcn_exp2f(down);
                     t[i] = f * __fmaf_rn(l[i], down, t[i]);
                     l[i] *= f;
                 }
@@ -340,13 +272,13 @@ __global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restri
         const bool real = mine && row < n;
         if (real && sum > m) {
             if (m > -INFINITY) {
-                const float down = (m - sum) * c2, f = __builtin_amdgcn_exp2f(down);
+                const float down = m * c2 - sum * c2, f = __builtin_amdgcn_exp2f(down);
                 t = f * __fmaf_rn(l, down, t);
                 l *= f;
             }
             m = sum;
         }
-        const float s2 = m > -INFINITY ? (sum - m) * c2 : sum, e = __builtin_amdgcn_exp2f(s2);
+        const float s2 = m > -INFINITY ? __fmaf_rn(sum, c2, -(m * c2)) : sum, e = __builtin_amdgcn_exp2f(s2);
         if (real) {
             l += e;
             t = __fmaf_rn(e, s2, t);
@@ -454,7 +386,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
                     const float top = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
                     if (top > m[j]) {
                         if (m[j] > -INFINITY) {
-                            const float down = (m[j] - top) * cq[j], f = __builtin_amdgcn_exp2f(down);
+                            const float down = m[j] * cq[j] - top * cq[j], f = __builtin_amdgcn_exp2f(down);
                             t[j] = f * __fmaf_rn(l[j], down, t[j]);
                             l[j] *= f;
                         }
@@ -506,67 +438,11 @@ __device__ __forceinline__ uint32_t order_of(float v)
 
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
 
-template <int R, int F> struct Shape { static constexpr int rows = R, loads = F; };
-
-// <q, x> of R rows at once by 16 lanes, F loads of 16 bytes a row in flight (fp32, the same order of additions whatever R and F:
-// a lane's coordinates in order, then the lanes); every lane of the group gets them. Loads past a row's last 16 bytes are made at
-// its start and count for nothing: no load waits for a branch.
-template <class T, int R, int F>
-__device__ __forceinline__ void dots16(const float *__restrict__ qf, const T *const (&row)[R], int d, int lane16, float (&s)[R])
-{
-    constexpr int E = kFragElems<T>;
-    const int whole = d / E * E;
-#pragma unroll
-    for (int r = 0; r < R; ++r) s[r] = 0.0f;
-#pragma unroll 1
-    for (int k0 = 0; k0 < whole; k0 += F * 16 * E) {
-        Frag f[R][F];
-#pragma unroll
-        for (int u = 0; u < F; ++u) {
-            const int k = k0 + (u * 16 + lane16) * E;
-#pragma unroll
-            for (int r = 0; r < R; ++r) f[r][u] = load_whole<T, false>(row[r] + (k < whole ? k : 0));
-        }
-#pragma unroll
-        for (int u = 0; u < F; ++u) {
-            const int k = k0 + (u * 16 + lane16) * E;
-            if (k0 + u * 16 * E >= whole) break;
-            float qv[E];
-#pragma unroll
-            for (int j = 0; j < E; ++j) qv[j] = qf[k < whole ? k + j : 0];
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                T e[E];
-                __builtin_memcpy(e, &f[r][u], 16);
-#pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    const float with = __fmaf_rn(qv[j], to_f32(e[j]), s[r]);
-                    s[r] = k < whole ? with : s[r];
-                }
-            }
-        }
-    }
-    if (lane16 < d - whole) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) s[r] = __fmaf_rn(qf[whole + lane16], to_f32(row[r][whole + lane16]), s[r]);
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r) s[r] = group_sum<16>(s[r]);
-}
-
-template <class T> __device__ __forceinline__ float dot16(const float *__restrict__ qf, const T *row, int d, int lane16)
-{
-    const T *const one[1] = {row};
-    float s[1];
-    dots16<T, 1, 8>(qf, one, d, lane16, s);
-    return s[0];
-}
-
 // A workgroup a query: joins the statistics, scores the given rows and the best ones. Latency: the fewest steps that wait for
 // one another. stats.w is the largest product of a part.
-template <class T, int NT>
-__global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, float scale,
-                                                         const float4 *__restrict__ stats, int parts, const int32_t *__restrict__ ids, int given, float *__restrict__ logp_out,
+template <int PATH, class T, int NT>
+__global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, float scale, int row_lanes,
+                                                         const Largest *__restrict__ largest, const float *__restrict__ q_inv, const float4 *__restrict__ stats, int parts, const int32_t *__restrict__ ids, int given, float *__restrict__ logp_out,
                                                          float *__restrict__ lse_out, float *__restrict__ entropy_out, const float *__restrict__ gmax, int64_t gstride, int k,
                                                          int32_t *__restrict__ alt_ids, float *__restrict__ alt_logp)
 {
@@ -575,16 +451,24 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
     __shared__ uint32_t list_count, found_count, bound_shared;
     __shared__ u64 least_best;
     extern __shared__ char lds[];
-    float *qf = (float *)lds;                                        // [d]
-    u64 *keys = (u64 *)(lds + (((size_t)d * 4 + 15) & ~(size_t)15)); // [max(32 k, kFinishList)]: candidate groups, then rows
-    u64 *best = keys + std::max(32 * k, kFinishList);                // [kFinishBest(k)]
+    T *qs = (T *)lds;                                                // the query (4 bytes a coordinate)
+    u64 *keys = (u64 *)(lds + (size_t)((d + 31) / 32 * 32) * 4);     // [max(32 k, kFinishList)]: candidate groups, then rows
+    u64 *best = keys + std::max(32 * k, kFinishList);                // [finish_best(k)]
     uint32_t *groups = (uint32_t *)(best + finish_best(k));          // [k]
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = blockIdx.x;
     uint32_t *tops = (uint32_t *)keys;      // [NT / per] largest product of a class
     const bool by_parts = parts >= 4 * k; // the parts' largest products are classes enough
     uint32_t mine_top = 0;
-    for (int c = tid; c < d; c += NT) qf[c] = to_f32(q[(int64_t)row * ld_q + c]);
+    stage_query(qs, q + (int64_t)row * ld_q, d, scale < 0.0f, NT);
+    // products in units of log 2, as the pass has them
+    float c2 = fabsf(scale) * 1.44269504088896341f;
+    Scoring how{row_lanes, 1.0f, 1.0f};
+    if (PATH == kByTiles && sizeof(T) == 4) {
+        how.x_scale = range_scale(largest->points);
+        how.q_scale = 1.0f / q_inv[row];
+        c2 = c2 * q_inv[row] * (1.0f / how.x_scale);
+    }
     Stat a{-INFINITY, 0.0f, 0.0f};
     for (int p = tid; p < parts; p += NT) {
         const float4 v = stats[(size_t)p * nq + row];
@@ -636,12 +520,15 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
         lse_out[row] = lse;
         if (entropy_out) entropy_out[row] = log_l - ln2 * (a.t / a.l);
     }
-    const int sub = tid >> 4, subs = NT / 16, lane16 = tid & 15;
-    for (int j = sub; j < given; j += subs) {
-        const int32_t id = ids[(int64_t)row * given + j];
-        const bool real = id >= 0 && (int64_t)id < n;
-        const float s = real ? dot16<T>(qf, x + (int64_t)id * ld_x, d, lane16) * scale : 0.0f;
-        if (lane16 == 0) logp_out[(int64_t)row * given + j] = real ? s - lse : -INFINITY;
+    // s - lse from the parts that lse has, before it is rounded
+    auto logp_of = [&](float product) { return __fmaf_rn(__fmaf_rn(product, c2, -a.m), ln2, -log_l); };
+    constexpr int kAhead = sizeof(T) == 4 && NT == 1024 ? 4 : 8; // (what the registers hold)
+    const int at_once = scored_at_once<PATH>(how);
+    for (int j0 = wave * at_once; j0 < given; j0 += NT / 64 * at_once) {
+        const int32_t *mine = ids + (int64_t)row * given + j0;
+        auto real = [&](int i) { return j0 + i < given && mine[i] >= 0 && (int64_t)mine[i] < n; };
+        score_rows<PATH, kAhead>(qs, d, how, [&](int i) { return x + (real(i) ? (int64_t)mine[i] * ld_x : 0); },
+                         [&](int i, float product) { if (j0 + i < given) logp_out[(int64_t)row * given + j0 + i] = real(i) ? logp_of(product) : -INFINITY; });
     }
     if (k == 0) return;
 
@@ -688,29 +575,15 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
         __syncthreads();
     }
     const uint32_t chosen = min(min(list_count, listed), (uint32_t)k), rows = chosen * 32u;
-    auto score = [&](auto shape) {
-        constexpr int R = decltype(shape)::rows, F = decltype(shape)::loads;
-        for (uint32_t i = sub * R; i < rows; i += subs * R) {
-            const T *p[R];
-            int64_t id[R];
-            float s[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                id[r] = (int64_t)groups[i / 32] * 32 + (i & 31) + r; // (R divides 32)
-                p[r] = x + min(id[r], n - 1) * ld_x;
-            }
-            dots16<T, R, F>(qf, p, d, lane16, s);
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (lane16 == r) keys[i + r] = id[r] < n ? ((u64)order_of(s[r] * scale) << 32) | (u64)(0xffffffffu - (uint32_t)id[r]) : 0;
-        }
-    };
-    // short rows several at a time, so that as many loads are in flight
-    constexpr int kPer = 16 * kFragElems<T>;
-    constexpr int kMore = NT == 1024 ? 2 : 1; // (a few queries: few workgroups, each of which has registers for it)
-    if (d <= 2 * kPer) score(Shape<4, 2>{});
-    else if (d <= 4 * kPer) score(Shape<2 * kMore, 4>{});
-    else score(Shape<kMore, 8>{});
+    for (uint32_t i0 = wave * at_once; i0 < rows; i0 += NT / 64 * at_once) {
+        auto id_of = [&](int i) { return (int64_t)groups[(i0 + i) / 32] * 32 + ((i0 + i) & 31); };
+        score_rows<PATH, kAhead>(qs, d, how, [&](int i) { return x + min(i0 + i < rows ? id_of(i) : 0, n - 1) * ld_x; },
+                         [&](int i, float product) {
+                             if (i0 + i >= rows) return;
+                             const int64_t id = id_of(i);
+                             keys[i0 + i] = id < n ? ((u64)order_of(product) << 32) | (u64)(0xffffffffu - (uint32_t)id) : 0;
+                         });
+    }
     __syncthreads();
     // The best row of every chosen group: with k of them, the least of those bounds the k-th best row from below.
     if (chosen == (uint32_t)k) {
@@ -753,7 +626,7 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
         for (uint32_t o = 0; o < found; ++o) rank += best[o] > mine;
         if (rank >= (uint32_t)k) continue;
         alt_ids[(int64_t)row * k + rank] = (int32_t)(0xffffffffu - (uint32_t)mine);
-        alt_logp[(int64_t)row * k + rank] = value_of((uint32_t)(mine >> 32)) - lse;
+        alt_logp[(int64_t)row * k + rank] = logp_of(value_of((uint32_t)(mine >> 32)));
     }
 }
 
@@ -779,15 +652,8 @@ static int stream_tile(int type, int d, int nq)
     return qt;
 }
 
-// From how many queries on the tiles take over: up to 64 the stream reads the rows once.
-static bool by_tiles(int nq) { return nq > 64; }
-
 constexpr int kTileGroups = 512; // two workgroups a compute unit
 constexpr size_t kPackBytes = (size_t)1 << 30; // most that packed rows take at a time
-
-// One query whose rows fit four loads of a wave goes by rows (two, by a kernel of two sums a row: 133 against 117 us through the
-// matrix instructions, 1,183,514 x 100 fp32).
-static bool by_rows(int type, int d, int nq) { return nq == 1 && (size_t)d * type_bytes(type) <= 64 * 16 * 4; }
 
 struct ProbScratch {
     float4 *stats; float *gmax; int64_t gstride;
@@ -807,10 +673,11 @@ static ProbScratch prob_scratch(const ProbParams &p, void *base)
         return q;
     };
     s.gstride = (p.n + kTileM - 1) / kTileM * (kTileM / 32);
-    if (!by_tiles(p.nq)) {
+    const int path = prob_path(type_bytes(p.type), p.d, p.nq);
+    if (path != kByTiles) {
         s.qt = stream_tile(p.type, p.d, p.nq);
         s.query_tiles = (p.nq + 16 * s.qt - 1) / (16 * s.qt);
-        s.groups = by_rows(p.type, p.d, p.nq) ? row_groups(p.n) : stream_groups(p.n, s.query_tiles);
+        s.groups = path == kByRow ? row_groups(p.n) : stream_groups(p.n, s.query_tiles);
         s.stats = (float4 *)take((size_t)s.groups * p.nq * sizeof(float4));
     } else {
         const bool split = p.type == AVQ_F32;
@@ -871,9 +738,9 @@ static int row_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
 template <class T>
 static int row_sized(const ProbParams &p, const ProbScratch &s, hipStream_t st)
 {
-    const int loads = (p.d + kFragElems<T> - 1) / kFragElems<T>; // 16 bytes of a row
-    if (loads <= 16) return row_run<T, 16, 1>(p, s, st);
-    if (loads <= 32) return row_run<T, 32, 1>(p, s, st);
+    const int lanes = row_lanes(sizeof(T), p.d), loads = (p.d + kFragElems<T> - 1) / kFragElems<T>; // of 16 bytes
+    if (lanes == 16) return row_run<T, 16, 1>(p, s, st);
+    if (lanes == 32) return row_run<T, 32, 1>(p, s, st);
     if (loads <= 64) return row_run<T, 64, 1>(p, s, st);
     return loads <= 128 ? row_run<T, 64, 2>(p, s, st) : row_run<T, 64, 4>(p, s, st);
 }
@@ -922,13 +789,14 @@ static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
     return AVQ_OK;
 }
 
-template <class T, int NT>
+template <int PATH, class T, int NT>
 static int finish_run(const ProbParams &p, const ProbScratch &s, int parts, hipStream_t st)
 {
     static LdsLimitOnce once;
-    AVQ_TRY(set_lds_limit((const void *)prob_finish_kernel<T, NT>, kFinishLds, &once));
-    prob_finish_kernel<T, NT><<<dim3(p.nq), dim3(NT), finish_lds(p.d, p.k), st>>>((const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.nq, p.ld_queries, p.scale, s.stats,
-                                                                                parts, p.ids, p.given, p.logp, p.lse, p.entropy, s.gmax, s.gstride, p.k, p.alt_ids, p.alt_logp);
+    AVQ_TRY(set_lds_limit((const void *)prob_finish_kernel<PATH, T, NT>, kFinishLds, &once));
+    prob_finish_kernel<PATH, T, NT><<<dim3(p.nq), dim3(NT), finish_lds(p.d, p.k), st>>>(
+        (const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.nq, p.ld_queries, p.scale, row_lanes(sizeof(T), p.d), s.largest, s.q_inv, s.stats, parts, p.ids, p.given,
+        p.logp, p.lse, p.entropy, s.gmax, s.gstride, p.k, p.alt_ids, p.alt_logp);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
@@ -937,19 +805,21 @@ template <class T>
 static int log_probs_typed(const ProbParams &p, hipStream_t st)
 {
     const ProbScratch s = prob_scratch(p, p.scratch);
-    int parts = s.groups;
-    if (by_tiles(p.nq)) {
+    const int path = prob_path(sizeof(T), p.d, p.nq);
+    if (path == kByTiles) {
         if constexpr (sizeof(T) == 4) AVQ_TRY((tiles_run<f16_t, true>(p, s, st)));
         else AVQ_TRY((tiles_run<T, false>(p, s, st)));
-        parts = s.launches * s.parts * 2;
-    } else if (by_rows(p.type, p.d, p.nq)) {
-        AVQ_TRY(row_sized<T>(p, s, st));
-    } else {
-        const bool aligned = ((uintptr_t)p.points % 16) == 0 && (p.ld_points * sizeof(T)) % 16 == 0;
-        AVQ_TRY(aligned ? (stream_sized<T, true>(p, s, st)) : (stream_sized<T, false>(p, s, st)));
+        // a few queries: as many threads a query as there can be
+        const int parts = s.launches * s.parts * 2;
+        return p.nq <= 256 ? finish_run<kByTiles, T, 1024>(p, s, parts, st) : finish_run<kByTiles, T, 512>(p, s, parts, st);
     }
-    // a few queries: as many threads a query as there can be
-    return p.nq <= 256 ? finish_run<T, 1024>(p, s, parts, st) : finish_run<T, 512>(p, s, parts, st);
+    if (path == kByRow) {
+        AVQ_TRY(row_sized<T>(p, s, st));
+        return finish_run<kByRow, T, 1024>(p, s, s.groups, st);
+    }
+    const bool aligned = ((uintptr_t)p.points % 16) == 0 && (p.ld_points * sizeof(T)) % 16 == 0;
+    AVQ_TRY(aligned ? (stream_sized<T, true>(p, s, st)) : (stream_sized<T, false>(p, s, st)));
+    return finish_run<kByStream, T, 1024>(p, s, s.groups, st);
 }
 
 int launch_log_probs(const ProbParams &p, hipStream_t st)

@@ -8,6 +8,7 @@
 // relative to a bound of its magnitude, so that f16 holds it down to 2^-38 of it; its rounding to 16 bits (bf16: 2^-9) is that of
 // the operands' own type. The entries of the given ids, where p is taken from g, are formed by themselves in fp32 before rounding.
 #include "mma_tiles.h"
+#include "prob_score.h"
 #include "probs.h"
 #include "row_types.h"
 
@@ -138,16 +139,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
         });
 }
 
-// The entries of the given ids among the part's rows, a wave each; the first of a query's equal ids has the sum of their g.
-template <class T>
-__global__ __launch_bounds__(256) void grad_given_kernel(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, int d, float scale,
-                                                         const int32_t *__restrict__ ids, int given, const float *__restrict__ g, const float *__restrict__ lse,
-                                                         const float2 *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, Rows16 G)
+// The entries of the given ids among the part's rows, a wave each; the first of a query's equal ids has the sum of their g. Their
+// logits as the pass formed them that lse is of.
+template <int PATH, class T>
+__global__ __launch_bounds__(64) void grad_given_kernel(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, int d, float scale, int row_lanes,
+                                                        const int32_t *__restrict__ ids, int given, const float *__restrict__ g, const float *__restrict__ lse,
+                                                        const float2 *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, Rows16 G)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (i >= (int64_t)nq * given) return;
-    const int64_t t = i / given, j = i - t * given;
+    extern __shared__ char lds[];
+    const int64_t i = blockIdx.x, t = i / given, j = i - t * given;
     const int64_t id = ids[i];
     if (id < lo || id >= lo + rows) return;
     float sum = 0.0f;
@@ -156,21 +156,29 @@ __global__ __launch_bounds__(256) void grad_given_kernel(const T *__restrict__ x
             if (o < j) return;
             sum += g[t * given + o];
         }
-    const T *xr = x + id * ld_x, *qr = q + t * ld_q;
-    float s = 0.0f;
-    for (int c = lane; c < d; c += 64) s = __fmaf_rn(to_f32(qr[c]), to_f32(xr[c]), s);
-    s = group_sum<64>(s) * scale - lse[t];
-    if (lane != 0) return;
-    const float2 c = coef[t];
-    const float p = __builtin_amdgcn_exp2f(s * 1.44269504088896341f);
-    const float v = sum - (p > 0.0f || p != p ? p * __fmaf_rn(c.y, s, c.x) : 0.0f);
-    uint16_t *to = (uint16_t *)G.p + block16<sizeof(T) == 4>(t) * G.block + (id - lo) * G.row + turned16((int)t & 15);
-    f32x8 one = {};
-    one[0] = v * grad_factor(largest);
-    Quad hi, low{};
-    put16(one, &hi, &low, T{});
-    *to = (uint16_t)hi.w[0];
-    if (sizeof(T) == 4) to[G.block] = (uint16_t)low.w[0];
+    T *qs = (T *)lds;
+    stage_query(qs, q + t * ld_q, d, false, 64);
+    __syncthreads();
+    float c = scale;
+    Scoring how{row_lanes, 1.0f, 1.0f};
+    if (PATH == kByTiles && sizeof(T) == 4) {
+        how.x_scale = range_scale(largest->points);
+        how.q_scale = range_scale(largest->queries);
+        c = c * (1.0f / how.q_scale) * (1.0f / how.x_scale);
+    }
+    score_rows<PATH, 8>(qs, d, how, [&](int) { return x + id * ld_x; }, [&](int slot, float product) {
+        if (slot != 0) return;
+        const float logp = __fmaf_rn(product, c, -lse[t]);
+        const float2 k = coef[t];
+        const float p = __builtin_amdgcn_exp2f(logp * 1.44269504088896341f);
+        f32x8 one = {};
+        one[0] = (sum - (p > 0.0f || p != p ? p * __fmaf_rn(k.y, logp, k.x) : 0.0f)) * grad_factor(largest);
+        Quad hi, low{};
+        put16(one, &hi, &low, T{});
+        uint16_t *to = (uint16_t *)G.p + block16<sizeof(T) == 4>(t) * G.block + (id - lo) * G.row + turned16((int)t & 15);
+        *to = (uint16_t)hi.w[0];
+        if (sizeof(T) == 4) to[G.block] = (uint16_t)low.w[0];
+    });
 }
 
 // fn for every four rows side by side of a lane's accumulators acc[a][j][4 b ..]. One after the other: the compiler would
@@ -394,8 +402,14 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         else grad_tile_kernel<T, H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, s.steps, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, G, s.qw);
         AVQ_HIP(hipGetLastError());
         if (p.given > 0) {
-            grad_given_kernel<T><<<dim3((unsigned)(((int64_t)p.nq * p.given + 3) / 4)), dim3(256), 0, st>>>((const T *)p.points, p.ld_points, q, p.nq, p.ld_queries, p.d, p.scale, p.ids, p.given,
-                                                                                                        p.grad_logp, p.lse, s.coef, s.largest, lo, rows, G);
+            auto run = [&](auto kernel) {
+                kernel<<<dim3((unsigned)((int64_t)p.nq * p.given)), dim3(64), staged_query_bytes(p.d), st>>>((const T *)p.points, p.ld_points, q, p.nq, p.ld_queries, p.d, p.scale, row_lanes(sizeof(T), p.d),
+                                                                                                    p.ids, p.given, p.grad_logp, p.lse, s.coef, s.largest, lo, rows, G);
+            };
+            const int path = prob_path(sizeof(T), p.d, p.nq);
+            if (path == kByTiles) run(grad_given_kernel<kByTiles, T>);
+            else if (path == kByStream) run(grad_given_kernel<kByStream, T>);
+            else run(grad_given_kernel<kByRow, T>);
             AVQ_HIP(hipGetLastError());
         }
         if (p.dpoints) {

@@ -68,6 +68,7 @@ int check_probs(int32_t type, int64_t n, int32_t d, int32_t nq, int32_t given, f
     AVQ_TRY(check_n(n));
     if (nq < 0 || nq > kMaxQueries) { set_error("nq must be 0 .. %d, got %d", kMaxQueries, nq); return AVQ_EINVAL; }
     if (given < 0 || given > kMaxGiven) { set_error("m must be 0 .. %d, got %d", kMaxGiven, given); return AVQ_EINVAL; }
+    if ((int64_t)nq * given > kMaxCount) { set_error("nq x m must be at most 2^28"); return AVQ_EINVAL; }
     if (!std::isfinite(scale) || scale == 0.0f) return refuse("scale must be finite and not 0");
     return AVQ_OK;
 }

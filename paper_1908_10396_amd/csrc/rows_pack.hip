@@ -67,13 +67,6 @@ int launch_largest(const float *x, int64_t rows, int d, int64_t ld, uint32_t *to
     return AVQ_OK;
 }
 
-__device__ __forceinline__ void split_f16(float v, uint16_t *hi, uint16_t *lo)
-{
-    const _Float16 h = (_Float16)v;
-    *hi = __builtin_bit_cast(uint16_t, h);
-    *lo = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)h));
-}
-
 constexpr int kPackRows = 64, kPackColumns = 128;
 
 // 64 rows a workgroup, 128 columns at a time by way of LDS: rows are read along, and half a block of 16 elements is written by each

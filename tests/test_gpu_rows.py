@@ -308,6 +308,29 @@ def test_log_probs_of_rows_of_unequal_size(kind, nq, size):
     _check_probs(avq.log_probs(x, q, k=3, scale=0.5), x, q, 0.5, None, 3)
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [1, 4, 90, 300])
+@pytest.mark.parametrize("n,d", [(4000, 475), (20_001, 100)])
+def test_log_probability_of_a_row_that_has_nearly_all_of_it(kind, nq, n, d):
+    """-log p is the sum of the other rows' e^(s_i - s_t): its relative error is that of the logits' differences, and
+    a few roundings of 1 come on top, not of lse."""
+    g = gen(nq + n)
+    x = normal((n, d), g, TYPES[kind])
+    ids = torch.randint(0, n, (nq,), generator=g, device="cuda", dtype=torch.int32)
+    q = (0.25 * normal((nq, d), g) + 0.9 * x[ids.long()].float()).to(TYPES[kind])
+    scale = 25.0 / d
+    r = avq.log_probs(x, q, ids, 1, scale)
+    s, e = _logits(x, q, scale)
+    away = s - s.gather(1, ids.long()[:, None])
+    away.scatter_(1, ids.long()[:, None], -math.inf)
+    want = -torch.log1p(torch.exp(away).sum(1))
+    assert want.max() < 0 and want.median() > -0.1
+    bound = want.abs() * (4 * e.amax(1) + 64 * U) + 16 * U
+    within(r.logp, want, bound, "logp")
+    assert torch.equal(r.alt_ids[:, 0], ids)
+    within(r.alt_logp[:, 0], want, bound, "alt_logp")
+
+
 # ---- their gradient ------------------------------------------------------------------------------------
 
 def _grad_formula(x, q, scale, ids, lse, entropy, up, up_h, up_l, kind):
