@@ -83,7 +83,6 @@ int launch_embed(const EmbedParams &p, hipStream_t st)
 // so that the sort is stable. All of it is latency: the launches also clear the table's rows, which needs none of it (FillJob).
 constexpr int kSortThreads = 256, kSortEach = 8, kSortTile = kSortThreads * kSortEach, kSortWaves = kSortThreads / 64;
 constexpr int kMaxBins = 2048;
-constexpr int kSortDirect = 4; // up to so many tiles every tile adds up the counts of the tiles itself, beyond a launch does (25 tiles: 40 against 5 us)
 
 __device__ __forceinline__ uint32_t key_of(int32_t id, uint32_t n) { return (uint32_t)id < n ? (uint32_t)id : n; }
 
@@ -97,7 +96,11 @@ template <int W> __device__ __forceinline__ void fill_rows(const FillJob &f, int
     if (f.ld == f.row_bytes) { // dense rows are one long row
         char *from = f.out + f.lo * f.ld;
         const int64_t units = (f.hi - f.lo) * f.row_bytes / W;
-        for (int64_t i = (int64_t)group * blockDim.x + threadIdx.x; i < units; i += step) *(Unit *)(from + i * W) = Unit{};
+        int64_t i = (int64_t)group * blockDim.x + threadIdx.x;
+        for (; i + 3 * step < units; i += 4 * step)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) *(Unit *)(from + (i + u * step) * W) = Unit{};
+        for (; i < units; i += step) *(Unit *)(from + i * W) = Unit{};
     } else {
         for (int64_t r = f.lo + group; r < f.hi; r += groups)
             for (int64_t c = threadIdx.x; c < f.row_bytes / W; c += blockDim.x) *(Unit *)(f.out + r * f.ld + c * W) = Unit{};
@@ -113,6 +116,88 @@ __device__ __forceinline__ void fill_rows(const FillJob &f, int group, int group
 }
 
 __global__ __launch_bounds__(256) void fill_rows_kernel(FillJob fill) { fill_rows(fill, blockIdx.x, gridDim.x); }
+
+// The same for rows that have no ids, where the ids have been sorted: the others are written meanwhile. kFillBytes of rows at a time.
+constexpr int kFillRows = 2048, kFillBytes = 128 << 10;
+
+template <int W> __device__ __forceinline__ void fill_other_rows(const FillJob &f, const uint32_t *__restrict__ keys, uint32_t count, int group, int groups)
+{
+    typedef Pack<uint16_t, W / 2> Unit;
+    __shared__ uint32_t taken[kFillRows / 32], range[2];
+    const uint32_t units = (uint32_t)(f.row_bytes / W), magic = magic_of(units);
+    const int64_t rows = max((int64_t)1, min((int64_t)kFillRows, (int64_t)kFillBytes / f.row_bytes));
+    for (int64_t r0 = f.lo + group * rows; r0 < f.hi; r0 += groups * rows) {
+        const int64_t r1 = min(f.hi, r0 + rows);
+        __syncthreads(); // (what the turn before read has been read)
+        if (threadIdx.x < kFillRows / 32) taken[threadIdx.x] = 0;
+        if (threadIdx.x < 2) {
+            const uint32_t want = (uint32_t)(threadIdx.x == 0 ? r0 : r1); // the first entry of this row or a later one
+            uint32_t lo = 0, hi = count;
+            while (lo < hi) {
+                const uint32_t mid = lo + (hi - lo) / 2;
+                if (keys[mid] < want) lo = mid + 1; else hi = mid;
+            }
+            range[threadIdx.x] = lo;
+        }
+        __syncthreads();
+        for (uint32_t i = range[0] + threadIdx.x; i < range[1]; i += blockDim.x) {
+            const uint32_t r = keys[i] - (uint32_t)r0;
+            if (i == range[0] || keys[i - 1] != keys[i]) atomicOr(&taken[r / 32], 1u << (r % 32)); // (bits: no order matters)
+        }
+        __syncthreads();
+        const uint32_t all = (uint32_t)(r1 - r0) * units; // (at most kFillBytes, or one row: 2^16 units)
+        for (uint32_t i = threadIdx.x; i < all; i += blockDim.x) {
+            const uint32_t r = magic_div(i, magic);
+            if (!(taken[r / 32] >> (r % 32) & 1u)) *(Unit *)(f.out + (r0 + r) * f.ld + (int64_t)(i - r * units) * W) = Unit{};
+        }
+    }
+}
+
+__device__ __forceinline__ void fill_other_rows(const FillJob &f, const uint32_t *keys, uint32_t count, int group, int groups)
+{
+    if (f.width == 16) fill_other_rows<16>(f, keys, count, group, groups);
+    else if (f.width == 8) fill_other_rows<8>(f, keys, count, group, groups);
+    else if (f.width == 4) fill_other_rows<4>(f, keys, count, group, groups);
+    else fill_other_rows<2>(f, keys, count, group, groups);
+}
+
+// Up to kSmallSort entries are sorted by one workgroup: a few by counting, more by exchanges.
+constexpr int kSmallSort = 2048;
+
+__global__ __launch_bounds__(256) void sort_small_kernel(const int32_t *__restrict__ ids, uint32_t count, uint32_t n, uint32_t *__restrict__ keys_out, uint32_t *__restrict__ pos_out,
+                                                         FillJob fill)
+{
+    if (blockIdx.x > 0) { fill_rows(fill, blockIdx.x - 1, gridDim.x - 1); return; }
+    __shared__ u64 e[kSmallSort];
+    uint32_t size = 2;
+    while (size < count) size *= 2;
+    for (uint32_t i = threadIdx.x; i < size; i += 256) e[i] = i < count ? ((u64)key_of(ids[i], n) << 32) | i : ~0ull;
+    __syncthreads();
+    if (count <= 256) {
+        if (threadIdx.x < count) {
+            const u64 mine = e[threadIdx.x];
+            uint32_t rank = 0;
+#pragma unroll 8
+            for (uint32_t o = 0; o < count; ++o) rank += e[o] < mine;
+            keys_out[rank] = (uint32_t)(mine >> 32);
+            pos_out[rank] = (uint32_t)mine;
+        }
+        return;
+    }
+    for (uint32_t k = 2; k <= size; k *= 2)
+        for (uint32_t j = k / 2; j > 0; j /= 2) {
+            for (uint32_t i = threadIdx.x; i < size / 2; i += 256) {
+                const uint32_t lo = 2 * j * (i / j) + i % j, hi = lo + j; // (j a power of two)
+                const u64 a = e[lo], b = e[hi];
+                if ((a > b) == ((lo & k) == 0)) { e[lo] = b; e[hi] = a; }
+            }
+            __syncthreads();
+        }
+    for (uint32_t i = threadIdx.x; i < count; i += 256) {
+        keys_out[i] = (uint32_t)(e[i] >> 32);
+        pos_out[i] = (uint32_t)e[i];
+    }
+}
 
 // hist[tile][digit]
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t *__restrict__ ids, const uint32_t *__restrict__ keys, uint32_t count, uint32_t n,
@@ -135,7 +220,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t 
     for (int b = threadIdx.x; b < bins; b += kSortThreads) hist[(size_t)blockIdx.x * bins + b] = h[b];
 }
 
-// Many tiles: each digit's counts become the counts of the tiles before, and totals[digit] their sum. A thread a digit.
+// Each digit's counts become the counts of the tiles before, and totals[digit] their sum. A thread a digit.
 __global__ __launch_bounds__(64) void sort_sums_kernel(uint32_t *__restrict__ hist, int bins, int tiles, uint32_t *__restrict__ totals)
 {
     const int b = blockIdx.x * 64 + threadIdx.x;
@@ -173,23 +258,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t 
 #pragma unroll
     for (int j = 0; j < kPer; ++j) earlier[j] = all[j] = 0;
     if (b0 < bins) {
-        if (totals) {
 #pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                if (j < per) {
-                    earlier[j] = hist[(size_t)blockIdx.x * bins + b0 + j];
-                    all[j] = totals[b0 + j];
-                }
-        } else {
-            for (int t = 0; t < tiles; ++t)
-#pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    if (j < per) {
-                        const uint32_t c = hist[(size_t)t * bins + b0 + j];
-                        if (t < (int)blockIdx.x) earlier[j] += c;
-                        all[j] += c;
-                    }
-        }
+        for (int j = 0; j < kPer; ++j)
+            if (j < per) {
+                earlier[j] = hist[(size_t)blockIdx.x * bins + b0 + j];
+                all[j] = totals[b0 + j];
+            }
     }
     uint32_t mine = 0;
 #pragma unroll
@@ -274,8 +348,9 @@ __device__ __forceinline__ void write_row(T *__restrict__ row, uint32_t col, con
 template <class T, int V>
 __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ grad, int64_t ld_grad, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos,
                                                        uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out, int64_t ld_out, int accumulate,
-                                                       float *__restrict__ partial)
+                                                       float *__restrict__ partial, int groups, FillJob fill)
 {
+    if ((int)blockIdx.x >= groups) { fill_other_rows(fill, keys, count, blockIdx.x - groups, gridDim.x - groups); return; }
     constexpr int kTeams = 64; // of 4 lanes, at most
     __shared__ uint32_t skeys[kTeams * kRunChunk], spos[kTeams * kRunChunk];
     const uint32_t teams = 256u / (uint32_t)lanes, team = threadIdx.x / (uint32_t)lanes;
@@ -443,7 +518,7 @@ static GradScratch grad_scratch(int64_t n, int d, int64_t count, void *base)
 
 size_t embed_grad_scratch_bytes(int64_t n, int d, int64_t count) { return grad_scratch(n, d, count, nullptr).bytes; }
 
-constexpr int kFillGroups = 1024;
+constexpr int kFillGroups = 2048;
 
 template <class T, int V>
 static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
@@ -458,31 +533,34 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
     const GradScratch s = grad_scratch(p.n, p.d, p.count, p.scratch);
     const uint32_t count = (uint32_t)p.count, n = (uint32_t)p.n;
     const int bins = 1 << s.bits;
-    // a share of the rows to be cleared with each launch of the sort
-    const int launches = 2 * s.passes;
-    const bool filling = !p.accumulate;
+    // The rows to be cleared are shared among the launches: half of them go with the sort's (all of a small one's), half with the sums.
+    const bool filling = !p.accumulate, small = count <= (uint32_t)kSmallSort;
+    const int launches = small ? 1 : 2 * s.passes;
+    const int64_t with_sort = small ? fill.hi : fill.hi / 2;
     int launch = 0;
     auto share = [&]() {
         FillJob f = fill;
-        f.lo = fill.hi * launch / launches;
-        f.hi = fill.hi * (launch + 1) / launches;
+        f.lo = with_sort * launch / launches;
+        f.hi = with_sort * (launch + 1) / launches;
         ++launch;
         return f;
     };
-    const int groups = s.tiles + (filling ? kFillGroups : 0);
     const uint32_t *keys = nullptr, *pos = nullptr;
-    for (int pass = 0; pass < s.passes; ++pass) {
+    if (small) {
+        sort_small_kernel<<<dim3(1 + (filling ? kFillGroups : 0)), dim3(256), 0, st>>>(p.ids, count, n, s.keys[0], s.pos[0], share());
+        AVQ_HIP(hipGetLastError());
+        keys = s.keys[0];
+        pos = s.pos[0];
+    }
+    const int groups = s.tiles + (filling ? kFillGroups : 0);
+    for (int pass = 0; pass < (small ? 0 : s.passes); ++pass) {
         const int32_t *ids = pass == 0 ? p.ids : nullptr;
         const int to = pass & 1;
         sort_count_kernel<<<dim3(groups), dim3(kSortThreads), 0, st>>>(ids, keys, count, n, pass * s.bits, bins, s.hist, s.tiles, share());
         AVQ_HIP(hipGetLastError());
-        const bool direct = s.tiles <= kSortDirect;
-        if (!direct) {
-            sort_sums_kernel<<<dim3((bins + 63) / 64), dim3(64), 0, st>>>(s.hist, bins, s.tiles, s.totals);
-            AVQ_HIP(hipGetLastError());
-        }
-        sort_place_kernel<<<dim3(groups), dim3(kSortThreads), 0, st>>>(ids, keys, pos, count, n, pass * s.bits, s.bits, s.hist, direct ? nullptr : s.totals, s.tiles, s.keys[to],
-                                                                       s.pos[to], share());
+        sort_sums_kernel<<<dim3((bins + 63) / 64), dim3(64), 0, st>>>(s.hist, bins, s.tiles, s.totals);
+        AVQ_HIP(hipGetLastError());
+        sort_place_kernel<<<dim3(groups), dim3(kSortThreads), 0, st>>>(ids, keys, pos, count, n, pass * s.bits, s.bits, s.hist, s.totals, s.tiles, s.keys[to], s.pos[to], share());
         AVQ_HIP(hipGetLastError());
         keys = s.keys[to];
         pos = s.pos[to];
@@ -490,11 +568,16 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
     int lanes = 4;
     while (lanes < 256 && lanes < p.d / V) lanes *= 2;
     const int64_t chunks = (p.count + kRunChunk - 1) / kRunChunk;
-    const dim3 grid((unsigned)((chunks + 256 / lanes - 1) / (256 / lanes)));
-    run_sums_kernel<T, V><<<grid, dim3(256), 0, st>>>((const T *)p.grad, p.ld_grad, keys, pos, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
+    const int sums = (int)((chunks + 256 / lanes - 1) / (256 / lanes));
+    FillJob rest = fill;
+    rest.lo = with_sort;
+    run_sums_kernel<T, V><<<dim3(sums + (filling && !small ? kFillGroups : 0)), dim3(256), 0, st>>>((const T *)p.grad, p.ld_grad, keys, pos, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out,
+                                                                                                  p.accumulate, s.partial, sums, rest);
     AVQ_HIP(hipGetLastError());
-    run_joins_kernel<T, V><<<dim3((unsigned)chunks), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
-    AVQ_HIP(hipGetLastError());
+    if (chunks > 1) {
+        run_joins_kernel<T, V><<<dim3((unsigned)chunks), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
+        AVQ_HIP(hipGetLastError());
+    }
     return AVQ_OK;
 }
 
