@@ -12,30 +12,31 @@ namespace avq {
 
 constexpr int kLookThreads = 256, kLookEach = 4;
 
-template <class T, int V>
-__global__ __launch_bounds__(kLookThreads) void embed_kernel(const T *__restrict__ table, int64_t n, int64_t ld_table, const int32_t *__restrict__ ids,
-                                                             int64_t count, int per_row, uint32_t magic, float scale, T *__restrict__ out, int64_t ld_out)
+template <class T, bool RAGGED>
+__global__ __launch_bounds__(kLookThreads) void embed_kernel(const T *__restrict__ table, int64_t n, int d, int64_t ld_table, const int32_t *__restrict__ ids, int64_t count,
+                                                             int per_row, uint32_t magic, float scale, T *__restrict__ out, int64_t ld_out)
 {
-    // the rows' vectors as one long list: a workgroup takes 1,024 of them, four loads a thread in flight
+    // the rows' units as one long list: a workgroup takes 1,024 of them, four loads a thread in flight (padding's from row 0)
+    constexpr int V = kUnit<T>;
     const int64_t first = (int64_t)blockIdx.x * (kLookThreads * kLookEach);
     const int64_t row0 = first / per_row;
     const uint32_t rem0 = (uint32_t)(first - row0 * per_row);
-    Pack<T, V> v[kLookEach];
+    Unit<T> v[kLookEach];
     int64_t row[kLookEach];
-    uint32_t col[kLookEach];
+    int col[kLookEach];
     int32_t id[kLookEach];
 #pragma unroll
     for (int u = 0; u < kLookEach; ++u) {
         const uint32_t at = rem0 + (uint32_t)(u * kLookThreads) + threadIdx.x;
         const uint32_t r = magic_div(at, magic);
         row[u] = row0 + r;
-        col[u] = at - r * (uint32_t)per_row;
+        col[u] = (int)(at - r * (uint32_t)per_row) * V;
         id[u] = row[u] < count ? ids[row[u]] : -1;
     }
 #pragma unroll
     for (int u = 0; u < kLookEach; ++u) {
-        v[u] = Pack<T, V>{};
-        if (id[u] >= 0 && (int64_t)id[u] < n) v[u] = *(const Pack<T, V> *)(table + (int64_t)id[u] * ld_table + (int64_t)col[u] * V);
+        const bool real = id[u] >= 0 && (int64_t)id[u] < n;
+        v[u] = load_unit<T, RAGGED>(table + (real ? (int64_t)id[u] * ld_table : 0), col[u], d);
     }
 #pragma unroll
     for (int u = 0; u < kLookEach; ++u) {
@@ -43,19 +44,19 @@ __global__ __launch_bounds__(kLookThreads) void embed_kernel(const T *__restrict
         if (scale != 1.0f) {
 #pragma unroll
             for (int e = 0; e < V; ++e) v[u].e[e] = from_f32<T>(to_f32(v[u].e[e]) * scale);
-            if (!(id[u] >= 0 && (int64_t)id[u] < n)) v[u] = Pack<T, V>{}; // (zeros, whatever the scale)
         }
-        *(Pack<T, V> *)(out + row[u] * ld_out + (int64_t)col[u] * V) = v[u];
+        if (!(id[u] >= 0 && (int64_t)id[u] < n)) v[u] = Unit<T>{}; // (zeros, whatever row 0 holds)
+        store_unit<T, RAGGED>(out + row[u] * ld_out, col[u], d, v[u]);
     }
 }
 
-template <class T, int V>
+template <class T, bool RAGGED>
 static int embed_run(const EmbedParams &p, hipStream_t st)
 {
-    const int per_row = p.d / V;
+    const int per_row = units_of<T>(p.d);
     const int64_t groups = (p.count * per_row + kLookThreads * kLookEach - 1) / (kLookThreads * kLookEach);
-    embed_kernel<T, V><<<dim3((unsigned)groups), dim3(kLookThreads), 0, st>>>((const T *)p.table, p.n, p.ld_table, p.ids, p.count, per_row, magic_of(per_row),
-                                                                             p.scale, (T *)p.out, p.ld_out);
+    embed_kernel<T, RAGGED><<<dim3((unsigned)groups), dim3(kLookThreads), 0, st>>>((const T *)p.table, p.n, p.d, p.ld_table, p.ids, p.count, per_row, magic_of(per_row), p.scale,
+                                                                                  (T *)p.out, p.ld_out);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
@@ -63,10 +64,8 @@ static int embed_run(const EmbedParams &p, hipStream_t st)
 template <class T>
 static int embed_typed(const EmbedParams &p, hipStream_t st)
 {
-    const int w = std::min(row_width(p.table, p.ld_table, p.d, sizeof(T)), row_width(p.out, p.ld_out, p.d, sizeof(T)));
-    if (w == 16) return embed_run<T, 16 / sizeof(T)>(p, st);
-    if (w == 8) return embed_run<T, 8 / sizeof(T)>(p, st);
-    return embed_run<T, 1>(p, st);
+    const bool whole = whole_units(p.table, p.ld_table, p.d, sizeof(T)) && whole_units(p.out, p.ld_out, p.d, sizeof(T));
+    return whole ? embed_run<T, false>(p, st) : embed_run<T, true>(p, st);
 }
 
 int launch_embed(const EmbedParams &p, hipStream_t st)
@@ -86,33 +85,34 @@ constexpr int kMaxBins = 2048;
 
 __device__ __forceinline__ uint32_t key_of(int32_t id, uint32_t n) { return (uint32_t)id < n ? (uint32_t)id : n; }
 
-// Rows [lo, hi) of the table to be cleared by the workgroups of a launch beyond its own ones; 16, 8, 4 or 2 bytes at a time.
-struct FillJob { char *out; int64_t lo, hi, ld, row_bytes; int32_t width; };
+// Rows [lo, hi) of the table to be cleared by the workgroups of a launch beyond its own ones (ld, row_bytes: in bytes).
+struct FillJob { char *out; int64_t lo, hi, ld, row_bytes; };
 
-template <int W> __device__ __forceinline__ void fill_rows(const FillJob &f, int group, int groups)
+// bytes [from, to) of an address, multiples of two bytes, by the threads t of n
+__device__ __forceinline__ void clear_bytes(char *from, char *to, int64_t t, int64_t n)
 {
-    typedef Pack<uint16_t, W / 2> Unit;
-    const int64_t step = (int64_t)groups * blockDim.x;
-    if (f.ld == f.row_bytes) { // dense rows are one long row
-        char *from = f.out + f.lo * f.ld;
-        const int64_t units = (f.hi - f.lo) * f.row_bytes / W;
-        int64_t i = (int64_t)group * blockDim.x + threadIdx.x;
-        for (; i + 3 * step < units; i += 4 * step)
+    char *head = min(to, (char *)(((uintptr_t)from + 15) & ~(uintptr_t)15)), *tail = max(head, (char *)((uintptr_t)to & ~(uintptr_t)15));
+    typedef Pack<uint32_t, 4> Word;
+    const int64_t words = (tail - head) / 16;
+    int64_t i = t;
+    for (; i + 3 * n < words; i += 4 * n)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) *(Unit *)(from + (i + u * step) * W) = Unit{};
-        for (; i < units; i += step) *(Unit *)(from + i * W) = Unit{};
-    } else {
-        for (int64_t r = f.lo + group; r < f.hi; r += groups)
-            for (int64_t c = threadIdx.x; c < f.row_bytes / W; c += blockDim.x) *(Unit *)(f.out + r * f.ld + c * W) = Unit{};
-    }
+        for (int u = 0; u < 4; ++u) *(Word *)(head + (i + u * n) * 16) = Word{};
+    for (; i < words; i += n) *(Word *)(head + i * 16) = Word{};
+    if (t < 8 && from + 2 * t < head) *(uint16_t *)(from + 2 * t) = 0;
+    if (t < 8 && tail + 2 * t < to) *(uint16_t *)(tail + 2 * t) = 0;
 }
 
 __device__ __forceinline__ void fill_rows(const FillJob &f, int group, int groups)
 {
-    if (f.width == 16) fill_rows<16>(f, group, groups);
-    else if (f.width == 8) fill_rows<8>(f, group, groups);
-    else if (f.width == 4) fill_rows<4>(f, group, groups);
-    else fill_rows<2>(f, group, groups);
+    if (f.ld == f.row_bytes) { // dense rows are one long row
+        clear_bytes(f.out + f.lo * f.ld, f.out + f.hi * f.ld, (int64_t)group * blockDim.x + threadIdx.x, (int64_t)groups * blockDim.x);
+    } else {
+        // a wave a row
+        const int waves = blockDim.x / 64;
+        for (int64_t r = f.lo + (int64_t)group * waves + threadIdx.x / 64; r < f.hi; r += (int64_t)groups * waves)
+            clear_bytes(f.out + r * f.ld, f.out + r * f.ld + f.row_bytes, threadIdx.x & 63, 64);
+    }
 }
 
 __global__ __launch_bounds__(256) void fill_rows_kernel(FillJob fill) { fill_rows(fill, blockIdx.x, gridDim.x); }
@@ -120,12 +120,11 @@ __global__ __launch_bounds__(256) void fill_rows_kernel(FillJob fill) { fill_row
 // The same for rows that have no ids, where the ids have been sorted: the others are written meanwhile. kFillBytes of rows at a time.
 constexpr int kFillRows = 2048, kFillBytes = 128 << 10;
 
-template <int W> __device__ __forceinline__ void fill_other_rows(const FillJob &f, const uint32_t *__restrict__ keys, uint32_t count, int group, int groups)
+__device__ __forceinline__ void fill_other_rows(const FillJob &f, const uint32_t *__restrict__ keys, uint32_t count, int group, int groups)
 {
-    typedef Pack<uint16_t, W / 2> Unit;
     __shared__ uint32_t taken[kFillRows / 32], range[2];
-    const uint32_t units = (uint32_t)(f.row_bytes / W), magic = magic_of(units);
     const int64_t rows = max((int64_t)1, min((int64_t)kFillRows, (int64_t)kFillBytes / f.row_bytes));
+    const uint32_t units = (uint32_t)((f.row_bytes + 15) / 16), magic = magic_of(units);
     for (int64_t r0 = f.lo + group * rows; r0 < f.hi; r0 += groups * rows) {
         const int64_t r1 = min(f.hi, r0 + rows);
         __syncthreads(); // (what the turn before read has been read)
@@ -140,25 +139,28 @@ template <int W> __device__ __forceinline__ void fill_other_rows(const FillJob &
             range[threadIdx.x] = lo;
         }
         __syncthreads();
-        for (uint32_t i = range[0] + threadIdx.x; i < range[1]; i += blockDim.x) {
+        const uint32_t k0 = range[0], k1 = range[1];
+        if (k0 == k1 && f.ld == f.row_bytes) {
+            clear_bytes(f.out + r0 * f.ld, f.out + r1 * f.ld, threadIdx.x, blockDim.x);
+            continue;
+        }
+        for (uint32_t i = k0 + threadIdx.x; i < k1; i += blockDim.x) {
             const uint32_t r = keys[i] - (uint32_t)r0;
-            if (i == range[0] || keys[i - 1] != keys[i]) atomicOr(&taken[r / 32], 1u << (r % 32)); // (bits: no order matters)
+            if (i == k0 || keys[i - 1] != keys[i]) atomicOr(&taken[r / 32], 1u << (r % 32)); // (bits: no order matters)
         }
         __syncthreads();
-        const uint32_t all = (uint32_t)(r1 - r0) * units; // (at most kFillBytes, or one row: 2^16 units)
+        const uint32_t all = (uint32_t)(r1 - r0) * units; // (kFillBytes, or one row: at most 2^16 pieces of 16 bytes)
         for (uint32_t i = threadIdx.x; i < all; i += blockDim.x) {
             const uint32_t r = magic_div(i, magic);
-            if (!(taken[r / 32] >> (r % 32) & 1u)) *(Unit *)(f.out + (r0 + r) * f.ld + (int64_t)(i - r * units) * W) = Unit{};
+            if (taken[r / 32] >> (r % 32) & 1u) continue;
+            const int64_t c = (int64_t)(i - r * units) * 16;
+            char *to = f.out + (r0 + r) * f.ld + c;
+            const Pack<uint32_t, 4> zero{};
+            if (c + 16 <= f.row_bytes) __builtin_memcpy(to, &zero, 16);
+            else
+                for (int64_t b = 0; c + b < f.row_bytes; b += 2) *(uint16_t *)(to + b) = 0;
         }
     }
-}
-
-__device__ __forceinline__ void fill_other_rows(const FillJob &f, const uint32_t *keys, uint32_t count, int group, int groups)
-{
-    if (f.width == 16) fill_other_rows<16>(f, keys, count, group, groups);
-    else if (f.width == 8) fill_other_rows<8>(f, keys, count, group, groups);
-    else if (f.width == 4) fill_other_rows<4>(f, keys, count, group, groups);
-    else fill_other_rows<2>(f, keys, count, group, groups);
 }
 
 // Up to kSmallSort entries are sorted by one workgroup: a few by counting, more by exchanges.
@@ -332,26 +334,28 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t 
 
 constexpr int kRunChunk = 32; // sorted entries that one group of lanes sums
 
-template <class T, int V>
-__device__ __forceinline__ void write_row(T *__restrict__ row, uint32_t col, const float *acc, float scale, bool accumulate)
+// a row's unit: acc scale, or that added to what is there
+template <class T, bool RAGGED>
+__device__ __forceinline__ void write_row(T *__restrict__ row, int k, int d, const float *acc, float scale, bool accumulate)
 {
-    Pack<T, V> o;
-    if (accumulate) o = *(const Pack<T, V> *)(row + (size_t)col * V);
+    constexpr int V = kUnit<T>;
+    Unit<T> o;
+    if (accumulate) o = load_unit<T, RAGGED>(row, k, d);
 #pragma unroll
     for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(accumulate ? to_f32(o.e[e]) + acc[e] * scale : acc[e] * scale);
-    *(Pack<T, V> *)(row + (size_t)col * V) = o;
+    store_unit<T, RAGGED>(row, k, d, o);
 }
 
 // Each team of `lanes` threads takes a chunk of kRunChunk sorted entries. A run that lies within the chunk goes to its
 // row; what belongs to a run that crosses the chunk's start or end goes to partial[chunk][0] or [1] (a run through the
 // whole chunk: [0]). The rows of eight entries are asked for while the eight before are added up.
-template <class T, int V>
+template <class T, bool RAGGED>
 __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ grad, int64_t ld_grad, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos,
                                                        uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out, int64_t ld_out, int accumulate,
                                                        float *__restrict__ partial, int groups, FillJob fill)
 {
     if ((int)blockIdx.x >= groups) { fill_other_rows(fill, keys, count, blockIdx.x - groups, gridDim.x - groups); return; }
-    constexpr int kTeams = 64; // of 4 lanes, at most
+    constexpr int kTeams = 64, V = kUnit<T>; // teams of 4 lanes, at most
     __shared__ uint32_t skeys[kTeams * kRunChunk], spos[kTeams * kRunChunk];
     const uint32_t teams = 256u / (uint32_t)lanes, team = threadIdx.x / (uint32_t)lanes;
     const uint32_t all_begin = blockIdx.x * teams * (uint32_t)kRunChunk;
@@ -365,7 +369,7 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
     if (begin >= count) return;
     const uint32_t *ks = skeys + team * kRunChunk, *ps = spos + team * kRunChunk;
     const uint32_t end = min(count, begin + (uint32_t)kRunChunk);
-    const uint32_t per_row = (uint32_t)d / V;
+    const uint32_t per_row = (uint32_t)units_of<T>(d), dp = per_row * V; // (parts are padded)
     const uint32_t before = begin > 0 ? keys[begin - 1] : 0xffffffffu; // (no key is that)
     const uint32_t after = end < count ? keys[end] : 0xffffffffu;
     for (uint32_t col = threadIdx.x % (uint32_t)lanes; col < per_row; col += (uint32_t)lanes) {
@@ -375,17 +379,17 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
         uint32_t key = ks[0];
         bool from_start = true;
         constexpr int kAhead = 8;
-        struct Rows { Pack<T, V> v[kAhead]; };
-        const T *from = grad + (int64_t)col * V;
+        struct Rows { Unit<T> v[kAhead]; };
+        const int k0 = (int)col * V;
         auto ask = [&](Rows &r, int i0) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) r.v[u] = *(const Pack<T, V> *)(from + (int64_t)ps[i0 + u] * ld_grad);
+            for (int u = 0; u < kAhead; ++u) r.v[u] = load_unit<T, RAGGED>(grad + (int64_t)ps[i0 + u] * ld_grad, k0, d);
         };
         auto partial_row = [&](int slot) __attribute__((always_inline)) {
             Pack<float, V> o;
 #pragma unroll
             for (int e = 0; e < V; ++e) o.e[e] = acc[e];
-            float *to = partial + ((size_t)chunk * 2 + slot) * d + (size_t)col * V;
+            float *to = partial + ((size_t)chunk * 2 + slot) * dp + k0;
             __builtin_memcpy(to, &o, sizeof(o));
         };
         auto add = [&](const Rows &r, int i0) __attribute__((always_inline)) {
@@ -395,7 +399,7 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
                 if (next != key) {
                     if (key < n) {
                         if (from_start && key == before) partial_row(0);
-                        else write_row<T, V>(out + (int64_t)key * ld_out, col, acc, scale, accumulate != 0);
+                        else write_row<T, RAGGED>(out + (int64_t)key * ld_out, (int)col * V, d, acc, scale, accumulate != 0);
                     }
                     from_start = false;
                     key = next;
@@ -419,7 +423,7 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
         if (key >= n) continue; // (the last chunk's entries past the end have the key n)
         const bool open_start = from_start && key == before;
         if (open_start || key == after) partial_row(open_start ? 0 : 1);
-        else write_row<T, V>(out + (int64_t)key * ld_out, col, acc, scale, accumulate != 0);
+        else write_row<T, RAGGED>(out + (int64_t)key * ld_out, (int)col * V, d, acc, scale, accumulate != 0);
     }
 }
 
@@ -427,12 +431,13 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
 // of the chunks each, in order, and then the shares in order.
 constexpr int kJoinThreads = 512;
 
-template <class T, int V>
+template <class T, bool RAGGED>
 __global__ __launch_bounds__(kJoinThreads) void run_joins_kernel(const uint32_t *__restrict__ keys, uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out,
                                                                  int64_t ld_out, int accumulate, const float *__restrict__ partial)
 {
+    constexpr int V = kUnit<T>;
     __shared__ float shares[kJoinThreads * V];
-    const uint32_t chunks = (count + kRunChunk - 1) / kRunChunk, per_row = (uint32_t)d / V;
+    const uint32_t chunks = (count + kRunChunk - 1) / kRunChunk, per_row = (uint32_t)units_of<T>(d), dp = per_row * V;
     const uint32_t teams = kJoinThreads / (uint32_t)lanes, team = threadIdx.x / (uint32_t)lanes, lane = threadIdx.x % (uint32_t)lanes;
     const uint32_t chunk = blockIdx.x;
     const uint32_t begin = chunk * (uint32_t)kRunChunk, end = begin + (uint32_t)kRunChunk;
@@ -458,12 +463,12 @@ __global__ __launch_bounds__(kJoinThreads) void run_joins_kernel(const uint32_t 
         if (team < used && col < per_row) {
             float acc[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) acc[e] = team == 0 ? partial[((size_t)chunk * 2 + 1) * d + (size_t)col * V + e] : 0.0f;
+            for (int e = 0; e < V; ++e) acc[e] = team == 0 ? partial[((size_t)chunk * 2 + 1) * dp + (size_t)col * V + e] : 0.0f;
             const uint32_t from = chunk + 1 + more * team / used, to = chunk + 1 + more * (team + 1) / used;
 #pragma unroll 16
             for (uint32_t c = from; c < to; ++c) {
                 Pack<float, V> v;
-                __builtin_memcpy(&v, partial + (size_t)c * 2 * d + (size_t)col * V, sizeof(v));
+                __builtin_memcpy(&v, partial + (size_t)c * 2 * dp + (size_t)col * V, sizeof(v));
 #pragma unroll
                 for (int e = 0; e < V; ++e) acc[e] += v.e[e];
             }
@@ -478,7 +483,7 @@ __global__ __launch_bounds__(kJoinThreads) void run_joins_kernel(const uint32_t 
             for (uint32_t t = 0; t < used; ++t)
 #pragma unroll
                 for (int e = 0; e < V; ++e) acc[e] += shares[(t * (uint32_t)lanes + lane) * V + e];
-            write_row<T, V>(out + (int64_t)key * ld_out, col, acc, scale, accumulate != 0);
+            write_row<T, RAGGED>(out + (int64_t)key * ld_out, (int)col * V, d, acc, scale, accumulate != 0);
         }
         __syncthreads();
     }
@@ -511,7 +516,7 @@ static GradScratch grad_scratch(int64_t n, int d, int64_t count, void *base)
     }
     s.hist = (uint32_t *)take(((size_t)4 << s.bits) * s.tiles);
     s.totals = (uint32_t *)take((size_t)4 << s.bits);
-    s.partial = (float *)take((size_t)((count + kRunChunk - 1) / kRunChunk) * 2 * d * sizeof(float));
+    s.partial = (float *)take((size_t)((count + kRunChunk - 1) / kRunChunk) * 2 * ((d + 7) / 8 * 8) * sizeof(float));
     s.bytes = at;
     return s;
 }
@@ -520,10 +525,10 @@ size_t embed_grad_scratch_bytes(int64_t n, int d, int64_t count) { return grad_s
 
 constexpr int kFillGroups = 2048;
 
-template <class T, int V>
+template <class T, bool RAGGED>
 static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
 {
-    FillJob fill{(char *)p.out, 0, p.accumulate ? 0 : p.n, p.ld_out * (int64_t)sizeof(T), p.d * (int64_t)sizeof(T), V * (int)sizeof(T)};
+    FillJob fill{(char *)p.out, 0, p.accumulate ? 0 : p.n, p.ld_out * (int64_t)sizeof(T), p.d * (int64_t)sizeof(T)};
     if (p.count == 0) {
         if (p.accumulate) return AVQ_OK;
         fill_rows_kernel<<<dim3(kFillGroups), dim3(256), 0, st>>>(fill);
@@ -566,16 +571,16 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
         pos = s.pos[to];
     }
     int lanes = 4;
-    while (lanes < 256 && lanes < p.d / V) lanes *= 2;
+    while (lanes < 256 && lanes < units_of<T>(p.d)) lanes *= 2;
     const int64_t chunks = (p.count + kRunChunk - 1) / kRunChunk;
     const int sums = (int)((chunks + 256 / lanes - 1) / (256 / lanes));
     FillJob rest = fill;
     rest.lo = with_sort;
-    run_sums_kernel<T, V><<<dim3(sums + (filling && !small ? kFillGroups : 0)), dim3(256), 0, st>>>((const T *)p.grad, p.ld_grad, keys, pos, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out,
+    run_sums_kernel<T, RAGGED><<<dim3(sums + (filling && !small ? kFillGroups : 0)), dim3(256), 0, st>>>((const T *)p.grad, p.ld_grad, keys, pos, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out,
                                                                                                   p.accumulate, s.partial, sums, rest);
     AVQ_HIP(hipGetLastError());
     if (chunks > 1) {
-        run_joins_kernel<T, V><<<dim3((unsigned)chunks), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
+        run_joins_kernel<T, RAGGED><<<dim3((unsigned)chunks), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
         AVQ_HIP(hipGetLastError());
     }
     return AVQ_OK;
@@ -584,11 +589,8 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
 template <class T>
 static int embed_grad_typed(const EmbedGradParams &p, hipStream_t st)
 {
-    int w = row_width(p.out, p.ld_out, p.d, sizeof(T));
-    if (p.count > 0) w = std::min(w, row_width(p.grad, p.ld_grad, p.d, sizeof(T)));
-    if (w == 16) return embed_grad_run<T, 16 / sizeof(T)>(p, st);
-    if (w == 8) return embed_grad_run<T, 8 / sizeof(T)>(p, st);
-    return embed_grad_run<T, 1>(p, st);
+    const bool whole = whole_units(p.out, p.ld_out, p.d, sizeof(T)) && (p.count == 0 || whole_units(p.grad, p.ld_grad, p.d, sizeof(T)));
+    return whole ? embed_grad_run<T, false>(p, st) : embed_grad_run<T, true>(p, st);
 }
 
 int launch_embed_grad(const EmbedGradParams &p, hipStream_t st)

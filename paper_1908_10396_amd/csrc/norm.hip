@@ -19,23 +19,23 @@ template <int L> __device__ __forceinline__ float row_sum(float v, float *red)
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-template <class T, int V, int L, int NV>
+template <class T, bool RAGGED, int L, int NV>
 __global__ __launch_bounds__(kNormThreads) void norm_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld_x, const T *__restrict__ weight, const T *__restrict__ bias,
                                                             float eps, T *__restrict__ y, int64_t ld_y, float *__restrict__ mean_out, float *__restrict__ rstd_out)
 {
     __shared__ float red[4];
-    constexpr int kRows = kNormThreads / L; // rows a workgroup has at a time
-    const int per_row = d / V, lane = threadIdx.x % L;
+    constexpr int V = kUnit<T>, kRows = kNormThreads / L; // rows a workgroup has at a time
+    const int per_row = units_of<T>(d), lane = threadIdx.x % L;
     const float inv_d = 1.0f / (float)d;
     for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / L; row - threadIdx.x / L < rows; row += (int64_t)gridDim.x * kRows) {
         const bool real = row < rows;
-        Pack<T, V> v[NV];
+        Unit<T> v[NV];
         float s = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            v[j] = Pack<T, V>{};
+            v[j] = Unit<T>{};
             const int col = lane + j * L;
-            if (real && col < per_row) v[j] = *(const Pack<T, V> *)(x + row * ld_x + (int64_t)col * V);
+            if (real && col < per_row) v[j] = load_unit<T, RAGGED>(x + row * ld_x, col * V, d);
 #pragma unroll
             for (int e = 0; e < V; ++e) s += to_f32(v[j].e[e]);
         }
@@ -43,7 +43,11 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(const T *__restrict_
         float q = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            if (lane + j * L < per_row) {
+            const int k = (lane + j * L) * V;
+            if (RAGGED) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) { const float off = k + e < d ? to_f32(v[j].e[e]) - mean : 0.0f; q = __fmaf_rn(off, off, q); }
+            } else if (k < d) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) { const float off = to_f32(v[j].e[e]) - mean; q = __fmaf_rn(off, off, q); }
             }
@@ -54,9 +58,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(const T *__restrict_
         for (int j = 0; j < NV; ++j) {
             const int col = lane + j * L;
             if (col >= per_row) continue;
-            Pack<T, V> w, b, o;
-            if (weight) w = *(const Pack<T, V> *)(weight + col * V);
-            if (bias) b = *(const Pack<T, V> *)(bias + col * V);
+            Unit<T> w, b, o;
+            if (weight) w = load_unit<T, RAGGED>(weight, col * V, d);
+            if (bias) b = load_unit<T, RAGGED>(bias, col * V, d);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 float r = (to_f32(v[j].e[e]) - mean) * rstd;
@@ -64,7 +68,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(const T *__restrict_
                 if (bias) r = r + to_f32(b.e[e]);
                 o.e[e] = from_f32<T>(r);
             }
-            *(Pack<T, V> *)(y + row * ld_y + (int64_t)col * V) = o;
+            store_unit<T, RAGGED>(y + row * ld_y, col * V, d, o);
         }
         if (lane == 0) {
             if (mean_out) mean_out[row] = mean;
@@ -74,15 +78,15 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(const T *__restrict_
 }
 
 // dx, and the workgroup's sums of dy xh and dy in part[workgroup][2][d].
-template <class T, int V, int L, int NV>
+template <class T, bool RAGGED, int L, int NV>
 __global__ __launch_bounds__(kNormThreads) void norm_grad_kernel(const T *__restrict__ dy, int64_t ld_dy, const T *__restrict__ x, int64_t ld_x, int64_t rows, int d,
                                                                  const float *__restrict__ mean_in, const float *__restrict__ rstd_in, const T *__restrict__ weight,
                                                                  T *__restrict__ dx, int64_t ld_dx, float *__restrict__ part)
 {
     __shared__ float red[4];
     extern __shared__ float sums[]; // [2][d], of the groups of lanes that were added so far
-    constexpr int kRows = kNormThreads / L;
-    const int per_row = d / V, lane = threadIdx.x % L, group = threadIdx.x / L;
+    constexpr int V = kUnit<T>, kRows = kNormThreads / L;
+    const int per_row = units_of<T>(d), lane = threadIdx.x % L, group = threadIdx.x / L;
     const float inv_d = 1.0f / (float)d;
     float dw[NV][V], db[NV][V], w[NV][V];
 #pragma unroll
@@ -91,21 +95,21 @@ __global__ __launch_bounds__(kNormThreads) void norm_grad_kernel(const T *__rest
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             dw[j][e] = db[j][e] = 0.0f;
-            w[j][e] = weight && col < per_row ? to_f32(weight[col * V + e]) : 1.0f;
+            w[j][e] = weight && col * V + e < d ? to_f32(weight[col * V + e]) : 1.0f;
         }
     }
     for (int64_t row = (int64_t)blockIdx.x * kRows + group; row - group < rows; row += (int64_t)gridDim.x * kRows) {
         const bool real = row < rows;
-        Pack<T, V> vx[NV], vg[NV];
+        Unit<T> vx[NV], vg[NV];
         const float mean = real ? mean_in[row] : 0.0f, rstd = real ? rstd_in[row] : 0.0f;
         float sg = 0.0f, sgx = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            vx[j] = vg[j] = Pack<T, V>{};
+            vx[j] = vg[j] = Unit<T>{};
             const int col = lane + j * L;
             if (real && col < per_row) {
-                vx[j] = *(const Pack<T, V> *)(x + row * ld_x + (int64_t)col * V);
-                vg[j] = *(const Pack<T, V> *)(dy + row * ld_dy + (int64_t)col * V);
+                vx[j] = load_unit<T, RAGGED>(x + row * ld_x, col * V, d);
+                vg[j] = load_unit<T, RAGGED>(dy + row * ld_dy, col * V, d);
             }
         }
 #pragma unroll
@@ -126,13 +130,13 @@ __global__ __launch_bounds__(kNormThreads) void norm_grad_kernel(const T *__rest
         for (int j = 0; j < NV; ++j) {
             const int col = lane + j * L;
             if (col >= per_row) continue;
-            Pack<T, V> o;
+            Unit<T> o;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float xh = (to_f32(vx[j].e[e]) - mean) * rstd, g = to_f32(vg[j].e[e]) * w[j][e];
                 o.e[e] = from_f32<T>(rstd * (g - mg - xh * mgx));
             }
-            *(Pack<T, V> *)(dx + row * ld_dx + (int64_t)col * V) = o;
+            store_unit<T, RAGGED>(dx + row * ld_dx, col * V, d, o);
         }
     }
     // the groups' sums, one group after the other
@@ -145,6 +149,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_grad_kernel(const T *__rest
                 if (col >= per_row) continue;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
+                    if (RAGGED && col * V + e >= d) break;
                     sums[col * V + e] = gi == 0 ? dw[j][e] : sums[col * V + e] + dw[j][e];
                     sums[d + col * V + e] = gi == 0 ? db[j][e] : sums[d + col * V + e] + db[j][e];
                 }
@@ -255,20 +260,20 @@ static int norm_groups(int64_t rows, int each, int most)
 constexpr int kNormParts = 1024;   // most workgroups that leave sums of dy xh and dy
 constexpr int kNormLongParts = 64;
 
-template <class T, int V, int L, int NV>
+template <class T, bool RAGGED, int L, int NV>
 static int norm_run(const NormParams &p, hipStream_t st)
 {
-    norm_kernel<T, V, L, NV><<<dim3(norm_groups(p.rows, kNormThreads / L, 8192)), dim3(kNormThreads), 0, st>>>(
+    norm_kernel<T, RAGGED, L, NV><<<dim3(norm_groups(p.rows, kNormThreads / L, 8192)), dim3(kNormThreads), 0, st>>>(
         (const T *)p.x, p.rows, p.d, p.ld_x, (const T *)p.weight, (const T *)p.bias, p.eps, (T *)p.y, p.ld_y, p.mean, p.rstd);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
 
-template <class T, int V, int L, int NV>
+template <class T, bool RAGGED, int L, int NV>
 static int norm_grad_run(const NormGradParams &p, hipStream_t st)
 {
     const int groups = norm_groups(p.rows, kNormThreads / L, kNormParts);
-    norm_grad_kernel<T, V, L, NV><<<dim3(groups), dim3(kNormThreads), 2 * p.d * sizeof(float), st>>>(
+    norm_grad_kernel<T, RAGGED, L, NV><<<dim3(groups), dim3(kNormThreads), 2 * p.d * sizeof(float), st>>>(
         (const T *)p.dy, p.ld_dy, (const T *)p.x, p.ld_x, p.rows, p.d, p.mean, p.rstd, (const T *)p.weight, (T *)p.dx, p.ld_dx, (float *)p.scratch);
     AVQ_HIP(hipGetLastError());
     norm_join_kernel<T><<<dim3((2 * p.d + 63) / 64), dim3(256), 0, st>>>((const float *)p.scratch, groups, p.d, (T *)p.dweight, (T *)p.dbias);
@@ -276,19 +281,16 @@ static int norm_grad_run(const NormGradParams &p, hipStream_t st)
     return AVQ_OK;
 }
 
-// lanes a row and vectors a lane, by the vectors a row has
+// lanes a row and units a lane, by the units a row has
 #define AVQ_NORM_BY_SIZE(RUN, LONG)                                   \
-    const int per_row = p.d / V;                                      \
-    if (per_row <= 16) return RUN<T, V, 16, 1>(p, st);                \
-    if (per_row <= 32) return RUN<T, V, 32, 1>(p, st);                \
-    if (per_row <= 64) return RUN<T, V, 64, 1>(p, st);                \
-    if (per_row <= 128) return RUN<T, V, 64, 2>(p, st);               \
-    if (per_row <= 256) return RUN<T, V, 64, 4>(p, st);               \
-    if constexpr (V <= 4) {                                           \
-        if (per_row <= 512) return RUN<T, V, 64, 8>(p, st);           \
-    }                                                                 \
-    if constexpr (V <= 2) {                                           \
-        if (per_row <= 1024) return RUN<T, V, 64, 16>(p, st);         \
+    const int per_row = units_of<T>(p.d);                             \
+    if (per_row <= 16) return RUN<T, RAGGED, 16, 1>(p, st);           \
+    if (per_row <= 32) return RUN<T, RAGGED, 32, 1>(p, st);           \
+    if (per_row <= 64) return RUN<T, RAGGED, 64, 1>(p, st);           \
+    if (per_row <= 128) return RUN<T, RAGGED, 64, 2>(p, st);          \
+    if (per_row <= 256) return RUN<T, RAGGED, 64, 4>(p, st);          \
+    if constexpr (sizeof(T) == 4) {                                   \
+        if (per_row <= 512) return RUN<T, RAGGED, 64, 8>(p, st);      \
     }                                                                 \
     return LONG<T>(p, st);
 
@@ -317,29 +319,22 @@ static int norm_grad_long(const NormGradParams &p, hipStream_t st)
     return AVQ_OK;
 }
 
-template <class T, int V> static int norm_sized(const NormParams &p, hipStream_t st) { AVQ_NORM_BY_SIZE(norm_run, norm_long) }
-template <class T, int V> static int norm_grad_sized(const NormGradParams &p, hipStream_t st) { AVQ_NORM_BY_SIZE(norm_grad_run, norm_grad_long) }
-
-// weight and bias are read in vectors too
-static int dense_width(const void *p, int d, int size) { return p ? row_width(p, d, d, size) : 16; }
+template <class T, bool RAGGED> static int norm_sized(const NormParams &p, hipStream_t st) { AVQ_NORM_BY_SIZE(norm_run, norm_long) }
+template <class T, bool RAGGED> static int norm_grad_sized(const NormGradParams &p, hipStream_t st) { AVQ_NORM_BY_SIZE(norm_grad_run, norm_grad_long) }
 
 template <class T>
 static int norm_typed(const NormParams &p, hipStream_t st)
 {
-    const int w = std::min(std::min(row_width(p.x, p.ld_x, p.d, sizeof(T)), row_width(p.y, p.ld_y, p.d, sizeof(T))),
-                           std::min(dense_width(p.weight, p.d, sizeof(T)), dense_width(p.bias, p.d, sizeof(T))));
-    if (w == 16) return norm_sized<T, 16 / sizeof(T)>(p, st);
-    if (w == 8) return norm_sized<T, 8 / sizeof(T)>(p, st);
-    return norm_sized<T, 1>(p, st);
+    const bool whole = whole_units(p.x, p.ld_x, p.d, sizeof(T)) && whole_units(p.y, p.ld_y, p.d, sizeof(T)) && whole_units(p.weight, p.d, p.d, sizeof(T)) &&
+                       whole_units(p.bias, p.d, p.d, sizeof(T)); // (NULL is aligned)
+    return whole ? norm_sized<T, false>(p, st) : norm_sized<T, true>(p, st);
 }
 
 template <class T>
 static int norm_grad_typed(const NormGradParams &p, hipStream_t st)
 {
-    const int w = std::min(row_width(p.x, p.ld_x, p.d, sizeof(T)), std::min(row_width(p.dy, p.ld_dy, p.d, sizeof(T)), row_width(p.dx, p.ld_dx, p.d, sizeof(T))));
-    if (w == 16) return norm_grad_sized<T, 16 / sizeof(T)>(p, st);
-    if (w == 8) return norm_grad_sized<T, 8 / sizeof(T)>(p, st);
-    return norm_grad_sized<T, 1>(p, st);
+    const bool whole = whole_units(p.x, p.ld_x, p.d, sizeof(T)) && whole_units(p.dy, p.ld_dy, p.d, sizeof(T)) && whole_units(p.dx, p.ld_dx, p.d, sizeof(T));
+    return whole ? norm_grad_sized<T, false>(p, st) : norm_grad_sized<T, true>(p, st);
 }
 
 size_t norm_grad_scratch_bytes(int64_t rows, int d)

@@ -33,6 +33,55 @@ template <> __device__ __forceinline__ f16_t from_f32<f16_t>(float v) { return f
 // V elements that are loaded and stored at once (V * sizeof(T) = 16, 8, 4 or 2 bytes).
 template <class T, int V> struct alignas(sizeof(T) * V) Pack { T e[V]; };
 
+// 16 bytes of a row: what a lane loads and stores at once.
+template <class T> constexpr int kUnit = 16 / (int)sizeof(T);
+template <class T> using Unit = Pack<T, kUnit<T>>;
+template <class T> __host__ __device__ inline int units_of(int d) { return (d + kUnit<T> - 1) / kUnit<T>; }
+
+// Whether every row of rows at `p`, `ld` elements apart and `d` long, is whole units on 16 bytes; others are RAGGED: their units lie
+// anywhere, and the last is part of one.
+inline bool whole_units(const void *p, int64_t ld, int64_t d, int size) { return (uintptr_t)p % 16 == 0 && (ld * size) % 16 == 0 && (d * size) % 16 == 0; }
+
+// Unit k / kUnit of a row, zeros past the row's end. The last one of a ragged row is read from the row's last 16 bytes and moved down:
+// no load past the row, and none that waits for a branch.
+template <class T, bool RAGGED> __device__ __forceinline__ Unit<T> load_unit(const T *__restrict__ row, int k, int d)
+{
+    constexpr int V = kUnit<T>;
+    Unit<T> v;
+    if (!RAGGED) return *(const Unit<T> *)(row + k);
+    if (d < V) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v.e[e] = k + e < d ? row[k + e] : T{};
+        return v;
+    }
+    const int past = k + V - d; // elements past the end
+    __builtin_memcpy(&v, row + (past > 0 ? d - V : k), 16);
+    unsigned long long lo, hi;
+    __builtin_memcpy(&lo, &v.e[0], 8);
+    __builtin_memcpy(&hi, &v.e[V / 2], 8);
+    const int bits = d % V == 0 ? 0 : (V - d % V) * 8 * (int)sizeof(T); // (the same for all lanes: scalar shifts)
+    const unsigned long long low = bits >= 64 ? hi >> (bits - 64) : bits == 0 ? lo : (lo >> bits) | (hi << (64 - bits)), high = bits >= 64 ? 0ull : hi >> bits;
+    lo = past > 0 ? low : lo;
+    hi = past > 0 ? high : hi;
+    __builtin_memcpy(&v.e[0], &lo, 8);
+    __builtin_memcpy(&v.e[V / 2], &hi, 8);
+    return v;
+}
+
+template <class T, bool RAGGED> __device__ __forceinline__ void store_unit(T *__restrict__ row, int k, int d, const Unit<T> &v)
+{
+    constexpr int V = kUnit<T>;
+    if (!RAGGED) {
+        *(Unit<T> *)(row + k) = v;
+    } else if (k + V <= d) {
+        __builtin_memcpy(row + k, &v, 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V - 1; ++e)
+            if (k + e < d) row[k + e] = v.e[e];
+    }
+}
+
 // Bytes that every row of rows at `p`, `ld` elements apart and `d` long, can be read in at once: 16, 8 or one element.
 inline int row_width(const void *p, int64_t ld, int64_t d, int size)
 {
