@@ -526,3 +526,40 @@ def test_more_than_two_to_the_31_logits_and_elements():
     assert got[[2_199_999, 2_199_998, 5, 6], 1000].tolist() == [2.0, 3.0, 1.0, 0.0]
     r = avq.log_probs(table, torch.full((1, 1024), 0.01, dtype=torch.bfloat16, device="cuda"), k=2)
     assert r.alt_ids[0].tolist() == [2_199_998, 2_199_999]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_small_model_learns_and_its_index_answers(dtype):
+    from paper_1908_10396_amd import learn
+
+    corpus = learn.Corpus(2000, topic=8, seed=3)
+    model = learn.Model(2000, 32, dtype, seed=3)
+    # the first step's gradients are those of the formula, in 64 bits
+    a, b = corpus.pairs(512)
+    table, weight, bias = (p.detach().double().requires_grad_() for p in model.cast())
+    x = table[a.long()]
+    off = x - x.mean(1, keepdim=True)
+    q = off / (off.square().mean(1, keepdim=True) + 1e-5).sqrt() * weight + bias
+    loss = -torch.log_softmax(model.scale * (q @ table.t()), 1)[torch.arange(512, device="cuda"), b.long()].mean()
+    loss.backward()
+    loss = loss.item()
+    got = model.gradients(a, b)
+    # fp32: sums of at most 2,000 terms, 2^-24 each; bf16: queries, dq and dx are rounded to 8 bits one after the other
+    tol = 2e-5 if dtype == torch.float32 else 2e-2
+    assert abs(float(got[0]) - loss) <= tol * loss
+    for g, want in zip(got[1:], (table.grad, weight.grad, bias.grad)):
+        assert float((g.double() - want).norm()) <= tol * float(want.norm())
+    first = loss
+    for _ in range(150):
+        last = float(model.step(*corpus.pairs(512)))
+    assert last < 0.7 * first
+    idx = learn.index_of(model, 16)
+    try:
+        ids, logp, p = learn.answer(model, idx, a, 8, 128)
+        s = model.scale * (model.queries(a).double() @ model.table.detach().double().t())
+        want = torch.log_softmax(s, 1)
+        assert float((logp.double() - want.gather(1, ids.long())).abs().max()) <= 1e-4
+        assert float((p.entropy.double() + (want.exp() * want).sum(1)).abs().max()) <= 1e-3
+        assert float(logp.exp().sum()) >= 0.9 * float(want.exp().topk(8, 1).values.sum())
+    finally:
+        idx.close()
