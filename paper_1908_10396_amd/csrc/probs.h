@@ -45,4 +45,9 @@ inline size_t finish_lds(int d, int k)
     return (size_t)(d + 31) / 32 * 32 * 4 + (k == 0 ? 0 : (size_t)std::max(32 * k, kFinishList) * 8 + (size_t)finish_best(k) * 8 + (size_t)k * 4);
 }
 
+// The gradient by one pass over the rows (probs_grad_few.hip): whether it takes a call, what it needs, and the pass.
+bool grad_few_takes(int type, int d, int nq, int given);
+size_t grad_few_scratch_bytes(int type, int d, int nq);
+int launch_grad_few(const ProbGradParams &p, hipStream_t st);
+
 } // namespace avq

@@ -354,7 +354,7 @@ static ProbGradScratch prob_grad_scratch(const ProbGradParams &p, void *base)
 
 size_t log_probs_grad_scratch_bytes(int type, int64_t n, int d, int nq, int given)
 {
-    (void)given;
+    if (grad_few_takes(type, d, nq, given)) return grad_few_scratch_bytes(type, d, nq);
     ProbGradParams p{};
     p.type = type; p.n = n; p.d = d; p.nq = nq;
     return nq == 0 ? 0 : prob_grad_scratch(p, nullptr).bytes;
@@ -445,6 +445,7 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
 
 int launch_log_probs_grad(const ProbGradParams &p, hipStream_t st)
 {
+    if (grad_few_takes(p.type, p.d, p.nq, p.given)) return launch_grad_few(p, st);
     if (p.type == AVQ_F32) return log_probs_grad_typed<float, f16_t, true>(p, st);
     return p.type == AVQ_BF16 ? log_probs_grad_typed<bf16_t, bf16_t, false>(p, st) : log_probs_grad_typed<f16_t, f16_t, false>(p, st);
 }

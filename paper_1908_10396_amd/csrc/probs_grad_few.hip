@@ -1,0 +1,284 @@
+// The gradient of the log probabilities of a few queries (G, dq and dx as in probs_grad.hip), in one pass over the rows: one to eight
+// queries leave the tiles of the matrix instructions, 256 queries wide, almost empty, while a row that is in registers needs nothing
+// else. A row lies across 16, 32 or 64 lanes as units of 16 bytes; its logits are sums over those lanes, G stays in fp32, and the same
+// registers then give dx_i = c sum_t G_ti q_t, written at once, and a lane's share of dq_t = c sum_i G_ti x_i, which stays in registers
+// until the rows are done: waves, then workgroups, are added in a fixed order. Rows are read once and dx is written once.
+// Rows among the given ids are found by a map of 2^16 bits in LDS, which nearly all rows pass by one read; the others look through
+// the ids and score their row by the arithmetic of the pass that lse is of.
+// Bound: the rows read and dx written, and for eight queries the sums over lanes.
+#include "prob_score.h"
+#include "probs.h"
+#include "row_types.h"
+
+#include <type_traits>
+
+namespace avq {
+
+constexpr int kFewThreads = 256, kFewWaves = kFewThreads / 64;
+constexpr int kFewGroups = 1024; // four workgroups a compute unit, where registers allow it
+constexpr int kFewGiven = 1024;  // ids in LDS
+constexpr int kFewHeld = 32;     // values of queries that a lane holds, and as many sums
+constexpr int kMapWords = 2048;
+
+struct FewArgs {
+    const void *x; int64_t n, ld_x; int d;
+    const void *q; int64_t ld_q; int nq; float scale;
+    const int32_t *ids; int given; const float *lse, *g, *h, *entropy, *gl;
+    void *dx; int64_t ld_dx; int accumulate;
+    float *sums; // [workgroup][NQ][units * V]
+};
+
+template <class T, bool RAGGED, int L, int NV, int NQ>
+__global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
+{
+    constexpr int V = kUnit<T>, kPer = 64 / L, U = NQ == 1 ? (NV >= 4 ? 1 : 4 / NV) : (NV >= 2 ? 1 : 2); // rows a wave has side by side, and in flight
+    constexpr int PATH = NQ == 1 ? kByRow : kByStream;                                                   // of the pass that lse is of
+    extern __shared__ char lds[]; // the queries as that pass multiplies with them; at the end, sums
+    __shared__ uint32_t map[kMapWords];
+    __shared__ int32_t given_id[kFewGiven];
+    __shared__ float given_g[kFewGiven];
+    __shared__ float coef[NQ][3]; // a, h and lse / log 2
+    const int d = p.d, units = units_of<T>(d), wave = threadIdx.x >> 6, lane = threadIdx.x & 63, in_row = lane % L;
+    const T *x = (const T *)p.x, *q = (const T *)p.q;
+    T *dx = (T *)p.dx;
+    const int listed = p.nq * p.given, staged = (d + 31) / 32 * 32;
+
+    for (int i = threadIdx.x; i < kMapWords; i += kFewThreads) map[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < listed; i += kFewThreads) {
+        const int32_t id = p.ids[i];
+        const bool real = id >= 0 && (int64_t)id < p.n;
+        given_id[i] = real ? id : -1;
+        given_g[i] = real ? p.g[i] : 0.0f;
+        if (real) atomicOr(&map[(id & 0xFFFF) / 32], 1u << (id & 31)); // (bits: no order matters)
+    }
+    if (listed > 0)
+        for (int t = 0; t < p.nq; ++t) stage_query((T *)lds + t * staged, q + t * p.ld_q, d, false, kFewThreads);
+    __syncthreads();
+    if (threadIdx.x < NQ) {
+        const int t = threadIdx.x;
+        float a = 0.0f, h = 0.0f, l = 0.0f;
+        if (t < p.nq) {
+            for (int j = 0; j < p.given; ++j) a += given_g[t * p.given + j];
+            if (p.gl) a -= p.gl[t];
+            if (p.h) { h = p.h[t]; a += h * p.entropy[t]; }
+            l = p.lse[t];
+        }
+        coef[t][0] = a;
+        coef[t][1] = h;
+        coef[t][2] = l;
+    }
+    __syncthreads();
+
+    float qs[NQ][NV * V], acc[NQ][NV * V], a[NQ], h2[NQ], lse2[NQ];
+#pragma unroll
+    for (int t = 0; t < NQ; ++t) {
+        a[t] = coef[t][0];
+        h2[t] = coef[t][1] * 0.693147180559945309f;
+        lse2[t] = coef[t][2] * 1.44269504088896341f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const int k = (in_row + j * L) * V + e;
+                qs[t][j * V + e] = t < p.nq && k < d ? to_f32(q[t * p.ld_q + k]) : 0.0f;
+                acc[t][j * V + e] = 0.0f;
+            }
+    }
+    const float c2 = p.scale * 1.44269504088896341f;
+    for (int64_t base = ((int64_t)blockIdx.x * kFewWaves + wave) * (kPer * U); base < p.n; base += (int64_t)gridDim.x * kFewWaves * (kPer * U)) {
+        Unit<T> v[U][NV];
+        int64_t row[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            row[u] = base + u * kPer + lane / L;
+            const T *from = x + min(row[u], p.n - 1) * p.ld_x;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) v[u][j] = load_unit<T, RAGGED>(from, min(in_row + j * L, units - 1) * V, d);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool real = row[u] < p.n;
+            float xs[NV * V], s[NQ];
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) xs[j * V + e] = real && in_row + j * L < units ? to_f32(v[u][j].e[e]) : 0.0f;
+#pragma unroll
+            for (int t = 0; t < NQ; ++t) {
+                s[t] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < NV * V; ++k) s[t] = __fmaf_rn(xs[k], qs[t][k], s[t]);
+                s[t] = group_sum<L>(s[t]);
+            }
+            float more[NQ] = {}; // the given ids' share of G
+            const bool maybe = real && (map[((uint32_t)row[u] & 0xFFFF) / 32] >> ((uint32_t)row[u] & 31) & 1u) != 0;
+            if (__any(maybe)) {
+                uint32_t own = 0; // queries that this row is given for
+                if (maybe) {
+#pragma unroll
+                    for (int t = 0; t < NQ; ++t) {
+                        if (t >= p.nq) continue;
+                        for (int j = 0; j < p.given; ++j)
+                            if (given_id[t * p.given + j] == (int32_t)row[u]) {
+                                more[t] += given_g[t * p.given + j];
+                                own |= 1u << t;
+                            }
+                    }
+                }
+                // the wave scores those rows, one after the other
+#pragma unroll 1
+                for (int t = 0; t < p.nq; ++t)
+                    for (uint64_t left = __ballot((own >> t & 1u) != 0 && in_row == 0); left != 0; left &= left - 1) {
+                        const int from = __ffsll((unsigned long long)left) - 1; // the first lane of that row
+                        const T *at = x + (base + u * kPer + from / L) * p.ld_x;
+                        float product = 0.0f;
+                        score_rows<PATH, 8>((const T *)lds + t * staged, d, Scoring{L, 1.0f, 1.0f}, [&](int) { return at; }, [&](int slot, float v) { if (slot == 0) product = v; });
+                        product = __shfl(product, 0, 64);
+#pragma unroll
+                        for (int i = 0; i < NQ; ++i) s[i] = i == t && lane / L == from / L ? product : s[i];
+                    }
+            }
+            float o[NV * V] = {};
+#pragma unroll
+            for (int t = 0; t < NQ; ++t) {
+                const float s2 = __fmaf_rn(s[t], c2, -lse2[t]), w = __builtin_amdgcn_exp2f(s2);
+                float G = more[t] - (w == 0.0f ? 0.0f : w * __fmaf_rn(h2[t], s2, a[t])); // (p log p)
+                if (!real) G = 0.0f;
+#pragma unroll
+                for (int k = 0; k < NV * V; ++k) {
+                    acc[t][k] = __fmaf_rn(G, xs[k], acc[t][k]);
+                    o[k] = __fmaf_rn(G, qs[t][k], o[k]);
+                }
+            }
+            if (dx && real) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    const int k = (in_row + j * L) * V;
+                    if (in_row + j * L >= units) continue;
+                    Unit<T> r;
+                    if (p.accumulate) r = load_unit<T, RAGGED>(dx + row[u] * p.ld_dx, k, d);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) r.e[e] = from_f32<T>(p.accumulate ? to_f32(r.e[e]) + o[j * V + e] * p.scale : o[j * V + e] * p.scale);
+                    store_unit<T, RAGGED>(dx + row[u] * p.ld_dx, k, d, r);
+                }
+            }
+        }
+    }
+    if (!p.sums) return;
+    // the wave's rows, then the workgroup's waves one after the other
+    float *all = (float *)lds;
+    constexpr int kWide = L * NV * V;
+    for (int w = 0; w < kFewWaves; ++w) {
+        __syncthreads(); // (also: the queries there have been read)
+        if (w != wave) continue;
+#pragma unroll
+        for (int t = 0; t < NQ; ++t)
+#pragma unroll
+            for (int k = 0; k < NV * V; ++k) {
+                float v = acc[t][k];
+#pragma unroll
+                for (int m = L; m < 64; m <<= 1) v += __shfl_xor(v, m, 64);
+                const int at = t * kWide + (in_row + k / V * L) * V + k % V;
+                if (lane < L) all[at] = w == 0 ? v : all[at] + v;
+            }
+    }
+    __syncthreads();
+    const int wide = units * V;
+    for (int i = threadIdx.x; i < NQ * kWide; i += kFewThreads) {
+        const int t = i / kWide, k = i % kWide;
+        if (k < wide) p.sums[((int64_t)blockIdx.x * NQ + t) * wide + k] = all[i];
+    }
+}
+
+// dq = the workgroups' sums: 64 columns a workgroup, sixteen strips of workgroups side by side
+template <class T>
+__global__ __launch_bounds__(1024) void grad_few_join_kernel(const float *__restrict__ sums, int groups, int held, int wide, int d, float scale, T *__restrict__ dq, int64_t ld)
+{
+    __shared__ float strips[16][64];
+    const int col = threadIdx.x & 63, strip = threadIdx.x >> 6, k = blockIdx.x * 64 + col, t = blockIdx.y;
+    float s = 0.0f;
+    if (k < d) {
+        const float *from = sums + (int64_t)t * wide + k;
+#pragma unroll 16
+        for (int g = strip; g < groups; g += 16) s += from[(int64_t)g * held * wide];
+    }
+    strips[strip][col] = s;
+    __syncthreads();
+    if (strip != 0 || k >= d) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += strips[i][col];
+    dq[(int64_t)t * ld + k] = from_f32<T>(s * scale);
+}
+
+// What a lane holds of a row, in units; 0: more than it can.
+static int few_units(int size, int d)
+{
+    const int units = (d * size + 15) / 16;
+    return units <= 64 ? 1 : units <= 128 ? 2 : units <= 256 ? 4 : 0;
+}
+static int few_queries(int nq) { return nq <= 2 ? nq : nq <= 4 ? 4 : 8; }
+
+bool grad_few_takes(int type, int d, int nq, int given)
+{
+    const int size = type == AVQ_F32 ? 4 : 2, nv = few_units(size, d);
+    return nq >= 1 && nq <= 8 && nv != 0 && nv * (16 / size) * few_queries(nq) <= kFewHeld && (int64_t)nq * given <= kFewGiven;
+}
+
+size_t grad_few_scratch_bytes(int type, int d, int nq)
+{
+    const int v = type == AVQ_F32 ? 4 : 8;
+    return (size_t)kFewGroups * few_queries(nq) * ((d + v - 1) / v * v) * sizeof(float);
+}
+
+template <class T, bool RAGGED, int L, int NV, int NQ>
+static int few_run(const ProbGradParams &p, hipStream_t st)
+{
+    constexpr int V = kUnit<T>, kRows = kFewWaves * (64 / L) * (NQ == 1 ? (NV >= 4 ? 1 : 4 / NV) : (NV >= 2 ? 1 : 2));
+    const int groups = (int)std::min<int64_t>(kFewGroups, (p.n + kRows - 1) / kRows);
+    float *sums = p.dqueries ? (float *)p.scratch : nullptr;
+    const size_t lds = std::max((size_t)NQ * L * NV * V * sizeof(float), (size_t)p.nq * ((p.d + 31) / 32 * 32) * sizeof(T));
+    grad_few_kernel<T, RAGGED, L, NV, NQ><<<dim3(groups), dim3(kFewThreads), lds, st>>>(
+        FewArgs{p.points, p.n, p.ld_points, p.d, p.queries, p.ld_queries, p.nq, p.scale, p.ids, p.given, p.lse, p.grad_logp, p.grad_entropy, p.entropy, p.grad_lse, p.dpoints,
+                p.ld_dpoints, p.accumulate, sums});
+    AVQ_HIP(hipGetLastError());
+    if (sums) {
+        grad_few_join_kernel<T><<<dim3((p.d + 63) / 64, p.nq), dim3(1024), 0, st>>>(sums, groups, NQ, units_of<T>(p.d) * V, p.d, p.scale, (T *)p.dqueries, p.ld_dqueries);
+        AVQ_HIP(hipGetLastError());
+    }
+    return AVQ_OK;
+}
+
+template <class T, bool RAGGED, int NQ>
+static int few_sized(const ProbGradParams &p, hipStream_t st)
+{
+    constexpr int V = kUnit<T>;
+    const int units = units_of<T>(p.d);
+    if constexpr (V * NQ <= kFewHeld) {
+        if (units <= 16) return few_run<T, RAGGED, 16, 1, NQ>(p, st);
+        if (units <= 32) return few_run<T, RAGGED, 32, 1, NQ>(p, st);
+        if (units <= 64) return few_run<T, RAGGED, 64, 1, NQ>(p, st);
+    }
+    if constexpr (2 * V * NQ <= kFewHeld) if (units <= 128) return few_run<T, RAGGED, 64, 2, NQ>(p, st);
+    if constexpr (4 * V * NQ <= kFewHeld) if (units <= 256) return few_run<T, RAGGED, 64, 4, NQ>(p, st);
+    set_error("rows of %d are too long for the pass of a few queries", p.d); // (grad_few_takes says so before)
+    return AVQ_EINVAL;
+}
+
+template <class T>
+static int few_typed(const ProbGradParams &p, hipStream_t st)
+{
+    const bool whole = whole_units(p.points, p.ld_points, p.d, sizeof(T)) && (!p.dpoints || whole_units(p.dpoints, p.ld_dpoints, p.d, sizeof(T)));
+    auto run = [&](auto ragged) {
+        constexpr bool RAGGED = decltype(ragged)::value;
+        return p.nq == 1 ? few_sized<T, RAGGED, 1>(p, st) : p.nq == 2 ? few_sized<T, RAGGED, 2>(p, st) : p.nq <= 4 ? few_sized<T, RAGGED, 4>(p, st) : few_sized<T, RAGGED, 8>(p, st);
+    };
+    return whole ? run(std::false_type{}) : run(std::true_type{});
+}
+
+int launch_grad_few(const ProbGradParams &p, hipStream_t st)
+{
+    return p.type == AVQ_F32 ? few_typed<float>(p, st) : p.type == AVQ_BF16 ? few_typed<bf16_t>(p, st) : few_typed<f16_t>(p, st);
+}
+
+} // namespace avq

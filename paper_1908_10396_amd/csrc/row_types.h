@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "avq_internal.h"
 
 namespace avq {
@@ -90,11 +92,23 @@ inline int row_width(const void *p, int64_t ld, int64_t d, int size)
     return size;
 }
 
-// sum over the L lanes (a power of two, at most 64) of an aligned group, in a fixed order; every lane gets it
+// sum over the L lanes (a power of two, at most 64) of an aligned group, in a fixed order; every lane gets it. Lanes are reached by the
+// adders' own operand paths, not through LDS (eight sums over 32 lanes a row, 1,183,514 x 100 fp32: SUM8_NEW against SUM8_OLD us).
 template <int L> __device__ __forceinline__ float group_sum(float v)
 {
-#pragma unroll
-    for (int m = 1; m < L; m <<= 1) v += __shfl_xor(v, m, 64);
+    auto moved = [](float x, auto ctrl) __attribute__((always_inline)) { return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), decltype(ctrl)::value, 0xF, 0xF, true)); };
+    if constexpr (L > 1) v += moved(v, std::integral_constant<int, 0xB1>{});  // the lane beside: quad_perm [1, 0, 3, 2]
+    if constexpr (L > 2) v += moved(v, std::integral_constant<int, 0x4E>{});  // the other pair: quad_perm [2, 3, 0, 1]
+    if constexpr (L > 4) v += moved(v, std::integral_constant<int, 0x141>{}); // the other four of eight: row_half_mirror
+    if constexpr (L > 8) v += moved(v, std::integral_constant<int, 0x140>{}); // the other eight of sixteen: row_mirror
+    if constexpr (L > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if constexpr (L > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
     return v;
 }
 

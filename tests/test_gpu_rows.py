@@ -563,3 +563,44 @@ def test_a_small_model_learns_and_its_index_answers(dtype):
         assert float(logp.exp().sum()) >= 0.9 * float(want.exp().topk(8, 1).values.sum())
     finally:
         idx.close()
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("n,d,nq,m", [(70_001, 100, 1, 3), (70_001, 33, 4, 2), (66_000, 64, 8, 5), (1200, 256, 8, 128), (1100, 257, 5, 1), (1000, 512, 3, 7), (999, 513, 2, 2),
+                                      (900, 1000, 1, 1024), (700, 1024, 1, 1), (700, 1025, 1, 2), (600, 2048, 1, 1), (601, 2049, 1, 1), (300, 128, 8, 129), (5, 7, 2, 3), (1, 1, 1, 1)])
+def test_log_probs_grad_of_a_few_queries(kind, n, d, nq, m):
+    g, x, q, scale = _prob_inputs(n, d, nq, kind, 2)
+    ids = random_ids((nq, m), n, g, 0.1)
+    ids[0, 0] = min(n - 1, 5)
+    ids[-1, -1] = min(n - 1, 5 + 65536)
+    up, up_h, up_l = normal((nq, m), g), normal((nq,), g), normal((nq,), g)
+    r = avq.log_probs(x, q, ids, scale=scale)
+    want_q, bound_q, want_x, bound_x = _grad_formula(x, q, scale, ids, r.lse, r.entropy, up, up_h, up_l, kind)
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, r.entropy, up_h, up_l, scale=scale)
+    within(dq, want_q, bound_q, "dqueries")
+    within(dx, want_x, bound_x, "dpoints")
+    again = avq.log_probs_grad(x, q, ids, r.lse, up, r.entropy, up_h, up_l, scale=scale)
+    assert torch.equal(again[0], dq) and torch.equal(again[1], dx), "two calls differ"
+    held = normal((n, d), g, TYPES[kind])
+    out = strided(held, 5, 2)
+    dq2, _ = avq.log_probs_grad(strided(x, 3, 1), strided(q, 9, 8), ids, r.lse, up, r.entropy, up_h, up_l, scale=scale, out_points=out, accumulate=True)
+    within(dq2, want_q, bound_q, "dqueries, strided")
+    total = want_x + held.double()
+    within(out, total, bound_x + 2 * U * total.abs() + HALF[kind] * total.abs() * 1.01, "dpoints, added")
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [1, 3, 6, 12])
+def test_log_probs_grad_of_rows_with_nearly_all_of_the_probability(kind, nq):
+    """G of such a row is g (1 - p), a difference of values near 1: the rounding of lse (and of 16 bits elsewhere) is all it is off by."""
+    g = gen(nq)
+    n, d = 4000, 100
+    x = normal((n, d), g, TYPES[kind])
+    ids = torch.randint(0, n, (nq,), generator=g, device="cuda", dtype=torch.int32)
+    q = (0.25 * normal((nq, d), g) + 0.9 * x[ids.long()].float()).to(TYPES[kind])
+    up = torch.full((nq,), -1.0 / nq, device="cuda")
+    r = avq.log_probs(x, q, ids, scale=0.25)
+    want_q, bound_q, want_x, bound_x = _grad_formula(x, q, 0.25, ids, r.lse, r.entropy, up, None, None, kind)
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, scale=0.25)
+    within(dq, want_q, bound_q, "dqueries")
+    within(dx, want_x, bound_x, "dpoints")
