@@ -107,8 +107,8 @@ struct Scoring { int lanes; float x_scale, q_scale; };
 template <int PATH> __device__ __forceinline__ int scored_at_once(const Scoring &how) { return PATH == kByTiles ? 32 : PATH == kByStream ? 16 : 4 * (64 / how.lanes); }
 
 // row(i): the i-th of those rows (a valid one always); emit(i, product): once for each, on some lane.
-// AHEAD: 16 coordinates' loads in flight (kByTiles).
-template <int PATH, int AHEAD, class T, class RowOf, class Emit>
+// AHEAD: 16 coordinates' loads in flight (kByTiles), STEPS: steps' (kByStream).
+template <int PATH, int AHEAD, int STEPS = 16, class T, class RowOf, class Emit>
 __device__ __forceinline__ void score_rows(const T *__restrict__ qs, int d, const Scoring &how, RowOf row, Emit emit)
 {
     constexpr int E = kFragElems<T>;
@@ -142,7 +142,7 @@ __device__ __forceinline__ void score_rows(const T *__restrict__ qs, int d, cons
         }
     } else if constexpr (PATH == kByStream) {
         // whole steps, NB of them asked for at once (some again past the last), and what is left
-        constexpr int S = kStepElems<T>, NB = 16;
+        constexpr int S = kStepElems<T>, NB = STEPS;
         const int r16 = lane & 15, kg = lane >> 4, whole = d / S;
         const T *p = row(r16);
         f32x4 acc{0.0f, 0.0f, 0.0f, 0.0f};

@@ -5,7 +5,10 @@
 // until the rows are done: waves, then workgroups, are added in a fixed order. Rows are read once and dx is written once.
 // Rows among the given ids are found by a map of 2^16 bits in LDS, which nearly all rows pass by one read; the others look through
 // the ids and score their row by the arithmetic of the pass that lse is of.
-// Bound: the rows read and dx written, and for eight queries the sums over lanes.
+// Bound: the rows read and dx written; 16-bit types and eight queries: the arithmetic around them, a lane's registers leaving two
+// waves a SIMD. 1,183,514 x 100 fp32 (0.95 GB): 188 us for one query (5.0 TB/s), 190 for two, 213 for four, 404 for eight, where the
+// tiles take 905 to 950; 200,000 x 1,024 bf16 (0.82 GB): 180 us for one, 206 for two, the tiles 400. The sizes that a lane's registers
+// hold without spilling are those that come here (grad_few_takes).
 #include "prob_score.h"
 #include "probs.h"
 #include "row_types.h"
@@ -20,6 +23,8 @@ constexpr int kFewGiven = 1024;  // ids in LDS
 constexpr int kFewHeld = 32;     // values of queries that a lane holds, and as many sums
 constexpr int kMapWords = 2048;
 
+constexpr int few_ahead(int units, int queries) { return std::max(1, (queries <= 2 ? 4 : 2) / units); } // a lane's rows in flight
+
 struct FewArgs {
     const void *x; int64_t n, ld_x; int d;
     const void *q; int64_t ld_q; int nq; float scale;
@@ -31,7 +36,7 @@ struct FewArgs {
 template <class T, bool RAGGED, int L, int NV, int NQ>
 __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
 {
-    constexpr int V = kUnit<T>, kPer = 64 / L, U = NQ == 1 ? (NV >= 4 ? 1 : 4 / NV) : (NV >= 2 ? 1 : 2); // rows a wave has side by side, and in flight
+    constexpr int V = kUnit<T>, kPer = 64 / L, U = few_ahead(NV, NQ); // rows a wave has side by side, and in flight
     constexpr int PATH = NQ == 1 ? kByRow : kByStream;                                                   // of the pass that lse is of
     extern __shared__ char lds[]; // the queries as that pass multiplies with them; at the end, sums
     __shared__ uint32_t map[kMapWords];
@@ -126,14 +131,15 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
                             }
                     }
                 }
-                // the wave scores those rows, one after the other
+                // the wave scores those rows, one after the other (two steps' loads in flight: sixteen's registers cost half of the
+                // waves, 292 against 190 us for two queries)
 #pragma unroll 1
                 for (int t = 0; t < p.nq; ++t)
                     for (uint64_t left = __ballot((own >> t & 1u) != 0 && in_row == 0); left != 0; left &= left - 1) {
                         const int from = __ffsll((unsigned long long)left) - 1; // the first lane of that row
                         const T *at = x + (base + u * kPer + from / L) * p.ld_x;
                         float product = 0.0f;
-                        score_rows<PATH, 8>((const T *)lds + t * staged, d, Scoring{L, 1.0f, 1.0f}, [&](int) { return at; }, [&](int slot, float v) { if (slot == 0) product = v; });
+                        score_rows<PATH, 8, 2>((const T *)lds + t * staged, d, Scoring{L, 1.0f, 1.0f}, [&](int) { return at; }, [&](int slot, float v) { if (slot == 0) product = v; });
                         product = __shfl(product, 0, 64);
 #pragma unroll
                         for (int i = 0; i < NQ; ++i) s[i] = i == t && lane / L == from / L ? product : s[i];
@@ -234,7 +240,7 @@ size_t grad_few_scratch_bytes(int type, int d, int nq)
 template <class T, bool RAGGED, int L, int NV, int NQ>
 static int few_run(const ProbGradParams &p, hipStream_t st)
 {
-    constexpr int V = kUnit<T>, kRows = kFewWaves * (64 / L) * (NQ == 1 ? (NV >= 4 ? 1 : 4 / NV) : (NV >= 2 ? 1 : 2));
+    constexpr int V = kUnit<T>, kRows = kFewWaves * (64 / L) * few_ahead(NV, NQ);
     const int groups = (int)std::min<int64_t>(kFewGroups, (p.n + kRows - 1) / kRows);
     float *sums = p.dqueries ? (float *)p.scratch : nullptr;
     const size_t lds = std::max((size_t)NQ * L * NV * V * sizeof(float), (size_t)p.nq * ((p.d + 31) / 32 * 32) * sizeof(T));
