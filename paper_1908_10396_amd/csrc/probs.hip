@@ -522,7 +522,7 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
     }
     // s - lse from the parts that lse has, before it is rounded
     auto logp_of = [&](float product) { return __fmaf_rn(__fmaf_rn(product, c2, -a.m), ln2, -log_l); };
-    constexpr int kAhead = sizeof(T) == 4 && NT == 1024 ? 4 : 8; // (what the registers hold)
+    constexpr int kAhead = sizeof(T) == 4 ? 4 : 8; // (what 128 registers hold: four waves a SIMD)
     const int at_once = scored_at_once<PATH>(how);
     for (int j0 = wave * at_once; j0 < given; j0 += NT / 64 * at_once) {
         const int32_t *mine = ids + (int64_t)row * given + j0;
