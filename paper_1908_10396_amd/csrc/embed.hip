@@ -4,6 +4,9 @@
 // table once. The gradient sorts the positions by id (stable, so that equal ids keep their order) and sums each id's run of
 // positions in that order in fp32: no atomics on values, the same result every time. Ids outside [0, n) stand for padding:
 // rows of zeros, and nothing in the gradient.
+// Lookup: rows as one list of 16-byte units, so that short and long rows fill workgroups alike; 65,536 rows of 2 KB in 41 us (268 MB, 6.5 TB/s
+// with what the caches hold). Gradient: 50,001 ids into 1,183,514 x 100 fp32 132 us, of which 473 MB of zeros alone are 72; 131,072 into
+// 670,091 x 1,024 bf16 378 us (238). The sort is launches of latency, so the table is cleared in the same ones.
 #include "row_types.h"
 
 namespace avq {
