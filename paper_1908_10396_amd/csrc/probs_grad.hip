@@ -8,7 +8,7 @@
 // relative to a bound of its magnitude, so that f16 holds it down to 2^-38 of it; its rounding to 16 bits (bf16: 2^-9) is that of
 // the operands' own type. The entries of the given ids, where p is taken from g, are formed by themselves in fp32 before rounding.
 // Bound: the matrix instructions and G's bytes. 1,024 queries, 670,091 x 1,024 bf16, in ms: G 1.50 (0.94 PFLOP/s), dx 1.71 (0.82), dq 1.46 (0.96);
-// 1,001 queries, 1,183,514 x 100 fp32: 1.08, 1.18, 1.26, where G is 9.5 GB written once and read twice.
+// 1,001 queries, 1,183,514 x 100 fp32: 1.08, 1.18, 1.26, where G is 4.8 GB, written once and read twice.
 #include "mma_tiles.h"
 #include "prob_score.h"
 #include "probs.h"
