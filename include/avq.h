@@ -466,7 +466,9 @@ int avq_layer_norm_grad(const void *grad, int32_t type, int64_t ld_grad, const v
  * are not stored. fp32 matrices are multiplied to fp32's accuracy; rows whose s_i
  * differ by less than its rounding may be ranked either way. log p is formed before
  * lse is rounded, so that it keeps its relative accuracy where p is nearly 1.
- * scale: finite, not 0. nq: 0 .. 2^19, nq x m at most 2^28. */
+ * scale: finite, not 0. nq: 0 .. 2^19, nq x m at most 2^28. A query and the rows of its k best
+ * groups of 32 have to fit a workgroup's memory: several hundred alternatives of very long
+ * rows are refused. */
 int64_t avq_log_probs_scratch(int32_t type, int64_t n, int32_t d, int32_t nq, int32_t m, int32_t k);
 int avq_log_probs(const void *points, int32_t type, int64_t n, int32_t d, int64_t ld_points, const void *queries, int32_t nq,
                   int64_t ld_queries, float scale, const int32_t *ids, int32_t m, float *logp_out, float *lse_out,
@@ -478,7 +480,8 @@ int avq_log_probs(const void *points, int32_t type, int64_t n, int32_t d, int64_
  *   a_t = sum_j grad_logp_tj - grad_lse_t + grad_entropy_t entropy_t   (sums over ids that are no padding)
  * dqueries_t = scale * sum_i G_ti x_i and dpoints_i = scale * sum_t G_ti q_t (accumulate != 0: added to
  * what dpoints holds). Either may be NULL. lse: as avq_log_probs gave it for the same
- * points, queries and scale. 16-bit types: G is rounded to the type for the products. */
+ * points, queries and scale, or that of more rows, these among them (a part of a table). 16-bit
+ * types: G is rounded to the type for the products of more than a few queries. */
 int64_t avq_log_probs_grad_scratch(int32_t type, int64_t n, int32_t d, int32_t nq, int32_t m);
 int avq_log_probs_grad(const void *points, int32_t type, int64_t n, int32_t d, int64_t ld_points, const void *queries,
                        int32_t nq, int64_t ld_queries, float scale, const int32_t *ids, int32_t m, const float *lse,

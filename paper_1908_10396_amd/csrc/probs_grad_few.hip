@@ -5,9 +5,12 @@
 // until the rows are done: waves, then workgroups, are added in a fixed order. Rows are read once and dx is written once.
 // Rows among the given ids are found by a map of 2^16 bits in LDS, which nearly all rows pass by one read; the others look through
 // the ids and score their row by the arithmetic of the pass that lse is of.
+// 1 - p of a row with nearly all of the probability would have the rounding of lse, 2^-24 |lse| / (1 - p) of it. fp32: the pass also sums
+// p over all rows, Z = 1 + delta; to first order p (a + h log p) is too large by delta p (a + h log p + h), which the given rows'
+// entries of G get back at the end, in dq and in dx (elsewhere it is a part in millions of what is there; 16-bit results hide it).
 // Bound: the rows read and dx written; 16-bit types and eight queries: the arithmetic around them, a lane's registers leaving two
-// waves a SIMD. 1,183,514 x 100 fp32 (0.95 GB): 188 us for one query (5.0 TB/s), 190 for two, 213 for four, 404 for eight, where the
-// tiles take 905 to 950; 200,000 x 1,024 bf16 (0.82 GB): 180 us for one, 206 for two, the tiles 400. The sizes that a lane's registers
+// waves a SIMD. 1,183,514 x 100 fp32 (0.95 GB): 194 us for one query (4.9 TB/s), 200 for two, 229 for four, 465 for eight, where the
+// tiles take 905 to 950; 200,000 x 1,024 bf16 (0.82 GB): 179 us for one, 205 for two, the tiles 395. Z and the given rows' mending cost 4 to 6 us of each fp32 call. The sizes that a lane's registers
 // hold without spilling are those that come here (grad_few_takes).
 #include "prob_score.h"
 #include "probs.h"
@@ -30,7 +33,9 @@ struct FewArgs {
     const void *q; int64_t ld_q; int nq; float scale;
     const int32_t *ids; int given; const float *lse, *g, *h, *entropy, *gl;
     void *dx; int64_t ld_dx; int accumulate;
-    float *sums; // [workgroup][NQ][units * V]
+    float *sums;   // [workgroup][NQ][units * V]
+    float2 *z;     // [workgroup][NQ] sums of p below 1/4, and of the others (fp32)
+    float *shares; // [nq][given] p (a + h log p + h); of a query's equal ids the first has it (fp32)
 };
 
 template <class T, bool RAGGED, int L, int NV, int NQ>
@@ -38,6 +43,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
 {
     constexpr int V = kUnit<T>, kPer = 64 / L, U = few_ahead(NV, NQ); // rows a wave has side by side, and in flight
     constexpr int PATH = NQ == 1 ? kByRow : kByStream;                                                   // of the pass that lse is of
+    constexpr bool MEND = sizeof(T) == 4;
     extern __shared__ char lds[]; // the queries as that pass multiplies with them; at the end, sums
     __shared__ uint32_t map[kMapWords];
     __shared__ int32_t given_id[kFewGiven];
@@ -55,6 +61,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
         const bool real = id >= 0 && (int64_t)id < p.n;
         given_id[i] = real ? id : -1;
         given_g[i] = real ? p.g[i] : 0.0f;
+        if (MEND && !real && blockIdx.x == 0) p.shares[i] = 0.0f;
         if (real) atomicOr(&map[(id & 0xFFFF) / 32], 1u << (id & 31)); // (bits: no order matters)
     }
     if (listed > 0)
@@ -90,6 +97,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
                 acc[t][j * V + e] = 0.0f;
             }
     }
+    float z_low = 0.0f, z_high = 0.0f; // of query in_row
     const float c2 = p.scale * 1.44269504088896341f;
     for (int64_t base = ((int64_t)blockIdx.x * kFewWaves + wave) * (kPer * U); base < p.n; base += (int64_t)gridDim.x * kFewWaves * (kPer * U)) {
         Unit<T> v[U][NV];
@@ -132,7 +140,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
                     }
                 }
                 // the wave scores those rows, one after the other (two steps' loads in flight: sixteen's registers cost half of the
-                // waves, 292 against 190 us for two queries)
+                // waves, 292 against 190 us for two queries of 1,183,514 x 100 fp32)
 #pragma unroll 1
                 for (int t = 0; t < p.nq; ++t)
                     for (uint64_t left = __ballot((own >> t & 1u) != 0 && in_row == 0); left != 0; left &= left - 1) {
@@ -143,6 +151,16 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
                         product = __shfl(product, 0, 64);
 #pragma unroll
                         for (int i = 0; i < NQ; ++i) s[i] = i == t && lane / L == from / L ? product : s[i];
+                        if (MEND && lane == 0) {
+                            const int32_t id = (int32_t)(base + u * kPer + from / L);
+                            const float s2 = __fmaf_rn(product, c2, -(coef[t][2] * 1.44269504088896341f)), w = __builtin_amdgcn_exp2f(s2), h = coef[t][1];
+                            float share = w == 0.0f ? 0.0f : w * (__fmaf_rn(h * 0.693147180559945309f, s2, coef[t][0]) + h);
+                            for (int j = 0; j < p.given; ++j)
+                                if (given_id[t * p.given + j] == id) {
+                                    p.shares[t * p.given + j] = share;
+                                    share = 0.0f;
+                                }
+                        }
                     }
             }
             float o[NV * V] = {};
@@ -151,6 +169,11 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
                 const float s2 = __fmaf_rn(s[t], c2, -lse2[t]), w = __builtin_amdgcn_exp2f(s2);
                 float G = more[t] - (w == 0.0f ? 0.0f : w * __fmaf_rn(h2[t], s2, a[t])); // (p log p)
                 if (!real) G = 0.0f;
+                if (MEND) {
+                    const float mine = real && in_row == t ? w : 0.0f;
+                    z_low += mine >= 0.25f ? 0.0f : mine;
+                    z_high += mine >= 0.25f ? mine : 0.0f;
+                }
 #pragma unroll
                 for (int k = 0; k < NV * V; ++k) {
                     acc[t][k] = __fmaf_rn(G, xs[k], acc[t][k]);
@@ -169,6 +192,21 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
                     store_unit<T, RAGGED>(dx + row[u] * p.ld_dx, k, d, r);
                 }
             }
+        }
+    }
+    if (MEND) {
+        __shared__ float2 waves_z[kFewWaves][NQ];
+#pragma unroll
+        for (int m = L; m < 64; m <<= 1) {
+            z_low += __shfl_xor(z_low, m, 64);
+            z_high += __shfl_xor(z_high, m, 64);
+        }
+        if (lane < NQ) waves_z[wave][lane] = make_float2(z_low, z_high);
+        __syncthreads();
+        if (threadIdx.x < NQ) {
+            float2 v = waves_z[0][threadIdx.x];
+            for (int w = 1; w < kFewWaves; ++w) { v.x += waves_z[w][threadIdx.x].x; v.y += waves_z[w][threadIdx.x].y; }
+            p.z[(int64_t)blockIdx.x * NQ + threadIdx.x] = v;
         }
     }
     if (!p.sums) return;
@@ -197,24 +235,71 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
     }
 }
 
-// dq = the workgroups' sums: 64 columns a workgroup, sixteen strips of workgroups side by side
+// delta of each query, a workgroup each. More than rounding is not mended: such an lse is of more rows than these (a part of a table).
+__global__ __launch_bounds__(kFewGroups) void grad_few_delta_kernel(const float2 *__restrict__ z, int groups, int held, const float *__restrict__ lse, float *__restrict__ delta)
+{
+    __shared__ double all[kFewGroups];
+    const int i = threadIdx.x, t = blockIdx.x;
+    const float2 v = i < groups ? z[(int64_t)i * held + t] : make_float2(0.0f, 0.0f);
+    all[i] = (double)v.x + (double)v.y;
+    for (int m = kFewGroups / 2; m > 0; m >>= 1) {
+        __syncthreads();
+        if (i < m) all[i] += all[i + m];
+    }
+    const float v1 = (float)(all[0] - 1.0);
+    if (i == 0) delta[t] = fabsf(v1) <= 1e-5f * (1.0f + fabsf(lse[t])) ? v1 : 0.0f;
+}
+
+// dq = the workgroups' sums and, in fp32, what the given rows' G gets back: 64 columns a workgroup, sixteen strips of workgroups, and of
+// ids, side by side
 template <class T>
-__global__ __launch_bounds__(1024) void grad_few_join_kernel(const float *__restrict__ sums, int groups, int held, int wide, int d, float scale, T *__restrict__ dq, int64_t ld)
+__global__ __launch_bounds__(1024) void grad_few_join_kernel(FewArgs p, int groups, int held, int wide, const float *__restrict__ delta, T *__restrict__ dq, int64_t ld)
 {
     __shared__ float strips[16][64];
     const int col = threadIdx.x & 63, strip = threadIdx.x >> 6, k = blockIdx.x * 64 + col, t = blockIdx.y;
     float s = 0.0f;
-    if (k < d) {
-        const float *from = sums + (int64_t)t * wide + k;
+    if (k < p.d) {
+        const float *from = p.sums + (int64_t)t * wide + k;
 #pragma unroll 16
         for (int g = strip; g < groups; g += 16) s += from[(int64_t)g * held * wide];
+        if (delta) {
+            for (int j = strip; j < p.given; j += 16) {
+                const float share = p.shares[t * p.given + j];
+                if (share != 0.0f) s = __fmaf_rn(share * delta[t], to_f32(((const T *)p.x)[(int64_t)p.ids[t * p.given + j] * p.ld_x + k]), s);
+            }
+        }
     }
     strips[strip][col] = s;
     __syncthreads();
-    if (strip != 0 || k >= d) return;
+    if (strip != 0 || k >= p.d) return;
 #pragma unroll
     for (int i = 1; i < 16; ++i) s += strips[i][col];
-    dq[(int64_t)t * ld + k] = from_f32<T>(s * scale);
+    dq[(int64_t)t * ld + k] = from_f32<T>(s * p.scale);
+}
+
+// The same for dx: a row at the first of all ids that name it, of all queries.
+__global__ __launch_bounds__(1024) void grad_few_mend_kernel(FewArgs p, const float *__restrict__ delta)
+{
+    __shared__ float strips[16][64];
+    const int col = threadIdx.x & 63, strip = threadIdx.x >> 6, k = blockIdx.x * 64 + col, i = blockIdx.y, listed = p.nq * p.given;
+    const int32_t id = p.ids[i];
+    if (id < 0 || (int64_t)id >= p.n) return;
+    bool later = false;
+    float s = 0.0f;
+    for (int e = strip; e < listed; e += 16) {
+        if (p.ids[e] != id) continue;
+        later = later || e < i;
+        const int t = e / p.given;
+        if (k < p.d) s = __fmaf_rn(p.shares[e] * delta[t], ((const float *)p.q)[t * p.ld_q + k], s);
+    }
+    if (__syncthreads_or(later)) return;
+    strips[strip][col] = s;
+    __syncthreads();
+    if (strip != 0 || k >= p.d) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += strips[w][col];
+    float *to = (float *)p.dx + (int64_t)id * p.ld_dx + k;
+    *to = __fmaf_rn(s, p.scale, *to);
 }
 
 // What a lane holds of a row, in units; 0: more than it can.
@@ -231,25 +316,51 @@ bool grad_few_takes(int type, int d, int nq, int given)
     return nq >= 1 && nq <= 8 && nv != 0 && nv * (16 / size) * few_queries(nq) <= kFewHeld && (int64_t)nq * given <= kFewGiven;
 }
 
-size_t grad_few_scratch_bytes(int type, int d, int nq)
+struct FewScratch { float *sums; float2 *z; float *shares, *delta; size_t bytes; };
+
+static FewScratch few_scratch(int size, int d, int nq, void *base)
 {
-    const int v = type == AVQ_F32 ? 4 : 8;
-    return (size_t)kFewGroups * few_queries(nq) * ((d + v - 1) / v * v) * sizeof(float);
+    FewScratch s{};
+    const int v = 16 / size, held = few_queries(nq);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        void *q = base ? (char *)base + at : nullptr;
+        at += (bytes + 255) & ~(size_t)255;
+        return q;
+    };
+    s.sums = (float *)take(sizeof(float) * kFewGroups * held * ((d + v - 1) / v * v));
+    s.z = (float2 *)take(sizeof(float2) * kFewGroups * held);
+    s.shares = (float *)take(sizeof(float) * kFewGiven);
+    s.delta = (float *)take(sizeof(float) * held);
+    s.bytes = at;
+    return s;
 }
+
+size_t grad_few_scratch_bytes(int type, int d, int nq) { return few_scratch(type == AVQ_F32 ? 4 : 2, d, nq, nullptr).bytes; }
 
 template <class T, bool RAGGED, int L, int NV, int NQ>
 static int few_run(const ProbGradParams &p, hipStream_t st)
 {
     constexpr int V = kUnit<T>, kRows = kFewWaves * (64 / L) * few_ahead(NV, NQ);
+    const FewScratch s = few_scratch(sizeof(T), p.d, p.nq, p.scratch);
     const int groups = (int)std::min<int64_t>(kFewGroups, (p.n + kRows - 1) / kRows);
-    float *sums = p.dqueries ? (float *)p.scratch : nullptr;
     const size_t lds = std::max((size_t)NQ * L * NV * V * sizeof(float), (size_t)p.nq * ((p.d + 31) / 32 * 32) * sizeof(T));
-    grad_few_kernel<T, RAGGED, L, NV, NQ><<<dim3(groups), dim3(kFewThreads), lds, st>>>(
-        FewArgs{p.points, p.n, p.ld_points, p.d, p.queries, p.ld_queries, p.nq, p.scale, p.ids, p.given, p.lse, p.grad_logp, p.grad_entropy, p.entropy, p.grad_lse, p.dpoints,
-                p.ld_dpoints, p.accumulate, sums});
+    const FewArgs args{p.points, p.n, p.ld_points, p.d, p.queries, p.ld_queries, p.nq, p.scale, p.ids, p.given, p.lse, p.grad_logp, p.grad_entropy, p.entropy, p.grad_lse, p.dpoints,
+                       p.ld_dpoints, p.accumulate, p.dqueries ? s.sums : nullptr, s.z, s.shares};
+    grad_few_kernel<T, RAGGED, L, NV, NQ><<<dim3(groups), dim3(kFewThreads), lds, st>>>(args);
     AVQ_HIP(hipGetLastError());
-    if (sums) {
-        grad_few_join_kernel<T><<<dim3((p.d + 63) / 64, p.nq), dim3(1024), 0, st>>>(sums, groups, NQ, units_of<T>(p.d) * V, p.d, p.scale, (T *)p.dqueries, p.ld_dqueries);
+    const bool mend = sizeof(T) == 4 && p.given > 0;
+    if (mend) {
+        grad_few_delta_kernel<<<dim3(p.nq), dim3(kFewGroups), 0, st>>>(s.z, groups, NQ, p.lse, s.delta);
+        AVQ_HIP(hipGetLastError());
+    }
+    const unsigned columns = (unsigned)((p.d + 63) / 64);
+    if (p.dqueries) {
+        grad_few_join_kernel<T><<<dim3(columns, p.nq), dim3(1024), 0, st>>>(args, groups, NQ, units_of<T>(p.d) * V, mend ? s.delta : nullptr, (T *)p.dqueries, p.ld_dqueries);
+        AVQ_HIP(hipGetLastError());
+    }
+    if (mend && p.dpoints) {
+        grad_few_mend_kernel<<<dim3(columns, p.nq * p.given), dim3(1024), 0, st>>>(args, s.delta);
         AVQ_HIP(hipGetLastError());
     }
     return AVQ_OK;

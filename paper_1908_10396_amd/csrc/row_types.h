@@ -93,7 +93,7 @@ inline int row_width(const void *p, int64_t ld, int64_t d, int size)
 }
 
 // sum over the L lanes (a power of two, at most 64) of an aligned group, in a fixed order; every lane gets it. Lanes are reached by the
-// adders' own operand paths, not through LDS (eight sums over 32 lanes a row, 1,183,514 x 100 fp32: the gradient 405 against 451 us).
+// adders' own operand paths, not through LDS (eight sums over 32 lanes a row, 1,183,514 x 100 fp32: the gradient took 405 against 451 us).
 template <int L> __device__ __forceinline__ float group_sum(float v)
 {
     auto moved = [](float x, auto ctrl) __attribute__((always_inline)) { return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), decltype(ctrl)::value, 0xF, 0xF, true)); };

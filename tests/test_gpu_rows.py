@@ -604,3 +604,43 @@ def test_log_probs_grad_of_rows_with_nearly_all_of_the_probability(kind, nq):
     dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, scale=0.25)
     within(dq, want_q, bound_q, "dqueries")
     within(dx, want_x, bound_x, "dpoints")
+
+
+@pytest.mark.parametrize("nq", [1, 2, 4, 7])
+@pytest.mark.parametrize("n,d", [(4000, 475), (36_249, 250)])
+def test_gradient_of_a_few_queries_whose_answer_is_nearly_certain(nq, n, d):
+    """G of the given row is g (1 - p), the sum of the other rows' p: its relative error is that of the logits' differences and a few
+    roundings of 1, not that of lse; elsewhere G is off by p's relative error, lse's rounding among it."""
+    if nq > 2 and d > 256:
+        d = 256  # (what a lane holds)
+    g = gen(nq + n)
+    x = normal((n, d), g)
+    ids = torch.randperm(n, generator=g, device="cuda")[:nq].to(torch.int32)
+    q = 0.25 * normal((nq, d), g) + 0.9 * x[ids.long()]
+    scale = 25.0 / d
+    up = torch.full((nq,), -1.0 / nq, device="cuda")
+    r = avq.log_probs(x, q, ids, scale=scale)
+    s, e = _logits(x, q, scale)
+    p = torch.softmax(s, 1)
+    at = torch.arange(nq, device="cuda"), ids.long()
+    away = s - s[at][:, None]
+    away[at] = -math.inf
+    rest = torch.exp(away).sum(1)
+    rest = rest / (1 + rest)
+    G = -p * up.double()[:, None]
+    G[at] = up.double() * rest
+    off = 4 * e.amax(1, keepdim=True) + 64 * U
+    e_G = G.abs() * (off + 2 * U * r.lse.double().abs()[:, None])
+    e_G[at] = up.double().abs() * (rest * off[:, 0] + 16 * U)
+    s32 = torch.tensor(scale, dtype=torch.float32).item()
+    xd, qd = x.double(), q.double()
+    want_q, want_x = G @ xd * scale, G.t() @ qd * scale
+    bound_q = s32 * (e_G @ xd.abs() + (4096 + 64) * U * (G.abs() @ xd.abs())) + 2 * U * want_q.abs()
+    bound_x = s32 * (e_G.t() @ qd.abs() + (nq + 8) * U * (G.abs().t() @ qd.abs())) + 2 * U * want_x.abs()
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, scale=scale)
+    within(dx, want_x, bound_x, "dpoints")
+    within(dq, want_q, bound_q, "dqueries")
+    # an lse of more rows than these is taken as it is
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse + 0.5, up, scale=scale)
+    G = up.double()[:, None] * (torch.nn.functional.one_hot(ids.long(), n).double() - p * math.exp(-0.5))
+    assert float((dx.double() - G.t() @ qd * scale).norm() / (G.t() @ qd * scale).norm()) < 1e-4
