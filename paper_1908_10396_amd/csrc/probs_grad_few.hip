@@ -10,8 +10,8 @@
 // entries of G get back at the end, in dq and in dx (elsewhere it is a part in millions of what is there; 16-bit results hide it).
 // Bound: the rows read and dx written; 16-bit types and eight queries: the arithmetic around them, a lane's registers leaving two
 // waves a SIMD. 1,183,514 x 100 fp32 (0.95 GB): 194 us for one query (4.9 TB/s), 200 for two, 229 for four, 465 for eight, where the
-// tiles take 905 to 950; 200,000 x 1,024 bf16 (0.82 GB): 179 us for one, 205 for two, the tiles 395. Z and the given rows' mending cost 4 to 6 us of each fp32 call. The sizes that a lane's registers
-// hold without spilling are those that come here (grad_few_takes).
+// tiles take 905 to 950; 200,000 x 1,024 bf16 (0.82 GB): 179 us for one, 205 for two, the tiles 395. Z and what the given rows get back
+// cost 4 to 6 us of an fp32 call. The sizes that a lane's registers hold without spilling are those that come here (grad_few_takes).
 #include "prob_score.h"
 #include "probs.h"
 #include "row_types.h"
