@@ -10,18 +10,43 @@
 
 namespace avq {
 
-// Running statistics of logits s (in units of log 2): the maximum m, the sums of 2^(s - m) and of 2^(s - m) (s - m).
-struct Stat { float m, l, t; };
+// sum + low + v, low what sum has no room for: what lies beside the maximum's 1 keeps its own relative accuracy, and with it log p
+// of an answer that has nearly all of the probability.
+__device__ __forceinline__ void add_wide(float &sum, float &low, float v)
+{
+    const float s = sum + v, part = s - sum;
+    low += (sum - (s - part)) + (v - part);
+    sum = s;
+}
 
-// Of two sets of logits; one without any has m = -inf and sums of 0.
-__device__ __forceinline__ Stat join(const Stat &a, const Stat &b)
+// log(sum + low)
+__device__ __forceinline__ float log_wide(float sum, float low)
+{
+    const float beside = (sum - 1.0f) + low;
+    return fabsf(beside) < 0.5f ? log1pf(beside) : logf(sum + low);
+}
+
+// Running statistics of logits: the maximum m of the products, and over the logits s, in units of log 2 and relative to that of m,
+// the sums of 2^s (l + low; that of m itself is 1, exactly) and of 2^s s.
+struct Stat { float m, l, low, t; };
+
+// Of two sets of logits; one without any has m = -inf and sums of 0. c2: from products to logits.
+__device__ __forceinline__ Stat join(const Stat &a, const Stat &b, float c2)
 {
     const float m = fmaxf(a.m, b.m);
-    if (!(m > -INFINITY)) return Stat{m, a.l + b.l, a.t + b.t}; // (NaN goes on in the sums)
-    const float da = a.m > -INFINITY ? a.m - m : 0.0f, db = b.m > -INFINITY ? b.m - m : 0.0f;
+    if (!(m > -INFINITY)) return Stat{m, a.l + b.l, 0.0f, a.t + b.t}; // (NaN goes on in the sums)
+    const float da = a.m > -INFINITY ? (a.m - m) * c2 : 0.0f, db = b.m > -INFINITY ? (b.m - m) * c2 : 0.0f;
     const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
-    return Stat{m, a.l * fa + b.l * fb, fa * __fmaf_rn(a.l, da, a.t) + fb * __fmaf_rn(b.l, db, b.t)};
+    Stat s{m, a.l * fa, a.low * fa, fa * __fmaf_rn(a.l, da, a.t) + fb * __fmaf_rn(b.l, db, b.t)};
+    add_wide(s.l, s.low, b.l * fb);
+    s.low = __fmaf_rn(b.low, fb, s.low);
+    return s;
 }
+
+// of the lane `mask` away
+__device__ __forceinline__ Stat across(const Stat &a, int mask) { return Stat{__shfl_xor(a.m, mask, 64), __shfl_xor(a.l, mask, 64), __shfl_xor(a.low, mask, 64), __shfl_xor(a.t, mask, 64)}; }
+__device__ __forceinline__ float4 packed(const Stat &a) { return make_float4(a.m, a.l, a.low, a.t); }
+__device__ __forceinline__ Stat unpacked(const float4 &v) { return Stat{v.x, v.y, v.z, v.w}; }
 
 // The pass that forms a query's statistics: one query whose rows fit four loads of a wave goes by rows (two, by a kernel of two sums a
 // row: 133 against 117 us through the matrix instructions, 1,183,514 x 100 fp32); up to 64 queries the rows are streamed once; more go

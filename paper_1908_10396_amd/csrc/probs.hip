@@ -44,12 +44,12 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prob_stream_kernel(const T 
         if (sizeof(T) == 4) mask[w] = k_last + w < d ? ~0u : 0u;
         else mask[w] = (k_last + 2 * w < d ? 0xffffu : 0u) | (k_last + 2 * w + 1 < d ? 0xffff0000u : 0u);
     }
-    float m[QT], l[QT], t[QT];
+    float m[QT], l[QT], low[QT], t[QT];
     f32x4 acc[2][QT];
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
         m[i] = -INFINITY;
-        l[i] = t[i] = 0.0f;
+        l[i] = low[i] = t[i] = 0.0f;
         acc[0][i] = acc[1][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
     const int64_t tiles = (n + 31) / 32, whole_tiles = d >= E ? (n - 1) / 32 : 0, stride = (int64_t)gridDim.x * kStreamWaves;
@@ -120,22 +120,25 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prob_stream_kernel(const T 
                     if (h * 16 + kg * 4 + r < valid) top = fmaxf(top, acc[h][i][r]);
             if (top > m[i]) {
                 if (m[i] > -INFINITY) {
-                    const float down = m[i] * c2 - top * c2, f = __builtin_amdgcn_exp2f(down);
+                    const float down = (m[i] - top) * c2, f = __builtin_amdgcn_exp2f(down);
                     t[i] = f * __fmaf_rn(l[i], down, t[i]);
                     l[i] *= f;
+                    low[i] *= f;
                 }
                 m[i] = top;
             }
-            const float shift = m[i] > -INFINITY ? -(m[i] * c2) : 0.0f;
+            const float base = m[i] > -INFINITY ? m[i] : 0.0f;
+            float sum = 0.0f;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     if (h * 16 + kg * 4 + r < valid) {
-                        const float s2 = __fmaf_rn(acc[h][i][r], c2, shift), e = __builtin_amdgcn_exp2f(s2);
-                        l[i] += e;
+                        const float s2 = (acc[h][i][r] - base) * c2, e = __builtin_amdgcn_exp2f(s2);
+                        sum += e;
                         t[i] = __fmaf_rn(e, s2, t[i]);
                     }
+            add_wide(l[i], low[i], sum);
             if (gmax) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -171,24 +174,17 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prob_stream_kernel(const T 
     // the four lanes of a query, then the waves
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
-        Stat a{m[i] > -INFINITY ? m[i] * c2 : -INFINITY, l[i], t[i]};
+        Stat a{m[i], l[i], low[i], t[i]};
 #pragma unroll
-        for (int x16 = 16; x16 < 64; x16 *= 2) a = join(a, Stat{__shfl_xor(a.m, x16, 64), __shfl_xor(a.l, x16, 64), __shfl_xor(a.t, x16, 64)});
-        float top = m[i];
-#pragma unroll
-        for (int x16 = 16; x16 < 64; x16 *= 2) top = fmaxf(top, __shfl_xor(top, x16, 64));
-        if (kg == 0) joined[wave][i * 16 + r16] = make_float4(a.m, a.l, a.t, top);
+        for (int x16 = 16; x16 < 64; x16 *= 2) a = join(a, across(a, x16), c2);
+        if (kg == 0) joined[wave][i * 16 + r16] = packed(a);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < QT * 16; i += kStreamThreads) {
         if (q0 + i >= nq) continue;
-        Stat a{joined[0][i].x, joined[0][i].y, joined[0][i].z};
-        float top = joined[0][i].w;
-        for (int w = 1; w < kStreamWaves; ++w) {
-            a = join(a, Stat{joined[w][i].x, joined[w][i].y, joined[w][i].z});
-            top = fmaxf(top, joined[w][i].w);
-        }
-        stats[(size_t)blockIdx.x * nq + q0 + i] = make_float4(a.m, a.l, a.t, top);
+        Stat a = unpacked(joined[0][i]);
+        for (int w = 1; w < kStreamWaves; ++w) a = join(a, unpacked(joined[w][i]), c2);
+        stats[(size_t)blockIdx.x * nq + q0 + i] = packed(a);
     }
 }
 
@@ -226,7 +222,7 @@ __global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restri
         for (int e = 0; e < E; ++e) qf[f][e] = k + e < d ? (c2 < 0.0f ? -1.0f : 1.0f) * to_f32(q[k + e]) : 0.0f;
     }
     c2 = fabsf(c2); // (so that the largest product is the largest logit)
-    float m = -INFINITY, l = 0.0f, t = 0.0f, top = -INFINITY, best = -INFINITY;
+    float m = -INFINITY, l = 0.0f, low = 0.0f, t = 0.0f, top = -INFINITY;
     // (16 bytes of the last row may run past the last element: the tile that holds it, and rows shorter than 16 bytes, go by themselves)
     const int64_t tiles = (n + 31) / 32, whole = d >= E ? (n - 1) / 32 : 0, stride = (int64_t)gridDim.x * kRowWaves;
 
@@ -274,15 +270,16 @@ __global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restri
         const bool real = mine && row < n;
         if (real && sum > m) {
             if (m > -INFINITY) {
-                const float down = m * c2 - sum * c2, f = __builtin_amdgcn_exp2f(down);
+                const float down = (m - sum) * c2, f = __builtin_amdgcn_exp2f(down);
                 t = f * __fmaf_rn(l, down, t);
                 l *= f;
+                low *= f;
             }
             m = sum;
         }
-        const float s2 = m > -INFINITY ? __fmaf_rn(sum, c2, -(m * c2)) : sum, e = __builtin_amdgcn_exp2f(s2);
+        const float s2 = m > -INFINITY ? (sum - m) * c2 : sum, e = __builtin_amdgcn_exp2f(s2);
         if (real) {
-            l += e;
+            add_wide(l, low, e);
             t = __fmaf_rn(e, s2, t);
             top = fmaxf(top, sum);
         }
@@ -291,7 +288,6 @@ __global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restri
 #pragma unroll
             for (int w = 1; w < 64; w <<= 1) g = fmaxf(g, __shfl_xor(g, w, 64));
             if (lane == 0) gmax[tile] = g;
-            best = fmaxf(best, g);
             top = -INFINITY;
         }
     };
@@ -325,24 +321,22 @@ __global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restri
                 }
             take(here, tile, turn);
         }
-    Stat a{m > -INFINITY ? m * c2 : -INFINITY, l, t};
+    Stat a{m, l, low, t};
 #pragma unroll
-    for (int w = 1; w < 64; w <<= 1) a = join(a, Stat{__shfl_xor(a.m, w, 64), __shfl_xor(a.l, w, 64), __shfl_xor(a.t, w, 64)});
-    if (lane == 0) joined[wave] = make_float4(a.m, a.l, a.t, best);
+    for (int w = 1; w < 64; w <<= 1) a = join(a, across(a, w), c2);
+    if (lane == 0) joined[wave] = packed(a);
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kRowWaves; ++w) {
-            a = join(a, Stat{joined[w].x, joined[w].y, joined[w].z});
-            best = fmaxf(best, joined[w].w);
-        }
-        stats[blockIdx.x] = make_float4(a.m, a.l, a.t, best);
+        for (int w = 1; w < kRowWaves; ++w) a = join(a, unpacked(joined[w]), c2);
+        stats[blockIdx.x] = packed(a);
     }
 }
 
 // ---- many queries: tiles of a matrix product ----------------------------------------------------
 
 // Statistics of 128 queries over a part of the rows, 256 rows at a time; a lane has two queries, 64 of a tile's rows of each.
-// X: the launch's rows, Q: all queries, negated where the scale is.
+// X: the launch's rows, Q: all queries, negated where the scale is. A lane's sums are relative to fl(m c2), one operation a logit instead
+// of two; at the end they are made relative to m itself, whose own term is known to the bit.
 template <class H, bool SPLIT, bool BEST>
 __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Rows16 Q, int steps, float c2, const Largest *__restrict__ largest, const float *__restrict__ q_inv, int parts,
                                                                     int others, float4 *__restrict__ stats, float *__restrict__ gmax, int64_t gstride)
@@ -355,7 +349,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
     int count;
     part_tiles(tiles, parts, place.part, &first, &count);
     const int64_t q0 = (int64_t)place.other * kTileN;
-    float cq[2], m[2], l[2], t[2];
+    float cq[2], m[2], l[2], low[2], t[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         cq[j] = c2;
@@ -364,7 +358,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
             cq[j] = c2 * q_inv[q] * (1.0f / range_scale(largest->points));
         }
         m[j] = -INFINITY;
-        l[j] = t[j] = 0.0f;
+        l[j] = low[j] = t[j] = 0.0f;
     }
     typedef RowCopies<SPLIT, true> Copies;
     run_tiles<H, SPLIT, BEST, Copies>(X, Q, steps, count, lds, [&](int i, Copies &c) { c.seek(X, (first + i) * kTileM, Q, q0); },
@@ -391,6 +385,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
                             const float down = m[j] * cq[j] - top * cq[j], f = __builtin_amdgcn_exp2f(down);
                             t[j] = f * __fmaf_rn(l[j], down, t[j]);
                             l[j] *= f;
+                            low[j] *= f;
                         }
                         m[j] = top;
                     }
@@ -406,7 +401,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
                                 ls[a] += e;
                                 ts[a] = __fmaf_rn(e, s2, ts[a]);
                             }
-                    l[j] += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+#pragma unroll
+                    for (int a = 0; a < 4; ++a) add_wide(l[j], low[j], ls[a]);
                     t[j] += (ts[0] + ts[1]) + (ts[2] + ts[3]);
                     if (BEST) {
 #pragma unroll
@@ -422,11 +418,17 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
         });
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        Stat a{m[j] > -INFINITY ? m[j] * cq[j] : -INFINITY, l[j], t[j]};
-        a = join(a, Stat{__shfl_xor(a.m, 32, 64), __shfl_xor(a.l, 32, 64), __shfl_xor(a.t, 32, 64)});
-        const float top = fmaxf(m[j], __shfl_xor(m[j], 32, 64));
+        Stat a{m[j], l[j], low[j], t[j]};
+        if (m[j] > -INFINITY) {
+            const float over = __fmaf_rn(m[j], cq[j], -(m[j] * cq[j])), up = __builtin_amdgcn_exp2f(-over); // (m's own term is 2^over)
+            a.t = up * __fmaf_rn(-over, l[j], t[j]);
+            a.l = 1.0f;
+            a.low = 0.0f;
+            add_wide(a.l, a.low, up * ((l[j] - __builtin_amdgcn_exp2f(over)) + low[j]));
+        }
+        a = join(a, across(a, 32), cq[j]);
         const int64_t q = q0 + acc_col(j);
-        if (lane < 32 && q < Q.rows) stats[(size_t)(place.part * 2 + (wave >> 1)) * Q.rows + q] = make_float4(a.m, a.l, a.t, top);
+        if (lane < 32 && q < Q.rows) stats[(size_t)(place.part * 2 + (wave >> 1)) * Q.rows + q] = packed(a);
     }
 }
 
@@ -441,7 +443,7 @@ __device__ __forceinline__ uint32_t order_of(float v)
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
 
 // A workgroup a query: joins the statistics, scores the given rows and the best ones. Latency: the fewest steps that wait for
-// one another. stats.w is the largest product of a part.
+// one another.
 template <int PATH, class T, int NT>
 __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, float scale, int row_lanes,
                                                          const Largest *__restrict__ largest, const float *__restrict__ q_inv, const float4 *__restrict__ stats, int parts, const int32_t *__restrict__ ids, int given, float *__restrict__ logp_out,
@@ -463,22 +465,23 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
     const bool by_parts = parts >= 4 * k; // the parts' largest products are classes enough
     uint32_t mine_top = 0;
     stage_query(qs, q + (int64_t)row * ld_q, d, scale < 0.0f, NT);
-    // products in units of log 2, as the pass has them
-    float c2 = fabsf(scale) * 1.44269504088896341f;
+    // from products to logits, and to logits in units of log 2 as the pass has them
+    float c = fabsf(scale), c2 = fabsf(scale) * 1.44269504088896341f;
     Scoring how{row_lanes, 1.0f, 1.0f};
     if (PATH == kByTiles && sizeof(T) == 4) {
         how.x_scale = range_scale(largest->points);
         how.q_scale = 1.0f / q_inv[row];
+        c = c * q_inv[row] * (1.0f / how.x_scale);
         c2 = c2 * q_inv[row] * (1.0f / how.x_scale);
     }
-    Stat a{-INFINITY, 0.0f, 0.0f};
+    Stat a{-INFINITY, 0.0f, 0.0f, 0.0f};
     for (int p = tid; p < parts; p += NT) {
-        const float4 v = stats[(size_t)p * nq + row];
-        a = join(a, Stat{v.x, v.y, v.z});
-        if (by_parts) mine_top = max(mine_top, order_of(v.w));
+        const Stat v = unpacked(stats[(size_t)p * nq + row]);
+        a = join(a, v, c2);
+        if (by_parts) mine_top = max(mine_top, order_of(v.m));
     }
 #pragma unroll
-    for (int w = 1; w < 64; w <<= 1) a = join(a, Stat{__shfl_xor(a.m, w, 64), __shfl_xor(a.l, w, 64), __shfl_xor(a.t, w, 64)});
+    for (int w = 1; w < 64; w <<= 1) a = join(a, across(a, w), c2);
     if (lane == 0) wave_stat[wave] = a;
     if (tid == 0) { list_count = found_count = bound_shared = 0; least_best = ~0ull; }
 
@@ -515,15 +518,15 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
     }
     __syncthreads();
     a = wave_stat[0];
-    for (int w = 1; w < NT / 64; ++w) a = join(a, wave_stat[w]);
+    for (int w = 1; w < NT / 64; ++w) a = join(a, wave_stat[w], c2);
     constexpr float ln2 = 0.693147180559945309f;
-    const float log_l = logf(a.l), lse = __fmaf_rn(a.m, ln2, log_l);
+    const float log_l = log_wide(a.l, a.low), lse = __fmaf_rn(a.m, c, log_l);
     if (tid == 0) {
         lse_out[row] = lse;
         if (entropy_out) entropy_out[row] = log_l - ln2 * (a.t / a.l);
     }
     // s - lse from the parts that lse has, before it is rounded
-    auto logp_of = [&](float product) { return __fmaf_rn(__fmaf_rn(product, c2, -a.m), ln2, -log_l); };
+    auto logp_of = [&](float product) { return __fmaf_rn(product - a.m, c, -log_l); };
     constexpr int kAhead = sizeof(T) == 4 ? 4 : 8; // (what 128 registers hold: four waves a SIMD)
     const int at_once = scored_at_once<PATH>(how);
     for (int j0 = wave * at_once; j0 < given; j0 += NT / 64 * at_once) {

@@ -1,0 +1,48 @@
+"""Operators on rows of learned vectors at the ends of their ranges, against plain forms in 64 bits: answers that are nearly certain,
+logits in the hundreds, rows and queries of very unequal size or weight, masks of large, lowest and infinite values, parts of a table,
+and the largest counts. Tolerances as in test_gpu_rows: bounds of what fp32 sums and roundings can be off."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+avq = pytest.importorskip("paper_1908_10396_amd")
+
+from test_gpu_rows import TYPES, U, gen, normal, within  # noqa: E402
+
+
+def grid(x, kind):
+    """Multiples of 1/32 of at most 8 bits: products and sums of a few hundred of them are exact in every type's arithmetic."""
+    return ((x * 32.0).round().clamp(-127, 127) / 32.0).to(TYPES[kind])
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [1, 5, 90, 300])
+def test_log_probability_and_entropy_of_a_sure_answer(kind, nq):
+    """-log p = log(1 + r), r the sum of the other rows' e^(s_i - s): off by the exponents' roundings, relative to r, whatever the size
+    of r beside 1; only what a lane adds up together with the answer itself, within 32 rows, may be lost beside it."""
+    g = gen(nq)
+    n, d, scale = 300_001, 64, 0.5
+    x = grid(normal((n, d), g), kind)
+    ids = torch.randint(0, n, (nq,), generator=g, device="cuda", dtype=torch.int32)
+    q = grid(0.9 * x[ids.long()].float() + 0.2 * normal((nq, d), g), kind)
+    r = avq.log_probs(x, q, ids, 1, scale)
+    s = q.double() @ x.double().t() * scale
+    away = s - s.gather(1, ids.long()[:, None])
+    away.scatter_(1, ids.long()[:, None], -math.inf)
+    assert away.max() < -2.0
+    e = away.exp()
+    rest = e.sum(1)
+    far = torch.where(e > 0, away.abs(), 0.0)
+    mates = (ids.long()[:, None] // 32 * 32 + torch.arange(32, device="cuda")).clamp(max=n - 1)
+    lost = e.gather(1, mates).sum(1)
+    off = (e * (6 * U * far + 256 * U)).sum(1) + lost
+    want = -torch.log1p(rest)
+    assert want.median() > -0.01
+    within(r.logp, want, off, "logp")
+    assert torch.equal(r.alt_ids[:, 0], ids)
+    within(r.alt_logp[:, 0], want, off, "alt_logp")
+    h = torch.log1p(rest) + (e * far).sum(1) / (1 + rest)
+    within(r.entropy, h, off + (e * far * (6 * U * far + 256 * U)).sum(1) + lost * 1e-2, "entropy")
