@@ -85,10 +85,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
     part_tiles(tiles, parts, place.part, &first, &count);
     {
         const int64_t t = q0 + threadIdx.x;
-        const bool real = t < Q.rows; // (queries past the last: a logit of 0 and no gradient)
+        const bool real = t < Q.rows; // (queries past the last have the last one's products: a probability of 0 all the same)
         const float f = grad_factor(largest);
         const float2 c = real ? coef[t] : make_float2(0.0f, 0.0f);
-        ((float *)shift)[threadIdx.x] = real ? -lse[t] * 1.44269504088896341f : 0.0f;
+        ((float *)shift)[threadIdx.x] = real ? -lse[t] * 1.44269504088896341f : -INFINITY;
         ((float *)up)[threadIdx.x] = -c.x * f;
         if (ENTROPY) ((float *)up_h)[threadIdx.x] = -c.y * f * 0.693147180559945309f;
     }

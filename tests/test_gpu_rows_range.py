@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 avq = pytest.importorskip("paper_1908_10396_amd")
 
-from test_gpu_rows import TYPES, U, gen, normal, within  # noqa: E402
+from test_gpu_rows import TYPES, U, _grad_formula, gen, normal, within  # noqa: E402
 
 
 def grid(x, kind):
@@ -46,3 +46,26 @@ def test_log_probability_and_entropy_of_a_sure_answer(kind, nq):
     within(r.alt_logp[:, 0], want, off, "alt_logp")
     h = torch.log1p(rest) + (e * far).sum(1) / (1 + rest)
     within(r.entropy, h, off + (e * far * (6 * U * far + 256 * U)).sum(1) + lost * 1e-2, "entropy")
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [9, 33, 65, 257])
+@pytest.mark.parametrize("entropy", [False, True])
+def test_gradients_of_logits_in_the_hundreds(kind, nq, entropy):
+    """The last query's logits are the largest, up to some 400: what the tiles hold past it must not show."""
+    g = gen(nq)
+    n, d = 700, 100
+    x = normal((n, d), g, TYPES[kind])
+    ids = torch.randint(0, n, (nq,), generator=g, device="cuda", dtype=torch.int32)
+    q = normal((nq, d), g) + 1.5 * x[ids.long()].float()
+    q[-1] = 4.0 * x[11].float()
+    q = q.to(TYPES[kind])
+    up, up_h = normal((nq,), g), normal((nq,), g) if entropy else None
+    r = avq.log_probs(x, q, ids)
+    assert (q[-1].float() @ x[11].float()).item() > 200
+    want_q, bound_q, want_x, bound_x = _grad_formula(x, q, 1.0, ids, r.lse, r.entropy, up, up_h, None, kind)
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, r.entropy, up_h)
+    # (probabilities and entries of G below the normal range, 2^-126, may be taken as 0: that, and there |log p| < 90, for every summand)
+    flushed = 2.0 ** -126 * (1 + up.abs().max().item() + (0.0 if up_h is None else 90 * up_h.abs().max().item()))
+    within(dx, want_x, bound_x + flushed * (1 + q.double().abs()).sum(0), "dpoints")
+    within(dq, want_q, bound_q + flushed * (1 + x.double().abs()).sum(0), "dqueries")
