@@ -48,7 +48,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
     __shared__ uint32_t map[kMapWords];
     __shared__ int32_t given_id[kFewGiven];
     __shared__ float given_g[kFewGiven];
-    __shared__ float coef[NQ][3]; // a, h and lse / log 2
+    __shared__ float coef[NQ][3]; // a, h and lse
     const int d = p.d, units = units_of<T>(d), wave = threadIdx.x >> 6, lane = threadIdx.x & 63, in_row = lane % L;
     const T *x = (const T *)p.x, *q = (const T *)p.q;
     T *dx = (T *)p.dx;
@@ -82,12 +82,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
     }
     __syncthreads();
 
-    float qs[NQ][NV * V], acc[NQ][NV * V], a[NQ], h2[NQ], lse2[NQ];
+    float qs[NQ][NV * V], acc[NQ][NV * V], a[NQ], h[NQ], lse[NQ];
 #pragma unroll
     for (int t = 0; t < NQ; ++t) {
         a[t] = coef[t][0];
-        h2[t] = coef[t][1] * 0.693147180559945309f;
-        lse2[t] = coef[t][2] * 1.44269504088896341f;
+        h[t] = coef[t][1];
+        lse[t] = coef[t][2];
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
             }
     }
     float z_low = 0.0f, z_high = 0.0f; // of query in_row
-    const float c2 = p.scale * 1.44269504088896341f;
+    constexpr float log2e = 1.44269504088896341f;
     for (int64_t base = ((int64_t)blockIdx.x * kFewWaves + wave) * (kPer * U); base < p.n; base += (int64_t)gridDim.x * kFewWaves * (kPer * U)) {
         Unit<T> v[U][NV];
         int64_t row[U];
@@ -153,8 +153,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
                         for (int i = 0; i < NQ; ++i) s[i] = i == t && lane / L == from / L ? product : s[i];
                         if (MEND && lane == 0) {
                             const int32_t id = (int32_t)(base + u * kPer + from / L);
-                            const float s2 = __fmaf_rn(product, c2, -(coef[t][2] * 1.44269504088896341f)), w = __builtin_amdgcn_exp2f(s2), h = coef[t][1];
-                            float share = w == 0.0f ? 0.0f : w * (__fmaf_rn(h * 0.693147180559945309f, s2, coef[t][0]) + h);
+                            const float logp = __fmaf_rn(product, p.scale, -coef[t][2]), w = __builtin_amdgcn_exp2f(logp * log2e), h = coef[t][1];
+                            float share = w == 0.0f ? 0.0f : w * (__fmaf_rn(h, logp, coef[t][0]) + h);
                             for (int j = 0; j < p.given; ++j)
                                 if (given_id[t * p.given + j] == id) {
                                     p.shares[t * p.given + j] = share;
@@ -166,8 +166,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
             float o[NV * V] = {};
 #pragma unroll
             for (int t = 0; t < NQ; ++t) {
-                const float s2 = __fmaf_rn(s[t], c2, -lse2[t]), w = __builtin_amdgcn_exp2f(s2);
-                float G = more[t] - (w == 0.0f ? 0.0f : w * __fmaf_rn(h2[t], s2, a[t])); // (p log p)
+                const float logp = __fmaf_rn(s[t], p.scale, -lse[t]), w = __builtin_amdgcn_exp2f(logp * log2e); // (one rounding of s - lse: only lse's own is in p)
+                float G = more[t] - (w == 0.0f ? 0.0f : w * __fmaf_rn(h[t], logp, a[t])); // (p log p)
                 if (!real) G = 0.0f;
                 if (MEND) {
                     const float mine = real && in_row == t ? w : 0.0f;
@@ -235,7 +235,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
     }
 }
 
-// delta of each query, a workgroup each. More than rounding is not mended: such an lse is of more rows than these (a part of a table).
+// delta of each query, a workgroup each. More than lse's rounding (2^-24 of it) and that of the sums (2^-20) is not mended: such an lse
+// is of more rows than these (a part of a table). What other rows may have that little in is then lost to 1 - p, as it is to lse.
 __global__ __launch_bounds__(kFewGroups) void grad_few_delta_kernel(const float2 *__restrict__ z, int groups, int held, const float *__restrict__ lse, float *__restrict__ delta)
 {
     __shared__ double all[kFewGroups];
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(kFewGroups) void grad_few_delta_kernel(const float2
         if (i < m) all[i] += all[i + m];
     }
     const float v1 = (float)(all[0] - 1.0);
-    if (i == 0) delta[t] = fabsf(v1) <= 1e-5f * (1.0f + fabsf(lse[t])) ? v1 : 0.0f;
+    if (i == 0) delta[t] = fabsf(v1) <= 0x1p-24f * fabsf(lse[t]) + 0x1p-20f ? v1 : 0.0f;
 }
 
 // dq = the workgroups' sums and, in fp32, what the given rows' G gets back: 64 columns a workgroup, sixteen strips of workgroups, and of

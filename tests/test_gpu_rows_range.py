@@ -69,3 +69,31 @@ def test_gradients_of_logits_in_the_hundreds(kind, nq, entropy):
     flushed = 2.0 ** -126 * (1 + up.abs().max().item() + (0.0 if up_h is None else 90 * up_h.abs().max().item()))
     within(dx, want_x, bound_x + flushed * (1 + q.double().abs()).sum(0), "dpoints")
     within(dq, want_q, bound_q + flushed * (1 + x.double().abs()).sum(0), "dqueries")
+
+
+@pytest.mark.parametrize("nq", [1, 2, 4, 7])
+@pytest.mark.parametrize("other", [2e-5, 5e-5, 1e-3])
+def test_gradient_of_a_part_of_a_table_whose_other_part_is_unlikely(nq, other):
+    """lse of a whole table, of which these rows lack a probability `other`: G of the given row is g (1 - p), p that of the whole
+    table, to what lse's rounding (2^-24 of it, of these rows' and of the whole's) and some roundings of 1 leave."""
+    g = gen(nq)
+    n, d = 4000, 250
+    x = normal((n, d), g)
+    ids = torch.randperm(n, generator=g, device="cuda")[:nq].to(torch.int32)
+    q = 0.25 * normal((nq, d), g) + 0.9 * x[ids.long()]
+    scale = 25.0 / d
+    up = torch.full((nq,), -1.0 / nq, device="cuda")
+    s = q.double() @ x.double().t() * torch.tensor(scale, dtype=torch.float32).item()
+    r = avq.log_probs(x, q, ids, scale=scale)  # (these rows' lse has the products' own errors, which are no part of 1 - p)
+    whole = r.lse.double() - math.log1p(-other)
+    dq, dx = avq.log_probs_grad(x, q, ids, whole.float(), up, scale=scale)
+    at = torch.arange(nq, device="cuda"), ids.long()
+    p = torch.softmax(s, 1) * (1 - other)
+    given = up.double() * (1 - p[at])
+    off = up.double().abs() * (2 * U * whole.abs() + 32 * U)
+    # the given rows' gradient along their query: G of that row times |q|^2, and the other queries' small shares
+    G = -p * up.double()[:, None]
+    G[at] = given
+    want = (G.t() @ q.double() * scale)[ids.long()]
+    bound = off[:, None] * q.double().abs() * scale + 1e-4 * (G.abs().t() @ q.double().abs() * scale)[ids.long()]
+    within(dx[ids.long()], want, bound, "dpoints of the given rows")
