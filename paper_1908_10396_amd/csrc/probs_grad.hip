@@ -141,26 +141,17 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
         });
 }
 
-// The entries of the given ids among the part's rows, a wave each; the first of a query's equal ids has the sum of their g. Their
-// logits as the pass formed them that lse is of.
+// The entries of the given ids among the part's rows, a wave each (with more ids than a launch has workgroups, one after the other); the
+// first of a query's equal ids has the sum of their g. Their logits as the pass formed them that lse is of.
+constexpr int64_t kGivenGroups = 1 << 22; // a launch has fewer than 2^32 threads
+
 template <int PATH, class T>
 __global__ __launch_bounds__(64) void grad_given_kernel(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, int d, float scale, int row_lanes,
                                                         const int32_t *__restrict__ ids, int given, const float *__restrict__ g, const float *__restrict__ lse,
                                                         const float2 *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, Rows16 G)
 {
     extern __shared__ char lds[];
-    const int64_t i = blockIdx.x, t = i / given, j = i - t * given;
-    const int64_t id = ids[i];
-    if (id < lo || id >= lo + rows) return;
-    float sum = 0.0f;
-    for (int64_t o = 0; o < given; ++o)
-        if (ids[t * given + o] == id) {
-            if (o < j) return;
-            sum += g[t * given + o];
-        }
     T *qs = (T *)lds;
-    stage_query(qs, q + t * ld_q, d, false, 64);
-    __syncthreads();
     float c = scale;
     Scoring how{row_lanes, 1.0f, 1.0f};
     if (PATH == kByTiles && sizeof(T) == 4) {
@@ -168,19 +159,36 @@ __global__ __launch_bounds__(64) void grad_given_kernel(const T *__restrict__ x,
         how.q_scale = range_scale(largest->queries);
         c = c * (1.0f / how.q_scale) * (1.0f / how.x_scale);
     }
-    score_rows<PATH, 8>(qs, d, how, [&](int) { return x + id * ld_x; }, [&](int slot, float product) {
-        if (slot != 0) return;
-        const float logp = __fmaf_rn(product, c, -lse[t]);
-        const float2 k = coef[t];
-        const float p = __builtin_amdgcn_exp2f(logp * 1.44269504088896341f);
-        f32x8 one = {};
-        one[0] = (sum - (p > 0.0f || p != p ? p * __fmaf_rn(k.y, logp, k.x) : 0.0f)) * grad_factor(largest);
-        Quad hi, low{};
-        put16(one, &hi, &low, T{});
-        uint16_t *to = (uint16_t *)G.p + block16<sizeof(T) == 4>(t) * G.block + (id - lo) * G.row + turned16((int)t & 15);
-        *to = (uint16_t)hi.w[0];
-        if (sizeof(T) == 4) to[G.block] = (uint16_t)low.w[0];
-    });
+    for (int64_t i = blockIdx.x; i < (int64_t)nq * given; i += gridDim.x) {
+        const int64_t t = i / given, j = i - t * given;
+        const int64_t id = ids[i];
+        if (id < lo || id >= lo + rows) continue;
+        float sum = 0.0f;
+        bool earlier = false;
+        for (int64_t o = threadIdx.x; o < given; o += 64)
+            if (ids[t * given + o] == id) {
+                earlier = earlier || o < j;
+                sum += g[t * given + o];
+            }
+        if (__any(earlier)) continue;
+        sum = group_sum<64>(sum);
+        __syncthreads(); // (the query before has been read)
+        stage_query(qs, q + t * ld_q, d, false, 64);
+        __syncthreads();
+        score_rows<PATH, 8>(qs, d, how, [&](int) { return x + id * ld_x; }, [&](int slot, float product) {
+            if (slot != 0) return;
+            const float logp = __fmaf_rn(product, c, -lse[t]);
+            const float2 k = coef[t];
+            const float p = __builtin_amdgcn_exp2f(logp * 1.44269504088896341f);
+            f32x8 one = {};
+            one[0] = (sum - (p > 0.0f || p != p ? p * __fmaf_rn(k.y, logp, k.x) : 0.0f)) * grad_factor(largest);
+            Quad hi, low{};
+            put16(one, &hi, &low, T{});
+            uint16_t *to = (uint16_t *)G.p + block16<sizeof(T) == 4>(t) * G.block + (id - lo) * G.row + turned16((int)t & 15);
+            *to = (uint16_t)hi.w[0];
+            if (sizeof(T) == 4) to[G.block] = (uint16_t)low.w[0];
+        });
+    }
 }
 
 // fn for every four rows side by side of a lane's accumulators acc[a][j][4 b ..]. One after the other: the compiler would
@@ -291,13 +299,14 @@ template <class T>
 __global__ __launch_bounds__(256) void grad_join_kernel(const float *__restrict__ sums, int splits, int nq, int d, float scale, int fp32, const Largest *__restrict__ largest,
                                                         T *__restrict__ out, int64_t ld)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)nq * d;
-    if (i >= all) return;
-    float s = 0.0f;
-#pragma unroll 8
-    for (int p = 0; p < splits; ++p) s += sums[p * all + i];
+    const int64_t all = (int64_t)nq * d;
     const float f = grad_bound(largest) * (1.0f / kGradTop) * scale * (fp32 ? 1.0f / range_scale(largest->points) : 1.0f);
-    out[(i / d) * ld + i % d] = from_f32<T>(s * f);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        float s = 0.0f;
+#pragma unroll 8
+        for (int p = 0; p < splits; ++p) s += sums[p * all + i];
+        out[(i / d) * ld + i % d] = from_f32<T>(s * f);
+    }
 }
 
 template <class T>
@@ -405,7 +414,7 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         AVQ_HIP(hipGetLastError());
         if (p.given > 0) {
             auto run = [&](auto kernel) {
-                kernel<<<dim3((unsigned)((int64_t)p.nq * p.given)), dim3(64), staged_query_bytes(p.d), st>>>((const T *)p.points, p.ld_points, q, p.nq, p.ld_queries, p.d, p.scale, row_lanes(sizeof(T), p.d),
+                kernel<<<dim3((unsigned)std::min((int64_t)p.nq * p.given, kGivenGroups)), dim3(64), staged_query_bytes(p.d), st>>>((const T *)p.points, p.ld_points, q, p.nq, p.ld_queries, p.d, p.scale, row_lanes(sizeof(T), p.d),
                                                                                                     p.ids, p.given, p.grad_logp, p.lse, s.coef, s.largest, lo, rows, G);
             };
             const int path = prob_path(sizeof(T), p.d, p.nq);
@@ -438,7 +447,7 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         }
     }
     if (p.dqueries) {
-        grad_join_kernel<T><<<dim3((unsigned)(((int64_t)p.nq * p.d + 255) / 256)), dim3(256), 0, st>>>(s.sums, s.splits, p.nq, p.d, p.scale, SPLIT, s.largest, (T *)p.dqueries,
+        grad_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(((int64_t)p.nq * p.d + 255) / 256, 1 << 22)), dim3(256), 0, st>>>(s.sums, s.splits, p.nq, p.d, p.scale, SPLIT, s.largest, (T *)p.dqueries,
                                                                                                    p.ld_dqueries);
         AVQ_HIP(hipGetLastError());
     }

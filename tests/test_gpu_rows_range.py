@@ -97,3 +97,25 @@ def test_gradient_of_a_part_of_a_table_whose_other_part_is_unlikely(nq, other):
     want = (G.t() @ q.double() * scale)[ids.long()]
     bound = off[:, None] * q.double().abs() * scale + 1e-4 * (G.abs().t() @ q.double().abs() * scale)[ids.long()]
     within(dx[ids.long()], want, bound, "dpoints of the given rows")
+
+
+def test_gradient_of_as_many_given_ids_as_there_can_be_threads():
+    g = gen(1)
+    n, d, nq, m = 64, 8, 1 << 16, 1 << 10
+    x, q = normal((n, d), g), normal((nq, d), g)
+    ids = torch.full((nq, m), -1, dtype=torch.int32, device="cuda")
+    ids[:, 5], ids[:, m - 1] = 3, 9
+    ids[7, ::2] = 3
+    up = torch.zeros((nq, m), device="cuda")
+    up[:, 5], up[:, m - 1] = 0.5, -1.0
+    up[7, ::2] = 2.0 ** -9
+    up[7, 5] = 0.0
+    ids[7, 5] = -1
+    r = avq.log_probs(x, q, scale=0.3)
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, scale=0.3)
+    two = torch.tensor([[3, 9]], dtype=torch.int32, device="cuda").expand(nq, 2).contiguous()
+    up2 = torch.tensor([[0.5, -1.0]], device="cuda").expand(nq, 2).contiguous()
+    up2[7, 0] = 1.0
+    want_q, bound_q, want_x, bound_x = _grad_formula(x, q, 0.3, two, r.lse, None, up2, None, None, "f32")
+    within(dq, want_q, bound_q, "dqueries")
+    within(dx, want_x, bound_x, "dpoints")
