@@ -14,14 +14,15 @@ namespace avq {
 // ---- lookup ------------------------------------------------------------------------------
 
 constexpr int kLookThreads = 256, kLookEach = 4;
+constexpr int64_t kLookGroups = 1 << 23; // a launch has fewer than 2^32 threads
 
 template <class T, bool RAGGED>
 __global__ __launch_bounds__(kLookThreads) void embed_kernel(const T *__restrict__ table, int64_t n, int d, int64_t ld_table, const int32_t *__restrict__ ids, int64_t count,
-                                                             int per_row, uint32_t magic, float scale, T *__restrict__ out, int64_t ld_out)
+                                                             int per_row, uint32_t magic, float scale, T *__restrict__ out, int64_t ld_out, int64_t group0)
 {
     // the rows' units as one long list: a workgroup takes 1,024 of them, four loads a thread in flight (padding's from row 0)
     constexpr int V = kUnit<T>;
-    const int64_t first = (int64_t)blockIdx.x * (kLookThreads * kLookEach);
+    const int64_t first = (group0 + blockIdx.x) * (kLookThreads * kLookEach);
     const int64_t row0 = first / per_row;
     const uint32_t rem0 = (uint32_t)(first - row0 * per_row);
     Unit<T> v[kLookEach];
@@ -58,9 +59,11 @@ static int embed_run(const EmbedParams &p, hipStream_t st)
 {
     const int per_row = units_of<T>(p.d);
     const int64_t groups = (p.count * per_row + kLookThreads * kLookEach - 1) / (kLookThreads * kLookEach);
-    embed_kernel<T, RAGGED><<<dim3((unsigned)groups), dim3(kLookThreads), 0, st>>>((const T *)p.table, p.n, p.d, p.ld_table, p.ids, p.count, per_row, magic_of(per_row), p.scale,
-                                                                                  (T *)p.out, p.ld_out);
-    AVQ_HIP(hipGetLastError());
+    for (int64_t g = 0; g < groups; g += kLookGroups) {
+        embed_kernel<T, RAGGED><<<dim3((unsigned)std::min(groups - g, kLookGroups)), dim3(kLookThreads), 0, st>>>((const T *)p.table, p.n, p.d, p.ld_table, p.ids, p.count, per_row,
+                                                                                                              magic_of(per_row), p.scale, (T *)p.out, p.ld_out, g);
+        AVQ_HIP(hipGetLastError());
+    }
     return AVQ_OK;
 }
 
@@ -399,6 +402,7 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
 // The runs that cross chunks: each by the workgroup that has the chunk which it begins in. Teams of `lanes` threads add up a share
 // of the chunks each, in order, and then the shares in order.
 constexpr int kJoinThreads = 512;
+constexpr int64_t kJoinGroups = 1 << 22; // a launch has fewer than 2^32 threads: with more chunks, a workgroup has several
 
 template <class T, bool RAGGED>
 __global__ __launch_bounds__(kJoinThreads) void run_joins_kernel(const uint32_t *__restrict__ keys, uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out,
@@ -408,53 +412,54 @@ __global__ __launch_bounds__(kJoinThreads) void run_joins_kernel(const uint32_t 
     __shared__ float shares[kJoinThreads * V];
     const uint32_t chunks = (count + kRunChunk - 1) / kRunChunk, per_row = (uint32_t)units_of<T>(d), dp = per_row * V;
     const uint32_t teams = kJoinThreads / (uint32_t)lanes, team = threadIdx.x / (uint32_t)lanes, lane = threadIdx.x % (uint32_t)lanes;
-    const uint32_t chunk = blockIdx.x;
-    const uint32_t begin = chunk * (uint32_t)kRunChunk, end = begin + (uint32_t)kRunChunk;
-    if (end >= count) return; // the last chunk's runs end in it
-    const uint32_t key = keys[end - 1];
-    if (key >= n || keys[end] != key) return;
-    if (keys[begin] == key && begin > 0 && keys[begin - 1] == key) return; // it began earlier
-    // the chunks that the run goes on in: those whose first entry has the key
-    uint32_t lo = chunk + 1, hi = min(chunks, lo + 1); // the first chunk of another key lies in (lo, hi]
-    while (hi < chunks && keys[hi * (uint32_t)kRunChunk] == key) {
-        const uint32_t step = 2 * (hi - chunk);
-        lo = hi;
-        hi = min(chunks, chunk + step);
-    }
-    while (lo + 1 < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        if (keys[mid * (uint32_t)kRunChunk] == key) lo = mid; else hi = mid;
-    }
-    const uint32_t more = lo - chunk; // chunk + 1 .. lo
-    const uint32_t used = min(teams, (more + 3) / 4); // (four chunks a team at least)
-    for (uint32_t c0 = 0; c0 < per_row; c0 += (uint32_t)lanes) {
-        const uint32_t col = c0 + lane;
-        if (team < used && col < per_row) {
-            float acc[V];
+    for (uint32_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+        const uint32_t begin = chunk * (uint32_t)kRunChunk, end = begin + (uint32_t)kRunChunk;
+        if (end >= count) break; // the last chunk's runs end in it
+        const uint32_t key = keys[end - 1];
+        if (key >= n || keys[end] != key) continue;
+        if (keys[begin] == key && begin > 0 && keys[begin - 1] == key) continue; // it began earlier
+        // the chunks that the run goes on in: those whose first entry has the key
+        uint32_t lo = chunk + 1, hi = min(chunks, lo + 1); // the first chunk of another key lies in (lo, hi]
+        while (hi < chunks && keys[hi * (uint32_t)kRunChunk] == key) {
+            const uint32_t step = 2 * (hi - chunk);
+            lo = hi;
+            hi = min(chunks, chunk + step);
+        }
+        while (lo + 1 < hi) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            if (keys[mid * (uint32_t)kRunChunk] == key) lo = mid; else hi = mid;
+        }
+        const uint32_t more = lo - chunk; // chunk + 1 .. lo
+        const uint32_t used = min(teams, (more + 3) / 4); // (four chunks a team at least)
+        for (uint32_t c0 = 0; c0 < per_row; c0 += (uint32_t)lanes) {
+            const uint32_t col = c0 + lane;
+            if (team < used && col < per_row) {
+                float acc[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) acc[e] = team == 0 ? partial[((size_t)chunk * 2 + 1) * dp + (size_t)col * V + e] : 0.0f;
-            const uint32_t from = chunk + 1 + more * team / used, to = chunk + 1 + more * (team + 1) / used;
+                for (int e = 0; e < V; ++e) acc[e] = team == 0 ? partial[((size_t)chunk * 2 + 1) * dp + (size_t)col * V + e] : 0.0f;
+                const uint32_t from = chunk + 1 + more * team / used, to = chunk + 1 + more * (team + 1) / used;
 #pragma unroll 16
-            for (uint32_t c = from; c < to; ++c) {
-                Pack<float, V> v;
-                __builtin_memcpy(&v, partial + (size_t)c * 2 * dp + (size_t)col * V, sizeof(v));
+                for (uint32_t c = from; c < to; ++c) {
+                    Pack<float, V> v;
+                    __builtin_memcpy(&v, partial + (size_t)c * 2 * dp + (size_t)col * V, sizeof(v));
 #pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] += v.e[e];
+                    for (int e = 0; e < V; ++e) acc[e] += v.e[e];
+                }
+#pragma unroll
+                for (int e = 0; e < V; ++e) shares[(team * (uint32_t)lanes + lane) * V + e] = acc[e];
             }
+            __syncthreads();
+            if (team == 0 && col < per_row) {
+                float acc[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) shares[(team * (uint32_t)lanes + lane) * V + e] = acc[e];
+                for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+                for (uint32_t t = 0; t < used; ++t)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[e] += shares[(t * (uint32_t)lanes + lane) * V + e];
+                write_row<T, RAGGED>(out + (int64_t)key * ld_out, (int)col * V, d, acc, scale, accumulate != 0);
+            }
+            __syncthreads();
         }
-        __syncthreads();
-        if (team == 0 && col < per_row) {
-            float acc[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) acc[e] = 0.0f;
-            for (uint32_t t = 0; t < used; ++t)
-#pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] += shares[(t * (uint32_t)lanes + lane) * V + e];
-            write_row<T, RAGGED>(out + (int64_t)key * ld_out, (int)col * V, d, acc, scale, accumulate != 0);
-        }
-        __syncthreads();
     }
 }
 
@@ -547,7 +552,7 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
                                                                                                   p.accumulate, s.partial);
     AVQ_HIP(hipGetLastError());
     if (chunks > 1) {
-        run_joins_kernel<T, RAGGED><<<dim3((unsigned)chunks), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
+        run_joins_kernel<T, RAGGED><<<dim3((unsigned)std::min(chunks, kJoinGroups)), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
         AVQ_HIP(hipGetLastError());
     }
     return AVQ_OK;

@@ -119,3 +119,13 @@ def test_gradient_of_as_many_given_ids_as_there_can_be_threads():
     want_q, bound_q, want_x, bound_x = _grad_formula(x, q, 0.3, two, r.lse, None, up2, None, None, "f32")
     within(dq, want_q, bound_q, "dqueries")
     within(dx, want_x, bound_x, "dpoints")
+
+
+def test_gradient_of_as_many_rows_as_can_be_looked_up():
+    g = gen(2)
+    count, n = 1 << 28, 1000
+    ids = torch.randint(-1, n, (count,), generator=g, device="cuda", dtype=torch.int32)
+    grad = torch.ones((count, 1), device="cuda")
+    got = avq.embed_grad(grad, ids, n)
+    want = torch.bincount((ids + 1).long(), minlength=n + 1)[1:]
+    assert torch.equal(got[:, 0].double(), want.double())  # (whole numbers below 2^24: every sum is exact)
