@@ -336,7 +336,10 @@ __global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restri
 
 // Statistics of 128 queries over a part of the rows, 256 rows at a time; a lane has two queries, 64 of a tile's rows of each.
 // X: the launch's rows, Q: all queries, negated where the scale is. A lane's sums are relative to fl(m c2), one operation a logit instead
-// of two; at the end they are made relative to m itself, whose own term is known to the bit.
+// of two; at the end they are made relative to m itself, whose own term is known to the bit. Beyond kTame fl's rounding would be an
+// exponent of its own: there differences are taken first.
+constexpr float kTame = 0x1p18f;
+
 template <class H, bool SPLIT, bool BEST>
 __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Rows16 Q, int steps, float c2, const Largest *__restrict__ largest, const float *__restrict__ q_inv, int parts,
                                                                     int others, float4 *__restrict__ stats, float *__restrict__ gmax, int64_t gstride)
@@ -382,25 +385,33 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
                     const float top = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
                     if (top > m[j]) {
                         if (m[j] > -INFINITY) {
-                            const float down = m[j] * cq[j] - top * cq[j], f = __builtin_amdgcn_exp2f(down);
+                            const float from = m[j] * cq[j], to = top * cq[j];
+                            const float down = fmaxf(fabsf(from), fabsf(to)) <= kTame ? from - to : (m[j] - top) * cq[j], f = __builtin_amdgcn_exp2f(down);
                             t[j] = f * __fmaf_rn(l[j], down, t[j]);
                             l[j] *= f;
                             low[j] *= f;
                         }
                         m[j] = top;
                     }
-                    const float shift = m[j] > -INFINITY ? -(m[j] * cq[j]) : 0.0f;
+                    const float base = m[j] > -INFINITY ? m[j] : 0.0f, shift = -(base * cq[j]);
+                    const bool tame = fabsf(shift) <= kTame;
                     // four sums side by side, then one
                     float ls[4] = {}, ts[4] = {};
+                    auto sums = [&](auto any_size) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int a = 0; a < 4; ++a)
+                        for (int a = 0; a < 4; ++a)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (!TAIL || acc_row(a, r) < valid) {
-                                const float s2 = __fmaf_rn(acc[a][j][r], cq[j], shift), e = __builtin_amdgcn_exp2f(s2);
-                                ls[a] += e;
-                                ts[a] = __fmaf_rn(e, s2, ts[a]);
-                            }
+                            for (int r = 0; r < 16; ++r)
+                                if (!TAIL || acc_row(a, r) < valid) {
+                                    float s2 = __fmaf_rn(acc[a][j][r], cq[j], shift);
+                                    if (decltype(any_size)::value) s2 = tame ? s2 : (acc[a][j][r] - base) * cq[j];
+                                    const float e = __builtin_amdgcn_exp2f(s2);
+                                    ls[a] += e;
+                                    ts[a] = __fmaf_rn(e, s2, ts[a]);
+                                }
+                    };
+                    if (TAIL || __any(!tame)) sums(std::true_type{});
+                    else sums(std::false_type{});
 #pragma unroll
                     for (int a = 0; a < 4; ++a) add_wide(l[j], low[j], ls[a]);
                     t[j] += (ts[0] + ts[1]) + (ts[2] + ts[3]);
@@ -420,7 +431,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
     for (int j = 0; j < 2; ++j) {
         Stat a{m[j], l[j], low[j], t[j]};
         if (m[j] > -INFINITY) {
-            const float over = __fmaf_rn(m[j], cq[j], -(m[j] * cq[j])), up = __builtin_amdgcn_exp2f(-over); // (m's own term is 2^over)
+            const float s = m[j] * cq[j], over = fabsf(s) <= kTame ? __fmaf_rn(m[j], cq[j], -s) : 0.0f, up = __builtin_amdgcn_exp2f(-over); // (m's own term is 2^over)
             a.t = up * __fmaf_rn(-over, l[j], t[j]);
             a.l = 1.0f;
             a.low = 0.0f;
