@@ -1,10 +1,11 @@
 // Tiles of matrix products on the 16-bit matrix instructions (32 x 32 x 16), for operands laid out by rows_pack.hip or
 // used as they are.
 //
-// fp32 operands (SPLIT) are two f16 values each: v = (hi + lo) / s with s a power of two that brings the largest magnitude to
-// 2^14 .. 2^15, hi = f16(v s), lo = f16(v s - hi). hi hi' + hi lo' + lo hi' differs from v v' s s' by less than 1.5 * 2^-23 of it (values
-// down to 2^-28 of the largest; below, by 2^-40 of the largest), which is what an fp32 product and its sum lose anyway, at a third
-// of the 16-bit rate: five times the fp32 matrix instruction's. A row holds 16 hi, then their 16 lo, and so on.
+// fp32 operands (SPLIT) are two f16 values each: v = (hi + lo) / s with s a power of two that brings the largest magnitude (of a row, or
+// of all rows) to 2^14 .. 2^15, hi = f16(v s), lo = f16(v s - hi). hi hi' + hi lo' + lo hi' differs from v v' s s' by at most 2^-21 of it
+// (lo lo', and the rounding of either lo) where v and v' are 2^-17 of their largest or more; below, lo is a multiple of 2^-24, and v has an
+// error of 2^-40 of the largest. Sums of fp32 products lose as much, at a third of the 16-bit rate: five times the fp32
+// matrix instruction's. A row holds 16 hi, then their 16 lo, and so on.
 //
 // A workgroup of four waves forms 256 x 128 values, a wave 128 x 64 (4 x 2 matrix instructions, 128 accumulators), over steps
 // of 32 of the inner dimension (SPLIT: 16, 24 matrix instructions rather than 16). A step's operands (24 KB, 64 bytes a row) come by
@@ -299,16 +300,28 @@ __device__ __forceinline__ float range_scale(uint32_t largest_bits)
     if (largest_bits == 0) return 1.0f;
     int e = (int)(largest_bits >> 23) - 127;
     e = 14 - e;
-    e = e > 100 ? 100 : e < -113 ? -113 : e;
+    e = e > 97 ? 97 : e < -113 ? -113 : e;
     return __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
+// Where rows have scales s of their own, what is kept is the inverse: kRowUnit / s for the table's rows, 1 / (kRowUnit s) for queries.
+// A sum of products of two rows times the table's inverse is then the product of the row with a query of magnitudes up to 1/2, which
+// stays in range for rows of any size; times the query's inverse it is the product itself. The kTileM rows of a tile have one scale
+// where their largest magnitudes lie within kTileSpread of one another (rows of nothing but zeros aside), so that a tile of ordinary rows
+// needs no factor a row: 8 % of a pass of 2,048 queries over 1,183,514 x 100.
+constexpr float kRowUnit = 0x1p-16f, kTileSpread = 0x1p8f;
+__device__ __forceinline__ float scale_of_inverse(float inv) { return kRowUnit / inv; }
+
 int launch_clear_largest(Largest *to, hipStream_t st);
+// inv[row] = kRowUnit / s of each row, and tile_inv[tile] that of the tile's rows where they have one, else 0
+int launch_row_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, float *tile_inv, hipStream_t st);
 // max over finite elements into *to
 int launch_largest(const float *x, int64_t rows, int d, int64_t ld, uint32_t *to, hipStream_t st);
 // Rows laid out as `to` says (to.p: where), `steps` steps of them, zeros past a row's end. fp32: pairs, scaled by
-// range_scale(*largest), or, largest == NULL, each row by its own, whose inverse goes to inv[row]. negate: with the other sign.
-int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, float *inv, bool negate, hipStream_t st);
+// range_scale(*largest), or, largest == NULL, each row by its own, of which inv[row] is the inverse. negate: with the other sign.
+int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, const float *inv, bool negate, hipStream_t st);
+// fp32 queries: pairs, each row by its own scale, whose inverse goes to inv[row].
+int launch_pack_queries(const float *q, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, float *inv, bool negate, hipStream_t st);
 // The transpose packed: row c < d of d holds x[t][c], 16 t in the order of turned16, zeros past the last t.
 int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, hipStream_t st);
 

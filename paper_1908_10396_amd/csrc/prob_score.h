@@ -100,16 +100,17 @@ __device__ __forceinline__ Frag checked(const Frag &f, const T *__restrict__ row
     return k < d ? load_frag<T, false>(row, k, d) : Frag{};
 }
 
-// What the pass of a query's statistics is described by. lanes: of a row (kByRow); x_scale, q_scale: of fp32 pairs (kByTiles).
-struct Scoring { int lanes; float x_scale, q_scale; };
+// What the pass of a query's statistics is described by. lanes: of a row (kByRow); q_scale: of the query's fp32 pairs (kByTiles).
+struct Scoring { int lanes; float q_scale; };
 
 // Rows that a wave scores at once.
 template <int PATH> __device__ __forceinline__ int scored_at_once(const Scoring &how) { return PATH == kByTiles ? 32 : PATH == kByStream ? 16 : 4 * (64 / how.lanes); }
 
-// row(i): the i-th of those rows (a valid one always); emit(i, product): once for each, on some lane.
+// row(i): the i-th of those rows (a valid one always); inverse(i): that of its scale (fp32 pairs); emit(i, product): once for each, on
+// some lane.
 // AHEAD: 16 coordinates' loads in flight (kByTiles), STEPS: steps' (kByStream).
-template <int PATH, int AHEAD, int STEPS = 16, class T, class RowOf, class Emit>
-__device__ __forceinline__ void score_rows(const T *__restrict__ qs, int d, const Scoring &how, RowOf row, Emit emit)
+template <int PATH, int AHEAD, int STEPS = 16, class T, class RowOf, class InverseOf, class Emit>
+__device__ __forceinline__ void score_rows(const T *__restrict__ qs, int d, const Scoring &how, RowOf row, InverseOf inverse, Emit emit)
 {
     constexpr int E = kFragElems<T>;
     const int lane = threadIdx.x & 63;
@@ -165,6 +166,7 @@ __device__ __forceinline__ void score_rows(const T *__restrict__ qs, int d, cons
         constexpr int NB = AHEAD, V = SPLIT ? 2 : 1; // loads of a lane's eight
         const int half = lane >> 5, whole = d / 16;
         const T *p = row(lane & 31);
+        const float inv = SPLIT ? inverse(lane & 31) : 1.0f, x_scale = SPLIT ? scale_of_inverse(inv) : 1.0f;
         f32x16 acc;
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
@@ -175,7 +177,7 @@ __device__ __forceinline__ void score_rows(const T *__restrict__ qs, int d, cons
                 uint16_t xh[8], xl[8], qh[8], ql[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    split_f16(xs[e] * how.x_scale, &xh[e], &xl[e]);
+                    split_f16(xs[e] * x_scale, &xh[e], &xl[e]);
                     split_f16(qs[k + e] * how.q_scale, &qh[e], &ql[e]);
                 }
                 Quad hi, lo, q_hi, q_lo;
@@ -208,10 +210,12 @@ __device__ __forceinline__ void score_rows(const T *__restrict__ qs, int d, cons
             for (int i = 0; i < V; ++i) v[i] = load_frag<T, false>(p, k + i * E, d);
             add(v, k);
         }
-        if ((lane & 31) == 0) {
+        // (every column is the same: of two lanes that loaded a row one has its product, at acc_row's place)
+        const int mine = lane & 31, at = (mine >> 3) * 4 + (mine & 3);
+        float product = acc[0];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) emit(8 * (r >> 2) + 4 * half + (r & 3), acc[r]);
-        }
+        for (int r = 1; r < 16; ++r) product = at == r ? acc[r] : product;
+        if ((mine >> 2 & 1) == half) emit(mine, SPLIT ? product * inv : product);
     }
 }
 

@@ -341,7 +341,7 @@ __global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restri
 constexpr float kTame = 0x1p18f;
 
 template <class H, bool SPLIT, bool BEST>
-__global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Rows16 Q, int steps, float c2, const Largest *__restrict__ largest, const float *__restrict__ q_inv, int parts,
+__global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Rows16 Q, int steps, float c2, const float *__restrict__ x_inv, const float *__restrict__ tile_inv, const float *__restrict__ q_inv, int parts,
                                                                     int others, float4 *__restrict__ stats, float *__restrict__ gmax, int64_t gstride)
 {
     extern __shared__ char lds[];
@@ -358,14 +358,31 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
         cq[j] = c2;
         if (SPLIT) {
             const int64_t q = min(q0 + acc_col(j), Q.rows - 1);
-            cq[j] = c2 * q_inv[q] * (1.0f / range_scale(largest->points));
+            cq[j] = c2 * q_inv[q];
         }
         m[j] = -INFINITY;
         l[j] = low[j] = t[j] = 0.0f;
     }
     typedef RowCopies<SPLIT, true> Copies;
-    run_tiles<H, SPLIT, BEST, Copies>(X, Q, steps, count, lds, [&](int i, Copies &c) { c.seek(X, (first + i) * kTileM, Q, q0); },
+    float ahead = SPLIT && count > 0 ? tile_inv[first] : 1.0f; // (asked for a tile before it is needed)
+    run_tiles<H, SPLIT, SPLIT || BEST, Copies>(X, Q, steps, count, lds, [&](int i, Copies &c) { c.seek(X, (first + i) * kTileM, Q, q0); },
         [&](int i, f32x16 (&acc)[4][2]) {
+            float unit = ahead; // of the products
+            if (SPLIT) ahead = tile_inv[first + (i + 1 < count ? i + 1 : i)];
+            if (SPLIT && unit == 0.0f) {
+                unit = 1.0f;
+                // (the last tile's rows past the end have a place too)
+                const float *inv = x_inv + (first + i) * kTileM + (wave >> 1) * 128 + 4 * (lane >> 5);
+#pragma unroll
+                for (int a = 0; a < 4; ++a)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const float4 v = *(const float4 *)(inv + a * 32 + b * 8);
+                        const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) { acc[a][0][4 * b + r] *= e[r]; acc[a][1][4 * b + r] *= e[r]; }
+                    }
+            }
             const int64_t row0 = (first + i) * kTileM;
             const bool whole = row0 + kTileM <= X.rows;
             const int valid = whole ? kTileM : (int)(X.rows - row0);
@@ -380,7 +397,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
 #pragma unroll
                         for (int r = 0; r < 16; ++r)
                             if (!TAIL || acc_row(a, r) < valid) g = fmaxf(g, acc[a][j][r]);
-                        group[a] = g;
+                        group[a] = SPLIT ? g * unit : g;
                     }
                     const float top = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
                     if (top > m[j]) {
@@ -395,6 +412,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
                     }
                     const float base = m[j] > -INFINITY ? m[j] : 0.0f, shift = -(base * cq[j]);
                     const bool tame = fabsf(shift) <= kTame;
+                    const float to_logit = SPLIT ? unit * cq[j] : cq[j];
                     // four sums side by side, then one
                     float ls[4] = {}, ts[4] = {};
                     auto sums = [&](auto any_size) __attribute__((always_inline)) {
@@ -403,8 +421,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
 #pragma unroll
                             for (int r = 0; r < 16; ++r)
                                 if (!TAIL || acc_row(a, r) < valid) {
-                                    float s2 = __fmaf_rn(acc[a][j][r], cq[j], shift);
-                                    if (decltype(any_size)::value) s2 = tame ? s2 : (acc[a][j][r] - base) * cq[j];
+                                    float s2 = __fmaf_rn(acc[a][j][r], to_logit, shift);
+                                    if (decltype(any_size)::value) s2 = tame ? s2 : (SPLIT ? __fmaf_rn(acc[a][j][r], unit, -base) : acc[a][j][r] - base) * cq[j];
                                     const float e = __builtin_amdgcn_exp2f(s2);
                                     ls[a] += e;
                                     ts[a] = __fmaf_rn(e, s2, ts[a]);
@@ -457,7 +475,7 @@ __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o
 // one another.
 template <int PATH, class T, int NT>
 __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, float scale, int row_lanes,
-                                                         const Largest *__restrict__ largest, const float *__restrict__ q_inv, const float4 *__restrict__ stats, int parts, const int32_t *__restrict__ ids, int given, float *__restrict__ logp_out,
+                                                         const float *__restrict__ x_inv, const float *__restrict__ q_inv, const float4 *__restrict__ stats, int parts, const int32_t *__restrict__ ids, int given, float *__restrict__ logp_out,
                                                          float *__restrict__ lse_out, float *__restrict__ entropy_out, const float *__restrict__ gmax, int64_t gstride, int k,
                                                          int32_t *__restrict__ alt_ids, float *__restrict__ alt_logp)
 {
@@ -478,12 +496,11 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
     stage_query(qs, q + (int64_t)row * ld_q, d, scale < 0.0f, NT);
     // from products to logits, and to logits in units of log 2 as the pass has them
     float c = fabsf(scale), c2 = fabsf(scale) * 1.44269504088896341f;
-    Scoring how{row_lanes, 1.0f, 1.0f};
+    Scoring how{row_lanes, 1.0f};
     if (PATH == kByTiles && sizeof(T) == 4) {
-        how.x_scale = range_scale(largest->points);
-        how.q_scale = 1.0f / q_inv[row];
-        c = c * q_inv[row] * (1.0f / how.x_scale);
-        c2 = c2 * q_inv[row] * (1.0f / how.x_scale);
+        how.q_scale = 1.0f / (kRowUnit * q_inv[row]);
+        c = c * q_inv[row];
+        c2 = c2 * q_inv[row];
     }
     Stat a{-INFINITY, 0.0f, 0.0f, 0.0f};
     for (int p = tid; p < parts; p += NT) {
@@ -543,7 +560,7 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
     for (int j0 = wave * at_once; j0 < given; j0 += NT / 64 * at_once) {
         const int32_t *mine = ids + (int64_t)row * given + j0;
         auto real = [&](int i) { return j0 + i < given && mine[i] >= 0 && (int64_t)mine[i] < n; };
-        score_rows<PATH, kAhead>(qs, d, how, [&](int i) { return x + (real(i) ? (int64_t)mine[i] * ld_x : 0); },
+        score_rows<PATH, kAhead>(qs, d, how, [&](int i) { return x + (real(i) ? (int64_t)mine[i] * ld_x : 0); }, [&](int i) { return x_inv[real(i) ? mine[i] : 0]; },
                          [&](int i, float product) { if (j0 + i < given) logp_out[(int64_t)row * given + j0 + i] = real(i) ? logp_of(product) : -INFINITY; });
     }
     if (k == 0) return;
@@ -593,7 +610,8 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
     const uint32_t chosen = min(min(list_count, listed), (uint32_t)k), rows = chosen * 32u;
     for (uint32_t i0 = wave * at_once; i0 < rows; i0 += NT / 64 * at_once) {
         auto id_of = [&](int i) { return (int64_t)groups[(i0 + i) / 32] * 32 + ((i0 + i) & 31); };
-        score_rows<PATH, kAhead>(qs, d, how, [&](int i) { return x + min(i0 + i < rows ? id_of(i) : 0, n - 1) * ld_x; },
+        auto row_of = [&](int i) { return min(i0 + i < rows ? id_of(i) : 0, n - 1); };
+        score_rows<PATH, kAhead>(qs, d, how, [&](int i) { return x + row_of(i) * ld_x; }, [&](int i) { return x_inv[row_of(i)]; },
                          [&](int i, float product) {
                              if (i0 + i >= rows) return;
                              const int64_t id = id_of(i);
@@ -675,7 +693,7 @@ struct ProbScratch {
     float4 *stats; float *gmax; int64_t gstride;
     int groups, qt, query_tiles;                         // stream
     bool pack; int steps, parts, launches; int64_t part; // tiles: steps of an inner product, rows a launch
-    uint16_t *x16, *q16; float *q_inv; Largest *largest;
+    uint16_t *x16, *q16; float *q_inv, *x_inv, *tile_inv;
     size_t bytes;
 };
 
@@ -710,7 +728,11 @@ static ProbScratch prob_scratch(const ProbParams &p, void *base)
         s.stats = (float4 *)take((size_t)s.launches * std::max(s.parts, parts_for((p.n + kTileM - 1) / kTileM, s.query_tiles, kTileGroups)) * 2 * p.nq * sizeof(float4));
         s.q16 = (uint16_t *)take(packed_bytes(p.nq, s.steps));
         s.q_inv = (float *)take((size_t)p.nq * sizeof(float));
-        s.largest = (Largest *)take(sizeof(Largest));
+        if (split) {
+            const size_t tiles = (size_t)(p.n + kTileM - 1) / kTileM;
+            s.x_inv = (float *)take(tiles * kTileM * sizeof(float));
+            s.tile_inv = (float *)take(tiles * sizeof(float));
+        }
         if (s.pack) s.x16 = (uint16_t *)take(packed_bytes(s.part, s.steps));
     }
     s.gmax = p.k > 0 ? (float *)take((size_t)s.gstride * p.nq * sizeof(float)) : nullptr;
@@ -776,10 +798,11 @@ static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
     const int size = type_bytes(p.type);
     const float c2 = fabsf(p.scale) * 1.44269504088896341f;
     const Rows16 Q = packed_rows(s.q16, p.nq);
-    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, Q, nullptr, s.q_inv, p.scale < 0.0f, st));
     if (SPLIT) {
-        AVQ_TRY(launch_clear_largest(s.largest, st));
-        AVQ_TRY(launch_largest((const float *)p.points, p.n, p.d, p.ld_points, &s.largest->points, st));
+        AVQ_TRY(launch_pack_queries((const float *)p.queries, p.nq, p.d, p.ld_queries, s.steps, Q, s.q_inv, p.scale < 0.0f, st));
+        AVQ_TRY(launch_row_inverses((const float *)p.points, p.n, p.d, p.ld_points, s.x_inv, s.tile_inv, st));
+    } else {
+        AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, Q, nullptr, nullptr, p.scale < 0.0f, st));
     }
     static LdsLimitOnce with_best, without;
     for (int i = 0; i < s.launches; ++i) {
@@ -788,17 +811,18 @@ static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
         Rows16 X{(const uint16_t *)from, p.ld_points, 16, rows};
         if (s.pack) {
             X = SPLIT ? packed_rows(s.x16, rows) : Rows16{s.x16, (int64_t)s.steps * 32, 16, rows};
-            AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, s.steps, X, SPLIT ? &s.largest->points : nullptr, nullptr, false, st));
+            AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, s.steps, X, nullptr, SPLIT ? s.x_inv + lo : nullptr, false, st));
         }
         float4 *stats = s.stats + (size_t)i * s.parts * 2 * p.nq;
+        const float *x_inv = SPLIT ? s.x_inv + lo : nullptr, *tile_inv = SPLIT ? s.tile_inv + lo / kTileM : nullptr;
         const dim3 grid((unsigned)(s.parts * s.query_tiles));
         if (p.k > 0) {
             AVQ_TRY(set_lds_limit((const void *)prob_tile_kernel<H, SPLIT, true>, kTileLds, &with_best));
-            prob_tile_kernel<H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, s.steps, c2, s.largest, s.q_inv, s.parts, s.query_tiles, stats,
+            prob_tile_kernel<H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, s.steps, c2, x_inv, tile_inv, s.q_inv, s.parts, s.query_tiles, stats,
                                                                                       s.gmax + lo / 32, s.gstride);
         } else {
             AVQ_TRY(set_lds_limit((const void *)prob_tile_kernel<H, SPLIT, false>, kTileLds, &without));
-            prob_tile_kernel<H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, s.steps, c2, s.largest, s.q_inv, s.parts, s.query_tiles, stats, nullptr, 0);
+            prob_tile_kernel<H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(X, Q, s.steps, c2, x_inv, tile_inv, s.q_inv, s.parts, s.query_tiles, stats, nullptr, 0);
         }
         AVQ_HIP(hipGetLastError());
     }
@@ -811,7 +835,7 @@ static int finish_run(const ProbParams &p, const ProbScratch &s, int parts, hipS
     static LdsLimitOnce once;
     AVQ_TRY(set_lds_limit((const void *)prob_finish_kernel<PATH, T, NT>, kFinishLds, &once));
     prob_finish_kernel<PATH, T, NT><<<dim3(p.nq), dim3(NT), finish_lds(p.d, p.k), st>>>(
-        (const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.nq, p.ld_queries, p.scale, row_lanes(sizeof(T), p.d), s.largest, s.q_inv, s.stats, parts, p.ids, p.given,
+        (const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.nq, p.ld_queries, p.scale, row_lanes(sizeof(T), p.d), s.x_inv, s.q_inv, s.stats, parts, p.ids, p.given,
         p.logp, p.lse, p.entropy, s.gmax, s.gstride, p.k, p.alt_ids, p.alt_logp);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;

@@ -153,11 +153,12 @@ __global__ __launch_bounds__(64) void grad_given_kernel(const T *__restrict__ x,
     extern __shared__ char lds[];
     T *qs = (T *)lds;
     float c = scale;
-    Scoring how{row_lanes, 1.0f, 1.0f};
+    Scoring how{row_lanes, 1.0f};
+    float x_inv = 1.0f;
     if (PATH == kByTiles && sizeof(T) == 4) {
-        how.x_scale = range_scale(largest->points);
+        x_inv = kRowUnit / range_scale(largest->points);
         how.q_scale = range_scale(largest->queries);
-        c = c * (1.0f / how.q_scale) * (1.0f / how.x_scale);
+        c = c * (1.0f / (kRowUnit * how.q_scale));
     }
     for (int64_t i = blockIdx.x; i < (int64_t)nq * given; i += gridDim.x) {
         const int64_t t = i / given, j = i - t * given;
@@ -175,7 +176,7 @@ __global__ __launch_bounds__(64) void grad_given_kernel(const T *__restrict__ x,
         __syncthreads(); // (the query before has been read)
         stage_query(qs, q + t * ld_q, d, false, 64);
         __syncthreads();
-        score_rows<PATH, 8>(qs, d, how, [&](int) { return x + id * ld_x; }, [&](int slot, float product) {
+        score_rows<PATH, 8>(qs, d, how, [&](int) { return x + id * ld_x; }, [&](int) { return x_inv; }, [&](int slot, float product) {
             if (slot != 0) return;
             const float logp = __fmaf_rn(product, c, -lse[t]);
             const float2 k = coef[t];

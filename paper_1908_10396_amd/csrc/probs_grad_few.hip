@@ -147,7 +147,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
                         const int from = __ffsll((unsigned long long)left) - 1; // the first lane of that row
                         const T *at = x + (base + u * kPer + from / L) * p.ld_x;
                         float product = 0.0f;
-                        score_rows<PATH, 8, 2>((const T *)lds + t * staged, d, Scoring{L, 1.0f, 1.0f}, [&](int) { return at; }, [&](int slot, float v) { if (slot == 0) product = v; });
+                        score_rows<PATH, 8, 2>((const T *)lds + t * staged, d, Scoring{L, 1.0f}, [&](int) { return at; }, [](int) { return 1.0f; }, [&](int slot, float v) { if (slot == 0) product = v; });
                         product = __shfl(product, 0, 64);
 #pragma unroll
                         for (int i = 0; i < NQ; ++i) s[i] = i == t && lane / L == from / L ? product : s[i];

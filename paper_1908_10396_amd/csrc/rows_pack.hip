@@ -68,21 +68,88 @@ int launch_largest(const float *x, int64_t rows, int d, int64_t ld, uint32_t *to
     return AVQ_OK;
 }
 
+// A row lies across L lanes, kInverseRows rows of them in flight. Bound by memory.
+constexpr int kInverseRows = 4;
+constexpr float kLeastInverse = kRowUnit * 0x1p-97f; // of rows too small for a scale, those of zeros among them
+
+template <bool RAGGED, int L>
+__global__ __launch_bounds__(256) void row_inverses_kernel(const float *__restrict__ x, int64_t rows, int d, int64_t ld, float *__restrict__ inv)
+{
+    constexpr int kPer = 64 / L, U = kInverseRows;
+    const int units = units_of<float>(d), wave = threadIdx.x >> 6, lane = threadIdx.x & 63, in_row = lane % L;
+    for (int64_t base = ((int64_t)blockIdx.x * 4 + wave) * (kPer * U); base < rows; base += (int64_t)gridDim.x * 4 * (kPer * U)) {
+        uint32_t m[U] = {};
+        for (int j = 0; j < units; j += L) {
+            Unit<float> v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = load_unit<float, RAGGED>(x + min(base + u * kPer + lane / L, rows - 1) * ld, min(j + in_row, units - 1) * kUnit<float>, d);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < kUnit<float>; ++e) m[u] = max(m[u], finite_bits(v[u].e[e]));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int w = 1; w < L; w <<= 1) m[u] = max(m[u], (uint32_t)__shfl_xor((int)m[u], w, 64));
+            const int64_t row = base + u * kPer + lane / L;
+            if (in_row == 0 && row < rows) inv[row] = m[u] == 0 ? kLeastInverse : kRowUnit / range_scale(m[u]);
+        }
+    }
+}
+
+// a tile's rows, a thread each
+__global__ __launch_bounds__(kTileM) void tile_inverses_kernel(float *__restrict__ inv, int64_t rows, float *__restrict__ tile_inv)
+{
+    __shared__ float top[kTileM / 64], least[kTileM / 64];
+    const int64_t row = (int64_t)blockIdx.x * kTileM + threadIdx.x;
+    const float mine = row < rows ? inv[row] : kLeastInverse;
+    float hi = mine, lo = mine == kLeastInverse ? INFINITY : mine;
+#pragma unroll
+    for (int w = 1; w < 64; w <<= 1) {
+        hi = fmaxf(hi, __shfl_xor(hi, w, 64));
+        lo = fminf(lo, __shfl_xor(lo, w, 64));
+    }
+    if ((threadIdx.x & 63) == 0) { top[threadIdx.x >> 6] = hi; least[threadIdx.x >> 6] = lo; }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kTileM / 64; ++w) { hi = fmaxf(hi, top[w]); lo = fminf(lo, least[w]); }
+    const bool one = hi <= lo * kTileSpread;
+    if (one && row < rows) inv[row] = hi;
+    if (threadIdx.x == 0) tile_inv[blockIdx.x] = one ? hi : 0.0f;
+}
+
+int launch_row_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, float *tile_inv, hipStream_t st)
+{
+    const bool whole = whole_units(x, ld, d, sizeof(float));
+    const int units = units_of<float>(d), lanes = units <= 16 ? 16 : units <= 32 ? 32 : 64;
+    const int64_t each = 4 * (64 / lanes) * kInverseRows;
+    auto run = [&](auto kernel) { kernel<<<dim3((unsigned)std::min<int64_t>(2048, (rows + each - 1) / each)), dim3(256), 0, st>>>(x, rows, d, ld, inv); };
+    if (lanes == 16) whole ? run(row_inverses_kernel<false, 16>) : run(row_inverses_kernel<true, 16>);
+    else if (lanes == 32) whole ? run(row_inverses_kernel<false, 32>) : run(row_inverses_kernel<true, 32>);
+    else whole ? run(row_inverses_kernel<false, 64>) : run(row_inverses_kernel<true, 64>);
+    AVQ_HIP(hipGetLastError());
+    tile_inverses_kernel<<<dim3((unsigned)((rows + kTileM - 1) / kTileM)), dim3(kTileM), 0, st>>>(inv, rows, tile_inv);
+    AVQ_HIP(hipGetLastError());
+    return AVQ_OK;
+}
+
 constexpr int kPackRows = 64, kPackColumns = 128;
 
 // 64 rows a workgroup, 128 columns at a time by way of LDS: rows are read along, and half a block of 16 elements is written by each
 // thread, so that threads side by side write the rows of a block, 2 KB. V: elements a load.
 template <class T, int V>
 __global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int blocks, Rows16 to_rows,
-                                                        const uint32_t *__restrict__ largest, uint16_t flip)
+                                                        const uint32_t *__restrict__ largest, const float *__restrict__ inv, uint16_t flip)
 {
     constexpr bool SPLIT = sizeof(T) == 4;
     constexpr int kLine = kPackColumns + 16 / sizeof(T); // (rows apart by 16 bytes more than a multiple of the banks)
     __shared__ __attribute__((aligned(16))) T tile[kPackRows * kLine];
     const int64_t row0 = (int64_t)blockIdx.x * kPackRows;
     const int here = (int)min(rows - row0, (int64_t)kPackRows);
+    const int r = threadIdx.x / 2 % kPackRows, u = threadIdx.x & 1;
     float scale = 1.0f;
-    if (SPLIT) scale = range_scale(*largest);
+    if (SPLIT) scale = largest ? range_scale(*largest) : scale_of_inverse(inv[min(row0 + r, rows - 1)]);
     for (int c0 = 0; c0 < blocks * 16; c0 += kPackColumns) {
         const int columns = min(d - c0, kPackColumns), per_row = max(columns, 0) / V;
         const uint32_t magic = magic_of(per_row);
@@ -92,7 +159,6 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x,
             *(Pack<T, V> *)(tile + r * kLine + c) = *(const Pack<T, V> *)(x + (row0 + r) * ld + c0 + c);
         }
         __syncthreads();
-        const int r = threadIdx.x / 2 % kPackRows, u = threadIdx.x & 1;
 #pragma unroll
         for (int b = threadIdx.x / (2 * kPackRows); b < kPackColumns / 16; b += 2) {
             const int c = b * 16 + u * 8;
@@ -134,27 +200,29 @@ __global__ __launch_bounds__(256) void pack_own_scale_kernel(const float *__rest
         uint16_t *to = (uint16_t *)to_rows.p + block16<true>(c) * to_rows.block + row * to_rows.row + (c & 15);
         split_f16(c < d ? x[row * ld + c] * (s * sign) : 0.0f, to, to + to_rows.block);
     }
-    if (threadIdx.x == 0) inv[row] = 1.0f / s;
+    if (threadIdx.x == 0) inv[row] = 1.0f / (kRowUnit * s);
 }
 
-int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, float *inv, bool negate, hipStream_t st)
+int launch_pack_queries(const float *q, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, float *inv, bool negate, hipStream_t st)
 {
-    if (type == AVQ_F32 && !largest) {
-        pack_own_scale_kernel<<<dim3((unsigned)rows), dim3(256), 0, st>>>((const float *)x, d, ld, steps, to, inv, negate ? -1.0f : 1.0f);
-        AVQ_HIP(hipGetLastError());
-        return AVQ_OK;
-    }
+    pack_own_scale_kernel<<<dim3((unsigned)rows), dim3(256), 0, st>>>(q, d, ld, steps, to, inv, negate ? -1.0f : 1.0f);
+    AVQ_HIP(hipGetLastError());
+    return AVQ_OK;
+}
+
+int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, const float *inv, bool negate, hipStream_t st)
+{
     const dim3 grid((unsigned)((rows + kPackRows - 1) / kPackRows));
     const int size = type_bytes(type), w = row_width(x, ld, d, size);
     const uint16_t flip = negate ? 0x8000 : 0;
     const int blocks = type == AVQ_F32 ? steps : 2 * steps; // of 16 coordinates
     if (type == AVQ_F32) {
-        if (w == 16) pack_rows_kernel<float, 4><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, largest, 0);
-        else pack_rows_kernel<float, 1><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, largest, 0);
+        if (w == 16) pack_rows_kernel<float, 4><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, largest, inv, 0);
+        else pack_rows_kernel<float, 1><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, largest, inv, 0);
     } else {
-        if (w == 16) pack_rows_kernel<uint16_t, 8><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
-        else if (w == 8) pack_rows_kernel<uint16_t, 4><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
-        else pack_rows_kernel<uint16_t, 1><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
+        if (w == 16) pack_rows_kernel<uint16_t, 8><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, nullptr, flip);
+        else if (w == 8) pack_rows_kernel<uint16_t, 4><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, nullptr, flip);
+        else pack_rows_kernel<uint16_t, 1><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, nullptr, flip);
     }
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;

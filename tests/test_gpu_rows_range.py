@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 avq = pytest.importorskip("paper_1908_10396_amd")
 
-from test_gpu_rows import TYPES, U, _check_probs, _grad_formula, gen, normal, within  # noqa: E402
+from test_gpu_rows import TYPES, U, _check_probs, _grad_formula, gen, normal, random_ids, within  # noqa: E402
 
 
 def grid(x, kind):
@@ -71,6 +71,87 @@ def test_gradients_of_logits_in_the_hundreds(kind, nq, entropy):
     within(dq, want_q, bound_q + flushed * (1 + x.double().abs()).sum(0), "dqueries")
 
 
+@pytest.mark.parametrize("kind,nq", [("f32", 1), ("f32", 3), ("f32", 64), ("bf16", 1), ("bf16", 3), ("bf16", 64), ("bf16", 65), ("bf16", 300)])
+@pytest.mark.parametrize("value", [-1e7, -1e12, -1e30])
+def test_log_probs_of_rows_behind_thousands_of_large_masks(kind, nq, value):
+    """Logits so large that the rounding of the first maxima, which are masks, is no small exponent."""
+    g = gen(nq)
+    n, d, k, scale = 5000, 32, 4, 0.3
+    x, q = normal((n, d), g), normal((nq, d), g)
+    masked = torch.arange(n, device="cuda") < 2500
+    x[masked] = 0.0
+    x[:, -1] = torch.where(masked, value, 0.0)
+    q[:, -1] = 1.0
+    x, q = x.to(TYPES[kind]), q.to(TYPES[kind])
+    r = avq.log_probs(x, q, k=k, scale=scale)
+    assert not bool(masked[r.alt_ids.long()].any())
+    part = avq.LogProbs(None, r.lse, r.entropy, r.alt_ids - 2500, r.alt_logp)
+    _check_probs(part, x[2500:], q, scale, None, k)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("nq", [1, 5, 80])
+def test_log_probs_of_logits_of_a_hundred_million(kind, nq):
+    """log p of the largest is 0 and the others' the logits' differences, whatever a logit's own rounding is."""
+    g = gen(nq)
+    n, d = 2000, 32
+    x = torch.randint(-8, 9, (n, d), generator=g, device="cuda").to(TYPES[kind])
+    q = torch.randint(-8, 9, (nq, d), generator=g, device="cuda").to(TYPES[kind])
+    scale = 2.0 ** 18
+    r = avq.log_probs(x, q, k=3, scale=scale)
+    s = q.double() @ x.double().t()
+    best = s.topk(3, dim=1).values
+    count = (s == best[:, :1]).double().sum(1)
+    within(r.alt_logp, (best - best[:, :1]) * scale - count.log()[:, None], ((best[:, :1] - best) * scale + 1) * 8 * U, "alt_logp")
+    within(r.lse, best[:, 0] * scale + count.log(), (best[:, 0].abs() * scale + 1) * 4 * U, "lse")
+    within(r.entropy, count.log(), torch.full_like(count, 64 * U), "entropy")
+
+
+def _masked(n, d, nq, kind, value, g, share=0.5):
+    """Rows whose last element is 0, or for some the mask's value; queries whose last element is 1."""
+    x = normal((n, d), g)
+    masked = torch.rand((n,), generator=g, device="cuda") < share
+    masked[3], masked[n - 1] = True, False
+    x[:, -1] = torch.where(masked, value, 0.0)
+    q = normal((nq, d), g)
+    q[:, -1] = 1.0
+    return x.to(TYPES[kind]), q.to(TYPES[kind]), masked
+
+
+def _without(r, masked, ids, k):
+    """The results as those of the rows without a mask: their ids among those."""
+    place = torch.where(masked, -1, torch.cumsum(~masked, 0) - 1).int()
+    alt = None
+    if k:
+        assert not bool(masked[r.alt_ids.long()].any()), "a masked alternative"
+        alt = place[r.alt_ids.long()]
+    real = (ids >= 0) & (ids < masked.numel())
+    return avq.LogProbs(r.logp, r.lse, r.entropy, alt, r.alt_logp), torch.where(real, place[torch.where(real, ids, 0).long()], -1)
+
+
+@pytest.mark.parametrize("kind,value", [("f32", -2.0 ** 24), ("f32", -1e9), ("f32", -1e12), ("f32", -1e30), ("bf16", -1e9), ("bf16", -1e30)])
+@pytest.mark.parametrize("nq", [1, 3, 64, 65, 300])
+@pytest.mark.parametrize("share", [0.0, 0.5])
+def test_log_probs_beside_rows_of_large_masks(kind, value, nq, share):
+    """A mask's value in some rows (or in one) costs the others nothing: their bound knows nothing of it."""
+    g = gen(nq)
+    n, d, k, scale = 3001, 100, 5, 0.3
+    x, q, masked = _masked(n, d, nq, kind, value, g, share)
+    ids = random_ids((nq, 3), n, g)
+    ids = torch.where((ids >= 0) & (ids < n) & masked[ids.clamp(0, n - 1).long()], n - 1, ids)
+    r, place = _without(avq.log_probs(x, q, ids, k, scale), masked, ids, k)
+    _check_probs(r, x[~masked], q, scale, place, k)
+    r = avq.log_probs(x, q, torch.full((nq,), 3, dtype=torch.int32, device="cuda"), 0, scale)
+    s = q.double() @ x[3].double() * scale
+    within(r.logp, s - r.lse.double(), s.abs() * 256 * U, "logp of a masked row")
+
+
+@pytest.mark.parametrize("nq", [65, 300])
+@pytest.mark.parametrize("value", [-1e7, -1e12, -1e30])
+def test_log_probs_of_fp32_rows_behind_thousands_of_large_masks(nq, value):
+    test_log_probs_of_rows_behind_thousands_of_large_masks("f32", nq, value)
+
+
 @pytest.mark.parametrize("nq", [1, 2, 4, 7])
 @pytest.mark.parametrize("other", [2e-5, 5e-5, 1e-3])
 def test_gradient_of_a_part_of_a_table_whose_other_part_is_unlikely(nq, other):
@@ -129,39 +210,3 @@ def test_gradient_of_as_many_rows_as_can_be_looked_up():
     got = avq.embed_grad(grad, ids, n)
     want = torch.bincount((ids + 1).long(), minlength=n + 1)[1:]
     assert torch.equal(got[:, 0].double(), want.double())  # (whole numbers below 2^24: every sum is exact)
-
-
-@pytest.mark.parametrize("kind,nq", [("f32", 1), ("f32", 3), ("f32", 64), ("bf16", 1), ("bf16", 3), ("bf16", 64), ("bf16", 65), ("bf16", 300)])
-@pytest.mark.parametrize("value", [-1e7, -1e12, -1e30])
-def test_log_probs_of_rows_behind_thousands_of_large_masks(kind, nq, value):
-    """Logits so large that the rounding of the first maxima, which are masks, is no small exponent."""
-    g = gen(nq)
-    n, d, k, scale = 5000, 32, 4, 0.3
-    x, q = normal((n, d), g), normal((nq, d), g)
-    masked = torch.arange(n, device="cuda") < 2500
-    x[masked] = 0.0
-    x[:, -1] = torch.where(masked, value, 0.0)
-    q[:, -1] = 1.0
-    x, q = x.to(TYPES[kind]), q.to(TYPES[kind])
-    r = avq.log_probs(x, q, k=k, scale=scale)
-    assert not bool(masked[r.alt_ids.long()].any())
-    part = avq.LogProbs(None, r.lse, r.entropy, r.alt_ids - 2500, r.alt_logp)
-    _check_probs(part, x[2500:], q, scale, None, k)
-
-
-@pytest.mark.parametrize("kind", ["f32", "bf16"])
-@pytest.mark.parametrize("nq", [1, 5, 80])
-def test_log_probs_of_logits_of_a_hundred_million(kind, nq):
-    """log p of the largest is 0 and the others' the logits' differences, whatever a logit's own rounding is."""
-    g = gen(nq)
-    n, d = 2000, 32
-    x = torch.randint(-8, 9, (n, d), generator=g, device="cuda").to(TYPES[kind])
-    q = torch.randint(-8, 9, (nq, d), generator=g, device="cuda").to(TYPES[kind])
-    scale = 2.0 ** 18
-    r = avq.log_probs(x, q, k=3, scale=scale)
-    s = q.double() @ x.double().t()
-    best = s.topk(3, dim=1).values
-    count = (s == best[:, :1]).double().sum(1)
-    within(r.alt_logp, (best - best[:, :1]) * scale - count.log()[:, None], ((best[:, :1] - best) * scale + 1) * 8 * U, "alt_logp")
-    within(r.lse, best[:, 0] * scale + count.log(), (best[:, 0].abs() * scale + 1) * 4 * U, "lse")
-    within(r.entropy, count.log(), torch.full_like(count, 64 * U), "entropy")
