@@ -312,16 +312,23 @@ __device__ __forceinline__ float range_scale(uint32_t largest_bits)
 constexpr float kRowUnit = 0x1p-16f, kTileSpread = 0x1p8f;
 __device__ __forceinline__ float scale_of_inverse(float inv) { return kRowUnit / inv; }
 
+// Odd rows hold an infinity or NaN. A pair has neither, so they are laid out as zeros with an infinite inverse, and their products taken as
+// -infinity, which is what a mask means; queries for which one of them is something else (an infinity times 0 or of the other sign, NaN)
+// are marked, and have no sum that is a number. A query that is not finite itself has zeros, and NaN for an inverse.
+struct OddRows { uint32_t *count, *rows, *seen; }; // how many, which (in any order), [queries] whether marked
+
 int launch_clear_largest(Largest *to, hipStream_t st);
 // inv[row] = kRowUnit / s of each row, and tile_inv[tile] that of the tile's rows where they have one, else 0
-int launch_row_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, float *tile_inv, hipStream_t st);
+int launch_row_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, float *tile_inv, const OddRows &odd, hipStream_t st);
+// marks the queries (negate: with the other sign) whose product with an odd row is not -infinity
+int launch_odd_rows(const float *x, int d, int64_t ld, const float *q, int nq, int64_t ld_q, bool negate, const OddRows &odd, hipStream_t st);
 // max over finite elements into *to
 int launch_largest(const float *x, int64_t rows, int d, int64_t ld, uint32_t *to, hipStream_t st);
 // Rows laid out as `to` says (to.p: where), `steps` steps of them, zeros past a row's end. fp32: pairs, scaled by
 // range_scale(*largest), or, largest == NULL, each row by its own, of which inv[row] is the inverse. negate: with the other sign.
 int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, const float *inv, bool negate, hipStream_t st);
-// fp32 queries: pairs, each row by its own scale, whose inverse goes to inv[row].
-int launch_pack_queries(const float *q, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, float *inv, bool negate, hipStream_t st);
+// fp32 queries: pairs, each row by its own scale, whose inverse goes to inv[row]. Also begins `odd`: no rows, no marks.
+int launch_pack_queries(const float *q, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, float *inv, const OddRows &odd, bool negate, hipStream_t st);
 // The transpose packed: row c < d of d holds x[t][c], 16 t in the order of turned16, zeros past the last t.
 int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, hipStream_t st);
 

@@ -177,7 +177,7 @@ __device__ __forceinline__ void score_rows(const T *__restrict__ qs, int d, cons
                 uint16_t xh[8], xl[8], qh[8], ql[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    split_f16(xs[e] * x_scale, &xh[e], &xl[e]);
+                    split_f16(x_scale == 0.0f ? 0.0f : xs[e] * x_scale, &xh[e], &xl[e]);
                     split_f16(qs[k + e] * how.q_scale, &qh[e], &ql[e]);
                 }
                 Quad hi, lo, q_hi, q_lo;
@@ -215,7 +215,7 @@ __device__ __forceinline__ void score_rows(const T *__restrict__ qs, int d, cons
         float product = acc[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) product = at == r ? acc[r] : product;
-        if ((mine >> 2 & 1) == half) emit(mine, SPLIT ? product * inv : product);
+        if ((mine >> 2 & 1) == half) emit(mine, SPLIT ? fmaxf(product * inv, -INFINITY) : product); // (an odd row's 0 times infinity: -infinity)
     }
 }
 

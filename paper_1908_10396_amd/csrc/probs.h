@@ -30,6 +30,11 @@ __device__ __forceinline__ float log_wide(float sum, float low)
 // the sums of 2^s (l + low; that of m itself is 1, exactly) and of 2^s s.
 struct Stat { float m, l, low, t; };
 
+// s where 2^s s is added: that is 0 wherever 2^s is, also where s is -inf (a masked row)
+__device__ __forceinline__ float times_power(float s) { return fmaxf(s, -200.0f); }
+// sums that are relative to a maximum that is `down` below the new one
+__device__ __forceinline__ float lowered(float t, float l, float down, float f) { return f == 0.0f ? 0.0f : f * __fmaf_rn(l, down, t); }
+
 // Of two sets of logits; one without any has m = -inf and sums of 0. c2: from products to logits.
 __device__ __forceinline__ Stat join(const Stat &a, const Stat &b, float c2)
 {
@@ -37,7 +42,7 @@ __device__ __forceinline__ Stat join(const Stat &a, const Stat &b, float c2)
     if (!(m > -INFINITY)) return Stat{m, a.l + b.l, 0.0f, a.t + b.t}; // (NaN goes on in the sums)
     const float da = a.m > -INFINITY ? (a.m - m) * c2 : 0.0f, db = b.m > -INFINITY ? (b.m - m) * c2 : 0.0f;
     const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
-    Stat s{m, a.l * fa, a.low * fa, fa * __fmaf_rn(a.l, da, a.t) + fb * __fmaf_rn(b.l, db, b.t)};
+    Stat s{m, a.l * fa, a.low * fa, lowered(a.t, a.l, da, fa) + lowered(b.t, b.l, db, fb)};
     add_wide(s.l, s.low, b.l * fb);
     s.low = __fmaf_rn(b.low, fb, s.low);
     return s;

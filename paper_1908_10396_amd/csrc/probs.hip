@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prob_stream_kernel(const T 
             if (top > m[i]) {
                 if (m[i] > -INFINITY) {
                     const float down = (m[i] - top) * c2, f = __builtin_amdgcn_exp2f(down);
-                    t[i] = f * __fmaf_rn(l[i], down, t[i]);
+                    t[i] = lowered(t[i], l[i], down, f);
                     l[i] *= f;
                     low[i] *= f;
                 }
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(kStreamThreads, 2) void prob_stream_kernel(const T 
                     if (h * 16 + kg * 4 + r < valid) {
                         const float s2 = (acc[h][i][r] - base) * c2, e = __builtin_amdgcn_exp2f(s2);
                         sum += e;
-                        t[i] = __fmaf_rn(e, s2, t[i]);
+                        t[i] = __fmaf_rn(e, times_power(s2), t[i]);
                     }
             add_wide(l[i], low[i], sum);
             if (gmax) {
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restri
         if (real && sum > m) {
             if (m > -INFINITY) {
                 const float down = (m - sum) * c2, f = __builtin_amdgcn_exp2f(down);
-                t = f * __fmaf_rn(l, down, t);
+                t = lowered(t, l, down, f);
                 l *= f;
                 low *= f;
             }
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(kRowThreads) void prob_row_kernel(const T *__restri
         const float s2 = m > -INFINITY ? (sum - m) * c2 : sum, e = __builtin_amdgcn_exp2f(s2);
         if (real) {
             add_wide(l, low, e);
-            t = __fmaf_rn(e, s2, t);
+            t = __fmaf_rn(e, times_power(s2), t);
             top = fmaxf(top, sum);
         }
         if (turn == kTurns - 1 && gmax) {
@@ -380,7 +380,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
                         const float4 v = *(const float4 *)(inv + a * 32 + b * 8);
                         const float e[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) { acc[a][0][4 * b + r] *= e[r]; acc[a][1][4 * b + r] *= e[r]; }
+                        for (int r = 0; r < 4; ++r) // (an odd row's 0 times infinity: -infinity)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) acc[a][j][4 * b + r] = fmaxf(acc[a][j][4 * b + r] * e[r], -INFINITY);
                     }
             }
             const int64_t row0 = (first + i) * kTileM;
@@ -390,13 +392,16 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
                 constexpr bool TAIL = decltype(tail)::value;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    float group[4];
+                    float group[4], least = INFINITY;
 #pragma unroll
                     for (int a = 0; a < 4; ++a) {
                         float g = -INFINITY;
 #pragma unroll
                         for (int r = 0; r < 16; ++r)
-                            if (!TAIL || acc_row(a, r) < valid) g = fmaxf(g, acc[a][j][r]);
+                            if (!TAIL || acc_row(a, r) < valid) {
+                                g = fmaxf(g, acc[a][j][r]);
+                                if (!TAIL) least = fminf(least, acc[a][j][r]);
+                            }
                         group[a] = SPLIT ? g * unit : g;
                     }
                     const float top = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
@@ -404,7 +409,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
                         if (m[j] > -INFINITY) {
                             const float from = m[j] * cq[j], to = top * cq[j];
                             const float down = fmaxf(fabsf(from), fabsf(to)) <= kTame ? from - to : (m[j] - top) * cq[j], f = __builtin_amdgcn_exp2f(down);
-                            t[j] = f * __fmaf_rn(l[j], down, t[j]);
+                            t[j] = lowered(t[j], l[j], down, f);
                             l[j] *= f;
                             low[j] *= f;
                         }
@@ -425,10 +430,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void prob_tile_kernel(Rows16 X, Ro
                                     if (decltype(any_size)::value) s2 = tame ? s2 : (SPLIT ? __fmaf_rn(acc[a][j][r], unit, -base) : acc[a][j][r] - base) * cq[j];
                                     const float e = __builtin_amdgcn_exp2f(s2);
                                     ls[a] += e;
-                                    ts[a] = __fmaf_rn(e, s2, ts[a]);
+                                    ts[a] = __fmaf_rn(e, decltype(any_size)::value ? times_power(s2) : s2, ts[a]);
                                 }
                     };
-                    if (TAIL || __any(!tame)) sums(std::true_type{});
+                    // (also where the least logit is -inf)
+                    if (TAIL || __any(!(tame && __fmaf_rn(least, to_logit, shift) > -INFINITY))) sums(std::true_type{});
                     else sums(std::false_type{});
 #pragma unroll
                     for (int a = 0; a < 4; ++a) add_wide(l[j], low[j], ls[a]);
@@ -475,7 +481,7 @@ __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o
 // one another.
 template <int PATH, class T, int NT>
 __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, float scale, int row_lanes,
-                                                         const float *__restrict__ x_inv, const float *__restrict__ q_inv, const float4 *__restrict__ stats, int parts, const int32_t *__restrict__ ids, int given, float *__restrict__ logp_out,
+                                                         const float *__restrict__ x_inv, const float *__restrict__ q_inv, const uint32_t *__restrict__ odd_seen, const float4 *__restrict__ stats, int parts, const int32_t *__restrict__ ids, int given, float *__restrict__ logp_out,
                                                          float *__restrict__ lse_out, float *__restrict__ entropy_out, const float *__restrict__ gmax, int64_t gstride, int k,
                                                          int32_t *__restrict__ alt_ids, float *__restrict__ alt_logp)
 {
@@ -546,6 +552,7 @@ __global__ __launch_bounds__(NT) void prob_finish_kernel(const T *__restrict__ x
     }
     __syncthreads();
     a = wave_stat[0];
+    if (PATH == kByTiles && sizeof(T) == 4 && odd_seen[row]) a.l = NAN;
     for (int w = 1; w < NT / 64; ++w) a = join(a, wave_stat[w], c2);
     constexpr float ln2 = 0.693147180559945309f;
     const float log_l = log_wide(a.l, a.low), lse = __fmaf_rn(a.m, c, log_l);
@@ -693,7 +700,7 @@ struct ProbScratch {
     float4 *stats; float *gmax; int64_t gstride;
     int groups, qt, query_tiles;                         // stream
     bool pack; int steps, parts, launches; int64_t part; // tiles: steps of an inner product, rows a launch
-    uint16_t *x16, *q16; float *q_inv, *x_inv, *tile_inv;
+    uint16_t *x16, *q16; float *q_inv, *x_inv, *tile_inv; OddRows odd;
     size_t bytes;
 };
 
@@ -732,6 +739,7 @@ static ProbScratch prob_scratch(const ProbParams &p, void *base)
             const size_t tiles = (size_t)(p.n + kTileM - 1) / kTileM;
             s.x_inv = (float *)take(tiles * kTileM * sizeof(float));
             s.tile_inv = (float *)take(tiles * sizeof(float));
+            s.odd = OddRows{(uint32_t *)take(sizeof(uint32_t)), (uint32_t *)take((size_t)p.n * sizeof(uint32_t)), (uint32_t *)take((size_t)p.nq * sizeof(uint32_t))};
         }
         if (s.pack) s.x16 = (uint16_t *)take(packed_bytes(s.part, s.steps));
     }
@@ -799,8 +807,9 @@ static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
     const float c2 = fabsf(p.scale) * 1.44269504088896341f;
     const Rows16 Q = packed_rows(s.q16, p.nq);
     if (SPLIT) {
-        AVQ_TRY(launch_pack_queries((const float *)p.queries, p.nq, p.d, p.ld_queries, s.steps, Q, s.q_inv, p.scale < 0.0f, st));
-        AVQ_TRY(launch_row_inverses((const float *)p.points, p.n, p.d, p.ld_points, s.x_inv, s.tile_inv, st));
+        AVQ_TRY(launch_pack_queries((const float *)p.queries, p.nq, p.d, p.ld_queries, s.steps, Q, s.q_inv, s.odd, p.scale < 0.0f, st));
+        AVQ_TRY(launch_row_inverses((const float *)p.points, p.n, p.d, p.ld_points, s.x_inv, s.tile_inv, s.odd, st));
+        AVQ_TRY(launch_odd_rows((const float *)p.points, p.d, p.ld_points, (const float *)p.queries, p.nq, p.ld_queries, p.scale < 0.0f, s.odd, st));
     } else {
         AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, Q, nullptr, nullptr, p.scale < 0.0f, st));
     }
@@ -835,7 +844,7 @@ static int finish_run(const ProbParams &p, const ProbScratch &s, int parts, hipS
     static LdsLimitOnce once;
     AVQ_TRY(set_lds_limit((const void *)prob_finish_kernel<PATH, T, NT>, kFinishLds, &once));
     prob_finish_kernel<PATH, T, NT><<<dim3(p.nq), dim3(NT), finish_lds(p.d, p.k), st>>>(
-        (const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.nq, p.ld_queries, p.scale, row_lanes(sizeof(T), p.d), s.x_inv, s.q_inv, s.stats, parts, p.ids, p.given,
+        (const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.nq, p.ld_queries, p.scale, row_lanes(sizeof(T), p.d), s.x_inv, s.q_inv, s.odd.seen, s.stats, parts, p.ids, p.given,
         p.logp, p.lse, p.entropy, s.gmax, s.gstride, p.k, p.alt_ids, p.alt_logp);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;

@@ -73,7 +73,7 @@ constexpr int kInverseRows = 4;
 constexpr float kLeastInverse = kRowUnit * 0x1p-97f; // of rows too small for a scale, those of zeros among them
 
 template <bool RAGGED, int L>
-__global__ __launch_bounds__(256) void row_inverses_kernel(const float *__restrict__ x, int64_t rows, int d, int64_t ld, float *__restrict__ inv)
+__global__ __launch_bounds__(256) void row_inverses_kernel(const float *__restrict__ x, int64_t rows, int d, int64_t ld, float *__restrict__ inv, OddRows odd)
 {
     constexpr int kPer = 64 / L, U = kInverseRows;
     const int units = units_of<float>(d), wave = threadIdx.x >> 6, lane = threadIdx.x & 63, in_row = lane % L;
@@ -86,14 +86,18 @@ __global__ __launch_bounds__(256) void row_inverses_kernel(const float *__restri
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int e = 0; e < kUnit<float>; ++e) m[u] = max(m[u], finite_bits(v[u].e[e]));
+                for (int e = 0; e < kUnit<float>; ++e) m[u] = max(m[u], __float_as_uint(v[u].e[e]) & 0x7fffffffu);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
             for (int w = 1; w < L; w <<= 1) m[u] = max(m[u], (uint32_t)__shfl_xor((int)m[u], w, 64));
             const int64_t row = base + u * kPer + lane / L;
-            if (in_row == 0 && row < rows) inv[row] = m[u] == 0 ? kLeastInverse : kRowUnit / range_scale(m[u]);
+            if (in_row == 0 && row < rows) {
+                const bool is_odd = m[u] >= 0x7f800000u;
+                inv[row] = is_odd ? INFINITY : m[u] == 0 ? kLeastInverse : kRowUnit / range_scale(m[u]);
+                if (is_odd) odd.rows[atomicAdd(odd.count, 1u)] = (uint32_t)row; // (what is done with them knows no order)
+            }
         }
     }
 }
@@ -114,17 +118,54 @@ __global__ __launch_bounds__(kTileM) void tile_inverses_kernel(float *__restrict
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kTileM / 64; ++w) { hi = fmaxf(hi, top[w]); lo = fminf(lo, least[w]); }
-    const bool one = hi <= lo * kTileSpread;
+    const bool one = hi < INFINITY && hi <= lo * kTileSpread;
     if (one && row < rows) inv[row] = hi;
     if (threadIdx.x == 0) tile_inv[blockIdx.x] = one ? hi : 0.0f;
 }
 
-int launch_row_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, float *tile_inv, hipStream_t st)
+// A thread a query: an odd row's elements that are not finite are found by the workgroup, and multiplied by each query.
+__global__ __launch_bounds__(256) void odd_rows_kernel(const float *__restrict__ x, int d, int64_t ld, const float *__restrict__ q, int nq, int64_t ld_q, float sign, OddRows odd)
+{
+    __shared__ int columns[256];
+    __shared__ float values[256];
+    __shared__ int found;
+    const uint32_t all = *odd.count;
+    const int t = blockIdx.x * 256 + threadIdx.x;
+    bool marked = false;
+    for (uint32_t i = blockIdx.y; i < all; i += gridDim.y) {
+        const float *row = x + (int64_t)odd.rows[i] * ld;
+        for (int c0 = 0; c0 < d; c0 += 256) {
+            __syncthreads(); // (the columns before have been read)
+            if (threadIdx.x == 0) found = 0;
+            __syncthreads();
+            const int c = c0 + threadIdx.x;
+            const float v = c < d ? row[c] : 0.0f;
+            if (!(fabsf(v) < INFINITY)) {
+                const int at = atomicAdd(&found, 1);
+                columns[at] = c;
+                values[at] = v;
+            }
+            __syncthreads();
+            if (t < nq)
+                for (int k = 0; k < found; ++k) marked = marked || !(q[t * ld_q + columns[k]] * sign * values[k] == -INFINITY);
+        }
+    }
+    if (marked) odd.seen[t] = 1u;
+}
+
+int launch_odd_rows(const float *x, int d, int64_t ld, const float *q, int nq, int64_t ld_q, bool negate, const OddRows &odd, hipStream_t st)
+{
+    odd_rows_kernel<<<dim3((unsigned)((nq + 255) / 256), 64), dim3(256), 0, st>>>(x, d, ld, q, nq, ld_q, negate ? -1.0f : 1.0f, odd);
+    AVQ_HIP(hipGetLastError());
+    return AVQ_OK;
+}
+
+int launch_row_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, float *tile_inv, const OddRows &odd, hipStream_t st)
 {
     const bool whole = whole_units(x, ld, d, sizeof(float));
     const int units = units_of<float>(d), lanes = units <= 16 ? 16 : units <= 32 ? 32 : 64;
     const int64_t each = 4 * (64 / lanes) * kInverseRows;
-    auto run = [&](auto kernel) { kernel<<<dim3((unsigned)std::min<int64_t>(2048, (rows + each - 1) / each)), dim3(256), 0, st>>>(x, rows, d, ld, inv); };
+    auto run = [&](auto kernel) { kernel<<<dim3((unsigned)std::min<int64_t>(2048, (rows + each - 1) / each)), dim3(256), 0, st>>>(x, rows, d, ld, inv, odd); };
     if (lanes == 16) whole ? run(row_inverses_kernel<false, 16>) : run(row_inverses_kernel<true, 16>);
     else if (lanes == 32) whole ? run(row_inverses_kernel<false, 32>) : run(row_inverses_kernel<true, 32>);
     else whole ? run(row_inverses_kernel<false, 64>) : run(row_inverses_kernel<true, 64>);
@@ -170,7 +211,7 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x,
             Pack<uint16_t, 8> hi, lo;
             if constexpr (SPLIT) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) split_f16(v[e] * scale, &hi.e[e], &lo.e[e]);
+                for (int e = 0; e < 8; ++e) split_f16(scale == 0.0f ? 0.0f : v[e] * scale, &hi.e[e], &lo.e[e]);
                 *(Pack<uint16_t, 8> *)(to + to_rows.block) = lo;
             } else {
                 __builtin_memcpy(&hi, v, 16);
@@ -185,27 +226,33 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x,
 
 // each row by its own scale, a workgroup a row
 __global__ __launch_bounds__(256) void pack_own_scale_kernel(const float *__restrict__ x, int d, int64_t ld, int steps, Rows16 to_rows, float *__restrict__ inv,
-                                                             float sign)
+                                                             OddRows odd, float sign)
 {
     __shared__ uint32_t red[4];
     const int64_t row = blockIdx.x;
     uint32_t m = 0;
-    for (int c = threadIdx.x; c < d; c += 256) m = max(m, finite_bits(x[row * ld + c]));
+    for (int c = threadIdx.x; c < d; c += 256) m = max(m, __float_as_uint(x[row * ld + c]) & 0x7fffffffu);
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, w, 64));
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
     __syncthreads();
-    const float s = range_scale(max(max(red[0], red[1]), max(red[2], red[3])));
+    m = max(max(red[0], red[1]), max(red[2], red[3]));
+    const bool finite = m < 0x7f800000u;
+    const float s = finite ? range_scale(m) : NAN;
     for (int c = threadIdx.x; c < steps * 16; c += 256) {
         uint16_t *to = (uint16_t *)to_rows.p + block16<true>(c) * to_rows.block + row * to_rows.row + (c & 15);
-        split_f16(c < d ? x[row * ld + c] * (s * sign) : 0.0f, to, to + to_rows.block);
+        split_f16(c < d && finite ? x[row * ld + c] * (s * sign) : 0.0f, to, to + to_rows.block);
     }
-    if (threadIdx.x == 0) inv[row] = 1.0f / (kRowUnit * s);
+    if (threadIdx.x == 0) {
+        inv[row] = 1.0f / (kRowUnit * s);
+        odd.seen[row] = 0u;
+        if (row == 0) *odd.count = 0u;
+    }
 }
 
-int launch_pack_queries(const float *q, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, float *inv, bool negate, hipStream_t st)
+int launch_pack_queries(const float *q, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, float *inv, const OddRows &odd, bool negate, hipStream_t st)
 {
-    pack_own_scale_kernel<<<dim3((unsigned)rows), dim3(256), 0, st>>>(q, d, ld, steps, to, inv, negate ? -1.0f : 1.0f);
+    pack_own_scale_kernel<<<dim3((unsigned)rows), dim3(256), 0, st>>>(q, d, ld, steps, to, inv, odd, negate ? -1.0f : 1.0f);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }

@@ -180,6 +180,44 @@ def test_gradient_of_a_part_of_a_table_whose_other_part_is_unlikely(nq, other):
     within(dx[ids.long()], want, bound, "dpoints of the given rows")
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [1, 2, 5, 64, 65, 300])
+@pytest.mark.parametrize("value", ["infinite", "lowest"])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_log_probs_beside_rows_of_infinite_and_lowest_masks(kind, nq, value, sign):
+    """Logits of -infinity are a probability of 0: lse, entropy and the alternatives are those of the other rows."""
+    g = gen(nq)
+    n, d, k, scale = 3001, 100, 5, 0.3 * sign
+    value = -sign * (math.inf if value == "infinite" else torch.finfo(TYPES[kind]).max)
+    x, q, masked = _masked(n, d, nq, kind, value, g)
+    ids = random_ids((nq, 3), n, g)
+    ids = torch.where((ids >= 0) & (ids < n) & masked[ids.clamp(0, n - 1).long()], n - 1, ids)
+    r, place = _without(avq.log_probs(x, q, ids, k, scale), masked, ids, k)
+    _check_probs(r, x[~masked], q, scale, place, k)
+    r = avq.log_probs(x, q, torch.full((nq,), 3, dtype=torch.int32, device="cuda"), 0, scale)
+    s = q.double() @ x[3].double() * scale
+    if math.isinf(value):
+        assert bool((r.logp == -math.inf).all())
+    else:
+        within(r.logp, s - r.lse.double(), s.abs() * 256 * U, "logp of a masked row")
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [1, 5, 70])
+def test_rows_that_are_not_finite_show(kind, nq):
+    """NaN, +infinity, and infinity times zero in any row: no query's sum is a number."""
+    g = gen(nq)
+    x, q, _ = _masked(3001, 100, nq, kind, 0.0, g)
+    for value, at in ((float("nan"), 5), (math.inf, 99), (-math.inf, 7)):
+        bad = x.clone()
+        bad[1234, at] = value
+        if at == 7:
+            q = q.clone()
+            q[:, 7] = 0.0
+        r = avq.log_probs(bad, q, k=2, scale=0.3)
+        assert not bool(torch.isfinite(r.lse).any())
+
+
 def test_gradient_of_as_many_given_ids_as_there_can_be_threads():
     g = gen(1)
     n, d, nq, m = 64, 8, 1 << 16, 1 << 10
