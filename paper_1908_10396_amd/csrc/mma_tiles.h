@@ -291,8 +291,9 @@ __host__ __device__ inline void part_tiles(int64_t tiles, int parts, int p, int6
 }
 
 // ---- rows_pack.hip -------------------------------------------------------------------------
-// Largest finite magnitudes, as bits of non-negative floats (0: nothing yet).
-struct Largest { uint32_t points, queries, upstream, pad; };
+// Largest finite magnitudes, as bits of non-negative floats (0: nothing yet); weighted: of queries over their factor in G, and the least
+// that a query has of them (infinity: nothing yet).
+struct Largest { uint32_t points, queries, weighted, least_weighted; };
 
 // the power of two that brings a largest magnitude to 2^14 .. 2^15 (1 where there is none)
 __device__ __forceinline__ float range_scale(uint32_t largest_bits)
@@ -329,7 +330,8 @@ int launch_largest(const float *x, int64_t rows, int d, int64_t ld, uint32_t *to
 int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, const float *inv, bool negate, hipStream_t st);
 // fp32 queries: pairs, each row by its own scale, whose inverse goes to inv[row]. Also begins `odd`: no rows, no marks.
 int launch_pack_queries(const float *q, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, float *inv, const OddRows &odd, bool negate, hipStream_t st);
-// The transpose packed: row c < d of d holds x[t][c], 16 t in the order of turned16, zeros past the last t.
-int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, hipStream_t st);
+// The transpose packed: row c < d of d holds x[t][c] factor[t] (factor == NULL: x[t][c]), 16 t in the order of turned16, zeros past the
+// last t and where the factor is 0.
+int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const float *factor, hipStream_t st);
 
 } // namespace avq

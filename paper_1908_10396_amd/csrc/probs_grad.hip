@@ -18,37 +18,68 @@
 
 namespace avq {
 
-constexpr float kGradTop = 16384.0f; // what the bound of |G| is brought to
+// G of a query is kept times a power of two of its own that brings a bound of its magnitude to 2^14 .. 2^15 (bf16 needs none), so that the
+// weight of other queries costs it nothing; the inverse goes to dq, and with the transposed queries into dx. What dx adds up has one scale
+// all the same: where queries over their factors are apart by more than kWeightSpread, pairs (and f16) would lose the least of them, and
+// dx goes by the fp32 matrix instruction.
+struct GradCoef { float a, h, factor, inverse; }; // (inverse 0: nothing comes from this query)
+constexpr float kWeightSpread = 0x1p16f;
+template <class T> constexpr bool kHasFactor = std::is_same<T, float>::value || std::is_same<T, f16_t>::value;
 
-// the factor that G is kept with, and its inverse
-__device__ __forceinline__ float grad_bound(const Largest *largest) { return fmaxf(__uint_as_float(largest->upstream), 1e-30f); }
-__device__ __forceinline__ float grad_factor(const Largest *largest) { return kGradTop / grad_bound(largest); }
+template <class T> __device__ __forceinline__ bool weights_apart(const Largest *largest)
+{
+    return kHasFactor<T> && __uint_as_float(largest->weighted) > kWeightSpread * __uint_as_float(largest->least_weighted);
+}
 
-// a_t and h_t, and the bound of |G|
-__global__ __launch_bounds__(256) void grad_coef_kernel(const int32_t *__restrict__ ids, int64_t n, int nq, int given, const float *__restrict__ g, const float *__restrict__ h,
-                                                        const float *__restrict__ entropy, const float *__restrict__ gl, float2 *__restrict__ coef, Largest *__restrict__ largest)
+// A wave a query: a_t, h_t, the factor, and the range of what dx adds up.
+template <class T>
+__global__ __launch_bounds__(256) void grad_coef_kernel(const T *__restrict__ q, int64_t ld_q, int d, const int32_t *__restrict__ ids, int64_t n, int nq, int given,
+                                                        const float *__restrict__ g, const float *__restrict__ h, const float *__restrict__ entropy, const float *__restrict__ gl,
+                                                        GradCoef *__restrict__ coef, Largest *__restrict__ largest)
+{
+    const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (t >= nq) return;
+    float a = 0.0f, mag = 0.0f;
+    for (int j = lane; j < given; j += 64) {
+        const int32_t id = ids[(int64_t)t * given + j];
+        if (id >= 0 && (int64_t)id < n) {
+            const float v = g[(int64_t)t * given + j];
+            a += v;
+            mag += fabsf(v);
+        }
+    }
+    a = group_sum<64>(a);
+    mag = group_sum<64>(mag);
+    uint32_t top = 0;
+    if (kHasFactor<T>) {
+        for (int c = lane; c < d; c += 64) {
+            const uint32_t bits = __float_as_uint(to_f32(q[t * ld_q + c])) & 0x7fffffffu;
+            top = max(top, bits < 0x7f800000u ? bits : 0u);
+        }
+#pragma unroll
+        for (int w = 1; w < 64; w <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, w, 64));
+    }
+    if (lane != 0) return;
+    const float ht = h ? h[t] : 0.0f;
+    if (gl) a -= gl[t];
+    if (h) a += ht * entropy[t];
+    const float bound = mag + fabsf(a) + fabsf(ht); // of |G| (p |log p| < 0.37)
+    const bool some = !(bound == 0.0f);
+    const float factor = kHasFactor<T> && bound < INFINITY ? range_scale(__float_as_uint(bound)) : 1.0f;
+    coef[t] = GradCoef{a, ht, factor, some ? 1.0f / factor : 0.0f};
+    if (!kHasFactor<T> || !some || !(bound < INFINITY) || top == 0) return;
+    const uint32_t weighted = __float_as_uint(__uint_as_float(top) / factor);
+    if (weighted >= 0x7f800000u) return;
+    // (maxima and minima: no order matters; asked for first, since most change nothing)
+    if (weighted > __hip_atomic_load(&largest->weighted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(&largest->weighted, weighted);
+    if (weighted < __hip_atomic_load(&largest->least_weighted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMin(&largest->least_weighted, weighted);
+}
+
+// what the transposed queries are multiplied by
+__global__ __launch_bounds__(256) void grad_factor_kernel(const GradCoef *__restrict__ coef, int nq, const Largest *__restrict__ largest, float *__restrict__ factor)
 {
     const int t = blockIdx.x * 256 + threadIdx.x;
-    float bound = 0.0f;
-    if (t < nq) {
-        float a = 0.0f, mag = 0.0f;
-        for (int j = 0; j < given; ++j) {
-            const int32_t id = ids[(int64_t)t * given + j];
-            if (id >= 0 && (int64_t)id < n) {
-                const float v = g[(int64_t)t * given + j];
-                a += v;
-                mag += fabsf(v);
-            }
-        }
-        if (gl) a -= gl[t];
-        if (h) a += h[t] * entropy[t];
-        coef[t] = make_float2(a, h ? h[t] : 0.0f);
-        bound = mag + fabsf(a) + (h ? fabsf(h[t]) : 0.0f); // (p |log p| < 0.37)
-    }
-    uint32_t m = bound < INFINITY ? __float_as_uint(bound) : 0u;
-#pragma unroll
-    for (int w = 1; w < 64; w <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, w, 64));
-    if ((threadIdx.x & 63) == 0 && m != 0) atomicMax(&largest->upstream, m);
+    if (t < nq) factor[t] = coef[t].inverse == 0.0f ? 0.0f : range_scale(largest->weighted) * coef[t].inverse;
 }
 
 // eight values as operands: rounded to the type, or (fp32) hi and lo
@@ -72,11 +103,11 @@ __device__ __forceinline__ void put_once(uint16_t *to, const Quad &v)
 
 // G^T of the part's rows: 256 queries of a workgroup by 128 rows at a time. T: the caller's type, H: the instructions'.
 template <class T, class H, bool SPLIT, bool ENTROPY>
-__global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Rows16 X, int steps, float c2, const float *__restrict__ lse, const float2 *__restrict__ coef,
+__global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Rows16 X, int steps, float c2, const float *__restrict__ lse, const GradCoef *__restrict__ coef,
                                                                     const Largest *__restrict__ largest, int parts, int others, Rows16 G, int width)
 {
     extern __shared__ char lds[];
-    __shared__ float4 shift[kTileM / 4], up[kTileM / 4], up_h[kTileM / 4]; // -lse / log 2; a and h, in G's units
+    __shared__ float4 shift[kTileM / 4], up[kTileM / 4], up_h[kTileM / 4]; // -lse / log 2; a and h, times the factor
     const Place place = place_of(blockIdx.x, others);
     const int wave = threadIdx.x >> 6, half = (threadIdx.x & 63) >> 5;
     const int64_t tiles = (X.rows + kTileN - 1) / kTileN, q0 = (int64_t)place.other * kTileM;
@@ -86,11 +117,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
     {
         const int64_t t = q0 + threadIdx.x;
         const bool real = t < Q.rows; // (queries past the last have the last one's products: a probability of 0 all the same)
-        const float f = grad_factor(largest);
-        const float2 c = real ? coef[t] : make_float2(0.0f, 0.0f);
+        const GradCoef c = real ? coef[t] : GradCoef{0.0f, 0.0f, 1.0f, 0.0f};
         ((float *)shift)[threadIdx.x] = real ? -lse[t] * 1.44269504088896341f : -INFINITY;
-        ((float *)up)[threadIdx.x] = -c.x * f;
-        if (ENTROPY) ((float *)up_h)[threadIdx.x] = -c.y * f * 0.693147180559945309f;
+        ((float *)up)[threadIdx.x] = -c.a * c.factor;
+        if (ENTROPY) ((float *)up_h)[threadIdx.x] = -c.h * c.factor * 0.693147180559945309f;
     }
     const float cq = SPLIT ? c2 * (1.0f / range_scale(largest->points)) * (1.0f / range_scale(largest->queries)) : c2;
     __syncthreads();
@@ -148,7 +178,7 @@ constexpr int64_t kGivenGroups = 1 << 22; // a launch has fewer than 2^32 thread
 template <int PATH, class T>
 __global__ __launch_bounds__(64) void grad_given_kernel(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, int d, float scale, int row_lanes,
                                                         const int32_t *__restrict__ ids, int given, const float *__restrict__ g, const float *__restrict__ lse,
-                                                        const float2 *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, Rows16 G)
+                                                        const GradCoef *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, Rows16 G)
 {
     extern __shared__ char lds[];
     T *qs = (T *)lds;
@@ -179,10 +209,10 @@ __global__ __launch_bounds__(64) void grad_given_kernel(const T *__restrict__ x,
         score_rows<PATH, 8>(qs, d, how, [&](int) { return x + id * ld_x; }, [&](int) { return x_inv; }, [&](int slot, float product) {
             if (slot != 0) return;
             const float logp = __fmaf_rn(product, c, -lse[t]);
-            const float2 k = coef[t];
+            const GradCoef k = coef[t];
             const float p = __builtin_amdgcn_exp2f(logp * 1.44269504088896341f);
             f32x8 one = {};
-            one[0] = (sum - (p > 0.0f || p != p ? p * __fmaf_rn(k.y, logp, k.x) : 0.0f)) * grad_factor(largest);
+            one[0] = (sum - (p > 0.0f || p != p ? p * __fmaf_rn(k.h, logp, k.a) : 0.0f)) * k.factor;
             Quad hi, low{};
             put16(one, &hi, &low, T{});
             uint16_t *to = (uint16_t *)G.p + block16<sizeof(T) == 4>(t) * G.block + (id - lo) * G.row + turned16((int)t & 15);
@@ -204,11 +234,52 @@ template <int I = 0, class Fn> __device__ __forceinline__ void for_quads(Fn fn)
     }
 }
 
+// A tile of dx by the fp32 matrix instruction, two queries at a time; acc as the other form has it.
+template <class T>
+__device__ __forceinline__ void rows_by_fp32(const Rows16 &G, int64_t row0, const T *__restrict__ q, int64_t ld_q, int nq, int d, int64_t c0, const GradCoef *__restrict__ coef, f32x16 (&acc)[4][2])
+{
+    constexpr bool SPLIT = sizeof(T) == 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const uint16_t *g[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        g[i] = G.p + min(row0 + (wave >> 1) * 128 + i * 32 + (lane & 31), G.rows - 1) * G.row + half * 8;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    }
+    for (int t0 = 0; t0 < nq; t0 += 16) {
+        float ga[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint16_t *from = g[i] + block16<SPLIT>(t0) * G.block;
+            uint16_t hi[8], lo[8];
+            __builtin_memcpy(hi, from, 16);
+            if (SPLIT) __builtin_memcpy(lo, from + G.block, 16);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ga[i][e] = SPLIT ? to_f32(f16_t{hi[e]}) + to_f32(f16_t{lo[e]}) : to_f32(f16_t{hi[e]});
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int t = t0 + turned16(half * 8 + e);
+            const float inverse = t < nq ? coef[t].inverse : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int64_t c = c0 + (wave & 1) * 64 + j * 32 + (lane & 31);
+                const float b = inverse != 0.0f && c < d ? to_f32(q[t * ld_q + c]) * inverse : 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(ga[i][e], b, acc[i][j], 0, 0, 0);
+            }
+        }
+    }
+}
+
 // dx of the part's rows: 256 rows by 128 dimensions.
 // PAIRS: 16-bit types of rows on 4 bytes, of an even number of elements.
 template <class T, class H, bool SPLIT, bool ACCUMULATE, bool PAIRS>
 __global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Rows16 Qt, int steps, float scale, const Largest *__restrict__ largest, int parts, int others, int64_t rows,
-                                                                    int d, T *__restrict__ dx, int64_t ld_dx)
+                                                                    int d, const T *__restrict__ q, int64_t ld_q, int nq, const GradCoef *__restrict__ coef, T *__restrict__ dx, int64_t ld_dx)
 {
     extern __shared__ char lds[];
     const Place place = place_of(blockIdx.x, others);
@@ -216,46 +287,55 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Ro
     int64_t first;
     int count;
     part_tiles(tiles, parts, place.part, &first, &count);
-    const float f = grad_bound(largest) * (1.0f / kGradTop) * scale * (SPLIT ? 1.0f / range_scale(largest->queries) : 1.0f);
+    const bool apart = weights_apart<T>(largest);
+    const float f = kHasFactor<T> && !apart ? scale * (1.0f / range_scale(largest->weighted)) : scale;
     typedef RowCopies<true, true> Copies;
-    run_tiles<H, SPLIT, true, Copies>(G, Qt, steps, count, lds, [&](int i, Copies &c) { c.seek(G, (first + i) * kTileM, Qt, c0); },
-        [&](int i, f32x16 (&acc)[4][2]) {
-            const int64_t row0 = (first + i) * kTileM + acc_row(0, 0);
-            const int64_t left = rows - row0; // rows from this lane's first one on
-            for_quads([&](auto at) {
-                constexpr int a = decltype(at)::a, b = decltype(at)::b, j = decltype(at)::j;
-                const int64_t c = c0 + acc_col(j);
-                T *to = dx + (row0 + a * 32 + b * 8) * ld_dx + c;
-                if (PAIRS) {
-                    // two lanes, two rows: each stores both columns of one
+    auto store = [&](int i, f32x16 (&acc)[4][2]) __attribute__((always_inline)) {
+        const int64_t row0 = (first + i) * kTileM + acc_row(0, 0);
+        const int64_t left = rows - row0; // rows from this lane's first one on
+        for_quads([&](auto at) {
+            constexpr int a = decltype(at)::a, b = decltype(at)::b, j = decltype(at)::j;
+            const int64_t c = c0 + acc_col(j);
+            T *to = dx + (row0 + a * 32 + b * 8) * ld_dx + c;
+            if (PAIRS) {
+                // two lanes, two rows: each stores both columns of one
 #pragma unroll
-                    for (int e = 0; e < 4; e += 2) {
-                        const float v0 = acc[a][j][4 * b + e] * f, v1 = acc[a][j][4 * b + e + 1] * f;
-                        const bool odd = threadIdx.x & 1;
-                        const float other = __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(odd ? v0 : v1), 0xB1 /* quad_perm [1, 0, 3, 2] */, 0xF, 0xF, true));
-                        T *at = to + (odd ? ld_dx - 1 : 0);
-                        if (c < d && a * 32 + b * 8 + e + (odd ? 1 : 0) < left) {
-                            Pack<T, 2> o;
-                            float lo = odd ? other : v0, hi = odd ? v1 : other;
-                            if (ACCUMULATE) { o = *(const Pack<T, 2> *)at; lo += to_f32(o.e[0]); hi += to_f32(o.e[1]); }
-                            o.e[0] = from_f32<T>(lo);
-                            o.e[1] = from_f32<T>(hi);
-                            *(Pack<T, 2> *)at = o;
-                        }
-                        to += 2 * ld_dx;
+                for (int e = 0; e < 4; e += 2) {
+                    const float v0 = acc[a][j][4 * b + e] * f, v1 = acc[a][j][4 * b + e + 1] * f;
+                    const bool odd = threadIdx.x & 1;
+                    const float other = __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(odd ? v0 : v1), 0xB1 /* quad_perm [1, 0, 3, 2] */, 0xF, 0xF, true));
+                    T *at = to + (odd ? ld_dx - 1 : 0);
+                    if (c < d && a * 32 + b * 8 + e + (odd ? 1 : 0) < left) {
+                        Pack<T, 2> o;
+                        float lo = odd ? other : v0, hi = odd ? v1 : other;
+                        if (ACCUMULATE) { o = *(const Pack<T, 2> *)at; lo += to_f32(o.e[0]); hi += to_f32(o.e[1]); }
+                        o.e[0] = from_f32<T>(lo);
+                        o.e[1] = from_f32<T>(hi);
+                        *(Pack<T, 2> *)at = o;
                     }
-                    return;
+                    to += 2 * ld_dx;
                 }
+                return;
+            }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (c < d && a * 32 + b * 8 + e < left) {
-                        const float v = acc[a][j][4 * b + e] * f;
-                        *to = from_f32<T>(ACCUMULATE ? to_f32(*to) + v : v);
-                    }
-                    to += ld_dx;
+            for (int e = 0; e < 4; ++e) {
+                if (c < d && a * 32 + b * 8 + e < left) {
+                    const float v = acc[a][j][4 * b + e] * f;
+                    *to = from_f32<T>(ACCUMULATE ? to_f32(*to) + v : v);
                 }
-            });
+                to += ld_dx;
+            }
         });
+    };
+    if (kHasFactor<T> && apart) {
+        for (int i = 0; i < count; ++i) {
+            f32x16 acc[4][2];
+            rows_by_fp32<T>(G, (first + i) * kTileM, q, ld_q, nq, d, c0, coef, acc);
+            store(i, acc);
+        }
+        return;
+    }
+    run_tiles<H, SPLIT, true, Copies>(G, Qt, steps, count, lds, [&](int i, Copies &c) { c.seek(G, (first + i) * kTileM, Qt, c0); }, store);
 }
 
 // The part's share of dq, split over the part's rows: sums[split][nq][d] in fp32, begun (first) or added to.
@@ -298,15 +378,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_queries_kernel(Rows16 G,
 // dq = the splits' sums, in their order
 template <class T>
 __global__ __launch_bounds__(256) void grad_join_kernel(const float *__restrict__ sums, int splits, int nq, int d, float scale, int fp32, const Largest *__restrict__ largest,
-                                                        T *__restrict__ out, int64_t ld)
+                                                        const GradCoef *__restrict__ coef, T *__restrict__ out, int64_t ld)
 {
     const int64_t all = (int64_t)nq * d;
-    const float f = grad_bound(largest) * (1.0f / kGradTop) * scale * (fp32 ? 1.0f / range_scale(largest->points) : 1.0f);
+    const float f = scale * (fp32 ? 1.0f / range_scale(largest->points) : 1.0f);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
         float s = 0.0f;
 #pragma unroll 8
         for (int p = 0; p < splits; ++p) s += sums[p * all + i];
-        out[(i / d) * ld + i % d] = from_f32<T>(s * f);
+        out[(i / d) * ld + i % d] = from_f32<T>(s * coef[i / d].inverse * f);
     }
 }
 
@@ -324,7 +404,7 @@ struct ProbGradScratch {
     bool pack;
     int steps, d_steps, qw, q_steps, splits, q_tiles, d_tiles; // steps of products over dimensions, of packed rows, of products over queries
     int64_t part;                                              // rows at a time
-    Largest *largest; float2 *coef; float *sums; uint16_t *q16, *qt16, *x16, *G;
+    Largest *largest; GradCoef *coef; float *factor, *sums; uint16_t *q16, *qt16, *x16, *G;
     size_t bytes;
 };
 
@@ -354,7 +434,8 @@ static ProbGradScratch prob_grad_scratch(const ProbGradParams &p, void *base)
         return q;
     };
     s.largest = (Largest *)take(sizeof(Largest));
-    s.coef = (float2 *)take(sizeof(float2) * (size_t)p.nq);
+    s.coef = (GradCoef *)take(sizeof(GradCoef) * (size_t)p.nq);
+    s.factor = (float *)take(sizeof(float) * (size_t)p.nq);
     s.sums = (float *)take(sizeof(float) * (size_t)s.splits * p.nq * p.d);
     s.q16 = (uint16_t *)take(packed_bytes(p.nq, s.steps));
     s.qt16 = (uint16_t *)take(packed_bytes(p.d, s.q_steps));
@@ -390,7 +471,7 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
     const float c2 = p.scale * 1.44269504088896341f;
     const T *q = (const T *)p.queries;
     AVQ_TRY(launch_clear_largest(s.largest, st));
-    grad_coef_kernel<<<dim3((p.nq + 255) / 256), dim3(256), 0, st>>>(p.ids, p.n, p.nq, p.given, p.grad_logp, p.grad_entropy, p.entropy, p.grad_lse, s.coef, s.largest);
+    grad_coef_kernel<T><<<dim3((p.nq + 3) / 4), dim3(256), 0, st>>>(q, p.ld_queries, p.d, p.ids, p.n, p.nq, p.given, p.grad_logp, p.grad_entropy, p.entropy, p.grad_lse, s.coef, s.largest);
     AVQ_HIP(hipGetLastError());
     if (SPLIT) {
         AVQ_TRY(launch_largest((const float *)p.points, p.n, p.d, p.ld_points, &s.largest->points, st));
@@ -398,7 +479,13 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
     }
     const Rows16 Q = packed_rows(s.q16, p.nq), Qt = packed_rows(s.qt16, p.d);
     AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, Q, SPLIT ? &s.largest->queries : nullptr, nullptr, false, st));
-    if (p.dpoints) AVQ_TRY(launch_pack_transposed(p.queries, p.type, p.nq, p.d, p.ld_queries, s.q_steps, Qt, &s.largest->queries, st));
+    if (p.dpoints) {
+        if (kHasFactor<T>) {
+            grad_factor_kernel<<<dim3((p.nq + 255) / 256), dim3(256), 0, st>>>(s.coef, p.nq, s.largest, s.factor);
+            AVQ_HIP(hipGetLastError());
+        }
+        AVQ_TRY(launch_pack_transposed(p.queries, p.type, p.nq, p.d, p.ld_queries, s.q_steps, Qt, kHasFactor<T> ? s.factor : nullptr, st));
+    }
     for (int64_t lo = 0; lo < p.n; lo += s.part) {
         const int64_t rows = std::min<int64_t>(s.part, p.n - lo), whole = (rows + kTileN - 1) / kTileN * kTileN; // rows past the last have G = 0
         const T *x = (const T *)p.points + lo * p.ld_points;
@@ -433,7 +520,7 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
                 static LdsLimitOnce row_once;
                 AVQ_TRY(set_lds_limit((const void *)grad_rows_kernel<T, H, SPLIT, ACCUMULATE, PAIRS>, kTileLds, &row_once));
                 grad_rows_kernel<T, H, SPLIT, ACCUMULATE, PAIRS><<<dim3((unsigned)(row_parts * s.d_tiles)), dim3(kTileThreads), kTileLds, st>>>(
-                    G, Qt, steps_of<SPLIT>(p.nq), p.scale, s.largest, row_parts, s.d_tiles, rows, p.d, dx, p.ld_dpoints);
+                    G, Qt, steps_of<SPLIT>(p.nq), p.scale, s.largest, row_parts, s.d_tiles, rows, p.d, q, p.ld_queries, p.nq, s.coef, dx, p.ld_dpoints);
                 AVQ_HIP(hipGetLastError());
                 return AVQ_OK;
             };
@@ -448,7 +535,7 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         }
     }
     if (p.dqueries) {
-        grad_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(((int64_t)p.nq * p.d + 255) / 256, 1 << 22)), dim3(256), 0, st>>>(s.sums, s.splits, p.nq, p.d, p.scale, SPLIT, s.largest, (T *)p.dqueries,
+        grad_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(((int64_t)p.nq * p.d + 255) / 256, 1 << 22)), dim3(256), 0, st>>>(s.sums, s.splits, p.nq, p.d, p.scale, SPLIT, s.largest, s.coef, (T *)p.dqueries,
                                                                                                    p.ld_dqueries);
         AVQ_HIP(hipGetLastError());
     }

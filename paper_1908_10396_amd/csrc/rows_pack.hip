@@ -5,7 +5,7 @@
 
 namespace avq {
 
-__global__ void clear_largest_kernel(Largest *to) { *to = Largest{0, 0, 0, 0}; }
+__global__ void clear_largest_kernel(Largest *to) { *to = Largest{0, 0, 0, 0x7f800000u}; }
 
 int launch_clear_largest(Largest *to, hipStream_t st)
 {
@@ -278,10 +278,11 @@ int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, i
 // 64 x 64 elements a workgroup, turned in LDS
 template <class T>
 __global__ __launch_bounds__(256) void pack_transposed_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int width, Rows16 to_rows,
-                                                              const uint32_t *__restrict__ largest)
+                                                              const float *__restrict__ factor)
 {
     constexpr bool SPLIT = sizeof(T) == 4;
     __shared__ T tile[64][65];
+    __shared__ float factors[64];
     const int64_t t0 = (int64_t)blockIdx.x * 64;
     const int c0 = blockIdx.y * 64;
     for (int i = threadIdx.x; i < 4096; i += 256) {
@@ -289,25 +290,28 @@ __global__ __launch_bounds__(256) void pack_transposed_kernel(const T *__restric
         const int c = c0 + (i & 63);
         tile[i >> 6][i & 63] = t < rows && c < d ? x[t * ld + c] : T{};
     }
+    if (threadIdx.x < 64) factors[threadIdx.x] = !factor ? 1.0f : t0 + threadIdx.x < rows ? factor[t0 + threadIdx.x] : 0.0f;
     __syncthreads();
-    float s = 1.0f;
-    if constexpr (SPLIT) s = range_scale(*largest);
     for (int i = threadIdx.x; i < 4096; i += 256) {
         const int c = c0 + (i >> 6);
         const int64_t t = t0 + (i & 63);
         if (c >= d || t >= width) continue;
         uint16_t *to = (uint16_t *)to_rows.p + block16<SPLIT>(t) * to_rows.block + c * to_rows.row + turned16((int)t & 15);
-        if constexpr (SPLIT) split_f16(tile[i & 63][i >> 6] * s, to, to + to_rows.block);
-        else *to = tile[i & 63][i >> 6];
+        const float f = factors[i & 63];
+        const T v = tile[i & 63][i >> 6];
+        if constexpr (SPLIT) split_f16(f == 0.0f ? 0.0f : v * f, to, to + to_rows.block);
+        else if (!factor) *to = v.bits;
+        else *to = f == 0.0f ? 0 : from_f32<T>(to_f32(v) * f).bits;
     }
 }
 
-int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, hipStream_t st)
+int launch_pack_transposed(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const float *factor, hipStream_t st)
 {
     const int width = steps * (type == AVQ_F32 ? 16 : 32);
     const dim3 grid((unsigned)((width + 63) / 64), (unsigned)((d + 63) / 64));
-    if (type == AVQ_F32) pack_transposed_kernel<float><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, width, to, largest);
-    else pack_transposed_kernel<uint16_t><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, width, to, nullptr);
+    if (type == AVQ_F32) pack_transposed_kernel<float><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, width, to, factor);
+    else if (type == AVQ_F16) pack_transposed_kernel<f16_t><<<grid, dim3(256), 0, st>>>((const f16_t *)x, rows, d, ld, width, to, factor);
+    else pack_transposed_kernel<bf16_t><<<grid, dim3(256), 0, st>>>((const bf16_t *)x, rows, d, ld, width, to, factor);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }

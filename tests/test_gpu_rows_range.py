@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 avq = pytest.importorskip("paper_1908_10396_amd")
 
-from test_gpu_rows import TYPES, U, _check_probs, _grad_formula, gen, normal, random_ids, within  # noqa: E402
+from test_gpu_rows import HALF, TINY, TYPES, U, _check_probs, _grad_formula, gen, normal, random_ids, within  # noqa: E402
 
 
 def grid(x, kind):
@@ -150,6 +150,66 @@ def test_log_probs_beside_rows_of_large_masks(kind, value, nq, share):
 @pytest.mark.parametrize("value", [-1e7, -1e12, -1e30])
 def test_log_probs_of_fp32_rows_behind_thousands_of_large_masks(nq, value):
     test_log_probs_of_rows_behind_thousands_of_large_masks("f32", nq, value)
+
+
+def _gradient_of_weighted(x, q, scale, ids, up, kind):
+    """The gradient of the loss in 64 bits; bounds as in _grad_formula, but what G is kept down to is relative to its own query's
+    upstream gradient."""
+    n = x.shape[0]
+    xd, qd = x.double(), q.double()
+    s32 = abs(torch.tensor(scale, dtype=torch.float32).item())
+    s = qd @ xd.t() * s32
+    e = ((x.shape[1] + 8) * U * (qd.abs() @ xd.abs().t()) + 1e-30) * s32
+    logp = s - torch.logsumexp(s, 1)[:, None]
+    w = up.double()[:, None]
+    one = torch.nn.functional.one_hot(ids.long(), n).double()
+    G = w * (one - logp.exp())
+    e_p = e + e.amax(1, keepdim=True) + (n / 64 + 96) * U + 8 * U * (s.abs().amax(1, keepdim=True) + logp.abs())
+    e_G = w.abs() * (one + logp.exp()) * (4 * e_p + 16 * U) + {"f32": 2.0 ** -21, "bf16": 2.0 ** -8, "f16": 2.0 ** -10}[kind] * G.abs()
+    if kind != "bf16":
+        e_G = e_G + 2.0 ** -36 * w.abs()
+    want_q, want_x = G @ xd * scale, G.t() @ qd * scale
+    bound_q = s32 * (e_G @ xd.abs() + (min(n, 4096) + 64) * U * (G.abs() @ xd.abs()))
+    bound_x = s32 * (e_G.t() @ qd.abs() + (q.shape[0] + 64) * U * (G.abs().t() @ qd.abs()))
+    return want_q, bound_q + HALF[kind] * want_q.abs() * 1.01 + TINY[kind], want_x, bound_x + HALF[kind] * want_x.abs() * 1.01 + TINY[kind]
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [7, 33, 70, 300])
+@pytest.mark.parametrize("least", [1e-4, 1e-8])
+def test_gradients_of_queries_of_unequal_weight(kind, nq, least):
+    """Upstream gradients between `least` and 1: each query's gradient is as exact as if it were alone."""
+    g = gen(nq)
+    n, d, scale = 20_000, 64, 0.25
+    x, q = normal((n, d), g, TYPES[kind]), normal((nq, d), g, TYPES[kind])
+    ids = torch.randint(0, n, (nq,), generator=g, device="cuda", dtype=torch.int32)
+    up = -torch.exp(math.log(least) * torch.rand((nq,), generator=g, device="cuda"))
+    up[0], up[-1] = -1.0, -least
+    r = avq.log_probs(x, q, ids, scale=scale)
+    # results large enough for their type: a common power of two, which changes no bound but by itself
+    up = up * 2.0 ** 12
+    want_q, bound_q, want_x, bound_x = _gradient_of_weighted(x, q, scale, ids, up, kind)
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, scale=scale)
+    within(dq, want_q, bound_q, "dqueries")
+    within(dx, want_x, bound_x, "dpoints")
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [33, 70])
+def test_queries_without_upstream_gradient_beside_others(kind, nq):
+    g = gen(nq)
+    n, d, scale = 3000, 64, 0.25
+    x, q = normal((n, d), g, TYPES[kind]), normal((nq, d), g, TYPES[kind])
+    ids = torch.randint(0, n, (nq,), generator=g, device="cuda", dtype=torch.int32)
+    up = torch.where(torch.arange(nq, device="cuda") % 3 == 0, 0.0, 1e-3)
+    r = avq.log_probs(x, q, ids, scale=scale)
+    want_q, bound_q, want_x, bound_x = _gradient_of_weighted(x, q, scale, ids, up, kind)
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, scale=scale)
+    within(dq, want_q, bound_q, "dqueries")
+    within(dx, want_x, bound_x, "dpoints")
+    assert not bool(dq[::3].any())
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, torch.zeros_like(up), scale=scale)
+    assert not bool(dq.any()) and not bool(dx.any())
 
 
 @pytest.mark.parametrize("nq", [1, 2, 4, 7])
