@@ -291,9 +291,9 @@ __host__ __device__ inline void part_tiles(int64_t tiles, int parts, int p, int6
 }
 
 // ---- rows_pack.hip -------------------------------------------------------------------------
-// Largest finite magnitudes, as bits of non-negative floats (0: nothing yet); weighted: of queries over their factor in G, and the least
-// that a query has of them (infinity: nothing yet).
-struct Largest { uint32_t points, queries, weighted, least_weighted; };
+// Ranges, as bits of non-negative floats (0, for the least infinity: nothing yet): of the rows' inverses, of the largest magnitudes that
+// queries have over their factor in G; and how many rows are odd.
+struct Ranges { uint32_t inverse, least_inverse, weighted, least_weighted, odd; };
 
 // the power of two that brings a largest magnitude to 2^14 .. 2^15 (1 where there is none)
 __device__ __forceinline__ float range_scale(uint32_t largest_bits)
@@ -318,17 +318,20 @@ __device__ __forceinline__ float scale_of_inverse(float inv) { return kRowUnit /
 // are marked, and have no sum that is a number. A query that is not finite itself has zeros, and NaN for an inverse.
 struct OddRows { uint32_t *count, *rows, *seen; }; // how many, which (in any order), [queries] whether marked
 
-int launch_clear_largest(Largest *to, hipStream_t st);
+int launch_clear_ranges(Ranges *to, hipStream_t st);
+// The same where a product adds rows up, so that they need one scale: inv[row] is the table's where its rows' largest magnitudes lie within
+// kTableSpread of one another (pairs then hold the least of them to 2^-24), and the row's own where they do not; odd rows are counted.
+constexpr float kTableSpread = 0x1p16f;
+__device__ __forceinline__ bool rows_apart(const Ranges *ranges) { return __uint_as_float(ranges->inverse) > kTableSpread * __uint_as_float(ranges->least_inverse); }
+int launch_common_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, Ranges *ranges, hipStream_t st);
 // inv[row] = kRowUnit / s of each row, and tile_inv[tile] that of the tile's rows where they have one, else 0
 int launch_row_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, float *tile_inv, const OddRows &odd, hipStream_t st);
 // marks the queries (negate: with the other sign) whose product with an odd row is not -infinity
 int launch_odd_rows(const float *x, int d, int64_t ld, const float *q, int nq, int64_t ld_q, bool negate, const OddRows &odd, hipStream_t st);
-// max over finite elements into *to
-int launch_largest(const float *x, int64_t rows, int d, int64_t ld, uint32_t *to, hipStream_t st);
-// Rows laid out as `to` says (to.p: where), `steps` steps of them, zeros past a row's end. fp32: pairs, scaled by
-// range_scale(*largest), or, largest == NULL, each row by its own, of which inv[row] is the inverse. negate: with the other sign.
-int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, const float *inv, bool negate, hipStream_t st);
-// fp32 queries: pairs, each row by its own scale, whose inverse goes to inv[row]. Also begins `odd`: no rows, no marks.
+// Rows laid out as `to` says (to.p: where), `steps` steps of them, zeros past a row's end. fp32: pairs, by scales of which inv[row] is the
+// inverse. negate: with the other sign.
+int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const float *inv, bool negate, hipStream_t st);
+// fp32 queries: pairs, each row by its own scale, whose inverse goes to inv[row]. Also begins `odd` where there is one: no rows, no marks.
 int launch_pack_queries(const float *q, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, float *inv, const OddRows &odd, bool negate, hipStream_t st);
 // The transpose packed: row c < d of d holds x[t][c] factor[t] (factor == NULL: x[t][c]), 16 t in the order of turned16, zeros past the
 // last t and where the factor is 0.

@@ -811,7 +811,7 @@ static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
         AVQ_TRY(launch_row_inverses((const float *)p.points, p.n, p.d, p.ld_points, s.x_inv, s.tile_inv, s.odd, st));
         AVQ_TRY(launch_odd_rows((const float *)p.points, p.d, p.ld_points, (const float *)p.queries, p.nq, p.ld_queries, p.scale < 0.0f, s.odd, st));
     } else {
-        AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, Q, nullptr, nullptr, p.scale < 0.0f, st));
+        AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, Q, nullptr, p.scale < 0.0f, st));
     }
     static LdsLimitOnce with_best, without;
     for (int i = 0; i < s.launches; ++i) {
@@ -820,7 +820,7 @@ static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
         Rows16 X{(const uint16_t *)from, p.ld_points, 16, rows};
         if (s.pack) {
             X = SPLIT ? packed_rows(s.x16, rows) : Rows16{s.x16, (int64_t)s.steps * 32, 16, rows};
-            AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, s.steps, X, nullptr, SPLIT ? s.x_inv + lo : nullptr, false, st));
+            AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, s.steps, X, SPLIT ? s.x_inv + lo : nullptr, false, st));
         }
         float4 *stats = s.stats + (size_t)i * s.parts * 2 * p.nq;
         const float *x_inv = SPLIT ? s.x_inv + lo : nullptr, *tile_inv = SPLIT ? s.tile_inv + lo / kTileM : nullptr;

@@ -26,16 +26,16 @@ struct GradCoef { float a, h, factor, inverse; }; // (inverse 0: nothing comes f
 constexpr float kWeightSpread = 0x1p16f;
 template <class T> constexpr bool kHasFactor = std::is_same<T, float>::value || std::is_same<T, f16_t>::value;
 
-template <class T> __device__ __forceinline__ bool weights_apart(const Largest *largest)
+template <class T> __device__ __forceinline__ bool weights_apart(const Ranges *ranges)
 {
-    return kHasFactor<T> && __uint_as_float(largest->weighted) > kWeightSpread * __uint_as_float(largest->least_weighted);
+    return kHasFactor<T> && __uint_as_float(ranges->weighted) > kWeightSpread * __uint_as_float(ranges->least_weighted);
 }
 
 // A wave a query: a_t, h_t, the factor, and the range of what dx adds up.
 template <class T>
 __global__ __launch_bounds__(256) void grad_coef_kernel(const T *__restrict__ q, int64_t ld_q, int d, const int32_t *__restrict__ ids, int64_t n, int nq, int given,
                                                         const float *__restrict__ g, const float *__restrict__ h, const float *__restrict__ entropy, const float *__restrict__ gl,
-                                                        GradCoef *__restrict__ coef, Largest *__restrict__ largest)
+                                                        GradCoef *__restrict__ coef, Ranges *__restrict__ ranges)
 {
     const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (t >= nq) return;
@@ -71,15 +71,15 @@ __global__ __launch_bounds__(256) void grad_coef_kernel(const T *__restrict__ q,
     const uint32_t weighted = __float_as_uint(__uint_as_float(top) / factor);
     if (weighted >= 0x7f800000u) return;
     // (maxima and minima: no order matters; asked for first, since most change nothing)
-    if (weighted > __hip_atomic_load(&largest->weighted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(&largest->weighted, weighted);
-    if (weighted < __hip_atomic_load(&largest->least_weighted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMin(&largest->least_weighted, weighted);
+    if (weighted > __hip_atomic_load(&ranges->weighted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(&ranges->weighted, weighted);
+    if (weighted < __hip_atomic_load(&ranges->least_weighted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMin(&ranges->least_weighted, weighted);
 }
 
 // what the transposed queries are multiplied by
-__global__ __launch_bounds__(256) void grad_factor_kernel(const GradCoef *__restrict__ coef, int nq, const Largest *__restrict__ largest, float *__restrict__ factor)
+__global__ __launch_bounds__(256) void grad_factor_kernel(const GradCoef *__restrict__ coef, int nq, const Ranges *__restrict__ ranges, float *__restrict__ factor)
 {
     const int t = blockIdx.x * 256 + threadIdx.x;
-    if (t < nq) factor[t] = coef[t].inverse == 0.0f ? 0.0f : range_scale(largest->weighted) * coef[t].inverse;
+    if (t < nq) factor[t] = coef[t].inverse == 0.0f ? 0.0f : range_scale(ranges->weighted) * coef[t].inverse;
 }
 
 // eight values as operands: rounded to the type, or (fp32) hi and lo
@@ -103,37 +103,51 @@ __device__ __forceinline__ void put_once(uint16_t *to, const Quad &v)
 
 // G^T of the part's rows: 256 queries of a workgroup by 128 rows at a time. T: the caller's type, H: the instructions'.
 template <class T, class H, bool SPLIT, bool ENTROPY>
-__global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Rows16 X, int steps, float c2, const float *__restrict__ lse, const GradCoef *__restrict__ coef,
-                                                                    const Largest *__restrict__ largest, int parts, int others, Rows16 G, int width)
+__global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Rows16 X, int steps, float c2, const float *__restrict__ x_inv, const float *__restrict__ q_inv, const float *__restrict__ lse, const GradCoef *__restrict__ coef,
+                                                                    const Ranges *__restrict__ ranges, int parts, int others, Rows16 G, int width)
 {
     extern __shared__ char lds[];
     __shared__ float4 shift[kTileM / 4], up[kTileM / 4], up_h[kTileM / 4]; // -lse / log 2; a and h, times the factor
+    __shared__ float4 to_logit[SPLIT ? kTileM / 4 : 1];
     const Place place = place_of(blockIdx.x, others);
     const int wave = threadIdx.x >> 6, half = (threadIdx.x & 63) >> 5;
     const int64_t tiles = (X.rows + kTileN - 1) / kTileN, q0 = (int64_t)place.other * kTileM;
     int64_t first;
     int count;
     part_tiles(tiles, parts, place.part, &first, &count);
+    const bool apart = SPLIT && rows_apart(ranges), odd = SPLIT && ranges->odd > 0;
     {
         const int64_t t = q0 + threadIdx.x;
         const bool real = t < Q.rows; // (queries past the last have the last one's products: a probability of 0 all the same)
         const GradCoef c = real ? coef[t] : GradCoef{0.0f, 0.0f, 1.0f, 0.0f};
         ((float *)shift)[threadIdx.x] = real ? -lse[t] * 1.44269504088896341f : -INFINITY;
+        if (SPLIT) ((float *)to_logit)[threadIdx.x] = real ? c2 * q_inv[t] * (apart ? 1.0f : __uint_as_float(ranges->inverse)) : 0.0f;
         ((float *)up)[threadIdx.x] = -c.a * c.factor;
         if (ENTROPY) ((float *)up_h)[threadIdx.x] = -c.h * c.factor * 0.693147180559945309f;
     }
-    const float cq = SPLIT ? c2 * (1.0f / range_scale(largest->points)) * (1.0f / range_scale(largest->queries)) : c2;
     __syncthreads();
     typedef RowCopies<true, SPLIT> Copies;
     run_tiles<H, SPLIT, true, Copies>(Q, X, steps, count, lds, [&](int i, Copies &c) { c.seek(Q, q0, X, (first + i) * kTileN); },
         [&](int i, f32x16 (&acc)[4][2]) {
             const int64_t row0 = (first + i) * kTileN;
+            bool none[2] = {false, false}; // odd rows: no gradient
+            if (SPLIT && (apart || odd)) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float inv = x_inv[min(row0 + acc_col(j), X.rows - 1)];
+                    none[j] = inv == INFINITY;
+#pragma unroll
+                    for (int a = 0; a < 4; ++a)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[a][j][r] *= apart && !none[j] ? inv : 1.0f;
+                }
+            }
             auto take = [&](auto tail) __attribute__((always_inline)) {
-                constexpr bool TAIL = decltype(tail)::value; // some rows are past the last: no gradient
+                constexpr bool TAIL = decltype(tail)::value; // some rows are past the last, or odd: no gradient
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const int64_t row = row0 + acc_col(j);
-                    const bool real = !TAIL || row < X.rows;
+                    const bool real = !TAIL || (row < X.rows && !none[j]);
 #pragma unroll
                     for (int a = 0; a < 4; ++a)
 #pragma unroll
@@ -146,10 +160,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
                                 const float4 s4 = shift[t / 4], u4 = up[t / 4];
                                 const float sh[4] = {s4.x, s4.y, s4.z, s4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
                                 float hh[4] = {};
+                                float cq[4] = {c2, c2, c2, c2};
+                                if (SPLIT) { const float4 w = to_logit[t / 4]; cq[0] = w.x; cq[1] = w.y; cq[2] = w.z; cq[3] = w.w; }
                                 if (ENTROPY) { const float4 w = up_h[t / 4]; hh[0] = w.x; hh[1] = w.y; hh[2] = w.z; hh[3] = w.w; }
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
-                                    const float s2 = __fmaf_rn(acc[a][j][8 * block + 4 * b + e], cq, sh[e]), p = __builtin_amdgcn_exp2f(s2);
+                                    const float s2 = __fmaf_rn(acc[a][j][8 * block + 4 * b + e], cq[e], sh[e]), p = __builtin_amdgcn_exp2f(s2);
                                     float g = p * (ENTROPY ? __fmaf_rn(hh[e], s2, u[e]) : u[e]);
                                     if (ENTROPY && p == 0.0f) g = 0.0f; // (p log p)
                                     v[4 * b + e] = real ? g : 0.0f;
@@ -166,7 +182,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
                         }
                 }
             };
-            if (row0 + kTileN <= X.rows) take(std::false_type{});
+            if (row0 + kTileN <= X.rows && !(SPLIT && __any(none[0] || none[1]))) take(std::false_type{});
             else take(std::true_type{});
         });
 }
@@ -178,18 +194,10 @@ constexpr int64_t kGivenGroups = 1 << 22; // a launch has fewer than 2^32 thread
 template <int PATH, class T>
 __global__ __launch_bounds__(64) void grad_given_kernel(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, int d, float scale, int row_lanes,
                                                         const int32_t *__restrict__ ids, int given, const float *__restrict__ g, const float *__restrict__ lse,
-                                                        const GradCoef *__restrict__ coef, const Largest *__restrict__ largest, int64_t lo, int64_t rows, Rows16 G)
+                                                        const GradCoef *__restrict__ coef, const float *__restrict__ x_inv, const float *__restrict__ q_inv, int64_t lo, int64_t rows, Rows16 G)
 {
     extern __shared__ char lds[];
     T *qs = (T *)lds;
-    float c = scale;
-    Scoring how{row_lanes, 1.0f};
-    float x_inv = 1.0f;
-    if (PATH == kByTiles && sizeof(T) == 4) {
-        x_inv = kRowUnit / range_scale(largest->points);
-        how.q_scale = range_scale(largest->queries);
-        c = c * (1.0f / (kRowUnit * how.q_scale));
-    }
     for (int64_t i = blockIdx.x; i < (int64_t)nq * given; i += gridDim.x) {
         const int64_t t = i / given, j = i - t * given;
         const int64_t id = ids[i];
@@ -203,12 +211,19 @@ __global__ __launch_bounds__(64) void grad_given_kernel(const T *__restrict__ x,
             }
         if (__any(earlier)) continue;
         sum = group_sum<64>(sum);
+        float c = scale;
+        Scoring how{row_lanes, 1.0f};
+        if (PATH == kByTiles && sizeof(T) == 4) {
+            how.q_scale = 1.0f / (kRowUnit * q_inv[t]);
+            c = c * q_inv[t];
+        }
         __syncthreads(); // (the query before has been read)
         stage_query(qs, q + t * ld_q, d, false, 64);
         __syncthreads();
-        score_rows<PATH, 8>(qs, d, how, [&](int) { return x + id * ld_x; }, [&](int) { return x_inv; }, [&](int slot, float product) {
+        score_rows<PATH, 8>(qs, d, how, [&](int) { return x + id * ld_x; }, [&](int) { return x_inv[id]; }, [&](int slot, float product) {
             if (slot != 0) return;
-            const float logp = __fmaf_rn(product, c, -lse[t]);
+            const bool odd = PATH == kByTiles && sizeof(T) == 4 && x_inv[id] == INFINITY; // (a logit of -infinity, whatever the scale's sign)
+            const float logp = odd ? -INFINITY : __fmaf_rn(product, c, -lse[t]);
             const GradCoef k = coef[t];
             const float p = __builtin_amdgcn_exp2f(logp * 1.44269504088896341f);
             f32x8 one = {};
@@ -278,7 +293,7 @@ __device__ __forceinline__ void rows_by_fp32(const Rows16 &G, int64_t row0, cons
 // dx of the part's rows: 256 rows by 128 dimensions.
 // PAIRS: 16-bit types of rows on 4 bytes, of an even number of elements.
 template <class T, class H, bool SPLIT, bool ACCUMULATE, bool PAIRS>
-__global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Rows16 Qt, int steps, float scale, const Largest *__restrict__ largest, int parts, int others, int64_t rows,
+__global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Rows16 Qt, int steps, float scale, const Ranges *__restrict__ ranges, int parts, int others, int64_t rows,
                                                                     int d, const T *__restrict__ q, int64_t ld_q, int nq, const GradCoef *__restrict__ coef, T *__restrict__ dx, int64_t ld_dx)
 {
     extern __shared__ char lds[];
@@ -287,8 +302,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Ro
     int64_t first;
     int count;
     part_tiles(tiles, parts, place.part, &first, &count);
-    const bool apart = weights_apart<T>(largest);
-    const float f = kHasFactor<T> && !apart ? scale * (1.0f / range_scale(largest->weighted)) : scale;
+    const bool apart = weights_apart<T>(ranges);
+    const float f = kHasFactor<T> && !apart ? scale * (1.0f / range_scale(ranges->weighted)) : scale;
     typedef RowCopies<true, true> Copies;
     auto store = [&](int i, f32x16 (&acc)[4][2]) __attribute__((always_inline)) {
         const int64_t row0 = (first + i) * kTileM + acc_row(0, 0);
@@ -338,9 +353,47 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Ro
     run_tiles<H, SPLIT, true, Copies>(G, Qt, steps, count, lds, [&](int i, Copies &c) { c.seek(G, (first + i) * kTileM, Qt, c0); }, store);
 }
 
-// The part's share of dq, split over the part's rows: sums[split][nq][d] in fp32, begun (first) or added to.
+// A tile of dq by the fp32 matrix instruction, 16 rows [row0, row0 + 16 steps) at a time, of which x has `rows`; acc as the other form has it.
+__device__ __forceinline__ void queries_by_fp32(const Rows16 &G, int64_t t0, int width, const float *__restrict__ x, int64_t ld_x, int64_t rows, int64_t row0, int steps, int d, int64_t c0,
+                                                f32x16 (&acc)[4][2])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const uint16_t *g[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t p = t0 + (wave >> 1) * 128 + i * 32 + (lane & 31), at = p < width ? p : 0; // (places past the last are not stored)
+        g[i] = G.p + block16<true>(at) * G.block + (at & 15);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    }
+    for (int s = 0; s < steps; ++s) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int64_t row = row0 + (int64_t)s * 16 + half * 8 + e, at = min(row, rows - 1);
+            float ga[4], b[2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ga[i] = row < rows ? to_f32(f16_t{g[i][at * G.row]}) + to_f32(f16_t{g[i][G.block + at * G.row]}) : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int64_t c = c0 + (wave & 1) * 64 + j * 32 + (lane & 31);
+                const float v = c < d ? x[at * ld_x + c] : 0.0f;
+                b[j] = fabsf(v) < INFINITY ? v : 0.0f; // (as zeros stand for odd rows among the pairs)
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(ga[i], b[j], acc[i][j], 0, 0, 0);
+        }
+    }
+}
+
+// The part's share of dq, split over the part's rows: sums[split][nq][d] in fp32, begun (first) or added to. x: the part's rows as they
+// are, for fp32 tables whose rows are apart.
 template <class H, bool SPLIT>
-__global__ __launch_bounds__(kTileThreads, 2) void grad_queries_kernel(Rows16 G, Rows16 X, int nq, int width, int d, int splits, int q_tiles, int d_tiles, int begin, float *__restrict__ sums)
+__global__ __launch_bounds__(kTileThreads, 2) void grad_queries_kernel(Rows16 G, Rows16 X, int nq, int width, int d, int splits, int q_tiles, int d_tiles, int begin, const float *__restrict__ x,
+                                                                       int64_t ld_x, const Ranges *__restrict__ ranges, float *__restrict__ sums)
 {
     extern __shared__ char lds[];
     const Place place = place_of(blockIdx.x, q_tiles * d_tiles);
@@ -372,16 +425,22 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_queries_kernel(Rows16 G,
         if (begin) store(0, none);
         return;
     }
+    if (SPLIT && rows_apart(ranges)) {
+        f32x16 acc[4][2];
+        queries_by_fp32(G, t0, width, x, ld_x, X.rows, first * Copies::kRows, count, d, c0, acc);
+        store(0, acc);
+        return;
+    }
     run_tiles<H, SPLIT, true, Copies>(G, X, count, 1, lds, [&](int, Copies &c) { c.row = first * Copies::kRows; c.seek(G, t0, width, X, c0); }, store);
 }
 
 // dq = the splits' sums, in their order
 template <class T>
-__global__ __launch_bounds__(256) void grad_join_kernel(const float *__restrict__ sums, int splits, int nq, int d, float scale, int fp32, const Largest *__restrict__ largest,
+__global__ __launch_bounds__(256) void grad_join_kernel(const float *__restrict__ sums, int splits, int nq, int d, float scale, int fp32, const Ranges *__restrict__ ranges,
                                                         const GradCoef *__restrict__ coef, T *__restrict__ out, int64_t ld)
 {
     const int64_t all = (int64_t)nq * d;
-    const float f = scale * (fp32 ? 1.0f / range_scale(largest->points) : 1.0f);
+    const float f = scale * (fp32 && !rows_apart(ranges) ? __uint_as_float(ranges->inverse) * (1.0f / kRowUnit) : 1.0f);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
         float s = 0.0f;
 #pragma unroll 8
@@ -404,7 +463,7 @@ struct ProbGradScratch {
     bool pack;
     int steps, d_steps, qw, q_steps, splits, q_tiles, d_tiles; // steps of products over dimensions, of packed rows, of products over queries
     int64_t part;                                              // rows at a time
-    Largest *largest; GradCoef *coef; float *factor, *sums; uint16_t *q16, *qt16, *x16, *G;
+    Ranges *ranges; GradCoef *coef; float *factor, *x_inv, *q_inv, *sums; uint16_t *q16, *qt16, *x16, *G;
     size_t bytes;
 };
 
@@ -433,9 +492,11 @@ static ProbGradScratch prob_grad_scratch(const ProbGradParams &p, void *base)
         at += (bytes + 255) & ~(size_t)255;
         return q;
     };
-    s.largest = (Largest *)take(sizeof(Largest));
+    s.ranges = (Ranges *)take(sizeof(Ranges));
     s.coef = (GradCoef *)take(sizeof(GradCoef) * (size_t)p.nq);
     s.factor = (float *)take(sizeof(float) * (size_t)p.nq);
+    s.x_inv = split ? (float *)take(sizeof(float) * (size_t)p.n) : nullptr;
+    s.q_inv = split ? (float *)take(sizeof(float) * (size_t)p.nq) : nullptr;
     s.sums = (float *)take(sizeof(float) * (size_t)s.splits * p.nq * p.d);
     s.q16 = (uint16_t *)take(packed_bytes(p.nq, s.steps));
     s.qt16 = (uint16_t *)take(packed_bytes(p.d, s.q_steps));
@@ -470,18 +531,19 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
     AVQ_TRY(set_lds_limit((const void *)grad_queries_kernel<H, SPLIT>, kTileLds, &once[2]));
     const float c2 = p.scale * 1.44269504088896341f;
     const T *q = (const T *)p.queries;
-    AVQ_TRY(launch_clear_largest(s.largest, st));
-    grad_coef_kernel<T><<<dim3((p.nq + 3) / 4), dim3(256), 0, st>>>(q, p.ld_queries, p.d, p.ids, p.n, p.nq, p.given, p.grad_logp, p.grad_entropy, p.entropy, p.grad_lse, s.coef, s.largest);
+    AVQ_TRY(launch_clear_ranges(s.ranges, st));
+    grad_coef_kernel<T><<<dim3((p.nq + 3) / 4), dim3(256), 0, st>>>(q, p.ld_queries, p.d, p.ids, p.n, p.nq, p.given, p.grad_logp, p.grad_entropy, p.entropy, p.grad_lse, s.coef, s.ranges);
     AVQ_HIP(hipGetLastError());
-    if (SPLIT) {
-        AVQ_TRY(launch_largest((const float *)p.points, p.n, p.d, p.ld_points, &s.largest->points, st));
-        AVQ_TRY(launch_largest((const float *)p.queries, p.nq, p.d, p.ld_queries, &s.largest->queries, st));
-    }
     const Rows16 Q = packed_rows(s.q16, p.nq), Qt = packed_rows(s.qt16, p.d);
-    AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, Q, SPLIT ? &s.largest->queries : nullptr, nullptr, false, st));
+    if (SPLIT) {
+        AVQ_TRY(launch_pack_queries((const float *)p.queries, p.nq, p.d, p.ld_queries, s.steps, Q, s.q_inv, OddRows{}, false, st));
+        AVQ_TRY(launch_common_inverses((const float *)p.points, p.n, p.d, p.ld_points, s.x_inv, s.ranges, st));
+    } else {
+        AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, Q, nullptr, false, st));
+    }
     if (p.dpoints) {
         if (kHasFactor<T>) {
-            grad_factor_kernel<<<dim3((p.nq + 255) / 256), dim3(256), 0, st>>>(s.coef, p.nq, s.largest, s.factor);
+            grad_factor_kernel<<<dim3((p.nq + 255) / 256), dim3(256), 0, st>>>(s.coef, p.nq, s.ranges, s.factor);
             AVQ_HIP(hipGetLastError());
         }
         AVQ_TRY(launch_pack_transposed(p.queries, p.type, p.nq, p.d, p.ld_queries, s.q_steps, Qt, kHasFactor<T> ? s.factor : nullptr, st));
@@ -492,18 +554,19 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         Rows16 X{(const uint16_t *)x, p.ld_points, 16, rows};
         if (s.pack) {
             X = SPLIT ? packed_rows(s.x16, rows) : Rows16{s.x16, (int64_t)s.d_steps * 32, 16, rows};
-            AVQ_TRY(launch_pack_rows(x, p.type, rows, p.d, p.ld_points, s.d_steps, X, SPLIT ? &s.largest->points : nullptr, nullptr, false, st));
+            AVQ_TRY(launch_pack_rows(x, p.type, rows, p.d, p.ld_points, s.d_steps, X, SPLIT ? s.x_inv + lo : nullptr, false, st));
         }
         const Rows16 G = packed_rows(s.G, whole);
         const int parts = parts_for((rows + kTileN - 1) / kTileN, s.q_tiles, kGradGroups);
         const dim3 grid((unsigned)(parts * s.q_tiles));
-        if (p.grad_entropy) grad_tile_kernel<T, H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, s.steps, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, G, s.qw);
-        else grad_tile_kernel<T, H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, s.steps, c2, p.lse, s.coef, s.largest, parts, s.q_tiles, G, s.qw);
+        const float *x_inv = SPLIT ? s.x_inv + lo : nullptr;
+        if (p.grad_entropy) grad_tile_kernel<T, H, SPLIT, true><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, s.steps, c2, x_inv, s.q_inv, p.lse, s.coef, s.ranges, parts, s.q_tiles, G, s.qw);
+        else grad_tile_kernel<T, H, SPLIT, false><<<grid, dim3(kTileThreads), kTileLds, st>>>(Q, X, s.steps, c2, x_inv, s.q_inv, p.lse, s.coef, s.ranges, parts, s.q_tiles, G, s.qw);
         AVQ_HIP(hipGetLastError());
         if (p.given > 0) {
             auto run = [&](auto kernel) {
                 kernel<<<dim3((unsigned)std::min((int64_t)p.nq * p.given, kGivenGroups)), dim3(64), staged_query_bytes(p.d), st>>>((const T *)p.points, p.ld_points, q, p.nq, p.ld_queries, p.d, p.scale, row_lanes(sizeof(T), p.d),
-                                                                                                    p.ids, p.given, p.grad_logp, p.lse, s.coef, s.largest, lo, rows, G);
+                                                                                                    p.ids, p.given, p.grad_logp, p.lse, s.coef, s.x_inv, s.q_inv, lo, rows, G);
             };
             const int path = prob_path(sizeof(T), p.d, p.nq);
             if (path == kByTiles) run(grad_given_kernel<kByTiles, T>);
@@ -520,7 +583,7 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
                 static LdsLimitOnce row_once;
                 AVQ_TRY(set_lds_limit((const void *)grad_rows_kernel<T, H, SPLIT, ACCUMULATE, PAIRS>, kTileLds, &row_once));
                 grad_rows_kernel<T, H, SPLIT, ACCUMULATE, PAIRS><<<dim3((unsigned)(row_parts * s.d_tiles)), dim3(kTileThreads), kTileLds, st>>>(
-                    G, Qt, steps_of<SPLIT>(p.nq), p.scale, s.largest, row_parts, s.d_tiles, rows, p.d, q, p.ld_queries, p.nq, s.coef, dx, p.ld_dpoints);
+                    G, Qt, steps_of<SPLIT>(p.nq), p.scale, s.ranges, row_parts, s.d_tiles, rows, p.d, q, p.ld_queries, p.nq, s.coef, dx, p.ld_dpoints);
                 AVQ_HIP(hipGetLastError());
                 return AVQ_OK;
             };
@@ -530,12 +593,12 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         }
         if (p.dqueries) {
             grad_queries_kernel<H, SPLIT><<<dim3((unsigned)(s.splits * s.q_tiles * s.d_tiles)), dim3(kTileThreads), kTileLds, st>>>(G, X, p.nq, s.qw, p.d, s.splits, s.q_tiles, s.d_tiles,
-                                                                                                                             lo == 0, s.sums);
+                                                                                                                             lo == 0, (const float *)x, p.ld_points, s.ranges, s.sums);
             AVQ_HIP(hipGetLastError());
         }
     }
     if (p.dqueries) {
-        grad_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(((int64_t)p.nq * p.d + 255) / 256, 1 << 22)), dim3(256), 0, st>>>(s.sums, s.splits, p.nq, p.d, p.scale, SPLIT, s.largest, s.coef, (T *)p.dqueries,
+        grad_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(((int64_t)p.nq * p.d + 255) / 256, 1 << 22)), dim3(256), 0, st>>>(s.sums, s.splits, p.nq, p.d, p.scale, SPLIT, s.ranges, s.coef, (T *)p.dqueries,
                                                                                                    p.ld_dqueries);
         AVQ_HIP(hipGetLastError());
     }

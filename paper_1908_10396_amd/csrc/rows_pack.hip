@@ -1,69 +1,15 @@
 // Rows laid out as operands of the 16-bit matrix instructions (mma_tiles.h): padded, and fp32 as pairs of f16.
-// Bound by memory: rows read once, operands written once (1,183,514 x 100 fp32 to pairs: 177 us for 473 + 530 MB, 5.7 TB/s; the largest
-// magnitude before it 84 us, 5.6 TB/s).
+// Bound by memory: rows read once, operands written once (1,183,514 x 100 fp32 to pairs: 182 us for 473 + 530 MB, 5.5 TB/s; the rows'
+// largest magnitudes before it 88 us, 5.4 TB/s).
 #include "mma_tiles.h"
 
 namespace avq {
 
-__global__ void clear_largest_kernel(Largest *to) { *to = Largest{0, 0, 0, 0x7f800000u}; }
+__global__ void clear_ranges_kernel(Ranges *to) { *to = Ranges{0, 0x7f800000u, 0, 0x7f800000u, 0}; }
 
-int launch_clear_largest(Largest *to, hipStream_t st)
+int launch_clear_ranges(Ranges *to, hipStream_t st)
 {
-    clear_largest_kernel<<<dim3(1), dim3(1), 0, st>>>(to);
-    AVQ_HIP(hipGetLastError());
-    return AVQ_OK;
-}
-
-__device__ __forceinline__ uint32_t finite_bits(float v)
-{
-    const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
-    return b < 0x7f800000u ? b : 0u;
-}
-
-template <int V>
-__global__ __launch_bounds__(256) void largest_kernel(const float *__restrict__ x, int64_t rows, int per_row, int64_t ld, uint32_t *__restrict__ to)
-{
-    uint32_t m = 0;
-    if (ld == (int64_t)per_row * V) { // dense: one long row
-        const int64_t all = rows * per_row, step = (int64_t)gridDim.x * 256;
-        int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-        for (; i + 3 * step < all; i += 4 * step) {
-            Pack<float, V> v[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = *(const Pack<float, V> *)(x + (i + u * step) * V);
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int e = 0; e < V; ++e) m = max(m, finite_bits(v[u].e[e]));
-        }
-        for (; i < all; i += step) {
-            const Pack<float, V> v = *(const Pack<float, V> *)(x + i * V);
-#pragma unroll
-            for (int e = 0; e < V; ++e) m = max(m, finite_bits(v.e[e]));
-        }
-    } else {
-        for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-            for (int c = threadIdx.x; c < per_row; c += 256) {
-                const Pack<float, V> v = *(const Pack<float, V> *)(x + r * ld + (int64_t)c * V);
-#pragma unroll
-                for (int e = 0; e < V; ++e) m = max(m, finite_bits(v.e[e]));
-            }
-    }
-#pragma unroll
-    for (int w = 1; w < 64; w <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, w, 64));
-    __shared__ uint32_t red[4];
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    m = max(max(red[0], red[1]), max(red[2], red[3]));
-    if (m != 0) atomicMax(to, m); // (a maximum: no order matters)
-}
-
-int launch_largest(const float *x, int64_t rows, int d, int64_t ld, uint32_t *to, hipStream_t st)
-{
-    const int64_t groups = std::min<int64_t>(2048, (rows * d + 4095) / 4096);
-    if (row_width(x, ld, d, 4) == 16) largest_kernel<4><<<dim3((unsigned)groups), dim3(256), 0, st>>>(x, rows, d / 4, ld, to);
-    else largest_kernel<1><<<dim3((unsigned)groups), dim3(256), 0, st>>>(x, rows, d, ld, to);
+    clear_ranges_kernel<<<dim3(1), dim3(1), 0, st>>>(to);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
@@ -96,18 +42,22 @@ __global__ __launch_bounds__(256) void row_inverses_kernel(const float *__restri
             if (in_row == 0 && row < rows) {
                 const bool is_odd = m[u] >= 0x7f800000u;
                 inv[row] = is_odd ? INFINITY : m[u] == 0 ? kLeastInverse : kRowUnit / range_scale(m[u]);
-                if (is_odd) odd.rows[atomicAdd(odd.count, 1u)] = (uint32_t)row; // (what is done with them knows no order)
+                if (is_odd) {
+                    const uint32_t at = atomicAdd(odd.count, 1u); // (what is done with them knows no order)
+                    if (odd.rows) odd.rows[at] = (uint32_t)row;
+                }
             }
         }
     }
 }
 
-// a tile's rows, a thread each
-__global__ __launch_bounds__(kTileM) void tile_inverses_kernel(float *__restrict__ inv, int64_t rows, float *__restrict__ tile_inv)
+// A tile's rows, a thread each: one inverse for them all where they lie together, or (ranges) their share of the table's range.
+__global__ __launch_bounds__(kTileM) void tile_inverses_kernel(float *__restrict__ inv, int64_t rows, float *__restrict__ tile_inv, Ranges *__restrict__ ranges)
 {
     __shared__ float top[kTileM / 64], least[kTileM / 64];
     const int64_t row = (int64_t)blockIdx.x * kTileM + threadIdx.x;
-    const float mine = row < rows ? inv[row] : kLeastInverse;
+    float mine = row < rows ? inv[row] : kLeastInverse;
+    if (ranges && mine == INFINITY) mine = kLeastInverse; // (odd rows have no share)
     float hi = mine, lo = mine == kLeastInverse ? INFINITY : mine;
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) {
@@ -118,6 +68,14 @@ __global__ __launch_bounds__(kTileM) void tile_inverses_kernel(float *__restrict
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kTileM / 64; ++w) { hi = fmaxf(hi, top[w]); lo = fminf(lo, least[w]); }
+    if (ranges) {
+        if (threadIdx.x != 0) return;
+        // (maxima and minima: no order matters; asked for first, since most change nothing)
+        const uint32_t most = __float_as_uint(hi), few = __float_as_uint(lo);
+        if (most > __hip_atomic_load(&ranges->inverse, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(&ranges->inverse, most);
+        if (few < __hip_atomic_load(&ranges->least_inverse, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMin(&ranges->least_inverse, few);
+        return;
+    }
     const bool one = hi < INFINITY && hi <= lo * kTileSpread;
     if (one && row < rows) inv[row] = hi;
     if (threadIdx.x == 0) tile_inv[blockIdx.x] = one ? hi : 0.0f;
@@ -160,7 +118,15 @@ int launch_odd_rows(const float *x, int d, int64_t ld, const float *q, int nq, i
     return AVQ_OK;
 }
 
-int launch_row_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, float *tile_inv, const OddRows &odd, hipStream_t st)
+__global__ __launch_bounds__(256) void common_inverses_kernel(float *__restrict__ inv, int64_t rows, const Ranges *__restrict__ ranges)
+{
+    if (rows_apart(ranges)) return;
+    const float common = __uint_as_float(ranges->inverse);
+    for (int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x; row < rows; row += (int64_t)gridDim.x * 256)
+        if (inv[row] != INFINITY) inv[row] = common;
+}
+
+static int own_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, const OddRows &odd, hipStream_t st)
 {
     const bool whole = whole_units(x, ld, d, sizeof(float));
     const int units = units_of<float>(d), lanes = units <= 16 ? 16 : units <= 32 ? 32 : 64;
@@ -170,7 +136,23 @@ int launch_row_inverses(const float *x, int64_t rows, int d, int64_t ld, float *
     else if (lanes == 32) whole ? run(row_inverses_kernel<false, 32>) : run(row_inverses_kernel<true, 32>);
     else whole ? run(row_inverses_kernel<false, 64>) : run(row_inverses_kernel<true, 64>);
     AVQ_HIP(hipGetLastError());
-    tile_inverses_kernel<<<dim3((unsigned)((rows + kTileM - 1) / kTileM)), dim3(kTileM), 0, st>>>(inv, rows, tile_inv);
+    return AVQ_OK;
+}
+
+int launch_row_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, float *tile_inv, const OddRows &odd, hipStream_t st)
+{
+    AVQ_TRY(own_inverses(x, rows, d, ld, inv, odd, st));
+    tile_inverses_kernel<<<dim3((unsigned)((rows + kTileM - 1) / kTileM)), dim3(kTileM), 0, st>>>(inv, rows, tile_inv, nullptr);
+    AVQ_HIP(hipGetLastError());
+    return AVQ_OK;
+}
+
+int launch_common_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, Ranges *ranges, hipStream_t st)
+{
+    AVQ_TRY(own_inverses(x, rows, d, ld, inv, OddRows{&ranges->odd, nullptr, nullptr}, st));
+    tile_inverses_kernel<<<dim3((unsigned)((rows + kTileM - 1) / kTileM)), dim3(kTileM), 0, st>>>(inv, rows, nullptr, ranges);
+    AVQ_HIP(hipGetLastError());
+    common_inverses_kernel<<<dim3((unsigned)std::min<int64_t>((rows + 255) / 256, 4096)), dim3(256), 0, st>>>(inv, rows, ranges);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
@@ -181,7 +163,7 @@ constexpr int kPackRows = 64, kPackColumns = 128;
 // thread, so that threads side by side write the rows of a block, 2 KB. V: elements a load.
 template <class T, int V>
 __global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x, int64_t rows, int d, int64_t ld, int blocks, Rows16 to_rows,
-                                                        const uint32_t *__restrict__ largest, const float *__restrict__ inv, uint16_t flip)
+                                                        const float *__restrict__ inv, uint16_t flip)
 {
     constexpr bool SPLIT = sizeof(T) == 4;
     constexpr int kLine = kPackColumns + 16 / sizeof(T); // (rows apart by 16 bytes more than a multiple of the banks)
@@ -190,7 +172,7 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const T *__restrict__ x,
     const int here = (int)min(rows - row0, (int64_t)kPackRows);
     const int r = threadIdx.x / 2 % kPackRows, u = threadIdx.x & 1;
     float scale = 1.0f;
-    if (SPLIT) scale = largest ? range_scale(*largest) : scale_of_inverse(inv[min(row0 + r, rows - 1)]);
+    if (SPLIT) scale = scale_of_inverse(inv[min(row0 + r, rows - 1)]);
     for (int c0 = 0; c0 < blocks * 16; c0 += kPackColumns) {
         const int columns = min(d - c0, kPackColumns), per_row = max(columns, 0) / V;
         const uint32_t magic = magic_of(per_row);
@@ -245,8 +227,8 @@ __global__ __launch_bounds__(256) void pack_own_scale_kernel(const float *__rest
     }
     if (threadIdx.x == 0) {
         inv[row] = 1.0f / (kRowUnit * s);
-        odd.seen[row] = 0u;
-        if (row == 0) *odd.count = 0u;
+        if (odd.seen) odd.seen[row] = 0u;
+        if (odd.seen && row == 0) *odd.count = 0u;
     }
 }
 
@@ -257,19 +239,19 @@ int launch_pack_queries(const float *q, int64_t rows, int d, int64_t ld, int ste
     return AVQ_OK;
 }
 
-int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const uint32_t *largest, const float *inv, bool negate, hipStream_t st)
+int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const float *inv, bool negate, hipStream_t st)
 {
     const dim3 grid((unsigned)((rows + kPackRows - 1) / kPackRows));
     const int size = type_bytes(type), w = row_width(x, ld, d, size);
     const uint16_t flip = negate ? 0x8000 : 0;
     const int blocks = type == AVQ_F32 ? steps : 2 * steps; // of 16 coordinates
     if (type == AVQ_F32) {
-        if (w == 16) pack_rows_kernel<float, 4><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, largest, inv, 0);
-        else pack_rows_kernel<float, 1><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, largest, inv, 0);
+        if (w == 16) pack_rows_kernel<float, 4><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, inv, 0);
+        else pack_rows_kernel<float, 1><<<grid, dim3(256), 0, st>>>((const float *)x, rows, d, ld, blocks, to, inv, 0);
     } else {
-        if (w == 16) pack_rows_kernel<uint16_t, 8><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, nullptr, flip);
-        else if (w == 8) pack_rows_kernel<uint16_t, 4><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, nullptr, flip);
-        else pack_rows_kernel<uint16_t, 1><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, nullptr, flip);
+        if (w == 16) pack_rows_kernel<uint16_t, 8><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
+        else if (w == 8) pack_rows_kernel<uint16_t, 4><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
+        else pack_rows_kernel<uint16_t, 1><<<grid, dim3(256), 0, st>>>((const uint16_t *)x, rows, d, ld, blocks, to, nullptr, flip);
     }
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;

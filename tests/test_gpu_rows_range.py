@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 avq = pytest.importorskip("paper_1908_10396_amd")
 
-from test_gpu_rows import HALF, TINY, TYPES, U, _check_probs, _grad_formula, gen, normal, random_ids, within  # noqa: E402
+from test_gpu_rows import HALF, TINY, TYPES, U, _check_probs, _grad_formula, gen, normal, random_ids, strided, within  # noqa: E402
 
 
 def grid(x, kind):
@@ -150,6 +150,77 @@ def test_log_probs_beside_rows_of_large_masks(kind, value, nq, share):
 @pytest.mark.parametrize("value", [-1e7, -1e12, -1e30])
 def test_log_probs_of_fp32_rows_behind_thousands_of_large_masks(nq, value):
     test_log_probs_of_rows_behind_thousands_of_large_masks("f32", nq, value)
+
+
+@pytest.mark.parametrize("kind,value", [("f32", -2.0 ** 24), ("f32", -1e9), ("f32", -1e30), ("bf16", -1e9)])
+@pytest.mark.parametrize("nq", [2, 12, 65, 300])
+def test_gradients_beside_rows_of_large_masks(kind, value, nq):
+    g = gen(nq + 1)
+    n, d, scale = 3001, 100, 0.3
+    x, q, masked = _masked(n, d, nq, kind, value, g)
+    ids = random_ids((nq,), n, g)
+    ids = torch.where((ids >= 0) & (ids < n) & masked[ids.clamp(0, n - 1).long()], n - 1, ids)
+    up, up_h = normal((nq,), g), normal((nq,), g)
+    r = avq.log_probs(x, q, ids, scale=scale)
+    _, place = _without(r, masked, ids, 0)
+    want_q, bound_q, want_x, bound_x = _grad_formula(x[~masked], q, scale, place, r.lse, r.entropy, up, up_h, None, kind)
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, r.entropy, up_h, scale=scale)
+    within(dx[~masked], want_x, bound_x, "dpoints")
+    assert not bool(dx[masked].any())
+    within(dq, want_q, bound_q, "dqueries")
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [70, 300])
+@pytest.mark.parametrize("rows,queries", [(10, 0), (0, 10), (22, 0), (0, 22), (22, 22)])
+def test_rows_and_queries_of_unequal_size(kind, nq, rows, queries):
+    """Sizes down to 2^-rows and 2^-queries of the largest."""
+    if kind == "f16" and max(rows, queries) > 10:
+        pytest.skip("beyond the range of f16")
+    g = gen(nq + rows + 2 * queries)
+    n, d, scale = 2500, 100, 0.2
+    x = normal((n, d), g) * torch.exp2(-rows * torch.rand((n, 1), generator=g, device="cuda"))
+    q = normal((nq, d), g) * torch.exp2(-queries * torch.rand((nq, 1), generator=g, device="cuda"))
+    x, q = x.to(TYPES[kind]), q.to(TYPES[kind])
+    ids = random_ids((nq,), n, g)
+    up, up_h = normal((nq,), g), normal((nq,), g)
+    r = avq.log_probs(x, q, ids, 3, scale)
+    _check_probs(r, x, q, scale, ids, 3)
+    want_q, bound_q, want_x, bound_x = _grad_formula(x, q, scale, ids, r.lse, r.entropy, up, up_h, None, kind)
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, r.entropy, up_h, scale=scale)
+    within(dx, want_x, bound_x, "dpoints")
+    within(dq, want_q, bound_q, "dqueries")
+    # rows and results apart, added to what is there, the other sign
+    r = avq.log_probs(x, q, ids, scale=-scale)
+    want_q, bound_q, want_x, bound_x = _grad_formula(x, q, -scale, ids, r.lse, r.entropy, up, up_h, None, kind)
+    held = want_x.abs().amax(1, keepdim=True).expand(n, d).to(TYPES[kind])
+    out = strided(held, 5, 2)
+    dq, dx = avq.log_probs_grad(strided(x, 3, 1), strided(q, 9, 8), ids, r.lse, up, r.entropy, up_h, scale=-scale, out_points=out, accumulate=True)
+    total = want_x + held.double()
+    within(dx, total, bound_x + 2 * U * total.abs() + HALF[kind] * total.abs() * 1.01, "dpoints, added")
+    within(dq, want_q, bound_q, "dqueries, strided")
+
+
+@pytest.mark.parametrize("value", [-2.0, -1e9, -math.inf])
+def test_gradients_beside_masks_in_several_parts_of_the_rows(value):
+    """So many queries that the rows are taken in parts; the given rows lie in all of them."""
+    g = gen(8)
+    n, d, nq, scale = 13_000, 16, 40_000, 0.5
+    x, q, masked = _masked(n, d, nq, "f32", value, g)
+    ids = torch.randint(0, n, (nq,), generator=g, device="cuda", dtype=torch.int32)
+    ids = torch.where(masked[ids.long()], n - 1, ids)
+    up = normal((nq,), g)
+    r = avq.log_probs(x, q, ids, scale=scale)
+    keep, place = slice(None), ids
+    if value < -1e3:
+        keep = ~masked
+        _, place = _without(r, masked, ids, 0)
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, scale=scale)
+    want_q, bound_q, want_x, bound_x = _grad_formula(x[keep], q, scale, place, r.lse, r.entropy, up, None, None, "f32")
+    within(dx[keep], want_x, bound_x, "dpoints")
+    within(dq[:, :-1], want_q[:, :-1], bound_q[:, :-1], "dqueries")
+    if value < -1e3:
+        assert not bool(dx[masked].any())
 
 
 def _gradient_of_weighted(x, q, scale, ids, up, kind):
