@@ -39,14 +39,31 @@ __global__ __launch_bounds__(256) void row_inverses_kernel(const float *__restri
 #pragma unroll
             for (int w = 1; w < L; w <<= 1) m[u] = max(m[u], (uint32_t)__shfl_xor((int)m[u], w, 64));
             const int64_t row = base + u * kPer + lane / L;
-            if (in_row == 0 && row < rows) {
-                const bool is_odd = m[u] >= 0x7f800000u;
-                inv[row] = is_odd ? INFINITY : m[u] == 0 ? kLeastInverse : kRowUnit / range_scale(m[u]);
-                if (is_odd) {
-                    const uint32_t at = atomicAdd(odd.count, 1u); // (what is done with them knows no order)
-                    if (odd.rows) odd.rows[at] = (uint32_t)row;
-                }
-            }
+            if (in_row == 0 && row < rows) inv[row] = m[u] >= 0x7f800000u ? INFINITY : m[u] == 0 ? kLeastInverse : kRowUnit / range_scale(m[u]);
+        }
+        // the wave's odd rows by one addition (what is done with them knows no order)
+        bool any = false;
+#pragma unroll
+        for (int u = 0; u < U; ++u) any = any || m[u] >= 0x7f800000u;
+        if (!__any(any)) continue;
+        uint64_t odd_lanes[U];
+        uint32_t many = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            odd_lanes[u] = __ballot(in_row == 0 && base + u * kPer + lane / L < rows && m[u] >= 0x7f800000u);
+            many += (uint32_t)__popcll(odd_lanes[u]);
+        }
+        if (!odd.rows) {
+            if (lane == 0) *odd.count = 1u; // (whether there are any is all that is asked)
+            continue;
+        }
+        uint32_t at = 0;
+        if (lane == 0) at = atomicAdd(odd.count, many);
+        at = (uint32_t)__shfl((int)at, 0, 64);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (odd_lanes[u] >> lane & 1) odd.rows[at + __popcll(odd_lanes[u] & (((uint64_t)1 << lane) - 1))] = (uint32_t)(base + u * kPer + lane / L);
+            at += (uint32_t)__popcll(odd_lanes[u]);
         }
     }
 }
@@ -81,39 +98,31 @@ __global__ __launch_bounds__(kTileM) void tile_inverses_kernel(float *__restrict
     if (threadIdx.x == 0) tile_inv[blockIdx.x] = one ? hi : 0.0f;
 }
 
-// A thread a query: an odd row's elements that are not finite are found by the workgroup, and multiplied by each query.
+// A wave an odd row: its elements that are not finite, each by every query.
+constexpr int kOddGroups = 2048;
+
 __global__ __launch_bounds__(256) void odd_rows_kernel(const float *__restrict__ x, int d, int64_t ld, const float *__restrict__ q, int nq, int64_t ld_q, float sign, OddRows odd)
 {
-    __shared__ int columns[256];
-    __shared__ float values[256];
-    __shared__ int found;
     const uint32_t all = *odd.count;
-    const int t = blockIdx.x * 256 + threadIdx.x;
-    bool marked = false;
-    for (uint32_t i = blockIdx.y; i < all; i += gridDim.y) {
+    const int lane = threadIdx.x & 63;
+    for (uint32_t i = blockIdx.x * 4 + (threadIdx.x >> 6); i < all; i += gridDim.x * 4) {
         const float *row = x + (int64_t)odd.rows[i] * ld;
-        for (int c0 = 0; c0 < d; c0 += 256) {
-            __syncthreads(); // (the columns before have been read)
-            if (threadIdx.x == 0) found = 0;
-            __syncthreads();
-            const int c = c0 + threadIdx.x;
-            const float v = c < d ? row[c] : 0.0f;
-            if (!(fabsf(v) < INFINITY)) {
-                const int at = atomicAdd(&found, 1);
-                columns[at] = c;
-                values[at] = v;
+        for (int c0 = 0; c0 < d; c0 += 64) {
+            const float v = c0 + lane < d ? row[c0 + lane] : 0.0f;
+            for (uint64_t left = __ballot(!(fabsf(v) < INFINITY)); left != 0; left &= left - 1) {
+                const int from = __ffsll((unsigned long long)left) - 1;
+                const float value = __shfl(v, from, 64) * sign;
+#pragma unroll 4
+                for (int t = lane; t < nq; t += 64)
+                    if (!(q[t * ld_q + c0 + from] * value == -INFINITY)) odd.seen[t] = 1u;
             }
-            __syncthreads();
-            if (t < nq)
-                for (int k = 0; k < found; ++k) marked = marked || !(q[t * ld_q + columns[k]] * sign * values[k] == -INFINITY);
         }
     }
-    if (marked) odd.seen[t] = 1u;
 }
 
 int launch_odd_rows(const float *x, int d, int64_t ld, const float *q, int nq, int64_t ld_q, bool negate, const OddRows &odd, hipStream_t st)
 {
-    odd_rows_kernel<<<dim3((unsigned)((nq + 255) / 256), 64), dim3(256), 0, st>>>(x, d, ld, q, nq, ld_q, negate ? -1.0f : 1.0f, odd);
+    odd_rows_kernel<<<dim3(kOddGroups), dim3(256), 0, st>>>(x, d, ld, q, nq, ld_q, negate ? -1.0f : 1.0f, odd);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
