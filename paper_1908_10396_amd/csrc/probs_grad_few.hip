@@ -168,7 +168,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void grad_few_kernel(FewArgs p)
             for (int t = 0; t < NQ; ++t) {
                 const float logp = __fmaf_rn(s[t], p.scale, -lse[t]), w = __builtin_amdgcn_exp2f(logp * log2e); // (one rounding of s - lse: only lse's own is in p)
                 float G = more[t] - (w == 0.0f ? 0.0f : w * __fmaf_rn(h[t], logp, a[t])); // (p log p)
-                if (!real) G = 0.0f;
+                if (!real || (NQ > 2 && t >= p.nq)) G = 0.0f; // (a place past the last query is 0 times the row: NaN where that holds an infinity)
                 if (MEND) {
                     const float mine = real && in_row == t ? w : 0.0f;
                     z_low += mine >= 0.25f ? 0.0f : mine;

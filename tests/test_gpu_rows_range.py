@@ -349,6 +349,27 @@ def test_rows_that_are_not_finite_show(kind, nq):
         assert not bool(torch.isfinite(r.lse).any())
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [1, 2, 3, 7, 12, 65, 300])
+@pytest.mark.parametrize("entropy", [False, True])
+def test_gradients_beside_rows_of_infinite_masks(kind, nq, entropy):
+    """Rows of probability 0 get no gradient; the queries' is that of the other rows, but in the mask's own column, where it is 0 times
+    infinity."""
+    g = gen(nq)
+    n, d, scale = 3001, 100, 0.3
+    x, q, masked = _masked(n, d, nq, kind, -math.inf, g)
+    ids = random_ids((nq,), n, g)
+    ids = torch.where((ids >= 0) & (ids < n) & masked[ids.clamp(0, n - 1).long()], n - 1, ids)
+    up, up_h = normal((nq,), g), normal((nq,), g) if entropy else None
+    r = avq.log_probs(x, q, ids, scale=scale)
+    _, place = _without(r, masked, ids, 0)
+    want_q, bound_q, want_x, bound_x = _grad_formula(x[~masked], q, scale, place, r.lse, r.entropy, up, up_h, None, kind)
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, r.entropy, up_h, scale=scale)
+    within(dx[~masked], want_x, bound_x, "dpoints")
+    assert not bool(dx[masked].any())
+    within(dq[:, :-1], want_q[:, :-1], bound_q[:, :-1], "dqueries")
+
+
 def test_gradient_of_as_many_given_ids_as_there_can_be_threads():
     g = gen(1)
     n, d, nq, m = 64, 8, 1 << 16, 1 << 10
