@@ -331,7 +331,7 @@ int launch_odd_rows(const float *x, int d, int64_t ld, const float *q, int nq, i
 // Rows laid out as `to` says (to.p: where), `steps` steps of them, zeros past a row's end. fp32: pairs, by scales of which inv[row] is the
 // inverse. negate: with the other sign.
 int launch_pack_rows(const void *x, int type, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, const float *inv, bool negate, hipStream_t st);
-// fp32 queries: pairs, each row by its own scale, whose inverse goes to inv[row]. Also begins `odd` where there is one: no rows, no marks.
+// fp32 queries: pairs, each row by its own scale, whose inverse goes to inv[row]. Also begins what `odd` has: no rows, no marks.
 int launch_pack_queries(const float *q, int64_t rows, int d, int64_t ld, int steps, const Rows16 &to, float *inv, const OddRows &odd, bool negate, hipStream_t st);
 // The transpose packed: row c < d of d holds x[t][c] factor[t] (factor == NULL: x[t][c]), 16 t in the order of turned16, zeros past the
 // last t and where the factor is 0.

@@ -695,6 +695,19 @@ static int stream_tile(int type, int d, int nq)
 
 constexpr int kTileGroups = 512; // two workgroups a compute unit
 constexpr size_t kPackBytes = (size_t)1 << 30; // most that packed rows take at a time
+constexpr size_t kGroupBytes = (size_t)1 << 30; // most that the groups' maxima of several query tiles take
+
+// Queries that a call takes at a time: all of them, unless the maxima of their groups would exceed kGroupBytes (7,168 for 1,183,514 rows);
+// then parts of equal size, whole query tiles.
+static int queries_at_once(int type, int64_t n, int d, int nq, int k)
+{
+    if (k == 0 || prob_path(type_bytes(type), d, nq) != kByTiles) return nq;
+    const size_t each = (size_t)((n + kTileM - 1) / kTileM) * (kTileM / 32) * sizeof(float);
+    const int64_t most = std::max<int64_t>(1, (int64_t)(kGroupBytes / each) / kTileN) * kTileN;
+    if (nq <= most) return nq;
+    const int64_t parts = (nq + most - 1) / most;
+    return (int)(((nq + parts - 1) / parts + kTileN - 1) / kTileN * kTileN);
+}
 
 struct ProbScratch {
     float4 *stats; float *gmax; int64_t gstride;
@@ -752,7 +765,7 @@ size_t log_probs_scratch_bytes(int type, int64_t n, int d, int nq, int given, in
 {
     (void)given;
     ProbParams p{};
-    p.type = type; p.n = n; p.d = d; p.nq = nq; p.k = k;
+    p.type = type; p.n = n; p.d = d; p.nq = queries_at_once(type, n, d, nq, k); p.k = k;
     return nq == 0 ? 0 : prob_scratch(p, nullptr).bytes;
 }
 
@@ -800,15 +813,17 @@ static int stream_sized(const ProbParams &p, const ProbScratch &s, hipStream_t s
     return s.qt == 2 ? stream_run<T, 2, ALIGNED, true>(p, s, st) : stream_run<T, 4, ALIGNED, true>(p, s, st);
 }
 
+// again: a further part of the queries; rows that were laid out at once are there.
 template <class H, bool SPLIT>
-static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
+static int tiles_run(const ProbParams &p, const ProbScratch &s, bool again, hipStream_t st)
 {
+    const bool laid_out = again && s.launches == 1;
     const int size = type_bytes(p.type);
     const float c2 = fabsf(p.scale) * 1.44269504088896341f;
     const Rows16 Q = packed_rows(s.q16, p.nq);
     if (SPLIT) {
-        AVQ_TRY(launch_pack_queries((const float *)p.queries, p.nq, p.d, p.ld_queries, s.steps, Q, s.q_inv, s.odd, p.scale < 0.0f, st));
-        AVQ_TRY(launch_row_inverses((const float *)p.points, p.n, p.d, p.ld_points, s.x_inv, s.tile_inv, s.odd, st));
+        AVQ_TRY(launch_pack_queries((const float *)p.queries, p.nq, p.d, p.ld_queries, s.steps, Q, s.q_inv, OddRows{again ? nullptr : s.odd.count, nullptr, s.odd.seen}, p.scale < 0.0f, st));
+        if (!again) AVQ_TRY(launch_row_inverses((const float *)p.points, p.n, p.d, p.ld_points, s.x_inv, s.tile_inv, s.odd, st));
         AVQ_TRY(launch_odd_rows((const float *)p.points, p.d, p.ld_points, (const float *)p.queries, p.nq, p.ld_queries, p.scale < 0.0f, s.odd, st));
     } else {
         AVQ_TRY(launch_pack_rows(p.queries, p.type, p.nq, p.d, p.ld_queries, s.steps, Q, nullptr, p.scale < 0.0f, st));
@@ -820,7 +835,7 @@ static int tiles_run(const ProbParams &p, const ProbScratch &s, hipStream_t st)
         Rows16 X{(const uint16_t *)from, p.ld_points, 16, rows};
         if (s.pack) {
             X = SPLIT ? packed_rows(s.x16, rows) : Rows16{s.x16, (int64_t)s.steps * 32, 16, rows};
-            AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, s.steps, X, SPLIT ? s.x_inv + lo : nullptr, false, st));
+            if (!laid_out) AVQ_TRY(launch_pack_rows(from, p.type, rows, p.d, p.ld_points, s.steps, X, SPLIT ? s.x_inv + lo : nullptr, false, st));
         }
         float4 *stats = s.stats + (size_t)i * s.parts * 2 * p.nq;
         const float *x_inv = SPLIT ? s.x_inv + lo : nullptr, *tile_inv = SPLIT ? s.tile_inv + lo / kTileM : nullptr;
@@ -853,15 +868,29 @@ static int finish_run(const ProbParams &p, const ProbScratch &s, int parts, hipS
 template <class T>
 static int log_probs_typed(const ProbParams &p, hipStream_t st)
 {
-    const ProbScratch s = prob_scratch(p, p.scratch);
     const int path = prob_path(sizeof(T), p.d, p.nq);
     if (path == kByTiles) {
-        if constexpr (sizeof(T) == 4) AVQ_TRY((tiles_run<f16_t, true>(p, s, st)));
-        else AVQ_TRY((tiles_run<T, false>(p, s, st)));
-        // a few queries: as many threads a query as there can be
-        const int parts = s.launches * s.parts * 2;
-        return p.nq <= 256 ? finish_run<kByTiles, T, 1024>(p, s, parts, st) : finish_run<kByTiles, T, 512>(p, s, parts, st);
+        ProbParams part = p;
+        part.nq = queries_at_once(p.type, p.n, p.d, p.nq, p.k);
+        ProbScratch s = prob_scratch(part, p.scratch);
+        for (int q0 = 0; q0 < p.nq; q0 += part.nq) {
+            ProbParams now = p;
+            now.nq = std::min(part.nq, p.nq - q0);
+            now.queries = (const T *)p.queries + q0 * p.ld_queries;
+            if (p.given > 0) { now.ids = p.ids + (int64_t)q0 * p.given; now.logp = p.logp + (int64_t)q0 * p.given; }
+            now.lse = p.lse + q0;
+            if (p.entropy) now.entropy = p.entropy + q0;
+            if (p.k > 0) { now.alt_ids = p.alt_ids + (int64_t)q0 * p.k; now.alt_logp = p.alt_logp + (int64_t)q0 * p.k; }
+            s.query_tiles = (now.nq + kTileN - 1) / kTileN;
+            if constexpr (sizeof(T) == 4) AVQ_TRY((tiles_run<f16_t, true>(now, s, q0 > 0, st)));
+            else AVQ_TRY((tiles_run<T, false>(now, s, q0 > 0, st)));
+            // a few queries: as many threads a query as there can be
+            const int parts = s.launches * s.parts * 2;
+            AVQ_TRY((now.nq <= 256 ? finish_run<kByTiles, T, 1024>(now, s, parts, st) : finish_run<kByTiles, T, 512>(now, s, parts, st)));
+        }
+        return AVQ_OK;
     }
+    const ProbScratch s = prob_scratch(p, p.scratch);
     if (path == kByRow) {
         AVQ_TRY(row_sized<T>(p, s, st));
         return finish_run<kByRow, T, 1024>(p, s, s.groups, st);

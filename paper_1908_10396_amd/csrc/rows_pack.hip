@@ -237,7 +237,7 @@ __global__ __launch_bounds__(256) void pack_own_scale_kernel(const float *__rest
     if (threadIdx.x == 0) {
         inv[row] = 1.0f / (kRowUnit * s);
         if (odd.seen) odd.seen[row] = 0u;
-        if (odd.seen && row == 0) *odd.count = 0u;
+        if (odd.count && row == 0) *odd.count = 0u;
     }
 }
 

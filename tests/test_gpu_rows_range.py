@@ -400,3 +400,22 @@ def test_gradient_of_as_many_rows_as_can_be_looked_up():
     got = avq.embed_grad(grad, ids, n)
     want = torch.bincount((ids + 1).long(), minlength=n + 1)[1:]
     assert torch.equal(got[:, 0].double(), want.double())  # (whole numbers below 2^24: every sum is exact)
+
+
+def test_many_queries_are_taken_in_parts():
+    g = gen(4)
+    n, d, nq = 4_200_000, 8, 2_200
+    x, q = normal((n, d), g), normal((nq, d), g)
+    ids = random_ids((nq, 2), n, g)
+    assert avq.lib().avq_log_probs_scratch(0, n, d, nq, 2, 3) < 3 << 29
+    r = avq.log_probs(x, q, ids, 3, 0.7)
+    pick = torch.tensor([0, 63, 64, 1099, 1100, 1151, 1152, 2198, 2199], device="cuda")
+    part = avq.LogProbs(r.logp[pick], r.lse[pick], r.entropy[pick], r.alt_ids[pick], r.alt_logp[pick])
+    _check_probs(part, x, q[pick], 0.7, ids[pick], 3)
+    for a, b in ((0, 1000), (1000, nq)):  # the whole call against its halves
+        half = avq.log_probs(x, q[a:b], ids[a:b].contiguous(), 3, 0.7)
+        real = torch.isfinite(half.logp)
+        assert torch.equal(torch.isfinite(r.logp[a:b]), real)
+        for u, v in ((r.lse[a:b], half.lse), (r.entropy[a:b], half.entropy), (r.logp[a:b][real], half.logp[real])):
+            assert float((u - v).abs().max()) <= 1e-4
+        assert float((r.alt_logp[a:b] - half.alt_logp).abs().max()) <= 1e-4
