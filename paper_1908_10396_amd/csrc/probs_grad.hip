@@ -37,42 +37,49 @@ __global__ __launch_bounds__(256) void grad_coef_kernel(const T *__restrict__ q,
                                                         const float *__restrict__ g, const float *__restrict__ h, const float *__restrict__ entropy, const float *__restrict__ gl,
                                                         GradCoef *__restrict__ coef, Ranges *__restrict__ ranges)
 {
-    const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (t >= nq) return;
-    float a = 0.0f, mag = 0.0f;
-    for (int j = lane; j < given; j += 64) {
-        const int32_t id = ids[(int64_t)t * given + j];
-        if (id >= 0 && (int64_t)id < n) {
-            const float v = g[(int64_t)t * given + j];
-            a += v;
-            mag += fabsf(v);
+    __shared__ uint32_t shared_most[4], shared_least[4];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, t = blockIdx.x * 4 + wave;
+    uint32_t most = 0, least = 0x7f800000u; // of the query's largest magnitude over its factor
+    if (t < nq) {
+        float a = 0.0f, mag = 0.0f;
+        for (int j = lane; j < given; j += 64) {
+            const int32_t id = ids[(int64_t)t * given + j];
+            if (id >= 0 && (int64_t)id < n) {
+                const float v = g[(int64_t)t * given + j];
+                a += v;
+                mag += fabsf(v);
+            }
         }
-    }
-    a = group_sum<64>(a);
-    mag = group_sum<64>(mag);
-    uint32_t top = 0;
-    if (kHasFactor<T>) {
-        for (int c = lane; c < d; c += 64) {
-            const uint32_t bits = __float_as_uint(to_f32(q[t * ld_q + c])) & 0x7fffffffu;
-            top = max(top, bits < 0x7f800000u ? bits : 0u);
-        }
+        a = group_sum<64>(a);
+        mag = group_sum<64>(mag);
+        uint32_t top = 0;
+        if (kHasFactor<T>) {
+            for (int c = lane; c < d; c += 64) {
+                const uint32_t bits = __float_as_uint(to_f32(q[t * ld_q + c])) & 0x7fffffffu;
+                top = max(top, bits < 0x7f800000u ? bits : 0u);
+            }
 #pragma unroll
-        for (int w = 1; w < 64; w <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, w, 64));
+            for (int w = 1; w < 64; w <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, w, 64));
+        }
+        const float ht = h ? h[t] : 0.0f;
+        if (gl) a -= gl[t];
+        if (h) a += ht * entropy[t];
+        const float bound = mag + fabsf(a) + fabsf(ht); // of |G| (p |log p| < 0.37)
+        const bool some = !(bound == 0.0f);
+        const float factor = kHasFactor<T> && bound < INFINITY ? range_scale(__float_as_uint(bound)) : 1.0f;
+        if (lane == 0) coef[t] = GradCoef{a, ht, factor, some ? 1.0f / factor : 0.0f};
+        const uint32_t weighted = __float_as_uint(__uint_as_float(top) / factor);
+        if (some && bound < INFINITY && top != 0 && weighted < 0x7f800000u) most = least = weighted;
     }
-    if (lane != 0) return;
-    const float ht = h ? h[t] : 0.0f;
-    if (gl) a -= gl[t];
-    if (h) a += ht * entropy[t];
-    const float bound = mag + fabsf(a) + fabsf(ht); // of |G| (p |log p| < 0.37)
-    const bool some = !(bound == 0.0f);
-    const float factor = kHasFactor<T> && bound < INFINITY ? range_scale(__float_as_uint(bound)) : 1.0f;
-    coef[t] = GradCoef{a, ht, factor, some ? 1.0f / factor : 0.0f};
-    if (!kHasFactor<T> || !some || !(bound < INFINITY) || top == 0) return;
-    const uint32_t weighted = __float_as_uint(__uint_as_float(top) / factor);
-    if (weighted >= 0x7f800000u) return;
+    if (!kHasFactor<T>) return;
+    if (lane == 0) { shared_most[wave] = most; shared_least[wave] = least; }
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) { most = max(most, shared_most[w]); least = min(least, shared_least[w]); }
     // (maxima and minima: no order matters; asked for first, since most change nothing)
-    if (weighted > __hip_atomic_load(&ranges->weighted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(&ranges->weighted, weighted);
-    if (weighted < __hip_atomic_load(&ranges->least_weighted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMin(&ranges->least_weighted, weighted);
+    if (most > __hip_atomic_load(&ranges->weighted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(&ranges->weighted, most);
+    if (least < __hip_atomic_load(&ranges->least_weighted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMin(&ranges->least_weighted, least);
 }
 
 // what the transposed queries are multiplied by

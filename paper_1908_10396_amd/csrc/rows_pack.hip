@@ -68,14 +68,10 @@ __global__ __launch_bounds__(256) void row_inverses_kernel(const float *__restri
     }
 }
 
-// A tile's rows, a thread each: one inverse for them all where they lie together, or (ranges) their share of the table's range.
-__global__ __launch_bounds__(kTileM) void tile_inverses_kernel(float *__restrict__ inv, int64_t rows, float *__restrict__ tile_inv, Ranges *__restrict__ ranges)
+// the largest and the least (of rows that have a scale) over a workgroup of kTileM threads
+__device__ __forceinline__ void range_of_tile(float &hi, float &lo)
 {
     __shared__ float top[kTileM / 64], least[kTileM / 64];
-    const int64_t row = (int64_t)blockIdx.x * kTileM + threadIdx.x;
-    float mine = row < rows ? inv[row] : kLeastInverse;
-    if (ranges && mine == INFINITY) mine = kLeastInverse; // (odd rows have no share)
-    float hi = mine, lo = mine == kLeastInverse ? INFINITY : mine;
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) {
         hi = fmaxf(hi, __shfl_xor(hi, w, 64));
@@ -85,17 +81,37 @@ __global__ __launch_bounds__(kTileM) void tile_inverses_kernel(float *__restrict
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kTileM / 64; ++w) { hi = fmaxf(hi, top[w]); lo = fminf(lo, least[w]); }
-    if (ranges) {
-        if (threadIdx.x != 0) return;
-        // (maxima and minima: no order matters; asked for first, since most change nothing)
-        const uint32_t most = __float_as_uint(hi), few = __float_as_uint(lo);
-        if (most > __hip_atomic_load(&ranges->inverse, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(&ranges->inverse, most);
-        if (few < __hip_atomic_load(&ranges->least_inverse, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMin(&ranges->least_inverse, few);
-        return;
-    }
+}
+
+// a tile's rows, a thread each
+__global__ __launch_bounds__(kTileM) void tile_inverses_kernel(float *__restrict__ inv, int64_t rows, float *__restrict__ tile_inv)
+{
+    const int64_t row = (int64_t)blockIdx.x * kTileM + threadIdx.x;
+    const float mine = row < rows ? inv[row] : kLeastInverse;
+    float hi = mine, lo = mine == kLeastInverse ? INFINITY : mine;
+    range_of_tile(hi, lo);
     const bool one = hi < INFINITY && hi <= lo * kTileSpread;
     if (one && row < rows) inv[row] = hi;
     if (threadIdx.x == 0) tile_inv[blockIdx.x] = one ? hi : 0.0f;
+}
+
+// The table's range, odd rows aside. A few workgroups: 4,624 of them took 60 us for their atomics.
+constexpr int kRangeGroups = 128;
+
+__global__ __launch_bounds__(kTileM) void inverse_range_kernel(const float *__restrict__ inv, int64_t rows, Ranges *__restrict__ ranges)
+{
+    float hi = kLeastInverse, lo = INFINITY;
+#pragma unroll 4
+    for (int64_t row = (int64_t)blockIdx.x * kTileM + threadIdx.x; row < rows; row += (int64_t)gridDim.x * kTileM) {
+        const float mine = inv[row];
+        if (mine == INFINITY || mine == kLeastInverse) continue;
+        hi = fmaxf(hi, mine);
+        lo = fminf(lo, mine);
+    }
+    range_of_tile(hi, lo);
+    if (threadIdx.x != 0) return;
+    atomicMax(&ranges->inverse, __float_as_uint(hi)); // (maxima and minima: no order matters)
+    atomicMin(&ranges->least_inverse, __float_as_uint(lo));
 }
 
 // A wave an odd row: its elements that are not finite, each by every query.
@@ -151,7 +167,7 @@ static int own_inverses(const float *x, int64_t rows, int d, int64_t ld, float *
 int launch_row_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, float *tile_inv, const OddRows &odd, hipStream_t st)
 {
     AVQ_TRY(own_inverses(x, rows, d, ld, inv, odd, st));
-    tile_inverses_kernel<<<dim3((unsigned)((rows + kTileM - 1) / kTileM)), dim3(kTileM), 0, st>>>(inv, rows, tile_inv, nullptr);
+    tile_inverses_kernel<<<dim3((unsigned)((rows + kTileM - 1) / kTileM)), dim3(kTileM), 0, st>>>(inv, rows, tile_inv);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
@@ -159,7 +175,7 @@ int launch_row_inverses(const float *x, int64_t rows, int d, int64_t ld, float *
 int launch_common_inverses(const float *x, int64_t rows, int d, int64_t ld, float *inv, Ranges *ranges, hipStream_t st)
 {
     AVQ_TRY(own_inverses(x, rows, d, ld, inv, OddRows{&ranges->odd, nullptr, nullptr}, st));
-    tile_inverses_kernel<<<dim3((unsigned)((rows + kTileM - 1) / kTileM)), dim3(kTileM), 0, st>>>(inv, rows, nullptr, ranges);
+    inverse_range_kernel<<<dim3((unsigned)std::min<int64_t>(kRangeGroups, (rows + kTileM - 1) / kTileM)), dim3(kTileM), 0, st>>>(inv, rows, ranges);
     AVQ_HIP(hipGetLastError());
     common_inverses_kernel<<<dim3((unsigned)std::min<int64_t>((rows + 255) / 256, 4096)), dim3(256), 0, st>>>(inv, rows, ranges);
     AVQ_HIP(hipGetLastError());
