@@ -283,6 +283,37 @@ def test_queries_without_upstream_gradient_beside_others(kind, nq):
     assert not bool(dq.any()) and not bool(dx.any())
 
 
+@pytest.mark.parametrize("nq", [12, 65, 300])
+def test_fp32_rows_a_little_within_the_spread_of_one_scale(nq):
+    """Rows 2^-14.5 of the table's largest, which has no probability: they are all that the queries' gradient is of."""
+    test_gradients_beside_rows_of_large_masks("f32", -(2.0 ** 16), nq)
+    test_log_probs_beside_rows_of_large_masks("f32", -(2.0 ** 16), nq, 0.5)
+    test_log_probs_beside_rows_of_large_masks("f32", -512.0, nq, 0.5)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [24, 130])
+@pytest.mark.parametrize("weight", [2.0 ** -15, 2.0 ** -20])
+def test_rows_that_only_queries_of_little_weight_reach(kind, nq, weight):
+    """Half of the rows are reached by half of the queries (logits 200 apart), whose upstream gradients are `weight` of the others'."""
+    g = gen(nq)
+    n, d = 1000, 32
+    x, q = 0.5 * normal((n, d), g), 0.5 * normal((nq, d), g)
+    x[:, :2] = 0.0
+    x[: n // 2, 0], x[n // 2:, 1] = 10.0, 10.0
+    sign = torch.where(torch.arange(nq, device="cuda") % 2 == 0, 10.0, -10.0)
+    q[:, 0], q[:, 1] = sign, -sign
+    x, q = x.to(TYPES[kind]), q.to(TYPES[kind])
+    ids = torch.randint(0, n // 2, (nq,), generator=g, device="cuda", dtype=torch.int32) + torch.where(sign > 0, 0, n // 2).int()
+    up = torch.where(sign > 0, 1.0, weight) * 2.0 ** 8
+    r = avq.log_probs(x, q, ids)
+    want_q, bound_q, want_x, bound_x = _gradient_of_weighted(x, q, 1.0, ids, up, kind)
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up)
+    within(dx[n // 2:], want_x[n // 2:], bound_x[n // 2:], "dpoints of little weight")
+    within(dx[: n // 2], want_x[: n // 2], bound_x[: n // 2], "dpoints")
+    within(dq, want_q, bound_q, "dqueries")
+
+
 @pytest.mark.parametrize("nq", [1, 2, 4, 7])
 @pytest.mark.parametrize("other", [2e-5, 5e-5, 1e-3])
 def test_gradient_of_a_part_of_a_table_whose_other_part_is_unlikely(nq, other):
