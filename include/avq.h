@@ -463,9 +463,12 @@ int avq_layer_norm_grad(const void *grad, int32_t type, int64_t ld_grad, const v
  * logp_out [nq][m] = log p of the rows ids [nq][m] (-inf for padding; m: 0 .. 4096);
  * alt_ids_out / alt_logp_out [nq][k] = the k rows of largest s_i and their log p,
  * by (s descending, id ascending), k: 0 .. min(n, AVQ_MAX_SELECT). The s_i themselves
- * are not stored. fp32 matrices are multiplied to fp32's accuracy; rows whose s_i
- * differ by less than its rounding may be ranked either way. log p is formed before
- * lse is rounded, so that it keeps its relative accuracy where p is nearly 1.
+ * are not stored. fp32 matrices are multiplied in fp32 for up to 64 queries, and for more as pairs of f16: a
+ * product of two elements is off by at most 2^-21 of it, or 2^-31 of their row's and query's largest
+ * magnitudes, whichever is more. Rows whose s_i differ by less than that may be ranked either way. log p is formed
+ * before lse is rounded, so that it keeps its relative accuracy where p is nearly 1. A row whose s_i is -infinity
+ * (a mask) has p = 0, log p = -infinity and no share in the entropy; with a NaN or +infinity among the s_i no result
+ * of that query is a number.
  * scale: finite, not 0. nq: 0 .. 2^19, nq x m at most 2^28. A query and the rows of its k best
  * groups of 32 have to fit a workgroup's memory: several hundred alternatives of very long
  * rows are refused. */
@@ -480,8 +483,17 @@ int avq_log_probs(const void *points, int32_t type, int64_t n, int32_t d, int64_
  *   a_t = sum_j grad_logp_tj - grad_lse_t + grad_entropy_t entropy_t   (sums over ids that are no padding)
  * dqueries_t = scale * sum_i G_ti x_i and dpoints_i = scale * sum_t G_ti q_t (accumulate != 0: added to
  * what dpoints holds). Either may be NULL. lse: as avq_log_probs gave it for the same
- * points, queries and scale, or that of more rows, these among them (a part of a table). 16-bit
- * types: G is rounded to the type for the products of more than a few queries. */
+ * points, queries and scale, or that of more rows, these among them (a part of a table).
+ * Accuracy. p is e^(s - lse), and lse is rounded to fp32: p is off by up to 2^-22 |lse| of itself, that of a given row by
+ * 2^-24 |lse|, of which its G, sum g - p a, has 2^-24 |lse| / (1 - p) of itself where p is nearly 1. Up to eight
+ * queries of fp32 rows (two of up to 1,024 elements, four of 512, eight of 256) are spared this: their p are summed, and
+ * the given rows' G corrected where the sum is within 2^-24 |lse| + 2^-20 of 1, the most that it can be off by
+ * rounding; other rows that have less than that in all count as none. 16-bit types: G is rounded to the type for the
+ * products of more than a few queries (f16: entries below 2^-28 of the query's upstream gradients to 2^-39 of them).
+ * fp32: G of more than a few queries is a pair of f16, off by 2^-21 of an entry or 2^-39 of the query's upstream
+ * gradients, whichever is more, and the s_i are formed again by pairs, a product of two elements being off by 2^-21 of it or
+ * 2^-23 of their row's and query's largest magnitudes. Rows of probability 0 get no gradient; where such a row
+ * holds an infinity, that element of dqueries, 0 times it, may be NaN. */
 int64_t avq_log_probs_grad_scratch(int32_t type, int64_t n, int32_t d, int32_t nq, int32_t m);
 int avq_log_probs_grad(const void *points, int32_t type, int64_t n, int32_t d, int64_t ld_points, const void *queries,
                        int32_t nq, int64_t ld_queries, float scale, const int32_t *ids, int32_t m, const float *lse,

@@ -3,8 +3,8 @@
 //
 // fp32 operands (SPLIT) are two f16 values each: v = (hi + lo) / s with s a power of two that brings the largest magnitude (of a row, or
 // of all rows) to 2^14 .. 2^15, hi = f16(v s), lo = f16(v s - hi). hi hi' + hi lo' + lo hi' differs from v v' s s' by at most 2^-21 of it
-// (lo lo', and the rounding of either lo) where v and v' are 2^-17 of their largest or more; below, lo is a multiple of 2^-24, and v has an
-// error of 2^-40 of the largest. Sums of fp32 products lose as much, at a third of the 16-bit rate: five times the fp32
+// (lo lo', and the rounding of either lo) where v and v' are 2^-16 of their largest or more; below, lo is a multiple of 2^-24, and v has an
+// error of 2^-39 of the largest. Sums of fp32 products lose as much, at a third of the 16-bit rate: five times the fp32
 // matrix instruction's. A row holds 16 hi, then their 16 lo, and so on.
 //
 // A workgroup of four waves forms 256 x 128 values, a wave 128 x 64 (4 x 2 matrix instructions, 128 accumulators), over steps

@@ -54,8 +54,9 @@ __device__ __forceinline__ float4 packed(const Stat &a) { return make_float4(a.m
 __device__ __forceinline__ Stat unpacked(const float4 &v) { return Stat{v.x, v.y, v.z, v.w}; }
 
 // The pass that forms a query's statistics: one query whose rows fit four loads of a wave goes by rows (two, by a kernel of two sums a
-// row: 133 against 117 us through the matrix instructions, 1,183,514 x 100 fp32); up to 64 queries the rows are streamed once; more go
-// by tiles of a matrix product.
+// row: 133 against 117 us through the matrix instructions, 1,183,514 x 100 fp32); up to 64 queries the rows are streamed, once for every 16,
+// 32 or 64 queries, as many as LDS has room for (stream_tile: rows of 1,024 fp32 once for 16, of 1,024 bf16 for 32); more go by tiles
+// of a matrix product. 64 is where the tiles' 128 queries are half full, whatever the type and length; a crossing of each was not measured.
 enum { kByRow = 0, kByStream = 1, kByTiles = 2 };
 inline int prob_path(int size, int d, int nq) { return nq > 64 ? kByTiles : nq == 1 && (size_t)d * size <= 64 * 16 * 4 ? kByRow : kByStream; }
 // Lanes of a row that goes by rows.

@@ -1,10 +1,10 @@
 // Log probabilities of rows of a table under the softmax of a query's inner products with all rows:
 //   s_i = c <q, x_i>,  lse = log sum_i e^s_i,  log p_i = s_i - lse,  H = lse - sum_i p_i s_i,
 // and the k rows of largest s_i (ties: the lower id). One pass over the rows keeps, per query and lane, the running maximum m
-// and the sums of e^(s - m) and e^(s - m) (s - m) in fp32; the logits are never stored. For the best rows it leaves the
+// and the sums of e^(s - m) and e^(s - m) (s - m) in fp32, the first with what fp32 has no room for; the logits are never stored. For the best rows it leaves the
 // largest inner product of every 32 rows; the k groups with the largest of those hold the k best rows, which are scored again.
-// A call: one query, 1,183,514 x 100 fp32, ten best 96 us (pass 72, 6.5 TB/s); 24 queries, 670,091 x 1,024 bf16, twenty best 312 us (pass 255,
-// 5.3 TB/s); 2,048 queries, 1,183,514 x 100 fp32 1.87 ms (pass 1.62: 0.90 PFLOP/s of f16, three products for one).
+// A call: one query, 1,183,514 x 100 fp32, ten best 97 us (pass 72, 6.5 TB/s); 24 queries, 670,091 x 1,024 bf16, twenty best 315 us (pass 256,
+// 5.3 TB/s); 2,048 queries, 1,183,514 x 100 fp32 1.95 ms (pass 1.69: 0.86 PFLOP/s of f16, three products for one).
 #include "mma_tiles.h"
 #include "prob_score.h"
 #include "probs.h"

@@ -5,10 +5,11 @@
 // Three products of 2 n nq d operations each, on the matrix instructions, a part of the rows at a time: the part's logits once
 // more, whose epilogue leaves G transposed, a row's queries side by side, in 16 bits (fp32: pairs of f16); dx = G^T Q, whose inner dimension
 // both operands hold side by side (Q transposed once); dq += G X by operands that are turned as they are read from LDS. G is kept
-// relative to a bound of its magnitude, so that f16 holds it down to 2^-38 of it; its rounding to 16 bits (bf16: 2^-9) is that of
-// the operands' own type. The entries of the given ids, where p is taken from g, are formed by themselves in fp32 before rounding.
+// relative to a bound of its query's, so that f16 holds it down to 2^-39 of that; its rounding to 16 bits (bf16: 2^-9) is that of
+// the operands' own type. The entries of the given ids, where p is taken from g, are formed by themselves in fp32 before rounding; p there
+// has lse's rounding, 2^-24 |lse| of it, which 1 - p keeps as it is however small it is.
 // Bound: the matrix instructions and G's bytes. 1,024 queries, 670,091 x 1,024 bf16, in ms: G 1.50 (0.94 PFLOP/s), dx 1.71 (0.82), dq 1.46 (0.96);
-// 1,001 queries, 1,183,514 x 100 fp32: 1.08, 1.18, 1.26, where G is 4.8 GB, written once and read twice.
+// 1,001 queries, 1,183,514 x 100 fp32: 1.10, 1.18, 1.26, where G is 4.8 GB, written once and read twice.
 #include "mma_tiles.h"
 #include "prob_score.h"
 #include "probs.h"

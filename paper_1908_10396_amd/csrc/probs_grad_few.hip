@@ -1,17 +1,19 @@
 // The gradient of the log probabilities of a few queries (G, dq and dx as in probs_grad.hip), in one pass over the rows: one to eight
 // queries leave the tiles of the matrix instructions, 256 queries wide, almost empty, while a row that is in registers needs nothing
-// else. A row lies across 16, 32 or 64 lanes as units of 16 bytes; its logits are sums over those lanes, G stays in fp32, and the same
+// else. What a lane's registers hold without spilling comes here (grad_few_takes): fp32 rows of up to 1,024 elements for one and two
+// queries, 512 for four, 256 for eight; 16-bit rows of 2,048 for one, 1,024 for two, 512 for four. A row lies across 16, 32 or 64 lanes as units of 16 bytes; its logits are sums over those lanes, G stays in fp32, and the same
 // registers then give dx_i = c sum_t G_ti q_t, written at once, and a lane's share of dq_t = c sum_i G_ti x_i, which stays in registers
 // until the rows are done: waves, then workgroups, are added in a fixed order. Rows are read once and dx is written once.
 // Rows among the given ids are found by a map of 2^16 bits in LDS, which nearly all rows pass by one read; the others look through
 // the ids and score their row by the arithmetic of the pass that lse is of.
 // 1 - p of a row with nearly all of the probability would have the rounding of lse, 2^-24 |lse| / (1 - p) of it. fp32: the pass also sums
 // p over all rows, Z = 1 + delta; to first order p (a + h log p) is too large by delta p (a + h log p + h), which the given rows'
-// entries of G get back at the end, in dq and in dx (elsewhere it is a part in millions of what is there; 16-bit results hide it).
+// entries of G get back at the end, in dq and in dx (elsewhere it is a part in millions of what is there). 16-bit types keep that
+// rounding: with lse near 20 it reaches a bf16 result's own where 1 - p is below 2^-12, an f16 one's below 2^-9.
 // Bound: the rows read and dx written; 16-bit types and eight queries: the arithmetic around them, a lane's registers leaving two
-// waves a SIMD. 1,183,514 x 100 fp32 (0.95 GB): 194 us for one query (4.9 TB/s), 200 for two, 229 for four, 465 for eight, where the
-// tiles take 905 to 950; 200,000 x 1,024 bf16 (0.82 GB): 179 us for one, 205 for two, the tiles 395. Z and what the given rows get back
-// cost 4 to 6 us of an fp32 call. The sizes that a lane's registers hold without spilling are those that come here (grad_few_takes).
+// waves a SIMD. 1,183,514 x 100 fp32 (0.95 GB): 192 us for one query (4.9 TB/s), 199 for two, 238 for four, 484 for eight, where the
+// tiles take 905 to 950; 200,000 x 1,024 bf16 (0.82 GB): 179 us for one, 208 for two, the tiles 395. Z and what the given rows get back
+// cost 4 to 6 us of an fp32 call.
 #include "prob_score.h"
 #include "probs.h"
 #include "row_types.h"

@@ -4,6 +4,10 @@ Rows are torch tensors on the GPU of dtype float32, bfloat16 or float16, one dty
 call; 2-D tensors may have any row stride (slices of wider matrices), with the elements of
 a row side by side. Ids are int32; an id outside [0, n) is padding. Scratch and
 results come from torch's allocator on the stream that the call runs on.
+
+None of this takes part in torch's autograd: results have no history, whatever their
+inputs require, and a model gets its gradients by calling the *_grad forms itself (as
+`learn.Model.gradients` does).
 """
 import collections
 import contextlib
