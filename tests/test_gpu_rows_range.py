@@ -381,6 +381,24 @@ def test_rows_that_are_not_finite_show(kind, nq):
 
 
 @pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [1, 3, 70, 300])
+def test_alternatives_where_there_are_fewer_rows_than_asked_for_without_a_mask(kind, nq):
+    """The masked rows come last, by their ids; a query with all rows masked has them all so."""
+    g = gen(nq)
+    n, d = 130, 40
+    x, q, masked = _masked(n, d, nq, kind, -math.inf, g)
+    r = avq.log_probs(x, q, k=n)
+    good = int((~masked).sum())
+    assert torch.equal(torch.sort(r.alt_ids[:, :good], 1).values.long(), torch.nonzero(~masked)[:, 0].expand(nq, good))
+    assert torch.equal(r.alt_ids[:, good:].long(), torch.nonzero(masked)[:, 0].expand(nq, n - good))
+    assert bool(torch.isfinite(r.alt_logp[:, :good]).all()) and bool((r.alt_logp[:, good:] == -math.inf).all())
+    x[:, -1] = -math.inf
+    r = avq.log_probs(x, q, k=n)
+    assert bool((r.lse == -math.inf).all())
+    assert torch.equal(r.alt_ids.long(), torch.arange(n, device="cuda").expand(nq, n))
+
+
+@pytest.mark.parametrize("kind", TYPES)
 @pytest.mark.parametrize("nq", [1, 2, 3, 7, 12, 65, 300])
 @pytest.mark.parametrize("entropy", [False, True])
 def test_gradients_beside_rows_of_infinite_masks(kind, nq, entropy):
