@@ -292,8 +292,8 @@ __host__ __device__ inline void part_tiles(int64_t tiles, int parts, int p, int6
 
 // ---- rows_pack.hip -------------------------------------------------------------------------
 // Ranges, as bits of non-negative floats (0, for the least infinity: nothing yet): of the rows' inverses, of the largest magnitudes that
-// queries have over their factor in G; and how many rows are odd.
-struct Ranges { uint32_t inverse, least_inverse, weighted, least_weighted, odd; };
+// queries have over their factor in G; the largest bound of a query's G; and how many rows are odd.
+struct Ranges { uint32_t inverse, least_inverse, weighted, least_weighted, upstream, odd; };
 
 // the power of two that brings a largest magnitude to 2^14 .. 2^15 (1 where there is none)
 __device__ __forceinline__ float range_scale(uint32_t largest_bits)

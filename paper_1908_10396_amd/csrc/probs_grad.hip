@@ -23,9 +23,16 @@ namespace avq {
 // weight of other queries costs it nothing; the inverse goes to dq, and with the transposed queries into dx. What dx adds up has one scale
 // all the same: where queries over their factors are apart by more than kWeightSpread, pairs (and f16) would lose the least of them, and
 // dx goes by the fp32 matrix instruction.
+// On top of it all queries have a constant in (1/2, 1] that brings the largest bound to a power of two: where the queries weigh the same, as
+// in a mean, g of a given row is then kept as it is, and not rounded alike in every query.
 struct GradCoef { float a, h, factor, inverse; }; // (inverse 0: nothing comes from this query)
 constexpr float kWeightSpread = 0x1p16f;
 template <class T> constexpr bool kHasFactor = std::is_same<T, float>::value || std::is_same<T, f16_t>::value;
+
+__device__ __forceinline__ float grad_constant(const Ranges *ranges)
+{
+    return ranges->upstream == 0 ? 1.0f : 0x1p14f / (__uint_as_float(ranges->upstream) * range_scale(ranges->upstream));
+}
 
 template <class T> __device__ __forceinline__ bool weights_apart(const Ranges *ranges)
 {
@@ -38,9 +45,9 @@ __global__ __launch_bounds__(256) void grad_coef_kernel(const T *__restrict__ q,
                                                         const float *__restrict__ g, const float *__restrict__ h, const float *__restrict__ entropy, const float *__restrict__ gl,
                                                         GradCoef *__restrict__ coef, Ranges *__restrict__ ranges)
 {
-    __shared__ uint32_t shared_most[4], shared_least[4];
+    __shared__ uint32_t shared_most[4], shared_least[4], shared_bound[4];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, t = blockIdx.x * 4 + wave;
-    uint32_t most = 0, least = 0x7f800000u; // of the query's largest magnitude over its factor
+    uint32_t most = 0, least = 0x7f800000u, bound_bits = 0; // of the query's largest magnitude over its factor; of its bound
     if (t < nq) {
         float a = 0.0f, mag = 0.0f;
         for (int j = lane; j < given; j += 64) {
@@ -67,18 +74,19 @@ __global__ __launch_bounds__(256) void grad_coef_kernel(const T *__restrict__ q,
         if (h) a += ht * entropy[t];
         const float bound = mag + fabsf(a) + fabsf(ht); // of |G| (p |log p| < 0.37)
         const bool some = !(bound == 0.0f);
+        bound_bits = bound < INFINITY ? __float_as_uint(bound) : 0u;
         const float factor = kHasFactor<T> && bound < INFINITY ? range_scale(__float_as_uint(bound)) : 1.0f;
         if (lane == 0) coef[t] = GradCoef{a, ht, factor, some ? 1.0f / factor : 0.0f};
         const uint32_t weighted = __float_as_uint(__uint_as_float(top) / factor);
-        if (some && bound < INFINITY && top != 0 && weighted < 0x7f800000u) most = least = weighted;
+        if (kHasFactor<T> && some && bound < INFINITY && top != 0 && weighted < 0x7f800000u) most = least = weighted;
     }
-    if (!kHasFactor<T>) return;
-    if (lane == 0) { shared_most[wave] = most; shared_least[wave] = least; }
+    if (lane == 0) { shared_most[wave] = most; shared_least[wave] = least; shared_bound[wave] = bound_bits; }
     __syncthreads();
     if (threadIdx.x != 0) return;
 #pragma unroll
-    for (int w = 1; w < 4; ++w) { most = max(most, shared_most[w]); least = min(least, shared_least[w]); }
+    for (int w = 1; w < 4; ++w) { most = max(most, shared_most[w]); least = min(least, shared_least[w]); bound_bits = max(bound_bits, shared_bound[w]); }
     // (maxima and minima: no order matters; asked for first, since most change nothing)
+    if (bound_bits > __hip_atomic_load(&ranges->upstream, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(&ranges->upstream, bound_bits);
     if (most > __hip_atomic_load(&ranges->weighted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(&ranges->weighted, most);
     if (least < __hip_atomic_load(&ranges->least_weighted, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMin(&ranges->least_weighted, least);
 }
@@ -130,8 +138,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_tile_kernel(Rows16 Q, Ro
         const GradCoef c = real ? coef[t] : GradCoef{0.0f, 0.0f, 1.0f, 0.0f};
         ((float *)shift)[threadIdx.x] = real ? -lse[t] * 1.44269504088896341f : -INFINITY;
         if (SPLIT) ((float *)to_logit)[threadIdx.x] = real ? c2 * q_inv[t] * (apart ? 1.0f : __uint_as_float(ranges->inverse)) : 0.0f;
-        ((float *)up)[threadIdx.x] = -c.a * c.factor;
-        if (ENTROPY) ((float *)up_h)[threadIdx.x] = -c.h * c.factor * 0.693147180559945309f;
+        const float f = c.factor * grad_constant(ranges);
+        ((float *)up)[threadIdx.x] = -c.a * f;
+        if (ENTROPY) ((float *)up_h)[threadIdx.x] = -c.h * f * 0.693147180559945309f;
     }
     __syncthreads();
     typedef RowCopies<true, SPLIT> Copies;
@@ -202,7 +211,8 @@ constexpr int64_t kGivenGroups = 1 << 22; // a launch has fewer than 2^32 thread
 template <int PATH, class T>
 __global__ __launch_bounds__(64) void grad_given_kernel(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ q, int nq, int64_t ld_q, int d, float scale, int row_lanes,
                                                         const int32_t *__restrict__ ids, int given, const float *__restrict__ g, const float *__restrict__ lse,
-                                                        const GradCoef *__restrict__ coef, const float *__restrict__ x_inv, const float *__restrict__ q_inv, int64_t lo, int64_t rows, Rows16 G)
+                                                        const GradCoef *__restrict__ coef, const Ranges *__restrict__ ranges, const float *__restrict__ x_inv, const float *__restrict__ q_inv, int64_t lo,
+                                                        int64_t rows, Rows16 G)
 {
     extern __shared__ char lds[];
     T *qs = (T *)lds;
@@ -235,7 +245,7 @@ __global__ __launch_bounds__(64) void grad_given_kernel(const T *__restrict__ x,
             const GradCoef k = coef[t];
             const float p = __builtin_amdgcn_exp2f(logp * 1.44269504088896341f);
             f32x8 one = {};
-            one[0] = (sum - (p > 0.0f || p != p ? p * __fmaf_rn(k.h, logp, k.a) : 0.0f)) * k.factor;
+            one[0] = (sum - (p > 0.0f || p != p ? p * __fmaf_rn(k.h, logp, k.a) : 0.0f)) * (k.factor * grad_constant(ranges));
             Quad hi, low{};
             put16(one, &hi, &low, T{});
             uint16_t *to = (uint16_t *)G.p + block16<sizeof(T) == 4>(t) * G.block + (id - lo) * G.row + turned16((int)t & 15);
@@ -311,7 +321,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void grad_rows_kernel(Rows16 G, Ro
     int count;
     part_tiles(tiles, parts, place.part, &first, &count);
     const bool apart = weights_apart<T>(ranges);
-    const float f = kHasFactor<T> && !apart ? scale * (1.0f / range_scale(ranges->weighted)) : scale;
+    const float f = (kHasFactor<T> && !apart ? scale * (1.0f / range_scale(ranges->weighted)) : scale) / grad_constant(ranges);
     typedef RowCopies<true, true> Copies;
     auto store = [&](int i, f32x16 (&acc)[4][2]) __attribute__((always_inline)) {
         const int64_t row0 = (first + i) * kTileM + acc_row(0, 0);
@@ -448,7 +458,7 @@ __global__ __launch_bounds__(256) void grad_join_kernel(const float *__restrict_
                                                         const GradCoef *__restrict__ coef, T *__restrict__ out, int64_t ld)
 {
     const int64_t all = (int64_t)nq * d;
-    const float f = scale * (fp32 && !rows_apart(ranges) ? __uint_as_float(ranges->inverse) * (1.0f / kRowUnit) : 1.0f);
+    const float f = scale * (fp32 && !rows_apart(ranges) ? __uint_as_float(ranges->inverse) * (1.0f / kRowUnit) : 1.0f) / grad_constant(ranges);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
         float s = 0.0f;
 #pragma unroll 8
@@ -574,7 +584,7 @@ static int log_probs_grad_typed(const ProbGradParams &p, hipStream_t st)
         if (p.given > 0) {
             auto run = [&](auto kernel) {
                 kernel<<<dim3((unsigned)std::min((int64_t)p.nq * p.given, kGivenGroups)), dim3(64), staged_query_bytes(p.d), st>>>((const T *)p.points, p.ld_points, q, p.nq, p.ld_queries, p.d, p.scale, row_lanes(sizeof(T), p.d),
-                                                                                                    p.ids, p.given, p.grad_logp, p.lse, s.coef, s.x_inv, s.q_inv, lo, rows, G);
+                                                                                                    p.ids, p.given, p.grad_logp, p.lse, s.coef, s.ranges, s.x_inv, s.q_inv, lo, rows, G);
             };
             const int path = prob_path(sizeof(T), p.d, p.nq);
             if (path == kByTiles) run(grad_given_kernel<kByTiles, T>);

@@ -5,7 +5,7 @@
 
 namespace avq {
 
-__global__ void clear_ranges_kernel(Ranges *to) { *to = Ranges{0, 0x7f800000u, 0, 0x7f800000u, 0}; }
+__global__ void clear_ranges_kernel(Ranges *to) { *to = Ranges{0, 0x7f800000u, 0, 0x7f800000u, 0, 0}; }
 
 int launch_clear_ranges(Ranges *to, hipStream_t st)
 {

@@ -283,6 +283,25 @@ def test_queries_without_upstream_gradient_beside_others(kind, nq):
     assert not bool(dq.any()) and not bool(dx.any())
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("nq", [12, 21, 77, 300])
+def test_gradient_of_given_rows_under_weights_that_are_alike(kind, nq):
+    """With the gradients of log p and of lse the same, G is g at the given row alone, -1 / nq: 16 bits hold it relative to the largest, so
+    that nothing but the results' own rounding is left."""
+    g = gen(nq)
+    n, d, scale = 900, 64, 0.25
+    x, q = normal((n, d), g, TYPES[kind]), normal((nq, d), g, TYPES[kind])
+    ids = torch.randperm(n, generator=g, device="cuda")[:nq].to(torch.int32)  # (no row is given twice)
+    up = torch.full((nq,), -1.0 / nq, device="cuda")
+    r = avq.log_probs(x, q, ids, scale=scale)
+    dq, dx = avq.log_probs_grad(x, q, ids, r.lse, up, grad_lse=up, scale=scale)
+    want_q, want_x = up.double()[:, None] * x[ids.long()].double() * scale, up.double()[:, None] * q.double() * scale
+    # fp32 beyond a few queries: pairs, 2^-21 of a product
+    bound = HALF[kind] * 1.01 + (2.0 ** -20 if kind == "f32" else 8 * U)
+    within(dq, want_q, bound * want_q.abs() + TINY[kind], "dqueries")
+    within(dx[ids.long()], want_x, bound * want_x.abs() + TINY[kind], "dpoints")
+
+
 @pytest.mark.parametrize("nq", [12, 65, 300])
 def test_fp32_rows_a_little_within_the_spread_of_one_scale(nq):
     """Rows 2^-14.5 of the table's largest, which has no probability: they are all that the queries' gradient is of."""
