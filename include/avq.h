@@ -507,6 +507,86 @@ int avq_index_log_probs(avq_index *idx, const float *queries, int32_t nq, float 
                         float *logp_out, float *lse_out, float *entropy_out, int32_t k, int32_t *alt_ids_out,
                         float *alt_logp_out, void *hip_stream);
 
+/* The softmax over a list of rows of each query's own (what a search returned, sampled rows, a teacher's best ones):
+ * s_tj = scale * <q_t, x_i> + offset_tj with i = ids_tj; lse_out [nq] = log sum_j e^s_tj; logp_out [nq][m] = s_tj - lse_t.
+ * offset: fp32 [nq][m] or NULL (0): minus the log of how likely a row was to be sampled, or -infinity for a mask.
+ * A padding id has no share and logp -infinity; so has an entry whose score is -infinity. A query with nothing else
+ * has lse -infinity. A row that is listed twice counts twice. With a NaN or +infinity among the scores of rows no result of that
+ * query is a number (padding keeps its -infinity). log p keeps its relative accuracy where p is nearly 1. All types are
+ * multiplied and summed in fp32. scale, nq, m and nq x m: as in avq_log_probs. */
+int avq_list_log_probs(const void *points, int32_t type, int64_t n, int32_t d, int64_t ld_points, const void *queries, int32_t nq,
+                       int64_t ld_queries, float scale, const int32_t *ids, int32_t m, const float *offset, float *logp_out,
+                       float *lse_out, void *hip_stream);
+/* Its gradient, for what the loss has as gradients of logp_out (grad_logp [nq][m]) and of lse_out (grad_lse [nq] or NULL), logp being
+ * that call's: with G_tj = grad_logp_tj - p_tj (sum_j grad_logp_tj - grad_lse_t) over the entries whose logp is not -infinity (others
+ * have G = 0, and their grad_logp is not looked at),
+ * doffset [nq][m] = G (always written, the offsets' gradient), dqueries_t = scale * sum_j G_tj x_i and, for all n rows,
+ * dpoints_i = scale * sum of G_tj q_t over ids_tj = i (accumulate != 0: added to the rows that are listed, in fp32 and before
+ * rounding). dqueries and dpoints may be NULL. Entries with G = 0 add nothing, whatever their rows hold. */
+int64_t avq_list_log_probs_grad_scratch(int64_t n, int32_t d, int32_t nq, int32_t m);
+int avq_list_log_probs_grad(const void *points, int32_t type, int64_t n, int32_t d, int64_t ld_points, const void *queries,
+                            int32_t nq, int64_t ld_queries, float scale, const int32_t *ids, int32_t m, const float *logp,
+                            const float *grad_logp, const float *grad_lse, float *doffset, void *dqueries, int64_t ld_dqueries,
+                            void *dpoints, int64_t ld_dpoints, int32_t accumulate, void *scratch, int64_t scratch_bytes,
+                            void *hip_stream);
+
+/* ---- losses of log probabilities ----------------------------------------------
+ * These take log probabilities as the calls above give them (fp32, contiguous) and give the gradient that those calls take as
+ * grad_logp. They are formed in 64 bits and rounded once. Each *_grad call gives the loss too, so that a training
+ * step needs no other; its gradients are those of the losses, times grad_loss. What was said of scratch, capture,
+ * repeated results and overlap holds here too.
+ *
+ * Distillation from a teacher's best rows: logp [rows][m] the student's log probabilities of them, teacher [rows][m] the
+ * teacher's logits z (any type, ld_teacher >= m), P_j = e^(z_j / temperature - lse). With teacher_lse = NULL lse is that of the list, and
+ *   loss = sum_j P_j (log P_j - logp_j).
+ * Else it is teacher_lse [rows], the log of the sum over all of the teacher's e^(z / temperature), and what
+ * teacher and student give to other rows counts as one answer more, R = max(0, 1 - sum_j P_j) and
+ * r = max(1 - sum_j e^logp_j, 2^-20):  loss += R log(R / r). (fp32 log probabilities do not know r better than that.)
+ * The gradient of logp_j is -P_j, + e^logp_j R / r where r is more than 2^-20. An entry with z = -infinity is padding: it
+ * is left out whatever its logp is and has no gradient; a row of nothing else has loss 0. A student's
+ * temperature is a matter of its scale. rows: 0 .. 2^28, m: 0 .. 4096, temperature: finite, > 0. */
+int avq_distill_loss(const float *logp, const void *teacher, int32_t type, int64_t rows, int32_t m, int64_t ld_teacher,
+                     const float *teacher_lse, double temperature, float *loss_out, void *hip_stream);
+int avq_distill_loss_grad(const float *logp, const void *teacher, int32_t type, int64_t rows, int32_t m, int64_t ld_teacher,
+                          const float *teacher_lse, double temperature, const float *grad_loss, float *loss_out /* or NULL */,
+                          float *grad_logp, void *hip_stream);
+
+/* Sequences of tokens lie side by side: sequence s is the tokens offsets[s] .. offsets[s + 1] - 1 of the call's (0 .. 2^28; offsets must
+ * not decrease; ones that leave the call's tokens are taken as their first or last). mask [tokens] or NULL: a token
+ * with 0 counts for nothing, whatever its other values are (log_probs gives -infinity for padding). Gradients are
+ * zeros for masked tokens and those of no sequence. average != 0: a sequence's sum is divided by the number of its
+ * tokens that count (an empty one's is 0 all the same).
+ *
+ * Preferences between two answers: sequence 2 p is preferred to sequence 2 p + 1. With D_s the sum of logp - ref (ref [tokens] or
+ * NULL: 0), reward_s = beta D_s (reward_out [2 pairs] or NULL), logit_p = reward_2p - reward_2p+1 - margin, and
+ *   loss_p = -(1 - smoothing) log sigma(logit_p) - smoothing log sigma(-logit_p).
+ * pairs: 0 .. 2^22; beta, margin finite; smoothing 0 .. 1. */
+int64_t avq_preference_loss_scratch(int64_t tokens, int32_t pairs);
+int avq_preference_loss(const float *logp, const float *ref, const uint8_t *mask, int64_t tokens, const int32_t *offsets,
+                        int32_t pairs, double beta, double margin, double smoothing, int32_t average, float *loss_out,
+                        float *logit_out, float *reward_out, void *scratch, int64_t scratch_bytes, void *hip_stream);
+int avq_preference_loss_grad(const float *logp, const float *ref, const uint8_t *mask, int64_t tokens, const int32_t *offsets,
+                             int32_t pairs, double beta, double margin, double smoothing, int32_t average,
+                             const float *grad_loss, float *loss_out, float *logit_out, float *reward_out, float *grad_logp,
+                             void *scratch, int64_t scratch_bytes, void *hip_stream);
+
+/* A policy's clipped loss: per token, r = e^(logp - old), A its advantage ([tokens] where each != 0, else [sequences]),
+ *   k = e^(ref - logp) - (ref - logp) - 1 (ref [tokens] or NULL: 0; needed where kl_weight is not 0),
+ *   l = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A) + kl_weight k,
+ * and per sequence the sum of l (loss_out) and of k (kl_out or NULL), and the share of its tokens that are
+ * clipped, r > 1 + clip_high with A > 0 or r < 1 - clip_low with A < 0 (clipped_out or NULL); those have the gradient of
+ * kl_weight k alone. sequences: 0 .. 2^23; clip_low 0 .. 1, clip_high and kl_weight finite, >= 0. */
+int64_t avq_policy_loss_scratch(int64_t tokens, int32_t sequences);
+int avq_policy_loss(const float *logp, const float *old, const float *ref, const float *advantage, int32_t each,
+                    const uint8_t *mask, int64_t tokens, const int32_t *offsets, int32_t sequences, double clip_low,
+                    double clip_high, double kl_weight, int32_t average, float *loss_out, float *kl_out, float *clipped_out,
+                    void *scratch, int64_t scratch_bytes, void *hip_stream);
+int avq_policy_loss_grad(const float *logp, const float *old, const float *ref, const float *advantage, int32_t each,
+                         const uint8_t *mask, int64_t tokens, const int32_t *offsets, int32_t sequences, double clip_low,
+                         double clip_high, double kl_weight, int32_t average, const float *grad_loss, float *loss_out,
+                         float *kl_out, float *clipped_out, float *grad_logp, void *scratch, int64_t scratch_bytes,
+                         void *hip_stream);
+
 const char *avq_last_error(void);
 const char *avq_version(void);
 

@@ -28,6 +28,8 @@ SYMBOLS = [
     "avq_profile_enable", "avq_profile_read", "avq_last_error", "avq_version",
     "avq_embed", "avq_embed_grad_scratch", "avq_embed_grad", "avq_layer_norm", "avq_layer_norm_grad_scratch", "avq_layer_norm_grad",
     "avq_log_probs_scratch", "avq_log_probs", "avq_log_probs_grad_scratch", "avq_log_probs_grad", "avq_index_log_probs",
+    "avq_list_log_probs", "avq_list_log_probs_grad_scratch", "avq_list_log_probs_grad", "avq_distill_loss", "avq_distill_loss_grad",
+    "avq_preference_loss_scratch", "avq_preference_loss", "avq_preference_loss_grad", "avq_policy_loss_scratch", "avq_policy_loss", "avq_policy_loss_grad",
 ]
 
 
@@ -100,7 +102,20 @@ def lib():
         L.avq_log_probs_grad_scratch.argtypes = [i32, i64, i32, i32, i32]
         L.avq_log_probs_grad.argtypes = [vp, i32, i64, i32, i64, vp, i32, i64, f32, vp, i32, vp, vp, vp, vp, vp, vp, i64, vp, i64, i32, vp, i64, vp]
         L.avq_index_log_probs.argtypes = [vp, vp, i32, f32, vp, i32, vp, vp, vp, i32, vp, vp, vp]
-        for name in ("avq_embed_grad_scratch", "avq_layer_norm_grad_scratch", "avq_log_probs_scratch", "avq_log_probs_grad_scratch"):
+        f64 = C.c_double
+        L.avq_list_log_probs.argtypes = [vp, i32, i64, i32, i64, vp, i32, i64, f32, vp, i32, vp, vp, vp, vp]
+        L.avq_list_log_probs_grad_scratch.argtypes = [i64, i32, i32, i32]
+        L.avq_list_log_probs_grad.argtypes = [vp, i32, i64, i32, i64, vp, i32, i64, f32, vp, i32, vp, vp, vp, vp, vp, i64, vp, i64, i32, vp, i64, vp]
+        L.avq_distill_loss.argtypes = [vp, vp, i32, i64, i32, i64, vp, f64, vp, vp]
+        L.avq_distill_loss_grad.argtypes = [vp, vp, i32, i64, i32, i64, vp, f64, vp, vp, vp, vp]
+        L.avq_preference_loss_scratch.argtypes = [i64, i32]
+        L.avq_preference_loss.argtypes = [vp, vp, vp, i64, vp, i32, f64, f64, f64, i32, vp, vp, vp, vp, i64, vp]
+        L.avq_preference_loss_grad.argtypes = [vp, vp, vp, i64, vp, i32, f64, f64, f64, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.avq_policy_loss_scratch.argtypes = [i64, i32]
+        L.avq_policy_loss.argtypes = [vp, vp, vp, vp, i32, vp, i64, vp, i32, f64, f64, f64, i32, vp, vp, vp, vp, i64, vp]
+        L.avq_policy_loss_grad.argtypes = [vp, vp, vp, vp, i32, vp, i64, vp, i32, f64, f64, f64, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+        for name in ("avq_embed_grad_scratch", "avq_layer_norm_grad_scratch", "avq_log_probs_scratch", "avq_log_probs_grad_scratch",
+                     "avq_list_log_probs_grad_scratch", "avq_preference_loss_scratch", "avq_policy_loss_scratch"):
             getattr(L, name).restype = i64
         L.avq_last_error.restype = C.c_char_p
         L.avq_version.restype = C.c_char_p
@@ -410,13 +425,19 @@ class Index:
         return ids, ip
 
 
-# the operators on rows of learned vectors; their module imports torch, which this one does not need to be imported
-_ROWS = ("LogProbs", "embed", "embed_grad", "layer_norm", "layer_norm_grad", "log_probs", "log_probs_grad")
+# the operators on rows of learned vectors, and the losses; their modules import torch, which this one does not need to be imported
+_ROWS = ("LogProbs", "embed", "embed_grad", "layer_norm", "layer_norm_grad", "log_probs", "log_probs_grad",
+         "ListLogProbs", "list_log_probs", "list_log_probs_grad")
+_LOSSES = ("PreferenceLoss", "PolicyLoss", "distill_loss", "distill_loss_grad", "preference_loss", "preference_loss_grad", "policy_loss", "policy_loss_grad")
 
 
 def __getattr__(name):
-    if name not in _ROWS:
+    if name in _ROWS:
+        from . import rows as module
+    elif name in _LOSSES:
+        from . import losses as module
+    else:
         raise AttributeError("module %r has no attribute %r" % (__name__, name))
-    from . import rows
-    globals().update({n: getattr(rows, n) for n in _ROWS})
+    names = _ROWS if name in _ROWS else _LOSSES
+    globals().update({n: getattr(module, n) for n in names})
     return globals()[name]

@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libavq.so")
 UNITS = ["api", "lut", "scan", "scan_mfma", "product", "product_leaf", "refine", "select", "ivf", "layout", "nearest", "exact", "train",
-         "rows_api", "rows_pack", "embed", "norm", "probs", "probs_grad", "probs_grad_few"]
+         "rows_api", "rows_pack", "embed", "norm", "probs", "probs_grad", "probs_grad_few", "list_probs", "losses"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17",

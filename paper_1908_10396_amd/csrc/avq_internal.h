@@ -561,6 +561,8 @@ struct EmbedGradParams {
     const int32_t *ids; int64_t count; float scale;
     void *out; int64_t n; int32_t d; int64_t ld_out; int32_t accumulate;
     void *scratch;
+    // position i adds weights[i] times row i / per_row of grad (NULL: row i itself)
+    const float *weights = nullptr; int32_t per_row = 1;
 };
 size_t embed_grad_scratch_bytes(int64_t n, int d, int64_t count);
 int launch_embed_grad(const EmbedGradParams &p, hipStream_t st);
@@ -602,5 +604,42 @@ struct ProbGradParams {
 };
 size_t log_probs_grad_scratch_bytes(int type, int64_t n, int d, int nq, int given);
 int launch_log_probs_grad(const ProbGradParams &p, hipStream_t st);
+
+// ---- what rows and log probabilities learn from (list_probs.hip, losses.hip) -----------------------
+struct ListParams {
+    const void *points; int32_t type; int64_t n; int32_t d; int64_t ld_points;
+    const void *queries; int32_t nq; int64_t ld_queries; float scale;
+    const int32_t *ids; int32_t m; const float *offset; float *logp, *lse;
+};
+int launch_list_probs(const ListParams &p, hipStream_t st);
+struct ListGradParams {
+    const void *points; int32_t type; int64_t n; int32_t d; int64_t ld_points;
+    const void *queries; int32_t nq; int64_t ld_queries; float scale;
+    const int32_t *ids; int32_t m; const float *logp, *grad_logp, *grad_lse; float *dscores;
+    void *dqueries; int64_t ld_dqueries; void *dpoints; int64_t ld_dpoints; int32_t accumulate;
+    void *scratch;
+};
+size_t list_grad_scratch_bytes(int64_t n, int d, int nq, int m);
+int launch_list_grad(const ListGradParams &p, hipStream_t st);
+
+struct DistillParams { // grad_loss and grad_logp: both or neither; loss may be NULL with them
+    const float *logp; const void *teacher; int32_t type; int64_t ld_teacher; const float *teacher_lse; double temperature;
+    int64_t rows; int32_t m; float *loss; const float *grad_loss; float *grad_logp;
+};
+int launch_distill(const DistillParams &p, hipStream_t st);
+struct PreferenceParams { // ref, mask may be NULL; so may reward; grad_loss and grad_logp: both or neither
+    const float *logp, *ref; const uint8_t *mask; int64_t tokens; const int32_t *offsets; int32_t pairs;
+    double beta, margin, smoothing; int32_t average;
+    float *loss, *logit, *reward; const float *grad_loss; float *grad_logp; void *scratch;
+};
+size_t preference_scratch_bytes(int64_t tokens, int pairs);
+int launch_preference(const PreferenceParams &p, hipStream_t st);
+struct PolicyParams { // ref, mask, kl, clipped may be NULL; grad_loss and grad_logp: both or neither
+    const float *logp, *old, *ref, *advantage; int32_t each; const uint8_t *mask; int64_t tokens; const int32_t *offsets; int32_t sequences;
+    double clip_low, clip_high, kl_weight; int32_t average;
+    float *loss, *kl, *clipped; const float *grad_loss; float *grad_logp; void *scratch;
+};
+size_t policy_scratch_bytes(int64_t tokens, int sequences);
+int launch_policy(const PolicyParams &p, hipStream_t st);
 
 } // namespace avq

@@ -322,24 +322,29 @@ __device__ __forceinline__ void write_row(T *__restrict__ row, int k, int d, con
 // Each team of `lanes` threads takes a chunk of kRunChunk sorted entries. A run that lies within the chunk goes to its
 // row; what belongs to a run that crosses the chunk's start or end goes to partial[chunk][0] or [1] (a run through the
 // whole chunk: [0]). The rows of eight entries are asked for while the eight before are added up.
-template <class T, bool RAGGED>
+// WEIGHTED: position i adds weights[i] times row i / per_grad of grad.
+template <class T, bool RAGGED, bool WEIGHTED>
 __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ grad, int64_t ld_grad, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos,
                                                        uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out, int64_t ld_out, int accumulate,
-                                                       float *__restrict__ partial)
+                                                       float *__restrict__ partial, const float *__restrict__ weights, uint32_t per_grad)
 {
     constexpr int kTeams = 64, V = kUnit<T>; // teams of 4 lanes, at most
     __shared__ uint32_t skeys[kTeams * kRunChunk], spos[kTeams * kRunChunk];
+    __shared__ float sweight[WEIGHTED ? kTeams * kRunChunk : 1];
     const uint32_t teams = 256u / (uint32_t)lanes, team = threadIdx.x / (uint32_t)lanes;
     const uint32_t all_begin = blockIdx.x * teams * (uint32_t)kRunChunk;
     for (uint32_t i = threadIdx.x; i < teams * (uint32_t)kRunChunk; i += 256) {
         // (key n: a run that goes nowhere; its rows are read all the same, so that no load waits for a branch)
         skeys[i] = all_begin + i < count ? keys[all_begin + i] : n;
-        spos[i] = all_begin + i < count ? pos[all_begin + i] : 0u;
+        const uint32_t p = all_begin + i < count ? pos[all_begin + i] : 0u;
+        spos[i] = WEIGHTED ? p / per_grad : p;
+        if (WEIGHTED) sweight[i] = skeys[i] < n ? weights[p] : 0.0f;
     }
     __syncthreads();
     const uint32_t chunk = blockIdx.x * teams + team, begin = chunk * (uint32_t)kRunChunk;
     if (begin >= count) return;
     const uint32_t *ks = skeys + team * kRunChunk, *ps = spos + team * kRunChunk;
+    const float *ws = sweight + (WEIGHTED ? team * kRunChunk : 0);
     const uint32_t end = min(count, begin + (uint32_t)kRunChunk);
     const uint32_t per_row = (uint32_t)units_of<T>(d), dp = per_row * V; // (parts are padded)
     const uint32_t before = begin > 0 ? keys[begin - 1] : 0xffffffffu; // (no key is that)
@@ -368,6 +373,7 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const uint32_t next = ks[i0 + u];
+                const float weight = WEIGHTED ? ws[i0 + u] : 1.0f;
                 if (next != key) {
                     if (key < n) {
                         if (from_start && key == before) partial_row(0);
@@ -379,7 +385,10 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
                     for (int e = 0; e < V; ++e) acc[e] = 0.0f;
                 }
 #pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] += to_f32(r.v[u].e[e]);
+                for (int e = 0; e < V; ++e) {
+                    if (!WEIGHTED) acc[e] += to_f32(r.v[u].e[e]);
+                    else if (weight != 0.0f) acc[e] = __fmaf_rn(weight, to_f32(r.v[u].e[e]), acc[e]); // (no weight: nothing, whatever the row holds)
+                }
             }
         };
         static_assert(kRunChunk == 4 * kAhead, "two pairs of eights");
@@ -548,8 +557,9 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
     while (lanes < 256 && lanes < units_of<T>(p.d)) lanes *= 2;
     const int64_t chunks = (p.count + kRunChunk - 1) / kRunChunk;
     const int sums = (int)((chunks + 256 / lanes - 1) / (256 / lanes));
-    run_sums_kernel<T, RAGGED><<<dim3(sums), dim3(256), 0, st>>>((const T *)p.grad, p.ld_grad, keys, pos, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out,
-                                                                                                  p.accumulate, s.partial);
+    const auto kernel = p.weights ? run_sums_kernel<T, RAGGED, true> : run_sums_kernel<T, RAGGED, false>;
+    kernel<<<dim3(sums), dim3(256), 0, st>>>((const T *)p.grad, p.ld_grad, keys, pos, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial, p.weights,
+                                             (uint32_t)p.per_row);
     AVQ_HIP(hipGetLastError());
     if (chunks > 1) {
         run_joins_kernel<T, RAGGED><<<dim3((unsigned)std::min(chunks, kJoinGroups)), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);

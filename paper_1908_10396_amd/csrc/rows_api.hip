@@ -210,3 +210,165 @@ extern "C" int avq_log_probs_grad(const void *points, int32_t type, int64_t n, i
                                                 ld_dqueries, dpoints, ld_dpoints, accumulate != 0, scratch},
                                  (hipStream_t)hip_stream);
 }
+
+extern "C" int avq_list_log_probs(const void *points, int32_t type, int64_t n, int32_t d, int64_t ld_points, const void *queries, int32_t nq, int64_t ld_queries, float scale,
+                                  const int32_t *ids, int32_t m, const float *offset, float *logp_out, float *lse_out, void *hip_stream)
+{
+    AVQ_TRY(check_probs(type, n, d, nq, m, scale));
+    AVQ_TRY(check_rows(points, n, d, ld_points, type, "points"));
+    AVQ_TRY(check_rows(queries, nq, d, ld_queries, type, "queries"));
+    if (nq > 0) {
+        if (!lse_out) return refuse("lse_out is NULL");
+        if (m > 0 && (!ids || !logp_out)) return refuse("ids and logp_out are needed for m > 0");
+    }
+    return launch_list_probs(ListParams{points, type, n, d, ld_points, queries, nq, ld_queries, scale, ids, m, offset, logp_out, lse_out}, (hipStream_t)hip_stream);
+}
+
+extern "C" int64_t avq_list_log_probs_grad_scratch(int64_t n, int32_t d, int32_t nq, int32_t m)
+{
+    if (check_probs(AVQ_F32, n, d, nq, m, 1.0f) != AVQ_OK) return AVQ_EINVAL;
+    return (int64_t)list_grad_scratch_bytes(n, d, nq, m);
+}
+
+extern "C" int avq_list_log_probs_grad(const void *points, int32_t type, int64_t n, int32_t d, int64_t ld_points, const void *queries, int32_t nq, int64_t ld_queries, float scale,
+                                       const int32_t *ids, int32_t m, const float *logp, const float *grad_logp, const float *grad_lse, float *doffset, void *dqueries,
+                                       int64_t ld_dqueries, void *dpoints, int64_t ld_dpoints, int32_t accumulate, void *scratch, int64_t scratch_bytes, void *hip_stream)
+{
+    AVQ_TRY(check_probs(type, n, d, nq, m, scale));
+    AVQ_TRY(check_rows(points, n, d, ld_points, type, "points"));
+    AVQ_TRY(check_rows(queries, nq, d, ld_queries, type, "queries"));
+    if (dqueries) AVQ_TRY(check_rows(dqueries, nq, d, ld_dqueries, type, "dqueries"));
+    if (dpoints) AVQ_TRY(check_rows(dpoints, n, d, ld_dpoints, type, "dpoints"));
+    if (nq > 0 && m > 0 && (!ids || !logp || !grad_logp || !doffset)) return refuse("ids, logp, grad_logp and doffset are needed for m > 0");
+    AVQ_TRY(check_scratch(scratch, scratch_bytes, list_grad_scratch_bytes(n, d, nq, m)));
+    return launch_list_grad(ListGradParams{points, type, n, d, ld_points, queries, nq, ld_queries, scale, ids, m, logp, grad_logp, grad_lse, doffset, dqueries, ld_dqueries, dpoints,
+                                           ld_dpoints, accumulate != 0, scratch},
+                            (hipStream_t)hip_stream);
+}
+
+namespace {
+
+int check_distill(const DistillParams &p)
+{
+    AVQ_TRY(check_type(p.type));
+    AVQ_TRY(check_count(p.rows));
+    if (p.m < 0 || p.m > kMaxGiven) { set_error("m must be 0 .. %d, got %d", kMaxGiven, p.m); return AVQ_EINVAL; }
+    AVQ_TRY(check_rows(p.teacher, p.m > 0 ? p.rows : 0, p.m, p.ld_teacher, p.type, "teacher"));
+    if (!(std::isfinite(p.temperature) && p.temperature > 0.0 && std::isfinite(1.0 / p.temperature))) return refuse("temperature must be finite and positive");
+    if (p.rows > 0 && p.m > 0 && !p.logp) return refuse("logp is NULL");
+    return AVQ_OK;
+}
+
+constexpr int kMaxSequences = 1 << 23;
+
+int check_sequences(const float *logp, int64_t tokens, const int32_t *offsets, int32_t sequences)
+{
+    AVQ_TRY(check_count(tokens));
+    if (sequences < 0 || sequences > kMaxSequences) { set_error("sequences must be 0 .. %d, got %d", kMaxSequences, sequences); return AVQ_EINVAL; }
+    if (tokens > 0 && !logp) return refuse("logp is NULL");
+    if (sequences > 0 && !offsets) return refuse("offsets is NULL");
+    return AVQ_OK;
+}
+
+// the gradient's part of the arguments
+int check_upstream(const float *grad_loss, const float *grad_logp, int64_t losses, int64_t tokens)
+{
+    if (losses > 0 && !grad_loss) return refuse("grad_loss is NULL");
+    return tokens > 0 && !grad_logp ? refuse("grad_logp is NULL") : AVQ_OK;
+}
+
+int check_preference(const PreferenceParams &p)
+{
+    if (p.pairs < 0 || p.pairs > kMaxSequences / 2) { set_error("pairs must be 0 .. %d, got %d", kMaxSequences / 2, p.pairs); return AVQ_EINVAL; }
+    AVQ_TRY(check_sequences(p.logp, p.tokens, p.offsets, 2 * p.pairs));
+    if (!std::isfinite(p.beta) || !std::isfinite(p.margin)) return refuse("beta and margin must be finite");
+    if (!(p.smoothing >= 0.0 && p.smoothing <= 1.0)) return refuse("smoothing must be 0 .. 1");
+    return p.pairs > 0 && (!p.loss || !p.logit) ? refuse("loss_out and logit_out are needed") : AVQ_OK;
+}
+
+int check_policy(const PolicyParams &p)
+{
+    AVQ_TRY(check_sequences(p.logp, p.tokens, p.offsets, p.sequences));
+    if (p.tokens > 0 && !p.old) return refuse("old is NULL");
+    if (!p.advantage && (p.each ? p.tokens : p.sequences) > 0) return refuse("advantage is NULL");
+    if (!(p.clip_low >= 0.0 && p.clip_low <= 1.0)) return refuse("clip_low must be 0 .. 1");
+    if (!(std::isfinite(p.clip_high) && p.clip_high >= 0.0)) return refuse("clip_high must be finite and not negative");
+    if (!(std::isfinite(p.kl_weight) && p.kl_weight >= 0.0)) return refuse("kl_weight must be finite and not negative");
+    if (p.kl_weight != 0.0 && !p.ref && p.tokens > 0) return refuse("kl_weight needs ref");
+    return p.sequences > 0 && !p.loss ? refuse("loss_out is NULL") : AVQ_OK;
+}
+
+} // namespace
+
+extern "C" int avq_distill_loss(const float *logp, const void *teacher, int32_t type, int64_t rows, int32_t m, int64_t ld_teacher, const float *teacher_lse, double temperature,
+                                float *loss_out, void *hip_stream)
+{
+    const DistillParams p{logp, teacher, type, ld_teacher, teacher_lse, temperature, rows, m, loss_out, nullptr, nullptr};
+    AVQ_TRY(check_distill(p));
+    if (rows > 0 && !loss_out) return refuse("loss_out is NULL");
+    return launch_distill(p, (hipStream_t)hip_stream);
+}
+
+extern "C" int avq_distill_loss_grad(const float *logp, const void *teacher, int32_t type, int64_t rows, int32_t m, int64_t ld_teacher, const float *teacher_lse, double temperature,
+                                     const float *grad_loss, float *loss_out, float *grad_logp, void *hip_stream)
+{
+    const DistillParams p{logp, teacher, type, ld_teacher, teacher_lse, temperature, rows, m, loss_out, grad_loss, grad_logp};
+    AVQ_TRY(check_distill(p));
+    AVQ_TRY(check_upstream(grad_loss, grad_logp, rows, rows * m));
+    return launch_distill(p, (hipStream_t)hip_stream);
+}
+
+extern "C" int64_t avq_preference_loss_scratch(int64_t tokens, int32_t pairs)
+{
+    if (check_count(tokens) != AVQ_OK || pairs < 0 || pairs > kMaxSequences / 2) return refuse("tokens must be 0 .. 2^28 and pairs 0 .. 2^22");
+    return (int64_t)preference_scratch_bytes(tokens, pairs);
+}
+
+extern "C" int avq_preference_loss(const float *logp, const float *ref, const uint8_t *mask, int64_t tokens, const int32_t *offsets, int32_t pairs, double beta, double margin,
+                                   double smoothing, int32_t average, float *loss_out, float *logit_out, float *reward_out, void *scratch, int64_t scratch_bytes, void *hip_stream)
+{
+    const PreferenceParams p{logp, ref, mask, tokens, offsets, pairs, beta, margin, smoothing, average != 0, loss_out, logit_out, reward_out, nullptr, nullptr, scratch};
+    AVQ_TRY(check_preference(p));
+    AVQ_TRY(check_scratch(scratch, scratch_bytes, preference_scratch_bytes(tokens, pairs)));
+    return launch_preference(p, (hipStream_t)hip_stream);
+}
+
+extern "C" int avq_preference_loss_grad(const float *logp, const float *ref, const uint8_t *mask, int64_t tokens, const int32_t *offsets, int32_t pairs, double beta, double margin,
+                                        double smoothing, int32_t average, const float *grad_loss, float *loss_out, float *logit_out, float *reward_out, float *grad_logp,
+                                        void *scratch, int64_t scratch_bytes, void *hip_stream)
+{
+    const PreferenceParams p{logp, ref, mask, tokens, offsets, pairs, beta, margin, smoothing, average != 0, loss_out, logit_out, reward_out, grad_loss, grad_logp, scratch};
+    AVQ_TRY(check_preference(p));
+    AVQ_TRY(check_upstream(grad_loss, grad_logp, pairs, tokens));
+    AVQ_TRY(check_scratch(scratch, scratch_bytes, preference_scratch_bytes(tokens, pairs)));
+    return tokens == 0 && pairs == 0 ? AVQ_OK : launch_preference(p, (hipStream_t)hip_stream);
+}
+
+extern "C" int64_t avq_policy_loss_scratch(int64_t tokens, int32_t sequences)
+{
+    if (check_count(tokens) != AVQ_OK || sequences < 0 || sequences > kMaxSequences) return refuse("tokens must be 0 .. 2^28 and sequences 0 .. 2^23");
+    return (int64_t)policy_scratch_bytes(tokens, sequences);
+}
+
+extern "C" int avq_policy_loss(const float *logp, const float *old, const float *ref, const float *advantage, int32_t each, const uint8_t *mask, int64_t tokens,
+                               const int32_t *offsets, int32_t sequences, double clip_low, double clip_high, double kl_weight, int32_t average, float *loss_out, float *kl_out,
+                               float *clipped_out, void *scratch, int64_t scratch_bytes, void *hip_stream)
+{
+    const PolicyParams p{logp, old, ref, advantage, each != 0, mask, tokens, offsets, sequences, clip_low, clip_high, kl_weight, average != 0, loss_out, kl_out, clipped_out, nullptr,
+                         nullptr, scratch};
+    AVQ_TRY(check_policy(p));
+    AVQ_TRY(check_scratch(scratch, scratch_bytes, policy_scratch_bytes(tokens, sequences)));
+    return launch_policy(p, (hipStream_t)hip_stream);
+}
+
+extern "C" int avq_policy_loss_grad(const float *logp, const float *old, const float *ref, const float *advantage, int32_t each, const uint8_t *mask, int64_t tokens,
+                                    const int32_t *offsets, int32_t sequences, double clip_low, double clip_high, double kl_weight, int32_t average, const float *grad_loss,
+                                    float *loss_out, float *kl_out, float *clipped_out, float *grad_logp, void *scratch, int64_t scratch_bytes, void *hip_stream)
+{
+    const PolicyParams p{logp, old, ref, advantage, each != 0, mask, tokens, offsets, sequences, clip_low, clip_high, kl_weight, average != 0, loss_out, kl_out, clipped_out, grad_loss,
+                         grad_logp, scratch};
+    AVQ_TRY(check_policy(p));
+    AVQ_TRY(check_upstream(grad_loss, grad_logp, sequences, tokens));
+    AVQ_TRY(check_scratch(scratch, scratch_bytes, policy_scratch_bytes(tokens, sequences)));
+    return tokens == 0 && sequences == 0 ? AVQ_OK : launch_policy(p, (hipStream_t)hip_stream);
+}

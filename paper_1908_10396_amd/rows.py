@@ -23,6 +23,9 @@ LogProbs = collections.namedtuple("LogProbs", "logp lse entropy alt_ids alt_logp
 LogProbs.__doc__ = """What log_probs returns: logp (log probabilities of the given ids, None without ids), lse and entropy [nq] (fp32),
 alt_ids (int32) and alt_logp [nq][k] (None for k = 0)."""
 
+ListLogProbs = collections.namedtuple("ListLogProbs", "logp lse")
+ListLogProbs.__doc__ = """What list_log_probs returns: logp [nq][m] and lse [nq] (fp32)."""
+
 
 def _type(t, what):
     kind = _TYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
@@ -299,3 +302,62 @@ def log_probs_grad(points, queries, ids, lse, grad_logp, entropy=None, grad_entr
         _check(lib().avq_log_probs_grad(pp, kind, n, d, lp, qp, nq, lq, scale, _ptr(ids), m, lsep, entp, up, upe, upl, dq.data_ptr(), d,
                                          op, lo, 1 if accumulate else 0, ws.data_ptr(), ws.numel(), st))
     return dq, out_points
+
+
+def _listed(ids, nq):
+    ids = _ids(ids)
+    if ids.dim() != 2 or ids.shape[0] != nq:
+        raise ValueError("ids: shape %s, expected (%d, *)" % (tuple(ids.shape), nq))
+    return ids, ids.shape[1]
+
+
+def list_log_probs(points, queries, ids, offset=None, scale=1.0, stream=None):
+    """avq_list_log_probs: the softmax over each query's own list of rows, ids [nq][m], of scale * <query, row> + offset
+    (fp32 [nq][m] or None). Returns ListLogProbs."""
+    kind = _type(points, "points")
+    _type(queries, "queries")
+    pp, lp = _matrix(points, "points")
+    n, d = points.shape
+    qp, lq = _matrix(queries, "queries", cols=d, like=points)
+    nq = queries.shape[0]
+    ids, m = _listed(ids, nq)
+    op = _vector(offset, "offset", nq * m, torch.float32)
+    _same_device(points, queries, ids, offset)
+    with _on(points, stream) as st:
+        logp = torch.empty((nq, m), dtype=torch.float32, device=points.device)
+        lse = torch.empty(nq, dtype=torch.float32, device=points.device)
+        _check(lib().avq_list_log_probs(pp, kind, n, d, lp, qp, nq, lq, scale, ids.data_ptr(), m, op, logp.data_ptr(), lse.data_ptr(), st))
+    return ListLogProbs(logp, lse)
+
+
+def list_log_probs_grad(points, queries, ids, logp, grad_logp, grad_lse=None, scale=1.0, out_points=None, accumulate=False, stream=None):
+    """avq_list_log_probs_grad: (dqueries, dpoints, doffset) for the gradients of the loss with respect to the results of
+    list_log_probs(points, queries, ids, scale=scale), grad_logp [nq][m] and grad_lse [nq] or None; logp is that call's.
+    With out_points dpoints goes there, and is added to it with accumulate=True."""
+    kind = _type(points, "points")
+    _type(queries, "queries")
+    pp, lp = _matrix(points, "points")
+    n, d = points.shape
+    qp, lq = _matrix(queries, "queries", cols=d, like=points)
+    nq = queries.shape[0]
+    ids, m = _listed(ids, nq)
+    f32 = torch.float32
+    logpp, up, upl = _vector(logp, "logp", nq * m, f32), _vector(grad_logp, "grad_logp", nq * m, f32), _vector(grad_lse, "grad_lse", nq, f32)
+    if logp is None or grad_logp is None:
+        raise ValueError("logp and grad_logp are needed")
+    if out_points is not None:
+        _type(out_points, "out_points")
+        _matrix(out_points, "out_points", cols=d, rows=n, like=points)
+    elif accumulate:
+        raise ValueError("accumulate needs out_points")
+    _same_device(points, queries, ids, logp, grad_logp, grad_lse, out_points)
+    with _on(points, stream) as st:
+        ws = _scratch(lib().avq_list_log_probs_grad_scratch(n, d, nq, m), points.device)
+        dq = torch.empty((nq, d), dtype=points.dtype, device=points.device)
+        do = torch.empty((nq, m), dtype=f32, device=points.device)
+        if out_points is None:
+            out_points = torch.empty((n, d), dtype=points.dtype, device=points.device)
+        op, lo = _matrix(out_points, "out_points")
+        _check(lib().avq_list_log_probs_grad(pp, kind, n, d, lp, qp, nq, lq, scale, ids.data_ptr(), m, logpp, up, upl, do.data_ptr(), dq.data_ptr(), d,
+                                              op, lo, 1 if accumulate else 0, ws.data_ptr(), ws.numel(), st))
+    return dq, out_points, do
