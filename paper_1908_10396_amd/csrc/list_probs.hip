@@ -39,105 +39,240 @@ __device__ __forceinline__ float list_sum(float v, float *red)
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// log p of a query's m entries from their scores (padding: NaN or anything, by its id), and lse. The sum is kept relative to the largest
-// score without the 1 of that itself, so that log p keeps its relative accuracy where p is nearly 1.
-__device__ __forceinline__ void list_softmax(const float *scores, const int32_t *__restrict__ ids, int64_t n, int m, float *red, float *logp, float *lse)
+// A few queries with long lists: a workgroup takes a part of a query's list, so that there are a thousand of them. 64 entries at least, with
+// which every lane has a load or more in flight.
+constexpr int kListGroups = 1024, kListPart = 64;
+struct ListParts { int parts, each; };
+__host__ __device__ inline ListParts list_parts(int nq, int m)
 {
-    float top = -INFINITY;
-    for (int j = threadIdx.x; j < m; j += kListThreads) {
-        const int32_t id = ids[j];
-        if (id >= 0 && (int64_t)id < n) top = fmaxf(top, scores[j]);
+    const int most = (m + kListPart - 1) / kListPart, want = (kListGroups + nq - 1) / nq;
+    const int parts = want < most ? want : most;
+    if (m <= 2 * kListPart || parts <= 1) return ListParts{1, m};
+    const int each = (m + parts - 1) / parts;
+    return ListParts{(m + each - 1) / each, each};
+}
+
+// log p of a query's m entries from their scores, and lse. The sum is kept relative to the largest score without the 1
+// of that itself, so that log p keeps its relative accuracy where p is nearly 1. By THREADS threads, EACH entries a thread in registers.
+template <int THREADS, int EACH>
+__device__ __forceinline__ void list_softmax(const float *scores, const int32_t *ids, int64_t n, int m, float *red, float *logp, float *lse)
+{
+    float s[EACH], top = -INFINITY;
+    int32_t id[EACH];
+    bool real[EACH];
+    if (m > 0) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int j = min((int)threadIdx.x + i * THREADS, m - 1); // (an entry always, so that no load waits for a branch)
+            id[i] = ids[j];
+            s[i] = scores[j];
+        }
     }
-    top = list_max(top, red);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        real[i] = (int)threadIdx.x + i * THREADS < m && id[i] >= 0 && (int64_t)id[i] < n;
+        if (real[i]) top = fmaxf(top, s[i]);
+    }
+    top = THREADS == 64 ? wave_max(top) : list_max(top, red);
     const float base = top > -INFINITY ? top : 0.0f;
     float beside = 0.0f, at_top = 0.0f;
-    for (int j = threadIdx.x; j < m; j += kListThreads) {
-        const int32_t id = ids[j];
-        if (!(id >= 0 && (int64_t)id < n)) continue;
-        const float s = scores[j];
-        if (s == base) at_top += 1.0f;
-        else beside += expf(s - base); // (NaN goes on in the sum)
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (!real[i]) continue;
+        if (s[i] == base) at_top += 1.0f;
+        else beside += expf(s[i] - base); // (NaN goes on in the sum)
     }
-    beside = list_sum(beside, red);
-    at_top = list_sum(at_top, red);
+    beside = THREADS == 64 ? group_sum<64>(beside) : list_sum(beside, red);
+    at_top = THREADS == 64 ? group_sum<64>(at_top) : list_sum(at_top, red);
     // (nothing but masks: log p and lse are -infinity; a score of +infinity: no result is a number)
     float sum = top > -INFINITY ? log1pf((at_top - 1.0f) + beside) : beside;
     if (top == INFINITY) sum = NAN;
     const float low = top > -INFINITY ? 0.0f : -INFINITY;
-    for (int j = threadIdx.x; j < m; j += kListThreads) {
-        const int32_t id = ids[j];
-        logp[j] = id >= 0 && (int64_t)id < n ? (scores[j] - base) - sum + low : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int j = threadIdx.x + i * THREADS;
+        if (j < m) logp[j] = real[i] ? (s[i] - base) - sum + low : -INFINITY;
     }
     if (threadIdx.x == 0) *lse = base + sum + low;
 }
 
-// The query in LDS in fp32, zeros to a whole unit.
-template <class T> __device__ __forceinline__ void list_query(const T *__restrict__ q, int d, float *qs)
+// One wave does lists of up to 256: no barrier, and the other waves make room for the next query's.
+__device__ __forceinline__ void list_softmax_any(const float *scores, const int32_t *ids, int64_t n, int m, float *red, float *logp, float *lse)
 {
-    const int padded = units_of<T>(d) * kUnit<T>;
-    for (int k = threadIdx.x; k < padded; k += kListThreads) qs[k] = k < d ? to_f32(q[k]) : 0.0f;
+    if (m <= 256) {
+        if (threadIdx.x < 64) list_softmax<64, 4>(scores, ids, n, m, red, logp, lse);
+    } else if (m <= 1024) {
+        list_softmax<kListThreads, 4>(scores, ids, n, m, red, logp, lse);
+    } else {
+        list_softmax<kListThreads, 16>(scores, ids, n, m, red, logp, lse);
+    }
 }
 
-template <class T, bool RAGGED>
-__global__ __launch_bounds__(kListThreads) void list_probs_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int64_t ld_q, float scale,
-                                                                  const int32_t *__restrict__ ids, int m, const float *__restrict__ offset, float *__restrict__ logp,
-                                                                  float *__restrict__ lse)
+// ids of a part in LDS, -1 for padding
+__device__ __forceinline__ void list_ids(const int32_t *__restrict__ ids, int64_t n, int count, int32_t *to)
 {
-    extern __shared__ float lds[]; // the query, the scores
+    for (int j = threadIdx.x; j < count; j += kListThreads) {
+        const int32_t id = ids[j];
+        to[j] = id >= 0 && (int64_t)id < n ? id : -1;
+    }
+}
+
+// Scores of a part of a query's list, and where that is all of it the softmax. A row lies across L lanes that hold NV units of it each, and of
+// the query in fp32; four rows at a time a team of lanes.
+template <class T, bool RAGGED, int L, int NV>
+__global__ __launch_bounds__(kListThreads) void list_probs_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int64_t ld_q, float scale,
+                                                                  const int32_t *__restrict__ ids, int m, int parts, int each, const float *__restrict__ offset,
+                                                                  float *__restrict__ logp, float *__restrict__ lse)
+{
+    extern __shared__ int32_t lds[]; // the part's ids and scores
+    __shared__ float red[kListWaves];
+    constexpr int V = kUnit<T>, kTeams = kListThreads / L, kRows = 4;
+    const int per_row = units_of<T>(d), lane = threadIdx.x % L, team = threadIdx.x / L;
+    const int64_t t = blockIdx.x / (uint32_t)parts;
+    const int first = (int)(blockIdx.x - (uint32_t)t * parts) * each, count = min(each, m - first);
+    int32_t *listed = lds;
+    float *scores = (float *)(lds + each);
+    list_ids(ids + t * m + first, n, count, listed);
+    float qf[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int u = lane + i * L;
+        Unit<T> v{};
+        if (u < per_row) v = load_unit<T, true>(q + t * ld_q, u * V, d);
+#pragma unroll
+        for (int e = 0; e < V; ++e) qf[i][e] = to_f32(v.e[e]);
+    }
+    __syncthreads();
+    for (int j0 = 0; j0 < count; j0 += kTeams * kRows) {
+        Unit<T> v[kRows][NV];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int j = j0 + r * kTeams + team, id = j < count ? max(listed[j], 0) : 0; // (a row always, so that no load waits for a branch)
+            const T *row = x + (int64_t)id * ld_x;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int u = lane + i * L;
+                v[r][i] = load_unit<T, RAGGED>(row, (u < per_row ? u : 0) * V, d);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int j = j0 + r * kTeams + team;
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (NV * L > 1 && lane + i * L >= per_row) continue;
+#pragma unroll
+                for (int e = 0; e < V; ++e) s = __fmaf_rn(to_f32(v[r][i].e[e]), qf[i][e], s);
+            }
+            s = group_sum<L>(s);
+            if (lane == 0 && j < count) scores[j] = s;
+        }
+    }
+    __syncthreads();
+    const int64_t at = t * m + first;
+    for (int j = threadIdx.x; j < count; j += kListThreads) {
+        const float s = offset ? __fmaf_rn(scores[j], scale, offset[at + j]) : scores[j] * scale;
+        if (parts == 1) scores[j] = s;
+        else logp[at + j] = s;
+    }
+    if (parts > 1) return;
+    __syncthreads();
+    list_softmax_any(scores, listed, n, m, red, logp + at, lse + t);
+}
+
+// The same for rows that registers do not hold: a wave a row, the query in LDS.
+template <class T, bool RAGGED>
+__global__ __launch_bounds__(kListThreads) void list_probs_long_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int64_t ld_q, float scale,
+                                                                       const int32_t *__restrict__ ids, int m, int parts, int each, const float *__restrict__ offset,
+                                                                       float *__restrict__ logp, float *__restrict__ lse)
+{
+    extern __shared__ int32_t lds[]; // the part's ids and scores, the query in fp32, zeros to a whole unit
     __shared__ float red[kListWaves];
     constexpr int V = kUnit<T>;
     const int per_row = units_of<T>(d), lane = threadIdx.x & 63;
-    float *qs = lds, *scores = lds + per_row * V;
-    const int64_t t = blockIdx.x;
-    ids += t * m;
-    list_query(q + t * ld_q, d, qs);
+    const int64_t t = blockIdx.x / (uint32_t)parts;
+    const int first = (int)(blockIdx.x - (uint32_t)t * parts) * each, count = min(each, m - first);
+    int32_t *listed = lds;
+    float *scores = (float *)(lds + each), *qs = scores + each;
+    list_ids(ids + t * m + first, n, count, listed);
+    for (int k = threadIdx.x; k < per_row * V; k += kListThreads) qs[k] = k < d ? to_f32(q[t * ld_q + k]) : 0.0f;
     __syncthreads();
-    for (int j = threadIdx.x >> 6; j < m; j += kListWaves) {
-        const int32_t id = ids[j];
-        const T *row = x + (id >= 0 && (int64_t)id < n ? (int64_t)id * ld_x : 0);
+    const int64_t at = t * m + first;
+    for (int j = threadIdx.x >> 6; j < count; j += kListWaves) {
+        const T *row = x + (int64_t)max(listed[j], 0) * ld_x;
         float s = 0.0f;
+#pragma unroll 4
         for (int u = lane; u < per_row; u += 64) {
             const Unit<T> v = load_unit<T, RAGGED>(row, u * V, d);
 #pragma unroll
             for (int e = 0; e < V; ++e) s = __fmaf_rn(to_f32(v.e[e]), qs[u * V + e], s);
         }
         s = group_sum<64>(s);
-        if (lane == 0) scores[j] = offset ? __fmaf_rn(s, scale, offset[t * m + j]) : s * scale;
+        if (lane == 0) {
+            s = offset ? __fmaf_rn(s, scale, offset[at + j]) : s * scale;
+            if (parts == 1) scores[j] = s;
+            else logp[at + j] = s;
+        }
     }
+    if (parts > 1) return;
     __syncthreads();
-    list_softmax(scores, ids, n, m, red, logp + t * m, lse + t);
+    list_softmax_any(scores, listed, n, m, red, logp + at, lse + t);
 }
 
-// G and dq of a query.
-template <class T, bool RAGGED>
-__global__ __launch_bounds__(kListThreads) void list_grad_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, float scale, const int32_t *__restrict__ ids, int m,
-                                                                 const float *__restrict__ logp, const float *__restrict__ g, const float *__restrict__ g_lse, int lanes,
-                                                                 float *__restrict__ dscores, T *__restrict__ dq, int64_t ld_dq)
+// Lists that were scored in parts: a workgroup a query, in place.
+__global__ __launch_bounds__(kListThreads) void list_softmax_kernel(const int32_t *__restrict__ ids, int64_t n, int m, float *logp, float *lse)
 {
-    extern __shared__ float lds[]; // G, the teams' sums of a unit column
     __shared__ float red[kListWaves];
-    constexpr int V = kUnit<T>;
-    float *G = lds, *sums = lds + m;
     const int64_t t = blockIdx.x;
+    list_softmax_any(logp + t * m, ids + t * m, n, m, red, logp + t * m, lse + t);
+}
+
+// G of a part of a query's list, and what its rows add to dq: dq itself where the part is the list, else sums for list_join_kernel. A row's
+// units lie across `lanes` lanes; kAhead rows at a time a team of them.
+template <class T, bool RAGGED>
+__global__ __launch_bounds__(kListThreads) void list_grad_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, float scale, const int32_t *__restrict__ ids, int m, int parts,
+                                                                 int each, const float *__restrict__ logp, const float *__restrict__ g, const float *__restrict__ g_lse, int lanes,
+                                                                 float *__restrict__ dscores, T *__restrict__ dq, int64_t ld_dq, float *__restrict__ partial)
+{
+    extern __shared__ int32_t lds[]; // the part's ids and G, the teams' sums of a unit column
+    __shared__ float red[kListWaves];
+    constexpr int V = kUnit<T>, kAhead = 8;
+    const int64_t t = blockIdx.x / (uint32_t)parts;
+    const int part = (int)(blockIdx.x - (uint32_t)t * parts), first = part * each, count = min(each, m - first);
+    int32_t *listed = lds;
+    float *G = (float *)(lds + each), *sums = G + each;
     ids += t * m;
+    logp += t * m;
+    g += t * m;
     float a = 0.0f;
-    for (int j = threadIdx.x; j < m; j += kListThreads) {
-        const int32_t id = ids[j];
-        if (id >= 0 && (int64_t)id < n && !(logp[t * m + j] == -INFINITY)) a += g[t * m + j];
+    for (int j0 = threadIdx.x; j0 < m; j0 += 4 * kListThreads) {
+        int32_t id[4];
+        float lp[4], up[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = min(j0 + i * kListThreads, m - 1); // (an entry always, so that no load waits for a branch)
+            id[i] = ids[j];
+            lp[i] = logp[j];
+            up[i] = g[j];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (j0 + i * kListThreads < m && id[i] >= 0 && (int64_t)id[i] < n && !(lp[i] == -INFINITY)) a += up[i];
     }
     a = list_sum(a, red);
     if (g_lse) a -= g_lse[t];
-    for (int j = threadIdx.x; j < m; j += kListThreads) {
-        const int32_t id = ids[j];
-        const float lp = logp[t * m + j];
+    for (int j = threadIdx.x; j < count; j += kListThreads) {
+        const int32_t id = ids[first + j];
+        const float lp = logp[first + j], up = g[first + j];
         float v = 0.0f;
         if (id >= 0 && (int64_t)id < n && !(lp == -INFINITY)) {
-            const float up = g[t * m + j];
             // (an answer that is nearly certain: 1 - p by itself)
             v = lp > -0.5f ? __fmaf_rn(-a, expm1f(lp), up - a) : __fmaf_rn(-a, expf(lp), up);
         }
+        listed[j] = v == 0.0f ? 0 : id; // (a row of no weight is read as row 0 and left out, whatever it holds)
         G[j] = v;
-        dscores[t * m + j] = v;
+        dscores[t * m + first + j] = v;
     }
     if (!dq) return;
     __syncthreads();
@@ -148,57 +283,137 @@ __global__ __launch_bounds__(kListThreads) void list_grad_kernel(const T *__rest
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] = 0.0f;
         if (u < per_row)
-            for (int j = team; j < m; j += teams) {
-                const float w = G[j];
-                if (w == 0.0f) continue; // (padding, and rows of no weight whatever they hold)
-                const Unit<T> v = load_unit<T, RAGGED>(x + (int64_t)ids[j] * ld_x, u * V, d);
+            for (int j0 = team; j0 < count; j0 += teams * kAhead) {
+                Unit<T> v[kAhead];
+                float w[kAhead];
 #pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] = __fmaf_rn(w, to_f32(v.e[e]), acc[e]);
+                for (int r = 0; r < kAhead; ++r) {
+                    const int j = j0 + r * teams;
+                    w[r] = j < count ? G[j] : 0.0f;
+                    v[r] = load_unit<T, RAGGED>(x + (int64_t)(j < count ? listed[j] : 0) * ld_x, u * V, d);
+                }
+#pragma unroll
+                for (int r = 0; r < kAhead; ++r)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[e] = w[r] != 0.0f ? __fmaf_rn(w[r], to_f32(v[r].e[e]), acc[e]) : acc[e];
             }
+        if (teams > 1) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) sums[threadIdx.x * V + e] = acc[e];
-        __syncthreads();
+            for (int e = 0; e < V; ++e) sums[threadIdx.x * V + e] = acc[e];
+            __syncthreads();
+        }
         if (team == 0 && u < per_row) {
             for (int o = 1; o < teams; ++o)
 #pragma unroll
                 for (int e = 0; e < V; ++e) acc[e] += sums[(o * lanes + lane) * V + e];
-            Unit<T> out;
+            if (parts == 1) {
+                Unit<T> out;
 #pragma unroll
-            for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(acc[e] * scale);
-            store_unit<T, RAGGED>(dq + t * ld_dq, u * V, d, out);
+                for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(acc[e] * scale);
+                store_unit<T, RAGGED>(dq + t * ld_dq, u * V, d, out);
+            } else {
+                Pack<float, V> out;
+#pragma unroll
+                for (int e = 0; e < V; ++e) out.e[e] = acc[e];
+                *(Pack<float, V> *)(partial + ((t * parts + part) * per_row + u) * V) = out;
+            }
         }
-        __syncthreads();
+        if (teams > 1) __syncthreads();
     }
 }
 
+// dq from its parts' sums, in order: a wave 64 units of a query.
 template <class T, bool RAGGED>
-static int list_run(const ListParams &p, hipStream_t st)
+__global__ __launch_bounds__(64) void list_join_kernel(const float *__restrict__ partial, int parts, int d, float scale, T *__restrict__ dq, int64_t ld_dq)
 {
-    static LdsLimitOnce limit;
-    AVQ_TRY(set_lds_limit((const void *)list_probs_kernel<T, RAGGED>, kMaxDynLds, &limit));
-    const size_t lds = ((size_t)units_of<T>(p.d) * kUnit<T> + p.m) * sizeof(float);
-    list_probs_kernel<T, RAGGED><<<dim3(p.nq), dim3(kListThreads), lds, st>>>((const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.ld_queries, p.scale, p.ids, p.m,
-                                                                           p.offset, p.logp, p.lse);
+    constexpr int V = kUnit<T>;
+    const int per_row = units_of<T>(d), u = blockIdx.y * 64 + threadIdx.x;
+    const int64_t t = blockIdx.x;
+    if (u >= per_row) return;
+    float acc[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) {
+        const Pack<float, V> v = *(const Pack<float, V> *)(partial + ((t * parts + p) * per_row + u) * V);
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += v.e[e];
+    }
+    Unit<T> out;
+#pragma unroll
+    for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(acc[e] * scale);
+    store_unit<T, RAGGED>(dq + t * ld_dq, u * V, d, out);
+}
+
+template <class T, bool RAGGED, int L, int NV>
+static int list_run(const ListParams &p, const ListParts &by, hipStream_t st)
+{
+    list_probs_kernel<T, RAGGED, L, NV><<<dim3((unsigned)p.nq * by.parts), dim3(kListThreads), (size_t)by.each * 8, st>>>(
+        (const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.ld_queries, p.scale, p.ids, p.m, by.parts, by.each, p.offset, p.logp, p.lse);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
 
 template <class T, bool RAGGED>
-static int list_grad_run(const ListGradParams &p, hipStream_t st)
+static int list_run_long(const ListParams &p, const ListParts &by, hipStream_t st)
 {
-    int lanes = 4;
-    while (lanes < kListThreads && lanes < units_of<T>(p.d)) lanes *= 2;
-    const size_t lds = ((size_t)p.m + kListThreads * kUnit<T>) * sizeof(float);
-    list_grad_kernel<T, RAGGED><<<dim3(p.nq), dim3(kListThreads), lds, st>>>((const T *)p.points, p.n, p.d, p.ld_points, p.scale, p.ids, p.m, p.logp, p.grad_logp, p.grad_lse, lanes,
-                                                                          p.dscores, (T *)p.dqueries, p.ld_dqueries);
+    static LdsLimitOnce limit;
+    AVQ_TRY(set_lds_limit((const void *)list_probs_long_kernel<T, RAGGED>, kMaxDynLds, &limit));
+    list_probs_long_kernel<T, RAGGED><<<dim3((unsigned)p.nq * by.parts), dim3(kListThreads), (size_t)by.each * 8 + (size_t)units_of<T>(p.d) * kUnit<T> * 4, st>>>(
+        (const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.ld_queries, p.scale, p.ids, p.m, by.parts, by.each, p.offset, p.logp, p.lse);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
+}
+
+template <class T, bool RAGGED>
+static int list_scores(const ListParams &p, const ListParts &by, hipStream_t st)
+{
+    const int per_row = units_of<T>(p.d);
+    if (per_row <= 8) return list_run<T, RAGGED, 8, 1>(p, by, st);
+    if (per_row <= 16) return list_run<T, RAGGED, 16, 1>(p, by, st);
+    if (per_row <= 32) return list_run<T, RAGGED, 32, 1>(p, by, st);
+    if (per_row <= 64) return list_run<T, RAGGED, 64, 1>(p, by, st);
+    if (per_row <= 128) return list_run<T, RAGGED, 64, 2>(p, by, st);
+    if (per_row <= 256) return list_run<T, RAGGED, 64, 4>(p, by, st);
+    return list_run_long<T, RAGGED>(p, by, st);
 }
 
 template <class T>
 static int list_typed(const ListParams &p, hipStream_t st)
 {
-    return whole_units(p.points, p.ld_points, p.d, sizeof(T)) ? list_run<T, false>(p, st) : list_run<T, true>(p, st);
+    const ListParts by = list_parts(p.nq, p.m);
+    AVQ_TRY((whole_units(p.points, p.ld_points, p.d, sizeof(T)) ? list_scores<T, false>(p, by, st) : list_scores<T, true>(p, by, st)));
+    if (by.parts > 1) {
+        list_softmax_kernel<<<dim3(p.nq), dim3(kListThreads), 0, st>>>(p.ids, p.n, p.m, p.logp, p.lse);
+        AVQ_HIP(hipGetLastError());
+    }
+    return AVQ_OK;
+}
+
+// the parts' sums of dq (fp32, rows of whole units), then the scratch of the sorted sums
+static size_t list_partial_bytes(int d, int nq, int m)
+{
+    const ListParts by = list_parts(nq, m);
+    return by.parts == 1 ? 0 : ((size_t)nq * by.parts * ((d + 7) / 8 * 8) * sizeof(float) + 255) & ~(size_t)255;
+}
+
+template <class T, bool RAGGED>
+static int list_grad_run(const ListGradParams &p, hipStream_t st)
+{
+    const ListParts by = list_parts(p.nq, p.m);
+    const int per_row = units_of<T>(p.d);
+    int lanes = 4;
+    while (lanes < kListThreads && lanes < per_row) lanes *= 2;
+    const size_t lds = (size_t)by.each * 8 + (size_t)kListThreads * kUnit<T> * sizeof(float);
+    list_grad_kernel<T, RAGGED><<<dim3((unsigned)p.nq * by.parts), dim3(kListThreads), lds, st>>>((const T *)p.points, p.n, p.d, p.ld_points, p.scale, p.ids, p.m, by.parts, by.each, p.logp,
+                                                                                               p.grad_logp, p.grad_lse, lanes, p.dscores, (T *)p.dqueries, p.ld_dqueries,
+                                                                                               (float *)p.scratch);
+    AVQ_HIP(hipGetLastError());
+    if (p.dqueries && by.parts > 1) {
+        list_join_kernel<T, RAGGED><<<dim3(p.nq, (per_row + 63) / 64), dim3(64), 0, st>>>((const float *)p.scratch, by.parts, p.d, p.scale, (T *)p.dqueries, p.ld_dqueries);
+        AVQ_HIP(hipGetLastError());
+    }
+    return AVQ_OK;
 }
 
 template <class T>
@@ -218,7 +433,7 @@ int launch_list_probs(const ListParams &p, hipStream_t st)
 size_t list_grad_scratch_bytes(int64_t n, int d, int nq, int m)
 {
     const int64_t count = (int64_t)nq * m;
-    return count == 0 ? 0 : embed_grad_scratch_bytes(n, d, count);
+    return count == 0 ? 0 : list_partial_bytes(d, nq, m) + embed_grad_scratch_bytes(n, d, count);
 }
 
 int launch_list_grad(const ListGradParams &p, hipStream_t st)
@@ -229,7 +444,8 @@ int launch_list_grad(const ListGradParams &p, hipStream_t st)
         else AVQ_TRY(list_grad_typed<f16_t>(p, st));
     }
     if (!p.dpoints) return AVQ_OK;
-    EmbedGradParams rows{p.queries, p.type, p.ld_queries, p.ids, (int64_t)p.nq * p.m, p.scale, p.dpoints, p.n, p.d, p.ld_dpoints, p.accumulate, p.scratch};
+    EmbedGradParams rows{p.queries, p.type, p.ld_queries, p.ids, (int64_t)p.nq * p.m, p.scale, p.dpoints, p.n, p.d, p.ld_dpoints, p.accumulate,
+                         (char *)p.scratch + (p.nq > 0 ? list_partial_bytes(p.d, p.nq, p.m) : 0)};
     rows.weights = p.dscores;
     rows.per_row = p.m;
     return launch_embed_grad(rows, st);

@@ -16,178 +16,263 @@
 
 namespace avq {
 
-constexpr int kLossThreads = 256, kLossWaves = kLossThreads / 64;
+constexpr int kLossThreads = 256;
 constexpr double kLeastRest = 0x1p-20; // a student's mass beside the list, at least: its log probabilities are not known better
+constexpr double kLog2 = 0.69314718055994530942, kPerLog2 = 1.4426950408889634074;
 
-// e^x to 1e-13 or better: x = n log 2 + f, Taylor's polynomial of degree 11 (|f| <= 0.347: the rest is below 7e-15; log 2 is off by 2^-54
-// of itself, n times)
+// a constant in scalar registers, where a multiply-add takes it from: else it is moved to vector registers first, for each use
+__device__ __forceinline__ double held(double c)
+{
+    asm("" : "+s"(c));
+    return c;
+}
+
+// x = n log 2 + f with |f| <= log(2) / 2, for x held to +-800 (where e^x is infinity and 0; a NaN is lost)
+struct Reduced { double n, f; };
+__device__ __forceinline__ Reduced reduced(double x)
+{
+    x = fmin(fmax(x, -800.0), 800.0);
+    const double n = rint(x * held(kPerLog2));
+    return Reduced{n, fma(n, held(-kLog2), x)};
+}
+
+// e^x to 1e-13 or better (no NaN): the Chebyshev series of e^f on |f| <= log(2) / 2 up to degree 9, 1.9e-14 of it; log 2 is off by 2^-54
+// of itself, n times
 __device__ __forceinline__ double exp_wide(double x)
 {
-    x = x > 800.0 ? 800.0 : x < -800.0 ? -800.0 : x; // (infinity and 0 there; NaN stays)
-    const double n = rint(x * 1.4426950408889634074);
-    const double f = fma(n, -0.69314718055994530942, x);
-    double p = 1.0 / 39916800.0;
-    p = fma(p, f, 1.0 / 3628800.0);
-    p = fma(p, f, 1.0 / 362880.0);
-    p = fma(p, f, 1.0 / 40320.0);
-    p = fma(p, f, 1.0 / 5040.0);
-    p = fma(p, f, 1.0 / 720.0);
-    p = fma(p, f, 1.0 / 120.0);
-    p = fma(p, f, 1.0 / 24.0);
-    p = fma(p, f, 1.0 / 6.0);
-    p = fma(p, f, 0.5);
-    p = fma(p, f, 1.0);
-    p = fma(p, f, 1.0);
-    return ldexp(p, (int)n);
+    const Reduced r = reduced(x);
+    double p = fma(held(2.762994375246158e-06), r.f, held(2.4884447491303006e-05));
+    p = fma(p, r.f, held(0.00019841197960142717));
+    p = fma(p, r.f, held(0.0013888801773822223));
+    p = fma(p, r.f, held(0.008333333360426695));
+    p = fma(p, r.f, held(0.04166666704037994));
+    p = fma(p, r.f, held(0.16666666666642443));
+    p = fma(p, r.f, held(0.4999999999943919));
+    p = fma(p, r.f, held(0.9999999999999977));
+    p = fma(p, r.f, held(1.0000000000000135));
+    return ldexp(p, (int)r.n);
 }
 
-// over L lanes side by side (L = 256: the workgroup, by a value a wave in red)
-template <int L> __device__ __forceinline__ double lanes_sum(double v, double *red)
+// e^x - 1 and e^x - 1 - x (no NaN), with their own relative accuracy near 0: Taylor's polynomial of (e^f - 1 - f) / f^2
+struct NearOne { double e1, e2; };
+__device__ __forceinline__ NearOne exp_near_one(double x)
 {
-    constexpr int W = L < 64 ? L : 64;
+    const Reduced r = reduced(x);
+    double q = fma(held(1.0 / 39916800.0), r.f, held(1.0 / 3628800.0));
+    q = fma(q, r.f, held(1.0 / 362880.0));
+    q = fma(q, r.f, held(1.0 / 40320.0));
+    q = fma(q, r.f, held(1.0 / 5040.0));
+    q = fma(q, r.f, held(1.0 / 720.0));
+    q = fma(q, r.f, held(1.0 / 120.0));
+    q = fma(q, r.f, held(1.0 / 24.0));
+    q = fma(q, r.f, held(1.0 / 6.0));
+    q = fma(q, r.f, 0.5);
+    const double square = r.f * r.f, e = ldexp(1.0 + fma(square, q, r.f), (int)r.n);
+    const bool near = r.n == 0.0;
+    return NearOne{near ? fma(square, q, r.f) : e - 1.0, near ? square * q : (e - 1.0) - fmin(x, 800.0)};
+}
+
+// v + its value `CTRL` lanes away, through the adders' operand paths
+template <int CTRL> __device__ __forceinline__ double moved_by(double v)
+{
+    const uint2 w = __builtin_bit_cast(uint2, v);
+    return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_mov_dpp(w.x, CTRL, 0xF, 0xF, true), __builtin_amdgcn_mov_dpp(w.y, CTRL, 0xF, 0xF, true)));
+}
+
+// over L lanes side by side, at most a wave
+template <int L> __device__ __forceinline__ double group_sum_wide(double v)
+{
+    if (L > 1) v += moved_by<0xB1>(v);  // the lane beside
+    if (L > 2) v += moved_by<0x4E>(v);  // the other pair
+    if (L > 4) v += moved_by<0x141>(v); // the other four of eight
+    if (L > 8) v += moved_by<0x140>(v); // the other eight of sixteen
+    if (L > 16) v += __shfl_xor(v, 16, 64);
+    if (L > 32) v += __shfl_xor(v, 32, 64);
+    return v;
+}
+
+__device__ __forceinline__ double of_lane(double v, int lane)
+{
+    const uint2 w = __builtin_bit_cast(uint2, v);
+    return __builtin_bit_cast(double, make_uint2(__builtin_amdgcn_readlane(w.x, lane), __builtin_amdgcn_readlane(w.y, lane)));
+}
+
+// N sums over L lanes side by side: part of a wave, or (L > 64) the whole workgroup by red[wave][N]
+template <int L, int N> __device__ __forceinline__ void lanes_sum(double (&v)[N], double *red)
+{
+    constexpr int W = L < 64 ? L : 64, kWaves = L <= 64 ? 1 : L / 64;
 #pragma unroll
-    for (int w = 1; w < W; w <<= 1) v += __shfl_xor(v, w, 64);
-    if (L <= 64) return v;
+    for (int i = 0; i < N; ++i) v[i] = group_sum_wide<W>(v[i]);
+    if (L <= 64) return;
+    static_assert(kWaves * N <= 64, "a lane a value");
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) red[(threadIdx.x >> 6) * N + i] = v[i];
     __syncthreads();
-    return (red[0] + red[1]) + (red[2] + red[3]);
+    // every wave joins them: lane i kWaves + w has sum i of wave w
+    const int lane = threadIdx.x & 63;
+    const double mine = group_sum_wide<kWaves>(lane < kWaves * N ? red[lane % kWaves * N + lane / kWaves] : 0.0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = of_lane(mine, i * kWaves);
 }
 
-template <int L> __device__ __forceinline__ float lanes_max(float v, double *red)
+// the bits that any of L lanes side by side has, at most a wave
+template <int L> __device__ __forceinline__ uint32_t lanes_or(uint32_t v)
 {
-    constexpr int W = L < 64 ? L : 64;
+    if (L > 1) v |= __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true);
+    if (L > 2) v |= __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true);
+    if (L > 4) v |= __builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, true);
+    if (L > 8) v |= __builtin_amdgcn_mov_dpp(v, 0x140, 0xF, 0xF, true);
+    if (L > 16) v |= (uint32_t)__shfl_xor((int)v, 16, 64);
+    if (L > 32) v |= (uint32_t)__shfl_xor((int)v, 32, 64);
+    return v;
+}
+
+template <int L> __device__ __forceinline__ float lanes_max(float v, float *red)
+{
+    constexpr int W = L < 64 ? L : 64, kWaves = L / 64;
 #pragma unroll
     for (int w = 1; w < W; w <<= 1) v = fmaxf(v, __shfl_xor(v, w, 64));
     if (L <= 64) return v;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
-    return (float)fmax(fmax(red[0], red[1]), fmax(red[2], red[3]));
+    v = red[0];
+    for (int w = 1; w < kWaves; ++w) v = fmaxf(v, red[w]);
+    return v;
 }
 
 // ---- distillation ----------------------------------------------------------------------------
 
-// Elements k .. k + 3 of a row of m, `none` past its end.
-template <class T> __device__ __forceinline__ void load4(const T *__restrict__ row, int k, int m, T none, T (&v)[4])
+// A row by L lanes, E elements a lane, L apart. ALL: the teacher's lse is that of all of its rows. GRAD: with the gradient.
+template <int L> constexpr int kDistillThreads = L > 64 ? L : kLossThreads; // a row has a part of a wave, or a workgroup
+template <class T, bool ALL, bool GRAD, int L, int E>
+__global__ __launch_bounds__(kDistillThreads<L>) void distill_kernel(const float *__restrict__ logp, const T *__restrict__ teacher, int64_t ld_teacher,
+                                                                     const float *__restrict__ teacher_lse, double per_tau, int64_t rows, int m, float *__restrict__ loss,
+                                                                     const float *__restrict__ g, float *__restrict__ out)
 {
-    if (k + 4 <= m) {
-        __builtin_memcpy(v, row + k, sizeof(v));
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = k + e < m ? row[k + e] : none;
-    }
-}
-
-template <class T> __device__ __forceinline__ T no_logit();
-template <> __device__ __forceinline__ float no_logit<float>() { return -INFINITY; }
-template <> __device__ __forceinline__ bf16_t no_logit<bf16_t>() { return bf16_t{0xff80}; }
-template <> __device__ __forceinline__ f16_t no_logit<f16_t>() { return f16_t{0xfc00}; }
-
-// A row by L lanes, NV times four elements a lane. ALL: the teacher's lse is that of all of its rows.
-template <class T, bool ALL, int L, int NV>
-__global__ __launch_bounds__(kLossThreads) void distill_kernel(const float *__restrict__ logp, const T *__restrict__ teacher, int64_t ld_teacher, const float *__restrict__ teacher_lse,
-                                                               double per_tau, int64_t rows, int m, float *__restrict__ loss, const float *__restrict__ g, float *__restrict__ out)
-{
-    __shared__ double red[kLossWaves];
-    constexpr int kRows = kLossThreads / L;
+    constexpr int B = kDistillThreads<L>, kRows = B / L;
+    __shared__ double red[B / 64 * 3];
+    __shared__ float red_max[B / 64];
+    __shared__ uint32_t red_odd[B / 64];
     const int lane = threadIdx.x % L;
     for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / L; row - threadIdx.x / L < rows; row += (int64_t)gridDim.x * kRows) {
         const bool real = row < rows;
-        float z[NV][4], lp[NV][4];
-        float top = -INFINITY, some = 0.0f;
+        float z[E], lp[E], top = -INFINITY;
+        {
+            const T *zr = teacher + (real ? row : 0) * ld_teacher;
+            const float *lr = logp + (real ? row : 0) * m;
+            T zt[E];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int k = (lane + i * L) * 4;
-            T zt[4];
-            load4<T>(teacher + (real ? row * ld_teacher : 0), k, real ? m : 0, no_logit<T>(), zt);
-            load4<float>(logp + (real ? row * m : 0), k, real ? m : 0, -INFINITY, lp[i]);
+            for (int e = 0; e < E; ++e) {
+                const int k = min(lane + e * L, m - 1); // (an element always, so that no load waits for a branch; m > 0)
+                zt[e] = zr[k];
+                lp[e] = lr[k];
+            }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                z[i][e] = to_f32(zt[e]);
-                top = fmaxf(top, z[i][e]);
-                if (!(z[i][e] == -INFINITY)) some = 1.0f; // (NaN is no padding)
+            for (int e = 0; e < E; ++e) z[e] = lane + e * L < m ? to_f32(zt[e]) : -INFINITY;
+        }
+        // what has no place in the exponentials: an entry that is no padding, a NaN of the teacher, of the student, an entry that the
+        // student gives nothing and the teacher something
+        bool some = false, odd_teacher = false, odd_student = false, none = false;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const bool there = !(z[e] == -INFINITY);
+            some |= there;
+            odd_teacher |= z[e] != z[e];
+            lp[e] = there ? lp[e] : -INFINITY;
+            odd_student |= lp[e] != lp[e];
+            if (!ALL) top = fmaxf(top, z[e]);
+        }
+        if (!ALL) top = lanes_max<L>(top, red_max);
+        const double base = ALL ? (real ? (double)teacher_lse[row] : 0.0) : top > -INFINITY ? (double)top * per_tau : 0.0;
+        double P[E], p[E], sums[3] = {0.0, 0.0, 0.0}; // of P, of P times (log P up to its constant - log p), of p
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const double a = fma((double)z[e], per_tau, -base);
+            P[e] = exp_wide(a);
+            sums[0] += P[e];
+            const bool counts = P[e] > 0.0, finite = lp[e] > -INFINITY;
+            none |= counts & !finite;
+            sums[1] = fma(P[e], (counts & finite) ? a - (double)lp[e] : 0.0, sums[1]);
+            if (ALL) {
+                p[e] = exp_wide((double)lp[e]);
+                sums[2] += p[e];
             }
         }
-        top = lanes_max<L>(top, red);
-        some = lanes_max<L>(some, red);
-        const double base = ALL ? (real ? (double)teacher_lse[row] : 0.0) : top > -INFINITY ? (double)top * per_tau : 0.0;
-        double P[NV][4], sum = 0.0;
+        uint32_t odd = (some ? 1u : 0u) | (odd_teacher ? 2u : 0u) | (odd_student ? 4u : 0u) | (none ? 8u : 0u);
+        if (base != base || base == INFINITY) odd |= 2u; // (no teacher's distribution)
+        odd = lanes_or<(L < 64 ? L : 64)>(odd);
+        if (L > 64) {
+            __syncthreads(); // (the row before has been read)
+            if ((threadIdx.x & 63) == 0) red_odd[threadIdx.x >> 6] = odd; // (read behind the barriers of the sums)
+        }
+        lanes_sum<L>(sums, red);
+        if (L > 64)
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                P[i][e] = z[i][e] == -INFINITY ? 0.0 : exp_wide(fma((double)z[i][e], per_tau, -base));
-                sum += P[i][e];
-            }
-        sum = lanes_sum<L>(sum, red);
-        const double log_sum = ALL ? 0.0 : log(sum), per_sum = ALL ? 1.0 : 1.0 / sum;
-        double total = 0.0, mine = 0.0;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (P[i][e] == 0.0) { if (!ALL || z[i][e] == -INFINITY) continue; }
-                else total = fma(P[i][e], fma((double)z[i][e], per_tau, -base) - log_sum - (double)lp[i][e], total);
-                if (ALL) mine += exp_wide((double)lp[i][e]);
-            }
-        total = lanes_sum<L>(total, red) * per_sum;
-        double pull = 0.0;
+            for (int w = 0; w < B / 64; ++w) odd |= red_odd[w];
+        if (odd & 2u) sums[0] = NAN;
+        if (odd & 4u) sums[1] = sums[2] = NAN;
+        const double per_sum = ALL ? 1.0 : 1.0 / sums[0];
+        double total = ALL ? sums[1] : fma(sums[1], per_sum, -log(sums[0])), pull = 0.0;
         if (ALL) {
-            mine = lanes_sum<L>(mine, red);
-            const double rest = 1.0 - sum, left = 1.0 - mine;
+            const double rest = 1.0 - sums[0], left = 1.0 - sums[2];
             if (!(rest <= 0.0)) { // (NaN goes on)
                 total += rest * log(rest / (left > kLeastRest ? left : kLeastRest));
                 if (left > kLeastRest) pull = rest / left;
             }
-            if (!(left == left)) total = pull = left;
+            if (left != left) total = pull = left;
         }
+        if ((odd & 8u) && total == total) total = INFINITY;
         if (!real) continue;
-        if (loss && lane == 0) loss[row] = some > 0.0f ? (float)total : 0.0f;
-        if (!out) continue;
-        const double up = (double)g[row];
+        if (loss && lane == 0) loss[row] = (odd & 1u) != 0u ? (float)total : 0.0f;
+        if (!GRAD) continue;
+        const double up = (double)g[row], up_teacher = -up * per_sum;
+        pull *= up;
+        float *to = out + row * m;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int k = (lane + i * L) * 4;
-            float o[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                double v = -P[i][e] * per_sum;
-                if (ALL) v = fma(pull, exp_wide((double)lp[i][e]), v);
-                o[e] = z[i][e] == -INFINITY ? 0.0f : (float)(v * up);
-            }
-            if (k + 4 <= m) {
-                __builtin_memcpy(out + row * m + k, o, sizeof(o));
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (k + e < m) out[row * m + k + e] = o[e];
-            }
+        for (int e = 0; e < E; ++e) {
+            double v = P[e] * up_teacher;
+            if (ALL) v = fma(pull, p[e], v);
+            float o = (odd & 2u) != 0u ? NAN : (float)v;
+            o = z[e] == -INFINITY ? 0.0f : o;
+            if (lane + e * L < m) to[lane + e * L] = o;
         }
     }
 }
 
-template <class T, bool ALL, int L, int NV>
+template <class T, bool ALL, int L, int E>
 static int distill_run(const DistillParams &p, hipStream_t st)
 {
-    const int64_t groups = (p.rows + kLossThreads / L - 1) / (kLossThreads / L);
-    distill_kernel<T, ALL, L, NV><<<dim3((unsigned)std::min<int64_t>(groups, 1 << 22)), dim3(kLossThreads), 0, st>>>(
-        p.logp, (const T *)p.teacher, p.ld_teacher, p.teacher_lse, 1.0 / p.temperature, p.rows, p.m, p.loss, p.grad_loss, p.grad_logp);
+    constexpr int B = kDistillThreads<L>, kRows = B / L;
+    const int64_t groups = (p.rows + kRows - 1) / kRows;
+    const auto kernel = p.grad_logp ? distill_kernel<T, ALL, true, L, E> : distill_kernel<T, ALL, false, L, E>;
+    kernel<<<dim3((unsigned)std::min<int64_t>(groups, 1 << 20)), dim3(B), 0, st>>>(p.logp, (const T *)p.teacher, p.ld_teacher, p.teacher_lse, 1.0 / p.temperature, p.rows, p.m, p.loss,
+                                                                                p.grad_loss, p.grad_logp);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
 
+// Elements a lane: what a row takes beside its exponentials (sums over lanes, logarithm, quotients) is some 400 instructions, shared by a lane's
+// elements.
 template <class T, bool ALL>
 static int distill_sized(const DistillParams &p, hipStream_t st)
 {
-    if (p.m <= 16) return distill_run<T, ALL, 4, 1>(p, st);
-    if (p.m <= 32) return distill_run<T, ALL, 8, 1>(p, st);
-    if (p.m <= 64) return distill_run<T, ALL, 16, 1>(p, st);
-    if (p.m <= 128) return distill_run<T, ALL, 32, 1>(p, st);
-    if (p.m <= 256) return distill_run<T, ALL, 64, 1>(p, st);
-    if (p.m <= 512) return distill_run<T, ALL, 64, 2>(p, st);
-    if (p.m <= 1024) return distill_run<T, ALL, 64, 4>(p, st);
-    return distill_run<T, ALL, 256, 4>(p, st);
+    if (p.m <= 16) return distill_run<T, ALL, 4, 4>(p, st);
+    if (p.m <= 32) return distill_run<T, ALL, 4, 8>(p, st);
+    if (p.m <= 64) return distill_run<T, ALL, 8, 8>(p, st);
+    if (p.m <= 128) return distill_run<T, ALL, 16, 8>(p, st);
+    if (p.m <= 256) return distill_run<T, ALL, 32, 8>(p, st);
+    if (p.m <= 512) return distill_run<T, ALL, 64, 8>(p, st);
+    if (p.m <= 1024) return distill_run<T, ALL, 64, 16>(p, st);
+    return distill_run<T, ALL, 256, 16>(p, st);
+}
+
+// lists of no entries: loss 0
+__global__ __launch_bounds__(kLossThreads) void no_loss_kernel(float *__restrict__ loss, int64_t rows)
+{
+    for (int64_t i = blockIdx.x * (int64_t)kLossThreads + threadIdx.x; i < rows; i += gridDim.x * (int64_t)kLossThreads) loss[i] = 0.0f;
 }
 
 template <class T> static int distill_typed(const DistillParams &p, hipStream_t st) { return p.teacher_lse ? distill_sized<T, true>(p, st) : distill_sized<T, false>(p, st); }
@@ -195,61 +280,88 @@ template <class T> static int distill_typed(const DistillParams &p, hipStream_t 
 int launch_distill(const DistillParams &p, hipStream_t st)
 {
     if (p.rows == 0) return AVQ_OK;
+    if (p.m == 0) {
+        if (p.loss) {
+            no_loss_kernel<<<dim3((unsigned)std::min<int64_t>((p.rows + kLossThreads - 1) / kLossThreads, 4096)), dim3(kLossThreads), 0, st>>>(p.loss, p.rows);
+            AVQ_HIP(hipGetLastError());
+        }
+        return AVQ_OK;
+    }
     if (p.type == AVQ_F32) return distill_typed<float>(p, st);
     return p.type == AVQ_BF16 ? distill_typed<bf16_t>(p, st) : distill_typed<f16_t>(p, st);
 }
 
 // ---- sequences of tokens ------------------------------------------------------------------------
 
-// Sequence s: the tokens [lo, hi). Offsets that are no offsets name no token outside of the call's.
-struct Span { int64_t lo, hi; };
-__device__ __forceinline__ Span span_of(const int32_t *__restrict__ offsets, int64_t s, int64_t tokens)
+// Sequence s: the tokens [lo, hi) of at most 2^28. Offsets that are no offsets name no token outside of the call's.
+struct Span { int lo, hi; };
+__device__ __forceinline__ Span span_of(const int32_t *__restrict__ offsets, int64_t s, int tokens)
 {
-    const int64_t lo = min(max((int64_t)offsets[s], (int64_t)0), tokens);
-    return Span{lo, min(max((int64_t)offsets[s + 1], lo), tokens)};
+    const int lo = min(max(offsets[s], 0), tokens);
+    return Span{lo, min(max(offsets[s + 1], lo), tokens)};
 }
 
-// Zeros for the tokens before the first sequence and behind the last, by the first and the last workgroup.
-__device__ __forceinline__ void clear_outside(float *__restrict__ out, const int32_t *__restrict__ offsets, int64_t sequences, int64_t tokens)
+// Zeros for the tokens before the first sequence and behind the last, by all workgroups.
+template <int B> __device__ __forceinline__ void clear_outside(float *__restrict__ out, const int32_t *__restrict__ offsets, int64_t sequences, int tokens)
 {
-    if (blockIdx.x == 0) {
-        const int64_t to = sequences > 0 ? span_of(offsets, 0, tokens).lo : 0;
-        for (int64_t i = threadIdx.x; i < to; i += kLossThreads) out[i] = 0.0f;
-    }
-    if (blockIdx.x == gridDim.x - 1) {
-        const int64_t from = sequences > 0 ? span_of(offsets, sequences - 1, tokens).hi : 0;
-        for (int64_t i = from + threadIdx.x; i < tokens; i += kLossThreads) out[i] = 0.0f;
-    }
+    const int to = sequences > 0 ? span_of(offsets, 0, tokens).lo : 0, from = sequences > 0 ? span_of(offsets, sequences - 1, tokens).hi : 0;
+    const int64_t first = blockIdx.x * (int64_t)B + threadIdx.x, step = gridDim.x * (int64_t)B;
+    for (int64_t i = first; i < to; i += step) out[i] = 0.0f;
+    for (int64_t i = from + first; i < tokens; i += step) out[i] = 0.0f;
 }
+// Workgroups beyond the sequences' own, for many tokens behind the last one.
+inline unsigned sequence_groups(int64_t tokens, int64_t sequences) { return (unsigned)(std::max<int64_t>(sequences, 1) + std::min<int64_t>(tokens >> 13, 512)); }
 
-// A workgroup a pair.
-__global__ __launch_bounds__(kLossThreads) void preference_kernel(const float *__restrict__ logp, const float *__restrict__ ref, const uint8_t *__restrict__ mask, int64_t tokens,
-                                                                  const int32_t *__restrict__ offsets, int pairs, double beta, double margin, double smoothing, int average,
-                                                                  float *__restrict__ loss, float *__restrict__ logit, float *__restrict__ reward, const float *__restrict__ g,
-                                                                  float *__restrict__ out)
+// A sequence (or pair) has a workgroup of B threads, that take kRound tokens each at a time: a wave for up to 64 tokens in the mean,
+// 256 threads up to 256 (pairs 1,024), else 1,024, so that most take one round, whose loads are all in flight.
+constexpr int kRound = 4;
+inline int sequence_threads(int64_t tokens, int64_t sequences) { return tokens <= 64 * sequences ? 64 : tokens <= 256 * sequences ? 256 : 1024; }
+
+template <int B>
+__global__ __launch_bounds__(B) void preference_kernel(const float *__restrict__ logp, const float *__restrict__ ref, const uint8_t *__restrict__ mask, int tokens,
+                                                       const int32_t *__restrict__ offsets, int pairs, double beta, double margin, double smoothing, int average,
+                                                       float *__restrict__ loss, float *__restrict__ logit, float *__restrict__ reward, const float *__restrict__ g,
+                                                       float *__restrict__ out)
 {
-    __shared__ double red[kLossWaves];
-    if (out) clear_outside(out, offsets, 2 * (int64_t)pairs, tokens);
+    __shared__ double red[B / 64 * 4];
+    if (out) clear_outside<B>(out, offsets, 2 * (int64_t)pairs, tokens);
     const int64_t pair = blockIdx.x;
     if (pair >= pairs) return;
-    double d[2], share[2];
-    Span span[2];
+    const Span span[2] = {span_of(offsets, 2 * pair, tokens), span_of(offsets, 2 * pair + 1, tokens)};
+    const double up = out ? (double)g[pair] : 0.0;
+    double sums[4] = {0.0, 0.0, 0.0, 0.0}; // of either side, its tokens that count
+    const int middle = span[0].hi, hi = span[1].hi; // (the pair's tokens lie side by side)
+    // (what is not given is read from logp all the same, and left out: no load waits for a branch)
+    const float *from_ref = ref ? ref : logp;
+    const uint8_t *from_mask = mask ? mask : (const uint8_t *)logp;
+    for (int i0 = span[0].lo + (int)threadIdx.x; i0 < hi; i0 += kRound * B) {
+        float v[kRound], r[kRound];
+        uint8_t set[kRound];
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const Span sp = span[side] = span_of(offsets, 2 * pair + side, tokens);
-        double sum = 0.0, many = 0.0;
-        for (int64_t i = sp.lo + threadIdx.x; i < sp.hi; i += kLossThreads) {
-            if (mask && !mask[i]) continue;
-            sum += (double)logp[i] - (ref ? (double)ref[i] : 0.0);
-            many += 1.0;
+        for (int u = 0; u < kRound; ++u) {
+            const uint32_t i = (uint32_t)min(i0 + u * B, hi - 1); // (a token of the pair always)
+            set[u] = from_mask[i];
+            v[u] = logp[i];
+            r[u] = from_ref[i];
         }
-        sum = lanes_sum<256>(sum, red);
-        share[side] = average ? 1.0 / fmax(lanes_sum<256>(many, red), 1.0) : 1.0;
-        d[side] = beta * sum * share[side];
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) {
+            const int i = i0 + u * B;
+            const bool counts = (i < hi) & (set[u] != 0 || !mask);
+            const double add = counts ? (double)v[u] - (ref ? (double)r[u] : 0.0) : 0.0, one = counts ? 1.0 : 0.0;
+            sums[0] += i < middle ? add : 0.0;
+            sums[1] += i < middle ? one : 0.0;
+            sums[2] += i < middle ? 0.0 : add;
+            sums[3] += i < middle ? 0.0 : one;
+        }
     }
-    const double x = d[0] - d[1] - margin, small = exp(-fabs(x)), more = log1p(small);
+    lanes_sum<B>(sums, red);
+    const double share[2] = {average ? 1.0 / fmax(sums[1], 1.0) : 1.0, average ? 1.0 / fmax(sums[3], 1.0) : 1.0};
+    const double d[2] = {beta * sums[0] * share[0], beta * sums[2] * share[1]};
+    const double x = d[0] - d[1] - margin, small = x == x ? exp_wide(-fabs(x)) : x;
     if (threadIdx.x == 0) {
         // -log sigma(x) = max(-x, 0) + log(1 + e^-|x|)
+        const double more = log1p(small);
         double v = 0.0; // (a side of no weight counts for nothing, also where it is infinite)
         if (smoothing < 1.0) v = (1.0 - smoothing) * (fmax(-x, 0.0) + more);
         if (smoothing > 0.0) v = fma(smoothing, fmax(x, 0.0) + more, v);
@@ -261,12 +373,12 @@ __global__ __launch_bounds__(kLossThreads) void preference_kernel(const float *_
         }
     }
     if (!out) return;
-    const double minus = (x > 0.0 ? small : 1.0) / (1.0 + small); // sigma(-x)
-    const double up = (double)g[pair] * beta * (smoothing * (x > 0.0 ? 1.0 : small) / (1.0 + small) - (1.0 - smoothing) * minus);
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const float v = (float)(side ? -up * share[1] : up * share[0]);
-        for (int64_t i = span[side].lo + threadIdx.x; i < span[side].hi; i += kLossThreads) out[i] = mask && !mask[i] ? 0.0f : v;
+    const double one = 1.0 / (1.0 + small), rest = small * one; // sigma(|x|), sigma(-|x|)
+    const double slope = up * beta * (x > 0.0 ? smoothing * one - (1.0 - smoothing) * rest : smoothing * rest - (1.0 - smoothing) * one);
+    const float to_first = (float)(slope * share[0]), to_second = (float)(-slope * share[1]);
+    for (int i = span[0].lo + (int)threadIdx.x; i < hi; i += B) {
+        const float v = i < middle ? to_first : to_second;
+        out[i] = mask && !mask[i] ? 0.0f : v;
     }
 }
 
@@ -275,8 +387,10 @@ size_t preference_scratch_bytes(int64_t, int) { return 0; }
 int launch_preference(const PreferenceParams &p, hipStream_t st)
 {
     if (p.pairs == 0 && !p.grad_logp) return AVQ_OK;
-    preference_kernel<<<dim3(std::max(p.pairs, 1)), dim3(kLossThreads), 0, st>>>(p.logp, p.ref, p.mask, p.tokens, p.offsets, p.pairs, p.beta, p.margin, p.smoothing, p.average, p.loss,
-                                                                              p.logit, p.reward, p.grad_loss, p.grad_logp);
+    const int threads = sequence_threads(p.tokens, 4 * (int64_t)p.pairs);
+    const auto kernel = threads == 64 ? preference_kernel<64> : threads == 256 ? preference_kernel<256> : preference_kernel<1024>;
+    kernel<<<dim3(sequence_groups(p.grad_logp ? p.tokens : 0, p.pairs)), dim3(threads), 0, st>>>(p.logp, p.ref, p.mask, (int)p.tokens, p.offsets, p.pairs, p.beta, p.margin, p.smoothing, p.average, p.loss, p.logit, p.reward,
+                                                                 p.grad_loss, p.grad_logp);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
@@ -285,58 +399,92 @@ int launch_preference(const PreferenceParams &p, hipStream_t st)
 struct PolicyTerm { double loss, kl, over, slope; };
 __device__ __forceinline__ PolicyTerm policy_term(double logp, double old, double advantage, bool has_ref, double ref, double least, double most, double weight)
 {
-    const double r = exp_wide(logp - old);
+    const double x = logp - old;
+    const double r = x == x ? exp_wide(x) : x;
     const bool over = (advantage > 0.0 && r > most) || (advantage < 0.0 && r < least);
     const double held = over ? (advantage > 0.0 ? most : least) : r;
     PolicyTerm t{-(held * advantage), 0.0, over ? 1.0 : 0.0, over ? 0.0 : -(r * advantage)};
     if (has_ref) {
-        const double away = ref - logp, e = expm1(away);
-        t.kl = e - away;
+        const double away = ref - logp;
+        const NearOne e = exp_near_one(away);
+        t.kl = away == away ? e.e2 : away;
         t.loss = fma(weight, t.kl, t.loss);
-        t.slope = fma(-weight, e, t.slope);
+        t.slope = away == away ? fma(-weight, e.e1, t.slope) : away;
     }
     return t;
 }
 
-// A workgroup a sequence.
-__global__ __launch_bounds__(kLossThreads) void policy_kernel(const float *__restrict__ logp, const float *__restrict__ old, const float *__restrict__ ref,
-                                                              const float *__restrict__ advantage, int each, const uint8_t *__restrict__ mask, int64_t tokens,
-                                                              const int32_t *__restrict__ offsets, int sequences, double least, double most, double weight, int average,
-                                                              float *__restrict__ loss, float *__restrict__ kl, float *__restrict__ clipped, const float *__restrict__ g,
-                                                              float *__restrict__ out)
+template <int B>
+__global__ __launch_bounds__(B, 8) void policy_kernel(const float *__restrict__ logp, const float *__restrict__ old, const float *__restrict__ ref, const float *__restrict__ advantage,
+                                                   int each, const uint8_t *__restrict__ mask, int tokens, const int32_t *__restrict__ offsets, int sequences, double least,
+                                                   double most, double weight, int average, float *__restrict__ loss, float *__restrict__ kl, float *__restrict__ clipped,
+                                                   const float *__restrict__ g, float *__restrict__ out)
 {
-    __shared__ double red[kLossWaves];
-    if (out) clear_outside(out, offsets, sequences, tokens);
+    __shared__ double red[B / 64 * 4];
+    if (out) clear_outside<B>(out, offsets, sequences, tokens);
     const int64_t s = blockIdx.x;
     if (s >= sequences) return;
     const Span span = span_of(offsets, s, tokens);
-    const double a = each ? 0.0 : (double)advantage[s];
-    double sum = 0.0, sum_kl = 0.0, over = 0.0, many = 0.0;
-    for (int64_t i = span.lo + threadIdx.x; i < span.hi; i += kLossThreads) {
-        if (mask && !mask[i]) continue;
-        const PolicyTerm t = policy_term(logp[i], old[i], each ? (double)advantage[i] : a, ref != nullptr, ref ? (double)ref[i] : 0.0, least, most, weight);
-        sum += t.loss;
-        sum_kl += t.kl;
-        over += t.over;
-        many += 1.0;
-    }
-    sum = lanes_sum<256>(sum, red);
-    sum_kl = lanes_sum<256>(sum_kl, red);
-    over = lanes_sum<256>(over, red);
-    many = fmax(lanes_sum<256>(many, red), 1.0);
-    const double share = average ? 1.0 / many : 1.0;
+    double up = out ? (double)g[s] : 0.0;
+    // (what is not given is read from logp all the same, and left out: no load waits for a branch)
+    const float *from_ref = ref ? ref : logp;
+    const uint8_t *from_mask = mask ? mask : (const uint8_t *)logp;
+    // the terms of kRound tokens from i0 on, in steps of B, for those that count: fn(u, the term)
+    auto round = [&](int i0, auto fn) __attribute__((always_inline)) {
+        float v[kRound], o[kRound], r[kRound], a[kRound];
+        uint8_t set[kRound];
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) {
+            const uint32_t i = (uint32_t)min(i0 + u * B, span.hi - 1); // (a token of the sequence always)
+            set[u] = from_mask[i];
+            v[u] = logp[i];
+            o[u] = old[i];
+            r[u] = from_ref[i];
+            a[u] = advantage[each ? i : (uint32_t)s];
+        }
+#pragma unroll
+        for (int u = 0; u < kRound; ++u)
+            if ((i0 + u * B < span.hi) & (set[u] != 0 || !mask)) fn(u, policy_term(v[u], o[u], a[u], ref != nullptr, r[u], least, most, weight));
+    };
+    // of the losses, of k, the clipped ones, those that count; the first round's slopes
+    double sums[4] = {0.0, 0.0, 0.0, 0.0}, slope[kRound] = {};
+    const int begin = span.lo + (int)threadIdx.x;
+    uint32_t counted = 0;
+    if (begin < span.hi)
+        round(begin, [&](int u, const PolicyTerm &t) __attribute__((always_inline)) {
+            sums[0] += t.loss;
+            sums[1] += t.kl;
+            sums[2] += t.over;
+            sums[3] += 1.0;
+            slope[u] = t.slope;
+            counted |= 1u << u;
+        });
+#pragma nounroll
+    for (int i0 = begin + kRound * B; i0 < span.hi; i0 += kRound * B)
+        round(i0, [&](int, const PolicyTerm &t) __attribute__((always_inline)) {
+            sums[0] += t.loss;
+            sums[1] += t.kl;
+            sums[2] += t.over;
+            sums[3] += 1.0;
+        });
+    lanes_sum<B>(sums, red);
+    const double many = fmax(sums[3], 1.0), share = average ? 1.0 / many : 1.0;
     if (threadIdx.x == 0) {
-        loss[s] = (float)(sum * share);
-        if (kl) kl[s] = (float)(sum_kl * share);
-        if (clipped) clipped[s] = (float)(over / many);
+        loss[s] = (float)(sums[0] * share);
+        if (kl) kl[s] = (float)(sums[1] * share);
+        if (clipped) clipped[s] = (float)(sums[2] / many);
     }
     if (!out) return;
-    const double up = (double)g[s] * share;
-    for (int64_t i = span.lo + threadIdx.x; i < span.hi; i += kLossThreads) {
-        float v = 0.0f;
-        if (!mask || mask[i])
-            v = (float)(up * policy_term(logp[i], old[i], each ? (double)advantage[i] : a, ref != nullptr, ref ? (double)ref[i] : 0.0, least, most, weight).slope);
-        out[i] = v;
+    up *= share;
+#pragma unroll
+    for (int u = 0; u < kRound; ++u)
+        if (begin + u * B < span.hi) out[begin + u * B] = counted >> u & 1u ? (float)(up * slope[u]) : 0.0f;
+#pragma nounroll
+    for (int i0 = begin + kRound * B; i0 < span.hi; i0 += kRound * B) {
+#pragma unroll
+        for (int u = 0; u < kRound; ++u)
+            if (i0 + u * B < span.hi) out[i0 + u * B] = 0.0f;
+        round(i0, [&](int u, const PolicyTerm &t) __attribute__((always_inline)) { out[i0 + u * B] = (float)(up * t.slope); });
     }
 }
 
@@ -345,9 +493,10 @@ size_t policy_scratch_bytes(int64_t, int) { return 0; }
 int launch_policy(const PolicyParams &p, hipStream_t st)
 {
     if (p.sequences == 0 && !p.grad_logp) return AVQ_OK;
-    policy_kernel<<<dim3(std::max(p.sequences, 1)), dim3(kLossThreads), 0, st>>>(p.logp, p.old, p.ref, p.advantage, p.each, p.mask, p.tokens, p.offsets, p.sequences,
-                                                                              1.0 - p.clip_low, 1.0 + p.clip_high, p.kl_weight, p.average, p.loss, p.kl, p.clipped, p.grad_loss,
-                                                                              p.grad_logp);
+    const int threads = sequence_threads(p.tokens, p.sequences);
+    const auto kernel = threads == 64 ? policy_kernel<64> : threads == 256 ? policy_kernel<256> : policy_kernel<1024>;
+    kernel<<<dim3(sequence_groups(p.grad_logp ? p.tokens : 0, p.sequences)), dim3(threads), 0, st>>>(p.logp, p.old, p.ref, p.advantage, p.each, p.mask, (int)p.tokens, p.offsets, p.sequences, 1.0 - p.clip_low,
+                                                                     1.0 + p.clip_high, p.kl_weight, p.average, p.loss, p.kl, p.clipped, p.grad_loss, p.grad_logp);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
