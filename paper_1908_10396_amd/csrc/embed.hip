@@ -113,9 +113,6 @@ __device__ __forceinline__ void clear_bytes(char *from, char *to, int64_t t, int
 // that stride over all of it 4.5 to 4.7 (0.42 to 1.37 GB).
 constexpr int kFillPiece = 16 << 10, kFillGroups = 2048;
 
-// Shares of the rows that the launches of a pass of the sort clear.
-constexpr int kShareCount = 3, kShareSums = 3, kSharePlace = 2;
-
 static int fill_groups(const FillJob &f)
 {
     const int64_t bytes = (f.hi - f.lo) * f.ld;
@@ -199,12 +196,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const int32_t 
 }
 
 // Each digit's counts become the counts of the tiles before, and totals[digit] their sum. A thread a digit.
-constexpr int kSumsThreads = 256;
-__global__ __launch_bounds__(kSumsThreads) void sort_sums_kernel(uint32_t *__restrict__ hist, int bins, int tiles, uint32_t *__restrict__ totals, FillJob fill)
+__global__ __launch_bounds__(64) void sort_sums_kernel(uint32_t *__restrict__ hist, int bins, int tiles, uint32_t *__restrict__ totals)
 {
-    const int groups = (bins + kSumsThreads - 1) / kSumsThreads;
-    if ((int)blockIdx.x >= groups) { fill_rows(fill, blockIdx.x - groups, gridDim.x - groups); return; }
-    const int b = blockIdx.x * kSumsThreads + threadIdx.x;
+    const int b = blockIdx.x * 64 + threadIdx.x;
     if (b >= bins) return;
     uint32_t run = 0;
     for (int t0 = 0; t0 < tiles; t0 += 16) {
@@ -414,102 +408,128 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
     }
 }
 
-// The runs that cross chunks: each by whoever has the chunk which it begins in. A team of `lanes` threads has a chunk, and adds a short run up
-// by itself; for a long one all of the workgroup's teams add up a share of its chunks each, in order, and then the shares in order. (Sampled
-// lists have thousands of short ones: a workgroup each took 26 us for 262,144 entries of 100 fp32.)
+// The runs that cross chunks: each by the workgroup that has the chunk which it begins in. Teams of `lanes` threads add up a share
+// of the chunks each, in order, and then the shares in order.
 constexpr int kJoinThreads = 512;
 constexpr int64_t kJoinGroups = 1 << 22; // a launch has fewer than 2^32 threads: with more chunks, a workgroup has several
+
+// The last chunk that the run goes on in which crosses this one's end, or 0: none does, or it began earlier.
+__device__ __forceinline__ uint32_t run_last(const uint32_t *__restrict__ keys, uint32_t chunk, uint32_t chunks, uint32_t count, uint32_t n)
+{
+    const uint32_t begin = chunk * (uint32_t)kRunChunk, end = begin + (uint32_t)kRunChunk;
+    if (end >= count) return 0; // the last chunk's runs end in it
+    const uint32_t key = keys[end - 1];
+    if (key >= n || keys[end] != key) return 0;
+    if (keys[begin] == key && begin > 0 && keys[begin - 1] == key) return 0;
+    // the chunks that the run goes on in: those whose first entry has the key
+    uint32_t lo = chunk + 1, hi = min(chunks, lo + 1); // the first chunk of another key lies in (lo, hi]
+    while (hi < chunks && keys[hi * (uint32_t)kRunChunk] == key) {
+        const uint32_t step = 2 * (hi - chunk);
+        lo = hi;
+        hi = min(chunks, chunk + step);
+    }
+    while (lo + 1 < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (keys[mid * (uint32_t)kRunChunk] == key) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// Joins the run that begins in `chunk` and ends in `last`, by all of the workgroup.
+template <class T, bool RAGGED>
+__device__ __forceinline__ void join_run(uint32_t key, uint32_t chunk, uint32_t last, int d, int lanes, float scale, T *__restrict__ out, int64_t ld_out, int accumulate,
+                                         const float *__restrict__ partial, float *shares)
+{
+    constexpr int V = kUnit<T>;
+    const uint32_t per_row = (uint32_t)units_of<T>(d), dp = per_row * V;
+    const uint32_t teams = kJoinThreads / (uint32_t)lanes, team = threadIdx.x / (uint32_t)lanes, lane = threadIdx.x % (uint32_t)lanes;
+    const uint32_t more = last - chunk; // chunk + 1 .. last
+    const uint32_t used = min(teams, (more + 3) / 4); // (four chunks a team at least)
+    for (uint32_t c0 = 0; c0 < per_row; c0 += (uint32_t)lanes) {
+        const uint32_t col = c0 + lane;
+        if (team < used && col < per_row) {
+            float acc[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] = team == 0 ? partial[((size_t)chunk * 2 + 1) * dp + (size_t)col * V + e] : 0.0f;
+            const uint32_t from = chunk + 1 + more * team / used, to = chunk + 1 + more * (team + 1) / used;
+#pragma unroll 16
+            for (uint32_t c = from; c < to; ++c) {
+                Pack<float, V> v;
+                __builtin_memcpy(&v, partial + (size_t)c * 2 * dp + (size_t)col * V, sizeof(v));
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] += v.e[e];
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) shares[(team * (uint32_t)lanes + lane) * V + e] = acc[e];
+        }
+        __syncthreads();
+        if (team == 0 && col < per_row) {
+            float acc[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+            for (uint32_t t = 0; t < used; ++t)
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] += shares[(t * (uint32_t)lanes + lane) * V + e];
+            write_row<T, RAGGED>(out + (int64_t)key * ld_out, (int)col * V, d, acc, scale, accumulate != 0);
+        }
+        __syncthreads();
+    }
+}
 
 template <class T, bool RAGGED>
 __global__ __launch_bounds__(kJoinThreads) void run_joins_kernel(const uint32_t *__restrict__ keys, uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out,
                                                                  int64_t ld_out, int accumulate, const float *__restrict__ partial)
+{
+    __shared__ float shares[kJoinThreads * kUnit<T>];
+    const uint32_t chunks = (count + kRunChunk - 1) / kRunChunk;
+    for (uint32_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+        const uint32_t last = run_last(keys, chunk, chunks, count, n);
+        if (last != 0) join_run<T, RAGGED>(keys[chunk * (uint32_t)kRunChunk + (uint32_t)kRunChunk - 1], chunk, last, d, lanes, scale, out, ld_out, accumulate, partial, shares);
+    }
+}
+
+// The same, bit for bit, where the chunks are more than fit the device at once and most runs are short, as those of sampled lists are: a team has a chunk, and
+// adds a run of up to five chunks up by itself (262,144 entries of 100 fp32: 14 against 26 us; 50,001: 8 against 4).
+constexpr int64_t kJoinByTeams = 4096;
+
+template <class T, bool RAGGED>
+__global__ __launch_bounds__(kJoinThreads) void run_joins_teams_kernel(const uint32_t *__restrict__ keys, uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out,
+                                                                       int64_t ld_out, int accumulate, const float *__restrict__ partial)
 {
     constexpr int V = kUnit<T>;
     __shared__ float shares[kJoinThreads * V];
     __shared__ uint32_t long_chunk[kJoinThreads / 4], long_last[kJoinThreads / 4], longs; // (teams have four lanes at least)
     const uint32_t chunks = (count + kRunChunk - 1) / kRunChunk, per_row = (uint32_t)units_of<T>(d), dp = per_row * V;
     const uint32_t teams = kJoinThreads / (uint32_t)lanes, team = threadIdx.x / (uint32_t)lanes, lane = threadIdx.x % (uint32_t)lanes;
-    for (uint32_t chunk0 = blockIdx.x * teams; chunk0 < chunks; chunk0 += gridDim.x * teams) {
-        if (threadIdx.x == 0) longs = 0;
-        __syncthreads();
-        const uint32_t mine = chunk0 + team, begin = mine * (uint32_t)kRunChunk, end = begin + (uint32_t)kRunChunk;
-        // (the last chunk's runs end in it; end does not pass 2^32: mine < chunks + teams)
-        if (mine < chunks && end < count) {
-            const uint32_t key = keys[end - 1];
-            const bool crosses = key < n && keys[end] == key;
-            if (crosses && !(keys[begin] == key && begin > 0 && keys[begin - 1] == key)) { // (else it began earlier)
-                // the chunks that the run goes on in: those whose first entry has the key
-                uint32_t lo = mine + 1, hi = min(chunks, lo + 1); // the first chunk of another key lies in (lo, hi]
-                while (hi < chunks && keys[hi * (uint32_t)kRunChunk] == key) {
-                    const uint32_t step = 2 * (hi - mine);
-                    lo = hi;
-                    hi = min(chunks, mine + step);
-                }
-                while (lo + 1 < hi) {
-                    const uint32_t mid = lo + (hi - lo) / 2;
-                    if (keys[mid * (uint32_t)kRunChunk] == key) lo = mid; else hi = mid;
-                }
-                if (lo - mine > 4) {
-                    if (lane == 0) {
-                        const uint32_t at = atomicAdd(&longs, 1u); // (runs have rows of their own: no order matters)
-                        long_chunk[at] = mine;
-                        long_last[at] = lo;
-                    }
-                } else {
-                    for (uint32_t col = lane; col < per_row; col += (uint32_t)lanes) {
-                        float acc[V];
-#pragma unroll
-                        for (int e = 0; e < V; ++e) acc[e] = partial[((size_t)mine * 2 + 1) * dp + (size_t)col * V + e];
-                        for (uint32_t c = mine + 1; c <= lo; ++c) {
-                            Pack<float, V> v;
-                            __builtin_memcpy(&v, partial + (size_t)c * 2 * dp + (size_t)col * V, sizeof(v));
-#pragma unroll
-                            for (int e = 0; e < V; ++e) acc[e] += v.e[e];
-                        }
-#pragma unroll
-                        for (int e = 0; e < V; ++e) acc[e] = 0.0f + acc[e]; // (as the shares are joined)
-                        write_row<T, RAGGED>(out + (int64_t)key * ld_out, (int)col * V, d, acc, scale, accumulate != 0);
-                    }
-                }
-            }
+    if (threadIdx.x == 0) longs = 0;
+    __syncthreads();
+    const uint32_t chunk = blockIdx.x * teams + team, last = chunk < chunks ? run_last(keys, chunk, chunks, count, n) : 0;
+    if (last != 0 && last - chunk > 4) {
+        if (lane == 0) {
+            const uint32_t at = atomicAdd(&longs, 1u); // (runs have rows of their own: no order matters)
+            long_chunk[at] = chunk;
+            long_last[at] = last;
         }
-        __syncthreads();
-        for (uint32_t i = 0; i < longs; ++i) {
-            const uint32_t chunk = long_chunk[i], more = long_last[i] - chunk; // chunk + 1 .. its last
-            const uint32_t key = keys[chunk * (uint32_t)kRunChunk + (uint32_t)kRunChunk - 1];
-            const uint32_t used = min(teams, (more + 3) / 4); // (four chunks a team at least)
-            for (uint32_t c0 = 0; c0 < per_row; c0 += (uint32_t)lanes) {
-                const uint32_t col = c0 + lane;
-                if (team < used && col < per_row) {
-                    float acc[V];
+    } else if (last != 0) {
+        const uint32_t key = keys[chunk * (uint32_t)kRunChunk + (uint32_t)kRunChunk - 1];
+        for (uint32_t col = lane; col < per_row; col += (uint32_t)lanes) {
+            float acc[V];
 #pragma unroll
-                    for (int e = 0; e < V; ++e) acc[e] = team == 0 ? partial[((size_t)chunk * 2 + 1) * dp + (size_t)col * V + e] : 0.0f;
-                    const uint32_t from = chunk + 1 + more * team / used, to = chunk + 1 + more * (team + 1) / used;
-#pragma unroll 16
-                    for (uint32_t c = from; c < to; ++c) {
-                        Pack<float, V> v;
-                        __builtin_memcpy(&v, partial + (size_t)c * 2 * dp + (size_t)col * V, sizeof(v));
+            for (int e = 0; e < V; ++e) acc[e] = partial[((size_t)chunk * 2 + 1) * dp + (size_t)col * V + e];
+            for (uint32_t c = chunk + 1; c <= last; ++c) {
+                Pack<float, V> v;
+                __builtin_memcpy(&v, partial + (size_t)c * 2 * dp + (size_t)col * V, sizeof(v));
 #pragma unroll
-                        for (int e = 0; e < V; ++e) acc[e] += v.e[e];
-                    }
-#pragma unroll
-                    for (int e = 0; e < V; ++e) shares[(team * (uint32_t)lanes + lane) * V + e] = acc[e];
-                }
-                __syncthreads();
-                if (team == 0 && col < per_row) {
-                    float acc[V];
-#pragma unroll
-                    for (int e = 0; e < V; ++e) acc[e] = 0.0f;
-                    for (uint32_t t = 0; t < used; ++t)
-#pragma unroll
-                        for (int e = 0; e < V; ++e) acc[e] += shares[(t * (uint32_t)lanes + lane) * V + e];
-                    write_row<T, RAGGED>(out + (int64_t)key * ld_out, (int)col * V, d, acc, scale, accumulate != 0);
-                }
-                __syncthreads();
+                for (int e = 0; e < V; ++e) acc[e] += v.e[e];
             }
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] = 0.0f + acc[e]; // (as the shares are joined)
+            write_row<T, RAGGED>(out + (int64_t)key * ld_out, (int)col * V, d, acc, scale, accumulate != 0);
         }
-        __syncthreads(); // (the list has been read)
     }
+    __syncthreads();
+    for (uint32_t i = 0; i < longs; ++i)
+        join_run<T, RAGGED>(keys[long_chunk[i] * (uint32_t)kRunChunk + (uint32_t)kRunChunk - 1], long_chunk[i], long_last[i], d, lanes, scale, out, ld_out, accumulate, partial, shares);
 }
 
 struct GradScratch {
@@ -563,18 +583,18 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
     // sums, which then have to pass over the rows with ids: 143 against 128 us for 50,001 ids of 1,183,514 x 100 fp32, 381 against 375
     // for 131,072 of 670,091 x 1,024 bf16.)
     const bool small = count <= (uint32_t)kSmallSort;
-    int done = 0;
-    const int all = small ? 1 : s.passes * (kShareCount + kShareSums + kSharePlace);
-    auto share = [&](int part) {
+    const int launches = small ? 1 : 2 * s.passes;
+    int launch = 0;
+    auto share = [&]() {
         FillJob f = fill;
-        f.lo = fill.hi * done / all;
-        done += part;
-        f.hi = fill.hi * done / all;
+        f.lo = fill.hi * launch / launches;
+        f.hi = fill.hi * (launch + 1) / launches;
+        ++launch;
         return f;
     };
     const uint32_t *keys = nullptr, *pos = nullptr;
     if (small) {
-        const FillJob f = share(1);
+        const FillJob f = share();
         sort_small_kernel<<<dim3(1 + fill_groups(f)), dim3(256), 0, st>>>(p.ids, count, n, s.keys[0], s.pos[0], f);
         AVQ_HIP(hipGetLastError());
         keys = s.keys[0];
@@ -583,10 +603,10 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
     for (int pass = 0; pass < (small ? 0 : s.passes); ++pass) {
         const int32_t *ids = pass == 0 ? p.ids : nullptr;
         const int to = pass & 1;
-        const FillJob f = share(kShareCount), h = share(kShareSums), g = share(kSharePlace);
+        const FillJob f = share(), g = share();
         sort_count_kernel<<<dim3(s.tiles + fill_groups(f)), dim3(kSortThreads), 0, st>>>(ids, keys, count, n, pass * s.bits, bins, s.hist, s.tiles, f);
         AVQ_HIP(hipGetLastError());
-        sort_sums_kernel<<<dim3((bins + kSumsThreads - 1) / kSumsThreads + fill_groups(h)), dim3(kSumsThreads), 0, st>>>(s.hist, bins, s.tiles, s.totals, h);
+        sort_sums_kernel<<<dim3((bins + 63) / 64), dim3(64), 0, st>>>(s.hist, bins, s.tiles, s.totals);
         AVQ_HIP(hipGetLastError());
         sort_place_kernel<<<dim3(s.tiles + fill_groups(g)), dim3(kSortThreads), 0, st>>>(ids, keys, pos, count, n, pass * s.bits, s.bits, s.hist, s.totals, s.tiles, s.keys[to], s.pos[to], g);
         AVQ_HIP(hipGetLastError());
@@ -603,7 +623,10 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
     AVQ_HIP(hipGetLastError());
     if (chunks > 1) {
         const int64_t teams = kJoinThreads / lanes;
-        run_joins_kernel<T, RAGGED><<<dim3((unsigned)std::min((chunks + teams - 1) / teams, kJoinGroups)), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
+        const bool by_teams = chunks > kJoinByTeams;
+        const auto joins = by_teams ? run_joins_teams_kernel<T, RAGGED> : run_joins_kernel<T, RAGGED>;
+        joins<<<dim3((unsigned)(by_teams ? (chunks + teams - 1) / teams : std::min(chunks, kJoinGroups))), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out,
+                                                                                                                                    p.ld_out, p.accumulate, s.partial);
         AVQ_HIP(hipGetLastError());
     }
     return AVQ_OK;
