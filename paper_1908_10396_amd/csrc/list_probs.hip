@@ -96,15 +96,16 @@ __device__ __forceinline__ void list_softmax(const float *scores, const int32_t 
     if (threadIdx.x == 0) *lse = base + sum + low;
 }
 
-// One wave does lists of up to 256: no barrier, and the other waves make room for the next query's.
-__device__ __forceinline__ void list_softmax_any(const float *scores, const int32_t *ids, int64_t n, int m, float *red, float *logp, float *lse)
+// Lists of up to kListFused get their softmax from the workgroup that scored them, longer ones and those in parts from list_softmax_kernel: its
+// sixteen entries a thread would cost the gather registers, and with them loads in flight. One wave does lists of up to 256: no barrier, and the
+// other waves make room for the next query's.
+constexpr int kListFused = 1024;
+__device__ __forceinline__ void list_softmax_fused(const float *scores, const int32_t *ids, int64_t n, int m, float *red, float *logp, float *lse)
 {
     if (m <= 256) {
         if (threadIdx.x < 64) list_softmax<64, 4>(scores, ids, n, m, red, logp, lse);
-    } else if (m <= 1024) {
-        list_softmax<kListThreads, 4>(scores, ids, n, m, red, logp, lse);
     } else {
-        list_softmax<kListThreads, 16>(scores, ids, n, m, red, logp, lse);
+        list_softmax<kListThreads, 4>(scores, ids, n, m, red, logp, lse);
     }
 }
 
@@ -118,15 +119,15 @@ __device__ __forceinline__ void list_ids(const int32_t *__restrict__ ids, int64_
 }
 
 // Scores of a part of a query's list, and where that is all of it the softmax. A row lies across L lanes that hold NV units of it each, and of
-// the query in fp32; four rows at a time a team of lanes.
+// the query in fp32; eight loads at a time a lane.
 template <class T, bool RAGGED, int L, int NV>
-__global__ __launch_bounds__(kListThreads) void list_probs_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int64_t ld_q, float scale,
+__global__ __launch_bounds__(kListThreads, NV == 4 || (RAGGED && (NV == 2 || sizeof(T) == 2)) ? 4 : 8) void list_probs_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int64_t ld_q, float scale,
                                                                   const int32_t *__restrict__ ids, int m, int parts, int each, const float *__restrict__ offset,
                                                                   float *__restrict__ logp, float *__restrict__ lse)
 {
     extern __shared__ int32_t lds[]; // the part's ids and scores
     __shared__ float red[kListWaves];
-    constexpr int V = kUnit<T>, kTeams = kListThreads / L, kRows = 4;
+    constexpr int V = kUnit<T>, kTeams = kListThreads / L, kRows = NV == 1 ? 8 : 4;
     const int per_row = units_of<T>(d), lane = threadIdx.x % L, team = threadIdx.x / L;
     const int64_t t = blockIdx.x / (uint32_t)parts;
     const int first = (int)(blockIdx.x - (uint32_t)t * parts) * each, count = min(each, m - first);
@@ -171,14 +172,15 @@ __global__ __launch_bounds__(kListThreads) void list_probs_kernel(const T *__res
     }
     __syncthreads();
     const int64_t at = t * m + first;
+    const bool fused = parts == 1 && m <= kListFused;
     for (int j = threadIdx.x; j < count; j += kListThreads) {
         const float s = offset ? __fmaf_rn(scores[j], scale, offset[at + j]) : scores[j] * scale;
-        if (parts == 1) scores[j] = s;
+        if (fused) scores[j] = s;
         else logp[at + j] = s;
     }
-    if (parts > 1) return;
+    if (!fused) return;
     __syncthreads();
-    list_softmax_any(scores, listed, n, m, red, logp + at, lse + t);
+    list_softmax_fused(scores, listed, n, m, red, logp + at, lse + t);
 }
 
 // The same for rows that registers do not hold: a wave a row, the query in LDS.
@@ -199,6 +201,7 @@ __global__ __launch_bounds__(kListThreads) void list_probs_long_kernel(const T *
     for (int k = threadIdx.x; k < per_row * V; k += kListThreads) qs[k] = k < d ? to_f32(q[t * ld_q + k]) : 0.0f;
     __syncthreads();
     const int64_t at = t * m + first;
+    const bool fused = parts == 1 && m <= kListFused;
     for (int j = threadIdx.x >> 6; j < count; j += kListWaves) {
         const T *row = x + (int64_t)max(listed[j], 0) * ld_x;
         float s = 0.0f;
@@ -211,21 +214,22 @@ __global__ __launch_bounds__(kListThreads) void list_probs_long_kernel(const T *
         s = group_sum<64>(s);
         if (lane == 0) {
             s = offset ? __fmaf_rn(s, scale, offset[at + j]) : s * scale;
-            if (parts == 1) scores[j] = s;
+            if (fused) scores[j] = s;
             else logp[at + j] = s;
         }
     }
-    if (parts > 1) return;
+    if (!fused) return;
     __syncthreads();
-    list_softmax_any(scores, listed, n, m, red, logp + at, lse + t);
+    list_softmax_fused(scores, listed, n, m, red, logp + at, lse + t);
 }
 
-// Lists that were scored in parts: a workgroup a query, in place.
+// Scores in logp, a workgroup a query, in place.
 __global__ __launch_bounds__(kListThreads) void list_softmax_kernel(const int32_t *__restrict__ ids, int64_t n, int m, float *logp, float *lse)
 {
     __shared__ float red[kListWaves];
     const int64_t t = blockIdx.x;
-    list_softmax_any(logp + t * m, ids + t * m, n, m, red, logp + t * m, lse + t);
+    if (m <= 4 * kListThreads) list_softmax<kListThreads, 4>(logp + t * m, ids + t * m, n, m, red, logp + t * m, lse + t);
+    else list_softmax<kListThreads, 16>(logp + t * m, ids + t * m, n, m, red, logp + t * m, lse + t);
 }
 
 // G of a part of a query's list, and what its rows add to dq: dq itself where the part is the list, else sums for list_join_kernel. A row's
@@ -383,7 +387,7 @@ static int list_typed(const ListParams &p, hipStream_t st)
 {
     const ListParts by = list_parts(p.nq, p.m);
     AVQ_TRY((whole_units(p.points, p.ld_points, p.d, sizeof(T)) ? list_scores<T, false>(p, by, st) : list_scores<T, true>(p, by, st)));
-    if (by.parts > 1) {
+    if (by.parts > 1 || p.m > kListFused) {
         list_softmax_kernel<<<dim3(p.nq), dim3(kListThreads), 0, st>>>(p.ids, p.n, p.m, p.logp, p.lse);
         AVQ_HIP(hipGetLastError());
     }

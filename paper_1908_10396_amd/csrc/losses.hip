@@ -382,8 +382,6 @@ __global__ __launch_bounds__(B) void preference_kernel(const float *__restrict__
     }
 }
 
-size_t preference_scratch_bytes(int64_t, int) { return 0; }
-
 int launch_preference(const PreferenceParams &p, hipStream_t st)
 {
     if (p.pairs == 0 && !p.grad_logp) return AVQ_OK;
@@ -487,8 +485,6 @@ __global__ __launch_bounds__(B, 8) void policy_kernel(const float *__restrict__ 
         round(i0, [&](int u, const PolicyTerm &t) __attribute__((always_inline)) { out[i0 + u * B] = (float)(up * t.slope); });
     }
 }
-
-size_t policy_scratch_bytes(int64_t, int) { return 0; }
 
 int launch_policy(const PolicyParams &p, hipStream_t st)
 {

@@ -254,7 +254,7 @@ int check_distill(const DistillParams &p)
     AVQ_TRY(check_count(p.rows));
     if (p.m < 0 || p.m > kMaxGiven) { set_error("m must be 0 .. %d, got %d", kMaxGiven, p.m); return AVQ_EINVAL; }
     AVQ_TRY(check_rows(p.teacher, p.m > 0 ? p.rows : 0, p.m, p.ld_teacher, p.type, "teacher"));
-    if (!(std::isfinite(p.temperature) && p.temperature > 0.0 && std::isfinite(1.0 / p.temperature))) return refuse("temperature must be finite and positive");
+    if (!(p.temperature >= 1e-6 && p.temperature <= 1e6)) return refuse("temperature must be 1e-6 .. 1e6");
     if (p.rows > 0 && p.m > 0 && !p.logp) return refuse("logp is NULL");
     return AVQ_OK;
 }
@@ -318,57 +318,40 @@ extern "C" int avq_distill_loss_grad(const float *logp, const void *teacher, int
     return launch_distill(p, (hipStream_t)hip_stream);
 }
 
-extern "C" int64_t avq_preference_loss_scratch(int64_t tokens, int32_t pairs)
-{
-    if (check_count(tokens) != AVQ_OK || pairs < 0 || pairs > kMaxSequences / 2) return refuse("tokens must be 0 .. 2^28 and pairs 0 .. 2^22");
-    return (int64_t)preference_scratch_bytes(tokens, pairs);
-}
-
 extern "C" int avq_preference_loss(const float *logp, const float *ref, const uint8_t *mask, int64_t tokens, const int32_t *offsets, int32_t pairs, double beta, double margin,
-                                   double smoothing, int32_t average, float *loss_out, float *logit_out, float *reward_out, void *scratch, int64_t scratch_bytes, void *hip_stream)
+                                   double smoothing, int32_t average, float *loss_out, float *logit_out, float *reward_out, void *hip_stream)
 {
-    const PreferenceParams p{logp, ref, mask, tokens, offsets, pairs, beta, margin, smoothing, average != 0, loss_out, logit_out, reward_out, nullptr, nullptr, scratch};
+    const PreferenceParams p{logp, ref, mask, tokens, offsets, pairs, beta, margin, smoothing, average != 0, loss_out, logit_out, reward_out, nullptr, nullptr};
     AVQ_TRY(check_preference(p));
-    AVQ_TRY(check_scratch(scratch, scratch_bytes, preference_scratch_bytes(tokens, pairs)));
     return launch_preference(p, (hipStream_t)hip_stream);
 }
 
 extern "C" int avq_preference_loss_grad(const float *logp, const float *ref, const uint8_t *mask, int64_t tokens, const int32_t *offsets, int32_t pairs, double beta, double margin,
-                                        double smoothing, int32_t average, const float *grad_loss, float *loss_out, float *logit_out, float *reward_out, float *grad_logp,
-                                        void *scratch, int64_t scratch_bytes, void *hip_stream)
+                                        double smoothing, int32_t average, const float *grad_loss, float *loss_out, float *logit_out, float *reward_out, float *grad_logp, void *hip_stream)
 {
-    const PreferenceParams p{logp, ref, mask, tokens, offsets, pairs, beta, margin, smoothing, average != 0, loss_out, logit_out, reward_out, grad_loss, grad_logp, scratch};
+    const PreferenceParams p{logp, ref, mask, tokens, offsets, pairs, beta, margin, smoothing, average != 0, loss_out, logit_out, reward_out, grad_loss, grad_logp};
     AVQ_TRY(check_preference(p));
     AVQ_TRY(check_upstream(grad_loss, grad_logp, pairs, tokens));
-    AVQ_TRY(check_scratch(scratch, scratch_bytes, preference_scratch_bytes(tokens, pairs)));
     return tokens == 0 && pairs == 0 ? AVQ_OK : launch_preference(p, (hipStream_t)hip_stream);
-}
-
-extern "C" int64_t avq_policy_loss_scratch(int64_t tokens, int32_t sequences)
-{
-    if (check_count(tokens) != AVQ_OK || sequences < 0 || sequences > kMaxSequences) return refuse("tokens must be 0 .. 2^28 and sequences 0 .. 2^23");
-    return (int64_t)policy_scratch_bytes(tokens, sequences);
 }
 
 extern "C" int avq_policy_loss(const float *logp, const float *old, const float *ref, const float *advantage, int32_t each, const uint8_t *mask, int64_t tokens,
                                const int32_t *offsets, int32_t sequences, double clip_low, double clip_high, double kl_weight, int32_t average, float *loss_out, float *kl_out,
-                               float *clipped_out, void *scratch, int64_t scratch_bytes, void *hip_stream)
+                               float *clipped_out, void *hip_stream)
 {
     const PolicyParams p{logp, old, ref, advantage, each != 0, mask, tokens, offsets, sequences, clip_low, clip_high, kl_weight, average != 0, loss_out, kl_out, clipped_out, nullptr,
-                         nullptr, scratch};
+                         nullptr};
     AVQ_TRY(check_policy(p));
-    AVQ_TRY(check_scratch(scratch, scratch_bytes, policy_scratch_bytes(tokens, sequences)));
     return launch_policy(p, (hipStream_t)hip_stream);
 }
 
 extern "C" int avq_policy_loss_grad(const float *logp, const float *old, const float *ref, const float *advantage, int32_t each, const uint8_t *mask, int64_t tokens,
                                     const int32_t *offsets, int32_t sequences, double clip_low, double clip_high, double kl_weight, int32_t average, const float *grad_loss,
-                                    float *loss_out, float *kl_out, float *clipped_out, float *grad_logp, void *scratch, int64_t scratch_bytes, void *hip_stream)
+                                    float *loss_out, float *kl_out, float *clipped_out, float *grad_logp, void *hip_stream)
 {
     const PolicyParams p{logp, old, ref, advantage, each != 0, mask, tokens, offsets, sequences, clip_low, clip_high, kl_weight, average != 0, loss_out, kl_out, clipped_out, grad_loss,
-                         grad_logp, scratch};
+                         grad_logp};
     AVQ_TRY(check_policy(p));
     AVQ_TRY(check_upstream(grad_loss, grad_logp, sequences, tokens));
-    AVQ_TRY(check_scratch(scratch, scratch_bytes, policy_scratch_bytes(tokens, sequences)));
     return tokens == 0 && sequences == 0 ? AVQ_OK : launch_policy(p, (hipStream_t)hip_stream);
 }

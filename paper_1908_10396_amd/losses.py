@@ -10,7 +10,7 @@ import collections
 import torch
 
 from . import _check, lib
-from .rows import _matrix, _on, _ptr, _same_device, _type, _vector
+from .rows import _matrix, _on, _same_device, _type, _vector
 
 PreferenceLoss = collections.namedtuple("PreferenceLoss", "loss logit reward")
 PreferenceLoss.__doc__ = """What preference_loss returns, fp32: loss and logit [pairs], reward [2 pairs] (the preferred answer's, then the other's)."""
@@ -36,11 +36,11 @@ def _distill(logp, teacher, teacher_lse, temperature, grad_loss, stream):
     up = None if grad_loss is None else _vector(grad_loss, "grad_loss", rows, _F32)
     _same_device(logp, teacher, teacher_lse, grad_loss)
     with _on(logp, stream) as st:
-        loss = torch.empty(rows, dtype=_F32, device=logp.device)
+        loss = logp.new_empty(rows)
         if up is None:
             _check(lib().avq_distill_loss(lp, tp, kind, rows, m, lt, sp, temperature, loss.data_ptr(), st))
             return None, loss
-        grad = torch.empty((rows, m), dtype=_F32, device=logp.device)
+        grad = torch.empty_like(logp)
         _check(lib().avq_distill_loss_grad(lp, tp, kind, rows, m, lt, sp, temperature, up, loss.data_ptr(), grad.data_ptr(), st))
     return grad, loss
 
@@ -65,19 +65,9 @@ def _sequences(logp, offsets):
         raise ValueError("logp must have one dimension")
     if not isinstance(offsets, torch.Tensor) or offsets.dtype != torch.int32 or not offsets.is_contiguous():
         raise TypeError("offsets must be a contiguous CUDA tensor of dtype torch.int32")
-    if offsets.dim() != 1 or offsets.shape[0] < 1:
+    if offsets.dim() != 1 or offsets.numel() < 1:
         raise ValueError("offsets: shape %s, expected (sequences + 1,)" % (tuple(offsets.shape),))
-    return logp.shape[0], offsets.shape[0] - 1
-
-
-def _loss_scratch(nbytes, device):
-    """(tensor, pointer, bytes); the small calls need none, and host time is what those take."""
-    if nbytes < 0:
-        _check(nbytes)
-    if nbytes == 0:
-        return None, None, 0
-    t = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return t, t.data_ptr(), nbytes
+    return logp.numel(), offsets.numel() - 1
 
 
 def _preference(logp, offsets, grad_loss, ref, mask, beta, margin, smoothing, average, stream):
@@ -89,16 +79,16 @@ def _preference(logp, offsets, grad_loss, ref, mask, beta, margin, smoothing, av
     up = None if grad_loss is None else _vector(grad_loss, "grad_loss", pairs, _F32)
     _same_device(logp, offsets, ref, mask, grad_loss)
     with _on(logp, stream) as st:
-        ws, wp, wn = _loss_scratch(lib().avq_preference_loss_scratch(tokens, pairs), logp.device)
-        loss, logit, reward = torch.empty(4 * pairs, dtype=_F32, device=logp.device).split([pairs, pairs, 2 * pairs])
-        out = PreferenceLoss(loss, logit, reward)
+        # (a few microseconds are most of a small call: tensors made one by one take less than views of one)
+        loss, logit, reward = logp.new_empty(pairs), logp.new_empty(pairs), logp.new_empty(sequences)
         args = (lp, rp, mp, tokens, offsets.data_ptr(), pairs, beta, margin, smoothing, 1 if average else 0)
         if up is None:
-            _check(lib().avq_preference_loss(*args, loss.data_ptr(), logit.data_ptr(), reward.data_ptr(), wp, wn, st))
-            return None, out
-        grad = torch.empty(tokens, dtype=_F32, device=logp.device)
-        _check(lib().avq_preference_loss_grad(*args, up, loss.data_ptr(), logit.data_ptr(), reward.data_ptr(), grad.data_ptr(), wp, wn, st))
-    return grad, out
+            grad = None
+            _check(lib().avq_preference_loss(*args, loss.data_ptr(), logit.data_ptr(), reward.data_ptr(), st))
+        else:
+            grad = logp.new_empty(tokens)
+            _check(lib().avq_preference_loss_grad(*args, up, loss.data_ptr(), logit.data_ptr(), reward.data_ptr(), grad.data_ptr(), st))
+    return grad, PreferenceLoss(loss, logit, reward)
 
 
 def preference_loss(logp, offsets, ref=None, mask=None, beta=0.1, margin=0.0, smoothing=0.0, average=False, stream=None):
@@ -127,15 +117,15 @@ def _policy(logp, old, advantage, offsets, grad_loss, ref, mask, clip, kl, avera
     up = None if grad_loss is None else _vector(grad_loss, "grad_loss", sequences, _F32)
     _same_device(logp, old, advantage, offsets, ref, mask, grad_loss)
     with _on(logp, stream) as st:
-        ws, wp, wn = _loss_scratch(lib().avq_policy_loss_scratch(tokens, sequences), logp.device)
-        out = PolicyLoss(*torch.empty((3, sequences), dtype=_F32, device=logp.device).unbind(0))
+        loss, kls, clipped = logp.new_empty(sequences), logp.new_empty(sequences), logp.new_empty(sequences)
         args = (lp, op, rp, ap, 1 if each else 0, mp, tokens, offsets.data_ptr(), sequences, low, high, kl, 1 if average else 0)
         if up is None:
-            _check(lib().avq_policy_loss(*args, _ptr(out.loss), _ptr(out.kl), _ptr(out.clipped), wp, wn, st))
-            return None, out
-        grad = torch.empty(tokens, dtype=_F32, device=logp.device)
-        _check(lib().avq_policy_loss_grad(*args, up, _ptr(out.loss), _ptr(out.kl), _ptr(out.clipped), grad.data_ptr(), wp, wn, st))
-    return grad, out
+            grad = None
+            _check(lib().avq_policy_loss(*args, loss.data_ptr(), kls.data_ptr(), clipped.data_ptr(), st))
+        else:
+            grad = logp.new_empty(tokens)
+            _check(lib().avq_policy_loss_grad(*args, up, loss.data_ptr(), kls.data_ptr(), clipped.data_ptr(), grad.data_ptr(), st))
+    return grad, PolicyLoss(loss, kls, clipped)
 
 
 def policy_loss(logp, old, advantage, offsets, ref=None, mask=None, clip=0.2, kl=0.0, average=True, each=None, stream=None):
