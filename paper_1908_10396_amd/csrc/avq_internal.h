@@ -563,7 +563,9 @@ struct EmbedGradParams {
     void *scratch;
     // position i adds weights[i] times row i / per_row of grad (NULL: row i itself)
     const float *weights = nullptr; int32_t per_row = 1;
+    int64_t cleared = 0; // the first rows of out, that are cleared already
 };
+int embed_grad_launches(int64_t n, int64_t count); // that clear rows, a share each
 size_t embed_grad_scratch_bytes(int64_t n, int d, int64_t count);
 int launch_embed_grad(const EmbedGradParams &p, hipStream_t st);
 

@@ -7,6 +7,7 @@
 // Lookup: rows as one list of 16-byte units, so that short and long rows fill workgroups alike; 65,536 rows of 2 KB in 41 us (268 MB, 6.5 TB/s
 // with what the caches hold). Gradient: 50,001 ids into 1,183,514 x 100 fp32 132 us, of which 473 MB of zeros alone are 72; 131,072 into
 // 670,091 x 1,024 bf16 378 us (238). The sort is launches of latency, so the table is cleared in the same ones.
+#include "fill_rows.h"
 #include "row_types.h"
 
 namespace avq {
@@ -90,49 +91,6 @@ constexpr int kSortThreads = 256, kSortEach = 8, kSortTile = kSortThreads * kSor
 constexpr int kMaxBins = 2048;
 
 __device__ __forceinline__ uint32_t key_of(int32_t id, uint32_t n) { return (uint32_t)id < n ? (uint32_t)id : n; }
-
-// Rows [lo, hi) of the table to be cleared by the workgroups of a launch beyond its own ones (ld, row_bytes: in bytes).
-struct FillJob { char *out; int64_t lo, hi, ld, row_bytes; };
-
-// bytes [from, to) of an address, multiples of two bytes, by the threads t of n
-__device__ __forceinline__ void clear_bytes(char *from, char *to, int64_t t, int64_t n)
-{
-    char *head = min(to, (char *)(((uintptr_t)from + 15) & ~(uintptr_t)15)), *tail = max(head, (char *)((uintptr_t)to & ~(uintptr_t)15));
-    typedef Pack<uint32_t, 4> Word;
-    const int64_t words = (tail - head) / 16;
-    int64_t i = t;
-    for (; i + 3 * n < words; i += 4 * n)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) *(Word *)(head + (i + u * n) * 16) = Word{};
-    for (; i < words; i += n) *(Word *)(head + i * 16) = Word{};
-    if (t < 8 && from + 2 * t < head) *(uint16_t *)(from + 2 * t) = 0;
-    if (t < 8 && tail + 2 * t < to) *(uint16_t *)(tail + 2 * t) = 0;
-}
-
-// Dense rows are one long row, a piece of it a workgroup: many short workgroups, four stores a thread, write 5.8 to 6.1 TB/s, 2,048
-// that stride over all of it 4.5 to 4.7 (0.42 to 1.37 GB).
-constexpr int kFillPiece = 16 << 10, kFillGroups = 2048;
-
-static int fill_groups(const FillJob &f)
-{
-    const int64_t bytes = (f.hi - f.lo) * f.ld;
-    if (bytes <= 0) return 0;
-    return (int)std::min<int64_t>(f.ld == f.row_bytes ? (bytes + kFillPiece - 1) / kFillPiece : kFillGroups, 1 << 20);
-}
-
-__device__ __forceinline__ void fill_rows(const FillJob &f, int group, int groups)
-{
-    if (f.ld == f.row_bytes) {
-        char *end = f.out + f.hi * f.ld;
-        for (char *at = f.out + f.lo * f.ld + (int64_t)group * kFillPiece; at < end; at += (int64_t)groups * kFillPiece)
-            clear_bytes(at, min(end, at + kFillPiece), threadIdx.x, blockDim.x);
-    } else {
-        // a wave a row
-        const int waves = blockDim.x / 64;
-        for (int64_t r = f.lo + (int64_t)group * waves + threadIdx.x / 64; r < f.hi; r += (int64_t)groups * waves)
-            clear_bytes(f.out + r * f.ld, f.out + r * f.ld + f.row_bytes, threadIdx.x & 63, 64);
-    }
-}
 
 __global__ __launch_bounds__(256) void fill_rows_kernel(FillJob fill) { fill_rows(fill, blockIdx.x, gridDim.x); }
 
@@ -564,15 +522,17 @@ static GradScratch grad_scratch(int64_t n, int d, int64_t count, void *base)
     return s;
 }
 
+int embed_grad_launches(int64_t n, int64_t count) { return count <= kSmallSort ? 1 : 2 * grad_scratch(n, 1, count, nullptr).passes; }
+
 size_t embed_grad_scratch_bytes(int64_t n, int d, int64_t count) { return grad_scratch(n, d, count, nullptr).bytes; }
 
 template <class T, bool RAGGED>
 static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
 {
-    FillJob fill{(char *)p.out, 0, p.accumulate ? 0 : p.n, p.ld_out * (int64_t)sizeof(T), p.d * (int64_t)sizeof(T)};
+    FillJob fill{(char *)p.out, p.accumulate ? 0 : p.cleared, p.accumulate ? 0 : p.n, p.ld_out * (int64_t)sizeof(T), p.d * (int64_t)sizeof(T)};
     if (p.count == 0) {
         if (p.accumulate) return AVQ_OK;
-        fill_rows_kernel<<<dim3(fill_groups(fill)), dim3(256), 0, st>>>(fill);
+        if (fill.lo < fill.hi) fill_rows_kernel<<<dim3(fill_groups(fill)), dim3(256), 0, st>>>(fill);
         AVQ_HIP(hipGetLastError());
         return AVQ_OK;
     }
@@ -587,8 +547,8 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
     int launch = 0;
     auto share = [&]() {
         FillJob f = fill;
-        f.lo = fill.hi * launch / launches;
-        f.hi = fill.hi * (launch + 1) / launches;
+        f.lo = fill.lo + (fill.hi - fill.lo) * launch / launches;
+        f.hi = fill.lo + (fill.hi - fill.lo) * (launch + 1) / launches;
         ++launch;
         return f;
     };

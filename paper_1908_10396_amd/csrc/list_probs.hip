@@ -7,6 +7,7 @@
 // the lookup's gradient (embed.hip) with G as weights. A workgroup a query: its scores stay in LDS between the products and the softmax.
 #include <math.h>
 
+#include "fill_rows.h"
 #include "row_types.h"
 
 namespace avq {
@@ -237,8 +238,9 @@ __global__ __launch_bounds__(kListThreads) void list_softmax_kernel(const int32_
 template <class T, bool RAGGED>
 __global__ __launch_bounds__(kListThreads) void list_grad_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, float scale, const int32_t *__restrict__ ids, int m, int parts,
                                                                  int each, const float *__restrict__ logp, const float *__restrict__ g, const float *__restrict__ g_lse, int lanes,
-                                                                 float *__restrict__ dscores, T *__restrict__ dq, int64_t ld_dq, float *__restrict__ partial)
+                                                                 float *__restrict__ dscores, T *__restrict__ dq, int64_t ld_dq, float *__restrict__ partial, unsigned own, FillJob fill)
 {
+    if (blockIdx.x >= own) { fill_rows(fill, blockIdx.x - own, gridDim.x - own); return; }
     extern __shared__ int32_t lds[]; // the part's ids and G, the teams' sums of a unit column
     __shared__ float red[kListWaves];
     constexpr int V = kUnit<T>, kAhead = 8;
@@ -402,16 +404,17 @@ static size_t list_partial_bytes(int d, int nq, int m)
 }
 
 template <class T, bool RAGGED>
-static int list_grad_run(const ListGradParams &p, hipStream_t st)
+static int list_grad_run(const ListGradParams &p, const FillJob &fill, hipStream_t st)
 {
     const ListParts by = list_parts(p.nq, p.m);
     const int per_row = units_of<T>(p.d);
     int lanes = 4;
     while (lanes < kListThreads && lanes < per_row) lanes *= 2;
     const size_t lds = (size_t)by.each * 8 + (size_t)kListThreads * kUnit<T> * sizeof(float);
-    list_grad_kernel<T, RAGGED><<<dim3((unsigned)p.nq * by.parts), dim3(kListThreads), lds, st>>>((const T *)p.points, p.n, p.d, p.ld_points, p.scale, p.ids, p.m, by.parts, by.each, p.logp,
-                                                                                               p.grad_logp, p.grad_lse, lanes, p.dscores, (T *)p.dqueries, p.ld_dqueries,
-                                                                                               (float *)p.scratch);
+    const unsigned own = (unsigned)p.nq * by.parts;
+    list_grad_kernel<T, RAGGED><<<dim3(own + fill_groups(fill)), dim3(kListThreads), lds, st>>>((const T *)p.points, p.n, p.d, p.ld_points, p.scale, p.ids, p.m, by.parts, by.each, p.logp,
+                                                                                             p.grad_logp, p.grad_lse, lanes, p.dscores, (T *)p.dqueries, p.ld_dqueries,
+                                                                                             (float *)p.scratch, own, fill);
     AVQ_HIP(hipGetLastError());
     if (p.dqueries && by.parts > 1) {
         list_join_kernel<T, RAGGED><<<dim3(p.nq, (per_row + 63) / 64), dim3(64), 0, st>>>((const float *)p.scratch, by.parts, p.d, p.scale, (T *)p.dqueries, p.ld_dqueries);
@@ -421,10 +424,10 @@ static int list_grad_run(const ListGradParams &p, hipStream_t st)
 }
 
 template <class T>
-static int list_grad_typed(const ListGradParams &p, hipStream_t st)
+static int list_grad_typed(const ListGradParams &p, const FillJob &fill, hipStream_t st)
 {
     const bool whole = whole_units(p.points, p.ld_points, p.d, sizeof(T)) && (!p.dqueries || whole_units(p.dqueries, p.ld_dqueries, p.d, sizeof(T)));
-    return whole ? list_grad_run<T, false>(p, st) : list_grad_run<T, true>(p, st);
+    return whole ? list_grad_run<T, false>(p, fill, st) : list_grad_run<T, true>(p, fill, st);
 }
 
 int launch_list_probs(const ListParams &p, hipStream_t st)
@@ -442,16 +445,21 @@ size_t list_grad_scratch_bytes(int64_t n, int d, int nq, int m)
 
 int launch_list_grad(const ListGradParams &p, hipStream_t st)
 {
+    // the launch that forms dq clears a share of dx too, as those of the sort do
+    const int size = type_bytes(p.type);
+    const int64_t count = (int64_t)p.nq * p.m;
+    FillJob fill{(char *)p.dpoints, 0, p.dpoints && !p.accumulate && count > 0 ? p.n / (1 + embed_grad_launches(p.n, count)) : 0, p.ld_dpoints * size, (int64_t)p.d * size};
     if (p.nq > 0) {
-        if (p.type == AVQ_F32) AVQ_TRY(list_grad_typed<float>(p, st));
-        else if (p.type == AVQ_BF16) AVQ_TRY(list_grad_typed<bf16_t>(p, st));
-        else AVQ_TRY(list_grad_typed<f16_t>(p, st));
+        if (p.type == AVQ_F32) AVQ_TRY(list_grad_typed<float>(p, fill, st));
+        else if (p.type == AVQ_BF16) AVQ_TRY(list_grad_typed<bf16_t>(p, fill, st));
+        else AVQ_TRY(list_grad_typed<f16_t>(p, fill, st));
     }
     if (!p.dpoints) return AVQ_OK;
-    EmbedGradParams rows{p.queries, p.type, p.ld_queries, p.ids, (int64_t)p.nq * p.m, p.scale, p.dpoints, p.n, p.d, p.ld_dpoints, p.accumulate,
+    EmbedGradParams rows{p.queries, p.type, p.ld_queries, p.ids, count, p.scale, p.dpoints, p.n, p.d, p.ld_dpoints, p.accumulate,
                          (char *)p.scratch + (p.nq > 0 ? list_partial_bytes(p.d, p.nq, p.m) : 0)};
     rows.weights = p.dscores;
     rows.per_row = p.m;
+    rows.cleared = fill.hi;
     return launch_embed_grad(rows, st);
 }
 
