@@ -124,7 +124,12 @@ __global__ __launch_bounds__(256) void sort_small_kernel(const int32_t *__restri
                 const u64 a = e[lo], b = e[hi];
                 if ((a > b) == ((lo & k) == 0)) { e[lo] = b; e[hi] = a; }
             }
-            __syncthreads();
+            // (pairs up to 64 apart lie within 128 entries that one wave has in this stage and the next)
+            if (j > 64 || (j == 1 && k >= 64)) __syncthreads();
+            else {
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
         }
     for (uint32_t i = threadIdx.x; i < count; i += 256) {
         keys_out[i] = (uint32_t)(e[i] >> 32);
@@ -264,18 +269,6 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t 
 // ---- sums of the runs ----------------------------------------------------------------------
 
 constexpr int kRunChunk = 32; // sorted entries that one group of lanes sums
-
-// a row's unit: acc scale, or that added to what is there
-template <class T, bool RAGGED>
-__device__ __forceinline__ void write_row(T *__restrict__ row, int k, int d, const float *acc, float scale, bool accumulate)
-{
-    constexpr int V = kUnit<T>;
-    Unit<T> o;
-    if (accumulate) o = load_unit<T, RAGGED>(row, k, d);
-#pragma unroll
-    for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(accumulate ? to_f32(o.e[e]) + acc[e] * scale : acc[e] * scale);
-    store_unit<T, RAGGED>(row, k, d, o);
-}
 
 // Each team of `lanes` threads takes a chunk of kRunChunk sorted entries. A run that lies within the chunk goes to its
 // row; what belongs to a run that crosses the chunk's start or end goes to partial[chunk][0] or [1] (a run through the

@@ -233,8 +233,50 @@ __global__ __launch_bounds__(kListThreads) void list_softmax_kernel(const int32_
     else list_softmax<kListThreads, 16>(logp + t * m, ids + t * m, n, m, red, logp + t * m, lse + t);
 }
 
-// G of a part of a query's list, and what its rows add to dq: dq itself where the part is the list, else sums for list_join_kernel. A row's
-// units lie across `lanes` lanes; kAhead rows at a time a team of them.
+// Sums of `count` weighted rows, by all of the workgroup: a row's units lie across `lanes` lanes, kAhead rows at a time a team of them, then the
+// teams' sums in order. row(j), weight(j): of the j-th (a readable row always); finish(u, acc): once for each unit, by the first team. A weight of 0 adds
+// nothing, whatever its row holds.
+template <class T, bool RAGGED, class RowOf, class WeightOf, class Finish>
+__device__ __forceinline__ void weighted_rows(int count, int d, int lanes, float *sums, RowOf row, WeightOf weight, Finish finish)
+{
+    constexpr int V = kUnit<T>, kAhead = 8;
+    const int per_row = units_of<T>(d), teams = kListThreads / lanes, team = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    for (int u0 = 0; u0 < per_row; u0 += lanes) {
+        const int u = u0 + lane;
+        float acc[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+        if (u < per_row)
+            for (int j0 = team; j0 < count; j0 += teams * kAhead) {
+                Unit<T> v[kAhead];
+                float w[kAhead];
+#pragma unroll
+                for (int r = 0; r < kAhead; ++r) {
+                    const int j = min(j0 + r * teams, count - 1);
+                    w[r] = j0 + r * teams < count ? weight(j) : 0.0f;
+                    v[r] = load_unit<T, RAGGED>(row(j), u * V, d);
+                }
+#pragma unroll
+                for (int r = 0; r < kAhead; ++r)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[e] = w[r] != 0.0f ? __fmaf_rn(w[r], to_f32(v[r].e[e]), acc[e]) : acc[e];
+            }
+        if (teams > 1) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) sums[threadIdx.x * V + e] = acc[e];
+            __syncthreads();
+        }
+        if (team == 0 && u < per_row) {
+            for (int o = 1; o < teams; ++o)
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] += sums[(o * lanes + lane) * V + e];
+            finish(u, acc);
+        }
+        if (teams > 1) __syncthreads();
+    }
+}
+
+// G of a part of a query's list, and what its rows add to dq: dq itself where the part is the list, else sums for list_join.
 template <class T, bool RAGGED>
 __global__ __launch_bounds__(kListThreads) void list_grad_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, float scale, const int32_t *__restrict__ ids, int m, int parts,
                                                                  int each, const float *__restrict__ logp, const float *__restrict__ g, const float *__restrict__ g_lse, int lanes,
@@ -243,7 +285,7 @@ __global__ __launch_bounds__(kListThreads) void list_grad_kernel(const T *__rest
     if (blockIdx.x >= own) { fill_rows(fill, blockIdx.x - own, gridDim.x - own); return; }
     extern __shared__ int32_t lds[]; // the part's ids and G, the teams' sums of a unit column
     __shared__ float red[kListWaves];
-    constexpr int V = kUnit<T>, kAhead = 8;
+    constexpr int V = kUnit<T>;
     const int64_t t = blockIdx.x / (uint32_t)parts;
     const int part = (int)(blockIdx.x - (uint32_t)t * parts), first = part * each, count = min(each, m - first);
     int32_t *listed = lds;
@@ -282,59 +324,28 @@ __global__ __launch_bounds__(kListThreads) void list_grad_kernel(const T *__rest
     }
     if (!dq) return;
     __syncthreads();
-    const int per_row = units_of<T>(d), teams = kListThreads / lanes, team = threadIdx.x / lanes, lane = threadIdx.x % lanes;
-    for (int u0 = 0; u0 < per_row; u0 += lanes) {
-        const int u = u0 + lane;
-        float acc[V];
+    const int per_row = units_of<T>(d);
+    weighted_rows<T, RAGGED>(count, d, lanes, sums, [&](int j) { return x + (int64_t)listed[j] * ld_x; }, [&](int j) { return G[j]; }, [&](int u, const float (&acc)[V]) {
+        if (parts == 1) {
+            Unit<T> out;
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] = 0.0f;
-        if (u < per_row)
-            for (int j0 = team; j0 < count; j0 += teams * kAhead) {
-                Unit<T> v[kAhead];
-                float w[kAhead];
+            for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(acc[e] * scale);
+            store_unit<T, RAGGED>(dq + t * ld_dq, u * V, d, out);
+        } else {
+            Pack<float, V> out;
 #pragma unroll
-                for (int r = 0; r < kAhead; ++r) {
-                    const int j = j0 + r * teams;
-                    w[r] = j < count ? G[j] : 0.0f;
-                    v[r] = load_unit<T, RAGGED>(x + (int64_t)(j < count ? listed[j] : 0) * ld_x, u * V, d);
-                }
-#pragma unroll
-                for (int r = 0; r < kAhead; ++r)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) acc[e] = w[r] != 0.0f ? __fmaf_rn(w[r], to_f32(v[r].e[e]), acc[e]) : acc[e];
-            }
-        if (teams > 1) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) sums[threadIdx.x * V + e] = acc[e];
-            __syncthreads();
+            for (int e = 0; e < V; ++e) out.e[e] = acc[e];
+            *(Pack<float, V> *)(partial + ((t * parts + part) * per_row + u) * V) = out;
         }
-        if (team == 0 && u < per_row) {
-            for (int o = 1; o < teams; ++o)
-#pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] += sums[(o * lanes + lane) * V + e];
-            if (parts == 1) {
-                Unit<T> out;
-#pragma unroll
-                for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(acc[e] * scale);
-                store_unit<T, RAGGED>(dq + t * ld_dq, u * V, d, out);
-            } else {
-                Pack<float, V> out;
-#pragma unroll
-                for (int e = 0; e < V; ++e) out.e[e] = acc[e];
-                *(Pack<float, V> *)(partial + ((t * parts + part) * per_row + u) * V) = out;
-            }
-        }
-        if (teams > 1) __syncthreads();
-    }
+    });
 }
 
-// dq from its parts' sums, in order: a wave 64 units of a query.
+// A unit of dq from its parts' sums, in order.
 template <class T, bool RAGGED>
-__global__ __launch_bounds__(64) void list_join_kernel(const float *__restrict__ partial, int parts, int d, float scale, T *__restrict__ dq, int64_t ld_dq)
+__device__ __forceinline__ void list_join(const float *__restrict__ partial, int64_t t, int u, int parts, int d, float scale, T *__restrict__ dq, int64_t ld_dq)
 {
     constexpr int V = kUnit<T>;
-    const int per_row = units_of<T>(d), u = blockIdx.y * 64 + threadIdx.x;
-    const int64_t t = blockIdx.x;
+    const int per_row = units_of<T>(d);
     if (u >= per_row) return;
     float acc[V];
 #pragma unroll
@@ -349,6 +360,61 @@ __global__ __launch_bounds__(64) void list_join_kernel(const float *__restrict__
 #pragma unroll
     for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(acc[e] * scale);
     store_unit<T, RAGGED>(dq + t * ld_dq, u * V, d, out);
+}
+
+// a wave 64 units of a query
+template <class T, bool RAGGED>
+__global__ __launch_bounds__(64) void list_join_kernel(const float *__restrict__ partial, int parts, int d, float scale, T *__restrict__ dq, int64_t ld_dq)
+{
+    list_join<T, RAGGED>(partial, blockIdx.x, blockIdx.y * 64 + threadIdx.x, parts, d, scale, dq, ld_dq);
+}
+
+// dx of a few entries without sorting them: a workgroup an entry, which looks for its id among those before, and if it is the first adds up
+// all that have it, in their order; the workgroups past the entries join dq. (50 to 2,048 entries take 5 to xx us, where sorting, sums and joins take
+// 25 to 55.)
+constexpr int kListFew = 2048;
+
+template <class T, bool RAGGED>
+__global__ __launch_bounds__(kListThreads) void list_few_rows_kernel(const T *__restrict__ q, int64_t ld_q, int d, float scale, const int32_t *__restrict__ ids, int count, int m, int64_t n,
+                                                                     const float *__restrict__ G, int lanes, T *__restrict__ dx, int64_t ld_dx, int accumulate,
+                                                                     const float *__restrict__ partial, int parts, int per_query, T *__restrict__ dq, int64_t ld_dq)
+{
+    __shared__ float sums[kListThreads * kUnit<T>];
+    __shared__ int listed[kListFew], found[kListWaves];
+    const int i = blockIdx.x;
+    if (i >= count) {
+        const int b = i - count;
+        list_join<T, RAGGED>(partial, b / per_query, b % per_query * kListThreads + threadIdx.x, parts, d, scale, dq, ld_dq);
+        return;
+    }
+    const int32_t id = ids[i];
+    if (id < 0 || (int64_t)id >= n) return;
+    int32_t v[kListFew / kListThreads];
+#pragma unroll
+    for (int k = 0; k < kListFew / kListThreads; ++k) v[k] = ids[min(k * kListThreads + (int)threadIdx.x, count - 1)]; // (an entry always: no load waits for a branch)
+    bool earlier = false;
+#pragma unroll
+    for (int k = 0; k < kListFew / kListThreads; ++k) earlier |= k * kListThreads + (int)threadIdx.x < i && v[k] == id;
+    if (__syncthreads_or(earlier)) return;
+    int many = 0;
+#pragma unroll
+    for (int k = 0; k < kListFew / kListThreads; ++k) {
+        if (k * kListThreads >= count) break;
+        const int j = k * kListThreads + threadIdx.x;
+        const bool same = j < count && v[k] == id;
+        const u64 which = __ballot(same);
+        if ((threadIdx.x & 63) == 0) found[threadIdx.x >> 6] = __popcll(which);
+        __syncthreads();
+        int at = many + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(which >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)which, 0u));
+        for (int w = 0; w < kListWaves; ++w) {
+            if (w < (int)(threadIdx.x >> 6)) at += found[w];
+            many += found[w];
+        }
+        if (same) listed[at] = j;
+        __syncthreads();
+    }
+    weighted_rows<T, RAGGED>(many, d, lanes, sums, [&](int j) { return q + (int64_t)(listed[j] / m) * ld_q; }, [&](int j) { return G[listed[j]]; },
+                             [&](int u, const float (&acc)[kUnit<T>]) { write_row<T, RAGGED>(dx + (int64_t)id * ld_dx, u * kUnit<T>, d, acc, scale, accumulate != 0); });
 }
 
 template <class T, bool RAGGED, int L, int NV>
@@ -403,6 +469,8 @@ static size_t list_partial_bytes(int d, int nq, int m)
     return by.parts == 1 ? 0 : ((size_t)nq * by.parts * ((d + 7) / 8 * 8) * sizeof(float) + 255) & ~(size_t)255;
 }
 
+static bool few_entries(const ListGradParams &p) { return p.nq > 0 && p.m > 0 && (int64_t)p.nq * p.m <= kListFew; }
+
 template <class T, bool RAGGED>
 static int list_grad_run(const ListGradParams &p, const FillJob &fill, hipStream_t st)
 {
@@ -416,7 +484,13 @@ static int list_grad_run(const ListGradParams &p, const FillJob &fill, hipStream
                                                                                              p.grad_logp, p.grad_lse, lanes, p.dscores, (T *)p.dqueries, p.ld_dqueries,
                                                                                              (float *)p.scratch, own, fill);
     AVQ_HIP(hipGetLastError());
-    if (p.dqueries && by.parts > 1) {
+    if (p.dpoints && few_entries(p)) {
+        const int per_query = p.dqueries && by.parts > 1 ? (per_row + kListThreads - 1) / kListThreads : 0;
+        list_few_rows_kernel<T, RAGGED><<<dim3((unsigned)(p.nq * p.m + p.nq * per_query)), dim3(kListThreads), 0, st>>>(
+            (const T *)p.queries, p.ld_queries, p.d, p.scale, p.ids, p.nq * p.m, p.m, p.n, p.dscores, lanes, (T *)p.dpoints, p.ld_dpoints, p.accumulate, (const float *)p.scratch, by.parts,
+            per_query, (T *)p.dqueries, p.ld_dqueries);
+        AVQ_HIP(hipGetLastError());
+    } else if (p.dqueries && by.parts > 1) {
         list_join_kernel<T, RAGGED><<<dim3(p.nq, (per_row + 63) / 64), dim3(64), 0, st>>>((const float *)p.scratch, by.parts, p.d, p.scale, (T *)p.dqueries, p.ld_dqueries);
         AVQ_HIP(hipGetLastError());
     }
@@ -426,7 +500,8 @@ static int list_grad_run(const ListGradParams &p, const FillJob &fill, hipStream
 template <class T>
 static int list_grad_typed(const ListGradParams &p, const FillJob &fill, hipStream_t st)
 {
-    const bool whole = whole_units(p.points, p.ld_points, p.d, sizeof(T)) && (!p.dqueries || whole_units(p.dqueries, p.ld_dqueries, p.d, sizeof(T)));
+    const bool whole = whole_units(p.points, p.ld_points, p.d, sizeof(T)) && (!p.dqueries || whole_units(p.dqueries, p.ld_dqueries, p.d, sizeof(T))) &&
+                       (!p.dpoints || !few_entries(p) || (whole_units(p.queries, p.ld_queries, p.d, sizeof(T)) && whole_units(p.dpoints, p.ld_dpoints, p.d, sizeof(T))));
     return whole ? list_grad_run<T, false>(p, fill, st) : list_grad_run<T, true>(p, fill, st);
 }
 
@@ -440,21 +515,23 @@ int launch_list_probs(const ListParams &p, hipStream_t st)
 size_t list_grad_scratch_bytes(int64_t n, int d, int nq, int m)
 {
     const int64_t count = (int64_t)nq * m;
-    return count == 0 ? 0 : list_partial_bytes(d, nq, m) + embed_grad_scratch_bytes(n, d, count);
+    return count == 0 ? 0 : list_partial_bytes(d, nq, m) + (count <= kListFew ? 0 : embed_grad_scratch_bytes(n, d, count));
 }
 
 int launch_list_grad(const ListGradParams &p, hipStream_t st)
 {
-    // the launch that forms dq clears a share of dx too, as those of the sort do
+    // the launch that forms dq clears a share of dx too, as those of the sort do, or all of it
     const int size = type_bytes(p.type);
     const int64_t count = (int64_t)p.nq * p.m;
-    FillJob fill{(char *)p.dpoints, 0, p.dpoints && !p.accumulate && count > 0 ? p.n / (1 + embed_grad_launches(p.n, count)) : 0, p.ld_dpoints * size, (int64_t)p.d * size};
+    const bool few = few_entries(p);
+    FillJob fill{(char *)p.dpoints, 0, 0, p.ld_dpoints * size, (int64_t)p.d * size};
+    if (p.dpoints && !p.accumulate && count > 0) fill.hi = few ? p.n : p.n / (1 + embed_grad_launches(p.n, count));
     if (p.nq > 0) {
         if (p.type == AVQ_F32) AVQ_TRY(list_grad_typed<float>(p, fill, st));
         else if (p.type == AVQ_BF16) AVQ_TRY(list_grad_typed<bf16_t>(p, fill, st));
         else AVQ_TRY(list_grad_typed<f16_t>(p, fill, st));
     }
-    if (!p.dpoints) return AVQ_OK;
+    if (!p.dpoints || few) return AVQ_OK;
     EmbedGradParams rows{p.queries, p.type, p.ld_queries, p.ids, count, p.scale, p.dpoints, p.n, p.d, p.ld_dpoints, p.accumulate,
                          (char *)p.scratch + (p.nq > 0 ? list_partial_bytes(p.d, p.nq, p.m) : 0)};
     rows.weights = p.dscores;

@@ -84,6 +84,18 @@ template <class T, bool RAGGED> __device__ __forceinline__ void store_unit(T *__
     }
 }
 
+// a row's unit: acc scale, or that added to what is there
+template <class T, bool RAGGED>
+__device__ __forceinline__ void write_row(T *__restrict__ row, int k, int d, const float *acc, float scale, bool accumulate)
+{
+    constexpr int V = kUnit<T>;
+    Unit<T> o;
+    if (accumulate) o = load_unit<T, RAGGED>(row, k, d);
+#pragma unroll
+    for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(accumulate ? to_f32(o.e[e]) + acc[e] * scale : acc[e] * scale);
+    store_unit<T, RAGGED>(row, k, d, o);
+}
+
 // Bytes that every row of rows at `p`, `ld` elements apart and `d` long, can be read in at once: 16, 8 or one element.
 inline int row_width(const void *p, int64_t ld, int64_t d, int size)
 {
