@@ -359,6 +359,94 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const T *__restrict__ gra
     }
 }
 
+// i / by for i < 2^28 and by of 1 .. 4096: with 2^(s-1) < by <= 2^s and m = ceil(2^(28+s) / by), m by is at most by - 1 above 2^(28+s), and
+// i times that below it.
+struct Divide { uint32_t m; int s; };
+inline Divide divide_by(uint32_t by)
+{
+    int s = 0;
+    while ((1u << s) < by) ++s;
+    return Divide{(uint32_t)((((uint64_t)1 << (28 + s)) + by - 1) / by), s};
+}
+__device__ __forceinline__ uint32_t divided(uint32_t i, const Divide &d) { return __umulhi(i << 4, d.m) >> d.s; }
+
+// The weighted sums of few entries: a team of L lanes has an entry, and sums the part of a run that begins there, most have none to; the parts go where
+// those of run_sums_kernel do. NV units a lane. (6,160 entries of 98 f16: 12 us against 25; 262,144 of 100 fp32, which take many rounds of
+// mostly idle teams: 62 against 20.)
+constexpr int64_t kFewEntries = 16384;
+
+template <class T, bool RAGGED, int L, int NV>
+__global__ __launch_bounds__(256) void run_sums_weighted_kernel(const T *__restrict__ grad, int64_t ld_grad, const float *__restrict__ weights, Divide per, const uint32_t *__restrict__ keys,
+                                                                const uint32_t *__restrict__ pos, uint32_t count, uint32_t n, int d, float scale, T *__restrict__ out, int64_t ld_out,
+                                                                int accumulate, float *__restrict__ partial)
+{
+    constexpr int V = kUnit<T>, kAhead = NV == 1 ? 8 : 4;
+    const uint32_t i = blockIdx.x * (256u / L) + threadIdx.x / L, lane = threadIdx.x % L;
+    if (i >= count) return;
+    const uint32_t key = keys[i], before = i > 0 ? keys[i - 1] : 0xffffffffu; // (no key is that)
+    const bool at_chunk = i % (uint32_t)kRunChunk == 0;
+    if (key >= n || (!at_chunk && before == key)) return;
+    const uint32_t chunk = i / (uint32_t)kRunChunk, end = min(count, (chunk + 1) * (uint32_t)kRunChunk);
+    const uint32_t per_row = (uint32_t)units_of<T>(d), dp = per_row * V;
+    for (uint32_t col0 = 0; col0 < per_row; col0 += L * NV) {
+        float acc[NV][V];
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[c][e] = 0.0f;
+        uint32_t j = i;
+        bool goes_on = true;
+        while (goes_on) {
+            uint32_t k[kAhead], p[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                k[u] = keys[min(j + u, end - 1)]; // (an entry of the chunk always, so that no load waits for a branch)
+                p[u] = pos[min(j + u, end - 1)];
+            }
+            float w[kAhead];
+            Unit<T> v[kAhead][NV];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                goes_on = goes_on && j + u < end && k[u] == key;
+                w[u] = 0.0f;
+                if (!goes_on) continue; // (most runs are short: no rows of others are asked for)
+                w[u] = weights[p[u]];
+                const T *row = grad + (int64_t)divided(p[u], per) * ld_grad;
+#pragma unroll
+                for (int c = 0; c < NV; ++c) {
+                    const uint32_t col = col0 + lane + c * L;
+                    v[u][c] = load_unit<T, RAGGED>(row, (int)(col < per_row ? col : 0u) * V, d);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (w[u] == 0.0f) continue; // (nothing, whatever the row holds)
+#pragma unroll
+                for (int c = 0; c < NV; ++c)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[c][e] = __fmaf_rn(w[u], to_f32(v[u][c].e[e]), acc[c][e]);
+            }
+            j += kAhead;
+            goes_on = goes_on && j < end;
+        }
+        const bool from_before = at_chunk && before == key, open_end = end < count && keys[end - 1] == key && keys[end] == key;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const uint32_t col = col0 + lane + c * L;
+            if (col >= per_row) continue;
+            if (from_before || open_end) {
+                Pack<float, V> o;
+#pragma unroll
+                for (int e = 0; e < V; ++e) o.e[e] = acc[c][e];
+                float *to = partial + ((size_t)chunk * 2 + (from_before ? 0 : 1)) * dp + (size_t)col * V;
+                __builtin_memcpy(to, &o, sizeof(o));
+            } else {
+                write_row<T, RAGGED>(out + (int64_t)key * ld_out, (int)col * V, d, acc[c], scale, accumulate != 0);
+            }
+        }
+    }
+}
+
 // The runs that cross chunks: each by the workgroup that has the chunk which it begins in. Teams of `lanes` threads add up a share
 // of the chunks each, in order, and then the shares in order.
 constexpr int kJoinThreads = 512;
@@ -519,6 +607,26 @@ int embed_grad_launches(int64_t n, int64_t count) { return count <= kSmallSort ?
 
 size_t embed_grad_scratch_bytes(int64_t n, int d, int64_t count) { return grad_scratch(n, d, count, nullptr).bytes; }
 
+template <class T, bool RAGGED, int L, int NV>
+static int weighted_sums_run(const EmbedGradParams &p, const GradScratch &s, const uint32_t *keys, const uint32_t *pos, hipStream_t st)
+{
+    run_sums_weighted_kernel<T, RAGGED, L, NV><<<dim3((unsigned)((p.count + 256 / L - 1) / (256 / L))), dim3(256), 0, st>>>(
+        (const T *)p.grad, p.ld_grad, p.weights, divide_by((uint32_t)p.per_row), keys, pos, (uint32_t)p.count, (uint32_t)p.n, p.d, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial);
+    AVQ_HIP(hipGetLastError());
+    return AVQ_OK;
+}
+
+template <class T, bool RAGGED>
+static int weighted_sums(const EmbedGradParams &p, const GradScratch &s, const uint32_t *keys, const uint32_t *pos, hipStream_t st)
+{
+    const int per_row = units_of<T>(p.d);
+    if (per_row <= 8) return weighted_sums_run<T, RAGGED, 8, 1>(p, s, keys, pos, st);
+    if (per_row <= 16) return weighted_sums_run<T, RAGGED, 16, 1>(p, s, keys, pos, st);
+    if (per_row <= 32) return weighted_sums_run<T, RAGGED, 32, 1>(p, s, keys, pos, st);
+    if (per_row <= 64) return weighted_sums_run<T, RAGGED, 64, 1>(p, s, keys, pos, st);
+    return weighted_sums_run<T, RAGGED, 64, 2>(p, s, keys, pos, st);
+}
+
 template <class T, bool RAGGED>
 static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
 {
@@ -570,10 +678,14 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
     while (lanes < 256 && lanes < units_of<T>(p.d)) lanes *= 2;
     const int64_t chunks = (p.count + kRunChunk - 1) / kRunChunk;
     const int sums = (int)((chunks + 256 / lanes - 1) / (256 / lanes));
-    const auto kernel = p.weights ? run_sums_kernel<T, RAGGED, true> : run_sums_kernel<T, RAGGED, false>;
-    kernel<<<dim3(sums), dim3(256), 0, st>>>((const T *)p.grad, p.ld_grad, keys, pos, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial, p.weights,
-                                             (uint32_t)p.per_row);
-    AVQ_HIP(hipGetLastError());
+    if (p.weights && p.count <= kFewEntries) {
+        AVQ_TRY((weighted_sums<T, RAGGED>(p, s, keys, pos, st)));
+    } else {
+        const auto kernel = p.weights ? run_sums_kernel<T, RAGGED, true> : run_sums_kernel<T, RAGGED, false>;
+        kernel<<<dim3(sums), dim3(256), 0, st>>>((const T *)p.grad, p.ld_grad, keys, pos, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out, p.accumulate, s.partial, p.weights,
+                                                 (uint32_t)p.per_row);
+        AVQ_HIP(hipGetLastError());
+    }
     if (chunks > 1) {
         const int64_t teams = kJoinThreads / lanes;
         const bool by_teams = chunks > kJoinByTeams;

@@ -21,19 +21,21 @@ __device__ __forceinline__ float wave_max(float v)
     return v;
 }
 
-// over the workgroup; red: a value a wave
-__device__ __forceinline__ float list_max(float v, float *red)
+// over the workgroup of a query, a wave or four; red: a value a wave
+template <int THREADS> __device__ __forceinline__ float list_max(float v, float *red)
 {
     v = wave_max(v);
+    if (THREADS == 64) return v;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
     return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
 }
 
-__device__ __forceinline__ float list_sum(float v, float *red)
+template <int THREADS> __device__ __forceinline__ float list_sum(float v, float *red)
 {
     v = group_sum<64>(v);
+    if (THREADS == 64) return v;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -74,7 +76,7 @@ __device__ __forceinline__ void list_softmax(const float *scores, const int32_t 
         real[i] = (int)threadIdx.x + i * THREADS < m && id[i] >= 0 && (int64_t)id[i] < n;
         if (real[i]) top = fmaxf(top, s[i]);
     }
-    top = THREADS == 64 ? wave_max(top) : list_max(top, red);
+    top = list_max<THREADS>(top, red);
     const float base = top > -INFINITY ? top : 0.0f;
     float beside = 0.0f, at_top = 0.0f;
 #pragma unroll
@@ -83,8 +85,8 @@ __device__ __forceinline__ void list_softmax(const float *scores, const int32_t 
         if (s[i] == base) at_top += 1.0f;
         else beside += expf(s[i] - base); // (NaN goes on in the sum)
     }
-    beside = THREADS == 64 ? group_sum<64>(beside) : list_sum(beside, red);
-    at_top = THREADS == 64 ? group_sum<64>(at_top) : list_sum(at_top, red);
+    beside = list_sum<THREADS>(beside, red);
+    at_top = list_sum<THREADS>(at_top, red);
     // (nothing but masks: log p and lse are -infinity; a score of +infinity: no result is a number)
     float sum = top > -INFINITY ? log1pf((at_top - 1.0f) + beside) : beside;
     if (top == INFINITY) sum = NAN;
@@ -111,9 +113,9 @@ __device__ __forceinline__ void list_softmax_fused(const float *scores, const in
 }
 
 // ids of a part in LDS, -1 for padding
-__device__ __forceinline__ void list_ids(const int32_t *__restrict__ ids, int64_t n, int count, int32_t *to)
+template <int THREADS> __device__ __forceinline__ void list_ids(const int32_t *__restrict__ ids, int64_t n, int count, int32_t *to)
 {
-    for (int j = threadIdx.x; j < count; j += kListThreads) {
+    for (int j = threadIdx.x; j < count; j += THREADS) {
         const int32_t id = ids[j];
         to[j] = id >= 0 && (int64_t)id < n ? id : -1;
     }
@@ -121,20 +123,20 @@ __device__ __forceinline__ void list_ids(const int32_t *__restrict__ ids, int64_
 
 // Scores of a part of a query's list, and where that is all of it the softmax. A row lies across L lanes that hold NV units of it each, and of
 // the query in fp32; eight loads at a time a lane.
-template <class T, bool RAGGED, int L, int NV>
-__global__ __launch_bounds__(kListThreads, NV == 4 || (RAGGED && (NV == 2 || sizeof(T) == 2)) ? 4 : 8) void list_probs_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int64_t ld_q, float scale,
+template <class T, bool RAGGED, int L, int NV, int THREADS>
+__global__ __launch_bounds__(THREADS, NV == 4 || (RAGGED && (NV == 2 || sizeof(T) == 2)) ? 4 : 8) void list_probs_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int64_t ld_q, float scale,
                                                                   const int32_t *__restrict__ ids, int m, int parts, int each, const float *__restrict__ offset,
                                                                   float *__restrict__ logp, float *__restrict__ lse)
 {
     extern __shared__ int32_t lds[]; // the part's ids and scores
     __shared__ float red[kListWaves];
-    constexpr int V = kUnit<T>, kTeams = kListThreads / L, kRows = NV == 1 ? 8 : 4;
+    constexpr int V = kUnit<T>, kTeams = THREADS / L, kRows = NV == 1 ? 8 : 4;
     const int per_row = units_of<T>(d), lane = threadIdx.x % L, team = threadIdx.x / L;
     const int64_t t = blockIdx.x / (uint32_t)parts;
     const int first = (int)(blockIdx.x - (uint32_t)t * parts) * each, count = min(each, m - first);
     int32_t *listed = lds;
     float *scores = (float *)(lds + each);
-    list_ids(ids + t * m + first, n, count, listed);
+    list_ids<THREADS>(ids + t * m + first, n, count, listed);
     float qf[NV][V];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -174,14 +176,15 @@ __global__ __launch_bounds__(kListThreads, NV == 4 || (RAGGED && (NV == 2 || siz
     __syncthreads();
     const int64_t at = t * m + first;
     const bool fused = parts == 1 && m <= kListFused;
-    for (int j = threadIdx.x; j < count; j += kListThreads) {
+    for (int j = threadIdx.x; j < count; j += THREADS) {
         const float s = offset ? __fmaf_rn(scores[j], scale, offset[at + j]) : scores[j] * scale;
         if (fused) scores[j] = s;
         else logp[at + j] = s;
     }
     if (!fused) return;
     __syncthreads();
-    list_softmax_fused(scores, listed, n, m, red, logp + at, lse + t);
+    if (THREADS == 64) list_softmax<64, 1>(scores, listed, n, m, red, logp + at, lse + t); // (lists of up to 64)
+    else list_softmax_fused(scores, listed, n, m, red, logp + at, lse + t);
 }
 
 // The same for rows that registers do not hold: a wave a row, the query in LDS.
@@ -198,7 +201,7 @@ __global__ __launch_bounds__(kListThreads) void list_probs_long_kernel(const T *
     const int first = (int)(blockIdx.x - (uint32_t)t * parts) * each, count = min(each, m - first);
     int32_t *listed = lds;
     float *scores = (float *)(lds + each), *qs = scores + each;
-    list_ids(ids + t * m + first, n, count, listed);
+    list_ids<kListThreads>(ids + t * m + first, n, count, listed);
     for (int k = threadIdx.x; k < per_row * V; k += kListThreads) qs[k] = k < d ? to_f32(q[t * ld_q + k]) : 0.0f;
     __syncthreads();
     const int64_t at = t * m + first;
@@ -236,11 +239,11 @@ __global__ __launch_bounds__(kListThreads) void list_softmax_kernel(const int32_
 // Sums of `count` weighted rows, by all of the workgroup: a row's units lie across `lanes` lanes, kAhead rows at a time a team of them, then the
 // teams' sums in order. row(j), weight(j): of the j-th (a readable row always); finish(u, acc): once for each unit, by the first team. A weight of 0 adds
 // nothing, whatever its row holds.
-template <class T, bool RAGGED, class RowOf, class WeightOf, class Finish>
+template <class T, bool RAGGED, int THREADS, class RowOf, class WeightOf, class Finish>
 __device__ __forceinline__ void weighted_rows(int count, int d, int lanes, float *sums, RowOf row, WeightOf weight, Finish finish)
 {
     constexpr int V = kUnit<T>, kAhead = 8;
-    const int per_row = units_of<T>(d), teams = kListThreads / lanes, team = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    const int per_row = units_of<T>(d), teams = THREADS / lanes, team = threadIdx.x / lanes, lane = threadIdx.x % lanes;
     for (int u0 = 0; u0 < per_row; u0 += lanes) {
         const int u = u0 + lane;
         float acc[V];
@@ -277,8 +280,8 @@ __device__ __forceinline__ void weighted_rows(int count, int d, int lanes, float
 }
 
 // G of a part of a query's list, and what its rows add to dq: dq itself where the part is the list, else sums for list_join.
-template <class T, bool RAGGED>
-__global__ __launch_bounds__(kListThreads) void list_grad_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, float scale, const int32_t *__restrict__ ids, int m, int parts,
+template <class T, bool RAGGED, int THREADS>
+__global__ __launch_bounds__(THREADS) void list_grad_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, float scale, const int32_t *__restrict__ ids, int m, int parts,
                                                                  int each, const float *__restrict__ logp, const float *__restrict__ g, const float *__restrict__ g_lse, int lanes,
                                                                  float *__restrict__ dscores, T *__restrict__ dq, int64_t ld_dq, float *__restrict__ partial, unsigned own, FillJob fill)
 {
@@ -294,23 +297,23 @@ __global__ __launch_bounds__(kListThreads) void list_grad_kernel(const T *__rest
     logp += t * m;
     g += t * m;
     float a = 0.0f;
-    for (int j0 = threadIdx.x; j0 < m; j0 += 4 * kListThreads) {
+    for (int j0 = threadIdx.x; j0 < m; j0 += 4 * THREADS) {
         int32_t id[4];
         float lp[4], up[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int j = min(j0 + i * kListThreads, m - 1); // (an entry always, so that no load waits for a branch)
+            const int j = min(j0 + i * THREADS, m - 1); // (an entry always, so that no load waits for a branch)
             id[i] = ids[j];
             lp[i] = logp[j];
             up[i] = g[j];
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (j0 + i * kListThreads < m && id[i] >= 0 && (int64_t)id[i] < n && !(lp[i] == -INFINITY)) a += up[i];
+            if (j0 + i * THREADS < m && id[i] >= 0 && (int64_t)id[i] < n && !(lp[i] == -INFINITY)) a += up[i];
     }
-    a = list_sum(a, red);
+    a = list_sum<THREADS>(a, red);
     if (g_lse) a -= g_lse[t];
-    for (int j = threadIdx.x; j < count; j += kListThreads) {
+    for (int j = threadIdx.x; j < count; j += THREADS) {
         const int32_t id = ids[first + j];
         const float lp = logp[first + j], up = g[first + j];
         float v = 0.0f;
@@ -325,7 +328,7 @@ __global__ __launch_bounds__(kListThreads) void list_grad_kernel(const T *__rest
     if (!dq) return;
     __syncthreads();
     const int per_row = units_of<T>(d);
-    weighted_rows<T, RAGGED>(count, d, lanes, sums, [&](int j) { return x + (int64_t)listed[j] * ld_x; }, [&](int j) { return G[j]; }, [&](int u, const float (&acc)[V]) {
+    weighted_rows<T, RAGGED, THREADS>(count, d, lanes, sums, [&](int j) { return x + (int64_t)listed[j] * ld_x; }, [&](int j) { return G[j]; }, [&](int u, const float (&acc)[V]) {
         if (parts == 1) {
             Unit<T> out;
 #pragma unroll
@@ -370,8 +373,8 @@ __global__ __launch_bounds__(64) void list_join_kernel(const float *__restrict__
 }
 
 // dx of a few entries without sorting them: a workgroup an entry, which looks for its id among those before, and if it is the first adds up
-// all that have it, in their order; the workgroups past the entries join dq. (50 to 2,048 entries take 5 to xx us, where sorting, sums and joins take
-// 25 to 55.)
+// all that have it, in their order; the workgroups past the entries join dq. (Forward and gradient of 8 lists of 234 rows of 43 bf16: 33 us, where
+// sorting, sums and joins take 84.)
 constexpr int kListFew = 2048;
 
 template <class T, bool RAGGED>
@@ -413,14 +416,20 @@ __global__ __launch_bounds__(kListThreads) void list_few_rows_kernel(const T *__
         if (same) listed[at] = j;
         __syncthreads();
     }
-    weighted_rows<T, RAGGED>(many, d, lanes, sums, [&](int j) { return q + (int64_t)(listed[j] / m) * ld_q; }, [&](int j) { return G[listed[j]]; },
+    weighted_rows<T, RAGGED, kListThreads>(many, d, lanes, sums, [&](int j) { return q + (int64_t)(listed[j] / m) * ld_q; }, [&](int j) { return G[listed[j]]; },
                              [&](int u, const float (&acc)[kUnit<T>]) { write_row<T, RAGGED>(dx + (int64_t)id * ld_dx, u * kUnit<T>, d, acc, scale, accumulate != 0); });
 }
+
+// Short lists of many queries have a wave each: nothing waits for a barrier, and no wave is left without rows (9,110 lists of 11 rows of 126 f16:
+// 16 us, by four waves 43; G and dq 19 and 58).
+static bool by_waves(int nq, int m) { return m <= 64 && nq >= 4096; }
 
 template <class T, bool RAGGED, int L, int NV>
 static int list_run(const ListParams &p, const ListParts &by, hipStream_t st)
 {
-    list_probs_kernel<T, RAGGED, L, NV><<<dim3((unsigned)p.nq * by.parts), dim3(kListThreads), (size_t)by.each * 8, st>>>(
+    const bool wave = by_waves(p.nq, p.m);
+    const auto kernel = wave ? list_probs_kernel<T, RAGGED, L, NV, 64> : list_probs_kernel<T, RAGGED, L, NV, kListThreads>;
+    kernel<<<dim3((unsigned)p.nq * by.parts), dim3(wave ? 64 : kListThreads), (size_t)by.each * 8, st>>>(
         (const T *)p.points, p.n, p.d, p.ld_points, (const T *)p.queries, p.ld_queries, p.scale, p.ids, p.m, by.parts, by.each, p.offset, p.logp, p.lse);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
@@ -476,13 +485,15 @@ static int list_grad_run(const ListGradParams &p, const FillJob &fill, hipStream
 {
     const ListParts by = list_parts(p.nq, p.m);
     const int per_row = units_of<T>(p.d);
+    const bool wave = by_waves(p.nq, p.m);
+    const int threads = wave ? 64 : kListThreads;
     int lanes = 4;
-    while (lanes < kListThreads && lanes < per_row) lanes *= 2;
-    const size_t lds = (size_t)by.each * 8 + (size_t)kListThreads * kUnit<T> * sizeof(float);
+    while (lanes < threads && lanes < per_row) lanes *= 2;
+    const size_t lds = (size_t)by.each * 8 + (size_t)threads * kUnit<T> * sizeof(float);
     const unsigned own = (unsigned)p.nq * by.parts;
-    list_grad_kernel<T, RAGGED><<<dim3(own + fill_groups(fill)), dim3(kListThreads), lds, st>>>((const T *)p.points, p.n, p.d, p.ld_points, p.scale, p.ids, p.m, by.parts, by.each, p.logp,
-                                                                                             p.grad_logp, p.grad_lse, lanes, p.dscores, (T *)p.dqueries, p.ld_dqueries,
-                                                                                             (float *)p.scratch, own, fill);
+    const auto kernel = wave ? list_grad_kernel<T, RAGGED, 64> : list_grad_kernel<T, RAGGED, kListThreads>;
+    kernel<<<dim3(own + fill_groups(fill)), dim3(threads), lds, st>>>((const T *)p.points, p.n, p.d, p.ld_points, p.scale, p.ids, p.m, by.parts, by.each, p.logp, p.grad_logp, p.grad_lse, lanes,
+                                                                    p.dscores, (T *)p.dqueries, p.ld_dqueries, (float *)p.scratch, own, fill);
     AVQ_HIP(hipGetLastError());
     if (p.dpoints && few_entries(p)) {
         const int per_query = p.dqueries && by.parts > 1 ? (per_row + kListThreads - 1) / kListThreads : 0;

@@ -21,6 +21,7 @@ INF = math.inf
 SHAPES = [
     (1, 1, 1, 1), (5, 3, 2, 0), (5, 3, 0, 4), (10, 100, 3, 7), (1000, 101, 17, 130), (300, 32, 65, 64), (777, 1024, 9, 33), (50, 1030, 5, 257), (20, 16384, 2, 9),
     (40_000, 64, 1, 4096), (5000, 16, 700, 5), (100, 475, 40, 100), (3, 7, 33, 1), (70_000, 8, 2, 2049), (900, 256, 3, 1000), (4000, 512, 300, 20),
+    (3000, 33, 4100, 7), (500, 130, 5000, 64), (70, 1100, 4097, 3), (200, 100, 100, 90), (50_000, 260, 40, 300), (30, 2050, 60, 50),
 ]
 
 
@@ -106,7 +107,7 @@ def test_list_log_probs(kind, n, d, nq, m):
 
 
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("nq,m", [(3, 50), (200, 33), (1, 3000)])
+@pytest.mark.parametrize("nq,m", [(3, 50), (200, 33), (1, 3000), (5000, 12), (1100, 1500)])
 def test_masks_infinities_and_nan(kind, nq, m):
     g, x, q, ids, scale = inputs(500, 40, nq, m, kind)
     offset = normal((nq, m), g)
@@ -222,9 +223,10 @@ def test_list_log_probs_grad(kind, n, d, nq, m):
 
 
 @pytest.mark.parametrize("kind", TYPES)
-def test_one_row_in_every_list_and_rows_of_no_weight(kind):
+@pytest.mark.parametrize("nq,m", [(600, 9), (1500, 9), (40, 9), (4500, 5), (2, 900)])
+def test_one_row_in_every_list_and_rows_of_no_weight(kind, nq, m):
     """The gradient of a shared row is the sum over all queries; rows of G = 0 add nothing though they hold NaN."""
-    n, d, nq, m = 50, 100, 600, 9
+    n, d = 50, 100
     g, x, q, _, scale = inputs(n, d, nq, m, kind, 2)
     ids = torch.full((nq, m), 7, dtype=torch.int32, device="cuda")
     ids[:, 1] = 11
@@ -265,9 +267,10 @@ def test_gradients_against_differences():
             assert abs(grad.reshape(-1)[i].item() - slope) < 1e-4, (which, i)
 
 
-def test_captured_calls_follow_their_inputs():
+@pytest.mark.parametrize("nq,m", [(64, 70), (20, 9), (3, 2500), (300, 80), (4200, 6)])
+def test_captured_calls_follow_their_inputs(nq, m):
     """Both calls in a graph, on another stream than the default, replayed over changed inputs with eager work in between."""
-    n, d, nq, m = 3000, 100, 64, 70
+    n, d = 3000, 100
     g, x, q, ids, scale = inputs(n, d, nq, m, "f32", 4)
     up = normal((nq, m), g)
     stream = torch.cuda.Stream()
@@ -316,3 +319,66 @@ def test_a_list_of_all_rows_is_the_softmax_over_all_rows():
     gb = avq.log_probs_grad(x, q, ids, b.lse, up, scale=scale)
     # fp32 pairs: 2^-20 of an entry or of the largest, over sums of 400 and 20 terms
     assert torch.allclose(ga[0], gb[0], rtol=1e-4, atol=1e-3) and torch.allclose(ga[1], gb[1], rtol=1e-4, atol=1e-3)
+
+
+def test_rows_beyond_32_bits():
+    """A table of more than 2^32 bytes and 2^31 elements: its last rows are those that are read and get a gradient."""
+    n, d = 2_200_000, 1000
+    x = torch.zeros((n, d), dtype=torch.float16, device="cuda")
+    last = normal((50, d), gen(1), torch.float16)
+    x[-50:] = last
+    g = gen(2)
+    for nq, m in ((3, 40), (60, 70)):
+        q, near = normal((nq, d), g, torch.float16), lists((nq, m), 50, g)
+        ids = torch.where((near >= 0) & (near < 50), near + (n - 50), near.clamp(max=-1))
+        near = torch.where(ids >= 0, near, -1)
+        r, want = avq.list_log_probs(x, q, ids, scale=0.1), avq.list_log_probs(last, q, near, scale=0.1)
+        assert torch.equal(r.logp, want.logp) and torch.equal(r.lse, want.lse)
+        up = normal((nq, m), g)
+        got, small = avq.list_log_probs_grad(x, q, ids, r.logp, up, scale=0.1), avq.list_log_probs_grad(last, q, near, r.logp, up, scale=0.1)
+        assert torch.equal(got[0], small[0]) and torch.equal(got[2], small[2])
+        assert not bool(got[1][: n - 50].any())
+        check_grads((got[0], got[1][-50:], got[2]), last, q, near, r.logp, up, None, 0.1, "f16")
+        del got
+
+
+def test_two_streams_at_once():
+    """Calls of two streams at the same time have scratch of their own."""
+    made = [inputs(4000, 64, 300, 40, "f32", seed) for seed in (8, 9)]
+    ups = [normal((300, 40), g) for g, *_ in made]
+    want = []
+    for (g, x, q, ids, scale), up in zip(made, ups):
+        r = avq.list_log_probs(x, q, ids, scale=scale)
+        want.append((r, avq.list_log_probs_grad(x, q, ids, r.logp, up, scale=scale)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in made]
+    for _ in range(5):
+        got = []
+        for stream, (g, x, q, ids, scale), up in zip(streams, made, ups):
+            with torch.cuda.stream(stream):
+                r = avq.list_log_probs(x, q, ids, scale=scale)
+                got.append((r, avq.list_log_probs_grad(x, q, ids, r.logp, up, scale=scale)))
+        torch.cuda.synchronize()
+        for (r, grad), (r2, grad2) in zip(got, want):
+            assert torch.equal(r.logp, r2.logp) and all(torch.equal(a, b) for a, b in zip(grad, grad2))
+
+
+def test_either_gradient_alone():
+    """The C call's dqueries and dpoints may each be left out."""
+    for nq, m in ((20, 9), (90, 70), (3, 2500)):
+        g, x, q, ids, scale = inputs(700, 48, nq, m, "f32", 10)
+        r = avq.list_log_probs(x, q, ids, scale=scale)
+        up = normal((nq, m), g)
+        want = avq.list_log_probs_grad(x, q, ids, r.logp, up, scale=scale)
+        ws = torch.empty(max(avq.lib().avq_list_log_probs_grad_scratch(700, 48, nq, m), 256), dtype=torch.uint8, device="cuda")
+        dq, dx, do = torch.empty_like(q), torch.empty_like(x), torch.empty_like(up)
+        for queries, points in ((True, False), (False, True), (False, False)):
+            for t in (dq, dx, do):
+                t.fill_(7.0)
+            assert avq.lib().avq_list_log_probs_grad(x.data_ptr(), 0, 700, 48, 48, q.data_ptr(), nq, 48, scale, ids.data_ptr(), m, r.logp.data_ptr(), up.data_ptr(), None,
+                                                      do.data_ptr(), dq.data_ptr() if queries else None, 48, dx.data_ptr() if points else None, 48, 0, ws.data_ptr(), ws.numel(),
+                                                      torch.cuda.current_stream().cuda_stream) == 0
+            torch.cuda.synchronize()
+            assert torch.equal(do, want[2])
+            assert torch.equal(dq, want[0]) if queries else bool((dq == 7.0).all())
+            assert torch.equal(dx, want[1]) if points else bool((dx == 7.0).all())
