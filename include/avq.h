@@ -533,8 +533,8 @@ int avq_list_log_probs_grad(const void *points, int32_t type, int64_t n, int32_t
 /* ---- losses of log probabilities ----------------------------------------------
  * These take log probabilities as the calls above give them (fp32, contiguous) and give the gradient that those calls take as
  * grad_logp. They are formed in 64 bits and rounded once. Each *_grad call gives the loss too, so that a training
- * step needs no other; its gradients are those of the losses, times grad_loss. They need no scratch; what was said of
- * capture, repeated results and overlap holds here too.
+ * step needs no other; its gradients are those of the losses, times grad_loss. What was said of scratch,
+ * capture, repeated results and overlap holds here too; distillation needs no scratch.
  *
  * Distillation from a teacher's best rows: logp [rows][m] the student's log probabilities of them, teacher [rows][m] the
  * teacher's logits z (any type, ld_teacher >= m), P_j = e^(z_j / temperature - lse). With teacher_lse = NULL lse is that of the list, and
@@ -561,13 +561,14 @@ int avq_distill_loss_grad(const float *logp, const void *teacher, int32_t type, 
  * NULL: 0), reward_s = beta D_s (reward_out [2 pairs] or NULL), logit_p = reward_2p - reward_2p+1 - margin, and
  *   loss_p = -(1 - smoothing) log sigma(logit_p) - smoothing log sigma(-logit_p).
  * pairs: 0 .. 2^22; beta, margin finite; smoothing 0 .. 1. */
+int64_t avq_preference_loss_scratch(int64_t tokens, int32_t pairs);
 int avq_preference_loss(const float *logp, const float *ref, const uint8_t *mask, int64_t tokens, const int32_t *offsets,
                         int32_t pairs, double beta, double margin, double smoothing, int32_t average, float *loss_out,
-                        float *logit_out, float *reward_out, void *hip_stream);
+                        float *logit_out, float *reward_out, void *scratch, int64_t scratch_bytes, void *hip_stream);
 int avq_preference_loss_grad(const float *logp, const float *ref, const uint8_t *mask, int64_t tokens, const int32_t *offsets,
                              int32_t pairs, double beta, double margin, double smoothing, int32_t average,
                              const float *grad_loss, float *loss_out, float *logit_out, float *reward_out, float *grad_logp,
-                             void *hip_stream);
+                             void *scratch, int64_t scratch_bytes, void *hip_stream);
 
 /* A policy's clipped loss: per token, r = e^(logp - old), A its advantage ([tokens] where each != 0, else [sequences]),
  *   k = e^(ref - logp) - (ref - logp) - 1 (ref [tokens] or NULL: 0; needed where kl_weight is not 0),
@@ -575,14 +576,16 @@ int avq_preference_loss_grad(const float *logp, const float *ref, const uint8_t 
  * and per sequence the sum of l (loss_out) and of k (kl_out or NULL), and the share of its tokens that are
  * clipped, r > 1 + clip_high with A > 0 or r < 1 - clip_low with A < 0 (clipped_out or NULL); those have the gradient of
  * kl_weight k alone. sequences: 0 .. 2^23; clip_low 0 .. 1, clip_high and kl_weight finite, >= 0. */
+int64_t avq_policy_loss_scratch(int64_t tokens, int32_t sequences);
 int avq_policy_loss(const float *logp, const float *old, const float *ref, const float *advantage, int32_t each,
                     const uint8_t *mask, int64_t tokens, const int32_t *offsets, int32_t sequences, double clip_low,
                     double clip_high, double kl_weight, int32_t average, float *loss_out, float *kl_out, float *clipped_out,
-                    void *hip_stream);
+                    void *scratch, int64_t scratch_bytes, void *hip_stream);
 int avq_policy_loss_grad(const float *logp, const float *old, const float *ref, const float *advantage, int32_t each,
                          const uint8_t *mask, int64_t tokens, const int32_t *offsets, int32_t sequences, double clip_low,
                          double clip_high, double kl_weight, int32_t average, const float *grad_loss, float *loss_out,
-                         float *kl_out, float *clipped_out, float *grad_logp, void *hip_stream);
+                         float *kl_out, float *clipped_out, float *grad_logp, void *scratch, int64_t scratch_bytes,
+                         void *hip_stream);
 
 const char *avq_last_error(void);
 const char *avq_version(void);

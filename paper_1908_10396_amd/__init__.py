@@ -29,7 +29,7 @@ SYMBOLS = [
     "avq_embed", "avq_embed_grad_scratch", "avq_embed_grad", "avq_layer_norm", "avq_layer_norm_grad_scratch", "avq_layer_norm_grad",
     "avq_log_probs_scratch", "avq_log_probs", "avq_log_probs_grad_scratch", "avq_log_probs_grad", "avq_index_log_probs",
     "avq_list_log_probs", "avq_list_log_probs_grad_scratch", "avq_list_log_probs_grad", "avq_distill_loss", "avq_distill_loss_grad",
-    "avq_preference_loss", "avq_preference_loss_grad", "avq_policy_loss", "avq_policy_loss_grad",
+    "avq_preference_loss_scratch", "avq_preference_loss", "avq_preference_loss_grad", "avq_policy_loss_scratch", "avq_policy_loss", "avq_policy_loss_grad",
 ]
 
 
@@ -108,12 +108,14 @@ def lib():
         L.avq_list_log_probs_grad.argtypes = [vp, i32, i64, i32, i64, vp, i32, i64, f32, vp, i32, vp, vp, vp, vp, vp, i64, vp, i64, i32, vp, i64, vp]
         L.avq_distill_loss.argtypes = [vp, vp, i32, i64, i32, i64, vp, f64, vp, vp]
         L.avq_distill_loss_grad.argtypes = [vp, vp, i32, i64, i32, i64, vp, f64, vp, vp, vp, vp]
-        L.avq_preference_loss.argtypes = [vp, vp, vp, i64, vp, i32, f64, f64, f64, i32, vp, vp, vp, vp]
-        L.avq_preference_loss_grad.argtypes = [vp, vp, vp, i64, vp, i32, f64, f64, f64, i32, vp, vp, vp, vp, vp, vp]
-        L.avq_policy_loss.argtypes = [vp, vp, vp, vp, i32, vp, i64, vp, i32, f64, f64, f64, i32, vp, vp, vp, vp]
-        L.avq_policy_loss_grad.argtypes = [vp, vp, vp, vp, i32, vp, i64, vp, i32, f64, f64, f64, i32, vp, vp, vp, vp, vp, vp]
+        L.avq_preference_loss_scratch.argtypes = [i64, i32]
+        L.avq_policy_loss_scratch.argtypes = [i64, i32]
+        L.avq_preference_loss.argtypes = [vp, vp, vp, i64, vp, i32, f64, f64, f64, i32, vp, vp, vp, vp, i64, vp]
+        L.avq_preference_loss_grad.argtypes = [vp, vp, vp, i64, vp, i32, f64, f64, f64, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.avq_policy_loss.argtypes = [vp, vp, vp, vp, i32, vp, i64, vp, i32, f64, f64, f64, i32, vp, vp, vp, vp, i64, vp]
+        L.avq_policy_loss_grad.argtypes = [vp, vp, vp, vp, i32, vp, i64, vp, i32, f64, f64, f64, i32, vp, vp, vp, vp, vp, vp, i64, vp]
         for name in ("avq_embed_grad_scratch", "avq_layer_norm_grad_scratch", "avq_log_probs_scratch", "avq_log_probs_grad_scratch",
-                     "avq_list_log_probs_grad_scratch"):
+                     "avq_list_log_probs_grad_scratch", "avq_preference_loss_scratch", "avq_policy_loss_scratch"):
             getattr(L, name).restype = i64
         L.avq_last_error.restype = C.c_char_p
         L.avq_version.restype = C.c_char_p

@@ -632,14 +632,16 @@ int launch_distill(const DistillParams &p, hipStream_t st);
 struct PreferenceParams { // ref, mask may be NULL; so may reward; grad_loss and grad_logp: both or neither
     const float *logp, *ref; const uint8_t *mask; int64_t tokens; const int32_t *offsets; int32_t pairs;
     double beta, margin, smoothing; int32_t average;
-    float *loss, *logit, *reward; const float *grad_loss; float *grad_logp;
+    float *loss, *logit, *reward; const float *grad_loss; float *grad_logp; void *scratch;
 };
+size_t preference_scratch_bytes(int64_t tokens, int pairs);
 int launch_preference(const PreferenceParams &p, hipStream_t st);
 struct PolicyParams { // ref, mask, kl, clipped may be NULL; grad_loss and grad_logp: both or neither
     const float *logp, *old, *ref, *advantage; int32_t each; const uint8_t *mask; int64_t tokens; const int32_t *offsets; int32_t sequences;
     double clip_low, clip_high, kl_weight; int32_t average;
-    float *loss, *kl, *clipped; const float *grad_loss; float *grad_logp;
+    float *loss, *kl, *clipped; const float *grad_loss; float *grad_logp; void *scratch;
 };
+size_t policy_scratch_bytes(int64_t tokens, int sequences);
 int launch_policy(const PolicyParams &p, hipStream_t st);
 
 } // namespace avq

@@ -9,7 +9,8 @@
 //   loss = -min(r A, clamp(r, 1 - lo, 1 + hi) A) + w k, d loss / d log p = -r A [not clipped] + w (1 - e^(log p_ref - log p)).
 //
 // All of it is formed in 64 bits and rounded once: where student and teacher, or policy and reference, agree, a loss is what is left of much
-// larger terms, and a sequence's sum may have tens of thousands of them. (A 64-bit multiply-add takes the time of a 32-bit one here.)
+// larger terms, and a sequence's sum may have tens of thousands of them. (A 64-bit multiply-add takes the time of 1.8 32-bit ones here: 2.2 and 1.26 ns
+// a wave and SIMD.)
 #include <math.h>
 
 #include "row_types.h"
@@ -317,182 +318,352 @@ inline unsigned sequence_groups(int64_t tokens, int64_t sequences) { return (uns
 constexpr int kRound = 4;
 inline int sequence_threads(int64_t tokens, int64_t sequences) { return tokens <= 64 * sequences ? 64 : tokens <= 256 * sequences ? 256 : 1024; }
 
-template <int B>
-__global__ __launch_bounds__(B) void preference_kernel(const float *__restrict__ logp, const float *__restrict__ ref, const uint8_t *__restrict__ mask, int tokens,
-                                                       const int32_t *__restrict__ offsets, int pairs, double beta, double margin, double smoothing, int average,
-                                                       float *__restrict__ loss, float *__restrict__ logit, float *__restrict__ reward, const float *__restrict__ g,
-                                                       float *__restrict__ out)
+// Few sequences of many tokens: each is taken in parts, 1,024 tokens or a thousand workgroups in all, whose sums a second launch joins. A call
+// takes 19 to 21 us that way, up to 1,048,576 tokens of one sequence; by one workgroup a sequence, policy takes 28 for 16,384 tokens and 1,740 for
+// 1,048,576, preferences 15, 61 (131,072) and 627. `least`: the tokens from which on that is worth the launch.
+constexpr int kPartThreads = 256, kPartTokens = 1024, kPartGroups = 1024, kPartSequences = 256;
+constexpr int64_t kPreferenceParts = 24576, kPolicyParts = 8192;
+inline int sequence_parts(int64_t tokens, int64_t sequences, int64_t least)
 {
-    __shared__ double red[B / 64 * 4];
-    if (out) clear_outside<B>(out, offsets, 2 * (int64_t)pairs, tokens);
-    const int64_t pair = blockIdx.x;
-    if (pair >= pairs) return;
-    const Span span[2] = {span_of(offsets, 2 * pair, tokens), span_of(offsets, 2 * pair + 1, tokens)};
-    const double up = out ? (double)g[pair] : 0.0;
-    double sums[4] = {0.0, 0.0, 0.0, 0.0}; // of either side, its tokens that count
-    const int middle = span[0].hi, hi = span[1].hi; // (the pair's tokens lie side by side)
+    if (sequences == 0 || sequences >= kPartSequences || tokens <= least) return 1;
+    return (int)std::min<int64_t>((tokens + kPartTokens - 1) / kPartTokens, kPartGroups / sequences);
+}
+__device__ __forceinline__ Span part_of(const Span &all, int part, int parts)
+{
+    const int64_t length = all.hi - all.lo;
+    return Span{all.lo + (int)(length * part / parts), all.lo + (int)(length * (part + 1) / parts)};
+}
+
+// The parts' sums of a sequence, joined by every workgroup of it in the same order.
+__device__ __forceinline__ void join_parts(const double *__restrict__ partial, int64_t sequence, int parts, double (&sums)[4], double *red)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[i] = 0.0;
+    for (int p = threadIdx.x; p < parts; p += kPartThreads)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[i] += partial[(sequence * parts + p) * 4 + i];
+    lanes_sum<kPartThreads>(sums, red);
+}
+__device__ __forceinline__ void store_part(double *__restrict__ partial, const double (&sums)[4])
+{
+    if (threadIdx.x == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) partial[blockIdx.x * (int64_t)4 + i] = sums[i];
+}
+
+static size_t parts_bytes(int64_t sequences, int parts) { return parts == 1 ? 0 : (size_t)sequences * parts * 4 * sizeof(double); }
+size_t preference_scratch_bytes(int64_t tokens, int pairs) { return parts_bytes(pairs, sequence_parts(tokens, pairs, kPreferenceParts)); }
+size_t policy_scratch_bytes(int64_t tokens, int sequences) { return parts_bytes(sequences, sequence_parts(tokens, sequences, kPolicyParts)); }
+
+// ---- preferences ---------------------------------------------------------------------------
+
+struct PreferenceArgs {
+    const float *logp, *ref; const uint8_t *mask; const int32_t *offsets; int tokens, pairs, average;
+    double beta, margin, smoothing;
+    float *loss, *logit, *reward; const float *g; float *out;
+};
+
+// Of the pair's tokens in [lo, hi), those before `middle` being the preferred answer's: sums of the ratios and counts of either side.
+template <int B> __device__ __forceinline__ void preference_sums(const PreferenceArgs &a, int lo, int middle, int hi, double (&sums)[4])
+{
     // (what is not given is read from logp all the same, and left out: no load waits for a branch)
-    const float *from_ref = ref ? ref : logp;
-    const uint8_t *from_mask = mask ? mask : (const uint8_t *)logp;
-    for (int i0 = span[0].lo + (int)threadIdx.x; i0 < hi; i0 += kRound * B) {
+    const float *ref = a.ref ? a.ref : a.logp;
+    const uint8_t *mask = a.mask ? a.mask : (const uint8_t *)a.logp;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[i] = 0.0;
+    for (int i0 = lo + (int)threadIdx.x; i0 < hi; i0 += kRound * B) {
         float v[kRound], r[kRound];
         uint8_t set[kRound];
 #pragma unroll
         for (int u = 0; u < kRound; ++u) {
             const uint32_t i = (uint32_t)min(i0 + u * B, hi - 1); // (a token of the pair always)
-            set[u] = from_mask[i];
-            v[u] = logp[i];
-            r[u] = from_ref[i];
+            set[u] = mask[i];
+            v[u] = a.logp[i];
+            r[u] = ref[i];
         }
 #pragma unroll
         for (int u = 0; u < kRound; ++u) {
             const int i = i0 + u * B;
-            const bool counts = (i < hi) & (set[u] != 0 || !mask);
-            const double add = counts ? (double)v[u] - (ref ? (double)r[u] : 0.0) : 0.0, one = counts ? 1.0 : 0.0;
+            const bool counts = (i < hi) & (set[u] != 0 || !a.mask);
+            const double add = counts ? (double)v[u] - (a.ref ? (double)r[u] : 0.0) : 0.0, one = counts ? 1.0 : 0.0;
             sums[0] += i < middle ? add : 0.0;
             sums[1] += i < middle ? one : 0.0;
             sums[2] += i < middle ? 0.0 : add;
             sums[3] += i < middle ? 0.0 : one;
         }
     }
-    lanes_sum<B>(sums, red);
-    const double share[2] = {average ? 1.0 / fmax(sums[1], 1.0) : 1.0, average ? 1.0 / fmax(sums[3], 1.0) : 1.0};
-    const double d[2] = {beta * sums[0] * share[0], beta * sums[2] * share[1]};
-    const double x = d[0] - d[1] - margin, small = x == x ? exp_wide(-fabs(x)) : x;
-    if (threadIdx.x == 0) {
+}
+
+// The pair's results (by whoever `writes`), and what its tokens in [lo, hi) get.
+template <int B> __device__ __forceinline__ void preference_finish(const PreferenceArgs &a, int64_t pair, const double (&sums)[4], bool writes, int lo, int middle, int hi)
+{
+    const double up = a.out ? (double)a.g[pair] : 0.0;
+    const double share[2] = {a.average ? 1.0 / fmax(sums[1], 1.0) : 1.0, a.average ? 1.0 / fmax(sums[3], 1.0) : 1.0};
+    const double d[2] = {a.beta * sums[0] * share[0], a.beta * sums[2] * share[1]};
+    const double x = d[0] - d[1] - a.margin, small = x == x ? exp_wide(-fabs(x)) : x;
+    if (writes && threadIdx.x == 0) {
         // -log sigma(x) = max(-x, 0) + log(1 + e^-|x|)
         const double more = log1p(small);
         double v = 0.0; // (a side of no weight counts for nothing, also where it is infinite)
-        if (smoothing < 1.0) v = (1.0 - smoothing) * (fmax(-x, 0.0) + more);
-        if (smoothing > 0.0) v = fma(smoothing, fmax(x, 0.0) + more, v);
-        loss[pair] = (float)v;
-        logit[pair] = (float)x;
-        if (reward) {
-            reward[2 * pair] = (float)d[0];
-            reward[2 * pair + 1] = (float)d[1];
+        if (a.smoothing < 1.0) v = (1.0 - a.smoothing) * (fmax(-x, 0.0) + more);
+        if (a.smoothing > 0.0) v = fma(a.smoothing, fmax(x, 0.0) + more, v);
+        a.loss[pair] = (float)v;
+        a.logit[pair] = (float)x;
+        if (a.reward) {
+            a.reward[2 * pair] = (float)d[0];
+            a.reward[2 * pair + 1] = (float)d[1];
         }
     }
-    if (!out) return;
+    if (!a.out) return;
     const double one = 1.0 / (1.0 + small), rest = small * one; // sigma(|x|), sigma(-|x|)
-    const double slope = up * beta * (x > 0.0 ? smoothing * one - (1.0 - smoothing) * rest : smoothing * rest - (1.0 - smoothing) * one);
+    const double slope = up * a.beta * (x > 0.0 ? a.smoothing * one - (1.0 - a.smoothing) * rest : a.smoothing * rest - (1.0 - a.smoothing) * one);
     const float to_first = (float)(slope * share[0]), to_second = (float)(-slope * share[1]);
-    for (int i = span[0].lo + (int)threadIdx.x; i < hi; i += B) {
+    for (int i = lo + (int)threadIdx.x; i < hi; i += B) {
         const float v = i < middle ? to_first : to_second;
-        out[i] = mask && !mask[i] ? 0.0f : v;
+        a.out[i] = a.mask && !a.mask[i] ? 0.0f : v;
     }
+}
+
+// (a pair's tokens lie side by side)
+struct Pair { Span all; int middle; };
+__device__ __forceinline__ Pair pair_of(const PreferenceArgs &a, int64_t pair)
+{
+    const Span first = span_of(a.offsets, 2 * pair, a.tokens), second = span_of(a.offsets, 2 * pair + 1, a.tokens);
+    return Pair{Span{first.lo, max(first.lo, second.hi)}, first.hi};
+}
+
+template <int B>
+__global__ __launch_bounds__(B) void preference_kernel(PreferenceArgs a)
+{
+    __shared__ double red[B / 64 * 4];
+    if (a.out) clear_outside<B>(a.out, a.offsets, 2 * (int64_t)a.pairs, a.tokens);
+    const int64_t pair = blockIdx.x;
+    if (pair >= a.pairs) return;
+    const Pair p = pair_of(a, pair);
+    double sums[4];
+    preference_sums<B>(a, p.all.lo, p.middle, p.all.hi, sums);
+    lanes_sum<B>(sums, red);
+    preference_finish<B>(a, pair, sums, true, p.all.lo, p.middle, p.all.hi);
+}
+
+__global__ __launch_bounds__(kPartThreads) void preference_parts_kernel(PreferenceArgs a, int parts, double *__restrict__ partial)
+{
+    __shared__ double red[kPartThreads / 64 * 4];
+    const Pair p = pair_of(a, blockIdx.x / (uint32_t)parts);
+    const Span mine = part_of(p.all, blockIdx.x % (uint32_t)parts, parts);
+    double sums[4];
+    preference_sums<kPartThreads>(a, mine.lo, p.middle, mine.hi, sums);
+    lanes_sum<kPartThreads>(sums, red);
+    store_part(partial, sums);
+}
+
+// A workgroup a part; without a gradient, a workgroup a pair.
+__global__ __launch_bounds__(kPartThreads) void preference_join_kernel(PreferenceArgs a, int parts, const double *__restrict__ partial)
+{
+    __shared__ double red[kPartThreads / 64 * 4];
+    const uint32_t each = a.out ? parts : 1;
+    if (a.out) clear_outside<kPartThreads>(a.out, a.offsets, 2 * (int64_t)a.pairs, a.tokens);
+    const int64_t pair = blockIdx.x / each;
+    if (pair >= a.pairs) return;
+    const int part = blockIdx.x % each;
+    const Pair p = pair_of(a, pair);
+    const Span mine = part_of(p.all, part, parts);
+    double sums[4];
+    join_parts(partial, pair, parts, sums, red);
+    preference_finish<kPartThreads>(a, pair, sums, part == 0, mine.lo, p.middle, mine.hi);
 }
 
 int launch_preference(const PreferenceParams &p, hipStream_t st)
 {
     if (p.pairs == 0 && !p.grad_logp) return AVQ_OK;
-    const int threads = sequence_threads(p.tokens, 4 * (int64_t)p.pairs);
-    const auto kernel = threads == 64 ? preference_kernel<64> : threads == 256 ? preference_kernel<256> : preference_kernel<1024>;
-    kernel<<<dim3(sequence_groups(p.grad_logp ? p.tokens : 0, p.pairs)), dim3(threads), 0, st>>>(p.logp, p.ref, p.mask, (int)p.tokens, p.offsets, p.pairs, p.beta, p.margin, p.smoothing, p.average, p.loss, p.logit, p.reward,
-                                                                 p.grad_loss, p.grad_logp);
+    const PreferenceArgs a{p.logp, p.ref, p.mask, p.offsets, (int)p.tokens, p.pairs, p.average, p.beta, p.margin, p.smoothing, p.loss, p.logit, p.reward, p.grad_loss, p.grad_logp};
+    const int parts = sequence_parts(p.tokens, p.pairs, kPreferenceParts);
+    const int64_t behind = p.grad_logp ? p.tokens : 0;
+    if (parts > 1) {
+        preference_parts_kernel<<<dim3((unsigned)p.pairs * parts), dim3(kPartThreads), 0, st>>>(a, parts, (double *)p.scratch);
+        AVQ_HIP(hipGetLastError());
+        preference_join_kernel<<<dim3(sequence_groups(behind, (int64_t)p.pairs * (p.grad_logp ? parts : 1))), dim3(kPartThreads), 0, st>>>(a, parts, (const double *)p.scratch);
+    } else {
+        const int threads = sequence_threads(p.tokens, 4 * (int64_t)p.pairs);
+        const auto kernel = threads == 64 ? preference_kernel<64> : threads == 256 ? preference_kernel<256> : preference_kernel<1024>;
+        kernel<<<dim3(sequence_groups(behind, p.pairs)), dim3(threads), 0, st>>>(a);
+    }
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }
 
+// ---- policy ----------------------------------------------------------------------------------
+
+struct PolicyArgs {
+    const float *logp, *old, *ref, *advantage; const uint8_t *mask; const int32_t *offsets; int each, tokens, sequences, average;
+    double least, most, weight;
+    float *loss, *kl, *clipped; const float *g; float *out;
+};
+
 // What one token adds: loss, k, whether it is clipped, and the slope of its loss.
 struct PolicyTerm { double loss, kl, over, slope; };
-__device__ __forceinline__ PolicyTerm policy_term(double logp, double old, double advantage, bool has_ref, double ref, double least, double most, double weight)
+__device__ __forceinline__ PolicyTerm policy_term(const PolicyArgs &a, double logp, double old, double advantage, double ref)
 {
     const double x = logp - old;
     const double r = x == x ? exp_wide(x) : x;
-    const bool over = (advantage > 0.0 && r > most) || (advantage < 0.0 && r < least);
-    const double held = over ? (advantage > 0.0 ? most : least) : r;
-    PolicyTerm t{-(held * advantage), 0.0, over ? 1.0 : 0.0, over ? 0.0 : -(r * advantage)};
-    if (has_ref) {
+    const bool over = (advantage > 0.0 && r > a.most) || (advantage < 0.0 && r < a.least);
+    const double held = over ? (advantage > 0.0 ? a.most : a.least) : r;
+    const bool none = advantage == 0.0; // (nothing, also of a ratio that is infinite)
+    PolicyTerm t{none ? 0.0 : -(held * advantage), 0.0, over ? 1.0 : 0.0, over || none ? 0.0 : -(r * advantage)};
+    if (none && x != x) t.loss = t.slope = x;
+    if (a.ref) {
         const double away = ref - logp;
         const NearOne e = exp_near_one(away);
         t.kl = away == away ? e.e2 : away;
-        t.loss = fma(weight, t.kl, t.loss);
-        t.slope = away == away ? fma(-weight, e.e1, t.slope) : away;
+        if (a.weight != 0.0) { // (no weight: nothing, also of a divergence that is infinite)
+            t.loss = fma(a.weight, t.kl, t.loss);
+            t.slope = away == away ? fma(-a.weight, e.e1, t.slope) : away;
+        }
     }
     return t;
 }
 
-template <int B>
-__global__ __launch_bounds__(B, 8) void policy_kernel(const float *__restrict__ logp, const float *__restrict__ old, const float *__restrict__ ref, const float *__restrict__ advantage,
-                                                   int each, const uint8_t *__restrict__ mask, int tokens, const int32_t *__restrict__ offsets, int sequences, double least,
-                                                   double most, double weight, int average, float *__restrict__ loss, float *__restrict__ kl, float *__restrict__ clipped,
-                                                   const float *__restrict__ g, float *__restrict__ out)
+// The terms of kRound tokens of sequence s from i0 on, in steps of B, for those before hi that count: fn(u, the term).
+template <int B, class Fn> __device__ __forceinline__ void policy_round(const PolicyArgs &a, int64_t s, int i0, int hi, Fn fn)
 {
-    __shared__ double red[B / 64 * 4];
-    if (out) clear_outside<B>(out, offsets, sequences, tokens);
-    const int64_t s = blockIdx.x;
-    if (s >= sequences) return;
-    const Span span = span_of(offsets, s, tokens);
-    double up = out ? (double)g[s] : 0.0;
     // (what is not given is read from logp all the same, and left out: no load waits for a branch)
-    const float *from_ref = ref ? ref : logp;
-    const uint8_t *from_mask = mask ? mask : (const uint8_t *)logp;
-    // the terms of kRound tokens from i0 on, in steps of B, for those that count: fn(u, the term)
-    auto round = [&](int i0, auto fn) __attribute__((always_inline)) {
-        float v[kRound], o[kRound], r[kRound], a[kRound];
-        uint8_t set[kRound];
+    const float *ref = a.ref ? a.ref : a.logp;
+    const uint8_t *mask = a.mask ? a.mask : (const uint8_t *)a.logp;
+    float v[kRound], o[kRound], r[kRound], adv[kRound];
+    uint8_t set[kRound];
 #pragma unroll
-        for (int u = 0; u < kRound; ++u) {
-            const uint32_t i = (uint32_t)min(i0 + u * B, span.hi - 1); // (a token of the sequence always)
-            set[u] = from_mask[i];
-            v[u] = logp[i];
-            o[u] = old[i];
-            r[u] = from_ref[i];
-            a[u] = advantage[each ? i : (uint32_t)s];
-        }
+    for (int u = 0; u < kRound; ++u) {
+        const uint32_t i = (uint32_t)min(i0 + u * B, hi - 1); // (a token of the sequence always)
+        set[u] = mask[i];
+        v[u] = a.logp[i];
+        o[u] = a.old[i];
+        r[u] = ref[i];
+        adv[u] = a.advantage[a.each ? i : (uint32_t)s];
+    }
 #pragma unroll
-        for (int u = 0; u < kRound; ++u)
-            if ((i0 + u * B < span.hi) & (set[u] != 0 || !mask)) fn(u, policy_term(v[u], o[u], a[u], ref != nullptr, r[u], least, most, weight));
-    };
-    // of the losses, of k, the clipped ones, those that count; the first round's slopes
-    double sums[4] = {0.0, 0.0, 0.0, 0.0}, slope[kRound] = {};
-    const int begin = span.lo + (int)threadIdx.x;
-    uint32_t counted = 0;
-    if (begin < span.hi)
-        round(begin, [&](int u, const PolicyTerm &t) __attribute__((always_inline)) {
+    for (int u = 0; u < kRound; ++u)
+        if ((i0 + u * B < hi) & (set[u] != 0 || !a.mask)) fn(u, policy_term(a, v[u], o[u], adv[u], r[u]));
+}
+
+// Sums over [lo, hi) of the losses, of k, of the clipped ones and of those that count; with the slopes of the first round, and which of it count.
+template <int B> __device__ __forceinline__ void policy_sums(const PolicyArgs &a, int64_t s, int lo, int hi, double (&sums)[4], double (&slope)[kRound], uint32_t *counted)
+{
+    const int begin = lo + (int)threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[i] = 0.0;
+#pragma unroll
+    for (int u = 0; u < kRound; ++u) slope[u] = 0.0;
+    uint32_t which = 0;
+    if (begin < hi)
+        policy_round<B>(a, s, begin, hi, [&](int u, const PolicyTerm &t) __attribute__((always_inline)) {
             sums[0] += t.loss;
             sums[1] += t.kl;
             sums[2] += t.over;
             sums[3] += 1.0;
             slope[u] = t.slope;
-            counted |= 1u << u;
+            which |= 1u << u;
         });
+    *counted = which;
 #pragma nounroll
-    for (int i0 = begin + kRound * B; i0 < span.hi; i0 += kRound * B)
-        round(i0, [&](int, const PolicyTerm &t) __attribute__((always_inline)) {
+    for (int i0 = begin + kRound * B; i0 < hi; i0 += kRound * B)
+        policy_round<B>(a, s, i0, hi, [&](int, const PolicyTerm &t) __attribute__((always_inline)) {
             sums[0] += t.loss;
             sums[1] += t.kl;
             sums[2] += t.over;
             sums[3] += 1.0;
         });
-    lanes_sum<B>(sums, red);
-    const double many = fmax(sums[3], 1.0), share = average ? 1.0 / many : 1.0;
-    if (threadIdx.x == 0) {
-        loss[s] = (float)(sums[0] * share);
-        if (kl) kl[s] = (float)(sums[1] * share);
-        if (clipped) clipped[s] = (float)(sums[2] / many);
+}
+
+// The sequence's results, and what the slopes are multiplied by.
+__device__ __forceinline__ double policy_finish(const PolicyArgs &a, int64_t s, const double (&sums)[4], bool writes)
+{
+    const double many = fmax(sums[3], 1.0), share = a.average ? 1.0 / many : 1.0;
+    if (writes && threadIdx.x == 0) {
+        a.loss[s] = (float)(sums[0] * share);
+        if (a.kl) a.kl[s] = (float)(sums[1] * share);
+        if (a.clipped) a.clipped[s] = (float)(sums[2] / many);
     }
-    if (!out) return;
-    up *= share;
-#pragma unroll
-    for (int u = 0; u < kRound; ++u)
-        if (begin + u * B < span.hi) out[begin + u * B] = counted >> u & 1u ? (float)(up * slope[u]) : 0.0f;
+    return a.out ? (double)a.g[s] * share : 0.0;
+}
+
+// The gradient of the tokens from `from` on, in rounds of B.
+template <int B> __device__ __forceinline__ void policy_slopes(const PolicyArgs &a, int64_t s, int from, int hi, double up)
+{
 #pragma nounroll
-    for (int i0 = begin + kRound * B; i0 < span.hi; i0 += kRound * B) {
+    for (int i0 = from + (int)threadIdx.x; i0 < hi; i0 += kRound * B) {
 #pragma unroll
         for (int u = 0; u < kRound; ++u)
-            if (i0 + u * B < span.hi) out[i0 + u * B] = 0.0f;
-        round(i0, [&](int u, const PolicyTerm &t) __attribute__((always_inline)) { out[i0 + u * B] = (float)(up * t.slope); });
+            if (i0 + u * B < hi) a.out[i0 + u * B] = 0.0f;
+        policy_round<B>(a, s, i0, hi, [&](int u, const PolicyTerm &t) __attribute__((always_inline)) { a.out[i0 + u * B] = (float)(up * t.slope); });
     }
+}
+
+template <int B>
+__global__ __launch_bounds__(B, 8) void policy_kernel(PolicyArgs a)
+{
+    __shared__ double red[B / 64 * 4];
+    if (a.out) clear_outside<B>(a.out, a.offsets, a.sequences, a.tokens);
+    const int64_t s = blockIdx.x;
+    if (s >= a.sequences) return;
+    const Span span = span_of(a.offsets, s, a.tokens);
+    double sums[4], slope[kRound];
+    uint32_t counted;
+    policy_sums<B>(a, s, span.lo, span.hi, sums, slope, &counted);
+    lanes_sum<B>(sums, red);
+    const double up = policy_finish(a, s, sums, true);
+    if (!a.out) return;
+    const int begin = span.lo + (int)threadIdx.x;
+#pragma unroll
+    for (int u = 0; u < kRound; ++u)
+        if (begin + u * B < span.hi) a.out[begin + u * B] = counted >> u & 1u ? (float)(up * slope[u]) : 0.0f;
+    policy_slopes<B>(a, s, span.lo + kRound * B, span.hi, up);
+}
+
+__global__ __launch_bounds__(kPartThreads, 8) void policy_parts_kernel(PolicyArgs a, int parts, double *__restrict__ partial)
+{
+    __shared__ double red[kPartThreads / 64 * 4];
+    const int64_t s = blockIdx.x / (uint32_t)parts;
+    const Span mine = part_of(span_of(a.offsets, s, a.tokens), blockIdx.x % (uint32_t)parts, parts);
+    double sums[4], slope[kRound];
+    uint32_t counted;
+    policy_sums<kPartThreads>(a, s, mine.lo, mine.hi, sums, slope, &counted);
+    lanes_sum<kPartThreads>(sums, red);
+    store_part(partial, sums);
+}
+
+// A workgroup a part; without a gradient, a workgroup a sequence.
+__global__ __launch_bounds__(kPartThreads, 8) void policy_join_kernel(PolicyArgs a, int parts, const double *__restrict__ partial)
+{
+    __shared__ double red[kPartThreads / 64 * 4];
+    const uint32_t each = a.out ? parts : 1;
+    if (a.out) clear_outside<kPartThreads>(a.out, a.offsets, a.sequences, a.tokens);
+    const int64_t s = blockIdx.x / each;
+    if (s >= a.sequences) return;
+    const int part = blockIdx.x % each;
+    double sums[4];
+    join_parts(partial, s, parts, sums, red);
+    const double up = policy_finish(a, s, sums, part == 0);
+    if (!a.out) return;
+    const Span mine = part_of(span_of(a.offsets, s, a.tokens), part, parts);
+    policy_slopes<kPartThreads>(a, s, mine.lo, mine.hi, up);
 }
 
 int launch_policy(const PolicyParams &p, hipStream_t st)
 {
     if (p.sequences == 0 && !p.grad_logp) return AVQ_OK;
-    const int threads = sequence_threads(p.tokens, p.sequences);
-    const auto kernel = threads == 64 ? policy_kernel<64> : threads == 256 ? policy_kernel<256> : policy_kernel<1024>;
-    kernel<<<dim3(sequence_groups(p.grad_logp ? p.tokens : 0, p.sequences)), dim3(threads), 0, st>>>(p.logp, p.old, p.ref, p.advantage, p.each, p.mask, (int)p.tokens, p.offsets, p.sequences, 1.0 - p.clip_low,
-                                                                     1.0 + p.clip_high, p.kl_weight, p.average, p.loss, p.kl, p.clipped, p.grad_loss, p.grad_logp);
+    const PolicyArgs a{p.logp, p.old, p.ref, p.advantage, p.mask, p.offsets, p.each, (int)p.tokens, p.sequences, p.average, 1.0 - p.clip_low, 1.0 + p.clip_high, p.kl_weight,
+                       p.loss, p.kl, p.clipped, p.grad_loss, p.grad_logp};
+    const int parts = sequence_parts(p.tokens, p.sequences, kPolicyParts);
+    const int64_t behind = p.grad_logp ? p.tokens : 0;
+    if (parts > 1) {
+        policy_parts_kernel<<<dim3((unsigned)p.sequences * parts), dim3(kPartThreads), 0, st>>>(a, parts, (double *)p.scratch);
+        AVQ_HIP(hipGetLastError());
+        policy_join_kernel<<<dim3(sequence_groups(behind, (int64_t)p.sequences * (p.grad_logp ? parts : 1))), dim3(kPartThreads), 0, st>>>(a, parts, (const double *)p.scratch);
+    } else {
+        const int threads = sequence_threads(p.tokens, p.sequences);
+        const auto kernel = threads == 64 ? policy_kernel<64> : threads == 256 ? policy_kernel<256> : policy_kernel<1024>;
+        kernel<<<dim3(sequence_groups(behind, p.sequences)), dim3(threads), 0, st>>>(a);
+    }
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;
 }

@@ -318,40 +318,56 @@ extern "C" int avq_distill_loss_grad(const float *logp, const void *teacher, int
     return launch_distill(p, (hipStream_t)hip_stream);
 }
 
-extern "C" int avq_preference_loss(const float *logp, const float *ref, const uint8_t *mask, int64_t tokens, const int32_t *offsets, int32_t pairs, double beta, double margin,
-                                   double smoothing, int32_t average, float *loss_out, float *logit_out, float *reward_out, void *hip_stream)
+extern "C" int64_t avq_preference_loss_scratch(int64_t tokens, int32_t pairs)
 {
-    const PreferenceParams p{logp, ref, mask, tokens, offsets, pairs, beta, margin, smoothing, average != 0, loss_out, logit_out, reward_out, nullptr, nullptr};
+    if (check_count(tokens) != AVQ_OK || pairs < 0 || pairs > kMaxSequences / 2) return refuse("tokens must be 0 .. 2^28 and pairs 0 .. 2^22");
+    return (int64_t)preference_scratch_bytes(tokens, pairs);
+}
+
+extern "C" int avq_preference_loss(const float *logp, const float *ref, const uint8_t *mask, int64_t tokens, const int32_t *offsets, int32_t pairs, double beta, double margin,
+                                   double smoothing, int32_t average, float *loss_out, float *logit_out, float *reward_out, void *scratch, int64_t scratch_bytes, void *hip_stream)
+{
+    const PreferenceParams p{logp, ref, mask, tokens, offsets, pairs, beta, margin, smoothing, average != 0, loss_out, logit_out, reward_out, nullptr, nullptr, scratch};
     AVQ_TRY(check_preference(p));
+    AVQ_TRY(check_scratch(scratch, scratch_bytes, preference_scratch_bytes(tokens, pairs)));
     return launch_preference(p, (hipStream_t)hip_stream);
 }
 
 extern "C" int avq_preference_loss_grad(const float *logp, const float *ref, const uint8_t *mask, int64_t tokens, const int32_t *offsets, int32_t pairs, double beta, double margin,
-                                        double smoothing, int32_t average, const float *grad_loss, float *loss_out, float *logit_out, float *reward_out, float *grad_logp, void *hip_stream)
+                                        double smoothing, int32_t average, const float *grad_loss, float *loss_out, float *logit_out, float *reward_out, float *grad_logp, void *scratch, int64_t scratch_bytes, void *hip_stream)
 {
-    const PreferenceParams p{logp, ref, mask, tokens, offsets, pairs, beta, margin, smoothing, average != 0, loss_out, logit_out, reward_out, grad_loss, grad_logp};
+    const PreferenceParams p{logp, ref, mask, tokens, offsets, pairs, beta, margin, smoothing, average != 0, loss_out, logit_out, reward_out, grad_loss, grad_logp, scratch};
     AVQ_TRY(check_preference(p));
     AVQ_TRY(check_upstream(grad_loss, grad_logp, pairs, tokens));
+    AVQ_TRY(check_scratch(scratch, scratch_bytes, preference_scratch_bytes(tokens, pairs)));
     return tokens == 0 && pairs == 0 ? AVQ_OK : launch_preference(p, (hipStream_t)hip_stream);
+}
+
+extern "C" int64_t avq_policy_loss_scratch(int64_t tokens, int32_t sequences)
+{
+    if (check_count(tokens) != AVQ_OK || sequences < 0 || sequences > kMaxSequences) return refuse("tokens must be 0 .. 2^28 and sequences 0 .. 2^23");
+    return (int64_t)policy_scratch_bytes(tokens, sequences);
 }
 
 extern "C" int avq_policy_loss(const float *logp, const float *old, const float *ref, const float *advantage, int32_t each, const uint8_t *mask, int64_t tokens,
                                const int32_t *offsets, int32_t sequences, double clip_low, double clip_high, double kl_weight, int32_t average, float *loss_out, float *kl_out,
-                               float *clipped_out, void *hip_stream)
+                               float *clipped_out, void *scratch, int64_t scratch_bytes, void *hip_stream)
 {
     const PolicyParams p{logp, old, ref, advantage, each != 0, mask, tokens, offsets, sequences, clip_low, clip_high, kl_weight, average != 0, loss_out, kl_out, clipped_out, nullptr,
-                         nullptr};
+                         nullptr, scratch};
     AVQ_TRY(check_policy(p));
+    AVQ_TRY(check_scratch(scratch, scratch_bytes, policy_scratch_bytes(tokens, sequences)));
     return launch_policy(p, (hipStream_t)hip_stream);
 }
 
 extern "C" int avq_policy_loss_grad(const float *logp, const float *old, const float *ref, const float *advantage, int32_t each, const uint8_t *mask, int64_t tokens,
                                     const int32_t *offsets, int32_t sequences, double clip_low, double clip_high, double kl_weight, int32_t average, const float *grad_loss,
-                                    float *loss_out, float *kl_out, float *clipped_out, float *grad_logp, void *hip_stream)
+                                    float *loss_out, float *kl_out, float *clipped_out, float *grad_logp, void *scratch, int64_t scratch_bytes, void *hip_stream)
 {
     const PolicyParams p{logp, old, ref, advantage, each != 0, mask, tokens, offsets, sequences, clip_low, clip_high, kl_weight, average != 0, loss_out, kl_out, clipped_out, grad_loss,
-                         grad_logp};
+                         grad_logp, scratch};
     AVQ_TRY(check_policy(p));
     AVQ_TRY(check_upstream(grad_loss, grad_logp, sequences, tokens));
+    AVQ_TRY(check_scratch(scratch, scratch_bytes, policy_scratch_bytes(tokens, sequences)));
     return tokens == 0 && sequences == 0 ? AVQ_OK : launch_policy(p, (hipStream_t)hip_stream);
 }

@@ -70,6 +70,15 @@ def _sequences(logp, offsets):
     return logp.numel(), offsets.numel() - 1
 
 
+def _part_sums(nbytes, like):
+    """(tensor, pointer, bytes) of the scratch that few long sequences need; most calls need none, and most of theirs is host time."""
+    if nbytes <= 0:
+        _check(nbytes)
+        return None, None, 0
+    t = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    return t, t.data_ptr(), nbytes
+
+
 def _preference(logp, offsets, grad_loss, ref, mask, beta, margin, smoothing, average, stream):
     tokens, sequences = _sequences(logp, offsets)
     if sequences % 2:
@@ -79,15 +88,16 @@ def _preference(logp, offsets, grad_loss, ref, mask, beta, margin, smoothing, av
     up = None if grad_loss is None else _vector(grad_loss, "grad_loss", pairs, _F32)
     _same_device(logp, offsets, ref, mask, grad_loss)
     with _on(logp, stream) as st:
+        ws, wp, wn = _part_sums(lib().avq_preference_loss_scratch(tokens, pairs), logp)
         # (a few microseconds are most of a small call: tensors made one by one take less than views of one)
         loss, logit, reward = logp.new_empty(pairs), logp.new_empty(pairs), logp.new_empty(sequences)
         args = (lp, rp, mp, tokens, offsets.data_ptr(), pairs, beta, margin, smoothing, 1 if average else 0)
         if up is None:
             grad = None
-            _check(lib().avq_preference_loss(*args, loss.data_ptr(), logit.data_ptr(), reward.data_ptr(), st))
+            _check(lib().avq_preference_loss(*args, loss.data_ptr(), logit.data_ptr(), reward.data_ptr(), wp, wn, st))
         else:
             grad = logp.new_empty(tokens)
-            _check(lib().avq_preference_loss_grad(*args, up, loss.data_ptr(), logit.data_ptr(), reward.data_ptr(), grad.data_ptr(), st))
+            _check(lib().avq_preference_loss_grad(*args, up, loss.data_ptr(), logit.data_ptr(), reward.data_ptr(), grad.data_ptr(), wp, wn, st))
     return grad, PreferenceLoss(loss, logit, reward)
 
 
@@ -117,14 +127,15 @@ def _policy(logp, old, advantage, offsets, grad_loss, ref, mask, clip, kl, avera
     up = None if grad_loss is None else _vector(grad_loss, "grad_loss", sequences, _F32)
     _same_device(logp, old, advantage, offsets, ref, mask, grad_loss)
     with _on(logp, stream) as st:
+        ws, wp, wn = _part_sums(lib().avq_policy_loss_scratch(tokens, sequences), logp)
         loss, kls, clipped = logp.new_empty(sequences), logp.new_empty(sequences), logp.new_empty(sequences)
         args = (lp, op, rp, ap, 1 if each else 0, mp, tokens, offsets.data_ptr(), sequences, low, high, kl, 1 if average else 0)
         if up is None:
             grad = None
-            _check(lib().avq_policy_loss(*args, loss.data_ptr(), kls.data_ptr(), clipped.data_ptr(), st))
+            _check(lib().avq_policy_loss(*args, loss.data_ptr(), kls.data_ptr(), clipped.data_ptr(), wp, wn, st))
         else:
             grad = logp.new_empty(tokens)
-            _check(lib().avq_policy_loss_grad(*args, up, loss.data_ptr(), kls.data_ptr(), clipped.data_ptr(), grad.data_ptr(), st))
+            _check(lib().avq_policy_loss_grad(*args, up, loss.data_ptr(), kls.data_ptr(), clipped.data_ptr(), grad.data_ptr(), wp, wn, st))
     return grad, PolicyLoss(loss, kls, clipped)
 
 

@@ -352,12 +352,13 @@ def list_log_probs_grad(points, queries, ids, logp, grad_logp, grad_lse=None, sc
         raise ValueError("accumulate needs out_points")
     _same_device(points, queries, ids, logp, grad_logp, grad_lse, out_points)
     with _on(points, stream) as st:
-        ws = _scratch(lib().avq_list_log_probs_grad_scratch(n, d, nq, m), points.device)
+        need = lib().avq_list_log_probs_grad_scratch(n, d, nq, m)
+        ws = None if need == 0 else _scratch(need, points.device)
         dq = torch.empty((nq, d), dtype=points.dtype, device=points.device)
         do = torch.empty((nq, m), dtype=f32, device=points.device)
         if out_points is None:
             out_points = torch.empty((n, d), dtype=points.dtype, device=points.device)
         op, lo = _matrix(out_points, "out_points")
         _check(lib().avq_list_log_probs_grad(pp, kind, n, d, lp, qp, nq, lq, scale, ids.data_ptr(), m, logpp, up, upl, do.data_ptr(), dq.data_ptr(), d,
-                                              op, lo, 1 if accumulate else 0, ws.data_ptr(), ws.numel(), st))
+                                              op, lo, 1 if accumulate else 0, _ptr(ws), 0 if ws is None else ws.numel(), st))
     return dq, out_points, do

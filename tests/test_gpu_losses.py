@@ -302,6 +302,23 @@ def test_policy(name, with_ref, with_mask, each, average):
     within(got, grad, e_grad, "gradient")
 
 
+def test_policy_far_apart():
+    """Ratios and divergences that are infinite count for nothing where they have no weight."""
+    logp = torch.tensor([-1.0, -1.0, -1.0, -2000.0, -INF, NAN], device="cuda")
+    old = torch.tensor([-2000.0, -2000.0, -2000.0, -1.0, -1.0, -1.0], device="cuda")
+    ref = torch.tensor([-1.0, -INF, -1.0, -1.0, -1.0, -1.0], device="cuda")
+    advantage = torch.tensor([0.0, 1.0, -1.0, 1.0, 1.0, 0.0], device="cuda")
+    offsets = torch.arange(7, dtype=torch.int32, device="cuda")
+    up = torch.ones(6, device="cuda")
+    grad, r = avq.policy_loss_grad(logp, old, advantage, offsets, up, ref=ref, clip=0.25)
+    assert r.loss[0] == 0 and grad[0] == 0                            # no advantage
+    assert r.loss[1] == -1.25 and grad[1] == 0 and r.kl[1] == INF     # clipped; the divergence has no weight here
+    assert r.loss[2] == INF and grad[2] == INF                        # a bad answer that has become certain
+    assert r.loss[3] == 0 and grad[3] == 0 and r.loss[4] == 0 and grad[4] == 0
+    assert bool(torch.isnan(r.loss[5])) and bool(torch.isnan(grad[5]))
+    assert r.clipped.tolist() == [0.0, 1.0, 0.0, 0.0, 0.0, 0.0]
+
+
 def test_token_gradients_against_differences():
     g, offsets, which, _, tokens = sequences("few", 2)
     logp = -normal((tokens,), g).abs()

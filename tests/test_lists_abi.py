@@ -92,10 +92,13 @@ LGRAD = dict(points=P, type=0, n=10, d=8, ld=8, queries=P, nq=3, ld_q=8, scale=1
              scratch=P, bytes=1 << 40, stream=None)
 DIST = dict(logp=P, teacher=P, type=0, rows=3, m=4, ld=4, lse=None, temperature=1.0, loss=P, stream=None)
 DGRAD = dict(logp=P, teacher=P, type=0, rows=3, m=4, ld=4, lse=None, temperature=1.0, up=P, loss=P, out=P, stream=None)
-PREF = dict(logp=P, ref=None, mask=None, tokens=9, offsets=P, pairs=1, beta=0.1, margin=0.0, smoothing=0.0, average=0, loss=P, logit=P, reward=None, stream=None)
-FGRAD = dict(logp=P, ref=None, mask=None, tokens=9, offsets=P, pairs=1, beta=0.1, margin=0.0, smoothing=0.0, average=0, up=P, loss=P, logit=P, reward=None, out=P, stream=None)
-POL = dict(logp=P, old=P, ref=None, adv=P, each=0, mask=None, tokens=9, offsets=P, sequences=2, low=0.2, high=0.2, kl=0.0, average=1, loss=P, kl_out=None, clipped=None, stream=None)
-OGRAD = dict(logp=P, old=P, ref=None, adv=P, each=0, mask=None, tokens=9, offsets=P, sequences=2, low=0.2, high=0.2, kl=0.0, average=1, up=P, loss=P, kl_out=None, clipped=None, out=P, stream=None)
+PREF = dict(logp=P, ref=None, mask=None, tokens=9, offsets=P, pairs=1, beta=0.1, margin=0.0, smoothing=0.0, average=0, loss=P, logit=P, reward=None, scratch=P, bytes=1 << 40, stream=None)
+FGRAD = dict(logp=P, ref=None, mask=None, tokens=9, offsets=P, pairs=1, beta=0.1, margin=0.0, smoothing=0.0, average=0, up=P, loss=P, logit=P, reward=None, out=P,
+             scratch=P, bytes=1 << 40, stream=None)
+POL = dict(logp=P, old=P, ref=None, adv=P, each=0, mask=None, tokens=9, offsets=P, sequences=2, low=0.2, high=0.2, kl=0.0, average=1, loss=P, kl_out=None, clipped=None, scratch=P,
+           bytes=1 << 40, stream=None)
+OGRAD = dict(logp=P, old=P, ref=None, adv=P, each=0, mask=None, tokens=9, offsets=P, sequences=2, low=0.2, high=0.2, kl=0.0, average=1, up=P, loss=P, kl_out=None, clipped=None, out=P,
+             scratch=P, bytes=1 << 40, stream=None)
 NAN, INF = float("nan"), float("inf")
 
 
@@ -126,6 +129,8 @@ NAN, INF = float("nan"), float("inf")
     ("avq_policy_loss", POL, dict(loss=None)), ("avq_policy_loss", POL, dict(kl=0.1)), ("avq_policy_loss", POL, dict(kl=-0.1)), ("avq_policy_loss", POL, dict(kl=NAN)),
     ("avq_policy_loss", POL, dict(low=-0.1)), ("avq_policy_loss", POL, dict(low=1.1)), ("avq_policy_loss", POL, dict(high=-0.1)), ("avq_policy_loss", POL, dict(high=INF)),
     ("avq_policy_loss", POL, dict(sequences=-1)), ("avq_policy_loss", POL, dict(sequences=(1 << 23) + 1)), ("avq_policy_loss", POL, dict(tokens=-5)),
+    ("avq_policy_loss", POL, dict(tokens=100_000, scratch=None)), ("avq_policy_loss_grad", OGRAD, dict(tokens=100_000, bytes=8)),
+    ("avq_preference_loss", PREF, dict(tokens=100_000, scratch=None)), ("avq_preference_loss_grad", FGRAD, dict(tokens=100_000, scratch=C.c_void_p(4100))),
     ("avq_policy_loss_grad", OGRAD, dict(up=None)), ("avq_policy_loss_grad", OGRAD, dict(out=None)), ("avq_policy_loss_grad", OGRAD, dict(kl=0.1)),
 ])
 def test_c_calls_refuse(name, base, change):
@@ -144,3 +149,8 @@ def test_scratch_sizes():
     assert L.avq_list_log_probs_grad_scratch(10, 0, 3, 4) == avq.AVQ_EINVAL
     assert L.avq_list_log_probs_grad_scratch(10, 8, 3, 4097) == avq.AVQ_EINVAL
     assert 0 < L.avq_list_log_probs_grad_scratch(670_091, 1024, 1024, 64) < 1 << 30
+    assert L.avq_preference_loss_scratch(-1, 1) == avq.AVQ_EINVAL
+    assert L.avq_preference_loss_scratch(1 << 28, 1 << 22) == 0 and L.avq_preference_loss_scratch(1000, 4) == 0
+    assert L.avq_policy_loss_scratch(10, -1) == avq.AVQ_EINVAL
+    assert 0 < L.avq_policy_loss_scratch(1 << 28, 1) < 1 << 20
+    assert 0 < L.avq_policy_loss_scratch(1 << 28, 255) < 1 << 20
