@@ -146,7 +146,8 @@ template <int L> __device__ __forceinline__ float lanes_max(float v, float *red)
 
 // ---- distillation ----------------------------------------------------------------------------
 
-// A row by L lanes, E elements a lane, L apart. ALL: the teacher's lse is that of all of its rows. GRAD: with the gradient.
+// A row by L lanes, E elements a lane, L apart. ALL: the teacher's lse is that of all of its rows. GRAD: with the gradient. Bound by vector instructions,
+// 70 an element of which 39 are in 64 bits: 8,191 rows of 1,000 fp32 20 us (65 MB, 3.2 TB/s), 65,536 of 64 bf16 with the gradient 16.
 template <int L> constexpr int kDistillThreads = L > 64 ? L : kLossThreads; // a row has a part of a wave, or a workgroup
 template <class T, bool ALL, bool GRAD, int L, int E>
 __global__ __launch_bounds__(kDistillThreads<L>) void distill_kernel(const float *__restrict__ logp, const T *__restrict__ teacher, int64_t ld_teacher,
