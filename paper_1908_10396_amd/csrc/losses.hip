@@ -250,7 +250,7 @@ static int distill_run(const DistillParams &p, hipStream_t st)
     constexpr int B = kDistillThreads<L>, kRows = B / L;
     const int64_t groups = (p.rows + kRows - 1) / kRows;
     const auto kernel = p.grad_logp ? distill_kernel<T, ALL, true, L, E> : distill_kernel<T, ALL, false, L, E>;
-    kernel<<<dim3((unsigned)std::min<int64_t>(groups, 1 << 20)), dim3(B), 0, st>>>(p.logp, (const T *)p.teacher, p.ld_teacher, p.teacher_lse, 1.0 / p.temperature, p.rows, p.m, p.loss,
+    kernel<<<dim3((unsigned)std::min<int64_t>(groups, 1 << 16)), dim3(B), 0, st>>>(p.logp, (const T *)p.teacher, p.ld_teacher, p.teacher_lse, 1.0 / p.temperature, p.rows, p.m, p.loss,
                                                                                 p.grad_loss, p.grad_logp);
     AVQ_HIP(hipGetLastError());
     return AVQ_OK;

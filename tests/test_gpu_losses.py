@@ -102,6 +102,20 @@ def test_distill(kind, rows, m, rest):
             within(g_got, grad, e_grad, "gradient")
 
 
+@pytest.mark.parametrize("rows,m", [(65_536 * 64 + 77, 5), (70_001, 1100)])
+@pytest.mark.parametrize("rest", [False, True])
+def test_distill_of_more_rows_than_workgroups(rows, m, rest):
+    g, logp, z, lse = distill_inputs(rows, m, "bf16", 1.0)
+    lse = lse if rest else None
+    up = normal((rows,), g)
+    got, l_got = avq.distill_loss_grad(logp, z, up, lse)
+    for at in (0, rows // 2, rows - 3000):  # (parts, for the memory of the 64-bit form)
+        part = slice(at, at + 3000)
+        loss, e_loss, grad, e_grad = distill_want(logp[part], z[part], None if lse is None else lse[part], 1.0, up[part])
+        within(l_got[part], loss, e_loss, "loss")
+        within(got[part], grad, e_grad, "gradient")
+
+
 def test_distill_where_student_and_teacher_agree():
     """The loss is what is left of terms a million times as large."""
     g = gen(1)
@@ -351,10 +365,12 @@ def test_offsets_that_leave_the_tokens_are_held_to_them():
     assert p.loss.tolist() == [-1.0, -1.0]
 
 
-def test_captured_losses_follow_their_inputs():
-    g, offsets, which, mask, tokens = sequences("tiles", 3)
+@pytest.mark.parametrize("name", ["tiles", "long", "few"])
+def test_captured_losses_follow_their_inputs(name):
+    g, offsets, which, mask, tokens = sequences(name, 3)
+    count = offsets.shape[0] - 1
     logp, old = -normal((tokens,), g).abs(), -normal((tokens,), g).abs()
-    advantage, up3, up6 = normal((tokens,), g), normal((3,), g), normal((6,), g)
+    advantage, up3, up6 = normal((tokens,), g), normal((count // 2,), g), normal((count,), g)
     z, student, up8 = normal((8, 77), g), torch.log_softmax(normal((8, 77), g), 1), normal((8,), g)
 
     def calls():
@@ -381,3 +397,35 @@ def test_captured_losses_follow_their_inputs():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, want))
+
+
+@pytest.mark.parametrize("name", ["ragged", "long"])
+def test_on_another_stream(name):
+    g, offsets, which, mask, tokens = sequences(name, 4)
+    count = offsets.shape[0] - 1
+    logp, old = -normal((tokens,), g).abs(), -normal((tokens,), g).abs()
+    z, student = normal((9, 70), g), torch.log_softmax(normal((9, 70), g), 1)
+    ups = [normal((n,), g) for n in (count // 2, count, 9)]
+
+    def calls(**how):
+        a = avq.preference_loss_grad(logp, offsets, ups[0], ref=old, mask=mask, **how)
+        b = avq.policy_loss_grad(logp, old, ups[1], offsets, ups[1], ref=old, mask=mask, kl=0.1, **how)
+        return [a[0], *a[1], b[0], *b[1], *avq.distill_loss_grad(student, z, ups[2], **how)]
+
+    want = calls()
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    got = calls(stream=stream)
+    stream.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_tokens_behind_the_last_sequence_are_zeros_however_many():
+    offsets = torch.tensor([70_000, 70_003, 70_005], dtype=torch.int32, device="cuda")
+    logp = -torch.ones(3_000_000, device="cuda")
+    up = torch.ones(1, device="cuda")
+    grad, r = avq.preference_loss_grad(logp, offsets, up, beta=1.0)
+    assert r.reward.tolist() == [-3.0, -2.0]
+    assert int((grad != 0).sum()) == 5 and bool((grad[70_000:70_005] != 0).all())
+    grad = avq.policy_loss_grad(logp, logp, torch.ones(2, device="cuda"), offsets, torch.ones(2, device="cuda"))[0]
+    assert int((grad != 0).sum()) == 5 and bool((grad[70_000:70_005] != 0).all())
