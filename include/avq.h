@@ -509,7 +509,8 @@ int avq_index_log_probs(avq_index *idx, const float *queries, int32_t nq, float 
 
 /* The softmax over a list of rows of each query's own (what a search returned, sampled rows, a teacher's best ones):
  * s_tj = scale * <q_t, x_i> + offset_tj with i = ids_tj; lse_out [nq] = log sum_j e^s_tj; logp_out [nq][m] = s_tj - lse_t.
- * offset: fp32 [nq][m] or NULL (0): minus the log of how likely a row was to be sampled, or -infinity for a mask.
+ * offset: fp32 [nq][m] or NULL (0): minus the log of how likely a row was to be sampled, or -infinity for a mask
+ * (whatever the row holds).
  * A padding id has no share and logp -infinity; so has an entry whose score is -infinity. A query with nothing else
  * has lse -infinity. A row that is listed twice counts twice. With a NaN or +infinity among the scores of rows no result of that
  * query is a number (padding keeps its -infinity). log p keeps its relative accuracy where p is nearly 1. All types are
@@ -543,7 +544,8 @@ int avq_list_log_probs_grad(const void *points, int32_t type, int64_t n, int32_t
  * teacher and student give to other rows counts as one answer more, R = max(0, 1 - sum_j P_j) and
  * r = max(1 - sum_j e^logp_j, 2^-20):  loss += R log(R / r). (fp32 log probabilities do not know r better than that.)
  * The gradient of logp_j is -P_j, + e^logp_j R / r where r is more than 2^-20. An entry with z = -infinity is padding: it
- * is left out whatever its logp is and has no gradient; a row of nothing else has loss 0. A student's
+ * is left out whatever its logp is and has no gradient; a row of nothing else has loss 0. Where the student gives
+ * nothing (logp = -infinity) to what the teacher gives something the loss is +infinity, its gradient -P all the same. A student's
  * temperature is a matter of its scale. rows: 0 .. 2^28, m: 0 .. 4096, temperature: 1e-6 .. 1e6. */
 int avq_distill_loss(const float *logp, const void *teacher, int32_t type, int64_t rows, int32_t m, int64_t ld_teacher,
                      const float *teacher_lse, double temperature, float *loss_out, void *hip_stream);

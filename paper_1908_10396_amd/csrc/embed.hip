@@ -372,8 +372,8 @@ __device__ __forceinline__ uint32_t divided(uint32_t i, const Divide &d) { retur
 
 // The weighted sums of few entries: a team of L lanes has an entry, and sums the part of a run that begins there, most have none to; the parts go where
 // those of run_sums_kernel do. NV units a lane. (6,160 entries of 98 f16: 12 us against 25; 262,144 of 100 fp32, which take many rounds of
-// mostly idle teams: 62 against 20.)
-constexpr int64_t kFewEntries = 16384;
+// mostly idle teams: 62 against 20. The whole gradient of 65,536 of 126 f16: 74 and 87; of 16,384 of 512 bf16 62 and 62, of 65,536 113 and 75.)
+constexpr int64_t kFewUnits = 1 << 20; // of 16 bytes, in the entries' rows
 
 template <class T, bool RAGGED, int L, int NV>
 __global__ __launch_bounds__(256) void run_sums_weighted_kernel(const T *__restrict__ grad, int64_t ld_grad, const float *__restrict__ weights, Divide per, const uint32_t *__restrict__ keys,
@@ -678,7 +678,7 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
     while (lanes < 256 && lanes < units_of<T>(p.d)) lanes *= 2;
     const int64_t chunks = (p.count + kRunChunk - 1) / kRunChunk;
     const int sums = (int)((chunks + 256 / lanes - 1) / (256 / lanes));
-    if (p.weights && p.count <= kFewEntries) {
+    if (p.weights && p.count * units_of<T>(p.d) <= kFewUnits) {
         AVQ_TRY((weighted_sums<T, RAGGED>(p, s, keys, pos, st)));
     } else {
         const auto kernel = p.weights ? run_sums_kernel<T, RAGGED, true> : run_sums_kernel<T, RAGGED, false>;

@@ -44,15 +44,16 @@ template <int THREADS> __device__ __forceinline__ float list_sum(float v, float 
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// A few queries with long lists: a workgroup takes a part of a query's list, so that there are a thousand of them. 64 entries at least, with
-// which every lane has a load or more in flight.
-constexpr int kListGroups = 1024, kListPart = 64;
+// A few queries with long lists: a workgroup takes a part of a query's list, so that there are a thousand of them, 32 entries at
+// least (2,986 rows of 813 fp32 for one query: 15 us, by 64 entries 25).
+constexpr int kListGroups = 1024, kListPart = 32;
+constexpr int kListWhole = 128; // a list that is not worth a second launch
 struct ListParts { int parts, each; };
 __host__ __device__ inline ListParts list_parts(int nq, int m)
 {
     const int most = (m + kListPart - 1) / kListPart, want = (kListGroups + nq - 1) / nq;
     const int parts = want < most ? want : most;
-    if (m <= 2 * kListPart || parts <= 1) return ListParts{1, m};
+    if (m <= kListWhole || parts <= 1) return ListParts{1, m};
     const int each = (m + parts - 1) / parts;
     return ListParts{(m + each - 1) / each, each};
 }
@@ -113,6 +114,9 @@ __device__ __forceinline__ void list_softmax_fused(const float *scores, const in
         list_softmax<kListThreads, 4>(scores, ids, n, m, red, logp, lse);
     }
 }
+
+// a mask is one whatever the row holds
+__device__ __forceinline__ float list_score(float product, float scale, float offset) { return offset == -INFINITY ? -INFINITY : __fmaf_rn(product, scale, offset); }
 
 // ids of a part in LDS, -1 for padding
 template <int THREADS> __device__ __forceinline__ void list_ids(const int32_t *__restrict__ ids, int64_t n, int count, int32_t *to)
@@ -179,7 +183,7 @@ __global__ __launch_bounds__(THREADS, NV == 4 || (RAGGED && (NV == 2 || sizeof(T
     const int64_t at = t * m + first;
     const bool fused = parts == 1 && m <= kListFused;
     for (int j = threadIdx.x; j < count; j += THREADS) {
-        const float s = offset ? __fmaf_rn(scores[j], scale, offset[at + j]) : scores[j] * scale;
+        const float s = offset ? list_score(scores[j], scale, offset[at + j]) : scores[j] * scale;
         if (fused) scores[j] = s;
         else logp[at + j] = s;
     }
@@ -219,7 +223,7 @@ __global__ __launch_bounds__(kListThreads) void list_probs_long_kernel(const T *
         }
         s = group_sum<64>(s);
         if (lane == 0) {
-            s = offset ? __fmaf_rn(s, scale, offset[at + j]) : s * scale;
+            s = offset ? list_score(s, scale, offset[at + j]) : s * scale;
             if (fused) scores[j] = s;
             else logp[at + j] = s;
         }
@@ -240,13 +244,13 @@ __global__ __launch_bounds__(kListThreads) void list_softmax_kernel(const int32_
 
 // Sums of `count` weighted rows, by all of the workgroup: a row's units lie across `lanes` lanes, kAhead rows at a time a team of them, then the
 // teams' sums in order. row(j), weight(j): of the j-th (a readable row always); finish(u, acc): once for each unit, by the first team. A weight of 0 adds
-// nothing, whatever its row holds.
+// nothing, whatever its row holds. Units [from, to) of the rows.
 template <class T, bool RAGGED, int THREADS, class RowOf, class WeightOf, class Finish>
-__device__ __forceinline__ void weighted_rows(int count, int d, int lanes, float *sums, RowOf row, WeightOf weight, Finish finish)
+__device__ __forceinline__ void weighted_rows(int count, int d, int from, int to, int lanes, float *sums, RowOf row, WeightOf weight, Finish finish)
 {
     constexpr int V = kUnit<T>, kAhead = 8;
-    const int per_row = units_of<T>(d), teams = THREADS / lanes, team = threadIdx.x / lanes, lane = threadIdx.x % lanes;
-    for (int u0 = 0; u0 < per_row; u0 += lanes) {
+    const int per_row = to, teams = THREADS / lanes, team = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    for (int u0 = from; u0 < per_row; u0 += lanes) {
         const int u = u0 + lane;
         float acc[V];
 #pragma unroll
@@ -330,7 +334,7 @@ __global__ __launch_bounds__(THREADS) void list_grad_kernel(const T *__restrict_
     if (!dq) return;
     __syncthreads();
     const int per_row = units_of<T>(d);
-    weighted_rows<T, RAGGED, THREADS>(count, d, lanes, sums, [&](int j) { return x + (int64_t)listed[j] * ld_x; }, [&](int j) { return G[j]; }, [&](int u, const float (&acc)[V]) {
+    weighted_rows<T, RAGGED, THREADS>(count, d, 0, per_row, lanes, sums, [&](int j) { return x + (int64_t)listed[j] * ld_x; }, [&](int j) { return G[j]; }, [&](int u, const float (&acc)[V]) {
         if (parts == 1) {
             Unit<T> out;
 #pragma unroll
@@ -345,65 +349,82 @@ __global__ __launch_bounds__(THREADS) void list_grad_kernel(const T *__restrict_
     });
 }
 
-// A unit of dq from its parts' sums, in order.
+// 64 units of dq of a query from its parts' sums, by all of the workgroup: its waves take the parts in turns, and their sums are added in order.
 template <class T, bool RAGGED>
-__device__ __forceinline__ void list_join(const float *__restrict__ partial, int64_t t, int u, int parts, int d, float scale, T *__restrict__ dq, int64_t ld_dq)
+__device__ __forceinline__ void list_join(const float *__restrict__ partial, int64_t t, int u0, int parts, int d, float scale, T *__restrict__ dq, int64_t ld_dq, float *sums)
 {
     constexpr int V = kUnit<T>;
-    const int per_row = units_of<T>(d);
-    if (u >= per_row) return;
+    const int per_row = units_of<T>(d), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, u = u0 + lane;
     float acc[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+    if (u < per_row) {
 #pragma unroll 8
-    for (int p = 0; p < parts; ++p) {
-        const Pack<float, V> v = *(const Pack<float, V> *)(partial + ((t * parts + p) * per_row + u) * V);
+        for (int p = wave; p < parts; p += kListWaves) {
+            const Pack<float, V> v = *(const Pack<float, V> *)(partial + ((t * parts + p) * per_row + u) * V);
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] += v.e[e];
+            for (int e = 0; e < V; ++e) acc[e] += v.e[e];
+        }
     }
+#pragma unroll
+    for (int e = 0; e < V; ++e) sums[threadIdx.x * V + e] = acc[e];
+    __syncthreads();
+    if (wave != 0 || u >= per_row) return;
     Unit<T> out;
 #pragma unroll
-    for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(acc[e] * scale);
+    for (int e = 0; e < V; ++e) {
+        for (int w = 1; w < kListWaves; ++w) acc[e] += sums[(w * 64 + lane) * V + e];
+        out.e[e] = from_f32<T>(acc[e] * scale);
+    }
     store_unit<T, RAGGED>(dq + t * ld_dq, u * V, d, out);
 }
 
-// a wave 64 units of a query
 template <class T, bool RAGGED>
-__global__ __launch_bounds__(64) void list_join_kernel(const float *__restrict__ partial, int parts, int d, float scale, T *__restrict__ dq, int64_t ld_dq)
+__global__ __launch_bounds__(kListThreads) void list_join_kernel(const float *__restrict__ partial, int parts, int d, float scale, T *__restrict__ dq, int64_t ld_dq)
 {
-    list_join<T, RAGGED>(partial, blockIdx.x, blockIdx.y * 64 + threadIdx.x, parts, d, scale, dq, ld_dq);
+    __shared__ float sums[kListThreads * kUnit<T>];
+    list_join<T, RAGGED>(partial, blockIdx.x, blockIdx.y * 64, parts, d, scale, dq, ld_dq, sums);
 }
 
-// dx of a few entries without sorting them: a workgroup an entry, which looks for its id among those before, and if it is the first adds up
-// all that have it, in their order; the workgroups past the entries join dq. (Forward and gradient of 8 lists of 234 rows of 43 bf16: 33 us, where
-// sorting, sums and joins take 84.)
-constexpr int kListFew = 2048;
+// dx of a few entries without sorting them: a workgroup an entry and 64 units of its row, which looks for its id among those before, and if it is the
+// first adds up all that have it, in their order; the workgroups past the entries join dq. (Forward and gradient of 8 lists of 234 rows of 43 bf16: 33
+// us, where sorting, sums and joins take 84.) Every workgroup reads all ids, so that their number is held to 4,096.
+constexpr int kListFew = 4096;
+__host__ __device__ constexpr int few_lanes(int per_row) { return per_row <= 4 ? 4 : per_row <= 8 ? 8 : per_row <= 16 ? 16 : per_row <= 32 ? 32 : 64; }
+static bool few_entries(int64_t count, int per_row) { return count > 0 && count * ((per_row + 63) / 64) <= kListFew; }
 
 template <class T, bool RAGGED>
 __global__ __launch_bounds__(kListThreads) void list_few_rows_kernel(const T *__restrict__ q, int64_t ld_q, int d, float scale, const int32_t *__restrict__ ids, int count, int m, int64_t n,
-                                                                     const float *__restrict__ G, int lanes, T *__restrict__ dx, int64_t ld_dx, int accumulate,
+                                                                     const float *__restrict__ G, int blocks, T *__restrict__ dx, int64_t ld_dx, int accumulate,
                                                                      const float *__restrict__ partial, int parts, int per_query, T *__restrict__ dq, int64_t ld_dq)
 {
     __shared__ float sums[kListThreads * kUnit<T>];
     __shared__ int listed[kListFew], found[kListWaves];
-    const int i = blockIdx.x;
-    if (i >= count) {
-        const int b = i - count;
-        list_join<T, RAGGED>(partial, b / per_query, b % per_query * kListThreads + threadIdx.x, parts, d, scale, dq, ld_dq);
+    if ((int)blockIdx.x >= count * blocks) {
+        const int b = blockIdx.x - count * blocks;
+        list_join<T, RAGGED>(partial, b / per_query, b % per_query * 64, parts, d, scale, dq, ld_dq, sums);
         return;
     }
+    const int i = blockIdx.x / (uint32_t)blocks, block = blockIdx.x % (uint32_t)blocks;
     const int32_t id = ids[i];
     if (id < 0 || (int64_t)id >= n) return;
-    int32_t v[kListFew / kListThreads];
+    constexpr int kEach = kListFew / kListThreads;
+    int32_t v[kEach];
 #pragma unroll
-    for (int k = 0; k < kListFew / kListThreads; ++k) v[k] = ids[min(k * kListThreads + (int)threadIdx.x, count - 1)]; // (an entry always: no load waits for a branch)
+    for (int k = 0; k < kEach; ++k) {
+        if (k * kListThreads >= count) break;
+        v[k] = ids[min(k * kListThreads + (int)threadIdx.x, count - 1)]; // (an entry always: no load waits for a branch)
+    }
     bool earlier = false;
 #pragma unroll
-    for (int k = 0; k < kListFew / kListThreads; ++k) earlier |= k * kListThreads + (int)threadIdx.x < i && v[k] == id;
+    for (int k = 0; k < kEach; ++k) {
+        if (k * kListThreads >= i) break;
+        earlier |= k * kListThreads + (int)threadIdx.x < i && v[k] == id;
+    }
     if (__syncthreads_or(earlier)) return;
     int many = 0;
 #pragma unroll
-    for (int k = 0; k < kListFew / kListThreads; ++k) {
+    for (int k = 0; k < kEach; ++k) {
         if (k * kListThreads >= count) break;
         const int j = k * kListThreads + threadIdx.x;
         const bool same = j < count && v[k] == id;
@@ -418,8 +439,11 @@ __global__ __launch_bounds__(kListThreads) void list_few_rows_kernel(const T *__
         if (same) listed[at] = j;
         __syncthreads();
     }
-    weighted_rows<T, RAGGED, kListThreads>(many, d, lanes, sums, [&](int j) { return q + (int64_t)(listed[j] / m) * ld_q; }, [&](int j) { return G[listed[j]]; },
-                             [&](int u, const float (&acc)[kUnit<T>]) { write_row<T, RAGGED>(dx + (int64_t)id * ld_dx, u * kUnit<T>, d, acc, scale, accumulate != 0); });
+    const int per_row = units_of<T>(d);
+    weighted_rows<T, RAGGED, kListThreads>(many, d, block * 64, min(per_row, block * 64 + 64), few_lanes(per_row), sums, [&](int j) { return q + (int64_t)(listed[j] / m) * ld_q; },
+                                           [&](int j) { return G[listed[j]]; }, [&](int u, const float (&acc)[kUnit<T>]) {
+        write_row<T, RAGGED>(dx + (int64_t)id * ld_dx, u * kUnit<T>, d, acc, scale, accumulate != 0);
+    });
 }
 
 // Short lists of many queries have a wave each: nothing waits for a barrier, and no wave is left without rows (9,110 lists of 11 rows of 126 f16:
@@ -480,7 +504,7 @@ static size_t list_partial_bytes(int d, int nq, int m)
     return by.parts == 1 ? 0 : ((size_t)nq * by.parts * ((d + 7) / 8 * 8) * sizeof(float) + 255) & ~(size_t)255;
 }
 
-static bool few_entries(const ListGradParams &p) { return p.nq > 0 && p.m > 0 && (int64_t)p.nq * p.m <= kListFew; }
+template <class T> static bool few_entries(const ListGradParams &p) { return few_entries((int64_t)p.nq * p.m, units_of<T>(p.d)); }
 
 template <class T, bool RAGGED>
 static int list_grad_run(const ListGradParams &p, const FillJob &fill, hipStream_t st)
@@ -497,14 +521,14 @@ static int list_grad_run(const ListGradParams &p, const FillJob &fill, hipStream
     kernel<<<dim3(own + fill_groups(fill)), dim3(threads), lds, st>>>((const T *)p.points, p.n, p.d, p.ld_points, p.scale, p.ids, p.m, by.parts, by.each, p.logp, p.grad_logp, p.grad_lse, lanes,
                                                                     p.dscores, (T *)p.dqueries, p.ld_dqueries, (float *)p.scratch, own, fill);
     AVQ_HIP(hipGetLastError());
-    if (p.dpoints && few_entries(p)) {
-        const int per_query = p.dqueries && by.parts > 1 ? (per_row + kListThreads - 1) / kListThreads : 0;
-        list_few_rows_kernel<T, RAGGED><<<dim3((unsigned)(p.nq * p.m + p.nq * per_query)), dim3(kListThreads), 0, st>>>(
-            (const T *)p.queries, p.ld_queries, p.d, p.scale, p.ids, p.nq * p.m, p.m, p.n, p.dscores, lanes, (T *)p.dpoints, p.ld_dpoints, p.accumulate, (const float *)p.scratch, by.parts,
+    if (p.dpoints && few_entries<T>(p)) {
+        const int blocks = (per_row + 63) / 64, per_query = p.dqueries && by.parts > 1 ? blocks : 0;
+        list_few_rows_kernel<T, RAGGED><<<dim3((unsigned)(p.nq * p.m * blocks + p.nq * per_query)), dim3(kListThreads), 0, st>>>(
+            (const T *)p.queries, p.ld_queries, p.d, p.scale, p.ids, p.nq * p.m, p.m, p.n, p.dscores, blocks, (T *)p.dpoints, p.ld_dpoints, p.accumulate, (const float *)p.scratch, by.parts,
             per_query, (T *)p.dqueries, p.ld_dqueries);
         AVQ_HIP(hipGetLastError());
     } else if (p.dqueries && by.parts > 1) {
-        list_join_kernel<T, RAGGED><<<dim3(p.nq, (per_row + 63) / 64), dim3(64), 0, st>>>((const float *)p.scratch, by.parts, p.d, p.scale, (T *)p.dqueries, p.ld_dqueries);
+        list_join_kernel<T, RAGGED><<<dim3(p.nq, (per_row + 63) / 64), dim3(kListThreads), 0, st>>>((const float *)p.scratch, by.parts, p.d, p.scale, (T *)p.dqueries, p.ld_dqueries);
         AVQ_HIP(hipGetLastError());
     }
     return AVQ_OK;
@@ -514,7 +538,7 @@ template <class T>
 static int list_grad_typed(const ListGradParams &p, const FillJob &fill, hipStream_t st)
 {
     const bool whole = whole_units(p.points, p.ld_points, p.d, sizeof(T)) && (!p.dqueries || whole_units(p.dqueries, p.ld_dqueries, p.d, sizeof(T))) &&
-                       (!p.dpoints || !few_entries(p) || (whole_units(p.queries, p.ld_queries, p.d, sizeof(T)) && whole_units(p.dpoints, p.ld_dpoints, p.d, sizeof(T))));
+                       (!p.dpoints || !few_entries<T>(p) || (whole_units(p.queries, p.ld_queries, p.d, sizeof(T)) && whole_units(p.dpoints, p.ld_dpoints, p.d, sizeof(T))));
     return whole ? list_grad_run<T, false>(p, fill, st) : list_grad_run<T, true>(p, fill, st);
 }
 
@@ -528,7 +552,8 @@ int launch_list_probs(const ListParams &p, hipStream_t st)
 size_t list_grad_scratch_bytes(int64_t n, int d, int nq, int m)
 {
     const int64_t count = (int64_t)nq * m;
-    return count == 0 ? 0 : list_partial_bytes(d, nq, m) + (count <= kListFew ? 0 : embed_grad_scratch_bytes(n, d, count));
+    // (fp32 rows have the most units: few entries of theirs are few of any type's)
+    return count == 0 ? 0 : list_partial_bytes(d, nq, m) + (few_entries(count, units_of<float>(d)) ? 0 : embed_grad_scratch_bytes(n, d, count));
 }
 
 int launch_list_grad(const ListGradParams &p, hipStream_t st)
@@ -536,7 +561,7 @@ int launch_list_grad(const ListGradParams &p, hipStream_t st)
     // the launch that forms dq clears a share of dx too, as those of the sort do, or all of it
     const int size = type_bytes(p.type);
     const int64_t count = (int64_t)p.nq * p.m;
-    const bool few = few_entries(p);
+    const bool few = p.type == AVQ_F32 ? few_entries<float>(p) : few_entries<bf16_t>(p);
     FillJob fill{(char *)p.dpoints, 0, 0, p.ld_dpoints * size, (int64_t)p.d * size};
     if (p.dpoints && !p.accumulate && count > 0) fill.hi = few ? p.n : p.n / (1 + embed_grad_launches(p.n, count));
     if (p.nq > 0) {

@@ -107,9 +107,9 @@ def test_list_log_probs(kind, n, d, nq, m):
 
 
 @pytest.mark.parametrize("kind", TYPES)
-@pytest.mark.parametrize("nq,m", [(3, 50), (200, 33), (1, 3000), (5000, 12), (1100, 1500)])
-def test_masks_infinities_and_nan(kind, nq, m):
-    g, x, q, ids, scale = inputs(500, 40, nq, m, kind)
+@pytest.mark.parametrize("nq,m,d", [(3, 50, 40), (200, 33, 40), (1, 3000, 40), (5000, 12, 40), (1100, 1500, 40), (6, 20, 4100)])
+def test_masks_infinities_and_nan(kind, nq, m, d):
+    g, x, q, ids, scale = inputs(500, d, nq, m, kind)
     offset = normal((nq, m), g)
     offset[:, ::3] = -INF
     offset[:, 1::7] = torch.finfo(torch.float32).min
@@ -125,6 +125,15 @@ def test_masks_infinities_and_nan(kind, nq, m):
     x2[500] = float("nan")
     r2 = avq.list_log_probs(x2[:500], q, ids, offset=bad, scale=scale)
     assert torch.equal(r.logp, r2.logp) and torch.equal(r.lse, r2.lse)
+    # nor do the rows that are masked
+    bad = x.clone()
+    bad[:100], bad[100:200] = float("nan"), INF
+    hidden = torch.where((ids >= 0) & (ids < 200), -INF, offset)
+    r2, want = avq.list_log_probs(bad, q, ids, offset=hidden, scale=scale), avq.list_log_probs(x, q, ids, offset=hidden, scale=scale)
+    assert torch.equal(r2.logp, want.logp) and torch.equal(r2.lse, want.lse)
+    up = normal((nq, m), g)
+    got, want = avq.list_log_probs_grad(bad, q, ids, r2.logp, up, scale=scale), avq.list_log_probs_grad(x, q, ids, r2.logp, up, scale=scale)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
     # +infinity or NaN among a query's scores: no number, and the other queries as before
     if nq > 2:
         for value in (INF, float("nan")):

@@ -111,8 +111,8 @@ NAN, INF = float("nan"), float("inf")
     ("avq_list_log_probs", LIST, dict(scale=NAN)), ("avq_list_log_probs", LIST, dict(points=ODD)), ("avq_list_log_probs", LIST, dict(d=16385, ld=20000, ld_q=20000)),
     ("avq_list_log_probs_grad", LGRAD, dict(logp=None)), ("avq_list_log_probs_grad", LGRAD, dict(up=None)), ("avq_list_log_probs_grad", LGRAD, dict(do=None)),
     ("avq_list_log_probs_grad", LGRAD, dict(ids=None)), ("avq_list_log_probs_grad", LGRAD, dict(ld_dq=7)), ("avq_list_log_probs_grad", LGRAD, dict(ld_dx=7)),
-    ("avq_list_log_probs_grad", LGRAD, dict(dx=ODD)), ("avq_list_log_probs_grad", LGRAD, dict(m=1000, scratch=None)), ("avq_list_log_probs_grad", LGRAD, dict(m=1000, bytes=64)),
-    ("avq_list_log_probs_grad", LGRAD, dict(m=1000, scratch=C.c_void_p(4100))),
+    ("avq_list_log_probs_grad", LGRAD, dict(dx=ODD)), ("avq_list_log_probs_grad", LGRAD, dict(m=4000, scratch=None)), ("avq_list_log_probs_grad", LGRAD, dict(m=4000, bytes=64)),
+    ("avq_list_log_probs_grad", LGRAD, dict(m=4000, scratch=C.c_void_p(4100))),
     ("avq_distill_loss", DIST, dict(logp=None)), ("avq_distill_loss", DIST, dict(teacher=None)), ("avq_distill_loss", DIST, dict(loss=None)), ("avq_distill_loss", DIST, dict(ld=3)),
     ("avq_distill_loss", DIST, dict(m=4097, ld=4097)), ("avq_distill_loss", DIST, dict(m=-1)), ("avq_distill_loss", DIST, dict(rows=-1)), ("avq_distill_loss", DIST, dict(type=7)),
     ("avq_distill_loss", DIST, dict(rows=(1 << 28) + 1)), ("avq_distill_loss", DIST, dict(temperature=0.0)), ("avq_distill_loss", DIST, dict(temperature=-1.0)),
@@ -145,7 +145,7 @@ def test_scratch_sizes():
     assert L.avq_list_log_probs_grad_scratch(10, 8, 0, 4) == 0
     assert L.avq_list_log_probs_grad_scratch(10, 8, 3, 0) == 0
     assert L.avq_list_log_probs_grad_scratch(10, 8, 3, 4) >= 0
-    assert L.avq_list_log_probs_grad_scratch(10, 8, 3, 1000) > 0
+    assert L.avq_list_log_probs_grad_scratch(10, 8, 3, 4000) > 0
     assert L.avq_list_log_probs_grad_scratch(10, 0, 3, 4) == avq.AVQ_EINVAL
     assert L.avq_list_log_probs_grad_scratch(10, 8, 3, 4097) == avq.AVQ_EINVAL
     assert 0 < L.avq_list_log_probs_grad_scratch(670_091, 1024, 1024, 64) < 1 << 30
