@@ -127,8 +127,33 @@ template <int THREADS> __device__ __forceinline__ void list_ids(const int32_t *_
     }
 }
 
+// acc + the inner product of two units. 16-bit elements two at a time, their products exact and two roundings at most a pair; subnormals are kept.
+__device__ __forceinline__ float unit_product(const Unit<float> &a, const Unit<float> &b, float acc)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __fmaf_rn(a.e[e], b.e[e], acc);
+    return acc;
+}
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+struct Pairs { uint32_t w[4]; };
+__device__ __forceinline__ float unit_product(const Unit<bf16_t> &a, const Unit<bf16_t> &b, float acc)
+{
+    const Pairs x = __builtin_bit_cast(Pairs, a), y = __builtin_bit_cast(Pairs, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x.w[e]), __builtin_bit_cast(bf16x2, y.w[e]), acc, false);
+    return acc;
+}
+__device__ __forceinline__ float unit_product(const Unit<f16_t> &a, const Unit<f16_t> &b, float acc)
+{
+    const Pairs x = __builtin_bit_cast(Pairs, a), y = __builtin_bit_cast(Pairs, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, x.w[e]), __builtin_bit_cast(f16x2, y.w[e]), acc, false);
+    return acc;
+}
+
 // Scores of a part of a query's list, and where that is all of it the softmax. A row lies across L lanes that hold NV units of it each, and of
-// the query in fp32; eight loads at a time a lane.
+// the query; eight loads at a time a lane.
 template <class T, bool RAGGED, int L, int NV, int THREADS>
 __global__ __launch_bounds__(THREADS, NV == 4 || (RAGGED && (NV == 2 || sizeof(T) == 2)) ? 4 : 8) void list_probs_kernel(const T *__restrict__ x, int64_t n, int d, int64_t ld_x, const T *__restrict__ q, int64_t ld_q, float scale,
                                                                   const int32_t *__restrict__ ids, int m, int parts, int each, const float *__restrict__ offset,
@@ -143,14 +168,12 @@ __global__ __launch_bounds__(THREADS, NV == 4 || (RAGGED && (NV == 2 || sizeof(T
     int32_t *listed = lds;
     float *scores = (float *)(lds + each);
     list_ids<THREADS>(ids + t * m + first, n, count, listed);
-    float qf[NV][V];
+    Unit<T> qv[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int u = lane + i * L;
-        Unit<T> v{};
-        if (u < per_row) v = load_unit<T, true>(q + t * ld_q, u * V, d);
-#pragma unroll
-        for (int e = 0; e < V; ++e) qf[i][e] = to_f32(v.e[e]);
+        qv[i] = Unit<T>{};
+        if (u < per_row) qv[i] = load_unit<T, true>(q + t * ld_q, u * V, d);
     }
     __syncthreads();
     for (int j0 = 0; j0 < count; j0 += kTeams * kRows) {
@@ -171,9 +194,7 @@ __global__ __launch_bounds__(THREADS, NV == 4 || (RAGGED && (NV == 2 || sizeof(T
             float s = 0.0f;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (NV * L > 1 && lane + i * L >= per_row) continue;
-#pragma unroll
-                for (int e = 0; e < V; ++e) s = __fmaf_rn(to_f32(v[r][i].e[e]), qf[i][e], s);
+                if (lane + i * L < per_row) s = unit_product(v[r][i], qv[i], s);
             }
             s = group_sum<L>(s);
             if (lane == 0 && j < count) scores[j] = s;
