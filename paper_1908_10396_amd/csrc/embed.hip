@@ -627,6 +627,10 @@ static int weighted_sums(const EmbedGradParams &p, const GradScratch &s, const u
     return weighted_sums_run<T, RAGGED, 64, 2>(p, s, keys, pos, st);
 }
 
+// Shares of the rows that the launches of a pass clear: placing takes longer by itself than counting, and hides more (2 and 3 against equal ones:
+// 50,001 ids into 1,183,514 x 100 fp32 126 us, 128.7; 1 and 2: 124, but 1,024 lists of 64 into 670,091 x 1,024 bf16 306 against 302).
+constexpr int kShareCount = 2, kSharePlace = 3;
+
 template <class T, bool RAGGED>
 static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
 {
@@ -644,18 +648,18 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
     // sums, which then have to pass over the rows with ids: 143 against 128 us for 50,001 ids of 1,183,514 x 100 fp32, 381 against 375
     // for 131,072 of 670,091 x 1,024 bf16.)
     const bool small = count <= (uint32_t)kSmallSort;
-    const int launches = small ? 1 : 2 * s.passes;
-    int launch = 0;
-    auto share = [&]() {
+    const int all = small ? 1 : s.passes * (kShareCount + kSharePlace);
+    int done = 0;
+    auto share = [&](int part) {
         FillJob f = fill;
-        f.lo = fill.lo + (fill.hi - fill.lo) * launch / launches;
-        f.hi = fill.lo + (fill.hi - fill.lo) * (launch + 1) / launches;
-        ++launch;
+        f.lo = fill.lo + (fill.hi - fill.lo) * done / all;
+        done += part;
+        f.hi = fill.lo + (fill.hi - fill.lo) * done / all;
         return f;
     };
     const uint32_t *keys = nullptr, *pos = nullptr;
     if (small) {
-        const FillJob f = share();
+        const FillJob f = share(1);
         sort_small_kernel<<<dim3(1 + fill_groups(f)), dim3(256), 0, st>>>(p.ids, count, n, s.keys[0], s.pos[0], f);
         AVQ_HIP(hipGetLastError());
         keys = s.keys[0];
@@ -664,7 +668,7 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
     for (int pass = 0; pass < (small ? 0 : s.passes); ++pass) {
         const int32_t *ids = pass == 0 ? p.ids : nullptr;
         const int to = pass & 1;
-        const FillJob f = share(), g = share();
+        const FillJob f = share(kShareCount), g = share(kSharePlace);
         sort_count_kernel<<<dim3(s.tiles + fill_groups(f)), dim3(kSortThreads), 0, st>>>(ids, keys, count, n, pass * s.bits, bins, s.hist, s.tiles, f);
         AVQ_HIP(hipGetLastError());
         sort_sums_kernel<<<dim3((bins + 63) / 64), dim3(64), 0, st>>>(s.hist, bins, s.tiles, s.totals);
