@@ -177,6 +177,39 @@ __global__ __launch_bounds__(64) void sort_sums_kernel(uint32_t *__restrict__ hi
     totals[b] = run;
 }
 
+// The same for more than kSumTiles tiles: a wave 64 digits and a quarter of 128 tiles at a time, whose counts are all asked for at once (128 tiles: 4.9 us
+// against 7.7; for 6 a thread a digit is faster, the gradient of 12,000 ids by 2 us).
+constexpr int kSumTiles = 32, kSumWaves = 4;
+__global__ __launch_bounds__(64 * kSumWaves) void sort_sums_many_kernel(uint32_t *__restrict__ hist, int bins, int tiles, uint32_t *__restrict__ totals)
+{
+    __shared__ uint32_t part[kSumWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = min((int)(blockIdx.x * 64) + lane, bins - 1); // (a digit always; of the last one's lanes all write the same)
+    uint32_t run = 0;
+    for (int t0 = 0; t0 < tiles; t0 += kSumWaves * kSumTiles) {
+        const int first = t0 + wave * kSumTiles;
+        uint32_t c[kSumTiles], sum = 0;
+#pragma unroll
+        for (int u = 0; u < kSumTiles; ++u) c[u] = first + u < tiles ? hist[(size_t)(first + u) * bins + b] : 0u;
+#pragma unroll
+        for (int u = 0; u < kSumTiles; ++u) sum += c[u];
+        part[wave][lane] = sum;
+        __syncthreads();
+        uint32_t at = run;
+#pragma unroll
+        for (int w = 0; w < kSumWaves; ++w) {
+            at += w < wave ? part[w][lane] : 0u;
+            run += part[w][lane];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kSumTiles; ++u) {
+            if (first + u < tiles) hist[(size_t)(first + u) * bins + b] = at;
+            at += c[u];
+        }
+    }
+    if (wave == 0) totals[b] = run;
+}
+
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t *__restrict__ ids, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos,
                                                                   uint32_t count, uint32_t n, int shift, int bits, const uint32_t *__restrict__ hist,
                                                                   const uint32_t *__restrict__ totals, int tiles, uint32_t *__restrict__ keys_out, uint32_t *__restrict__ pos_out,
@@ -671,7 +704,8 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
         const FillJob f = share(kShareCount), g = share(kSharePlace);
         sort_count_kernel<<<dim3(s.tiles + fill_groups(f)), dim3(kSortThreads), 0, st>>>(ids, keys, count, n, pass * s.bits, bins, s.hist, s.tiles, f);
         AVQ_HIP(hipGetLastError());
-        sort_sums_kernel<<<dim3((bins + 63) / 64), dim3(64), 0, st>>>(s.hist, bins, s.tiles, s.totals);
+        const bool many = s.tiles > kSumTiles;
+        (many ? sort_sums_many_kernel : sort_sums_kernel)<<<dim3((bins + 63) / 64), dim3(many ? 64 * kSumWaves : 64), 0, st>>>(s.hist, bins, s.tiles, s.totals);
         AVQ_HIP(hipGetLastError());
         sort_place_kernel<<<dim3(s.tiles + fill_groups(g)), dim3(kSortThreads), 0, st>>>(ids, keys, pos, count, n, pass * s.bits, s.bits, s.hist, s.totals, s.tiles, s.keys[to], s.pos[to], g);
         AVQ_HIP(hipGetLastError());
