@@ -5,7 +5,7 @@
 //
 // Bound by memory: the listed rows are gathered, once for the scores and once more for dq; dx writes the whole table, by the sorted sums of
 // the lookup's gradient (embed.hip) with G as weights. A workgroup a query: its scores stay in LDS between the products and the softmax. 2,047 lists of
-// 200 rows of 1,024 bf16: 64 us (0.75 GB gathered, 11.8 TB/s, 208 MB of it from beyond the L2); 2,048 of 127 rows of 100 fp32, with offsets: 23 for
+// 200 rows of 1,024 bf16: 64 us (0.75 GB gathered, 11.8 TB/s, 208 MB of it from beyond the L2; 34 with all of it there, 127 with next to nothing); 2,048 of 127 rows of 100 fp32, with offsets: 23 for
 // the scores, 161 for the gradient, of which zeros for 1,183,514 rows alone are 69.
 #include <math.h>
 
