@@ -561,18 +561,21 @@ __global__ __launch_bounds__(kJoinThreads) void run_joins_kernel(const uint32_t 
 }
 
 // The same, bit for bit, where the chunks are more than fit the device at once and most runs are short, as those of sampled lists are: a team has a chunk, and
-// adds a run of up to five chunks up by itself (262,144 entries of 100 fp32: 14 against 26 us; 50,001: 8 against 4).
+// adds a run of up to five chunks up by itself (262,144 entries of 100 fp32: 14 against 26 us; 50,001: 8 against 4). Longer runs are the workgroup's, one
+// after the other, so that a chunk has kJoinLanes threads at least, whatever a row needs (`wide` of them): with as many as a row of 32 bf16 needs, 128 chunks a
+// workgroup, the gradient of 140,001 ids of 823 rows took 72 us, with 16, 32 and 64 threads a chunk 43, 40 and 41.
 constexpr int64_t kJoinByTeams = 4096;
+constexpr int kJoinLanes = 32;
 
 template <class T, bool RAGGED>
-__global__ __launch_bounds__(kJoinThreads) void run_joins_teams_kernel(const uint32_t *__restrict__ keys, uint32_t count, uint32_t n, int d, int lanes, float scale, T *__restrict__ out,
-                                                                       int64_t ld_out, int accumulate, const float *__restrict__ partial)
+__global__ __launch_bounds__(kJoinThreads) void run_joins_teams_kernel(const uint32_t *__restrict__ keys, uint32_t count, uint32_t n, int d, int lanes, int wide, float scale,
+                                                                       T *__restrict__ out, int64_t ld_out, int accumulate, const float *__restrict__ partial)
 {
     constexpr int V = kUnit<T>;
     __shared__ float shares[kJoinThreads * V];
-    __shared__ uint32_t long_chunk[kJoinThreads / 4], long_last[kJoinThreads / 4], longs; // (teams have four lanes at least)
+    __shared__ uint32_t long_chunk[kJoinThreads / kJoinLanes], long_last[kJoinThreads / kJoinLanes], longs;
     const uint32_t chunks = (count + kRunChunk - 1) / kRunChunk, per_row = (uint32_t)units_of<T>(d), dp = per_row * V;
-    const uint32_t teams = kJoinThreads / (uint32_t)lanes, team = threadIdx.x / (uint32_t)lanes, lane = threadIdx.x % (uint32_t)lanes;
+    const uint32_t teams = kJoinThreads / (uint32_t)wide, team = threadIdx.x / (uint32_t)wide, lane = threadIdx.x % (uint32_t)wide;
     if (threadIdx.x == 0) longs = 0;
     __syncthreads();
     const uint32_t chunk = blockIdx.x * teams + team, last = chunk < chunks ? run_last(keys, chunk, chunks, count, n) : 0;
@@ -584,7 +587,7 @@ __global__ __launch_bounds__(kJoinThreads) void run_joins_teams_kernel(const uin
         }
     } else if (last != 0) {
         const uint32_t key = keys[chunk * (uint32_t)kRunChunk + (uint32_t)kRunChunk - 1];
-        for (uint32_t col = lane; col < per_row; col += (uint32_t)lanes) {
+        for (uint32_t col = lane; col < per_row; col += (uint32_t)wide) {
             float acc[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) acc[e] = partial[((size_t)chunk * 2 + 1) * dp + (size_t)col * V + e];
@@ -725,11 +728,14 @@ static int embed_grad_run(const EmbedGradParams &p, hipStream_t st)
         AVQ_HIP(hipGetLastError());
     }
     if (chunks > 1) {
-        const int64_t teams = kJoinThreads / lanes;
-        const bool by_teams = chunks > kJoinByTeams;
-        const auto joins = by_teams ? run_joins_teams_kernel<T, RAGGED> : run_joins_kernel<T, RAGGED>;
-        joins<<<dim3((unsigned)(by_teams ? (chunks + teams - 1) / teams : std::min(chunks, kJoinGroups))), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out,
-                                                                                                                                    p.ld_out, p.accumulate, s.partial);
+        if (chunks > kJoinByTeams) {
+            const int wide = std::max(lanes, kJoinLanes), teams = kJoinThreads / wide;
+            run_joins_teams_kernel<T, RAGGED><<<dim3((unsigned)((chunks + teams - 1) / teams)), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, wide, p.scale, (T *)p.out,
+                                                                                                                             p.ld_out, p.accumulate, s.partial);
+        } else {
+            run_joins_kernel<T, RAGGED><<<dim3((unsigned)std::min(chunks, kJoinGroups)), dim3(kJoinThreads), 0, st>>>(keys, count, n, p.d, lanes, p.scale, (T *)p.out, p.ld_out,
+                                                                                                                      p.accumulate, s.partial);
+        }
         AVQ_HIP(hipGetLastError());
     }
     return AVQ_OK;

@@ -644,3 +644,41 @@ def test_gradient_of_a_few_queries_whose_answer_is_nearly_certain(nq, n, d):
     dq, dx = avq.log_probs_grad(x, q, ids, r.lse + 0.5, up, scale=scale)
     G = up.double()[:, None] * (torch.nn.functional.one_hot(ids.long(), n).double() - p * math.exp(-0.5))
     assert float((dx.double() - G.t() @ qd * scale).norm() / (G.t() @ qd * scale).norm()) < 1e-4
+
+
+# ---- runs of many lengths among many ids ---------------------------------------------------------
+
+def runs_ids(count, n, g):
+    """`count` ids of n rows in random places: rows of some hundreds, of 33 to 150, of one and two entries; the last row has the last 400 places
+    of the order, which end inside a chunk of 32."""
+    r = torch.arange(n, device="cuda")
+    many = torch.where(r % 5 == 0, 150 + r * 37 % 700, torch.where(r % 5 < 3, 33 + r * 11 % 118, 1 + r % 2))
+    many[-1] = 400
+    ids = torch.repeat_interleave(r, many)
+    assert ids.numel() >= count
+    ids = ids[ids.numel() - count:]  # (the first rows of the order lose some)
+    return ids[torch.randperm(count, generator=g, device="cuda")].int()
+
+
+@pytest.mark.parametrize("kind,d", [("f32", 3), ("f32", 100), ("bf16", 33), ("f16", 130), ("bf16", 1030)])
+@pytest.mark.parametrize("count", [140_001, 200_011])
+def test_embed_grad_of_many_ids(kind, d, count):
+    """More than 4,096 chunks of sorted ids: short runs over chunks are joined by a few lanes, long ones by a workgroup."""
+    n = 1030 if count < 150_000 else 1470
+    g = gen(count + d)
+    ids = runs_ids(count, n, g)
+    grad = normal((count, d), g, TYPES[kind])
+    want, bound = _grad_table(grad, ids, n, 0.7)
+    got = avq.embed_grad(grad, ids, n, 0.7)
+    within(got, want, bound + HALF[kind] * want.abs() + TINY[kind], "gradient")
+    held = normal((n, d), g, TYPES[kind])
+    out = strided(held, 3, 1)
+    avq.embed_grad(strided(grad, 2), ids, scale=0.7, out=out, accumulate=True)
+    want = want + held.double()
+    within(out, want, bound + U * want.abs() + HALF[kind] * want.abs() * 1.01 + TINY[kind], "accumulated gradient")
+    # The first rows' entries alone, in the same order, lie in the same chunks, fewer than 4,096 of them: the same sums in the same order.
+    order = torch.sort(ids.long(), stable=True).values
+    rows = int(order[131_000])
+    first = ids < rows
+    few = avq.embed_grad(grad[first].contiguous(), ids[first].contiguous(), n, 0.7)
+    assert torch.equal(few[:rows], got[:rows]), "the joins of few and of many chunks differ"
