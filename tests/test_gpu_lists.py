@@ -391,3 +391,56 @@ def test_either_gradient_alone():
             assert torch.equal(do, want[2])
             assert torch.equal(dq, want[0]) if queries else bool((dq == 7.0).all())
             assert torch.equal(dx, want[1]) if points else bool((dx == 7.0).all())
+
+
+# ---- subnormal elements --------------------------------------------------------------------------
+
+# deviations of the rows, of the queries and the scale; most of the rows' elements are subnormal in their type, and decide the scores
+SUBNORMAL = {"f32": (2.0 ** -128, 2.0 ** 120, 256.0), "bf16": (2.0 ** -128, 2.0 ** 120, 256.0), "f16": (2.0 ** -16, 2.0 ** 10, 64.0)}
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("n,d,nq,m", [(200, 7, 5, 60), (300, 64, 40, 33), (20_000, 101, 4100, 9), (80, 1030, 6, 40), (60, 2050, 3, 30), (30, 4100, 2, 20)])
+@pytest.mark.parametrize("swapped", [False, True])
+def test_subnormal_elements_count(kind, n, d, nq, m, swapped):
+    """Rows (or queries) of subnormal elements: products and sums keep them, as the bound of every other test has it; a flush to zero would make
+    all scores 0."""
+    g = gen(n + d + nq + m)
+    small, large, scale = SUBNORMAL[kind]
+    if swapped:
+        small, large = large, small
+    # (a power of two times normal values in 64 bits, rounded once to the type)
+    x = (torch.randn((n, d), generator=g, device="cuda", dtype=torch.float64) * small).to(TYPES[kind])
+    q = (torch.randn((nq, d), generator=g, device="cuda", dtype=torch.float64) * large).to(TYPES[kind])
+    tiny = q if swapped else x
+    least = torch.finfo(TYPES[kind]).smallest_normal
+    assert float(((tiny != 0) & (tiny.double().abs() < least)).double().mean()) > 0.5
+    ids = lists((nq, m), n, g)
+    scale = scale / math.sqrt(d)
+    s = scores(x, q, ids, scale, None)[0]
+    assert float(s[s > -INF].std()) > 0.5
+    r = avq.list_log_probs(x, q, ids, scale=scale)
+    check_probs(r, x, q, ids, scale)
+    check_probs(avq.list_log_probs(strided(x, 5, 3), strided(q, 7, 1), ids, scale=scale), x, q, ids, scale)
+    # (a scale of the gradient's own, so that it stays within the type)
+    up, scale = normal((nq, m), g), 0.5 if kind == "f16" else 2.0
+    check_grads(avq.list_log_probs_grad(x, q, ids, r.logp, up, scale=scale), x, q, ids, r.logp, up, None, scale, kind)
+
+
+@pytest.mark.parametrize("kind,d", [("f32", 100), ("bf16", 40), ("f16", 300)])
+def test_gradient_of_many_listed_entries(kind, d):
+    """More than 4,096 chunks of sorted entries, rows as frequent as words are: listed once or twice, some tens, hundreds, and thousands of times."""
+    n, nq, m = 6000, 1501, 150
+    g, x, q, _, scale = inputs(n, d, nq, m, kind, 12)
+    u = torch.rand((nq, m), generator=g, device="cuda", dtype=torch.float64)
+    ids = (torch.exp(u * math.log(n + 1.0)).long() - 1).clamp(0, n - 1).int()
+    many = torch.bincount(ids.reshape(-1).long(), minlength=n)
+    assert int(((many > 32) & (many < 150)).sum()) > 50 and int((many > 1000).sum()) > 5 and int(((many > 0) & (many < 5)).sum()) > 50
+    logp = avq.list_log_probs(x, q, ids, scale=scale).logp
+    up = normal((nq, m), g)
+    got = avq.list_log_probs_grad(x, q, ids, logp, up, scale=scale)
+    check_grads(got, x, q, ids, logp, up, None, scale, kind)
+    held = normal((n, d), g, TYPES[kind])
+    out = strided(held, 3, 1)
+    got = avq.list_log_probs_grad(x, q, ids, logp, up, scale=scale, out_points=out, accumulate=True)
+    check_grads(got, x, q, ids, logp, up, None, scale, kind, held)

@@ -429,3 +429,42 @@ def test_tokens_behind_the_last_sequence_are_zeros_however_many():
     assert int((grad != 0).sum()) == 5 and bool((grad[70_000:70_005] != 0).all())
     grad = avq.policy_loss_grad(logp, logp, torch.ones(2, device="cuda"), offsets, torch.ones(2, device="cuda"))[0]
     assert int((grad != 0).sum()) == 5 and bool((grad[70_000:70_005] != 0).all())
+
+
+# ---- more rounds of a workgroup's tokens than one ----------------------------------------------------
+
+# A workgroup of 64, 256 or 1,024 threads takes four tokens a thread at a time: sequences that take it several rounds, and parts that do
+ROUNDS = {
+    "waves": [5] * 298 + [257, 700],                                                  # 64 threads, rounds of 256
+    "fours": [150] * 532 + [1024, 1025, 5000, 2049],                                  # 256 threads, rounds of 1,024
+    "groups": [600] * 516 + [4096, 4097, 8193, 10_000],                               # 1,024 threads, rounds of 4,096
+    "parts": [50] * 198 + [100_000, 7],                                               # parts of up to 20,000 tokens
+}
+
+
+def threads_of(name, pairs):
+    """Threads of a workgroup by the lengths alone, or None for parts."""
+    tokens, many = sum(ROUNDS[name]) + 8, len(ROUNDS[name]) // (2 if pairs else 1)
+    if many < 256 and tokens > (24_576 if pairs else 8192):
+        return None
+    mean = tokens / (4 * many if pairs else many)
+    return 64 if mean <= 64 else 256 if mean <= 256 else 1024
+
+
+def test_the_rounds_are_of_every_kind():
+    assert [threads_of(name, False) for name in ROUNDS] == [64, 256, 1024, None]
+    assert [threads_of(name, True) for name in ROUNDS] == [64, 256, 1024, None]
+
+
+@pytest.mark.parametrize("name", ROUNDS)
+@pytest.mark.parametrize("with_ref,with_mask,each,average", [(True, True, True, True), (False, False, False, False), (True, False, False, True)])
+def test_policy_of_several_rounds(name, with_ref, with_mask, each, average, monkeypatch):
+    monkeypatch.setitem(LENGTHS, name, ROUNDS[name])
+    test_policy(name, with_ref, with_mask, each, average)
+
+
+@pytest.mark.parametrize("name", ROUNDS)
+@pytest.mark.parametrize("with_ref,with_mask,average,smoothing", [(True, True, False, 0.1), (False, False, True, 0.0)])
+def test_preference_of_several_rounds(name, with_ref, with_mask, average, smoothing, monkeypatch):
+    monkeypatch.setitem(LENGTHS, name, ROUNDS[name])
+    test_preference(name, with_ref, with_mask, average, smoothing)
