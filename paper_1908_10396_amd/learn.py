@@ -102,7 +102,10 @@ class Model:
 
     def distill_gradients(self, a, ids, teacher, teacher_lse=None, temperature=1.0, listed=False):
         """Mean loss of distillation from a teacher's logits of ids [words][m], the student's probabilities being those of the softmax
-        over all words, or over the list alone (`listed`)."""
+        over all words, or over the list alone (`listed`, without teacher_lse: a list has all of the student's probability, and nothing is
+        left for the teacher's other words)."""
+        if listed and teacher_lse is not None:
+            raise ValueError("teacher_lse needs the softmax over all words")
         q, made = self.forward(a)
         table, scale = made[1], self.scale / temperature
         ones = torch.full((a.numel(),), 1.0 / a.numel(), device=a.device)

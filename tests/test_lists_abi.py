@@ -154,3 +154,11 @@ def test_scratch_sizes():
     assert L.avq_policy_loss_scratch(10, -1) == avq.AVQ_EINVAL
     assert 0 < L.avq_policy_loss_scratch(1 << 28, 1) < 1 << 20
     assert 0 < L.avq_policy_loss_scratch(1 << 28, 255) < 1 << 20
+
+
+def test_a_student_of_lists_alone_takes_no_lse_of_the_teacher():
+    """Its list has all of its probability: the loss would have a term that no gradient moves."""
+    from paper_1908_10396_amd import learn
+    model = learn.Model(20, 8, device="cpu")
+    with pytest.raises(ValueError, match="teacher_lse"):
+        model.distill_gradients(i32(3), i32(3, 4), f32(3, 4), f32(3), listed=True)
