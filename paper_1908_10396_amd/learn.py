@@ -16,7 +16,7 @@ encoded and searched as any other points are, and what the search returns gets i
 --sampled m learns from the softmax over the pair's word and m drawn ones instead. --student d has a second model, of d
 dimensions, learn from what the first one's index returns (distillation, all other words as one answer more). --tune goes on with
 walks that the model takes through its own index, word by word: of two walks from a word the one with more words of
-even number is preferred, or it is such words that are rewarded.
+even number is preferred (of two that have as many, neither), or it is such words that are rewarded.
 """
 import argparse
 import json
@@ -187,9 +187,41 @@ def walks(model, idx, a, length, gen, k=16, reorder_k=256):
     return torch.stack(before, 1), torch.stack(words, 1)
 
 
+def compared(reward):
+    """Of pairs of walks [pairs][2] those of unequal rewards: the places of their walks, a pair's better one first."""
+    better = (reward[:, 1] > reward[:, 0]).long()
+    even = 2 * torch.arange(reward.shape[0], device=reward.device)
+    return torch.stack([even + better, even + 1 - better], 1)[reward[:, 0] != reward[:, 1]].view(-1)
+
+
+def tune_on(model, how, before, words, reward, first, steps=4):
+    """Steps on walks, [2 pairs][length], of which two are from one word each, with rewards [pairs][2]; first: the parameters of the reference."""
+    length = words.shape[1]
+    if how == "preference":
+        order = compared(reward)
+        if order.numel() == 0:  # (equal walks say nothing)
+            return
+        before, words = before[order], words[order]
+    before, words = before.reshape(-1).contiguous(), words.reshape(-1).contiguous()
+    offsets = torch.arange(0, words.numel() + 1, length, dtype=torch.int32, device=words.device)
+    old = model.log_probs(before, words)
+    now = [p.data for p in (model.table, model.weight, model.bias)]
+    for p, value in zip((model.table, model.weight, model.bias), first):
+        p.data = value
+    ref = model.log_probs(before, words)
+    for p, value in zip((model.table, model.weight, model.bias), now):
+        p.data = value
+    for _ in range(steps):
+        if how == "preference":
+            model.apply(*model.preference_gradients(before, words, offsets, ref=ref, beta=0.5, smoothing=0.1))
+        else:
+            advantage = (reward - reward.mean(1, keepdim=True)).view(-1).contiguous()
+            model.apply(*model.policy_gradients(before, words, old, advantage, offsets, ref=ref, clip=(0.2, 0.28), kl=0.04))
+
+
 def tune(model, corpus, how, rounds=4, count=256, length=6, M=None):
     """Rounds of walks through the model's index, and a few steps on them each. Gives the share of even words by round."""
-    shares, first = [], None
+    shares, first = [], [p.detach().clone() for p in (model.table, model.weight, model.bias)]
     for _ in range(rounds):
         idx = index_of(model, M or model.table.shape[1] // 2)
         a = corpus.pairs(count)[0].repeat_interleave(2)  # two walks from each word
@@ -197,28 +229,7 @@ def tune(model, corpus, how, rounds=4, count=256, length=6, M=None):
         idx.close()
         even = (words % 2 == 0).float()
         shares.append(float(even.mean()))
-        reward = even.mean(1).view(-1, 2)
-        if how == "preference":  # the better walk first
-            order = torch.arange(2 * count, device=a.device).view(-1, 2)
-            order = torch.where((reward[:, 1:] > reward[:, :1]), order.flip(1), order).view(-1)
-            before, words = before[order], words[order]
-        before, words = before.reshape(-1).contiguous(), words.reshape(-1).contiguous()
-        offsets = torch.arange(0, words.numel() + 1, length, dtype=torch.int32, device=a.device)
-        old = model.log_probs(before, words)
-        if first is None:
-            first = [p.detach().clone() for p in (model.table, model.weight, model.bias)]
-        now = [p.data for p in (model.table, model.weight, model.bias)]
-        for p, value in zip((model.table, model.weight, model.bias), first):
-            p.data = value
-        ref = model.log_probs(before, words)
-        for p, value in zip((model.table, model.weight, model.bias), now):
-            p.data = value
-        for _ in range(4):
-            if how == "preference":
-                model.apply(*model.preference_gradients(before, words, offsets, ref=ref, beta=0.5, smoothing=0.1))
-            else:
-                advantage = (reward - reward.mean(1, keepdim=True)).view(-1).contiguous()
-                model.apply(*model.policy_gradients(before, words, old, advantage, offsets, ref=ref, clip=(0.2, 0.28), kl=0.04))
+        tune_on(model, how, before, words, even.mean(1).view(-1, 2), first)
     return shares
 
 

@@ -141,3 +141,66 @@ def test_a_student_and_walks():
         shares = learn.tune(model, corpus, how, rounds=2, count=16, length=3)
         assert len(shares) == 2 and all(0.0 <= x <= 1.0 for x in shares)
         assert all(bool(torch.isfinite(p).all()) for p in (model.table, model.weight, model.bias))
+
+
+def tuning(seed):
+    """A model away from its reference's parameters, walks of three words and their rewards, of which some are equal."""
+    model, g, words = model_and_inputs(seed)
+    first = [p.detach().clone() for p in (model.table, model.weight, model.bias)]
+    with torch.no_grad():
+        for p in (model.table, model.weight, model.bias):
+            p.add_(0.1 * torch.randn(p.shape, generator=g, device="cuda"))
+    reward = torch.tensor([[0.0, 1.0], [2 / 3, 1 / 3], [1 / 3, 1 / 3], [1.0, 2 / 3], [0.0, 0.0], [1 / 3, 1.0]], device="cuda")
+    return model, first, words(12, 3), words(12, 3), reward
+
+
+def walks_log_probs(model, first, before, after):
+    """Leaves, log p of the walks' words in 64 bits from the model's parameters, and from the reference's: [12][3]."""
+    leaves, s = logits(model, before.view(-1))
+    at = after.view(-1, 1).long()
+    now = torch.log_softmax(s, 1).gather(1, at).view(12, 3)
+    held = [p.data for p in (model.table, model.weight, model.bias)]
+    for p, value in zip((model.table, model.weight, model.bias), first):
+        p.data = value
+    ref = torch.log_softmax(logits(model, before.view(-1))[1], 1).gather(1, at).view(12, 3).detach()
+    for p, value in zip((model.table, model.weight, model.bias), held):
+        p.data = value
+    return leaves, now, ref
+
+
+@pytest.mark.parametrize("how", ["preference", "policy"])
+def test_tuning_steps_have_the_gradient_of_their_definition(how, monkeypatch):
+    """Which walk is preferred or rewarded, that pairs of equal rewards are left out, whose log probabilities the reference's are, and
+    that the step is taken from the model's own parameters."""
+    from paper_1908_10396_amd import learn
+    model, first, before, after, reward = tuning(6)
+    held = [p.detach().clone() for p in (model.table, model.weight, model.bias)]
+    applied = []
+    monkeypatch.setattr(model, "apply", lambda *got: applied.append(got))
+    learn.tune_on(model, how, before, after, reward, first, steps=1)
+    assert all(torch.equal(p, h) for p, h in zip((model.table, model.weight, model.bias), held))
+    leaves, now, ref = walks_log_probs(model, first, before, after)
+    losses = []
+    for pair in range(6):
+        a, b = 2 * pair, 2 * pair + 1
+        if how == "preference":
+            if reward[pair, 0] == reward[pair, 1]:
+                continue
+            w, l = (a, b) if reward[pair, 0] > reward[pair, 1] else (b, a)
+            x = 0.5 * ((now[w] - ref[w]).sum() - (now[l] - ref[l]).sum())
+            losses.append(-0.9 * torch.nn.functional.logsigmoid(x) - 0.1 * torch.nn.functional.logsigmoid(-x))
+        else:
+            for walk, other in ((a, b), (b, a)):
+                A = (reward[pair, walk - a] - reward[pair, other - a]).double() / 2
+                r = torch.exp(now[walk] - now[walk].detach())
+                away = ref[walk] - now[walk]
+                losses.append((-r * A + 0.04 * (torch.expm1(away) - away)).mean())
+    assert len(applied) == 1
+    agree(applied[0], torch.stack(losses).mean(), leaves)
+
+
+def test_walks_of_equal_rewards_are_not_compared(monkeypatch):
+    from paper_1908_10396_amd import learn
+    model, first, before, after, reward = tuning(7)
+    monkeypatch.setattr(model, "apply", lambda *got: pytest.fail("a step on walks that are equal"))
+    learn.tune_on(model, "preference", before, after, torch.full_like(reward, 0.5), first)
