@@ -513,8 +513,9 @@ int avq_index_log_probs(avq_index *idx, const float *queries, int32_t nq, float 
  * (whatever the row holds).
  * A padding id has no share and logp -infinity; so has an entry whose score is -infinity. A query with nothing else
  * has lse -infinity. A row that is listed twice counts twice. With a NaN or +infinity among the scores of rows no result of that
- * query is a number (padding keeps its -infinity). log p keeps its relative accuracy where p is nearly 1. All types are
- * multiplied and summed in fp32. scale, nq, m and nq x m: as in avq_log_probs. */
+ * query is a number (padding keeps its -infinity). log p keeps its relative accuracy where p is nearly 1. Products
+ * and sums are fp32 for all types (those of 16-bit elements are exact as products); subnormal elements count. scale, nq, m and
+ * nq x m: as in avq_log_probs. */
 int avq_list_log_probs(const void *points, int32_t type, int64_t n, int32_t d, int64_t ld_points, const void *queries, int32_t nq,
                        int64_t ld_queries, float scale, const int32_t *ids, int32_t m, const float *offset, float *logp_out,
                        float *lse_out, void *hip_stream);

@@ -5,8 +5,10 @@
 //
 // Bound by memory: the listed rows are gathered, once for the scores and once more for dq; dx writes the whole table, by the sorted sums of
 // the lookup's gradient (embed.hip) with G as weights. A workgroup a query: its scores stay in LDS between the products and the softmax. 2,047 lists of
-// 200 rows of 1,024 bf16: 64 us (0.75 GB gathered, 11.8 TB/s, 208 MB of it from beyond the L2; 34 with all of it there, 127 with next to nothing); 2,048 of 127 rows of 100 fp32, with offsets: 23 for
-// the scores, 161 for the gradient, of which zeros for 1,183,514 rows alone are 69.
+// 200 rows of 1,024 bf16: 64 us (0.76 GB gathered, 425 MB of it from beyond the L2s at 6.6 TB/s: the 205 MB of different rows twice, since each of eight L2s
+// fetches those of its queries; lists of 409,400 different rows fetch 845 MB in 149 us, of 1,500 ones 31 MB in 38). 1,024 lists of 64 different rows of 1,024 fp32, 2,048 bf16,
+// 4,096 bf16 and 4,096 fp32: 44, 46, 131 and 186 us, 6.1, 5.8, 4.1 and 5.8 TB/s. 2,048 of 127 rows of 100 fp32, with offsets: 23 for the scores, 161 for the gradient, of
+// which zeros for 1,183,514 rows alone are 69.
 #include <math.h>
 
 #include "fill_rows.h"
@@ -127,7 +129,7 @@ template <int THREADS> __device__ __forceinline__ void list_ids(const int32_t *_
     }
 }
 
-// acc + the inner product of two units. 16-bit elements two at a time, their products exact and two roundings at most a pair; subnormals are kept.
+// acc + the inner product of two units. 16-bit elements two at a time, their products exact and two roundings at most a pair; subnormal elements count.
 __device__ __forceinline__ float unit_product(const Unit<float> &a, const Unit<float> &b, float acc)
 {
 #pragma unroll

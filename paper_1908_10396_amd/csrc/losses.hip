@@ -321,7 +321,8 @@ inline int sequence_threads(int64_t tokens, int64_t sequences) { return tokens <
 
 // Few sequences of many tokens: each is taken in parts, 1,024 tokens or a thousand workgroups in all, whose sums a second launch joins. A call
 // takes 19 to 21 us that way, up to 1,048,576 tokens of one sequence; by one workgroup a sequence, policy takes 28 for 16,384 tokens and 1,740 for
-// 1,048,576, preferences 15, 61 (131,072) and 627. `least`: the tokens from which on that is worth the launch.
+// 1,048,576, preferences 15, 61 (131,072) and 627. `least`: the tokens from which on that is worth the launch. The parts are those of a sequence among equals: one of
+// 1,048,576 tokens has four beside 253 of 100 tokens and takes 908 us (preferences, 254 pairs: 173), and one workgroup beside 299 (1,792 and 335).
 constexpr int kPartThreads = 256, kPartTokens = 1024, kPartGroups = 1024, kPartSequences = 256;
 constexpr int64_t kPreferenceParts = 24576, kPolicyParts = 8192;
 inline int sequence_parts(int64_t tokens, int64_t sequences, int64_t least)
